@@ -10,7 +10,7 @@ Three kinds of work, as a program makes them:
           fp32, pc_q4_evict for rows in 4 bits)
 
 A group of 32 neighbouring dims of a row shares the power of two 2^e, e the least integer for which the group's
-largest magnitude is at most 7 * 2^e, from -120 to 126; an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times
+largest magnitude is at most 7 * 2^e, from -120 to 125; an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times
 2^e (ties to the even code).  The byte of the scale is e + 127; element 2i of a row is the low half of its byte i.
 
 Head counts, frame sizes and cache lengths are those of this repository's configurations, tests and bench.py.
@@ -165,10 +165,10 @@ def prepare(case: dict, seed: int):
 
 # ------------------------------------------------------------------------------ plain forms
 def _exponent(a):
-    """The least e with a <= 7 * 2^e, from -120 to 126."""
+    """The least e with a <= 7 * 2^e, from -120 to 125."""
     m, x = torch.frexp(a)
     e = torch.where(m <= 0.875, x - 3, x - 2)
-    return torch.where(a > 0, e, torch.full_like(e, -120)).clamp(-120, 126)
+    return torch.where(a > 0, e, torch.full_like(e, -120)).clamp(-120, 125)
 
 
 def _to_grid(v):
@@ -299,9 +299,9 @@ def _exact_grid(x):
     """The 4-bit value of every element, found by comparing distances in 64 bits."""
     g = x.double().unflatten(-1, (-1, 32))
     top = g.abs().amax(-1, keepdim=True)
-    e = torch.ceil(torch.log2(top / 7)).clamp(-120, 126)
+    e = torch.ceil(torch.log2(top / 7)).clamp(-120, 125)
     e = torch.where(top > 7 * torch.exp2(e), e + 1, e)                       # the logarithm may be off beside a border
-    e = torch.where((top <= 7 * torch.exp2(e - 1)) & (e > -120), e - 1, e).clamp(-120, 126)
+    e = torch.where((top <= 7 * torch.exp2(e - 1)) & (e > -120), e - 1, e).clamp(-120, 125)
     v = (g / torch.exp2(e)).abs()
     grid = torch.tensor(GRID, dtype=torch.float64, device=x.device)
     border = (grid[1:] + grid[:-1]) / 2
