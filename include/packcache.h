@@ -61,7 +61,7 @@ typedef struct pc_segment {
   int32_t frame; /* frame id (caller's bookkeeping; copied through) */
 } pc_segment;
 
-#define PC_VERSION 105          /* goes up with every change of an entry point's arguments, and with new ones */
+#define PC_VERSION 106          /* goes up with every change of an entry point's arguments, and with new ones */
 #define PC_MAX_SEGMENTS 120
 #define PC_MAX_SELECT_LEN 4096 /* longest FRAME segment the register-resident select handles
                                   (one work-group per segment); longer segments take a slower
@@ -363,6 +363,91 @@ int pc_frame_attn(const void* Q, const void* K, const void* V, int dtype, int Hq
                   int Nq, int Nk, int D, int64_t q_stride_h, int64_t kv_stride_h,
                   int64_t o_stride_h, float scale, void* O, float* lse, void* ws,
                   size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * The cache in 4 bits: the same rows in a quarter of the bytes (D/2 + D/32 per row of K or V; 68
+ * instead of 256 for D = 128).  32 neighbouring dims of a row are a group and share the scale 2^e,
+ * e the least integer with max|x| <= 7 * 2^e, from -120 to 125; an element is 2^e times one of 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, the nearest (between two the one with the even code).  Every
+ * value is a bf16 number.  The scale's byte is e + 127; a group that held a NaN or an infinity has
+ * the byte 255 and reads as NaN.  Element 2i of a row is the low half of its byte i.
+ * D is 64 or 128.  Queries, and rows that go in or come out, are bf16 or fp32.
+ */
+typedef struct pc_q4_cache {
+  uint8_t* k_codes;       /* dev [Hkv][cap][D/2] */
+  uint8_t* k_scales;      /* dev [Hkv][cap][D/32] */
+  uint8_t* v_codes;       /* dev, as k_codes */
+  uint8_t* v_scales;      /* dev, as k_scales */
+  int64_t code_stride_h;  /* bytes between heads of k_codes and of v_codes; pointers and stride % 16 == 0 */
+  int64_t scale_stride_h; /* bytes between heads of k_scales and of v_scales; % (D/32) == 0 */
+} pc_q4_cache;
+
+/* ---------------------------------------------------------------------------------------
+ * pc_q4_store -- rows row0 .. row0 + n - 1 of every head of a 4-bit cache, from K and V (keys rotated
+ * already: pc_rope3d).  H counts heads, or layers x heads where the layers lie at the heads' stride.
+ *   K, V     dev [H][n][D] of dtype, head strides in elements
+ *   pos_new  dev or NULL, int32 [n][3]: coordinates of the rows, written to rows row0 .. of
+ *   pos      dev int32 [Hsel][cap][3], every selection head
+ *   weights  dev or NULL, fp32 [Hsel][cap]: the rows' sums, set to 0
+ * n = 0 does nothing.  pc_q4_load reads rows back: K and V dev [H][n][D] of dtype, either may be NULL.
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_HIP.
+ */
+int pc_q4_store(const void* K, const void* V, int dtype, int H, int n, int D, int64_t k_stride_h,
+                int64_t v_stride_h, const pc_q4_cache* cache, int row0, const int32_t* pos_new,
+                int32_t* pos, int64_t pos_stride_h, float* weights, int64_t weights_stride_h,
+                int Hsel, void* stream);
+int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype, void* K, void* V,
+               int64_t k_stride_h, int64_t v_stride_h, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * pc_q4_attn -- pc_frame_attn over the first Nk rows of a 4-bit cache, for one token up to whole
+ * frames: O = softmax(Q K^T * scale) V, no mask.
+ *   Q, O     dev [Hq][Nq][D] of dtype, head strides in elements; Nq, Nk >= 1, Nk <= 2^30
+ *   lse      dev or NULL, fp32 [Hq][Nq] = ln sum_j exp(scale * q.k_j)
+ *   weights  dev or NULL, fp32 [Hsel][Nk], Hsel = Hkv or 1: every key's attention weight is added to its
+ *            sum, weights[h][j] = decay * weights[h][j] + the sum of row j's probabilities over the
+ *            Nq rows and the query heads of KV head h (Hsel = 1: all of them).  decay >= 0; 0 does
+ *            not read the old value.  The order of the sum is fixed: results are bit-reproducible.
+ *   ws       dev, pc_q4_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls
+ *            that may overlap on the GPU must not share one.
+ * fp32 queries: products and sums are those of fp32 (the cache's values are exact).
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_BUDGET (decay),
+ * PC_ERR_WORKSPACE, PC_ERR_HIP.
+ */
+size_t pc_q4_attn_workspace_bytes(int dtype, int Hq, int Hkv, int Nq, int Nk, int D, int weights);
+int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, int Hq, int Hkv, int Nq, int Nk,
+               int D, int64_t q_stride_h, int64_t o_stride_h, float scale, void* O, float* lse,
+               float* weights, int64_t weights_stride_h, int Hsel, float decay, void* ws,
+               size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * pc_evict, pc_q4_evict -- of a cache's first Nk rows keep n_keep, those of largest accumulated weight,
+ * in rows 0 .. n_keep - 1, in place.  For every selection head on its own, in this order:
+ *   rows below n_anchor, and rows whose t = pos[row][0] is above t of row Nk - 1 minus recent_t
+ *   (recent_t = 0: none; pos may then be NULL); then larger weights first, NaN last; equal ones: the
+ *   lower row first.
+ * A kept row below n_keep stays where it is.  The kept rows from n_keep on fill the rows that were
+ * evicted below n_keep, both in ascending order: attention does not ask for an order of its keys,
+ * and only these rows move (K, V, pos and weights, bit for bit).  Rows from n_keep on are left as they
+ * were.  Order in time has to be read from pos, not from the row.
+ *   K, V     dev [H][cap][D] of dtype, head strides in elements, 16-byte aligned; D % 8 == 0, D <= 1024
+ *   pos      dev or NULL, int32 [Hsel][cap][3]; weights dev fp32 [Hsel][cap]; strides in elements.
+ *            Head h belongs to selection head h / (H / Hsel): Hsel = H, one per KV head; H / Hsel > 1,
+ *            heads that share a selection (of each of several layers).
+ *   idx_out  dev or NULL, int32 [Hsel][n_keep]: the row that each of rows 0 .. n_keep - 1 holds now
+ * n_keep >= Nk evicts nothing (idx_out must then be NULL).
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_BUDGET, PC_ERR_WORKSPACE,
+ * PC_ERR_HIP.
+ */
+size_t pc_evict_workspace_bytes(int Hsel, int Nk, int n_keep);
+int pc_evict(void* K, void* V, int dtype, int H, int D, int64_t k_stride_h, int64_t v_stride_h,
+             int32_t* pos, int64_t pos_stride_h, float* weights, int64_t weights_stride_h, int Hsel,
+             int Nk, int n_keep, int n_anchor, int recent_t, int32_t* idx_out, int64_t idx_stride_h,
+             void* ws, size_t ws_bytes, void* stream);
+int pc_q4_evict(const pc_q4_cache* cache, int H, int D, int32_t* pos, int64_t pos_stride_h,
+                float* weights, int64_t weights_stride_h, int Hsel, int Nk, int n_keep, int n_anchor,
+                int recent_t, int32_t* idx_out, int64_t idx_stride_h, void* ws, size_t ws_bytes,
+                void* stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,8 @@ __all__ = [
     "pc_score", "pc_score_workspace_bytes", "pc_compact_plan", "pc_compact", "pc_compact_batch", "pc_compact_batch_workspace_bytes", "PC_COMPACT_SELECT", "PC_COMPACT_GATHER", "PC_SCALE_FOLDED", "folded_q_scale", "pc_masked_budgets", "pc_mask_scores", "pc_compact_status",
     "pc_compact_workspace_bytes", "pc_compact_prepared", "pc_compact_static", "pc_compact_static_capacity", "pc_frame_attn", "pc_frame_attn_workspace_bytes",
     "pc_frame_attn_workspace_bytes_for", "pc_frame_attn_cut", "pc_score_cut", "pc_compact_cut",
-    "segment_budgets",
+    "segment_budgets", "q4_cache", "pc_q4_store", "pc_q4_load", "pc_q4_attn", "pc_q4_attn_workspace_bytes", "pc_evict",
+    "pc_q4_evict", "pc_evict_workspace_bytes",
 ]
 
 PC_F32, PC_BF16 = 0, 1
@@ -52,6 +53,11 @@ class PackCacheError(RuntimeError):
 
 class pc_segment(C.Structure):
     _fields_ = [("start", C.c_int32), ("len", C.c_int32), ("kind", C.c_int32), ("frame", C.c_int32)]
+
+
+class _Q4(C.Structure):    # pc_q4_cache
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("code_stride_h", C.c_int64), ("scale_stride_h", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -109,6 +115,19 @@ def lib() -> C.CDLL:
         L.pc_compact_cut.argtypes = [C.c_int] * 4 + [segp, C.c_int, i32p, C.c_int, C.c_int, i32p]
         L.pc_frame_attn.argtypes = [vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, i64,
                                     i64, i64, C.c_float, vp, vp, vp, sz, vp]
+        q4p = C.POINTER(_Q4)
+        L.pc_q4_store.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, i64, i64, q4p, C.c_int, vp, vp, i64, vp, i64,
+                                  C.c_int, vp]
+        L.pc_q4_load.argtypes = [q4p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, i64, i64, vp]
+        L.pc_q4_attn_workspace_bytes.restype = sz
+        L.pc_q4_attn_workspace_bytes.argtypes = [C.c_int] * 7
+        L.pc_q4_attn.argtypes = [vp, q4p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, i64, i64, C.c_float, vp, vp,
+                                 vp, i64, C.c_int, C.c_float, vp, sz, vp]
+        L.pc_evict_workspace_bytes.restype = sz
+        L.pc_evict_workspace_bytes.argtypes = [C.c_int] * 3
+        evict_tail = [vp, i64, vp, i64] + [C.c_int] * 5 + [vp, i64, vp, sz, vp]
+        L.pc_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, i64, i64] + evict_tail
+        L.pc_q4_evict.argtypes = [q4p, C.c_int, C.c_int] + evict_tail
         L.pc_last_error_detail()    # touches the library's thread-local storage (see build.build_marshal)
         _LIB = L
     if _NATIVE is None and "torch" in sys.modules:
@@ -568,3 +587,196 @@ def pc_frame_attn(Q, K, V, Nk: int, scale: float, O=None, lse=None, ws=None):
                                Q.stride(0), K.stride(0), O.stride(0), float(scale), O.data_ptr(), _ptr(lse),
                                _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
     return O
+
+
+# ---- the cache in 4 bits, and eviction by accumulated weight ---------------------------------------------
+def q4_cache(Hkv: int, cap: int, D: int, device="cuda:0"):
+    """An empty 4-bit cache of cap rows per head: (k_codes, k_scales, v_codes, v_scales), uint8 [Hkv][cap][D/2] and
+    [Hkv][cap][D/32].  Any four tensors of these shapes are one (views of some heads or layers too)."""
+    import torch
+    if D not in (64, 128):
+        raise PackCacheError(-4, f"a 4-bit cache needs D = 64 or 128, got {D}")
+    return tuple(torch.zeros((Hkv, cap, w), dtype=torch.uint8, device=device) for w in (D // 2, D // 32) * 2)
+
+
+def _on_device(**tensors) -> None:
+    """Calls go to the current device's stream: everything has to be there."""
+    import torch
+    for name, t in tensors.items():
+        if t is not None and not (t.is_cuda and t.get_device() == torch.cuda.current_device()):
+            raise PackCacheError(-2, f"{name} is on {t.device}, not on the current GPU")
+
+
+def _q4_struct(cache):
+    """(struct, H, cap, D) of a 4-bit cache."""
+    import torch
+    try:
+        kc, ks, vc, vs = cache
+    except (TypeError, ValueError):
+        raise PackCacheError(-2, "a 4-bit cache is (k_codes, k_scales, v_codes, v_scales)") from None
+    for t, name in ((kc, "k_codes"), (ks, "k_scales"), (vc, "v_codes"), (vs, "v_scales")):
+        if t.dtype != torch.uint8 or t.dim() != 3:
+            raise PackCacheError(-2, f"{name}: uint8 [Hkv][cap][..], got {t.dtype} {tuple(t.shape)}")
+        _rows_dense(t, name)
+    if (vc.shape != kc.shape or vs.shape != ks.shape or ks.shape[:2] != kc.shape[:2] or kc.shape[2] != 16 * ks.shape[2]
+            or vc.stride(0) != kc.stride(0) or vs.stride(0) != ks.stride(0)):
+        raise PackCacheError(-2, "codes [Hkv][cap][D/2] and scales [Hkv][cap][D/32] of K and V must agree in shape and stride")
+    _on_device(k_codes=kc, k_scales=ks, v_codes=vc, v_scales=vs)
+    return (_Q4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), kc.stride(0), ks.stride(0)),
+            kc.shape[0], kc.shape[1], 2 * kc.shape[2])
+
+
+def _check_book(pos, weights, H: int, rows: int):
+    """Coordinates int32 [Hsel][>= rows][3] and sums fp32 [Hsel][>= rows] of one cache, either may be None; Hsel."""
+    import torch
+    hsel = None
+    if pos is not None:
+        if pos.dtype != torch.int32 or pos.dim() != 3 or pos.shape[2] != 3 or pos.shape[1] < rows:
+            raise PackCacheError(-2, f"pos: int32 [Hsel][>= {rows}][3], got {pos.dtype} {tuple(pos.shape)}")
+        _rows_dense(pos, "pos")
+        hsel = pos.shape[0]
+    if weights is not None:
+        if weights.dtype != torch.float32 or weights.dim() != 2 or weights.shape[1] < rows or (
+                weights.shape[1] > 1 and weights.stride(1) != 1):
+            raise PackCacheError(-2, f"weights: fp32 [Hsel][>= {rows}], got {weights.dtype} {tuple(weights.shape)}")
+        if hsel is not None and weights.shape[0] != hsel:
+            raise PackCacheError(-2, f"pos has {hsel} selection heads, weights {weights.shape[0]}")
+        hsel = weights.shape[0]
+    if hsel is not None and (hsel < 1 or H % hsel):
+        raise PackCacheError(-2, f"{hsel} selection heads for {H} heads")
+    _on_device(pos=pos, weights=weights)
+    return hsel
+
+
+def pc_q4_store(K, V, cache, row0: int, pos_new=None, pos=None, weights=None) -> None:
+    """Rows K, V [H][n][D] (bf16/fp32; keys rotated already) become rows row0 .. of a 4-bit cache.  pos_new (int32
+    [n][3]) goes to the same rows of pos (int32 [Hsel][cap][3]); weights (fp32 [Hsel][cap]) begin at 0 there."""
+    import torch
+    q4, H, cap, D = _q4_struct(cache)
+    if K.shape != V.shape or K.dim() != 3 or K.shape[0] != H or K.shape[2] != D or K.dtype != V.dtype:
+        raise PackCacheError(-2, f"K and V must be [{H}][n][{D}] of one type, got {tuple(K.shape)} and {tuple(V.shape)}")
+    n = K.shape[1]
+    _rows_dense(K, "K")
+    _rows_dense(V, "V")
+    if row0 < 0 or row0 + n > cap:
+        raise PackCacheError(-2, f"rows {row0} .. {row0 + n} of a cache of {cap}")
+    if (pos is None) != (pos_new is None):
+        raise PackCacheError(-1, "pos and pos_new go together")
+    if pos_new is not None and (pos_new.dtype != torch.int32 or tuple(pos_new.shape) != (n, 3) or not pos_new.is_contiguous()):
+        raise PackCacheError(-2, f"pos_new: contiguous int32 [{n}][3], got {pos_new.dtype} {tuple(pos_new.shape)}")
+    hsel = _check_book(pos, weights, H, row0 + n)
+    _on_device(K=K, V=V, pos_new=pos_new)
+    _check(lib().pc_q4_store(K.data_ptr(), V.data_ptr(), _dtype_code(K), H, n, D, K.stride(0), V.stride(0), C.byref(q4), int(row0),
+                             _ptr(pos_new), _ptr(pos), 0 if pos is None else pos.stride(0), _ptr(weights),
+                             0 if weights is None else weights.stride(0), hsel or 0, _stream()))
+
+
+def pc_q4_load(cache, row0: int, K=None, V=None):
+    """Rows row0 .. of a 4-bit cache as values into K and / or V [H][n][D] (bf16/fp32); returns (K, V)."""
+    q4, H, cap, D = _q4_struct(cache)
+    some = K if K is not None else V
+    if some is None:
+        raise PackCacheError(-1, "K and V are None")
+    n = some.shape[1] if some.dim() == 3 else -1
+    for t, name in ((K, "K"), (V, "V")):
+        if t is not None:
+            if tuple(t.shape) != (H, n, D) or t.dtype != some.dtype:
+                raise PackCacheError(-2, f"{name} must be [{H}][n][{D}], both of one type, got {tuple(t.shape)}")
+            _rows_dense(t, name)
+    if row0 < 0 or row0 + n > cap:
+        raise PackCacheError(-2, f"rows {row0} .. {row0 + n} of a cache of {cap}")
+    _on_device(K=K, V=V)
+    _check(lib().pc_q4_load(C.byref(q4), H, int(row0), n, D, _dtype_code(some), _ptr(K), _ptr(V), 0 if K is None else K.stride(0),
+                            0 if V is None else V.stride(0), _stream()))
+    return K, V
+
+
+def pc_q4_attn_workspace_bytes(dtype: int, Hq: int, Hkv: int, Nq: int, Nk: int, D: int, weights: bool = False) -> int:
+    return lib().pc_q4_attn_workspace_bytes(dtype, Hq, Hkv, Nq, Nk, D, int(weights))
+
+
+def pc_q4_attn(Q, cache, Nk: int, scale: float, O=None, lse=None, weights=None, decay: float = 1.0, ws=None):
+    """Q [Hq][Nq][D] (bf16/fp32) over the first Nk rows of a 4-bit cache -> O [Hq][Nq][D].  weights (fp32 [Hkv or 1][>= Nk]):
+    decay * weights + the attention weight of every key, summed over rows and heads.  ws: not to be shared by calls
+    that may overlap; None: one of the call's own, from torch's allocator."""
+    import torch
+    q4, Hkv, cap, D = _q4_struct(cache)
+    if Q.dim() != 3 or Q.shape[2] != D or Q.shape[0] % Hkv:
+        raise PackCacheError(-2, f"Q must be [a multiple of {Hkv}][Nq][{D}], got {tuple(Q.shape)}")
+    Hq, Nq, _ = Q.shape
+    _rows_dense(Q, "Q")
+    if O is None:
+        O = torch.empty((Hq, Nq, D), dtype=Q.dtype, device=Q.device)
+    if tuple(O.shape) != (Hq, Nq, D) or O.dtype != Q.dtype:
+        raise PackCacheError(-2, f"O must be [{Hq}][{Nq}][{D}] of Q's type, got {O.dtype} {tuple(O.shape)}")
+    _rows_dense(O, "O")
+    if not 1 <= Nk <= cap:
+        raise PackCacheError(-2, f"Nk = {Nk} of a cache of {cap} rows")
+    if lse is not None and (tuple(lse.shape) != (Hq, Nq) or not lse.is_contiguous() or lse.dtype != torch.float32):
+        raise PackCacheError(-2, f"lse must be a contiguous fp32 [{Hq}][{Nq}] tensor")
+    hsel = _check_book(None, weights, Hkv, Nk)
+    dtype = _dtype_code(Q)
+    if ws is None:
+        nws = _q4_attn_workspace_bytes(dtype, Hq, Hkv, Nq, Nk, D, weights is not None)
+        if nws:
+            ws = _workspace(nws, Q)
+    _on_device(Q=Q, O=O, lse=lse, ws=ws)
+    _check(lib().pc_q4_attn(Q.data_ptr(), C.byref(q4), dtype, Hq, Hkv, Nq, int(Nk), D, Q.stride(0), O.stride(0), float(scale),
+                            O.data_ptr(), _ptr(lse), _ptr(weights), 0 if weights is None else weights.stride(0), hsel or 0,
+                            float(decay), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return O
+
+
+@lru_cache(maxsize=1024)
+def _q4_attn_workspace_bytes(*sizes: int) -> int:
+    return pc_q4_attn_workspace_bytes(*sizes)
+
+
+def pc_evict_workspace_bytes(Hsel: int, Nk: int, n_keep: int) -> int:
+    return lib().pc_evict_workspace_bytes(Hsel, Nk, n_keep)
+
+
+def _evict_book(pos, weights, H, cap, Nk, n_keep, idx, ws, like):
+    """What both evictions check and pass on: (Hsel, idx stride, ws)."""
+    import torch
+    if weights is None:
+        raise PackCacheError(-1, "weights is None")
+    if not 0 <= Nk <= cap:
+        raise PackCacheError(-2, f"Nk = {Nk} of a cache of {cap} rows")
+    hsel = _check_book(pos, weights, H, Nk)
+    if idx is not None and (idx.dtype != torch.int32 or idx.dim() != 2 or idx.shape[0] != hsel or idx.shape[1] < n_keep or
+                            (idx.shape[1] > 1 and idx.stride(1) != 1)):
+        raise PackCacheError(-2, f"idx: int32 [{hsel}][>= {n_keep}], got {idx.dtype} {tuple(idx.shape)}")
+    if ws is None:
+        nws = pc_evict_workspace_bytes(hsel, Nk, n_keep)
+        if nws:
+            ws = _workspace(nws, like)
+    _on_device(idx=idx, ws=ws)
+    return hsel, 0 if idx is None else idx.stride(0), ws
+
+
+def pc_evict(K, V, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent_t: int = 0, idx=None, ws=None) -> int:
+    """Of the first Nk rows of K, V [H][cap][D] keep n_keep: rows below n_anchor, rows whose t is within recent_t of row
+    Nk - 1's, then those of largest weight (fp32 [Hsel][cap]; pos int32 [Hsel][cap][3] or None).  In place; rows that
+    stay below n_keep do not move.  idx (int32 [Hsel][n_keep]): where each row came from.  Returns the rows left."""
+    if K.shape != V.shape or K.dim() != 3 or K.dtype != V.dtype:
+        raise PackCacheError(-2, f"K and V must be [H][cap][D] of one type, got {tuple(K.shape)} and {tuple(V.shape)}")
+    H, cap, D = K.shape
+    _rows_dense(K, "K")
+    _rows_dense(V, "V")
+    hsel, idx_stride, ws = _evict_book(pos, weights, H, cap, Nk, n_keep, idx, ws, K)
+    _on_device(K=K, V=V)
+    _check(lib().pc_evict(K.data_ptr(), V.data_ptr(), _dtype_code(K), H, D, K.stride(0), V.stride(0), _ptr(pos),
+                          0 if pos is None else pos.stride(0), weights.data_ptr(), weights.stride(0), hsel, int(Nk), int(n_keep),
+                          int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return min(Nk, n_keep)
+
+
+def pc_q4_evict(cache, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent_t: int = 0, idx=None, ws=None) -> int:
+    """pc_evict on a 4-bit cache."""
+    q4, H, cap, D = _q4_struct(cache)
+    hsel, idx_stride, ws = _evict_book(pos, weights, H, cap, Nk, n_keep, idx, ws, cache[0])
+    _check(lib().pc_q4_evict(C.byref(q4), H, D, _ptr(pos), 0 if pos is None else pos.stride(0), weights.data_ptr(),
+                             weights.stride(0), hsel, int(Nk), int(n_keep), int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws),
+                             0 if ws is None else ws.numel(), _stream()))
+    return min(Nk, n_keep)

@@ -1,0 +1,700 @@
+// The KV cache held in 4 bits: rows into it and out of it, and attention over it.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "q4.h"
+
+namespace pc {
+namespace {
+
+constexpr float kNoRef = -3.0e38f;     // the reference of a row that has seen no score yet
+
+// ------------------------------------------------------------------------------------------
+// pc_q4_store, pc_q4_load.  Bound: bytes.  A lane owns eight elements, so four lanes are a group and agree on its
+// largest magnitude by two lane exchanges; rows of K and V of all heads are one run of rows, so that one token of
+// many heads fills a launch.
+// ------------------------------------------------------------------------------------------
+constexpr int kCopyThreads = 256;
+
+struct RowsAt {          // rows 0 .. n - 1 of H heads of two tensors
+  int H, D;
+  Divisor by_n;
+  int64_t k_stride_h, v_stride_h;
+};
+
+// the rows' bookkeeping that pc_q4_store writes as well (either pointer may be NULL)
+struct Book {
+  const int32_t* pos_new;
+  int32_t* pos;
+  float* weights;
+  int64_t pos_stride_h, w_stride_h;
+  int Hsel;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kCopyThreads) void q4_store_kernel(const T* __restrict__ K, const T* __restrict__ V, RowsAt at,
+                                                                Q4Rows cache, int row0, int n_units, Book book) {
+  constexpr int kLanes = D / 8;      // lanes of a row
+  const int n = at.by_n.d;
+  const int idx = blockIdx.x * kCopyThreads + threadIdx.x;
+  const int unit = idx / kLanes, part = idx % kLanes;
+  if (unit < n_units) {
+    int rest = at.by_n.of(unit);
+    const int i = unit - rest * n;
+    const bool value = rest >= at.H;
+    const int h = value ? rest - at.H : rest;
+    const T* src = (value ? V + h * at.v_stride_h : K + h * at.k_stride_h) + static_cast<int64_t>(i) * D + part * 8;
+    uint32_t top = 0, codes = 0;
+    float scale;
+    int byte;
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(src);
+      for (int k = 0; k < 4; ++k) top = max(top, max(x[k] << 16 & 0x7fffffffu, x[k] & 0x7fff0000u));
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+      byte = q4_scale_byte(top);
+      scale = q4_scale(byte);
+      // (a vector's element is copied before its bits are taken as another type: the compiler takes element 0 of it otherwise)
+      const uint32_t w0 = x[0], w1 = x[1], w2 = x[2], w3 = x[3];
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, w0), scale, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, w1), scale, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, w2), scale, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, w3), scale, 3);
+    } else {
+      const f32x4 x = load_f32x4(reinterpret_cast<const float*>(src)), y = load_f32x4(reinterpret_cast<const float*>(src) + 4);
+      for (int k = 0; k < 4; ++k)
+        top = max(top, max(__float_as_uint(x[k]) & 0x7fffffffu, __float_as_uint(y[k]) & 0x7fffffffu));
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+      byte = q4_scale_byte(top);
+      scale = q4_scale(byte);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], scale, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], scale, 3);
+    }
+    if (byte == kQ4BadScale) codes = 0;
+    const int64_t row = static_cast<int64_t>(row0) + i;
+    uint8_t* out = const_cast<uint8_t*>(value ? cache.v_codes : cache.k_codes) + h * cache.code_stride_h + row * (D / 2);
+    uint8_t* out_s = const_cast<uint8_t*>(value ? cache.v_scales : cache.k_scales) + h * cache.scale_stride_h + row * (D / 32);
+    reinterpret_cast<uint32_t*>(out)[part] = codes;
+    if (part % 4 == 0) out_s[part / 4] = static_cast<uint8_t>(byte);
+  }
+  // the rows' coordinates and their sums, which begin at zero
+  if (book.pos == nullptr && book.weights == nullptr) return;
+  for (int64_t t = idx; t < static_cast<int64_t>(book.Hsel) * n; t += static_cast<int64_t>(gridDim.x) * kCopyThreads) {
+    const int h = at.by_n.of(static_cast<int>(t));
+    const int i = static_cast<int>(t) - h * n;
+    const int64_t row = static_cast<int64_t>(row0) + i;
+    if (book.pos != nullptr)
+      for (int k = 0; k < 3; ++k) book.pos[h * book.pos_stride_h + row * 3 + k] = book.pos_new[i * 3 + k];
+    if (book.weights != nullptr) book.weights[h * book.w_stride_h + row] = 0.f;
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K, T* __restrict__ V, RowsAt at, Q4Rows cache,
+                                                               int row0, int first_unit, int n_units) {
+  constexpr int kLanes = D / 8;
+  const int n = at.by_n.d;
+  const int idx = blockIdx.x * kCopyThreads + threadIdx.x;
+  int unit = idx / kLanes;
+  const int part = idx % kLanes;
+  if (unit >= n_units) return;
+  unit += first_unit;
+  const int rest = at.by_n.of(unit);
+  const int i = unit - rest * n;
+  const bool value = rest >= at.H;
+  const int h = value ? rest - at.H : rest;
+  const int64_t row = static_cast<int64_t>(row0) + i;
+  const uint8_t* codes = (value ? cache.v_codes : cache.k_codes) + h * cache.code_stride_h + row * (D / 2);
+  const uint8_t* scales = (value ? cache.v_scales : cache.k_scales) + h * cache.scale_stride_h + row * (D / 32);
+  const bf16x8 x = q4_to_bf16(reinterpret_cast<const uint32_t*>(codes)[part], q4_scale(scales[part / 4]));
+  T* dst = (value ? V + h * at.v_stride_h : K + h * at.k_stride_h) + static_cast<int64_t>(i) * D + part * 8;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<bf16x8*>(dst) = x;
+  } else {
+    f32x4 lo, hi;
+    for (int k = 0; k < 4; ++k) lo[k] = static_cast<float>(x[k]), hi[k] = static_cast<float>(x[4 + k]);
+    store_f32x4(reinterpret_cast<float*>(dst), lo);
+    store_f32x4(reinterpret_cast<float*>(dst) + 4, hi);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Attention straight from the codes, for few query rows: 16 kRT rows per work-group, its eight waves deal the keys in
+// steps of 32.
+//   * S^T = K Q^T by 16x16x32 products.  Which dims a product contracts is free as long as both operands agree: lane
+//     (r = l % 16, g = l / 16) takes dims g D/4 .. of key row r, which lie in one scale group and are one load,
+//     and its dwords of eight codes are the operands of the D/32 products after four conversions each.  K never
+//     touches LDS.
+//   * The result leaves lane (q, g) with keys 4 g .. 4 g + 3 of query q, of two tiles of 16: the eight k-slots of
+//     O^T += V^T P^T.  V is converted by the lane that loads it (one scale for its 32 dims) and goes
+//     through LDS of the wave's own as bf16 rows, read back by transposing loads.
+//   * Softmax in base 2 against a reference that lags the maximum by at most 2^8; sums in fp32.
+//   * fp32 queries and probabilities are three bf16 parts each: keys and values are exact in bf16, so the
+//     products are exact and the sums are the fp32 ones.
+// ------------------------------------------------------------------------------------------
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kStep = 32;                   // keys of a wave's step
+
+struct AttnArgs {
+  Q4Rows cache;
+  int rep, Nk;
+  Divisor by_nq, by_tiles;                  // rows per head, row tiles per KV head
+  int n_tiles, share_steps;                 // row tiles of all KV heads, steps of a key share
+  int64_t q_stride_h, o_stride_h;
+  float c;                                  // scale * log2(e)
+  float* part_o;                            // NULL: one share
+  float2* part_ml;
+  float* lse;                               // natural logarithm, or NULL
+  float* lse2;                              // base 2, for the weights, or NULL
+  int64_t rows_all;
+};
+
+template <int D>
+__device__ __forceinline__ int v_place(int key, int chunk) {      // a 32-byte chunk of a key's row in LDS
+  return chunk ^ (D == 128 ? key & 7 : (key >> 1) & 3);
+}
+
+template <typename T, int D>
+struct QueryFrags {
+  static constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kSteps = D / 32;
+  bf16x8 f[kSteps][kParts];
+  // the row's dims g D/4 + 8 b .. + 7
+  __device__ __forceinline__ void load(const T* row, int g) {
+#pragma unroll
+    for (int b = 0; b < kSteps; ++b) {
+      const T* src = row + g * (D / 4) + b * 8;
+      if constexpr (kParts == 1) {
+        f[b][0] = *reinterpret_cast<const bf16x8*>(src);
+      } else {
+        const f32x4 x = load_f32x4(src), y = load_f32x4(src + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          __bf16 hi, mid, lo;
+          split3(e < 4 ? x[e] : y[e - 4], hi, mid, lo);
+          f[b][0][e] = hi, f[b][1][e] = mid, f[b][2][e] = lo;
+        }
+      }
+    }
+  }
+};
+
+// A lane's piece of a key row: D/8 bytes of codes, as D/32 dwords.
+template <int D>
+struct KeyCodes {
+  uint32_t w[D / 32];
+  int byte;
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t row, int g) {
+    const uint8_t* src = codes + row * (D / 2) + g * (D / 8);
+    if constexpr (D == 128) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(src);
+      w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+      byte = scales[row * 4 + g];
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(src);
+      w[0] = x[0], w[1] = x[1];
+      byte = scales[row * 2 + g / 2];
+    }
+  }
+};
+
+// 16 keys by 16 queries: key rows of the lanes' pieces times the queries' fragments.  Small parts first.
+template <typename T, int D>
+__device__ __forceinline__ f32x4 scores(const bf16x8 (&k)[D / 32], const QueryFrags<T, D>& q) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b], q.f[b][p], s, 0, 0, 0);
+  return s;
+}
+
+template <typename T, int D, int kRT>
+__global__ __launch_bounds__(kThreads, 1) void q4_attn_kernel(const T* __restrict__ Q, T* __restrict__ O, AttnArgs a) {
+  using lds_byte = __attribute__((address_space(3))) uint8_t;
+  constexpr int kParts = QueryFrags<T, D>::kParts;
+  constexpr int kTileBytes = kStep * D * 2;                 // a wave's V rows; its partial output as well
+  constexpr int kGroups = D / 32, kVRows = 64 / kGroups, kVLoads = kStep / kVRows;
+  static_assert(16 * D * 4 == kTileBytes, "partial outputs take the place of the V rows");
+  __shared__ __align__(16) uint8_t smem[kWaves * kTileBytes + kWaves * 16 * 8];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  int unit = xcd_contiguous_index(blockIdx.x, gridDim.x);
+  const int split = unit / a.n_tiles;
+  unit -= split * a.n_tiles;
+  const int kvh = a.by_tiles.of(unit), tile = unit - kvh * a.by_tiles.d;
+  const int n_rows = a.rep * a.by_nq.d;
+  const uint8_t* kc = a.cache.k_codes + kvh * a.cache.code_stride_h;
+  const uint8_t* ks = a.cache.k_scales + kvh * a.cache.scale_stride_h;
+  const uint8_t* vc = a.cache.v_codes + kvh * a.cache.code_stride_h;
+  const uint8_t* vs = a.cache.v_scales + kvh * a.cache.scale_stride_h;
+  const int n_steps = (a.Nk + kStep - 1) / kStep;
+  const int step_end = min((split + 1) * a.share_steps, n_steps);
+
+  KeyCodes<D> raw_k[2];
+  u32x4 raw_v[kVLoads];
+  int raw_s[kVLoads];
+  auto fetch = [&](int step) {
+    const int64_t k0 = static_cast<int64_t>(step) * kStep;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) raw_k[t].load(kc, ks, min(k0 + t * 16 + r, static_cast<int64_t>(a.Nk) - 1), g);
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i) {
+      const int64_t row = min(k0 + i * kVRows + lane / kGroups, static_cast<int64_t>(a.Nk) - 1);
+      raw_v[i] = *reinterpret_cast<const u32x4*>(vc + row * (D / 2) + lane % kGroups * 16);
+      raw_s[i] = vs[row * kGroups + lane % kGroups];
+    }
+  };
+  int step = split * a.share_steps + wave;
+  if (step < step_end) fetch(step);
+
+  QueryFrags<T, D> q[kRT];
+#pragma unroll
+  for (int rt = 0; rt < kRT; ++rt) {
+    const int rho = min((tile * kRT + rt) * 16 + r, n_rows - 1);
+    const int head = a.by_nq.of(rho);
+    q[rt].load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
+  }
+  f32x4 o[kRT][D / 16];
+  float m[kRT], l[kRT];
+#pragma unroll
+  for (int rt = 0; rt < kRT; ++rt) {
+    m[rt] = kNoRef, l[rt] = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) o[rt][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  lds_byte* mine = (lds_byte*)smem + wave * kTileBytes;
+  // where a transposing load of 16 dims finds the four dims 4 (r % 4) of key 4 g + r / 4
+  const int v_key = g * 4 + (r >> 2);
+  lds_byte* v_at = mine + v_key * (D * 2) + (r & 3) * 8;
+
+  for (; step < step_end; step += kWaves) {
+    const int k0 = step * kStep;
+    bf16x8 kf[2][D / 32];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) kf[t][b] = q4_to_bf16(raw_k[t].w[b], q4_scale(raw_k[t].byte));
+    wave_lds_sync();       // the step before has read its values
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i) {
+      const int key = i * kVRows + lane / kGroups, grp = lane % kGroups;
+      const float scale = q4_scale(raw_s[i]);
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>(
+            mine + key * (D * 2) + v_place<D>(key, grp * 2 + b / 2) * 32 + (b & 1) * 16) = q4_to_bf16(raw_v[i][b], scale);
+    }
+    wave_lds_sync();
+    if (step + kWaves < step_end) fetch(step + kWaves);
+    bf16x8 pf[kRT][kParts];
+#pragma unroll
+    for (int rt = 0; rt < kRT; ++rt) {
+      f32x4 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] = scores<T, D>(kf[t], q[rt]);
+      if (k0 + kStep > a.Nk) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (k0 + t * 16 + g * 4 + i >= a.Nk) s[t][i] = -INFINITY;
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
+      mx *= a.c;
+      if (__any(!(mx <= m[rt] + 8.f))) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m[rt], mx), alpha = __builtin_amdgcn_exp2f(m[rt] - m_new);
+        l[rt] *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) o[rt][db] *= alpha;
+        m[rt] = m_new;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], a.c, -m[rt]));
+        l[rt] += p;
+        if constexpr (kParts == 1) {
+          pf[rt][0][i] = static_cast<__bf16>(p);
+        } else {
+          __bf16 hi, mid, lo;
+          split3(p, hi, mid, lo);
+          pf[rt][0][i] = hi, pf[rt][1][i] = mid, pf[rt][2][i] = lo;
+        }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      lds_byte* src = v_at + v_place<D>(v_key, db) * 32;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(src));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+          reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(src + 16 * D * 2));
+      const bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+      for (int rt = 0; rt < kRT; ++rt)
+#pragma unroll
+        for (int p = kParts - 1; p >= 0; --p) o[rt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt][p], o[rt][db], 0, 0, 0);
+    }
+  }
+
+  // the waves' parts, 16 rows at a time: 16-byte unit u of row q lies at u ^ q
+  constexpr int kUnits = D / 4;
+  auto* s_ml = reinterpret_cast<__attribute__((address_space(3))) float*>((lds_byte*)smem + kWaves * kTileBytes);
+#pragma unroll
+  for (int rt = 0; rt < kRT; ++rt) {
+    float sum = l[rt];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    __syncthreads();
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+      *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(mine + r * (D * 4) + ((db * 4 + g) ^ r) * 16) = o[rt][db];
+    if (lane < 16) {
+      s_ml[(wave * 16 + lane) * 2] = m[rt];
+      s_ml[(wave * 16 + lane) * 2 + 1] = sum;
+    }
+    __syncthreads();
+    const int row = threadIdx.x / kUnits, u = threadIdx.x % kUnits;
+    const int rho = (tile * kRT + rt) * 16 + row;
+    if (row < 16 && rho < n_rows) {
+      float M = kNoRef, lt = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[(w * 16 + row) * 2]);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float wt = __builtin_amdgcn_exp2f(s_ml[(w * 16 + row) * 2] - M);
+        lt += wt * s_ml[(w * 16 + row) * 2 + 1];
+        const f32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>((lds_byte*)smem + w * kTileBytes +
+                                                                                         row * (D * 4) + (u ^ row) * 16);
+        acc += wt * v;
+      }
+      const int64_t at = static_cast<int64_t>(kvh) * n_rows + rho;
+      if (a.part_o != nullptr) {
+        const int64_t at_s = split * a.rows_all + at;
+        *reinterpret_cast<f32x4*>(a.part_o + at_s * D + u * 4) = acc;
+        if (u == 0) a.part_ml[at_s] = make_float2(M, lt);
+      } else {
+        const float inv = 1.f / lt;
+        const int head = a.by_nq.of(rho);
+        T* to = O + (kvh * a.rep + head) * a.o_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D + u * 4;
+        if constexpr (kParts == 1) {
+          *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+        } else {
+          store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+        }
+        if (u == 0) {
+          const float e2 = M + log2f(lt);
+          if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
+          if (a.lse2 != nullptr) a.lse2[at] = e2;
+        }
+      }
+    }
+  }
+}
+
+// The shares of a row: a work-group of 256 threads per row, the shares dealt to its 1024 / D groups of threads.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q4_merge_kernel(T* __restrict__ O, int n_splits, AttnArgs a) {
+  constexpr int kUnits = D / 4, kLanes = 256 / kUnits;
+  __shared__ f32x4 s_o[kLanes][kUnits];
+  __shared__ float s_l[kLanes];
+  const int64_t at = blockIdx.x;
+  const int u = threadIdx.x % kUnits, part = threadIdx.x / kUnits;
+  float M = kNoRef;
+  for (int s = 0; s < n_splits; ++s) M = fmaxf(M, a.part_ml[s * a.rows_all + at].x);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float lt = 0.f;
+  for (int s = part; s < n_splits; s += kLanes) {
+    const int64_t at_s = s * a.rows_all + at;
+    const float2 ml = a.part_ml[at_s];
+    const float wt = __builtin_amdgcn_exp2f(ml.x - M);
+    lt += wt * ml.y;
+    acc += wt * *reinterpret_cast<const f32x4*>(a.part_o + at_s * D + u * 4);
+  }
+  s_o[part][u] = acc;
+  if (u == 0) s_l[part] = lt;
+  __syncthreads();
+  if (part != 0) return;
+  lt = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < kLanes; ++p) acc += s_o[p][u], lt += s_l[p];
+  const float inv = 1.f / lt;
+  const int head = a.by_nq.of(static_cast<int>(at));
+  T* to = O + head * a.o_stride_h + (at - static_cast<int64_t>(head) * a.by_nq.d) * D + u * 4;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+  } else {
+    store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+  }
+  if (u == 0) {
+    const float e2 = M + log2f(lt);
+    if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
+    if (a.lse2 != nullptr) a.lse2[at] = e2;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// The weights: weights[j] = decay * weights[j] + sum over the query rows of exp2(c s - lse2), the scores formed once
+// more from the keys' codes.  A wave owns 16 keys, as the second operand (a lane sums its key's column over the
+// queries it sees), and walks the query rows; with one sum for all heads it walks the KV heads as well.  The
+// order of the sum is fixed.
+// ------------------------------------------------------------------------------------------
+struct WeighArgs {
+  Q4Rows cache;
+  int rep, Nk, Hkv, Hsel;
+  Divisor by_nq, by_blocks;                 // rows per head, key blocks of a selection head
+  int64_t q_stride_h, w_stride_h;
+  float c, decay;
+  const float* lse2;
+  float* weights;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q4_weigh_kernel(const T* __restrict__ Q, WeighArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int sel = a.by_blocks.of(blockIdx.x), block = blockIdx.x - sel * a.by_blocks.d;
+  const int k0 = (block * 4 + wave) * 16;
+  if (k0 >= a.Nk) return;
+  const int n_rows = a.rep * a.by_nq.d, per = a.Hkv / a.Hsel;
+  const int key = min(k0 + r, a.Nk - 1);
+  float sum = 0.f;
+  for (int kvh = sel * per; kvh < (sel + 1) * per; ++kvh) {
+    KeyCodes<D> raw;
+    raw.load(a.cache.k_codes + kvh * a.cache.code_stride_h, a.cache.k_scales + kvh * a.cache.scale_stride_h, key, g);
+    bf16x8 kf[D / 32];
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) kf[b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
+    for (int row0 = 0; row0 < n_rows; row0 += 16) {
+      const int rho = min(row0 + r, n_rows - 1);
+      const int head = a.by_nq.of(rho);
+      QueryFrags<T, D> q;
+      q.load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.f[b][p], kf[b], s, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = row0 + g * 4 + i;
+        const float e2 = a.lse2[static_cast<int64_t>(kvh) * n_rows + min(row, n_rows - 1)];
+        if (row < n_rows) sum += __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -e2));
+      }
+    }
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (g == 0 && k0 + r < a.Nk) {
+    float* w = a.weights + sel * a.w_stride_h + k0 + r;
+    *w = a.decay == 0.f ? sum : fmaf(a.decay, *w, sum);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------
+constexpr size_t kWsAlign = 256;
+
+struct Q4Plan {
+  int row_tiles;      // tiles of 16 queries per work-group
+  int n_splits;
+  size_t ml_at, lse_at, bytes;
+};
+
+Q4Plan plan_q4(int Hkv, int rows, int Nk, int D, bool weights) {
+  Q4Plan p = {};
+  p.row_tiles = rows <= 16 ? 1 : 2;
+  const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 16 * p.row_tiles)) * Hkv;
+  const int steps = ceil_div(Nk, kStep);
+  int64_t want = std::max<int64_t>(1, 512 / tiles);
+  want = std::min<int64_t>(want, ceil_div(steps, kWaves));
+  const int share = ceil_div(steps, static_cast<int>(std::min<int64_t>(want, 128)));
+  p.n_splits = ceil_div(steps, share);
+  const int64_t all = static_cast<int64_t>(Hkv) * rows;
+  size_t at = 0;
+  if (p.n_splits > 1) {
+    at = align_up(static_cast<size_t>(all) * p.n_splits * D * 4, kWsAlign);
+    p.ml_at = at;
+    at += align_up(static_cast<size_t>(all) * p.n_splits * 8, kWsAlign);
+  }
+  p.lse_at = at;
+  if (weights) at += align_up(static_cast<size_t>(all) * 4, kWsAlign);
+  p.bytes = at;
+  return p;
+}
+
+int check_kind(int dtype, int D, const char* who) {
+  PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  PC_REQUIRE(D == 64 || D == 128, PC_ERR_UNSUPPORTED, "%s: needs D = 64 or 128, got %d", who, D);
+  return PC_OK;
+}
+
+Q4Rows rows_of(const pc_q4_cache* c) {
+  return {c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->code_stride_h, c->scale_stride_h};
+}
+
+bool aligned16(const void* p, int64_t stride, int dtype) {
+  return dtype == PC_F32 ? reinterpret_cast<uintptr_t>(p) % 4 == 0
+                         : reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0;
+}
+
+}  // namespace
+}  // namespace pc
+
+using namespace pc;
+
+extern "C" int pc_q4_store(const void* K, const void* V, int dtype, int H, int n, int D, int64_t k_stride_h,
+                           int64_t v_stride_h, const pc_q4_cache* cache, int row0, const int32_t* pos_new, int32_t* pos,
+                           int64_t pos_stride_h, float* weights, int64_t weights_stride_h, int Hsel, void* stream) {
+  const char* who = "pc_q4_store";
+  if (int rc = check_kind(dtype, D, who)) return rc;
+  PC_REQUIRE(H > 0 && n >= 0 && row0 >= 0, PC_ERR_SHAPE, "%s: H=%d n=%d row0=%d", who, H, n, row0);
+  if (int rc = check_q4_cache(cache, D, who)) return rc;
+  if (int rc = check_q4_span(cache, H, row0, n, D, who)) return rc;
+  PC_REQUIRE((pos == nullptr) == (pos_new == nullptr), PC_ERR_NULL, "%s: pos and pos_new go together", who);
+  const bool book = pos != nullptr || weights != nullptr;
+  PC_REQUIRE(!book || (Hsel > 0 && Hsel <= H && H % Hsel == 0), PC_ERR_SHAPE, "%s: Hsel=%d for %d heads", who, Hsel, H);
+  const int64_t end = static_cast<int64_t>(row0) + n;
+  PC_REQUIRE(!book || Hsel == 1 || ((pos == nullptr || pos_stride_h >= end * 3) && (weights == nullptr || weights_stride_h >= end)),
+             PC_ERR_SHAPE, "%s: rows up to %lld do not fit the strides of pos or weights", who, static_cast<long long>(end));
+  if (n == 0) return PC_OK;
+  PC_REQUIRE(K && V, PC_ERR_NULL, "%s: K or V is NULL", who);
+  PC_REQUIRE(H == 1 || (k_stride_h >= static_cast<int64_t>(n) * D && v_stride_h >= static_cast<int64_t>(n) * D), PC_ERR_SHAPE,
+             "%s: a head stride is smaller than rows*D", who);
+  PC_REQUIRE(aligned16(K, k_stride_h, dtype) && aligned16(V, v_stride_h, dtype), PC_ERR_SHAPE,
+             "%s: bf16 rows and head strides must be 16-byte aligned", who);
+  const int64_t units = 2ll * H * n;
+  PC_REQUIRE(units * (D / 8) <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
+  const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
+  const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
+  const Book b = {pos_new, pos, weights, pos_stride_h, weights_stride_h, book ? Hsel : 0};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto go = [&](auto kernel, auto* k, auto* v) {
+    kernel<<<blocks, kCopyThreads, 0, s>>>(k, v, at, rows_of(cache), row0, static_cast<int>(units), b);
+  };
+  if (dtype == PC_BF16) {
+    const auto *k = static_cast<const uint16_t*>(K), *v = static_cast<const uint16_t*>(V);
+    D == 64 ? go(q4_store_kernel<uint16_t, 64>, k, v) : go(q4_store_kernel<uint16_t, 128>, k, v);
+  } else {
+    const auto *k = static_cast<const float*>(K), *v = static_cast<const float*>(V);
+    D == 64 ? go(q4_store_kernel<float, 64>, k, v) : go(q4_store_kernel<float, 128>, k, v);
+  }
+  PC_CHECK_LAUNCH(who);
+  return PC_OK;
+}
+
+extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype, void* K, void* V,
+                          int64_t k_stride_h, int64_t v_stride_h, void* stream) {
+  const char* who = "pc_q4_load";
+  if (int rc = check_kind(dtype, D, who)) return rc;
+  PC_REQUIRE(H > 0 && n >= 0 && row0 >= 0, PC_ERR_SHAPE, "%s: H=%d n=%d row0=%d", who, H, n, row0);
+  if (int rc = check_q4_cache(cache, D, who)) return rc;
+  if (int rc = check_q4_span(cache, H, row0, n, D, who)) return rc;
+  PC_REQUIRE(K || V, PC_ERR_NULL, "%s: K and V are NULL", who);
+  if (n == 0) return PC_OK;
+  PC_REQUIRE(H == 1 || ((!K || k_stride_h >= static_cast<int64_t>(n) * D) && (!V || v_stride_h >= static_cast<int64_t>(n) * D)),
+             PC_ERR_SHAPE, "%s: a head stride is smaller than rows*D", who);
+  PC_REQUIRE((!K || aligned16(K, k_stride_h, dtype)) && (!V || aligned16(V, v_stride_h, dtype)), PC_ERR_SHAPE,
+             "%s: bf16 rows and head strides must be 16-byte aligned", who);
+  const int64_t per = static_cast<int64_t>(H) * n, units = per * ((K != nullptr) + (V != nullptr));
+  PC_REQUIRE(2 * per * (D / 8) <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
+  const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
+  const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
+  const int first = K ? 0 : static_cast<int>(per);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto go = [&](auto kernel, auto* k, auto* v) {
+    kernel<<<blocks, kCopyThreads, 0, s>>>(k, v, at, rows_of(cache), row0, first, static_cast<int>(units));
+  };
+  if (dtype == PC_BF16) {
+    auto *k = static_cast<uint16_t*>(K), *v = static_cast<uint16_t*>(V);
+    D == 64 ? go(q4_load_kernel<uint16_t, 64>, k, v) : go(q4_load_kernel<uint16_t, 128>, k, v);
+  } else {
+    auto *k = static_cast<float*>(K), *v = static_cast<float*>(V);
+    D == 64 ? go(q4_load_kernel<float, 64>, k, v) : go(q4_load_kernel<float, 128>, k, v);
+  }
+  PC_CHECK_LAUNCH(who);
+  return PC_OK;
+}
+
+namespace {
+bool sizes_ok(int Hq, int Hkv, int Nq, int Nk) {
+  return Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq >= 1 && Nk >= 1 && Nk <= (1 << 30) && static_cast<int64_t>(Hq) * Nq <= INT_MAX / 2;
+}
+}  // namespace
+
+extern "C" size_t pc_q4_attn_workspace_bytes(int dtype, int Hq, int Hkv, int Nq, int Nk, int D, int weights) {
+  if (!sizes_ok(Hq, Hkv, Nq, Nk) || (dtype != PC_F32 && dtype != PC_BF16) || (D != 64 && D != 128)) return 0;
+  return plan_q4(Hkv, Hq / Hkv * Nq, Nk, D, weights != 0).bytes;
+}
+
+extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, int Hq, int Hkv, int Nq, int Nk, int D,
+                          int64_t q_stride_h, int64_t o_stride_h, float scale, void* O, float* lse, float* weights,
+                          int64_t weights_stride_h, int Hsel, float decay, void* ws, size_t ws_bytes, void* stream) {
+  const char* who = "pc_q4_attn";
+  if (int rc = check_kind(dtype, D, who)) return rc;
+  PC_REQUIRE(sizes_ok(Hq, Hkv, Nq, Nk), PC_ERR_SHAPE,
+             "%s: Hq=%d must be a positive multiple of Hkv=%d, Nq=%d and Nk=%d at least 1", who, Hq, Hkv, Nq, Nk);
+  PC_REQUIRE(scale > 0.f && isfinite(scale), PC_ERR_SHAPE, "%s: scale %g must be > 0", who, scale);
+  PC_REQUIRE(Q && O, PC_ERR_NULL, "%s: Q or O is NULL", who);
+  if (int rc = check_q4_cache(cache, D, who)) return rc;
+  if (int rc = check_q4_span(cache, Hkv, 0, Nk, D, who)) return rc;
+  PC_REQUIRE(Hq == 1 || (q_stride_h >= static_cast<int64_t>(Nq) * D && o_stride_h >= static_cast<int64_t>(Nq) * D), PC_ERR_SHAPE,
+             "%s: a head stride is smaller than rows*D", who);
+  PC_REQUIRE(aligned16(Q, q_stride_h, dtype) && aligned16(O, o_stride_h, dtype), PC_ERR_SHAPE,
+             "%s: bf16 tensors and head strides must be 16-byte aligned", who);
+  if (weights != nullptr) {
+    PC_REQUIRE(Hsel == 1 || Hsel == Hkv, PC_ERR_SHAPE, "%s: weights of %d heads for %d KV heads", who, Hsel, Hkv);
+    PC_REQUIRE(Hsel == 1 || weights_stride_h >= Nk, PC_ERR_SHAPE, "%s: weights' head stride is smaller than Nk", who);
+    PC_REQUIRE(decay >= 0.f && isfinite(decay), PC_ERR_BUDGET, "%s: decay %g", who, decay);
+  }
+  const int rep = Hq / Hkv, rows = rep * Nq;
+  const Q4Plan plan = plan_q4(Hkv, rows, Nk, D, weights != nullptr);
+  PC_REQUIRE(plan.bytes == 0 || (ws != nullptr && ws_bytes >= plan.bytes && reinterpret_cast<uintptr_t>(ws) % 16 == 0),
+             PC_ERR_WORKSPACE, "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, plan.bytes, ws_bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto* base = static_cast<uint8_t*>(ws);
+  const int tiles_q = ceil_div(rows, 16 * plan.row_tiles);
+  AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, 0, q_stride_h, o_stride_h,
+                scale * 1.4426950408889634f, nullptr, nullptr, lse, nullptr, static_cast<int64_t>(Hkv) * rows};
+  a.share_steps = ceil_div(ceil_div(Nk, kStep), plan.n_splits);
+  if (plan.n_splits > 1) {
+    a.part_o = reinterpret_cast<float*>(base);
+    a.part_ml = reinterpret_cast<float2*>(base + plan.ml_at);
+  }
+  if (weights != nullptr) a.lse2 = reinterpret_cast<float*>(base + plan.lse_at);
+  auto run = [&](auto zero, auto dims) -> int {
+    using T = decltype(zero);
+    constexpr int kDims = decltype(dims)::value;
+    const T* q = static_cast<const T*>(Q);
+    const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
+    kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
+    PC_CHECK_LAUNCH(who);
+    if (plan.n_splits > 1) {
+      q4_merge_kernel<T, kDims><<<static_cast<unsigned>(a.rows_all), 256, 0, s>>>(static_cast<T*>(O), plan.n_splits, a);
+      PC_CHECK_LAUNCH(who);
+    }
+    if (weights != nullptr) {
+      const int blocks = ceil_div(Nk, 64);
+      const WeighArgs w = {a.cache, rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(blocks), q_stride_h, weights_stride_h, a.c, decay,
+                           a.lse2, weights};
+      q4_weigh_kernel<T, kDims><<<blocks * Hsel, 256, 0, s>>>(q, w);
+      PC_CHECK_LAUNCH(who);
+    }
+    return PC_OK;
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (dtype == PC_BF16) return D == 64 ? run(uint16_t{}, D64{}) : run(uint16_t{}, D128{});
+  return D == 64 ? run(float{}, D64{}) : run(float{}, D128{});
+}

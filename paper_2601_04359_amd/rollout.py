@@ -18,6 +18,11 @@ A model that makes several attention passes per frame (iterative decoding) calls
 on the un-packed cache first, hands its log-sum-exp to refresh() and makes the remaining
 passes on the packed cache: the compaction is paid once per frame.
 
+EvictingStack is the cache of a stack of layers for generation in small steps (text, or video token
+by token), held in 4 bits and kept within a budget by what attention itself looks at instead of by
+the frames' age: pc_q4_store, pc_q4_attn (which adds up every key's attention weight) and one
+pc_q4_evict for all layers when a step ends.
+
 With slide_t_scale set the window slides (Sec. 3.4, Slide-Cache): when a step begins, the
 oldest frames that the step before evicted completely leave the segment table and
 pc_rebase lowers the temporal coordinate of every retained frame row by slide_t_scale per
@@ -282,3 +287,68 @@ class RollingStack:
             return
         self.segments, self.nk = pk.pc_compact_batch(self.K, self.V, self.pos, self.score, self.segments, budgets,
                                                      share_heads=self.share_heads, ws=self._ws_compact)
+
+
+class EvictingStack:
+    """The caches of a stack of layers in 4 bits, kept to `budget` rows per head by accumulated attention weight.
+
+    Per step:
+        append(layer, K, V, pos)   the step's keys (rotated on insertion) and values enter the layer's cache
+        attend(layer, Q)           the step's queries over the cache with the new rows in it; every key's
+                                   attention weight is added to its sum (times `decay` per step)
+        end_step()                 a cache above its budget loses the rows of least weight, all layers in one call
+
+    Rows below n_anchor (the prompt) and rows whose t coordinate is within recent_t of the newest row's are kept
+    whatever their weight.  With the budget reached, a step of n rows goes from budget to budget + n rows and back:
+    the same launches every time, so a step can be recorded into a HIP graph and replayed.
+    """
+
+    def __init__(self, n_layers: int, Hq: int, Hkv: int, D: int, budget: int, scale: float, step_rows: int = 1,
+                 n_anchor: int = 0, recent_t: int = 0, decay: float = 1.0, sections=(32, 48, 48), base: float = 10000.0,
+                 device="cuda:0", share_heads: bool = False):
+        import torch
+        if not 0 <= n_anchor <= budget or budget < 1 or step_rows < 1:
+            raise ValueError(f"budget {budget} rows, {n_anchor} of them anchors, {step_rows} new ones per step")
+        self.L, self.Hq, self.Hkv, self.D, self.budget, self.scale = n_layers, Hq, Hkv, D, budget, scale
+        self.capacity, self.n_anchor, self.recent_t, self.decay = budget + step_rows, n_anchor, recent_t, decay
+        self.sections, self.base, self.hsel = tuple(sections), base, 1 if share_heads else Hkv
+        # layers x heads are the heads of one cache, so that one call evicts from all of them
+        self.cache = pk.q4_cache(n_layers * Hkv, self.capacity, D, device)
+        self.pos = torch.zeros((n_layers * self.hsel, self.capacity, 3), dtype=torch.int32, device=device)
+        self.weights = torch.zeros((n_layers * self.hsel, self.capacity), dtype=torch.float32, device=device)
+        self.nk = 0      # rows when a step begins
+        self.n_new = 0   # rows of the step under way
+
+    def layer(self, layer: int):
+        """The layer's part: (4-bit cache, pos, weights), as views."""
+        a, s = layer * self.Hkv, layer * self.hsel
+        return (tuple(t[a:a + self.Hkv] for t in self.cache), self.pos[s:s + self.hsel], self.weights[s:s + self.hsel])
+
+    def append(self, layer: int, K, V, pos_new, rotate: bool = True) -> None:
+        """K, V [Hkv][n][D] of the step become the layer's newest rows, at coordinates pos_new (int32 [n][3], device);
+        with `rotate` the keys are rotated in place first.  Every layer of a step appends the same number of rows."""
+        n = K.shape[1]
+        if self.nk + n > self.capacity:
+            raise ValueError(f"cache capacity {self.capacity} < {self.nk} + {n}")
+        if self.n_new not in (0, n):
+            raise ValueError(f"{n} rows after {self.n_new} in another layer of the same step")
+        self.n_new = n
+        cache, pos, weights = self.layer(layer)
+        if rotate:
+            pk.pc_rope3d(K, pos_new, self.sections, self.base)
+        pk.pc_q4_store(K, V, cache, self.nk, pos_new=pos_new, pos=pos, weights=weights)
+
+    def attend(self, layer: int, Q, O=None, q_pos=None, lse=None, accumulate: bool = True):
+        """Queries Q [Hq][n][D] over the layer's cache -> O.  q_pos (int32 [n][3], device): rotate Q in place first."""
+        if q_pos is not None:
+            pk.pc_rope3d(Q, q_pos, self.sections, self.base)
+        cache, _, weights = self.layer(layer)
+        return pk.pc_q4_attn(Q, cache, self.nk + self.n_new, self.scale, O=O, lse=lse,
+                             weights=weights if accumulate else None, decay=self.decay)
+
+    def end_step(self) -> int:
+        """The step's rows are part of the cache; above the budget all layers are cut to it.  Returns the rows left."""
+        self.nk, self.n_new = self.nk + self.n_new, 0
+        if self.nk > self.budget:
+            self.nk = pk.pc_q4_evict(self.cache, self.pos, self.weights, self.nk, self.budget, self.n_anchor, self.recent_t)
+        return self.nk

@@ -1,0 +1,351 @@
+"""The 4-bit cache (pc_q4_store, pc_q4_load, pc_q4_attn) and eviction by weight against plain 64-bit forms.
+
+Codes, scales, moved rows and indices have to be equal bit for bit.  Tolerances of the attention, element by element,
+with u = 2^-24 (half a step of fp32), A = the largest sum_d |q_d k_d| * scale of the call, in units of the logits:
+  * a logit: D products summed in fp32 in any order, the scale folded into base 2 (three roundings), the subtraction
+    of the reference: |ds| <= (D + 8) u A; the exponential adds a step of its result (v_exp_f32: 2 u) and its argument's
+    rounding, up to u * 2 A * log2(e).  A probability is off by a factor of at most 1 + e, e = (D + 16) u A + 8 u.
+  * O, fp32 inputs: (2 e + (Nk + 64) u) sum_j p_j |v_j|: probability and normaliser, sums of Nk terms, merges.
+  * O, bf16 inputs: the probabilities are rounded to bf16 before the second product and O at the end, half a step each:
+    2^-8 (|O| + sum_j p_j |v_j|) more.
+  * lse: (D + 16) u A + (|lse| + Nk + 64) u;  weights: (2 e + (rows + 64) u) mass + 2 u (decay |w| + mass).
+(Nk u is the worst case of a serial sum; the largest Nk here makes it 2^-11.)
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_04359_amd as pk
+from oracle import q4_oracle as orc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def f64(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def packed(K, V, spare=3, head_gap=0):
+    """A cache that holds float arrays K, V [H][n][D] in its first rows, quantised by the oracle; spare rows behind them
+    hold NaN groups, head_gap more rows lie between heads."""
+    H, n, D = K.shape
+    out = []
+    for x in (K, V):
+        codes, scales = orc.q4_store(x)
+        c = torch.full((H, n + spare + head_gap, D // 2), 0x77, dtype=torch.uint8)
+        s = torch.full((H, n + spare + head_gap, D // 32), 255, dtype=torch.uint8)
+        c[:, :n], s[:, :n] = torch.from_numpy(codes), torch.from_numpy(scales)
+        out += [c.to(DEV)[:, :n + spare], s.to(DEV)[:, :n + spare]]
+    return tuple(out)
+
+
+def cache_values(cache, n):
+    kc, ks, vc, vs = (t[:, :n].cpu().numpy() for t in cache)
+    return orc.q4_load(kc, ks), orc.q4_load(vc, vs)
+
+
+def rows(rng, shape, hard=True):
+    """Rows with channels and groups of very different sizes, ties of the grid, zeros and tiny numbers."""
+    x = rng.standard_normal(shape) * np.exp(rng.standard_normal(shape[:-2] + (1, shape[-1])))
+    if hard:
+        flat = x.reshape(-1, shape[-1])
+        n = len(flat)
+        grid = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 6.0, -0.25, -2.5, -5.0, -7.0])
+        flat[rng.integers(n), :32] = 0.0
+        flat[rng.integers(n), :32] = np.resize(grid, 32)                 # every border between codes
+        flat[rng.integers(n), 32:64] = np.resize(grid, 32) * 2.0 ** -100
+        flat[rng.integers(n), 32:64] = np.resize(grid, 32) * 2.0 ** -122  # below the least scale
+        flat[rng.integers(n), :32] = np.resize(grid, 32) * 2.0 ** 125     # the largest scale
+        flat[rng.integers(n), 32:64] = 3.3e38
+        flat[rng.integers(n), 0] = 1e-40
+    return x
+
+
+# ------------------------------------------------------------------------------ rows in, rows out
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,n,row0", [(1, 1, 0), (3, 7, 2), (112, 1, 5), (2, 129, 0), (5, 64, 31)])
+def test_store_and_load(dtype, D, H, n, row0):
+    rng = np.random.default_rng(H * n + D)
+    big = [torch.from_numpy(rows(rng, (H, n + 4, D))).to(TYPES[dtype]).to(DEV) for _ in range(2)]
+    K, V = big[0][:, :n], big[1][:, 2:n + 2]       # rows of longer heads
+    K[0, 0, 3], V[-1, -1, 40], V[0, -1, 1] = float("nan"), float("inf"), -float("inf")
+    cap = row0 + n + 3
+    cache = tuple(torch.full((H, cap, w), 0xA5, dtype=torch.uint8, device=DEV) for w in (D // 2, D // 32) * 2)
+    pk.pc_q4_store(K, V, cache, row0)
+    for x, codes, scales in ((K, *cache[:2]), (V, *cache[2:])):
+        want_c, want_s = orc.q4_store(f64(x))
+        assert np.array_equal(scales[:, row0:row0 + n].cpu().numpy(), want_s)
+        assert np.array_equal(codes[:, row0:row0 + n].cpu().numpy(), want_c)
+        for t in (codes, scales):                   # the rows before and behind are as they were
+            assert (t[:, :row0] == 0xA5).all() and (t[:, row0 + n:] == 0xA5).all()
+    want = cache_values(tuple(t[:, row0:] for t in cache), n)
+    for out in ("bf16", "f32"):
+        Ko = torch.full((H, n + 1, D), 7.0, dtype=TYPES[out], device=DEV)
+        Vo = Ko.clone()
+        pk.pc_q4_load(cache, row0, Ko[:, :n], Vo[:, :n])
+        for got, w in ((Ko, want[0]), (Vo, want[1])):
+            assert np.array_equal(f64(got[:, :n]), w, equal_nan=True) and (got[:, n] == 7.0).all()
+        one = torch.empty((H, n, D), dtype=TYPES[out], device=DEV)
+        assert pk.pc_q4_load(cache, row0, V=one)[1] is one and np.array_equal(f64(one), want[1], equal_nan=True)
+        assert pk.pc_q4_load(cache, row0, K=one)[0] is one and np.array_equal(f64(one), want[0], equal_nan=True)
+
+
+@pytest.mark.parametrize("H,Hsel,n", [(4, 4, 3), (4, 1, 130), (6, 2, 1)])
+def test_store_writes_the_rows_bookkeeping(H, Hsel, n):
+    D, row0, cap = 128, 4, 4 + n + 2
+    x = torch.randn((H, n, D), device=DEV, dtype=torch.bfloat16)
+    cache = pk.q4_cache(H, cap, D)
+    pos = torch.full((Hsel, cap, 3), -7, dtype=torch.int32, device=DEV)
+    w = torch.full((Hsel, cap), 3.0, device=DEV)
+    new = torch.arange(3 * n, dtype=torch.int32, device=DEV).view(n, 3)
+    pk.pc_q4_store(x, x, cache, row0, pos_new=new, pos=pos, weights=w)
+    assert torch.equal(pos[:, row0:row0 + n], new.expand(Hsel, n, 3)) and (w[:, row0:row0 + n] == 0).all()
+    for rest in (slice(0, row0), slice(row0 + n, cap)):
+        assert (pos[:, rest] == -7).all() and (w[:, rest] == 3.0).all()
+    pk.pc_q4_store(x, x, cache, row0, weights=w.fill_(2.0))
+    assert (w[:, row0:row0 + n] == 0).all() and (w[:, :row0] == 2.0).all()
+    pk.pc_q4_store(x[:, :0], x[:, :0], cache, cap, weights=w)      # nothing to store
+
+
+# ------------------------------------------------------------------------------ attention
+def check_attn(dtype, Hq, Hkv, Nq, Nk, D, *, weights=None, decay=1.0, seed=0, scale=None, K=None, V=None, Q=None, q_gap=0,
+               head_gap=0, lse=True, ws=None, visible=slice(None)):
+    rng = np.random.default_rng(1000 * seed + Hq * 7 + Nq * 13 + Nk)
+    scale = D ** -0.5 if scale is None else scale
+    K = rng.standard_normal((Hkv, Nk, D)) if K is None else K
+    V = rng.standard_normal((Hkv, Nk, D)) if V is None else V
+    Q = rng.standard_normal((Hq, Nq, D)) * 1.5 if Q is None else Q
+    cache = packed(K, V, head_gap=head_gap)
+    Qd = torch.zeros((Hq, Nq + q_gap, D), dtype=TYPES[dtype], device=DEV)[:, :Nq]
+    Qd.copy_(torch.from_numpy(Q))
+    O = torch.full((Hq, Nq + q_gap, D), 9.0, dtype=TYPES[dtype], device=DEV)
+    L = torch.empty((Hq, Nq), device=DEV) if lse else None
+    w = None
+    if weights is not None:
+        w = torch.full((1 if weights == "one" else Hkv, Nk + 5), 3.0, device=DEV)
+        w[:, :Nk] = torch.from_numpy(rng.exponential(1.0, (w.shape[0], Nk)))
+        if decay == 0.0:
+            w[:, :Nk] = float("nan")
+        w0 = f64(w)
+    pk.pc_q4_attn(Qd, cache, Nk, scale, O=O[:, :Nq], lse=L, weights=w, decay=decay, ws=ws)
+    assert (O[:, Nq:] == 9.0).all()
+    Kv, Vv = cache_values(cache, Nk)
+    Qv = f64(Qd)
+    want, want_l, mass = orc.attn(Qv, Kv, Vv, scale)
+    spread = orc.attn(Qv, Kv, np.abs(Vv), scale)[0]            # sum_j p_j |v_j|
+    rep = Hq // Hkv
+    # keys that a call hides have probability 0 in either form: the bound is that of the others
+    A = max(float((np.abs(Qv[h]) @ np.abs(Kv[h // rep][visible]).T).max()) for h in range(Hq)) * scale
+    e = (D + 16) * U * A + 8 * U
+    tol = (2 * e + (Nk + 64) * U) * spread
+    if dtype == "bf16":
+        tol += 2.0 ** -8 * (np.abs(want) + spread)
+    err = np.abs(f64(O[:, :Nq]) - want)
+    assert np.all(err <= tol + 1e-30), (err.max(), (err / (tol + 1e-30)).max())
+    if lse:
+        err = np.abs(f64(L) - want_l)
+        assert np.all(err <= (D + 16) * U * A + (np.abs(want_l) + Nk + 64) * U), err.max()
+    if w is not None:
+        mass = mass.sum(0, keepdims=True) if weights == "one" else mass
+        old = 0.0 if decay == 0.0 else decay * w0[:, :Nk]
+        n = Hq * Nq if weights == "one" else rep * Nq
+        tol = (2 * e + (n + 64) * U) * mass + 2 * U * (np.abs(old) + mass)
+        err = np.abs(f64(w[:, :Nk]) - (old + mass))
+        assert np.all(err <= tol + 1e-37), (err.max(), (err / (tol + 1e-37)).max())
+        assert (w[:, Nk:] == 3.0).all()
+    return O[:, :Nq], L, w
+
+
+SHAPES = [   # Hq, Hkv, Nq, Nk
+    (1, 1, 1, 1), (2, 1, 1, 2), (4, 4, 1, 15), (8, 2, 1, 16), (8, 2, 1, 17), (6, 2, 3, 31), (4, 1, 4, 32), (16, 4, 1, 33),
+    (3, 1, 5, 64), (24, 8, 1, 255), (8, 2, 2, 257), (5, 1, 3, 511), (2, 2, 9, 1000), (16, 4, 4, 1179), (8, 8, 17, 300),
+    (2, 1, 16, 777), (4, 2, 23, 90), (16, 1, 1, 5000), (32, 1, 1, 640), (6, 2, 40, 129), (4, 2, 64, 1804), (2, 2, 131, 515),
+    (8, 2, 100, 260), (16, 4, 37, 2000),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk", SHAPES)
+def test_attn(dtype, D, Hq, Hkv, Nq, Nk):
+    check_attn(dtype, Hq, Hkv, Nq, Nk, D)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("weights", ["each", "one"])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk,D,decay", [
+    (1, 1, 1, 1, 64, 1.0), (8, 2, 1, 17, 128, 0.98), (16, 4, 1, 1179, 128, 0.0), (6, 2, 11, 64, 64, 0.5), (24, 8, 1, 260, 128, 1.0),
+    (4, 2, 23, 515, 64, 0.9), (8, 2, 37, 1804, 128, 0.0), (3, 1, 70, 33, 128, 1.0), (4, 4, 1, 4097, 64, 0.25),
+    (8, 2, 100, 300, 128, 2.0)])
+def test_attn_weights(dtype, weights, Hq, Hkv, Nq, Nk, D, decay):
+    check_attn(dtype, Hq, Hkv, Nq, Nk, D, weights=weights, decay=decay, lse=Nk % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 30, 150])
+def test_attn_long(dtype, Nq):
+    """Many shares, and far more keys than a share."""
+    check_attn(dtype, 4, 2, Nq, 20011, 128, weights="each", decay=0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Nq,D", [(1, 128), (21, 64), (90, 128)])
+def test_attn_strides(dtype, Nq, D):
+    """Heads of the cache, the queries and the output further apart than their rows."""
+    check_attn(dtype, 6, 3, Nq, 203, D, weights="each", q_gap=3, head_gap=17)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 40, 130])
+@pytest.mark.parametrize("order", ["up", "down", "peak"])
+def test_attn_reference_moves(dtype, Nq, order):
+    """Logits that climb through the keys by hundreds, fall, or peak at one key in the middle."""
+    Hq, Hkv, Nk, D = 4, 2, 700, 128
+    rng = np.random.default_rng(5)
+    K, Q = rng.standard_normal((Hkv, Nk, D)) * 0.1, rng.standard_normal((Hq, Nq, D)) * 0.1
+    K[..., 0] = {"up": np.linspace(0, 6, Nk), "down": np.linspace(6, 0, Nk), "peak": (np.arange(Nk) == 351) * 6.0}[order]
+    Q[..., 0] = 1000.0 if order != "peak" else 300.0
+    check_attn(dtype, Hq, Hkv, Nq, Nk, D, K=K, Q=Q, weights="each")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 33, 130])
+def test_attn_masked_by_a_coordinate(dtype, Nq):
+    """Keys that a caller hides through a dimension of its own: logits of -1e30 in the first and the last shares, one
+    key in a hundred visible.  Hidden keys get weight 0."""
+    Hq, Hkv, Nk, D = 4, 2, 3000, 128
+    rng = np.random.default_rng(9)
+    K, Q = rng.standard_normal((Hkv, Nk, D)), rng.standard_normal((Hq, Nq, D))
+    hidden = np.arange(Nk) % 100 != 57
+    K[:, :, 127] = np.where(hidden, -6.0, 0.0)
+    K[:, :, 96:127] = 0.0
+    Q[..., 127] = 2.0 ** 100
+    _, _, w = check_attn(dtype, Hq, Hkv, Nq, Nk, D, K=K, Q=Q, weights="each", decay=0.0, visible=~hidden)
+    assert (w[:, :Nk][:, torch.from_numpy(hidden).to(DEV)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Nq", [1, 20, 130])
+def test_attn_not_a_number(dtype, Nq):
+    """A key group that holds a NaN spoils its KV head's rows, a value group its 32 dims; the other head is untouched."""
+    Hq, Hkv, Nk, D = 4, 2, 400, 128
+    rng = np.random.default_rng(2)
+    K, V = rng.standard_normal((Hkv, Nk, D)), rng.standard_normal((Hkv, Nk, D))
+    V[1, 399, 70] = np.inf
+    cache, Q = packed(K, V), torch.randn((Hq, Nq, D), device=DEV).to(TYPES[dtype])
+    O = pk.pc_q4_attn(Q, cache, Nk, 0.1)
+    bad = torch.isnan(O)
+    assert bad[2:, :, 64:96].all() and not bad[2:, :, :64].any() and not bad[2:, :, 96:].any() and not bad[:2].any()
+    K[1, 17, 5] = np.nan
+    L, w = torch.zeros((Hq, Nq), device=DEV), torch.zeros((Hkv, Nk), device=DEV)
+    O = pk.pc_q4_attn(Q, packed(K, V), Nk, 0.1, lse=L, weights=w)
+    assert torch.isnan(O[2:]).all() and not torch.isnan(O[:2]).any()
+    assert torch.isnan(L[2:]).all() and not torch.isnan(L[:2]).any() and not torch.isnan(w[0]).any()
+
+
+@pytest.mark.parametrize("Nq,Nk", [(1, 5000), (50, 700), (150, 700)])
+def test_attn_is_reproducible_and_takes_a_workspace(Nq, Nk):
+    Hq, Hkv, D = 8, 2, 128
+    rng = np.random.default_rng(3)
+    cache = packed(rng.standard_normal((Hkv, Nk, D)), rng.standard_normal((Hkv, Nk, D)))
+    Q = torch.randn((Hq, Nq, D), device=DEV, dtype=torch.bfloat16)
+    n = pk.pc_q4_attn_workspace_bytes(pk.PC_BF16, Hq, Hkv, Nq, Nk, D, True)
+    assert n > 0
+    outs = []
+    for _ in range(3):
+        ws = torch.randint(0, 255, (n,), dtype=torch.uint8, device=DEV)
+        w = torch.ones((Hkv, Nk), device=DEV)
+        outs.append((pk.pc_q4_attn(Q, cache, Nk, 0.09, weights=w, ws=ws), w))
+    for O, w in outs[1:]:
+        assert torch.equal(O, outs[0][0]) and torch.equal(w, outs[0][1])
+    with pytest.raises(pk.PackCacheError) as e:
+        pk.pc_q4_attn(Q, cache, Nk, 0.09, weights=w, ws=torch.empty(n - 1, dtype=torch.uint8, device=DEV))
+    assert e.value.status == -6
+
+
+# ------------------------------------------------------------------------------ eviction
+def check_evict(kind, H, Hsel, Nk, n_keep, D=128, n_anchor=0, recent_t=0, w=None, t=None, with_pos=True, with_idx=True, seed=0):
+    rng = np.random.default_rng(seed + Nk * 3 + n_keep)
+    cap = Nk + 2
+    w = rng.exponential(1.0, (Hsel, Nk)) if w is None else w
+    wd = torch.full((Hsel, cap), 5.0, device=DEV)
+    wd[:, :Nk] = torch.from_numpy(np.asarray(w, np.float64))
+    pos = torch.from_numpy(rng.integers(-1000, 1000, (Hsel, cap, 3))).int().to(DEV)
+    if t is not None:
+        pos[:, :Nk, 0] = torch.from_numpy(np.asarray(t)).int().to(DEV)
+    if kind == "q4":
+        data = tuple(torch.randint(0, 255, (H, cap, b), dtype=torch.uint8, device=DEV) for b in (D // 2, D // 32) * 2)
+    else:
+        data = tuple(torch.randn((H, cap, D), device=DEV).to(TYPES[kind]) for _ in range(2))
+    before = [x.clone() for x in data] + ([pos.clone()] if with_pos else []) + [wd.clone()]
+    idx = torch.full((Hsel, n_keep + 1), -1, dtype=torch.int32, device=DEV)[:, :n_keep] if with_idx else None
+    args = (pos if with_pos else None, wd, Nk, n_keep, n_anchor, recent_t)
+    left = pk.pc_q4_evict(data, *args, idx=idx) if kind == "q4" else pk.pc_evict(*data, *args, idx=idx)
+    assert left == min(n_keep, Nk)
+    after = list(data) + ([pos] if with_pos else []) + [wd]
+    t_host = pos_t = before[-2][..., 0].cpu().numpy() if with_pos else None
+    w_host = before[-1].cpu().numpy()
+    for s in range(Hsel):
+        src = orc.evict_rows(w_host[s], None if pos_t is None else t_host[s], Nk, n_keep, n_anchor, recent_t)
+        if with_idx:
+            assert np.array_equal(idx[s].cpu().numpy(), src)
+        src = torch.from_numpy(src).to(DEV)
+        per = H // Hsel
+        for a, b in zip(after, before):
+            for h in range(s * per, (s + 1) * per) if a.shape[0] == H and a is not wd and a is not pos else (s,):
+                assert torch.equal(a[h, :left].view(torch.uint8), b[h][src].view(torch.uint8))
+                assert torch.equal(a[h, left:].view(torch.uint8), b[h, left:].view(torch.uint8))
+
+
+@pytest.mark.parametrize("kind,D", [("bf16", 128), ("f32", 64), ("q4", 128), ("q4", 64), ("bf16", 72)])
+@pytest.mark.parametrize("H,Hsel,Nk,n_keep", [(1, 1, 2, 1), (2, 2, 65, 64), (4, 1, 300, 17), (4, 4, 1025, 1000), (6, 2, 1024, 512),
+                                              (2, 2, 5000, 4999), (3, 3, 2049, 1), (112, 28, 33, 20)])
+def test_evict(kind, D, H, Hsel, Nk, n_keep):
+    check_evict(kind, H, Hsel, Nk, n_keep, D=D)
+
+
+@pytest.mark.parametrize("Nk,n_keep", [(20000, 19999), (20000, 300), (70001, 35000), (33000, 32768)])
+def test_evict_long(Nk, n_keep):
+    check_evict("q4", 2, 2, Nk, n_keep, n_anchor=100, recent_t=40)
+
+
+@pytest.mark.parametrize("Nk", [100, 3000, 40000])
+@pytest.mark.parametrize("what", ["equal", "zeros", "few", "special", "narrow", "spread", "ramp"])
+def test_evict_weights_that_tie(Nk, what):
+    rng = np.random.default_rng(11)
+    w = {"equal": np.full(Nk, 0.37), "zeros": np.where(rng.random(Nk) < 0.9, 0.0, -0.0), "few": rng.integers(0, 3, Nk) * 1.0,
+         "special": rng.choice([np.nan, -np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45, -1e-45, 3.4e38, 1.0, -1.0], Nk),
+         "narrow": 1.0 + rng.integers(0, 50, Nk) * 2.0 ** -23, "spread": np.exp(rng.normal(0, 25, Nk)).clip(0, 3e38),
+         "ramp": np.arange(Nk)[::-1] * 1.0}[what]
+    for n_keep in (1, Nk // 3, Nk - 1):
+        check_evict("q4", 2, 2, Nk, n_keep, w=np.stack([w, np.roll(w, 7)]))
+
+
+@pytest.mark.parametrize("Nk,n_keep,n_anchor,recent_t", [
+    (50, 20, 20, 0), (50, 20, 0, 1), (50, 20, 5, 30), (50, 3, 3, 1000), (9000, 40, 10, 5), (9000, 8999, 4000, 2 ** 31 - 1)])
+@pytest.mark.parametrize("order", ["up", "same", "mixed", "far"])
+def test_evict_anchors_and_recent_rows(Nk, n_keep, n_anchor, recent_t, order):
+    rng = np.random.default_rng(4)
+    t = {"up": np.arange(Nk), "same": np.full(Nk, 3), "mixed": rng.integers(0, Nk, Nk),
+         "far": rng.choice([-2 ** 31, 2 ** 31 - 1, 0], Nk)}[order]
+    check_evict("bf16", 2, 2, Nk, n_keep, n_anchor=n_anchor, recent_t=recent_t, t=np.stack([t, t[::-1]]))
+
+
+def test_evict_without_coordinates_or_index():
+    check_evict("bf16", 4, 2, 900, 700, with_pos=False, n_anchor=10)
+    check_evict("q4", 4, 4, 900, 5, with_pos=False, with_idx=False)
+    check_evict("f32", 4, 1, 900, 899, with_idx=False)
+
+
+def test_evict_nothing():
+    for n_keep in (10, 11):
+        check_evict("bf16", 2, 2, 10, n_keep, with_idx=False)
+    data = torch.randn((2, 10, 128), device=DEV)
+    w = torch.ones((2, 10), device=DEV)
+    assert pk.pc_evict(data, data.clone(), None, w, 10, 0) == 0 and pk.pc_evict(data, data.clone(), None, w, 0, 4) == 0
+    with pytest.raises(pk.PackCacheError):
+        pk.pc_evict(data, data.clone(), None, w, 10, 10, idx=torch.empty((2, 10), dtype=torch.int32, device=DEV))
