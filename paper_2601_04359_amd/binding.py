@@ -148,6 +148,9 @@ def _bind_native(L) -> None:
         entries = [C.cast(f, C.c_void_p).value for f in (L.pc_rope3d, L.pc_score, L.pc_compact, L.pc_compact_batch,
                                                          L.pc_frame_attn, L.pc_frame_attn_workspace_bytes_for, L.pc_budget)]
         _marshal.bind(*entries, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _marshal.bind_q4(*[C.cast(f, C.c_void_p).value for f in (L.pc_q4_store, L.pc_q4_load, L.pc_q4_attn,
+                                                                 L.pc_q4_attn_workspace_bytes, L.pc_evict, L.pc_q4_evict,
+                                                                 L.pc_evict_workspace_bytes)])
         _NATIVE = _marshal
     except (ImportError, AttributeError) as e:
         _NATIVE = False
@@ -651,6 +654,10 @@ def _check_book(pos, weights, H: int, rows: int):
 def pc_q4_store(K, V, cache, row0: int, pos_new=None, pos=None, weights=None) -> None:
     """Rows K, V [H][n][D] (bf16/fp32; keys rotated already) become rows row0 .. of a 4-bit cache.  pos_new (int32
     [n][3]) goes to the same rows of pos (int32 [Hsel][cap][3]); weights (fp32 [Hsel][cap]) begin at 0 there."""
+    if _NATIVE:
+        r = _NATIVE.q4_store(K, V, cache, row0, pos_new, pos, weights)
+        if r is not None:
+            return _check(r)
     import torch
     q4, H, cap, D = _q4_struct(cache)
     if K.shape != V.shape or K.dim() != 3 or K.shape[0] != H or K.shape[2] != D or K.dtype != V.dtype:
@@ -673,6 +680,11 @@ def pc_q4_store(K, V, cache, row0: int, pos_new=None, pos=None, weights=None) ->
 
 def pc_q4_load(cache, row0: int, K=None, V=None):
     """Rows row0 .. of a 4-bit cache as values into K and / or V [H][n][D] (bf16/fp32); returns (K, V)."""
+    if _NATIVE:
+        r = _NATIVE.q4_load(cache, row0, K, V)
+        if r is not None:
+            _check(r)
+            return K, V
     q4, H, cap, D = _q4_struct(cache)
     some = K if K is not None else V
     if some is None:
@@ -699,6 +711,11 @@ def pc_q4_attn(Q, cache, Nk: int, scale: float, O=None, lse=None, weights=None, 
     """Q [Hq][Nq][D] (bf16/fp32) over the first Nk rows of a 4-bit cache -> O [Hq][Nq][D].  weights (fp32 [Hkv or 1][>= Nk]):
     decay * weights + the attention weight of every key, summed over rows and heads.  ws: not to be shared by calls
     that may overlap; None: one of the call's own, from torch's allocator."""
+    if _NATIVE and O is not None:
+        r = _NATIVE.q4_attn(Q, cache, Nk, scale, O, lse, weights, decay, ws)
+        if r is not None:
+            _check(r)
+            return O
     import torch
     q4, Hkv, cap, D = _q4_struct(cache)
     if Q.dim() != 3 or Q.shape[2] != D or Q.shape[0] % Hkv:
@@ -723,7 +740,7 @@ def pc_q4_attn(Q, cache, Nk: int, scale: float, O=None, lse=None, weights=None, 
     _on_device(Q=Q, O=O, lse=lse, ws=ws)
     _check(lib().pc_q4_attn(Q.data_ptr(), C.byref(q4), dtype, Hq, Hkv, Nq, int(Nk), D, Q.stride(0), O.stride(0), float(scale),
                             O.data_ptr(), _ptr(lse), _ptr(weights), 0 if weights is None else weights.stride(0), hsel or 0,
-                            float(decay), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+                            float(decay), _ptr(ws), 0 if ws is None else ws.nbytes, _stream()))
     return O
 
 
@@ -759,6 +776,11 @@ def pc_evict(K, V, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent
     """Of the first Nk rows of K, V [H][cap][D] keep n_keep: rows below n_anchor, rows whose t is within recent_t of row
     Nk - 1's, then those of largest weight (fp32 [Hsel][cap]; pos int32 [Hsel][cap][3] or None).  In place; rows that
     stay below n_keep do not move.  idx (int32 [Hsel][n_keep]): where each row came from.  Returns the rows left."""
+    if _NATIVE:
+        r = _NATIVE.evict(K, V, pos, weights, Nk, n_keep, n_anchor, recent_t, idx, ws)
+        if r is not None:
+            _check(r)
+            return min(Nk, n_keep)
     if K.shape != V.shape or K.dim() != 3 or K.dtype != V.dtype:
         raise PackCacheError(-2, f"K and V must be [H][cap][D] of one type, got {tuple(K.shape)} and {tuple(V.shape)}")
     H, cap, D = K.shape
@@ -774,6 +796,11 @@ def pc_evict(K, V, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent
 
 def pc_q4_evict(cache, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent_t: int = 0, idx=None, ws=None) -> int:
     """pc_evict on a 4-bit cache."""
+    if _NATIVE:
+        r = _NATIVE.q4_evict(cache, pos, weights, Nk, n_keep, n_anchor, recent_t, idx, ws)
+        if r is not None:
+            _check(r)
+            return min(Nk, n_keep)
     q4, H, cap, D = _q4_struct(cache)
     hsel, idx_stride, ws = _evict_book(pos, weights, H, cap, Nk, n_keep, idx, ws, cache[0])
     _check(lib().pc_q4_evict(C.byref(q4), H, D, _ptr(pos), 0 if pos is None else pos.stride(0), weights.data_ptr(),

@@ -17,6 +17,7 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <vector>
 
 #include "packcache.h"
@@ -32,6 +33,15 @@ struct Library {
   decltype(&pc_frame_attn_workspace_bytes_for) attn_bytes;
   decltype(&pc_budget) budget;
 } lib = {};
+struct Q4Library {
+  decltype(&pc_q4_store) store;
+  decltype(&pc_q4_load) load;
+  decltype(&pc_q4_attn) attn;
+  decltype(&pc_q4_attn_workspace_bytes) attn_bytes;
+  decltype(&pc_evict) evict;
+  decltype(&pc_q4_evict) q4_evict;
+  decltype(&pc_evict_workspace_bytes) evict_bytes;
+} q4 = {};
 PyObject* current_device = nullptr;   // torch's raw queries of the current device and of its stream
 PyObject* raw_stream = nullptr;
 
@@ -326,6 +336,257 @@ PyObject* frame_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // Q,
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the cache in 4 bits, and eviction by accumulated weight -----------------------------------------
+PyObject* bind_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {   // 7 addresses
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "bind_q4: 7 arguments");
+    return nullptr;
+  }
+  void* p[7];
+  for (int i = 0; i < 7; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  if (PyErr_Occurred()) return nullptr;
+  q4 = {reinterpret_cast<decltype(&pc_q4_store)>(p[0]),
+        reinterpret_cast<decltype(&pc_q4_load)>(p[1]),
+        reinterpret_cast<decltype(&pc_q4_attn)>(p[2]),
+        reinterpret_cast<decltype(&pc_q4_attn_workspace_bytes)>(p[3]),
+        reinterpret_cast<decltype(&pc_evict)>(p[4]),
+        reinterpret_cast<decltype(&pc_q4_evict)>(p[5]),
+        reinterpret_cast<decltype(&pc_evict_workspace_bytes)>(p[6])};
+  Py_RETURN_NONE;
+}
+bool ready_q4() { return ready() && q4.store != nullptr; }
+
+// The current stream, and whether every tensor is on its device: calls go there.
+struct Place {
+  void* stream = nullptr;
+  int device = -1;
+  bool find() {
+    PyObject* d = PyObject_CallNoArgs(current_device);
+    if (!d) return false;
+    device = static_cast<int>(PyLong_AsLong(d));
+    PyObject* handle = PyObject_CallOneArg(raw_stream, d);
+    Py_DECREF(d);
+    if (!handle) return false;
+    stream = PyLong_AsVoidPtr(handle);
+    Py_DECREF(handle);
+    return !PyErr_Occurred();
+  }
+  bool holds(std::initializer_list<const at::Tensor*> all) const {
+    for (const at::Tensor* t : all)
+      if (t && t->get_device() != device) return false;
+    return true;
+  }
+};
+bool optional(PyObject* o, const at::Tensor** t) { return o == Py_None || (*t = plain(o)) != nullptr; }
+void* pointer(const at::Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
+
+// What binding.py's _q4_struct accepts, a tuple of four.
+struct Cache4 {
+  pc_q4_cache c;
+  const at::Tensor* t[4];
+  int H, cap, D;
+  bool from(PyObject* o) {
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) return false;
+    for (int i = 0; i < 4; ++i)
+      if (!(t[i] = plain(PyTuple_GET_ITEM(o, i))) || t[i]->scalar_type() != at::kByte || !rows_dense(*t[i], 3)) return false;
+    const at::Tensor &kc = *t[0], &ks = *t[1], &vc = *t[2], &vs = *t[3];
+    if (vc.sizes() != kc.sizes() || vs.sizes() != ks.sizes() || ks.size(0) != kc.size(0) || ks.size(1) != kc.size(1) ||
+        kc.size(2) != 16 * ks.size(2) || vc.stride(0) != kc.stride(0) || vs.stride(0) != ks.stride(0))
+      return false;
+    int half;
+    if (!size_as_int(kc.size(0), &H) || !size_as_int(kc.size(1), &cap) || !size_as_int(kc.size(2), &half) || half > 1024) return false;
+    D = 2 * half;
+    auto bytes = [](const at::Tensor& x) { return static_cast<uint8_t*>(x.mutable_data_ptr()); };
+    c = {bytes(kc), bytes(ks), bytes(vc), bytes(vs), kc.stride(0), ks.stride(0)};
+    return true;
+  }
+  bool on(const Place& at) const { return at.holds({t[0], t[1], t[2], t[3]}); }
+};
+
+// Coordinates and sums as binding.py's _check_book takes them; Hsel 0: neither is there.
+struct Book {
+  const at::Tensor *pos = nullptr, *weights = nullptr;
+  int Hsel = 0;
+  bool from(PyObject* p, PyObject* w, int H, int64_t rows) {
+    if (!optional(p, &pos) || !optional(w, &weights)) return false;
+    int64_t n = 0;
+    if (pos) {
+      if (pos->scalar_type() != at::kInt || !rows_dense(*pos, 3) || pos->size(2) != 3 || pos->size(1) < rows) return false;
+      n = pos->size(0);
+    }
+    if (weights) {
+      if (weights->scalar_type() != at::kFloat || weights->dim() != 2 || weights->size(1) < rows ||
+          (weights->size(1) > 1 && weights->stride(1) != 1) || (pos && weights->size(0) != n))
+        return false;
+      n = weights->size(0);
+    }
+    Hsel = static_cast<int>(n);
+    return (!pos && !weights) || (n >= 1 && n <= H && H % n == 0);
+  }
+  int32_t* pos_at() const { return static_cast<int32_t*>(pointer(pos)); }
+  float* weights_at() const { return static_cast<float*>(pointer(weights)); }
+  int64_t pos_stride() const { return pos ? pos->stride(0) : 0; }
+  int64_t weights_stride() const { return weights ? weights->stride(0) : 0; }
+};
+// a workspace of the call's own, from torch's stream-ordered allocator
+at::Tensor make_workspace(size_t bytes, const at::Tensor& like) {
+  return at::empty({static_cast<int64_t>(bytes < 16 ? 16 : bytes)}, at::TensorOptions().dtype(at::kByte).device(like.device()));
+}
+
+PyObject* q4_store(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // K, V, cache, row0, pos_new, pos, weights
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 7 && ready_q4());
+  const at::Tensor *K = plain(a[0]), *V = plain(a[1]), *fresh = nullptr;
+  Cache4 cache;
+  Book book;
+  int32_t row0;
+  int n;
+  PLAIN_OR_NONE(K && V && cache.from(a[2]) && as_int(a[3], &row0) && optional(a[4], &fresh) && rows_dense(*K, 3) &&
+                rows_dense(*V, 3) && K->sizes() == V->sizes() && K->scalar_type() == V->scalar_type() &&
+                K->size(0) == cache.H && K->size(2) == cache.D && size_as_int(K->size(1), &n) && row0 >= 0 &&
+                static_cast<int64_t>(row0) + n <= cache.cap &&
+                book.from(a[5], a[6], cache.H, static_cast<int64_t>(row0) + n) && !fresh == !book.pos);
+  PLAIN_OR_NONE(!fresh || (fresh->scalar_type() == at::kInt && fresh->dim() == 2 && fresh->size(0) == n && fresh->size(1) == 3 &&
+                           fresh->is_contiguous()));
+  const int dt = dtype_code(*K);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && cache.on(at) && at.holds({K, V, fresh, book.pos, book.weights}));
+  void *kp = pointer(K), *vp = pointer(V);
+  auto* np = static_cast<int32_t*>(pointer(fresh));
+  const int64_t ks = K->stride(0), vs = V->stride(0);
+  return PyLong_FromLong(unlocked([&] {
+    return q4.store(kp, vp, dt, cache.H, n, cache.D, ks, vs, &cache.c, row0, np, book.pos_at(), book.pos_stride(),
+                    book.weights_at(), book.weights_stride(), book.Hsel, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* q4_load(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // cache, row0, K, V
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 4 && ready_q4());
+  Cache4 cache;
+  int32_t row0;
+  const at::Tensor *K = nullptr, *V = nullptr;
+  PLAIN_OR_NONE(cache.from(a[0]) && as_int(a[1], &row0) && optional(a[2], &K) && optional(a[3], &V) && (K || V));
+  const at::Tensor& some = K ? *K : *V;
+  int n;
+  PLAIN_OR_NONE(some.dim() == 3 && size_as_int(some.size(1), &n) && row0 >= 0 && static_cast<int64_t>(row0) + n <= cache.cap);
+  for (const at::Tensor* t : {K, V})
+    PLAIN_OR_NONE(!t || (rows_dense(*t, 3) && t->size(0) == cache.H && t->size(1) == n && t->size(2) == cache.D &&
+                         t->scalar_type() == some.scalar_type()));
+  const int dt = dtype_code(some);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && cache.on(at) && at.holds({K, V}));
+  void *kp = pointer(K), *vp = pointer(V);
+  const int64_t ks = K ? K->stride(0) : 0, vs = V ? V->stride(0) : 0;
+  return PyLong_FromLong(unlocked([&] {
+    return q4.load(&cache.c, cache.H, row0, n, cache.D, dt, kp, vp, ks, vs, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* q4_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // Q, cache, Nk, scale, O, lse, weights, decay, ws
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 9 && ready_q4());
+  const at::Tensor *Q = plain(a[0]), *O = plain(a[4]), *lse = nullptr, *ws = nullptr;
+  Cache4 cache;
+  Book book;
+  int32_t Nk;
+  double scale, decay;
+  int Hq, Nq;
+  PLAIN_OR_NONE(Q && O && cache.from(a[1]) && as_int(a[2], &Nk) && as_double(a[3], &scale) && optional(a[5], &lse) &&
+                as_double(a[7], &decay) && optional(a[8], &ws) && rows_dense(*Q, 3) && rows_dense(*O, 3) &&
+                O->sizes() == Q->sizes() && O->scalar_type() == Q->scalar_type() && Q->size(2) == cache.D && cache.H > 0 &&
+                size_as_int(Q->size(0), &Hq) && size_as_int(Q->size(1), &Nq) && Hq % cache.H == 0 && Nk >= 1 &&
+                Nk <= cache.cap && book.from(Py_None, a[6], cache.H, Nk));
+  PLAIN_OR_NONE(!lse || (lse->scalar_type() == at::kFloat && lse->dim() == 2 && lse->size(0) == Hq && lse->size(1) == Nq &&
+                         lse->is_contiguous()));
+  const int dt = dtype_code(*Q);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && cache.on(at) && at.holds({Q, O, lse, book.weights, ws}));
+  at::Tensor own;
+  if (!ws) {
+    const size_t bytes = q4.attn_bytes(dt, Hq, cache.H, Nq, Nk, cache.D, book.weights != nullptr);
+    if (bytes) ws = &(own = make_workspace(bytes, *Q));
+  }
+  void *qp = pointer(Q), *op = pointer(O), *wp = pointer(ws);
+  auto* lp = static_cast<float*>(pointer(lse));
+  const int64_t qs = Q->stride(0), os = O->stride(0);
+  const size_t wn = ws ? ws->nbytes() : 0;
+  return PyLong_FromLong(unlocked([&] {
+    return q4.attn(qp, &cache.c, dt, Hq, cache.H, Nq, Nk, cache.D, qs, os, static_cast<float>(scale), op, lp, book.weights_at(),
+                   book.weights_stride(), book.Hsel, static_cast<float>(decay), wp, wn, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// pos, weights, Nk, n_keep, n_anchor, recent_t, idx, ws from a[0] on
+struct Eviction {
+  Book book;
+  int32_t Nk, n_keep, n_anchor, recent_t;
+  const at::Tensor *idx = nullptr, *ws = nullptr;
+  at::Tensor own;
+  bool from(PyObject* const* a, int H, int64_t cap) {
+    return as_int(a[2], &Nk) && as_int(a[3], &n_keep) && as_int(a[4], &n_anchor) && as_int(a[5], &recent_t) && a[1] != Py_None &&
+           Nk >= 0 && Nk <= cap && H > 0 && book.from(a[0], a[1], H, Nk) && optional(a[6], &idx) && optional(a[7], &ws) &&
+           (!idx || (idx->scalar_type() == at::kInt && idx->dim() == 2 && idx->size(0) == book.Hsel && idx->size(1) >= n_keep &&
+                     (idx->size(1) <= 1 || idx->stride(1) == 1)));
+  }
+  void workspace(const at::Tensor& like) {
+    const size_t bytes = ws ? 0 : q4.evict_bytes(book.Hsel, Nk, n_keep);
+    if (bytes) ws = &(own = make_workspace(bytes, like));
+  }
+};
+
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // K, V, then as above
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 10 && ready_q4());
+  const at::Tensor *K = plain(a[0]), *V = plain(a[1]);
+  Eviction e;
+  int H, D;
+  PLAIN_OR_NONE(K && V && rows_dense(*K, 3) && rows_dense(*V, 3) && K->sizes() == V->sizes() &&
+                K->scalar_type() == V->scalar_type() && size_as_int(K->size(0), &H) && size_as_int(K->size(2), &D) &&
+                e.from(a + 2, H, K->size(1)));
+  const int dt = dtype_code(*K);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && at.holds({K, V, e.book.pos, e.book.weights, e.idx, e.ws}));
+  e.workspace(*K);
+  void *kp = pointer(K), *vp = pointer(V), *wp = pointer(e.ws);
+  auto* ip = static_cast<int32_t*>(pointer(e.idx));
+  const int64_t ks = K->stride(0), vs = V->stride(0), is = e.idx ? e.idx->stride(0) : 0;
+  const size_t wn = e.ws ? e.ws->nbytes() : 0;
+  return PyLong_FromLong(unlocked([&] {
+    return q4.evict(kp, vp, dt, H, D, ks, vs, e.book.pos_at(), e.book.pos_stride(), e.book.weights_at(), e.book.weights_stride(),
+                    e.book.Hsel, e.Nk, e.n_keep, e.n_anchor, e.recent_t, ip, is, wp, wn, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* q4_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // cache, then as above
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 9 && ready_q4());
+  Cache4 cache;
+  Eviction e;
+  PLAIN_OR_NONE(cache.from(a[0]) && e.from(a + 1, cache.H, cache.cap));
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(cache.on(at) && at.holds({e.book.pos, e.book.weights, e.idx, e.ws}));
+  e.workspace(*cache.t[0]);
+  void* wp = pointer(e.ws);
+  auto* ip = static_cast<int32_t*>(pointer(e.idx));
+  const int64_t is = e.idx ? e.idx->stride(0) : 0;
+  const size_t wn = e.ws ? e.ws->nbytes() : 0;
+  return PyLong_FromLong(unlocked([&] {
+    return q4.q4_evict(&cache.c, cache.H, cache.D, e.book.pos_at(), e.book.pos_stride(), e.book.weights_at(),
+                       e.book.weights_stride(), e.book.Hsel, e.Nk, e.n_keep, e.n_anchor, e.recent_t, ip, is, wp, wn, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
 // Rows start .. start + n - 1 of three caches as views: K, V, pos, dim, start, n
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
@@ -406,7 +667,8 @@ PyObject* prunable_span(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(bind),       ENTRY(rope3d),      ENTRY(score),  ENTRY(compact),
                          ENTRY(compact_batch), ENTRY(frame_attn), ENTRY(rows), ENTRY(budget), ENTRY(segment_budgets),
-                         ENTRY(past_frames), ENTRY(prunable_span), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(past_frames), ENTRY(prunable_span), ENTRY(bind_q4), ENTRY(q4_store), ENTRY(q4_load),
+                         ENTRY(q4_attn), ENTRY(evict), ENTRY(q4_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
