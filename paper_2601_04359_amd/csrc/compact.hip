@@ -55,23 +55,6 @@ __device__ __forceinline__ uint32_t order_key(float f) {
 
 __device__ __forceinline__ int popc64(uint64_t v) { return __popcll(v); }
 
-// Inclusive scan over the 64 lanes (lane l gets op over lanes 0..l) with data-parallel-primitive
-// moves: shifts by 1, 2, 4, 8 inside each row of 16 lanes, then lane 15 of a row into the row
-// after it and lane 31 into the upper half.  Each step is one vector instruction; a shuffle
-// through the LDS crossbar costs a round trip of a hundred cycles per step.
-template <class Op>
-__device__ __forceinline__ int wave_scan(int x, int identity, Op op) {
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x111, 0xf, 0xf, false));  // row_shr:1
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x112, 0xf, 0xf, false));  // row_shr:2
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x114, 0xf, 0xf, false));  // row_shr:4
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x118, 0xf, 0xf, false));  // row_shr:8
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x142, 0xa, 0xf, false));  // row_bcast:15 -> rows 1, 3
-  x = op(x, __builtin_amdgcn_update_dpp(identity, x, 0x143, 0xc, 0xf, false));  // row_bcast:31 -> rows 2, 3
-  return x;
-}
-__device__ __forceinline__ int wave_prefix_sum(int x) {  // sum over lanes 0..l
-  return wave_scan(x, 0, [](int a, int b) { return a + b; });
-}
 __device__ __forceinline__ uint32_t wave_or(uint32_t x) {  // OR over the wave, in every lane
   const int r = wave_scan(static_cast<int>(x), 0, [](int a, int b) { return a | b; });
   return static_cast<uint32_t>(__builtin_amdgcn_readlane(r, 63));
@@ -419,11 +402,6 @@ __device__ __forceinline__ void rows_down_from(int n, F&& f) {
     asm volatile("" : "+s"(n));  // one scalar compare here, not 64 lane masks kept from sweep to sweep
     if (i < n) f(i);
   }
-}
-
-__device__ __forceinline__ int lanes_below(uint64_t mask, int base) {  // base + set bits of mask below this lane
-  return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
-                                   __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), base));
 }
 
 // The k best of the len scores at sc, by one wave: store(at, source row) for the at-th of them in

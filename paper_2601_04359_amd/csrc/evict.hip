@@ -14,7 +14,8 @@
 namespace pc {
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kTopBits = 11, kTopBins = 1 << kTopBits;     // of a rank, looked at first
 
 struct Ranks {
   const float* weights;
@@ -41,120 +42,481 @@ struct HeadRanks {
         newest(a.recent_t > 0 ? t[static_cast<int64_t>(a.Nk - 1) * 3] : 0), n_anchor(a.n_anchor), recent_t(a.recent_t) {}
   __device__ __forceinline__ uint32_t of(int j) const {
     const bool safe = j < n_anchor || (t != nullptr && t[static_cast<int64_t>(j) * 3] > newest - recent_t);
-    return safe ? 0xffffffffu : weight_rank(w[j]);
+    const uint32_t rank = weight_rank(w[j]);
+    return safe ? 0xffffffffu : rank;
   }
 };
 
-// exclusive sum over the work-group, and the total; s: one word per wave
-__device__ __forceinline__ int block_scan(int v, int* s, int& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+// One more in a bin for every active lane; lanes of a wave that agree (rows of equal weight) are one addition.
+__device__ __forceinline__ void vote(int* hist, int bin, bool active) {
+  const uint64_t all = __ballot(active);
+  if (all == 0) return;
+  const int first = __builtin_amdgcn_readlane(bin, __builtin_ctzll(all));
+  if (__ballot(active && bin == first) == all) {
+    if (lanes_below(all, 0) == 0 && active) atomicAdd(&hist[first], __popcll(all));
+  } else if (active) {
+    atomicAdd(&hist[bin], 1);
   }
-  __syncthreads();
-  if (lane == 63) s[wave] = x;
-  __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int k = 0; k < kSelThreads / 64; ++k) {
-    if (k < wave) before += s[k];
-    total += s[k];
-  }
-  return before + x - v;
 }
 
-// lists: per selection head `room` holes, then `room` movers
+// Where the left-th row from the top lies among kBins counted bins: s_found = (bin, rows still wanted of it, rows in it).
+// Every thread calls it, between barriers; s_wave: a word per wave.
+template <int kBins>
+__device__ __forceinline__ void find_bin(const int* hist, int left, int* s_wave, int* s_found) {
+  constexpr int kPer = kBins > kSelThreads ? kBins / kSelThreads : kBins > 64 ? (kBins + 1023) / 1024 : 1;
+  constexpr int kUsed = kBins / kPer;            // threads with bins, from the top bin down
+  static_assert(kUsed % 64 == 0 && kUsed <= kSelThreads, "whole waves");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int c[kPer], sum = 0;
+  const bool mine = threadIdx.x < kUsed;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    c[k] = mine ? hist[kBins - 1 - (static_cast<int>(threadIdx.x) * kPer + k)] : 0;
+    sum += c[k];
+  }
+  const int upto = wave_prefix_sum(sum);
+  if (mine && lane == 63) s_wave[wave] = upto;
+  __syncthreads();
+  if (mine) {
+    int at = upto - sum;
+    for (int w = 0; w < wave; ++w) at += s_wave[w];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (at < left && left <= at + c[k]) {
+        s_found[0] = kBins - 1 - (static_cast<int>(threadIdx.x) * kPer + k);
+        s_found[1] = left - at;
+        s_found[2] = c[k];
+      }
+      at += c[k];
+    }
+  }
+  __syncthreads();
+}
+
+// ------------------------------------------------------------------------------------------
+// What moves: rows of whole 16-byte pieces of every head, and the small things beside them.
+// ------------------------------------------------------------------------------------------
+struct Moves {
+  u32x4* rows[2];              // K and V, or their codes
+  int64_t row_stride_h[2];     // in 16-byte pieces
+  Divisor by_pieces, by_both;  // pieces of a row of one of them, and of both
+  uint8_t* scales[2];          // of a 4-bit cache, else NULL
+  int64_t scale_stride_h;
+  int scale_bytes;             // of a row: 2 or 4
+  int32_t* pos;                // of a selection head, may be NULL
+  float* weights;
+  int64_t pos_stride_h, w_stride_h;
+  int32_t* idx;                // may be NULL
+  int64_t idx_stride_h;
+  int per;                     // heads of a selection head
+};
+
+// Units first, first + step, ... of the 16-byte pieces of head h's n moved rows, four loads in flight per thread
+__device__ __forceinline__ void move_rows(const Moves& m, int h, int n, const int32_t* __restrict__ holes,
+                                          const int32_t* __restrict__ movers, int first, int step) {
+  const int n_units = n * m.by_both.d, pieces = m.by_pieces.d;
+  for (int u0 = first; u0 < n_units; u0 += 4 * step) {
+    u32x4 v[4];
+    u32x4* to[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int u = u0 + k * step;
+      if (u >= n_units) continue;
+      const int i = m.by_both.of(u);
+      const int both = u - i * m.by_both.d, second = both >= pieces;
+      u32x4* base = m.rows[second] + h * m.row_stride_h[second] + (both - second * pieces);
+      to[k] = base + static_cast<int64_t>(holes[i]) * pieces;
+      v[k] = base[static_cast<int64_t>(movers[i]) * pieces];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (u0 + k * step < n_units) *to[k] = v[k];
+  }
+}
+
+// The small things of moved rows first, first + step, ...; the selection head's own with its first head
+__device__ __forceinline__ void move_book(const Moves& m, int h, int sel, int n, const int32_t* __restrict__ holes,
+                                          const int32_t* __restrict__ movers, int first, int step) {
+  const bool own = h == sel * m.per;
+  for (int i = first; i < n; i += step) {
+    const int64_t to = holes[i], from = movers[i];
+    if (m.scales[0] != nullptr)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint8_t* base = m.scales[k] + h * m.scale_stride_h;
+        if (m.scale_bytes == 4) reinterpret_cast<uint32_t*>(base)[to] = reinterpret_cast<uint32_t*>(base)[from];
+        else reinterpret_cast<uint16_t*>(base)[to] = reinterpret_cast<uint16_t*>(base)[from];
+      }
+    if (!own) continue;
+    float* w = m.weights + sel * m.w_stride_h;
+    const float was = w[from];
+    if (m.pos != nullptr) {
+      int32_t* p = m.pos + sel * m.pos_stride_h;
+      const int32_t a = p[from * 3], b = p[from * 3 + 1], c = p[from * 3 + 2];
+      p[to * 3] = a, p[to * 3 + 1] = b, p[to * 3 + 2] = c;
+    }
+    w[to] = was;
+    if (m.idx != nullptr) m.idx[sel * m.idx_stride_h + to] = static_cast<int32_t>(from);
+  }
+}
+
+__global__ __launch_bounds__(256) void evict_move_kernel(Moves m, int book_blocks, int room, const int32_t* __restrict__ counts,
+                                                         const int32_t* __restrict__ lists) {
+  const int h = blockIdx.y, sel = h / m.per, n = counts[sel];
+  const int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
+  const int block = static_cast<int>(blockIdx.x) - book_blocks;
+  if (block < 0)
+    move_book(m, h, sel, n, holes, holes + room, blockIdx.x * 256 + threadIdx.x, book_blocks * 256);
+  else
+    move_rows(m, h, n, holes, holes + room, block * 256 + threadIdx.x, (gridDim.x - book_blocks) * 256);
+}
+
+// ------------------------------------------------------------------------------------------
+// Up to 32 x 1,024 rows: a work-group per selection head, the ranks in registers (wave w owns 64 kItems
+// rows in a row, so that list places are a ballot per 64 of them and one sum over the waves).  The n_keep-th rank is
+// found from the top bits down, 11 then 7 at a time, in LDS counters; a step whose bin is wanted whole ends it.
+// With `move` the same work-group moves the rows: a second launch costs more than it takes for few.
+// ------------------------------------------------------------------------------------------
+template <int kItems>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int room, int32_t* __restrict__ counts,
-                                                                   int32_t* __restrict__ lists, int32_t* __restrict__ idx,
-                                                                   int64_t idx_stride_h) {
-  __shared__ int hist[256];
-  __shared__ int s_scan[kSelThreads / 64];
-  __shared__ int s_bin, s_left;
-  const int sel = blockIdx.x;
+                                                                   int32_t* __restrict__ lists, Moves m, int move) {
+  __shared__ int hist[kTopBins + 3 * 128];
+  __shared__ int s_wave[3][kSelWaves], s_found[3];
+  const int sel = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const HeadRanks rank(a, sel);
+  const int j0 = wave * 64 * kItems + lane;
+  uint32_t key[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) key[i] = rank.of(min(j0 + i * 64, a.Nk - 1));
+  for (int b = threadIdx.x; b < kTopBins + 3 * 128; b += kSelThreads) hist[b] = 0;
+  __syncthreads();
   uint32_t prefix = 0;
-  int left = a.n_keep;                    // rows to keep among those that share the prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+  int left = a.n_keep, shift = 32 - kTopBits;
+  bool whole = false;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) vote(hist, key[i] >> (32 - kTopBits), j0 + i * 64 < a.Nk);
+  __syncthreads();
+  find_bin<kTopBins>(hist, left, s_wave[0], s_found);
+  for (int pass = 0;; ++pass) {
+    prefix |= static_cast<uint32_t>(s_found[0]) << shift;
+    left = s_found[1];
+    whole = s_found[2] == left;
+    if (whole || shift == 0) break;
+    shift -= 7;
+    int* h = hist + kTopBins + pass * 128;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      vote(h, key[i] >> shift & 127, j0 + i * 64 < a.Nk && (key[i] ^ prefix) >> (shift + 7) == 0);
     __syncthreads();
-    for (int j = threadIdx.x; j < a.Nk; j += kSelThreads) {
-      const uint32_t k = rank.of(j);
-      if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1);
+    find_bin<128>(h, left, s_wave[0], s_found);
+  }
+  // rows above the threshold stay; of those at it (not whole: several of one weight, left of them wanted) the first ones
+  uint64_t keep[kItems];
+  int ties_before = 0;
+  if (!whole) {
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) mine += __popcll(__ballot(j0 + i * 64 < a.Nk && key[i] == prefix));
+    if (lane == 0) s_wave[0][wave] = mine;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) ties_before += s_wave[0][w];
+  }
+  int n_holes = 0, n_movers = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int j = j0 + i * 64;
+    bool stays = j < a.Nk && (whole ? key[i] >= prefix : key[i] > prefix);
+    if (!whole) {
+      const uint64_t tied = __ballot(j < a.Nk && key[i] == prefix);
+      stays |= j < a.Nk && key[i] == prefix && lanes_below(tied, ties_before) < left;
+      ties_before += __popcll(tied);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      int b = 255, n = left;
-      while (hist[b] < n) n -= hist[b--];
-      s_bin = b;
-      s_left = n;
-    }
-    __syncthreads();
-    prefix |= static_cast<uint32_t>(s_bin) << shift;
-    left = s_left;
-    __syncthreads();
+    keep[i] = __ballot(stays);
+    n_holes += __popcll(__ballot(j < a.n_keep && !stays));
+    n_movers += __popcll(__ballot(j >= a.n_keep && stays));
+    if (m.idx != nullptr && stays && j < a.n_keep) m.idx[sel * m.idx_stride_h + j] = j;
+  }
+  if (lane == 0) s_wave[1][wave] = n_holes, s_wave[2][wave] = n_movers;
+  __syncthreads();
+  int at_h = 0, at_m = 0, n = 0;
+  for (int w = 0; w < kSelWaves; ++w) {
+    if (w < wave) at_h += s_wave[1][w], at_m += s_wave[2][w];
+    n += s_wave[1][w];
   }
   int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
   int32_t* movers = holes + room;
-  int ties = 0, n_holes = 0, n_movers = 0;
-  for (int j0 = 0; j0 < a.Nk; j0 += kSelThreads) {
-    const int j = j0 + threadIdx.x;
-    const uint32_t k = j < a.Nk ? rank.of(j) : 0;
-    const bool tie = j < a.Nk && k == prefix;
-    int total;
-    const int nth = ties + block_scan(tie, s_scan, total);
-    ties += total;
-    const bool keep = j < a.Nk && (k > prefix || (tie && nth < left));
-    const bool hole = j < a.n_keep && !keep, mover = j >= a.n_keep && keep;
-    const int at_h = n_holes + block_scan(hole, s_scan, total);
-    n_holes += total;
-    const int at_m = n_movers + block_scan(mover, s_scan, total);
-    n_movers += total;
-    if (hole) holes[at_h] = j;
-    if (mover) movers[at_m] = j;
-    if (idx != nullptr && keep && j < a.n_keep) idx[sel * idx_stride_h + j] = j;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int j = j0 + i * 64;
+    const bool stays = keep[i] >> lane & 1;
+    const uint64_t bh = __ballot(j < a.n_keep && !stays), bm = __ballot(j >= a.n_keep && stays);
+    if (j < a.n_keep && !stays) holes[lanes_below(bh, at_h)] = j;
+    if (j >= a.n_keep && stays) movers[lanes_below(bm, at_m)] = j;
+    at_h += __popcll(bh), at_m += __popcll(bm);
   }
-  if (threadIdx.x == 0) counts[sel] = n_holes;
+  if (!move) {
+    if (threadIdx.x == 0) counts[sel] = n;
+    return;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (int h = sel * m.per; h < (sel + 1) * m.per; ++h) {
+    move_rows(m, h, n, holes, movers, threadIdx.x, kSelThreads);
+    move_book(m, h, sel, n, holes, movers, threadIdx.x, kSelThreads);
+  }
 }
 
-// What moves with a row: planes of whole words, one run of words per row.
-constexpr int kMaxPlanes = 6;
-struct Planes {
-  uint16_t* base[kMaxPlanes];
-  int64_t stride_h[kMaxPlanes];     // in 2-byte units
-  int words[kMaxPlanes];            // 2-byte units of a row
-  int n_heads_planes, n;            // the first planes are of every head, the rest of a selection head
+// ------------------------------------------------------------------------------------------
+// More rows: slices of them, a work-group each, in four launches.
+//   count    ranks (written out: the rows' t lies 12 bytes apart) and the slice's counts of the top bits
+//   gather   the bin that the threshold lies in; rows above and below it are decided, rows in it are
+//            appended to the selection head's candidates (their order does not matter: what is kept is a cut
+//            through the order by rank, then row)
+//   resolve  a work-group per selection head: the cut, and where every slice's holes and movers begin
+//   place    the lists
+// ------------------------------------------------------------------------------------------
+constexpr int kSlice = 4096, kMaxSlices = 512, kItemsOfSlice = kSlice / kSelThreads;
+
+struct Slices {
+  int n, rows;                // slices, rows of one (a multiple of kSlice)
+  uint32_t* ranks;            // [Hsel][Nk]
+  int32_t* hist;              // [Hsel][n][kTopBins]
+  int32_t* candidates;        // [Hsel][Nk]: rows
+  int32_t* decided;           // [Hsel][n][2]: holes and movers of the gather, then where a slice's begin
+  int32_t* head;              // [Hsel][4]: candidates so far; bin, rows wanted of it, rows in it
+  uint32_t* cut;              // [Hsel][2]: rank and row: rows of a higher rank stay, of this rank up to this row
 };
 
-__global__ __launch_bounds__(256) void evict_move_kernel(Planes p, int per, int room, const int32_t* __restrict__ counts,
-                                                         const int32_t* __restrict__ lists, int32_t* __restrict__ idx,
-                                                         int64_t idx_stride_h) {
-  const int lane = threadIdx.x & 63;
-  const int h = blockIdx.y, sel = h / per;
-  const bool first = h == sel * per;
-  const int n = counts[sel];
-  const int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
-  for (int i = blockIdx.x * 4 + (threadIdx.x >> 6); i < n; i += gridDim.x * 4) {
-    const int64_t to = holes[i], from = holes[room + i];
-    for (int q = 0; q < p.n; ++q) {
-      if (q >= p.n_heads_planes && !first) break;
-      uint16_t* base = p.base[q] + (q < p.n_heads_planes ? h : sel) * p.stride_h[q];
-      for (int w = lane; w < p.words[q]; w += 64) base[to * p.words[q] + w] = base[from * p.words[q] + w];
+__global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slices s) {
+  __shared__ int hist[kTopBins];
+  const int sel = blockIdx.y, slice = blockIdx.x;
+  const HeadRanks rank(a, sel);
+  for (int b = threadIdx.x; b < kTopBins; b += kSelThreads) hist[b] = 0;
+  if (slice == 0 && threadIdx.x == 0) s.head[sel * 4] = 0;
+  __syncthreads();
+  const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
+  uint32_t* out = s.ranks + static_cast<int64_t>(sel) * a.Nk;
+  for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice) {
+    uint32_t key[kItemsOfSlice];
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i)
+      key[i] = rank.of(static_cast<int>(min(r0 + i * kSelThreads + threadIdx.x, static_cast<int64_t>(a.Nk) - 1)));
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) {
+      const int64_t j = r0 + i * kSelThreads + threadIdx.x;
+      if (j < end) out[j] = key[i];
+      vote(hist, key[i] >> (32 - kTopBits), j < end);
     }
-    if (idx != nullptr && first && lane == 0) idx[sel * idx_stride_h + to] = static_cast<int32_t>(from);
+  }
+  __syncthreads();
+  int32_t* to = s.hist + (static_cast<int64_t>(sel) * s.n + slice) * kTopBins;
+  for (int b = threadIdx.x; b < kTopBins; b += kSelThreads) to[b] = hist[b];
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slices s) {
+  __shared__ int hist[kTopBins];
+  __shared__ int s_wave[kSelWaves], s_found[3], s_count[2], s_at;
+  const int sel = blockIdx.y, slice = blockIdx.x, lane = threadIdx.x & 63;
+  const int32_t* all = s.hist + static_cast<int64_t>(sel) * s.n * kTopBins;
+  {
+    int c0 = 0, c1 = 0;
+    for (int k = 0; k < s.n; ++k) {
+      c0 += all[static_cast<int64_t>(k) * kTopBins + threadIdx.x];
+      c1 += all[static_cast<int64_t>(k) * kTopBins + kSelThreads + threadIdx.x];
+    }
+    hist[threadIdx.x] = c0, hist[kSelThreads + threadIdx.x] = c1;
+  }
+  if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
+  __syncthreads();
+  find_bin<kTopBins>(hist, a.n_keep, s_wave, s_found);
+  const uint32_t bin = s_found[0];
+  if (threadIdx.x == 0) {
+    s_at = atomicAdd(&s.head[sel * 4], all[static_cast<int64_t>(slice) * kTopBins + bin]);
+    if (slice == 0)
+      for (int k = 0; k < 3; ++k) s.head[sel * 4 + 1 + k] = s_found[k];
+  }
+  __syncthreads();
+  const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
+  const uint32_t* in = s.ranks + static_cast<int64_t>(sel) * a.Nk;
+  int32_t* out = s.candidates + static_cast<int64_t>(sel) * a.Nk;
+  int holes = 0, movers = 0;
+  for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice) {
+    uint32_t key[kItemsOfSlice];
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = in[min(r0 + i * kSelThreads + threadIdx.x, end - 1)] >> (32 - kTopBits);
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) {
+      const int64_t j = r0 + i * kSelThreads + threadIdx.x;
+      holes += __popcll(__ballot(j < end && j < a.n_keep && key[i] < bin));
+      movers += __popcll(__ballot(j < end && j >= a.n_keep && key[i] > bin));
+      const bool open = j < end && key[i] == bin;
+      const uint64_t b = __ballot(open);
+      if (b != 0) {      // the wave's place among the slice's candidates
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s_at, __popcll(b));
+        at = __builtin_amdgcn_readfirstlane(at);
+        if (open) out[lanes_below(b, at)] = static_cast<int32_t>(j);
+      }
+    }
+  }
+  if (lane == 0) {
+    atomicAdd(&s_count[0], holes);
+    atomicAdd(&s_count[1], movers);
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) s.decided[(static_cast<int64_t>(sel) * s.n + slice) * 2 + threadIdx.x] = s_count[threadIdx.x];
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Slices s, int32_t* __restrict__ counts) {
+  __shared__ int hist[2048], s_wave[kSelWaves], s_found[3], s_holes[kMaxSlices], s_movers[kMaxSlices];
+  const int sel = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t* ranks = s.ranks + static_cast<int64_t>(sel) * a.Nk;
+  const int32_t* cand = s.candidates + static_cast<int64_t>(sel) * a.Nk;
+  int32_t* decided = s.decided + static_cast<int64_t>(sel) * s.n * 2;
+  const uint32_t bin = s.head[sel * 4 + 1];
+  int left = s.head[sel * 4 + 2];
+  const int n = s.head[sel * 4 + 3];
+  for (int k = threadIdx.x; k < s.n; k += kSelThreads) s_holes[k] = decided[k * 2], s_movers[k] = decided[k * 2 + 1];
+  // the candidates' order: the other 21 bits of the rank, then 30 of the row, lower rows first
+  constexpr int kRest = 32 - kTopBits;
+  auto order = [&](int row) {
+    return static_cast<uint64_t>(ranks[row] & ((1u << kRest) - 1)) << 30 | static_cast<uint32_t>((1 << 30) - 1 - row);
+  };
+  uint64_t prefix = 0;
+  bool whole = n == left;
+  // 11, 10 and three times 10 bits
+  for (int shift = kRest + 30; !whole && shift > 0;) {
+    const int bits = shift == kRest + 30 ? 11 : 10, upper = shift;
+    shift -= bits;
+    __syncthreads();
+    for (int b = threadIdx.x; b < 2048; b += kSelThreads) hist[b] = 0;
+    __syncthreads();
+    for (int c = threadIdx.x; c - lane < n; c += kSelThreads) {
+      const uint64_t o = order(cand[min(c, n - 1)]);
+      vote(hist, static_cast<int>(o >> shift) & ((1 << bits) - 1), c < n && (o ^ prefix) >> upper == 0);
+    }
+    __syncthreads();
+    find_bin<2048>(hist, left, s_wave, s_found);
+    prefix |= static_cast<uint64_t>(s_found[0]) << shift;
+    left = s_found[1];
+    whole = s_found[2] == left;
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < n; c += kSelThreads) {
+    const int row = cand[c];
+    const bool stays = order(row) >= prefix;
+    if (row < a.n_keep && !stays) atomicAdd(&s_holes[row / s.rows], 1);
+    if (row >= a.n_keep && stays) atomicAdd(&s_movers[row / s.rows], 1);
+  }
+  __syncthreads();
+  // where the slices' holes and movers begin: a wave each, 64 slices at a time
+  if (wave < 2) {
+    const int* c = wave == 0 ? s_holes : s_movers;
+    int before = 0;
+    for (int k0 = 0; k0 < s.n; k0 += 64) {
+      const int v = k0 + lane < s.n ? c[k0 + lane] : 0, upto = wave_prefix_sum(v);
+      if (k0 + lane < s.n) decided[(k0 + lane) * 2 + wave] = before + upto - v;
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (wave == 0 && lane == 0) {
+      counts[sel] = before;
+      s.cut[sel * 2] = bin << kRest | static_cast<uint32_t>(prefix >> 30);
+      s.cut[sel * 2 + 1] = (1u << 30) - 1 - static_cast<uint32_t>(prefix & ((1u << 30) - 1));
+    }
   }
 }
 
-constexpr size_t kWsAlign = 256;
-int list_room(int Nk, int n_keep) { return std::min(Nk - n_keep, n_keep); }
+__global__ __launch_bounds__(kSelThreads) void evict_place_kernel(Ranks a, Slices s, int room, int32_t* __restrict__ lists,
+                                                                  int32_t* __restrict__ idx, int64_t idx_stride_h) {
+  __shared__ int s_wave[2][2][kSelWaves];
+  const int sel = blockIdx.y, slice = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t* ranks = s.ranks + static_cast<int64_t>(sel) * a.Nk;
+  const uint32_t cut = s.cut[sel * 2], cut_row = s.cut[sel * 2 + 1];
+  const int32_t* begin = s.decided + (static_cast<int64_t>(sel) * s.n + slice) * 2;
+  int at_h = begin[0], at_m = begin[1];
+  int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
+  int32_t* movers = holes + room;
+  const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
+  int turn = 0;
+  for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice, turn ^= 1) {
+    const int64_t j0 = r0 + wave * 64 * kItemsOfSlice + lane;
+    uint32_t key[kItemsOfSlice];
+    uint64_t bh[kItemsOfSlice], bm[kItemsOfSlice];
+    int n_holes = 0, n_movers = 0;
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = ranks[min(j0 + i * 64, static_cast<int64_t>(a.Nk) - 1)];
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) {
+      const int64_t j = j0 + i * 64;
+      const bool stays = j < end && (key[i] > cut || (key[i] == cut && j <= cut_row));
+      bh[i] = __ballot(j < end && j < a.n_keep && !stays), bm[i] = __ballot(j >= a.n_keep && stays);
+      n_holes += __popcll(bh[i]), n_movers += __popcll(bm[i]);
+      if (idx != nullptr && stays && j < a.n_keep) idx[sel * idx_stride_h + j] = static_cast<int32_t>(j);
+    }
+    if (lane == 0) s_wave[turn][0][wave] = n_holes, s_wave[turn][1][wave] = n_movers;
+    __syncthreads();
+    int mine_h = at_h, mine_m = at_m;
+    for (int w = 0; w < kSelWaves; ++w) {
+      const int h = s_wave[turn][0][w], m = s_wave[turn][1][w];
+      if (w < wave) mine_h += h, mine_m += m;
+      at_h += h, at_m += m;
+    }
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) {
+      const int j = static_cast<int>(j0) + i * 64;
+      if (bh[i] >> lane & 1) holes[lanes_below(bh[i], mine_h)] = j;
+      if (bm[i] >> lane & 1) movers[lanes_below(bm[i], mine_m)] = j;
+      mine_h += __popcll(bh[i]), mine_m += __popcll(bm[i]);
+    }
+  }
+}
 
-int evict(const char* who, Planes p, int H, int32_t* pos, int64_t pos_stride_h, float* weights, int64_t w_stride_h, int Hsel,
-          int Nk, int n_keep, int n_anchor, int recent_t, int32_t* idx_out, int64_t idx_stride_h, void* ws, size_t ws_bytes,
-          void* stream) {
+// ------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------
+constexpr size_t kWsAlign = 256;
+constexpr int kMaxInRegisters = 32 * kSelThreads;
+constexpr int64_t kMoveWithSelect = 64 << 10;     // bytes that a work-group of the one-launch form moves at most
+
+// What a call keeps in its workspace; `base` may be NULL where only the size is asked for.
+struct EvictPlan {
+  int room, n_slices, slice_rows;       // room: of a list; n_slices 0: one work-group per selection head
+  int32_t *counts, *lists;
+  Slices s;
+  size_t bytes;
+  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), s() {
+    size_t at = 0;
+    auto take = [&](size_t n) {
+      void* p = static_cast<uint8_t*>(base) + at;
+      at += align_up(n, kWsAlign);
+      return p;
+    };
+    const size_t heads = Hsel;
+    counts = static_cast<int32_t*>(take(heads * 4));
+    lists = static_cast<int32_t*>(take(heads * 2 * room * 4));
+    if (Nk > kMaxInRegisters) {
+      slice_rows = kSlice * ceil_div(ceil_div(Nk, kSlice), kMaxSlices);
+      n_slices = ceil_div(Nk, slice_rows);
+      s = {n_slices, slice_rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+      s.ranks = static_cast<uint32_t*>(take(heads * Nk * 4));
+      s.hist = static_cast<int32_t*>(take(heads * n_slices * kTopBins * 4));
+      s.candidates = static_cast<int32_t*>(take(heads * Nk * 4));
+      s.decided = static_cast<int32_t*>(take(heads * n_slices * 8));
+      s.head = static_cast<int32_t*>(take(heads * 16));
+      s.cut = static_cast<uint32_t*>(take(heads * 8));
+    }
+    bytes = at;
+  }
+};
+
+int evict(const char* who, Moves m, int64_t row_bytes, int H, int32_t* pos, int64_t pos_stride_h, float* weights,
+          int64_t w_stride_h, int Hsel, int Nk, int n_keep, int n_anchor, int recent_t, int32_t* idx_out, int64_t idx_stride_h,
+          void* ws, size_t ws_bytes, void* stream) {
   PC_REQUIRE(H > 0 && Hsel > 0 && Hsel <= H && H % Hsel == 0, PC_ERR_SHAPE, "%s: %d selection heads for %d heads", who, Hsel, H);
   PC_REQUIRE(H <= 65535, PC_ERR_SHAPE, "%s: %d heads in one call", who, H);
-  PC_REQUIRE(Nk >= 0 && Nk <= (1 << 30), PC_ERR_SHAPE, "%s: Nk=%d", who, Nk);
+  PC_REQUIRE(Nk >= 0 && Nk <= kMaxRows, PC_ERR_SHAPE, "%s: Nk=%d", who, Nk);
   PC_REQUIRE(n_keep >= 0 && n_anchor >= 0 && recent_t >= 0 && n_anchor <= n_keep, PC_ERR_BUDGET,
              "%s: n_keep=%d n_anchor=%d recent_t=%d", who, n_keep, n_anchor, recent_t);
   PC_REQUIRE(weights, PC_ERR_NULL, "%s: weights is NULL", who);
@@ -168,27 +530,38 @@ int evict(const char* who, Planes p, int H, int32_t* pos, int64_t pos_stride_h, 
     return PC_OK;
   }
   if (n_keep == 0) return PC_OK;
-  const int room = list_room(Nk, n_keep);
-  const size_t lists_at = align_up(static_cast<size_t>(Hsel) * 4, kWsAlign);
-  const size_t bytes = lists_at + static_cast<size_t>(Hsel) * 2 * room * 4;
-  PC_REQUIRE(ws && ws_bytes >= bytes && reinterpret_cast<uintptr_t>(ws) % 16 == 0, PC_ERR_WORKSPACE,
-             "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, bytes, ws_bytes);
-  auto plane = [&](void* base, int64_t stride_bytes, int row_bytes) {
-    p.base[p.n] = static_cast<uint16_t*>(base);
-    p.stride_h[p.n] = stride_bytes / 2;
-    p.words[p.n++] = row_bytes / 2;
-  };
-  p.n_heads_planes = p.n;
-  if (pos) plane(pos, pos_stride_h * 4, 12);
-  plane(weights, w_stride_h * 4, 4);
+  const EvictPlan plan(Hsel, Nk, n_keep, ws);
+  PC_REQUIRE(ws && ws_bytes >= plan.bytes && reinterpret_cast<uintptr_t>(ws) % 16 == 0, PC_ERR_WORKSPACE,
+             "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, plan.bytes, ws_bytes);
+  m.pos = pos, m.weights = weights, m.pos_stride_h = pos_stride_h, m.w_stride_h = w_stride_h;
+  m.idx = idx_out, m.idx_stride_h = idx_stride_h, m.per = H / Hsel;
+  const int64_t units = static_cast<int64_t>(plan.room) * m.by_both.d;
+  PC_REQUIRE(units <= INT_MAX - (1 << 22), PC_ERR_SHAPE, "%s: %d rows may move in one call", who, plan.room);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto* counts = static_cast<int32_t*>(ws);
-  auto* lists = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + lists_at);
   const Ranks a = {weights, pos, w_stride_h, pos_stride_h, Nk, n_keep, n_anchor, recent_t};
-  evict_select_kernel<<<Hsel, kSelThreads, 0, s>>>(a, room, counts, lists, idx_out, idx_stride_h);
-  PC_CHECK_LAUNCH(who);
-  evict_move_kernel<<<dim3(std::min(ceil_div(room, 4), 1024), H), 256, 0, s>>>(p, H / Hsel, room, counts, lists, idx_out,
-                                                                             idx_stride_h);
+  if (plan.n_slices == 0) {
+    const int move = plan.room * row_bytes * m.per <= kMoveWithSelect;
+    const auto kernel = Nk <= 4 * kSelThreads    ? evict_select_kernel<4>
+                        : Nk <= 8 * kSelThreads  ? evict_select_kernel<8>
+                        : Nk <= 16 * kSelThreads ? evict_select_kernel<16>
+                                                 : evict_select_kernel<32>;
+    kernel<<<Hsel, kSelThreads, 0, s>>>(a, plan.room, plan.counts, plan.lists, m, move);
+    PC_CHECK_LAUNCH(who);
+    if (move) return PC_OK;
+  } else {
+    const dim3 grid(plan.n_slices, Hsel);
+    evict_count_kernel<<<grid, kSelThreads, 0, s>>>(a, plan.s);
+    PC_CHECK_LAUNCH(who);
+    evict_gather_kernel<<<grid, kSelThreads, 0, s>>>(a, plan.s);
+    PC_CHECK_LAUNCH(who);
+    evict_resolve_kernel<<<Hsel, kSelThreads, 0, s>>>(a, plan.s, plan.counts);
+    PC_CHECK_LAUNCH(who);
+    evict_place_kernel<<<grid, kSelThreads, 0, s>>>(a, plan.s, plan.room, plan.lists, idx_out, idx_stride_h);
+    PC_CHECK_LAUNCH(who);
+  }
+  const int book = std::min(ceil_div(plan.room, 256), 64);
+  const int rows = static_cast<int>(std::min<int64_t>((units + 1023) / 1024, 4096));
+  evict_move_kernel<<<dim3(book + rows, H), 256, 0, s>>>(m, book, plan.room, plan.counts, plan.lists);
   PC_CHECK_LAUNCH(who);
   return PC_OK;
 }
@@ -199,8 +572,8 @@ int evict(const char* who, Planes p, int H, int32_t* pos, int64_t pos_stride_h, 
 using namespace pc;
 
 extern "C" size_t pc_evict_workspace_bytes(int Hsel, int Nk, int n_keep) {
-  if (Hsel <= 0 || Nk <= 0 || n_keep <= 0 || n_keep >= Nk) return 0;
-  return align_up(static_cast<size_t>(Hsel) * 4, kWsAlign) + static_cast<size_t>(Hsel) * 2 * list_room(Nk, n_keep) * 4;
+  if (Hsel <= 0 || Nk <= 0 || n_keep <= 0 || n_keep >= Nk || Nk > kMaxRows) return 0;
+  return EvictPlan(Hsel, Nk, n_keep, nullptr).bytes;
 }
 
 extern "C" int pc_evict(void* K, void* V, int dtype, int H, int D, int64_t k_stride_h, int64_t v_stride_h, int32_t* pos,
@@ -216,12 +589,10 @@ extern "C" int pc_evict(void* K, void* V, int dtype, int H, int D, int64_t k_str
   const int elt = dtype == PC_BF16 ? 2 : 4;
   PC_REQUIRE((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | k_stride_h * elt | v_stride_h * elt) % 16 == 0,
              PC_ERR_SHAPE, "%s: K, V and their head strides must be 16-byte aligned", who);
-  Planes p = {};
-  p.base[0] = static_cast<uint16_t*>(K), p.base[1] = static_cast<uint16_t*>(V);
-  p.stride_h[0] = k_stride_h * elt / 2, p.stride_h[1] = v_stride_h * elt / 2;
-  p.words[0] = p.words[1] = D * elt / 2;
-  p.n = 2;
-  return evict(who, p, H, pos, pos_stride_h, weights, weights_stride_h, Hsel, Nk, n_keep, n_anchor, recent_t, idx_out,
+  const int pieces = D * elt / 16;
+  const Moves m = {{static_cast<u32x4*>(K), static_cast<u32x4*>(V)}, {k_stride_h * elt / 16, v_stride_h * elt / 16}, Divisor(pieces),
+                   Divisor(2 * pieces)};
+  return evict(who, m, 32ll * pieces, H, pos, pos_stride_h, weights, weights_stride_h, Hsel, Nk, n_keep, n_anchor, recent_t, idx_out,
                idx_stride_h, ws, ws_bytes, stream);
 }
 
@@ -232,14 +603,10 @@ extern "C" int pc_q4_evict(const pc_q4_cache* cache, int H, int D, int32_t* pos,
   PC_REQUIRE(D == 64 || D == 128, PC_ERR_UNSUPPORTED, "%s: needs D = 64 or 128, got %d", who, D);
   if (int rc = check_q4_cache(cache, D, who)) return rc;
   if (int rc = check_q4_span(cache, H, 0, Nk, D, who)) return rc;
-  Planes p = {};
-  uint8_t* const planes[4] = {cache->k_codes, cache->v_codes, cache->k_scales, cache->v_scales};
-  for (int i = 0; i < 4; ++i) {
-    p.base[i] = reinterpret_cast<uint16_t*>(planes[i]);
-    p.stride_h[i] = (i < 2 ? cache->code_stride_h : cache->scale_stride_h) / 2;
-    p.words[i] = (i < 2 ? D / 2 : D / 32) / 2;
-  }
-  p.n = 4;
-  return evict(who, p, H, pos, pos_stride_h, weights, weights_stride_h, Hsel, Nk, n_keep, n_anchor, recent_t, idx_out,
+  const int pieces = D / 32;
+  const Moves m = {{reinterpret_cast<u32x4*>(cache->k_codes), reinterpret_cast<u32x4*>(cache->v_codes)},
+                   {cache->code_stride_h / 16, cache->code_stride_h / 16}, Divisor(pieces), Divisor(2 * pieces),
+                   {cache->k_scales, cache->v_scales}, cache->scale_stride_h, D / 32};
+  return evict(who, m, 32ll * pieces, H, pos, pos_stride_h, weights, weights_stride_h, Hsel, Nk, n_keep, n_anchor, recent_t, idx_out,
                idx_stride_h, ws, ws_bytes, stream);
 }

@@ -15,6 +15,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 
 constexpr int kQ4MinExp = -120, kQ4MaxExp = 125;
 constexpr int kQ4BadScale = 255;
+constexpr int kMaxRows = 1 << 30;      // of a call over a cache
 
 // A cache in 4 bits as the kernels see it (pc_q4_cache with the heads' strides in bytes).
 struct Q4Rows {

@@ -629,7 +629,7 @@ extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int 
 
 namespace {
 bool sizes_ok(int Hq, int Hkv, int Nq, int Nk) {
-  return Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq >= 1 && Nk >= 1 && Nk <= (1 << 30) && static_cast<int64_t>(Hq) * Nq <= INT_MAX / 2;
+  return Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Nq >= 1 && Nk >= 1 && Nk <= kMaxRows && static_cast<int64_t>(Hq) * Nq <= INT_MAX / 2;
 }
 }  // namespace
 
