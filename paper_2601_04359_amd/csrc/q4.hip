@@ -38,8 +38,8 @@ __global__ __launch_bounds__(kCopyThreads) void q4_store_kernel(const T* __restr
                                                                 Q4Rows cache, int row0, int n_units, Book book) {
   constexpr int kLanes = D / 8;      // lanes of a row
   const int n = at.by_n.d;
-  const int idx = blockIdx.x * kCopyThreads + threadIdx.x;
-  const int unit = idx / kLanes, part = idx % kLanes;
+  const int64_t idx = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x;
+  const int unit = static_cast<int>(idx / kLanes), part = static_cast<int>(idx % kLanes);
   if (unit < n_units) {
     int rest = at.by_n.of(unit);
     const int i = unit - rest * n;
@@ -99,9 +99,9 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
                                                                int row0, int first_unit, int n_units) {
   constexpr int kLanes = D / 8;
   const int n = at.by_n.d;
-  const int idx = blockIdx.x * kCopyThreads + threadIdx.x;
-  int unit = idx / kLanes;
-  const int part = idx % kLanes;
+  const int64_t idx = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x;
+  int unit = static_cast<int>(idx / kLanes);
+  const int part = static_cast<int>(idx % kLanes);
   if (unit >= n_units) return;
   unit += first_unit;
   const int rest = at.by_n.of(unit);
@@ -139,6 +139,9 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
 // ------------------------------------------------------------------------------------------
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kStep = 32;                   // keys of a wave's step
+constexpr int kMaxShares = 128;             // of the keys
+constexpr int kLogitRows = 8;               // per KV head: up to here the weights come from logits that are kept
+constexpr int kMaxJoinRows = 64;            // of a selection head, at a time
 
 struct AttnArgs {
   Q4Rows cache;
@@ -151,6 +154,7 @@ struct AttnArgs {
   float2* part_ml;
   float* lse;                               // natural logarithm, or NULL
   float* lse2;                              // base 2, for the weights, or NULL
+  float* logits;                            // [rows_all][whole steps] for the weights of few rows, or NULL
   int64_t rows_all;
 };
 
@@ -305,6 +309,11 @@ __global__ __launch_bounds__(kThreads, 1) void q4_attn_kernel(const T* __restric
           for (int i = 0; i < 4; ++i)
             if (k0 + t * 16 + g * 4 + i >= a.Nk) s[t][i] = -INFINITY;
       }
+      if (kRT == 1 && a.logits != nullptr && r < n_rows) {
+        float* to = a.logits + (static_cast<int64_t>(kvh) * n_rows + r) * (static_cast<int64_t>(n_steps) * kStep) + k0 + g * 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4*>(to + t * 16) = s[t];
+      }
       float mx = s[0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
@@ -401,103 +410,195 @@ __global__ __launch_bounds__(kThreads, 1) void q4_attn_kernel(const T* __restric
   }
 }
 
-// The shares of a row: a work-group of 256 threads per row, the shares dealt to its 1024 / D groups of threads.
+// ------------------------------------------------------------------------------------------
+// What follows the attention of few rows, in one launch: a work-group per row that joins its key shares, and
+// work-groups that form the weights of 1,024 keys each from the logits that the attention left (8 R bytes per key there
+// and back for R rows, where forming them again reads 68 and multiplies).  Each work-group joins the shares'
+// (reference, sum) pairs for itself.  Bound: two memory latencies.
+// ------------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 256;
+
+struct JoinArgs {
+  int n_splits, rows, Hkv, Hsel, Nk;        // rows per KV head
+  int row_blocks;                           // work-groups that join rows: all of them, or 0
+  Divisor by_blocks;                        // key blocks of a selection head
+  int64_t logit_stride, w_stride_h;
+  float c, decay;
+  float* weights;
+};
+
+// Reference and sum of a row over its shares, by one wave: in every lane.
+__device__ __forceinline__ float2 join_ml(const float2* __restrict__ ml, int64_t stride, int n, int lane) {
+  float M = kNoRef, l = 0.f;
+  float2 x[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    x[k] = lane + k * 64 < n ? ml[(lane + k * 64) * stride] : make_float2(kNoRef, 0.f);
+    M = fmaxf(M, x[k].x);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+#pragma unroll
+  for (int k = 0; k < 2; ++k) l += __builtin_amdgcn_exp2f(x[k].x - M) * x[k].y;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d);
+  return make_float2(M, l);
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q4_merge_kernel(T* __restrict__ O, int n_splits, AttnArgs a) {
-  constexpr int kUnits = D / 4, kLanes = 256 / kUnits;
+__global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O, AttnArgs a, JoinArgs j) {
+  constexpr int kUnits = D / 4, kLanes = kJoinThreads / kUnits;
   __shared__ f32x4 s_o[kLanes][kUnits];
-  __shared__ float s_l[kLanes];
-  const int64_t at = blockIdx.x;
-  const int u = threadIdx.x % kUnits, part = threadIdx.x / kUnits;
-  float M = kNoRef;
-  for (int s = 0; s < n_splits; ++s) M = fmaxf(M, a.part_ml[s * a.rows_all + at].x);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float lt = 0.f;
-  for (int s = part; s < n_splits; s += kLanes) {
-    const int64_t at_s = s * a.rows_all + at;
-    const float2 ml = a.part_ml[at_s];
-    const float wt = __builtin_amdgcn_exp2f(ml.x - M);
-    lt += wt * ml.y;
-    acc += wt * *reinterpret_cast<const f32x4*>(a.part_o + at_s * D + u * 4);
+  __shared__ float s_w[kMaxShares], s_e2[kMaxJoinRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (static_cast<int>(blockIdx.x) < j.row_blocks) {
+    const int64_t at = blockIdx.x;
+    const int u = threadIdx.x % kUnits, part = threadIdx.x / kUnits;
+    const float2 row = join_ml(a.part_ml + at, a.rows_all, j.n_splits, lane);
+    for (int s = threadIdx.x; s < j.n_splits; s += kJoinThreads) s_w[s] = __builtin_amdgcn_exp2f(a.part_ml[s * a.rows_all + at].x - row.x);
+    __syncthreads();
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const float* from = a.part_o + at * D + u * 4;
+    for (int s0 = part; s0 < j.n_splits; s0 += 8 * kLanes) {
+      f32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const f32x4*>(from + min(s0 + k * kLanes, j.n_splits - 1) * a.rows_all * D);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (s0 + k * kLanes < j.n_splits) acc += s_w[s0 + k * kLanes] * v[k];
+    }
+    s_o[part][u] = acc;
+    __syncthreads();
+    if (part != 0) return;
+#pragma unroll
+    for (int p = 1; p < kLanes; ++p) acc += s_o[p][u];
+    const float inv = 1.f / row.y;
+    const int head = a.by_nq.of(static_cast<int>(at));
+    T* to = O + head * a.o_stride_h + (at - static_cast<int64_t>(head) * a.by_nq.d) * D + u * 4;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    } else {
+      store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+    }
+    if (u == 0) {
+      const float e2 = row.x + log2f(row.y);
+      if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
+      if (a.lse2 != nullptr) a.lse2[at] = e2;
+    }
+    return;
   }
-  s_o[part][u] = acc;
-  if (u == 0) s_l[part] = lt;
-  __syncthreads();
-  if (part != 0) return;
-  lt = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < kLanes; ++p) acc += s_o[p][u], lt += s_l[p];
-  const float inv = 1.f / lt;
-  const int head = a.by_nq.of(static_cast<int>(at));
-  T* to = O + head * a.o_stride_h + (at - static_cast<int64_t>(head) * a.by_nq.d) * D + u * 4;
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-  } else {
-    store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+  // weights
+  const int unit = blockIdx.x - j.row_blocks;
+  const int sel = j.by_blocks.of(unit), block = unit - sel * j.by_blocks.d;
+  const int per = j.Hkv / j.Hsel * j.rows;          // rows of the selection head
+  const int64_t row0 = static_cast<int64_t>(sel) * per;
+  const int k0 = block * (4 * kJoinThreads) + threadIdx.x * 4;
+  const bool mine = k0 < j.Nk;
+  const float* from = a.logits + row0 * j.logit_stride + (mine ? k0 : 0);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < per; r0 += kMaxJoinRows) {
+    const int n = min(per - r0, kMaxJoinRows);
+    __syncthreads();
+    for (int r = wave; r < n; r += kJoinThreads / 64) {
+      float e2;
+      if (j.n_splits > 1) {
+        const float2 row = join_ml(a.part_ml + row0 + r0 + r, a.rows_all, j.n_splits, lane);
+        e2 = row.x + log2f(row.y);
+      } else {
+        e2 = a.lse2[row0 + r0 + r];
+      }
+      if (lane == 0) s_e2[r] = e2;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int r = 0; r < n; ++r) {
+      const f32x4 s = *reinterpret_cast<const f32x4*>(from + (r0 + r) * j.logit_stride);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(s[i], j.c, -s_e2[r]));
+    }
   }
-  if (u == 0) {
-    const float e2 = M + log2f(lt);
-    if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
-    if (a.lse2 != nullptr) a.lse2[at] = e2;
-  }
+  float* w = j.weights + sel * j.w_stride_h + k0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (k0 + i < j.Nk) w[i] = j.decay == 0.f ? sum[i] : fmaf(j.decay, w[i], sum[i]);
 }
 
 // ------------------------------------------------------------------------------------------
-// The weights: weights[j] = decay * weights[j] + sum over the query rows of exp2(c s - lse2), the scores formed once
-// more from the keys' codes.  A wave owns 16 keys, as the second operand (a lane sums its key's column over the
-// queries it sees), and walks the query rows; with one sum for all heads it walks the KV heads as well.  The
-// order of the sum is fixed.
+// The weights of many rows: weights[j] = decay * weights[j] + sum over the query rows of exp2(c s - lse2), the scores
+// formed once more from the keys' codes.  A work-group owns 64 keys, which every wave holds as the second operand (a lane
+// sums its keys' columns over the queries it sees); the waves deal the query rows in tiles of 16 and are
+// added up in their order.  With one sum for all heads a work-group walks the KV heads as well.
 // ------------------------------------------------------------------------------------------
 struct WeighArgs {
   Q4Rows cache;
   int rep, Nk, Hkv, Hsel;
   Divisor by_nq, by_blocks;                 // rows per head, key blocks of a selection head
   int64_t q_stride_h, w_stride_h;
-  float c, decay;
-  const float* lse2;
+  float c, decay, lse_mul;                  // lse_mul: brings lse to base 2
+  const float* lse;
   float* weights;
 };
+constexpr int kWeighTiles = 4, kWeighKeys = 16 * kWeighTiles;
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q4_weigh_kernel(const T* __restrict__ Q, WeighArgs a) {
+__global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict__ Q, WeighArgs a) {
+  __shared__ float s_sum[kWaves][kWeighKeys];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int sel = a.by_blocks.of(blockIdx.x), block = blockIdx.x - sel * a.by_blocks.d;
-  const int k0 = (block * 4 + wave) * 16;
-  if (k0 >= a.Nk) return;
+  const int unit = xcd_contiguous_index(blockIdx.x, gridDim.x);
+  const int sel = a.by_blocks.of(unit), block = unit - sel * a.by_blocks.d;
+  const int k0 = block * kWeighKeys;
   const int n_rows = a.rep * a.by_nq.d, per = a.Hkv / a.Hsel;
-  const int key = min(k0 + r, a.Nk - 1);
-  float sum = 0.f;
+  float sum[kWeighTiles] = {};
   for (int kvh = sel * per; kvh < (sel + 1) * per; ++kvh) {
-    KeyCodes<D> raw;
-    raw.load(a.cache.k_codes + kvh * a.cache.code_stride_h, a.cache.k_scales + kvh * a.cache.scale_stride_h, key, g);
-    bf16x8 kf[D / 32];
+    bf16x8 kf[kWeighTiles][D / 32];
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b) kf[b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
-    for (int row0 = 0; row0 < n_rows; row0 += 16) {
+    for (int t = 0; t < kWeighTiles; ++t) {
+      KeyCodes<D> raw;
+      raw.load(a.cache.k_codes + kvh * a.cache.code_stride_h, a.cache.k_scales + kvh * a.cache.scale_stride_h,
+               min(k0 + t * 16 + r, a.Nk - 1), g);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b) kf[t][b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
+    }
+    const float* lse = a.lse + static_cast<int64_t>(kvh) * n_rows;
+    for (int row0 = wave * 16; row0 < n_rows; row0 += 16 * kWaves) {
       const int rho = min(row0 + r, n_rows - 1);
       const int head = a.by_nq.of(rho);
       QueryFrags<T, D> q;
       q.load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      float e2[4];
 #pragma unroll
-      for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.f[b][p], kf[b], s, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 4; ++i) {     // a row that is not there has probability 0
         const int row = row0 + g * 4 + i;
-        const float e2 = a.lse2[static_cast<int64_t>(kvh) * n_rows + min(row, n_rows - 1)];
-        if (row < n_rows) sum += __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -e2));
+        const float x = lse[min(row, n_rows - 1)] * a.lse_mul;
+        e2[i] = row < n_rows ? x : INFINITY;
+      }
+#pragma unroll
+      for (int t = 0; t < kWeighTiles; ++t) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
+#pragma unroll
+          for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.f[b][p], kf[t][b], s, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[t] += __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -e2[i]));
       }
     }
   }
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  if (g == 0 && k0 + r < a.Nk) {
-    float* w = a.weights + sel * a.w_stride_h + k0 + r;
-    *w = a.decay == 0.f ? sum : fmaf(a.decay, *w, sum);
+#pragma unroll
+  for (int t = 0; t < kWeighTiles; ++t) {
+    sum[t] += __shfl_xor(sum[t], 16);
+    sum[t] += __shfl_xor(sum[t], 32);
+    if (g == 0) s_sum[wave][t * 16 + r] = sum[t];
+  }
+  __syncthreads();
+  if (threadIdx.x < kWeighKeys && k0 + static_cast<int>(threadIdx.x) < a.Nk) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += s_sum[w][threadIdx.x];
+    float* w = a.weights + sel * a.w_stride_h + k0 + threadIdx.x;
+    *w = a.decay == 0.f ? x : fmaf(a.decay, *w, x);
   }
 }
 
@@ -505,34 +606,56 @@ __global__ __launch_bounds__(256) void q4_weigh_kernel(const T* __restrict__ Q, 
 // host
 // ------------------------------------------------------------------------------------------
 constexpr size_t kWsAlign = 256;
+// Query rows of a KV head from which on the cache is turned into bf16 rows first.
+constexpr int kExpandRows = 768;
 
+// How a call is made, and what lies where in its workspace (`base` may be NULL where only the size is asked for).
 struct Q4Plan {
-  int row_tiles;      // tiles of 16 queries per work-group
-  int n_splits;
-  size_t ml_at, lse_at, bytes;
-};
-
-Q4Plan plan_q4(int Hkv, int rows, int Nk, int D, bool weights) {
-  Q4Plan p = {};
-  p.row_tiles = rows <= 16 ? 1 : 2;
-  const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 16 * p.row_tiles)) * Hkv;
-  const int steps = ceil_div(Nk, kStep);
-  int64_t want = std::max<int64_t>(1, 512 / tiles);
-  want = std::min<int64_t>(want, ceil_div(steps, kWaves));
-  const int share = ceil_div(steps, static_cast<int>(std::min<int64_t>(want, 128)));
-  p.n_splits = ceil_div(steps, share);
-  const int64_t all = static_cast<int64_t>(Hkv) * rows;
-  size_t at = 0;
-  if (p.n_splits > 1) {
-    at = align_up(static_cast<size_t>(all) * p.n_splits * D * 4, kWsAlign);
-    p.ml_at = at;
-    at += align_up(static_cast<size_t>(all) * p.n_splits * 8, kWsAlign);
+  bool expand, keep_logits;     // the cache as bf16 rows and pc_frame_attn; weights from kept logits
+  int row_tiles, n_splits;      // tiles of 16 queries per work-group, key shares
+  float *part_o, *lse, *logits;
+  float2* part_ml;
+  uint16_t *k_rows, *v_rows;
+  void* attn_ws;
+  size_t attn_bytes, bytes;
+  Q4Plan(int dtype, int Hq, int Hkv, int Nq, int Nk, int D, bool weights, void* base) {
+    *this = Q4Plan();
+    const int rows = Hq / Hkv * Nq;
+    const int64_t all = static_cast<int64_t>(Hkv) * rows;
+    size_t at = 0;
+    auto take = [&](int64_t n) {
+      void* p = static_cast<uint8_t*>(base) + at;
+      at += align_up(static_cast<size_t>(n), kWsAlign);
+      return p;
+    };
+    expand = dtype == PC_BF16 && D == 128 && rows >= kExpandRows;
+    if (expand) {
+      const int64_t bytes_kv = static_cast<int64_t>(Hkv) * Nk * D * 2;
+      k_rows = static_cast<uint16_t*>(take(bytes_kv));
+      v_rows = static_cast<uint16_t*>(take(bytes_kv));
+      attn_bytes = pc_frame_attn_workspace_bytes_for(dtype, Hq, Hkv, Nq, Nk, D);
+      attn_ws = take(attn_bytes);
+    } else {
+      row_tiles = rows <= 16 ? 1 : 2;
+      const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 16 * row_tiles)) * Hkv;
+      const int steps = ceil_div(Nk, kStep);
+      int64_t want = std::max<int64_t>(1, 512 / tiles);
+      want = std::min<int64_t>(want, ceil_div(steps, kWaves));
+      n_splits = ceil_div(steps, ceil_div(steps, static_cast<int>(std::min<int64_t>(want, kMaxShares))));
+      if (n_splits > 1) {
+        part_o = static_cast<float*>(take(all * n_splits * D * 4));
+        part_ml = static_cast<float2*>(take(all * n_splits * 8));
+      }
+      keep_logits = weights && rows <= kLogitRows;
+      if (keep_logits) logits = static_cast<float*>(take(all * steps * kStep * 4));
+    }
+    if (weights) lse = static_cast<float*>(take(all * 4));
+    bytes = at;
   }
-  p.lse_at = at;
-  if (weights) at += align_up(static_cast<size_t>(all) * 4, kWsAlign);
-  p.bytes = at;
-  return p;
-}
+
+ private:
+  Q4Plan() = default;
+};
 
 int check_kind(int dtype, int D, const char* who) {
   PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "%s: dtype %d", who, dtype);
@@ -575,7 +698,7 @@ extern "C" int pc_q4_store(const void* K, const void* V, int dtype, int H, int n
   PC_REQUIRE(aligned16(K, k_stride_h, dtype) && aligned16(V, v_stride_h, dtype), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
   const int64_t units = 2ll * H * n;
-  PC_REQUIRE(units * (D / 8) <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
+  PC_REQUIRE(units <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
   const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
   const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
   const Book b = {pos_new, pos, weights, pos_stride_h, weights_stride_h, book ? Hsel : 0};
@@ -608,7 +731,7 @@ extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int 
   PC_REQUIRE((!K || aligned16(K, k_stride_h, dtype)) && (!V || aligned16(V, v_stride_h, dtype)), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
   const int64_t per = static_cast<int64_t>(H) * n, units = per * ((K != nullptr) + (V != nullptr));
-  PC_REQUIRE(2 * per * (D / 8) <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
+  PC_REQUIRE(2 * per <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
   const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
   const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
   const int first = K ? 0 : static_cast<int>(per);
@@ -635,7 +758,7 @@ bool sizes_ok(int Hq, int Hkv, int Nq, int Nk) {
 
 extern "C" size_t pc_q4_attn_workspace_bytes(int dtype, int Hq, int Hkv, int Nq, int Nk, int D, int weights) {
   if (!sizes_ok(Hq, Hkv, Nq, Nk) || (dtype != PC_F32 && dtype != PC_BF16) || (D != 64 && D != 128)) return 0;
-  return plan_q4(Hkv, Hq / Hkv * Nq, Nk, D, weights != 0).bytes;
+  return Q4Plan(dtype, Hq, Hkv, Nq, Nk, D, weights != 0, nullptr).bytes;
 }
 
 extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, int Hq, int Hkv, int Nq, int Nk, int D,
@@ -659,36 +782,47 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
     PC_REQUIRE(decay >= 0.f && isfinite(decay), PC_ERR_BUDGET, "%s: decay %g", who, decay);
   }
   const int rep = Hq / Hkv, rows = rep * Nq;
-  const Q4Plan plan = plan_q4(Hkv, rows, Nk, D, weights != nullptr);
+  const Q4Plan plan(dtype, Hq, Hkv, Nq, Nk, D, weights != nullptr, ws);
   PC_REQUIRE(plan.bytes == 0 || (ws != nullptr && ws_bytes >= plan.bytes && reinterpret_cast<uintptr_t>(ws) % 16 == 0),
              PC_ERR_WORKSPACE, "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, plan.bytes, ws_bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto* base = static_cast<uint8_t*>(ws);
-  const int tiles_q = ceil_div(rows, 16 * plan.row_tiles);
-  AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, 0, q_stride_h, o_stride_h,
-                scale * 1.4426950408889634f, nullptr, nullptr, lse, nullptr, static_cast<int64_t>(Hkv) * rows};
-  a.share_steps = ceil_div(ceil_div(Nk, kStep), plan.n_splits);
-  if (plan.n_splits > 1) {
-    a.part_o = reinterpret_cast<float*>(base);
-    a.part_ml = reinterpret_cast<float2*>(base + plan.ml_at);
+  const float c = scale * 1.4426950408889634f;
+  WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, kWeighKeys)), q_stride_h, weights_stride_h,
+                 c, decay, 1.f, plan.lse, weights};
+  if (plan.expand) {
+    // rows as they lie in the cache, so that one launch's worth of copying serves every query row
+    const int64_t per = static_cast<int64_t>(Nk) * D;
+    if (int rc = pc_q4_load(cache, Hkv, 0, Nk, D, PC_BF16, plan.k_rows, plan.v_rows, per, per, stream)) return rc;
+    float* e = lse != nullptr ? lse : weights != nullptr ? plan.lse : nullptr;
+    if (int rc = pc_frame_attn(Q, plan.k_rows, plan.v_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, o_stride_h, scale, O, e,
+                               plan.attn_ws, plan.attn_bytes, stream))
+      return rc;
+    w.lse = e;
+    w.lse_mul = 1.4426950408889634f;
   }
-  if (weights != nullptr) a.lse2 = reinterpret_cast<float*>(base + plan.lse_at);
   auto run = [&](auto zero, auto dims) -> int {
     using T = decltype(zero);
     constexpr int kDims = decltype(dims)::value;
     const T* q = static_cast<const T*>(Q);
-    const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
-    kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
-    PC_CHECK_LAUNCH(who);
-    if (plan.n_splits > 1) {
-      q4_merge_kernel<T, kDims><<<static_cast<unsigned>(a.rows_all), 256, 0, s>>>(static_cast<T*>(O), plan.n_splits, a);
+    if (!plan.expand) {
+      const int tiles_q = ceil_div(rows, 16 * plan.row_tiles), steps = ceil_div(Nk, kStep);
+      const AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, ceil_div(steps, plan.n_splits),
+                          q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.logits,
+                          static_cast<int64_t>(Hkv) * rows};
+      const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
+      kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
       PC_CHECK_LAUNCH(who);
+      const int blocks = ceil_div(Nk, 4 * kJoinThreads);
+      const JoinArgs j = {plan.n_splits, rows, Hkv, Hsel, Nk, plan.n_splits > 1 ? static_cast<int>(a.rows_all) : 0, Divisor(blocks),
+                          static_cast<int64_t>(steps) * kStep, weights_stride_h, c, decay, weights};
+      const int grid = j.row_blocks + (plan.keep_logits ? blocks * Hsel : 0);
+      if (grid > 0) {
+        q4_join_kernel<T, kDims><<<grid, kJoinThreads, 0, s>>>(static_cast<T*>(O), a, j);
+        PC_CHECK_LAUNCH(who);
+      }
     }
-    if (weights != nullptr) {
-      const int blocks = ceil_div(Nk, 64);
-      const WeighArgs w = {a.cache, rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(blocks), q_stride_h, weights_stride_h, a.c, decay,
-                           a.lse2, weights};
-      q4_weigh_kernel<T, kDims><<<blocks * Hsel, 256, 0, s>>>(q, w);
+    if (weights != nullptr && !plan.keep_logits) {
+      q4_weigh_kernel<T, kDims><<<w.by_blocks.d * Hsel, kThreads, 0, s>>>(q, w);
       PC_CHECK_LAUNCH(who);
     }
     return PC_OK;
