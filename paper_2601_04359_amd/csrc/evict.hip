@@ -47,16 +47,11 @@ struct HeadRanks {
   }
 };
 
-// One more in a bin for every active lane; lanes of a wave that agree (rows of equal weight) are one addition.
-__device__ __forceinline__ void vote(int* hist, int bin, bool active) {
-  const uint64_t all = __ballot(active);
-  if (all == 0) return;
-  const int first = __builtin_amdgcn_readlane(bin, __builtin_ctzll(all));
-  if (__ballot(active && bin == first) == all) {
-    if (lanes_below(all, 0) == 0 && active) atomicAdd(&hist[first], __popcll(all));
-  } else if (active) {
-    atomicAdd(&hist[bin], 1);
-  }
+// Sum of the first n waves' words, in every lane of the wave; s: a word per wave, n <= kSelWaves.
+__device__ __forceinline__ int before_wave(const int* s, int n) {
+  const int lane = threadIdx.x & 63;
+  const int upto = wave_prefix_sum(lane < kSelWaves ? s[lane] : 0);
+  return n == 0 ? 0 : __builtin_amdgcn_readlane(upto, n - 1);
 }
 
 // Where the left-th row from the top lies among kBins counted bins: s_found = (bin, rows still wanted of it, rows in it).
@@ -66,7 +61,7 @@ __device__ __forceinline__ void find_bin(const int* hist, int left, int* s_wave,
   constexpr int kPer = kBins > kSelThreads ? kBins / kSelThreads : kBins > 64 ? (kBins + 1023) / 1024 : 1;
   constexpr int kUsed = kBins / kPer;            // threads with bins, from the top bin down
   static_assert(kUsed % 64 == 0 && kUsed <= kSelThreads, "whole waves");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int c[kPer], sum = 0;
   const bool mine = threadIdx.x < kUsed;
 #pragma unroll
@@ -78,8 +73,7 @@ __device__ __forceinline__ void find_bin(const int* hist, int left, int* s_wave,
   if (mine && lane == 63) s_wave[wave] = upto;
   __syncthreads();
   if (mine) {
-    int at = upto - sum;
-    for (int w = 0; w < wave; ++w) at += s_wave[w];
+    int at = upto - sum + before_wave(s_wave, wave);
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       if (at < left && left <= at + c[k]) {
@@ -185,17 +179,20 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
   const int sel = blockIdx.x, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const HeadRanks rank(a, sel);
-  const int j0 = wave * 64 * kItems + lane;
+  const int items = (a.Nk + kSelThreads - 1) / kSelThreads;     // at most kItems
+  const int j0 = wave * 64 * items + lane;
   uint32_t key[kItems];
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) key[i] = rank.of(min(j0 + i * 64, a.Nk - 1));
+  for (int i = 0; i < kItems; ++i)
+    if (i < items) key[i] = rank.of(min(j0 + i * 64, a.Nk - 1));
   for (int b = threadIdx.x; b < kTopBins + 3 * 128; b += kSelThreads) hist[b] = 0;
   __syncthreads();
   uint32_t prefix = 0;
   int left = a.n_keep, shift = 32 - kTopBits;
   bool whole = false;
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) vote(hist, key[i] >> (32 - kTopBits), j0 + i * 64 < a.Nk);
+  for (int i = 0; i < kItems; ++i)
+    if (i < items && j0 + i * 64 < a.Nk) atomicAdd(&hist[key[i] >> (32 - kTopBits)], 1);
   __syncthreads();
   find_bin<kTopBins>(hist, left, s_wave[0], s_found);
   for (int pass = 0;; ++pass) {
@@ -207,7 +204,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
     int* h = hist + kTopBins + pass * 128;
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
-      vote(h, key[i] >> shift & 127, j0 + i * 64 < a.Nk && (key[i] ^ prefix) >> (shift + 7) == 0);
+      if (i < items && j0 + i * 64 < a.Nk && (key[i] ^ prefix) >> (shift + 7) == 0) atomicAdd(&h[key[i] >> shift & 127], 1);
     __syncthreads();
     find_bin<128>(h, left, s_wave[0], s_found);
   }
@@ -217,19 +214,22 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
   if (!whole) {
     int mine = 0;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) mine += __popcll(__ballot(j0 + i * 64 < a.Nk && key[i] == prefix));
+    for (int i = 0; i < kItems; ++i)
+      if (i < items) mine += __popcll(__ballot(j0 + i * 64 < a.Nk && key[i] == prefix));
     if (lane == 0) s_wave[0][wave] = mine;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) ties_before += s_wave[0][w];
+    ties_before = before_wave(s_wave[0], wave);
   }
   int n_holes = 0, n_movers = 0;
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
+    if (i >= items) continue;
     const int j = j0 + i * 64;
     bool stays = j < a.Nk && (whole ? key[i] >= prefix : key[i] > prefix);
     if (!whole) {
-      const uint64_t tied = __ballot(j < a.Nk && key[i] == prefix);
-      stays |= j < a.Nk && key[i] == prefix && lanes_below(tied, ties_before) < left;
+      const bool tie = j < a.Nk && key[i] == prefix;
+      const uint64_t tied = __ballot(tie);
+      stays |= tie && lanes_below(tied, ties_before) < left;
       ties_before += __popcll(tied);
     }
     keep[i] = __ballot(stays);
@@ -239,20 +239,19 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
   }
   if (lane == 0) s_wave[1][wave] = n_holes, s_wave[2][wave] = n_movers;
   __syncthreads();
-  int at_h = 0, at_m = 0, n = 0;
-  for (int w = 0; w < kSelWaves; ++w) {
-    if (w < wave) at_h += s_wave[1][w], at_m += s_wave[2][w];
-    n += s_wave[1][w];
-  }
+  int at_h = before_wave(s_wave[1], wave), at_m = before_wave(s_wave[2], wave);
+  const int n = before_wave(s_wave[1], kSelWaves);
   int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
   int32_t* movers = holes + room;
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
+    if (i >= items) continue;
     const int j = j0 + i * 64;
     const bool stays = keep[i] >> lane & 1;
-    const uint64_t bh = __ballot(j < a.n_keep && !stays), bm = __ballot(j >= a.n_keep && stays);
-    if (j < a.n_keep && !stays) holes[lanes_below(bh, at_h)] = j;
-    if (j >= a.n_keep && stays) movers[lanes_below(bm, at_m)] = j;
+    const bool hole = j < a.n_keep && !stays, mover = j >= a.n_keep && stays;
+    const uint64_t bh = __ballot(hole), bm = __ballot(mover);
+    if (hole) holes[lanes_below(bh, at_h)] = j;
+    if (mover) movers[lanes_below(bm, at_m)] = j;
     at_h += __popcll(bh), at_m += __popcll(bm);
   }
   if (!move) {
@@ -282,11 +281,20 @@ struct Slices {
   int n, rows;                // slices, rows of one (a multiple of kSlice)
   uint32_t* ranks;            // [Hsel][Nk]
   int32_t* hist;              // [Hsel][n][kTopBins]
-  int32_t* candidates;        // [Hsel][Nk]: rows
+  uint64_t* candidates;       // [Hsel][Nk]
   int32_t* decided;           // [Hsel][n][2]: holes and movers of the gather, then where a slice's begin
   int32_t* head;              // [Hsel][4]: candidates so far; bin, rows wanted of it, rows in it
   uint32_t* cut;              // [Hsel][2]: rank and row: rows of a higher rank stay, of this rank up to this row
 };
+
+// A row whose rank lies in the threshold's bin, in the order by rank (its other 21 bits), then row, lower rows above
+constexpr int kRest = 32 - kTopBits, kRowBits = 30;
+__device__ __forceinline__ uint64_t candidate(uint32_t rank, int row) {
+  return static_cast<uint64_t>(rank & ((1u << kRest) - 1)) << kRowBits | static_cast<uint32_t>((1 << kRowBits) - 1 - row);
+}
+__device__ __forceinline__ int row_of(uint64_t candidate) {
+  return (1 << kRowBits) - 1 - static_cast<int>(candidate & ((1u << kRowBits) - 1));
+}
 
 __global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slices s) {
   __shared__ int hist[kTopBins];
@@ -306,7 +314,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slice
     for (int i = 0; i < kItemsOfSlice; ++i) {
       const int64_t j = r0 + i * kSelThreads + threadIdx.x;
       if (j < end) out[j] = key[i];
-      vote(hist, key[i] >> (32 - kTopBits), j < end);
+      if (j < end) atomicAdd(&hist[key[i] >> (32 - kTopBits)], 1);
     }
   }
   __syncthreads();
@@ -315,17 +323,23 @@ __global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slice
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slices s) {
-  __shared__ int hist[kTopBins];
+  __shared__ __align__(16) int hist[kTopBins];
   __shared__ int s_wave[kSelWaves], s_found[3], s_count[2], s_at;
   const int sel = blockIdx.y, slice = blockIdx.x, lane = threadIdx.x & 63;
   const int32_t* all = s.hist + static_cast<int64_t>(sel) * s.n * kTopBins;
   {
-    int c0 = 0, c1 = 0;
-    for (int k = 0; k < s.n; ++k) {
-      c0 += all[static_cast<int64_t>(k) * kTopBins + threadIdx.x];
-      c1 += all[static_cast<int64_t>(k) * kTopBins + kSelThreads + threadIdx.x];
+    static_assert(kTopBins == 2 * kSelThreads, "two bins per thread");
+    u32x2 c = {0, 0};
+    const u32x2* from = reinterpret_cast<const u32x2*>(all) + threadIdx.x;
+    for (int k0 = 0; k0 < s.n; k0 += 16) {
+      u32x2 v[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = from[min(k0 + k, s.n - 1) * kSelThreads];
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k0 + k < s.n) c += v[k];
     }
-    hist[threadIdx.x] = c0, hist[kSelThreads + threadIdx.x] = c1;
+    reinterpret_cast<u32x2*>(hist)[threadIdx.x] = c;
   }
   if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
   __syncthreads();
@@ -339,24 +353,25 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
   __syncthreads();
   const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
   const uint32_t* in = s.ranks + static_cast<int64_t>(sel) * a.Nk;
-  int32_t* out = s.candidates + static_cast<int64_t>(sel) * a.Nk;
+  uint64_t* out = s.candidates + static_cast<int64_t>(sel) * a.Nk;
   int holes = 0, movers = 0;
   for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice) {
     uint32_t key[kItemsOfSlice];
 #pragma unroll
-    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = in[min(r0 + i * kSelThreads + threadIdx.x, end - 1)] >> (32 - kTopBits);
+    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = in[min(r0 + i * kSelThreads + threadIdx.x, end - 1)];
 #pragma unroll
     for (int i = 0; i < kItemsOfSlice; ++i) {
       const int64_t j = r0 + i * kSelThreads + threadIdx.x;
-      holes += __popcll(__ballot(j < end && j < a.n_keep && key[i] < bin));
-      movers += __popcll(__ballot(j < end && j >= a.n_keep && key[i] > bin));
-      const bool open = j < end && key[i] == bin;
+      const uint32_t top = key[i] >> kRest;
+      holes += __popcll(__ballot(j < end && j < a.n_keep && top < bin));
+      movers += __popcll(__ballot(j < end && j >= a.n_keep && top > bin));
+      const bool open = j < end && top == bin;
       const uint64_t b = __ballot(open);
       if (b != 0) {      // the wave's place among the slice's candidates
         int at = 0;
         if (lane == 0) at = atomicAdd(&s_at, __popcll(b));
         at = __builtin_amdgcn_readfirstlane(at);
-        if (open) out[lanes_below(b, at)] = static_cast<int32_t>(j);
+        if (open) out[lanes_below(b, at)] = candidate(key[i], static_cast<int>(j));
       }
     }
   }
@@ -369,33 +384,36 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Slices s, int32_t* __restrict__ counts) {
+  constexpr int kHeld = 12;          // candidates of a thread that stay in registers; more are read again each time
   __shared__ int hist[2048], s_wave[kSelWaves], s_found[3], s_holes[kMaxSlices], s_movers[kMaxSlices];
   const int sel = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t* ranks = s.ranks + static_cast<int64_t>(sel) * a.Nk;
-  const int32_t* cand = s.candidates + static_cast<int64_t>(sel) * a.Nk;
+  const uint64_t* cand = s.candidates + static_cast<int64_t>(sel) * a.Nk;
   int32_t* decided = s.decided + static_cast<int64_t>(sel) * s.n * 2;
   const uint32_t bin = s.head[sel * 4 + 1];
   int left = s.head[sel * 4 + 2];
   const int n = s.head[sel * 4 + 3];
-  for (int k = threadIdx.x; k < s.n; k += kSelThreads) s_holes[k] = decided[k * 2], s_movers[k] = decided[k * 2 + 1];
-  // the candidates' order: the other 21 bits of the rank, then 30 of the row, lower rows first
-  constexpr int kRest = 32 - kTopBits;
-  auto order = [&](int row) {
-    return static_cast<uint64_t>(ranks[row] & ((1u << kRest) - 1)) << 30 | static_cast<uint32_t>((1 << 30) - 1 - row);
+  uint64_t held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = cand[min(i * kSelThreads + static_cast<int>(threadIdx.x), n - 1)];
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (i * kSelThreads + static_cast<int>(threadIdx.x) < n) f(held[i]);
+    for (int c = kHeld * kSelThreads + threadIdx.x; c < n; c += kSelThreads) f(cand[c]);
   };
+  for (int k = threadIdx.x; k < s.n; k += kSelThreads) s_holes[k] = decided[k * 2], s_movers[k] = decided[k * 2 + 1];
   uint64_t prefix = 0;
   bool whole = n == left;
   // 11, 10 and three times 10 bits
-  for (int shift = kRest + 30; !whole && shift > 0;) {
-    const int bits = shift == kRest + 30 ? 11 : 10, upper = shift;
+  for (int shift = kRest + kRowBits; !whole && shift > 0;) {
+    const int bits = shift == kRest + kRowBits ? 11 : 10, upper = shift;
     shift -= bits;
     __syncthreads();
     for (int b = threadIdx.x; b < 2048; b += kSelThreads) hist[b] = 0;
     __syncthreads();
-    for (int c = threadIdx.x; c - lane < n; c += kSelThreads) {
-      const uint64_t o = order(cand[min(c, n - 1)]);
-      vote(hist, static_cast<int>(o >> shift) & ((1 << bits) - 1), c < n && (o ^ prefix) >> upper == 0);
-    }
+    each([&](uint64_t o) {
+      if ((o ^ prefix) >> upper == 0) atomicAdd(&hist[static_cast<int>(o >> shift) & ((1 << bits) - 1)], 1);
+    });
     __syncthreads();
     find_bin<2048>(hist, left, s_wave, s_found);
     prefix |= static_cast<uint64_t>(s_found[0]) << shift;
@@ -403,12 +421,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
     whole = s_found[2] == left;
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < n; c += kSelThreads) {
-    const int row = cand[c];
-    const bool stays = order(row) >= prefix;
+  each([&](uint64_t o) {
+    const int row = row_of(o);
+    const bool stays = o >= prefix;
     if (row < a.n_keep && !stays) atomicAdd(&s_holes[row / s.rows], 1);
     if (row >= a.n_keep && stays) atomicAdd(&s_movers[row / s.rows], 1);
-  }
+  });
   __syncthreads();
   // where the slices' holes and movers begin: a wave each, 64 slices at a time
   if (wave < 2) {
@@ -421,8 +439,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
     }
     if (wave == 0 && lane == 0) {
       counts[sel] = before;
-      s.cut[sel * 2] = bin << kRest | static_cast<uint32_t>(prefix >> 30);
-      s.cut[sel * 2 + 1] = (1u << 30) - 1 - static_cast<uint32_t>(prefix & ((1u << 30) - 1));
+      s.cut[sel * 2] = bin << kRest | static_cast<uint32_t>(prefix >> kRowBits);
+      s.cut[sel * 2 + 1] = row_of(prefix);
     }
   }
 }
@@ -457,12 +475,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_place_kernel(Ranks a, Slice
     }
     if (lane == 0) s_wave[turn][0][wave] = n_holes, s_wave[turn][1][wave] = n_movers;
     __syncthreads();
-    int mine_h = at_h, mine_m = at_m;
-    for (int w = 0; w < kSelWaves; ++w) {
-      const int h = s_wave[turn][0][w], m = s_wave[turn][1][w];
-      if (w < wave) mine_h += h, mine_m += m;
-      at_h += h, at_m += m;
-    }
+    int mine_h = at_h + before_wave(s_wave[turn][0], wave), mine_m = at_m + before_wave(s_wave[turn][1], wave);
+    at_h += before_wave(s_wave[turn][0], kSelWaves), at_m += before_wave(s_wave[turn][1], kSelWaves);
 #pragma unroll
     for (int i = 0; i < kItemsOfSlice; ++i) {
       const int j = static_cast<int>(j0) + i * 64;
@@ -502,7 +516,7 @@ struct EvictPlan {
       s = {n_slices, slice_rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
       s.ranks = static_cast<uint32_t*>(take(heads * Nk * 4));
       s.hist = static_cast<int32_t*>(take(heads * n_slices * kTopBins * 4));
-      s.candidates = static_cast<int32_t*>(take(heads * Nk * 4));
+      s.candidates = static_cast<uint64_t*>(take(heads * Nk * 8));
       s.decided = static_cast<int32_t*>(take(heads * n_slices * 8));
       s.head = static_cast<int32_t*>(take(heads * 16));
       s.cut = static_cast<uint32_t*>(take(heads * 8));
