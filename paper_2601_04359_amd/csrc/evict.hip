@@ -31,21 +31,38 @@ __device__ __forceinline__ uint32_t weight_rank(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One selection head's rows: anchors and recent rows rank above every weight.
+// One selection head's rows: anchors and recent rows rank above every weight.  What a row's rank is made of is
+// fetched apart from the arithmetic, so that a thread has all its rows' loads in flight.
 struct HeadRanks {
   const float* w;
   const int32_t* t;
-  int64_t newest;
+  const int32_t* last;
   int n_anchor, recent_t;
+  struct Row {
+    float w;
+    int32_t t;
+  };
   __device__ HeadRanks(const Ranks& a, int sel)
       : w(a.weights + sel * a.w_stride_h), t(a.recent_t > 0 ? a.pos + sel * a.pos_stride_h : nullptr),
-        newest(a.recent_t > 0 ? t[static_cast<int64_t>(a.Nk - 1) * 3] : 0), n_anchor(a.n_anchor), recent_t(a.recent_t) {}
-  __device__ __forceinline__ uint32_t of(int j) const {
-    const bool safe = j < n_anchor || (t != nullptr && t[static_cast<int64_t>(j) * 3] > newest - recent_t);
-    const uint32_t rank = weight_rank(w[j]);
-    return safe ? 0xffffffffu : rank;
+        last(t == nullptr ? nullptr : t + static_cast<int64_t>(a.Nk - 1) * 3), n_anchor(a.n_anchor), recent_t(a.recent_t) {}
+  __device__ __forceinline__ Row fetch(int j) const { return {w[j], t == nullptr ? 0 : t[static_cast<int64_t>(j) * 3]}; }
+  // the t above which a row is recent
+  __device__ __forceinline__ int64_t border() const { return t == nullptr ? INT_MAX : static_cast<int64_t>(*last) - recent_t; }
+  __device__ __forceinline__ uint32_t rank(const Row& row, int j, int64_t border) const {
+    return j < n_anchor || row.t > border ? 0xffffffffu : weight_rank(row.w);
   }
 };
+
+// Counters of the top bits in four copies, a lane's by its number: weights crowd into few bins (a factor of two
+// is four of them), and lanes of a wave that count in one bin take turns.
+constexpr int kCopies = 4;
+__device__ __forceinline__ void count_top(int* hist, uint32_t key) {
+  atomicAdd(&hist[(key >> (32 - kTopBits)) * kCopies + (threadIdx.x & (kCopies - 1))], 1);
+}
+__device__ __forceinline__ int counted_top(const int* hist, int bin) {
+  const u32x4 c = *reinterpret_cast<const u32x4*>(hist + bin * kCopies);
+  return static_cast<int>(c[0] + c[1] + c[2] + c[3]);
+}
 
 // Sum of the first n waves' words, in every lane of the wave; s: a word per wave, n <= kSelWaves.
 __device__ __forceinline__ int before_wave(const int* s, int n) {
@@ -56,9 +73,9 @@ __device__ __forceinline__ int before_wave(const int* s, int n) {
 
 // Where the left-th row from the top lies among kBins counted bins: s_found = (bin, rows still wanted of it, rows in it).
 // Every thread calls it, between barriers; s_wave: a word per wave.
-template <int kBins>
-__device__ __forceinline__ void find_bin(const int* hist, int left, int* s_wave, int* s_found) {
-  constexpr int kPer = kBins > kSelThreads ? kBins / kSelThreads : kBins > 64 ? (kBins + 1023) / 1024 : 1;
+template <int kBins, class Count>
+__device__ __forceinline__ void find_bin(Count&& count, int left, int* s_wave, int* s_found) {
+  constexpr int kPer = kBins > kSelThreads ? kBins / kSelThreads : 1;
   constexpr int kUsed = kBins / kPer;            // threads with bins, from the top bin down
   static_assert(kUsed % 64 == 0 && kUsed <= kSelThreads, "whole waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -66,7 +83,7 @@ __device__ __forceinline__ void find_bin(const int* hist, int left, int* s_wave,
   const bool mine = threadIdx.x < kUsed;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    c[k] = mine ? hist[kBins - 1 - (static_cast<int>(threadIdx.x) * kPer + k)] : 0;
+    c[k] = mine ? count(kBins - 1 - (static_cast<int>(threadIdx.x) * kPer + k)) : 0;
     sum += c[k];
   }
   const int upto = wave_prefix_sum(sum);
@@ -166,75 +183,82 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Moves m, int book_block
 }
 
 // ------------------------------------------------------------------------------------------
-// Up to 32 x 1,024 rows: a work-group per selection head, the ranks in registers (wave w owns 64 kItems
+// Up to 24 x 1,024 rows: a work-group per selection head, the ranks in registers (wave w owns 64 kItems
 // rows in a row, so that list places are a ballot per 64 of them and one sum over the waves).  The n_keep-th rank is
-// found from the top bits down, 11 then 7 at a time, in LDS counters; a step whose bin is wanted whole ends it.
+// found from the top bits down, 11, 11 and 10 at a time, in LDS counters; a step whose bin is wanted whole ends it.
 // With `move` the same work-group moves the rows: a second launch costs more than it takes for few.
+// Bound: latency, a chain of barriers behind one fetch.
 // ------------------------------------------------------------------------------------------
 template <int kItems>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int room, int32_t* __restrict__ counts,
                                                                    int32_t* __restrict__ lists, Moves m, int move) {
-  __shared__ int hist[kTopBins + 3 * 128];
+  __shared__ __align__(16) int hist[kTopBins * kCopies + 2048 + 1024];
   __shared__ int s_wave[3][kSelWaves], s_found[3];
   const int sel = blockIdx.x, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const HeadRanks rank(a, sel);
-  const int items = (a.Nk + kSelThreads - 1) / kSelThreads;     // at most kItems
-  const int j0 = wave * 64 * items + lane;
+  const HeadRanks head(a, sel);
+  const int first = wave * 64 * kItems, j0 = first + lane;
+  HeadRanks::Row row[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) row[i] = head.fetch(min(j0 + i * 64, a.Nk - 1));
+  const int64_t border = head.border();
+  for (int b = threadIdx.x * 4; b < kTopBins * kCopies + 2048 + 1024; b += kSelThreads * 4)
+    *reinterpret_cast<u32x4*>(hist + b) = u32x4{0, 0, 0, 0};
+  __syncthreads();
   uint32_t key[kItems];
 #pragma unroll
-  for (int i = 0; i < kItems; ++i)
-    if (i < items) key[i] = rank.of(min(j0 + i * 64, a.Nk - 1));
-  for (int b = threadIdx.x; b < kTopBins + 3 * 128; b += kSelThreads) hist[b] = 0;
+  for (int i = 0; i < kItems; ++i) {
+    key[i] = head.rank(row[i], j0 + i * 64, border);
+    if (j0 + i * 64 < a.Nk) count_top(hist, key[i]);
+  }
   __syncthreads();
   uint32_t prefix = 0;
   int left = a.n_keep, shift = 32 - kTopBits;
   bool whole = false;
-#pragma unroll
-  for (int i = 0; i < kItems; ++i)
-    if (i < items && j0 + i * 64 < a.Nk) atomicAdd(&hist[key[i] >> (32 - kTopBits)], 1);
-  __syncthreads();
-  find_bin<kTopBins>(hist, left, s_wave[0], s_found);
-  for (int pass = 0;; ++pass) {
+  find_bin<kTopBins>([&](int b) { return counted_top(hist, b); }, left, s_wave[0], s_found);
+  for (;;) {
     prefix |= static_cast<uint32_t>(s_found[0]) << shift;
     left = s_found[1];
     whole = s_found[2] == left;
     if (whole || shift == 0) break;
-    shift -= 7;
-    int* h = hist + kTopBins + pass * 128;
+    const int upper = shift;
+    shift = upper == 21 ? 10 : 0;
+    int* h = hist + kTopBins * kCopies + (upper == 21 ? 0 : 2048);
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
-      if (i < items && j0 + i * 64 < a.Nk && (key[i] ^ prefix) >> (shift + 7) == 0) atomicAdd(&h[key[i] >> shift & 127], 1);
+      if (j0 + i * 64 < a.Nk && (key[i] ^ prefix) >> upper == 0) atomicAdd(&h[key[i] >> shift & ((1 << (upper - shift)) - 1)], 1);
     __syncthreads();
-    find_bin<128>(h, left, s_wave[0], s_found);
+    if (upper == 21) find_bin<2048>([&](int b) { return h[b]; }, left, s_wave[0], s_found);
+    else find_bin<1024>([&](int b) { return h[b]; }, left, s_wave[0], s_found);
   }
   // rows above the threshold stay; of those at it (not whole: several of one weight, left of them wanted) the first ones
-  uint64_t keep[kItems];
   int ties_before = 0;
   if (!whole) {
     int mine = 0;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (i < items) mine += __popcll(__ballot(j0 + i * 64 < a.Nk && key[i] == prefix));
+    for (int i = 0; i < kItems; ++i) mine += __popcll(__ballot(j0 + i * 64 < a.Nk && key[i] == prefix));
     if (lane == 0) s_wave[0][wave] = mine;
     __syncthreads();
     ties_before = before_wave(s_wave[0], wave);
   }
+  uint32_t leaves = 0;         // a bit per row of the lane
   int n_holes = 0, n_movers = 0;
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
-    if (i >= items) continue;
+    if (first + i * 64 >= a.Nk) break;
     const int j = j0 + i * 64;
-    bool stays = j < a.Nk && (whole ? key[i] >= prefix : key[i] > prefix);
+    bool stays = key[i] > prefix || (whole && key[i] == prefix);
     if (!whole) {
       const bool tie = j < a.Nk && key[i] == prefix;
       const uint64_t tied = __ballot(tie);
-      stays |= tie && lanes_below(tied, ties_before) < left;
-      ties_before += __popcll(tied);
+      if (tied != 0) {
+        stays |= tie && lanes_below(tied, ties_before) < left;
+        ties_before += __popcll(tied);
+      }
     }
-    keep[i] = __ballot(stays);
-    n_holes += __popcll(__ballot(j < a.n_keep && !stays));
-    n_movers += __popcll(__ballot(j >= a.n_keep && stays));
+    if (!stays) leaves |= 1u << i;
+    if (first + i * 64 < a.n_keep) n_holes += __popcll(__ballot(!stays && j < a.n_keep));
+    if (first + i * 64 + 63 >= a.n_keep) n_movers += __popcll(__ballot(stays && j >= a.n_keep && j < a.Nk));
     if (m.idx != nullptr && stays && j < a.n_keep) m.idx[sel * m.idx_stride_h + j] = j;
   }
   if (lane == 0) s_wave[1][wave] = n_holes, s_wave[2][wave] = n_movers;
@@ -243,16 +267,17 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
   const int n = before_wave(s_wave[1], kSelWaves);
   int32_t* holes = lists + static_cast<int64_t>(sel) * 2 * room;
   int32_t* movers = holes + room;
+  if (n_holes + n_movers > 0) {
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    if (i >= items) continue;
-    const int j = j0 + i * 64;
-    const bool stays = keep[i] >> lane & 1;
-    const bool hole = j < a.n_keep && !stays, mover = j >= a.n_keep && stays;
-    const uint64_t bh = __ballot(hole), bm = __ballot(mover);
-    if (hole) holes[lanes_below(bh, at_h)] = j;
-    if (mover) movers[lanes_below(bm, at_m)] = j;
-    at_h += __popcll(bh), at_m += __popcll(bm);
+    for (int i = 0; i < kItems; ++i) {
+      const int j = j0 + i * 64;
+      const bool gone = leaves >> i & 1;
+      const bool hole = gone && j < a.n_keep, mover = !gone && j >= a.n_keep && j < a.Nk;
+      const uint64_t bh = __ballot(hole), bm = __ballot(mover);
+      if (hole) holes[lanes_below(bh, at_h)] = j;
+      if (mover) movers[lanes_below(bm, at_m)] = j;
+      at_h += __popcll(bh), at_m += __popcll(bm);
+    }
   }
   if (!move) {
     if (threadIdx.x == 0) counts[sel] = n;
@@ -283,7 +308,7 @@ struct Slices {
   int32_t* hist;              // [Hsel][n][kTopBins]
   uint64_t* candidates;       // [Hsel][Nk]
   int32_t* decided;           // [Hsel][n][2]: holes and movers of the gather, then where a slice's begin
-  int32_t* head;              // [Hsel][4]: candidates so far; bin, rows wanted of it, rows in it
+  int32_t* head;              // [Hsel][4]: the threshold's bin, rows wanted of it, rows in it
   uint32_t* cut;              // [Hsel][2]: rank and row: rows of a higher rank stay, of this rank up to this row
 };
 
@@ -297,36 +322,49 @@ __device__ __forceinline__ int row_of(uint64_t candidate) {
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slices s) {
-  __shared__ int hist[kTopBins];
+  __shared__ __align__(16) int hist[kTopBins * kCopies];
   const int sel = blockIdx.y, slice = blockIdx.x;
-  const HeadRanks rank(a, sel);
-  for (int b = threadIdx.x; b < kTopBins; b += kSelThreads) hist[b] = 0;
-  if (slice == 0 && threadIdx.x == 0) s.head[sel * 4] = 0;
+  const HeadRanks head(a, sel);
+  const int64_t border = head.border();
+  for (int b = threadIdx.x * 4; b < kTopBins * kCopies; b += kSelThreads * 4)
+    *reinterpret_cast<u32x4*>(hist + b) = u32x4{0, 0, 0, 0};
   __syncthreads();
   const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
   uint32_t* out = s.ranks + static_cast<int64_t>(sel) * a.Nk;
   for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice) {
-    uint32_t key[kItemsOfSlice];
+    HeadRanks::Row row[kItemsOfSlice];
 #pragma unroll
     for (int i = 0; i < kItemsOfSlice; ++i)
-      key[i] = rank.of(static_cast<int>(min(r0 + i * kSelThreads + threadIdx.x, static_cast<int64_t>(a.Nk) - 1)));
+      row[i] = head.fetch(static_cast<int>(min(r0 + i * kSelThreads + threadIdx.x, static_cast<int64_t>(a.Nk) - 1)));
 #pragma unroll
     for (int i = 0; i < kItemsOfSlice; ++i) {
       const int64_t j = r0 + i * kSelThreads + threadIdx.x;
-      if (j < end) out[j] = key[i];
-      if (j < end) atomicAdd(&hist[key[i] >> (32 - kTopBits)], 1);
+      const uint32_t key = head.rank(row[i], static_cast<int>(j), border);
+      if (j < end) {
+        out[j] = key;
+        count_top(hist, key);
+      }
     }
   }
   __syncthreads();
   int32_t* to = s.hist + (static_cast<int64_t>(sel) * s.n + slice) * kTopBins;
-  for (int b = threadIdx.x; b < kTopBins; b += kSelThreads) to[b] = hist[b];
+  for (int b = threadIdx.x; b < kTopBins; b += kSelThreads) to[b] = counted_top(hist, b);
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slices s) {
   __shared__ __align__(16) int hist[kTopBins];
   __shared__ int s_wave[kSelWaves], s_found[3], s_count[2], s_at;
-  const int sel = blockIdx.y, slice = blockIdx.x, lane = threadIdx.x & 63;
+  const int sel = blockIdx.y, slice = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t* all = s.hist + static_cast<int64_t>(sel) * s.n * kTopBins;
+  const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
+  const uint32_t* in = s.ranks + static_cast<int64_t>(sel) * a.Nk;
+  int64_t r0 = static_cast<int64_t>(slice) * s.rows;
+  uint32_t key[kItemsOfSlice];
+  auto fetch = [&] {
+#pragma unroll
+    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = in[min(r0 + i * kSelThreads + threadIdx.x, end - 1)];
+  };
+  fetch();
   {
     static_assert(kTopBins == 2 * kSelThreads, "two bins per thread");
     u32x2 c = {0, 0};
@@ -343,22 +381,20 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
   }
   if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
   __syncthreads();
-  find_bin<kTopBins>(hist, a.n_keep, s_wave, s_found);
+  find_bin<kTopBins>([&](int b) { return hist[b]; }, a.n_keep, s_wave, s_found);
   const uint32_t bin = s_found[0];
-  if (threadIdx.x == 0) {
-    s_at = atomicAdd(&s.head[sel * 4], all[static_cast<int64_t>(slice) * kTopBins + bin]);
-    if (slice == 0)
-      for (int k = 0; k < 3; ++k) s.head[sel * 4 + 1 + k] = s_found[k];
+  // the slice's candidates begin behind those of the slices before it
+  if (wave == 0) {
+    int before = 0;
+    for (int k = lane; k < slice; k += 64) before += all[static_cast<int64_t>(k) * kTopBins + bin];
+    before = wave_prefix_sum(before);
+    if (lane == 63) s_at = before;
   }
+  if (slice == 0 && threadIdx.x < 3) s.head[sel * 4 + threadIdx.x] = s_found[threadIdx.x];
   __syncthreads();
-  const int64_t end = min(static_cast<int64_t>(slice + 1) * s.rows, static_cast<int64_t>(a.Nk));
-  const uint32_t* in = s.ranks + static_cast<int64_t>(sel) * a.Nk;
   uint64_t* out = s.candidates + static_cast<int64_t>(sel) * a.Nk;
   int holes = 0, movers = 0;
-  for (int64_t r0 = static_cast<int64_t>(slice) * s.rows; r0 < end; r0 += kSlice) {
-    uint32_t key[kItemsOfSlice];
-#pragma unroll
-    for (int i = 0; i < kItemsOfSlice; ++i) key[i] = in[min(r0 + i * kSelThreads + threadIdx.x, end - 1)];
+  for (;;) {
 #pragma unroll
     for (int i = 0; i < kItemsOfSlice; ++i) {
       const int64_t j = r0 + i * kSelThreads + threadIdx.x;
@@ -374,6 +410,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
         if (open) out[lanes_below(b, at)] = candidate(key[i], static_cast<int>(j));
       }
     }
+    r0 += kSlice;
+    if (r0 >= end) break;
+    fetch();
   }
   if (lane == 0) {
     atomicAdd(&s_count[0], holes);
@@ -389,9 +428,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
   const int sel = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t* cand = s.candidates + static_cast<int64_t>(sel) * a.Nk;
   int32_t* decided = s.decided + static_cast<int64_t>(sel) * s.n * 2;
-  const uint32_t bin = s.head[sel * 4 + 1];
-  int left = s.head[sel * 4 + 2];
-  const int n = s.head[sel * 4 + 3];
+  const uint32_t bin = s.head[sel * 4];
+  int left = s.head[sel * 4 + 1];
+  const int n = s.head[sel * 4 + 2];
   uint64_t held[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) held[i] = cand[min(i * kSelThreads + static_cast<int>(threadIdx.x), n - 1)];
@@ -415,7 +454,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
       if ((o ^ prefix) >> upper == 0) atomicAdd(&hist[static_cast<int>(o >> shift) & ((1 << bits) - 1)], 1);
     });
     __syncthreads();
-    find_bin<2048>(hist, left, s_wave, s_found);
+    find_bin<2048>([&](int b) { return hist[b]; }, left, s_wave, s_found);
     prefix |= static_cast<uint64_t>(s_found[0]) << shift;
     left = s_found[1];
     whole = s_found[2] == left;
@@ -491,7 +530,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_place_kernel(Ranks a, Slice
 // host
 // ------------------------------------------------------------------------------------------
 constexpr size_t kWsAlign = 256;
-constexpr int kMaxInRegisters = 32 * kSelThreads;
+constexpr int kMaxInRegisters = 24 * kSelThreads;
 constexpr int64_t kMoveWithSelect = 64 << 10;     // bytes that a work-group of the one-launch form moves at most
 
 // What a call keeps in its workspace; `base` may be NULL where only the size is asked for.
@@ -555,10 +594,15 @@ int evict(const char* who, Moves m, int64_t row_bytes, int H, int32_t* pos, int6
   const Ranks a = {weights, pos, w_stride_h, pos_stride_h, Nk, n_keep, n_anchor, recent_t};
   if (plan.n_slices == 0) {
     const int move = plan.room * row_bytes * m.per <= kMoveWithSelect;
-    const auto kernel = Nk <= 4 * kSelThreads    ? evict_select_kernel<4>
-                        : Nk <= 8 * kSelThreads  ? evict_select_kernel<8>
-                        : Nk <= 16 * kSelThreads ? evict_select_kernel<16>
-                                                 : evict_select_kernel<32>;
+    const int items = ceil_div(Nk, kSelThreads);
+    const auto kernel = items <= 2    ? evict_select_kernel<2>
+                        : items <= 4  ? evict_select_kernel<4>
+                        : items <= 6  ? evict_select_kernel<6>
+                        : items <= 8  ? evict_select_kernel<8>
+                        : items <= 10 ? evict_select_kernel<10>
+                        : items <= 12 ? evict_select_kernel<12>
+                        : items <= 16 ? evict_select_kernel<16>
+                                      : evict_select_kernel<24>;
     kernel<<<Hsel, kSelThreads, 0, s>>>(a, plan.room, plan.counts, plan.lists, m, move);
     PC_CHECK_LAUNCH(who);
     if (move) return PC_OK;

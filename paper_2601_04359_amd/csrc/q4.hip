@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
 
 // ------------------------------------------------------------------------------------------
 // Attention straight from the codes, for few query rows: 16 kRT rows per work-group, its eight waves deal the keys in
-// steps of 32.
+// steps of 32 (sixteen waves were 20 % faster per step where one compute unit does all, and 0.5 us slower to end).
 //   * S^T = K Q^T by 16x16x32 products.  Which dims a product contracts is free as long as both operands agree: lane
 //     (r = l % 16, g = l / 16) takes dims g D/4 .. of key row r, which lie in one scale group and are one load,
 //     and its dwords of eight codes are the operands of the D/32 products after four conversions each.  K never
@@ -140,7 +140,10 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kStep = 32;                   // keys of a wave's step
 constexpr int kMaxShares = 128;             // of the keys
-constexpr int kLogitRows = 8;               // per KV head: up to here the weights come from logits that are kept
+// Rows per KV head up to which the weights come from logits that are kept (against 68 bytes and the products: 12 rows x
+// 16,000 keys 13.1 us, 14.1 formed again; 16 rows 15.0 and 14.6).  Where the attention is not cut, that launch would be one
+// more for it: up to 8 rows (12 rows x 300 keys 10.1 us, 8.5 formed again).
+constexpr int kLogitRows = 12, kLogitRowsFewKeys = 8;
 constexpr int kMaxJoinRows = 64;            // of a selection head, at a time
 
 struct AttnArgs {
@@ -218,7 +221,7 @@ __device__ __forceinline__ f32x4 scores(const bf16x8 (&k)[D / 32], const QueryFr
 }
 
 template <typename T, int D, int kRT>
-__global__ __launch_bounds__(kThreads, 1) void q4_attn_kernel(const T* __restrict__ Q, T* __restrict__ O, AttnArgs a) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void q4_attn_kernel(const T* __restrict__ Q, T* __restrict__ O, AttnArgs a) {
   using lds_byte = __attribute__((address_space(3))) uint8_t;
   constexpr int kParts = QueryFrags<T, D>::kParts;
   constexpr int kTileBytes = kStep * D * 2;                 // a wave's V rows; its partial output as well
@@ -454,18 +457,27 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
   if (static_cast<int>(blockIdx.x) < j.row_blocks) {
     const int64_t at = blockIdx.x;
     const int u = threadIdx.x % kUnits, part = threadIdx.x / kUnits;
-    const float2 row = join_ml(a.part_ml + at, a.rows_all, j.n_splits, lane);
-    for (int s = threadIdx.x; s < j.n_splits; s += kJoinThreads) s_w[s] = __builtin_amdgcn_exp2f(a.part_ml[s * a.rows_all + at].x - row.x);
-    __syncthreads();
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    // the first partial rows are fetched in front of the pairs they are weighed by
     const float* from = a.part_o + at * D + u * 4;
-    for (int s0 = part; s0 < j.n_splits; s0 += 8 * kLanes) {
-      f32x4 v[8];
+    auto fetch = [&](f32x4 (&v)[8], int s0) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const f32x4*>(from + min(s0 + k * kLanes, j.n_splits - 1) * a.rows_all * D);
+    };
+    f32x4 v[8];
+    fetch(v, part);
+    const float own = static_cast<int>(threadIdx.x) < j.n_splits ? a.part_ml[threadIdx.x * a.rows_all + at].x : kNoRef;
+    const float2 row = join_ml(a.part_ml + at, a.rows_all, j.n_splits, lane);
+    static_assert(kMaxShares <= kJoinThreads, "a thread per share");
+    if (static_cast<int>(threadIdx.x) < j.n_splits) s_w[threadIdx.x] = __builtin_amdgcn_exp2f(own - row.x);
+    __syncthreads();
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = part;;) {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         if (s0 + k * kLanes < j.n_splits) acc += s_w[s0 + k * kLanes] * v[k];
+      s0 += 8 * kLanes;
+      if (s0 >= j.n_splits) break;
+      fetch(v, s0);
     }
     s_o[part][u] = acc;
     __syncthreads();
@@ -524,37 +536,42 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
 }
 
 // ------------------------------------------------------------------------------------------
-// The weights of many rows: weights[j] = decay * weights[j] + sum over the query rows of exp2(c s - lse2), the scores
-// formed once more from the keys' codes.  A work-group owns 64 keys, which every wave holds as the second operand (a lane
-// sums its keys' columns over the queries it sees); the waves deal the query rows in tiles of 16 and are
-// added up in their order.  With one sum for all heads a work-group walks the KV heads as well.
+// The weights of more rows: weights[j] = decay * weights[j] + sum over the query rows of exp2(c s - lse2), the scores
+// formed once more from the keys' codes.  A wave owns 64 or 128 keys as the second operand (a lane sums its keys' columns
+// over the queries it sees) and walks the query rows in tiles of 16, the next one in flight.  Where keys are few, the
+// waves of a work-group share 64 keys, deal the row tiles and are added up in their order; where they are many, each
+// has keys of its own: dealing 16 row tiles of 60,000 keys over eight waves converted every key eight times (57 us
+// instead of 35), and 128 keys per wave halve the queries' way through L2 (24).  With one sum for all heads a wave
+// walks the KV heads as well.
 // ------------------------------------------------------------------------------------------
 struct WeighArgs {
   Q4Rows cache;
   int rep, Nk, Hkv, Hsel;
   Divisor by_nq, by_blocks;                 // rows per head, key blocks of a selection head
+  int dealt;                                // waves that share keys: 1, 2, 4 or 8
   int64_t q_stride_h, w_stride_h;
-  float c, decay, lse_mul;                  // lse_mul: brings lse to base 2
-  const float* lse;
+  float c, decay;
+  const float* lse;                         // base 2
   float* weights;
 };
-constexpr int kWeighTiles = 4, kWeighKeys = 16 * kWeighTiles;
-
-template <typename T, int D>
+template <typename T, int D, int kTiles>
 __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict__ Q, WeighArgs a) {
-  __shared__ float s_sum[kWaves][kWeighKeys];
+  constexpr int kKeys = 16 * kTiles;
+  __shared__ float s_sum[kWaves][kKeys];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int unit = xcd_contiguous_index(blockIdx.x, gridDim.x);
   const int sel = a.by_blocks.of(unit), block = unit - sel * a.by_blocks.d;
-  const int k0 = block * kWeighKeys;
+  const int row_wave = wave & (a.dealt - 1), step = 16 * a.dealt;
+  const int groups = blockDim.x / 64 / a.dealt;
+  const int block0 = block * groups * kKeys, k0 = block0 + wave / a.dealt * kKeys;
   const int n_rows = a.rep * a.by_nq.d, per = a.Hkv / a.Hsel;
-  float sum[kWeighTiles] = {};
+  float sum[kTiles] = {};
   for (int kvh = sel * per; kvh < (sel + 1) * per; ++kvh) {
-    bf16x8 kf[kWeighTiles][D / 32];
+    bf16x8 kf[kTiles][D / 32];
 #pragma unroll
-    for (int t = 0; t < kWeighTiles; ++t) {
+    for (int t = 0; t < kTiles; ++t) {
       KeyCodes<D> raw;
       raw.load(a.cache.k_codes + kvh * a.cache.code_stride_h, a.cache.k_scales + kvh * a.cache.scale_stride_h,
                min(k0 + t * 16 + r, a.Nk - 1), g);
@@ -562,20 +579,24 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
       for (int b = 0; b < D / 32; ++b) kf[t][b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
     }
     const float* lse = a.lse + static_cast<int64_t>(kvh) * n_rows;
-    for (int row0 = wave * 16; row0 < n_rows; row0 += 16 * kWaves) {
+    QueryFrags<T, D> next;
+    float next_e2[4];
+    auto fetch = [&](int row0) {
       const int rho = min(row0 + r, n_rows - 1);
       const int head = a.by_nq.of(rho);
-      QueryFrags<T, D> q;
-      q.load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
+      next.load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) next_e2[i] = lse[min(row0 + g * 4 + i, n_rows - 1)];
+    };
+    if (row_wave * 16 < n_rows) fetch(row_wave * 16);
+    for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
+      const QueryFrags<T, D> q = next;
       float e2[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {     // a row that is not there has probability 0
-        const int row = row0 + g * 4 + i;
-        const float x = lse[min(row, n_rows - 1)] * a.lse_mul;
-        e2[i] = row < n_rows ? x : INFINITY;
-      }
+      for (int i = 0; i < 4; ++i) e2[i] = row0 + g * 4 + i < n_rows ? next_e2[i] : INFINITY;   // a row that is not there: probability 0
+      if (row0 + step < n_rows) fetch(row0 + step);
 #pragma unroll
-      for (int t = 0; t < kWeighTiles; ++t) {
+      for (int t = 0; t < kTiles; ++t) {
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
@@ -587,19 +608,30 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
     }
   }
 #pragma unroll
-  for (int t = 0; t < kWeighTiles; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     sum[t] += __shfl_xor(sum[t], 16);
     sum[t] += __shfl_xor(sum[t], 32);
     if (g == 0) s_sum[wave][t * 16 + r] = sum[t];
   }
   __syncthreads();
-  if (threadIdx.x < kWeighKeys && k0 + static_cast<int>(threadIdx.x) < a.Nk) {
+  // key i of the work-group: of the waves from i / kKeys * dealt on
+  for (int i = threadIdx.x; i < groups * kKeys && block0 + i < a.Nk; i += blockDim.x) {
+    const int from = i / kKeys * a.dealt;
     float x = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) x += s_sum[w][threadIdx.x];
-    float* w = a.weights + sel * a.w_stride_h + k0 + threadIdx.x;
+    for (int w = 0; w < a.dealt; ++w) x += s_sum[from + w][i % kKeys];
+    float* w = a.weights + sel * a.w_stride_h + block0 + i;
     *w = a.decay == 0.f ? x : fmaf(a.decay, *w, x);
   }
+}
+
+// weights = decay * weights + scores, a row of blocks per selection head
+__global__ __launch_bounds__(256) void q4_add_kernel(float* __restrict__ weights, int64_t w_stride_h, const float* __restrict__ score,
+                                                     int Nk, float decay) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= Nk) return;
+  float* w = weights + blockIdx.y * w_stride_h + j;
+  const float x = score[static_cast<int64_t>(blockIdx.y) * Nk + j];
+  *w = decay == 0.f ? x : fmaf(decay, *w, x);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -613,11 +645,11 @@ constexpr int kExpandRows = 768;
 struct Q4Plan {
   bool expand, keep_logits;     // the cache as bf16 rows and pc_frame_attn; weights from kept logits
   int row_tiles, n_splits;      // tiles of 16 queries per work-group, key shares
-  float *part_o, *lse, *logits;
+  float *part_o, *lse, *logits, *score;
   float2* part_ml;
   uint16_t *k_rows, *v_rows;
   void* attn_ws;
-  size_t attn_bytes, bytes;
+  size_t attn_bytes, bytes;    // of attn_ws, which the scoring takes after the attention
   Q4Plan(int dtype, int Hq, int Hkv, int Nq, int Nk, int D, bool weights, void* base) {
     *this = Q4Plan();
     const int rows = Hq / Hkv * Nq;
@@ -634,19 +666,25 @@ struct Q4Plan {
       k_rows = static_cast<uint16_t*>(take(bytes_kv));
       v_rows = static_cast<uint16_t*>(take(bytes_kv));
       attn_bytes = pc_frame_attn_workspace_bytes_for(dtype, Hq, Hkv, Nq, Nk, D);
+      if (weights) {
+        attn_bytes = std::max(attn_bytes, std::max(pc_score_workspace_bytes(Hq, Hkv, Nq, Nk, 0), pc_score_workspace_bytes(Hq, Hkv, Nq, Nk, 1)));
+        score = static_cast<float*>(take(static_cast<int64_t>(Hkv) * Nk * 4));
+      }
       attn_ws = take(attn_bytes);
     } else {
       row_tiles = rows <= 16 ? 1 : 2;
       const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 16 * row_tiles)) * Hkv;
       const int steps = ceil_div(Nk, kStep);
-      int64_t want = std::max<int64_t>(1, 512 / tiles);
-      want = std::min<int64_t>(want, ceil_div(steps, kWaves));
+      keep_logits = weights && rows <= (steps <= 3 * kWaves ? kLogitRowsFewKeys : kLogitRows);
+      // One round of work-groups, each with a step per wave at least.  Joining shares is a launch (3.8 us), a step of all
+      // waves 1.1 (bf16) to 2 us: up to three of them are not cut, unless the weights need that launch anyway.
+      int64_t want = std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), ceil_div(steps, kWaves));
+      if (steps <= 3 * kWaves && !keep_logits) want = 1;
       n_splits = ceil_div(steps, ceil_div(steps, static_cast<int>(std::min<int64_t>(want, kMaxShares))));
       if (n_splits > 1) {
         part_o = static_cast<float*>(take(all * n_splits * D * 4));
         part_ml = static_cast<float2*>(take(all * n_splits * 8));
       }
-      keep_logits = weights && rows <= kLogitRows;
       if (keep_logits) logits = static_cast<float*>(take(all * steps * kStep * 4));
     }
     if (weights) lse = static_cast<float*>(take(all * 4));
@@ -787,8 +825,6 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
              PC_ERR_WORKSPACE, "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, plan.bytes, ws_bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const float c = scale * 1.4426950408889634f;
-  WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, kWeighKeys)), q_stride_h, weights_stride_h,
-                 c, decay, 1.f, plan.lse, weights};
   if (plan.expand) {
     // rows as they lie in the cache, so that one launch's worth of copying serves every query row
     const int64_t per = static_cast<int64_t>(Nk) * D;
@@ -797,32 +833,48 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
     if (int rc = pc_frame_attn(Q, plan.k_rows, plan.v_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, o_stride_h, scale, O, e,
                                plan.attn_ws, plan.attn_bytes, stream))
       return rc;
-    w.lse = e;
-    w.lse_mul = 1.4426950408889634f;
+    if (weights == nullptr) return PC_OK;
+    if (int rc = pc_score(Q, plan.k_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, nullptr, scale, e, Nq, plan.score, Nk,
+                          Hsel != Hkv, 0, 0, plan.attn_ws, plan.attn_bytes, stream))
+      return rc;
+    q4_add_kernel<<<dim3(ceil_div(Nk, 256), Hsel), 256, 0, s>>>(weights, weights_stride_h, plan.score, Nk, decay);
+    PC_CHECK_LAUNCH(who);
+    return PC_OK;
   }
   auto run = [&](auto zero, auto dims) -> int {
     using T = decltype(zero);
     constexpr int kDims = decltype(dims)::value;
     const T* q = static_cast<const T*>(Q);
-    if (!plan.expand) {
-      const int tiles_q = ceil_div(rows, 16 * plan.row_tiles), steps = ceil_div(Nk, kStep);
-      const AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, ceil_div(steps, plan.n_splits),
-                          q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.logits,
-                          static_cast<int64_t>(Hkv) * rows};
-      const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
-      kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
+    const int tiles_q = ceil_div(rows, 16 * plan.row_tiles), steps = ceil_div(Nk, kStep);
+    const AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, ceil_div(steps, plan.n_splits),
+                        q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.logits,
+                        static_cast<int64_t>(Hkv) * rows};
+    const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
+    kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
+    PC_CHECK_LAUNCH(who);
+    const int blocks = ceil_div(Nk, 4 * kJoinThreads);
+    const JoinArgs j = {plan.n_splits, rows, Hkv, Hsel, Nk, plan.n_splits > 1 ? static_cast<int>(a.rows_all) : 0, Divisor(blocks),
+                        static_cast<int64_t>(steps) * kStep, weights_stride_h, c, decay, weights};
+    const int grid = j.row_blocks + (plan.keep_logits ? blocks * Hsel : 0);
+    if (grid > 0) {
+      q4_join_kernel<T, kDims><<<grid, kJoinThreads, 0, s>>>(static_cast<T*>(O), a, j);
       PC_CHECK_LAUNCH(who);
-      const int blocks = ceil_div(Nk, 4 * kJoinThreads);
-      const JoinArgs j = {plan.n_splits, rows, Hkv, Hsel, Nk, plan.n_splits > 1 ? static_cast<int>(a.rows_all) : 0, Divisor(blocks),
-                          static_cast<int64_t>(steps) * kStep, weights_stride_h, c, decay, weights};
-      const int grid = j.row_blocks + (plan.keep_logits ? blocks * Hsel : 0);
-      if (grid > 0) {
-        q4_join_kernel<T, kDims><<<grid, kJoinThreads, 0, s>>>(static_cast<T*>(O), a, j);
-        PC_CHECK_LAUNCH(who);
-      }
     }
     if (weights != nullptr && !plan.keep_logits) {
-      q4_weigh_kernel<T, kDims><<<w.by_blocks.d * Hsel, kThreads, 0, s>>>(q, w);
+      // 128 keys per wave where that leaves most of the chip's 1,024 SIMDs one; else waves share keys until there are two
+      // per SIMD.  Work-groups of few waves where keys are few: the chip has room for them side by side.
+      const int64_t wide = static_cast<int64_t>(ceil_div(Nk, 128)) * Hsel, narrow = static_cast<int64_t>(ceil_div(Nk, 64)) * Hsel;
+      const int keys = sizeof(T) == 2 && wide >= 448 ? 128 : 64;      // (fp32 queries in three parts leave no registers for it)
+      int dealt = 1;
+      while (keys == 64 && dealt < kWaves && 16 * dealt < rows && narrow * dealt < 2048) dealt *= 2;
+      int groups = 1;           // powers of two: a compute unit holds eight waves of the widest form
+      while (groups * dealt < kWaves && (keys == 128 ? wide : narrow) >= 1024 * groups) groups *= 2;
+      const WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, groups * keys)), dealt,
+                           q_stride_h, weights_stride_h, c, decay, plan.lse, weights};
+      auto weigh = q4_weigh_kernel<T, kDims, 4>;
+      if constexpr (sizeof(T) == 2)
+        if (keys == 128) weigh = q4_weigh_kernel<T, kDims, 8>;
+      weigh<<<w.by_blocks.d * Hsel, 64 * groups * dealt, 0, s>>>(q, w);
       PC_CHECK_LAUNCH(who);
     }
     return PC_OK;
