@@ -17,6 +17,7 @@ import torch
 
 import paper_2601_04359_amd as pk
 from oracle import q4_oracle as orc
+from paper_2601_04359_amd.rollout import EvictingStack
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -185,6 +186,35 @@ def test_attn_weights(dtype, weights, Hq, Hkv, Nq, Nk, D, decay):
     check_attn(dtype, Hq, Hkv, Nq, Nk, D, weights=weights, decay=decay, lse=Nk % 2 == 0)
 
 
+@pytest.mark.parametrize("weights", [None, "each", "one"])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk,gaps,decay", [
+    (4, 1, 192, 33, 0, 1.0), (8, 2, 200, 300, 0, 0.9), (6, 2, 257, 1000, 5, 0.0), (4, 1, 1000, 1, 0, 0.5), (16, 4, 193, 130, 3, 2.0),
+    (2, 2, 800, 515, 0, 1.0), (2, 2, 767, 400, 1, 0.3)])
+def test_attn_many_rows(weights, Hq, Hkv, Nq, Nk, gaps, decay):
+    """On both sides of the 768 rows per KV head from which on the cache is turned into bf16 rows."""
+    check_attn("bf16", Hq, Hkv, Nq, Nk, 128, weights=weights, decay=decay, q_gap=gaps, head_gap=gaps, lse=weights != "one")
+
+
+@pytest.mark.parametrize("Nq", [200, 400])
+def test_attn_many_rows_hard(Nq):
+    """Climbing logits, hidden keys and values that are not numbers, in the form for many rows."""
+    Hq, Hkv, Nk, D = 8, 2, 500, 128
+    rng = np.random.default_rng(6)
+    K, Q = rng.standard_normal((Hkv, Nk, D)) * 0.1, rng.standard_normal((Hq, Nq, D)) * 0.1
+    K[..., 0], Q[..., 0] = np.linspace(0, 6, Nk), 1000.0
+    check_attn("bf16", Hq, Hkv, Nq, Nk, D, K=K, Q=Q, weights="each")
+    hidden = np.arange(Nk) % 50 != 17
+    K, Q = rng.standard_normal((Hkv, Nk, D)), rng.standard_normal((Hq, Nq, D))
+    K[:, :, 127], K[:, :, 96:127], Q[..., 127] = np.where(hidden, -6.0, 0.0), 0.0, 2.0 ** 100
+    _, _, w = check_attn("bf16", Hq, Hkv, Nq, Nk, D, K=K, Q=Q, weights="each", decay=0.0, visible=~hidden)
+    assert (w[:, :Nk][:, torch.from_numpy(hidden).to(DEV)] == 0).all()
+    V = rng.standard_normal((Hkv, Nk, D))
+    V[1, 3, 70] = np.nan
+    O = pk.pc_q4_attn(torch.randn((Hq, Nq, D), device=DEV).to(torch.bfloat16), packed(rng.standard_normal((Hkv, Nk, D)), V), Nk, 0.1)
+    bad = torch.isnan(O)
+    assert bad[4:, :, 64:96].all() and not bad[4:, :, :64].any() and not bad[4:, :, 96:].any() and not bad[:4].any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Nq", [1, 30, 150])
 def test_attn_long(dtype, Nq):
@@ -349,3 +379,201 @@ def test_evict_nothing():
     assert pk.pc_evict(data, data.clone(), None, w, 10, 0) == 0 and pk.pc_evict(data, data.clone(), None, w, 0, 4) == 0
     with pytest.raises(pk.PackCacheError):
         pk.pc_evict(data, data.clone(), None, w, 10, 10, idx=torch.empty((2, 10), dtype=torch.int32, device=DEV))
+
+
+# ------------------------------------------------------------------------------ the calls together
+def test_offsets_beyond_32_bits():
+    """A cache whose rows pass 2^31 and whose heads pass 2^32 bytes: 36 million rows of 64 bytes, two heads.  All keys are
+    zero but for a few far apart that every query looks at."""
+    H, Nk, D = 2, 36_000_000, 128
+    cache = tuple(torch.zeros((H, Nk, w), dtype=torch.uint8, device=DEV) for w in (D // 2, D // 32) * 2)
+    rows = torch.tensor([5, 17_000_000, 33_600_000, Nk - 1], device=DEV)
+    K = torch.zeros((H, 4, D), device=DEV)
+    K[..., 3] = 6.0
+    V = torch.arange(4, device=DEV)[None, :, None] % 2 * 2.0 + torch.arange(H, device=DEV)[:, None, None] * 4.0 + torch.zeros((H, 4, D), device=DEV)
+    small = pk.q4_cache(H, 4, D)
+    pk.pc_q4_store(K, V, small, 0)
+    for big, part in zip(cache, small):
+        big[:, rows] = part
+    Q = torch.zeros((H, 1, D), device=DEV)
+    Q[..., 3] = 20.0
+    lse, w = torch.zeros((H, 1), device=DEV), torch.zeros((H, Nk), device=DEV)
+    O = pk.pc_q4_attn(Q, cache, Nk, 1.0, lse=lse, weights=w)
+    # logits 120 against 0: the others' mass is 36e6 e^-120
+    assert torch.allclose(O, V.mean(1, keepdim=True), atol=1e-5) and torch.allclose(lse, torch.full_like(lse, 120 + np.log(4)), rtol=1e-6)
+    assert torch.allclose(w[:, rows], torch.full((H, 4), 0.25, device=DEV), rtol=1e-5)
+    w[:, 20:1020] = 1e-3      # and they are what an eviction keeps
+    left = pk.pc_q4_evict(cache, None, w, Nk, 1004)
+    want = torch.cat([torch.tensor([5], device=DEV), rows[1:], ])
+    assert left == 1004 and torch.allclose(w[:, :1020].sum(1), torch.full((2,), 1.0 + 1000 * 1e-3 + 16 * 1e-3, device=DEV), rtol=1e-3)
+    Ko, Vo = (torch.empty((H, 1004, D), device=DEV) for _ in range(2))
+    pk.pc_q4_load(cache, 0, Ko, Vo)
+    assert torch.equal((Ko[..., 3] == 6.0).sum(1), torch.full((H,), len(want), device=DEV))
+    one = torch.empty((H, 1, D), device=DEV)
+    pk.pc_q4_load(cache, Nk - 1, V=one)
+    assert torch.equal(one, V[:, 3:])
+    pk.pc_q4_store(K[:, :1], V[:, 1:2], cache, Nk - 2)
+    pk.pc_q4_load(cache, Nk - 2, V=one)
+    assert torch.equal(one, V[:, 1:2])
+
+
+@pytest.mark.parametrize("Nq", [1, 30, 300])
+def test_both_halves_of_the_binding_give_the_same_bits(monkeypatch, Nq):
+    from paper_2601_04359_amd import binding
+    H, Hq, D, n = 2, 6, 128, 200
+    x = [torch.randn((H, n, D), device=DEV).to(torch.bfloat16) for _ in range(2)]
+    Q = torch.randn((Hq, Nq, D), device=DEV).to(torch.bfloat16)
+    new = torch.arange(3 * n, dtype=torch.int32, device=DEV).view(n, 3)
+    results = []
+    for native in (True, False):
+        assert pk.lib() and binding._NATIVE
+        with monkeypatch.context() as m:
+            if not native:
+                m.setattr(binding, "_NATIVE", False)
+            cache, pos, w = pk.q4_cache(H, n + 4, D), torch.zeros((H, n + 4, 3), dtype=torch.int32, device=DEV), torch.ones((H, n + 4), device=DEV)
+            pk.pc_q4_store(*x, cache, 2, new, pos, w)
+            O, lse = torch.empty_like(Q), torch.empty((Hq, Nq), device=DEV)
+            assert pk.pc_q4_attn(Q, cache, n + 2, 0.1, O=O, lse=lse, weights=w, decay=0.5) is O
+            idx = torch.empty((H, 77), dtype=torch.int32, device=DEV)
+            assert pk.pc_q4_evict(cache, pos, w, n + 2, 77, n_anchor=3, recent_t=20, idx=idx) == 77
+            K, V = torch.empty((H, 77, D), device=DEV), torch.empty((H, 77, D), device=DEV)
+            assert pk.pc_q4_load(cache, 0, K, V) == (K, V)
+            rows_k, rows_v = x[0].clone(), x[1].clone()
+            w2 = w[:, :n].contiguous()
+            assert pk.pc_evict(rows_k, rows_v, None, w2, n, 50) == 50
+            results.append([*cache, pos, w, O, lse, idx, K, V, rows_k, rows_v, w2])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def step_inputs(rng, layers, Hq, Hkv, n, D, t):
+    K, V = (torch.from_numpy(rng.standard_normal((layers, Hkv, n, D))).to(torch.bfloat16).to(DEV) for _ in range(2))
+    Q = torch.from_numpy(rng.standard_normal((layers, Hq, n, D)) * 2).to(torch.bfloat16).to(DEV)
+    pos = torch.stack([torch.arange(t, t + n), torch.arange(n) % 3, torch.arange(n) % 5], 1).int().to(DEV)
+    return K, V, Q, pos
+
+
+@pytest.mark.parametrize("share", [False, True])
+@pytest.mark.parametrize("budget", [45, 24])
+@pytest.mark.parametrize("n,n_anchor,recent,decay", [(1, 4, 6, 1.0), (3, 0, 0, 0.9), (7, 10, 14, 0.5)])
+def test_stack_step_by_step(share, n, n_anchor, recent, decay, budget):
+    """A prompt and a dozen steps of two layers; each step is checked from the state the device holds when it begins."""
+    layers, Hq, Hkv, D = 2, 8, 2, 128
+    rng = np.random.default_rng(n)
+    s = EvictingStack(layers, Hq, Hkv, D, budget, D ** -0.5, step_rows=20, n_anchor=n_anchor, recent_t=recent, decay=decay,
+                      share_heads=share)
+    hsel = 1 if share else Hkv
+    t = 0
+    for step in range(12):
+        rows_in = 20 if step == 0 else n
+        K, V, Q, pos = step_inputs(rng, layers, Hq, Hkv, rows_in, D, t)
+        t += rows_in
+        w_before, before = f64(s.weights), s.nk
+        for layer in range(layers):
+            s.append(layer, K[layer], V[layer], pos)
+            O = s.attend(layer, Q[layer], q_pos=pos)
+            cache, p, w = s.layer(layer)
+            nk = before + rows_in
+            assert torch.equal(p[:, before:nk], pos.expand(hsel, rows_in, 3))
+            Kv, Vv = cache_values(cache, nk)
+            for x, v, c, sc in ((K, Kv, cache[0], cache[1]), (V, Vv, cache[2], cache[3])):
+                codes, scales = orc.q4_store(f64(x[layer]))        # the rotated keys, as they lie in K now
+                assert np.array_equal(c[:, before:nk].cpu().numpy(), codes) and np.array_equal(sc[:, before:nk].cpu().numpy(), scales)
+            want, _, mass = orc.attn(f64(Q[layer]), Kv, Vv, s.scale)
+            spread = orc.attn(f64(Q[layer]), Kv, np.abs(Vv), s.scale)[0]
+            assert np.all(np.abs(f64(O) - want) <= 2.0 ** -8 * (np.abs(want) + spread) + 1e-4 * spread)
+            mass = mass.sum(0, keepdims=True) if share else mass
+            old = decay * w_before[layer * hsel:(layer + 1) * hsel, :nk]
+            old[:, before:] = 0
+            assert np.allclose(f64(w[:, :nk]), old + mass, rtol=1e-4, atol=1e-7)
+        state = [x.clone() for x in (*s.cache, s.pos, s.weights)]
+        left = s.end_step()
+        nk = before + rows_in
+        assert left == s.nk == min(nk, budget)
+        for sel in range(layers * hsel):
+            src = orc.evict_rows(state[5][sel].cpu().numpy(), state[4][sel, :, 0].cpu().numpy(), nk, left, n_anchor, recent)
+            src = torch.from_numpy(src).to(DEV)
+            per = Hkv // hsel
+            for h in range(sel * per, (sel + 1) * per):
+                for a, b in zip(s.cache, state):
+                    assert torch.equal(a[h, :left], b[h][src])
+            assert torch.equal(s.pos[sel, :left], state[4][sel][src]) and torch.equal(s.weights[sel, :left], state[5][sel][src])
+    assert s.nk == min(20 + 11 * n, budget)
+
+
+@pytest.mark.parametrize("n,budget", [(1, 700), (5, 90), (210, 400)])
+def test_stack_step_in_a_graph(n, budget):
+    """A step of the full cache, recorded once and replayed with eager work in between, leaves what eager steps leave."""
+    layers, Hq, Hkv, D = 2, 8, 2, 128
+    rng = np.random.default_rng(8)
+    args = (layers, Hq, Hkv, D, budget, D ** -0.5)
+    kw = dict(step_rows=max(n, budget), n_anchor=8, recent_t=4, decay=0.97)
+    a, b = EvictingStack(*args, **kw), EvictingStack(*args, **kw)
+    K, V, Q, pos = step_inputs(rng, layers, Hq, Hkv, budget, D, 0)
+    for s in (a, b):
+        for layer in range(layers):
+            s.append(layer, K[layer].clone(), V[layer], pos)
+        s.end_step()
+    ins = [x.clone() for x in step_inputs(rng, layers, Hq, Hkv, n, D, 0)]
+    Oa = torch.empty_like(ins[2])
+
+    def one(s, K, V, Q, pos, O):
+        for layer in range(layers):
+            s.append(layer, K[layer], V[layer], pos)
+            s.attend(layer, Q[layer], O=O[layer], q_pos=pos)
+        assert s.end_step() == budget
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):            # the eager side first: nothing is lazily set up inside the capture
+        outs = []
+        fresh = [step_inputs(np.random.default_rng(50 + i), layers, Hq, Hkv, n, D, budget + i * n) for i in range(4)]
+        for x in fresh:
+            K, V, Q, pos = (y.clone() for y in x)
+            O = torch.empty_like(Q)
+            one(b, K, V, Q, pos, O)
+            outs.append((O.clone(), *[y.clone() for y in (*b.cache, b.pos, b.weights)]))
+    torch.cuda.current_stream().wait_stream(stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one(a, *ins, Oa)
+    for x, want in zip(fresh, outs):
+        for to, y in zip(ins, x):
+            to.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((Oa, *a.cache, a.pos, a.weights), want):
+            assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))
+        torch.randn((100, 100), device=DEV) @ torch.randn((100, 100), device=DEV)
+        torch.cuda.synchronize()
+
+
+def test_calls_on_two_streams_do_not_meet():
+    """Attention with weights and eviction of two caches at once, each on a stream of its own."""
+    def work(seed):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        cache = tuple(torch.randint(100, 130, (4, 30000, b), dtype=torch.uint8, device=DEV, generator=g) for b in (64, 4) * 2)
+        Q = torch.empty((8, 3, 128), device=DEV, dtype=torch.bfloat16).normal_(generator=g)
+        return cache, Q, torch.zeros((4, 30000), device=DEV)
+
+    def run(state):
+        cache, Q, w = state
+        outs = []
+        for k in range(6):
+            outs.append(pk.pc_q4_attn(Q, cache, 30000 - 100 * k, 0.05, weights=w, decay=0.9))
+            pk.pc_q4_evict(cache, None, w, 30000 - 100 * k, 29900 - 100 * k)
+        return [*outs, *cache, w]
+
+    want = [run(work(s)) for s in (1, 2)]
+    torch.cuda.synchronize()
+    states, got = [work(s) for s in (1, 2)], []
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in states]
+    for st, stream in zip(states, streams):
+        with torch.cuda.stream(stream):
+            got.append(run(st))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
