@@ -303,7 +303,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
 constexpr int kSlice = 4096, kMaxSlices = 512, kItemsOfSlice = kSlice / kSelThreads;
 
 struct Slices {
-  int n, rows;                // slices, rows of one (a multiple of kSlice)
+  int n, rows, row_bits;      // slices, rows of one (a multiple of kSlice), bits of a row number
+  Divisor by_rows;
   uint32_t* ranks;            // [Hsel][Nk]
   int32_t* hist;              // [Hsel][n][kTopBins]
   uint64_t* candidates;       // [Hsel][Nk]
@@ -312,13 +313,14 @@ struct Slices {
   uint32_t* cut;              // [Hsel][2]: rank and row: rows of a higher rank stay, of this rank up to this row
 };
 
-// A row whose rank lies in the threshold's bin, in the order by rank (its other 21 bits), then row, lower rows above
-constexpr int kRest = 32 - kTopBits, kRowBits = 30;
-__device__ __forceinline__ uint64_t candidate(uint32_t rank, int row) {
-  return static_cast<uint64_t>(rank & ((1u << kRest) - 1)) << kRowBits | static_cast<uint32_t>((1 << kRowBits) - 1 - row);
+// A row whose rank lies in the threshold's bin, in the order by rank (its other 21 bits), then row, lower rows above;
+// row_bits of them hold any row of the call.
+constexpr int kRest = 32 - kTopBits;
+__device__ __forceinline__ uint64_t candidate(uint32_t rank, int row, int row_bits) {
+  return static_cast<uint64_t>(rank & ((1u << kRest) - 1)) << row_bits | static_cast<uint32_t>((1 << row_bits) - 1 - row);
 }
-__device__ __forceinline__ int row_of(uint64_t candidate) {
-  return (1 << kRowBits) - 1 - static_cast<int>(candidate & ((1u << kRowBits) - 1));
+__device__ __forceinline__ int row_of(uint64_t candidate, int row_bits) {
+  return (1 << row_bits) - 1 - static_cast<int>(candidate & ((1u << row_bits) - 1));
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_count_kernel(Ranks a, Slices s) {
@@ -366,18 +368,22 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
   };
   fetch();
   {
-    static_assert(kTopBins == 2 * kSelThreads, "two bins per thread");
-    u32x2 c = {0, 0};
-    const u32x2* from = reinterpret_cast<const u32x2*>(all) + threadIdx.x;
-    for (int k0 = 0; k0 < s.n; k0 += 16) {
-      u32x2 v[16];
+    // the slices' counts: half of the threads each, four bins per thread, twelve slices in flight
+    static_assert(kTopBins == 2 * kSelThreads, "four bins per thread of a half");
+    const int half = threadIdx.x >= kSelThreads / 2, quad = threadIdx.x % (kSelThreads / 2);
+    const u32x4* from = reinterpret_cast<const u32x4*>(all) + quad;
+    u32x4 c = {0, 0, 0, 0};
+    for (int k0 = half; k0 < s.n; k0 += 24) {
+      u32x4 v[12];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = from[min(k0 + k, s.n - 1) * kSelThreads];
+      for (int k = 0; k < 12; ++k) v[k] = from[static_cast<int64_t>(min(k0 + 2 * k, s.n - 1)) * (kTopBins / 4)];
 #pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (k0 + k < s.n) c += v[k];
+      for (int k = 0; k < 12; ++k)
+        if (k0 + 2 * k < s.n) c += v[k];
     }
-    reinterpret_cast<u32x2*>(hist)[threadIdx.x] = c;
+    if (half) reinterpret_cast<u32x4*>(hist)[quad] = c;
+    __syncthreads();
+    if (!half) reinterpret_cast<u32x4*>(hist)[quad] += c;
   }
   if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
   __syncthreads();
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
         int at = 0;
         if (lane == 0) at = atomicAdd(&s_at, __popcll(b));
         at = __builtin_amdgcn_readfirstlane(at);
-        if (open) out[lanes_below(b, at)] = candidate(key[i], static_cast<int>(j));
+        if (open) out[lanes_below(b, at)] = candidate(key[i], static_cast<int>(j), s.row_bits);
       }
     }
     r0 += kSlice;
@@ -443,9 +449,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
   for (int k = threadIdx.x; k < s.n; k += kSelThreads) s_holes[k] = decided[k * 2], s_movers[k] = decided[k * 2 + 1];
   uint64_t prefix = 0;
   bool whole = n == left;
-  // 11, 10 and three times 10 bits
-  for (int shift = kRest + kRowBits; !whole && shift > 0;) {
-    const int bits = shift == kRest + kRowBits ? 11 : 10, upper = shift;
+  // 11 and 10 bits of the rank, up to 11 at a time of the row
+  for (int shift = kRest + s.row_bits; !whole && shift > 0;) {
+    const int bits = shift > s.row_bits ? (shift - s.row_bits > 10 ? 11 : 10) : min(11, shift), upper = shift;
     shift -= bits;
     __syncthreads();
     for (int b = threadIdx.x; b < 2048; b += kSelThreads) hist[b] = 0;
@@ -461,10 +467,10 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
   }
   __syncthreads();
   each([&](uint64_t o) {
-    const int row = row_of(o);
+    const int row = row_of(o, s.row_bits);
     const bool stays = o >= prefix;
-    if (row < a.n_keep && !stays) atomicAdd(&s_holes[row / s.rows], 1);
-    if (row >= a.n_keep && stays) atomicAdd(&s_movers[row / s.rows], 1);
+    if (row < a.n_keep && !stays) atomicAdd(&s_holes[s.by_rows.of(row)], 1);
+    if (row >= a.n_keep && stays) atomicAdd(&s_movers[s.by_rows.of(row)], 1);
   });
   __syncthreads();
   // where the slices' holes and movers begin: a wave each, 64 slices at a time
@@ -478,8 +484,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
     }
     if (wave == 0 && lane == 0) {
       counts[sel] = before;
-      s.cut[sel * 2] = bin << kRest | static_cast<uint32_t>(prefix >> kRowBits);
-      s.cut[sel * 2 + 1] = row_of(prefix);
+      s.cut[sel * 2] = bin << kRest | static_cast<uint32_t>(prefix >> s.row_bits);
+      s.cut[sel * 2 + 1] = row_of(prefix, s.row_bits);
     }
   }
 }
@@ -539,7 +545,7 @@ struct EvictPlan {
   int32_t *counts, *lists;
   Slices s;
   size_t bytes;
-  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), s() {
+  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), s{0, 0, 0, Divisor(1)} {
     size_t at = 0;
     auto take = [&](size_t n) {
       void* p = static_cast<uint8_t*>(base) + at;
@@ -552,7 +558,9 @@ struct EvictPlan {
     if (Nk > kMaxInRegisters) {
       slice_rows = kSlice * ceil_div(ceil_div(Nk, kSlice), kMaxSlices);
       n_slices = ceil_div(Nk, slice_rows);
-      s = {n_slices, slice_rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+      int row_bits = 1;
+      while ((1ll << row_bits) < Nk) ++row_bits;
+      s = {n_slices, slice_rows, row_bits, Divisor(slice_rows), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
       s.ranks = static_cast<uint32_t*>(take(heads * Nk * 4));
       s.hist = static_cast<int32_t*>(take(heads * n_slices * kTopBins * 4));
       s.candidates = static_cast<uint64_t*>(take(heads * Nk * 8));
