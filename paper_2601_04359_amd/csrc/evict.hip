@@ -15,6 +15,7 @@ namespace pc {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSlice = 4096, kMaxSlices = 512, kItemsOfSlice = kSlice / kSelThreads;     // of rows beyond one work-group's
 constexpr int kTopBits = 11, kTopBins = 1 << kTopBits;     // of a rank, looked at first
 
 struct Ranks {
@@ -292,6 +293,162 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
 }
 
 // ------------------------------------------------------------------------------------------
+// Few rows leave (a cache at its budget that takes a token or a few per step): they are found one after another as
+// the least of all, at one barrier each (0.56 us; 1.2 in two launches), where a threshold takes three counted passes:
+// 4 heads losing one of 3,000 rows 8.3 -> 4.9 us, of 24,000 28 -> 8.2, of 193,792 50 -> 12.4; 112 heads one of 8,321 17.9 -> 13.3.
+// Two launches, for caches beyond the registers and where work-groups of 4,096 rows are half of the chip at most: those
+// find the least of theirs, and a work-group per selection head the least of these (8,321 rows of 4 heads 8.0 us, 8.7 in
+// one launch; of 112 heads 15.2 and 13.3).
+// ------------------------------------------------------------------------------------------
+constexpr int kFew = 8;
+// up to four rows of any cache, up to eight of more than 16,384 rows (eight of 1,180 rows 8.4 us one by one, 7.2 by a threshold)
+inline bool few_leave(int Nk, int n_keep) { return Nk - n_keep <= (Nk > 16 * kSelThreads ? kFew : kFew / 2); }
+
+// The row that leaves first: lowest rank, of equal ones the highest row; row -1: none.
+struct Least {
+  uint32_t rank;
+  int row;
+  __device__ __forceinline__ void take(uint32_t other_rank, int other_row) {
+    if (other_row >= 0 && (row < 0 || other_rank < rank || (other_rank == rank && other_row > row))) rank = other_rank, row = other_row;
+  }
+};
+__device__ __forceinline__ Least wave_least(Least x) {
+  auto least = [](int a, int b) { return static_cast<int>(min(static_cast<uint32_t>(a), static_cast<uint32_t>(b))); };
+  // a lane without a row has the highest rank there is, and loses to any row of that rank
+  const uint32_t rank = x.row < 0 ? 0xffffffffu : x.rank;
+  const uint32_t lowest = __builtin_amdgcn_readlane(wave_scan(static_cast<int>(rank), -1, least), 63);
+  const int row = wave_scan(rank == lowest ? x.row : -1, -1, [](int a, int b) { return max(a, b); });
+  return {lowest, __builtin_amdgcn_readlane(row, 63)};
+}
+// of the work-group, in every thread; s: an entry per wave, not used by the call before
+__device__ __forceinline__ Least block_least(Least x, Least* s) {
+  const int lane = threadIdx.x & 63;
+  x = wave_least(x);
+  if (lane == 0) s[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return wave_least(lane < kSelWaves ? s[lane] : Least{0, -1});
+}
+
+// The rows that leave, in any order, become holes and movers, both ascending; by one wave.  Returns how many.
+__device__ __forceinline__ int pair_few(const int (&out)[kFew], int Nk, int n_keep, int32_t* holes, int32_t* movers) {
+  const int lane = threadIdx.x & 63, n_out = Nk - n_keep;
+  int mine = INT_MAX, before = 0;
+#pragma unroll
+  for (int k = 0; k < kFew; ++k)
+    if (k == lane && k < n_out) mine = out[k];
+  const bool hole = mine < n_keep;
+  bool leaves = false;
+#pragma unroll
+  for (int k = 0; k < kFew; ++k) {
+    before += k < n_out && out[k] < mine;
+    leaves |= k < n_out && out[k] == n_keep + lane;
+  }
+  if (hole) holes[before] = mine;            // rows below a hole that leave are holes
+  const uint64_t kept = __ballot(lane < n_out && !leaves);
+  if (kept >> lane & 1) movers[lanes_below(kept, 0)] = n_keep + lane;
+  return __popcll(__ballot(hole));
+}
+
+// Ends both forms: the pairs, and the rows' moves or what the launch that makes them reads.
+__device__ __forceinline__ void finish_few(const int (&out)[kFew], const Ranks& a, int sel, int room, int32_t* counts,
+                                           int32_t* lists, const Moves& m, int move) {
+  __shared__ int32_t s_lists[2 * kFew], s_n;
+  if (threadIdx.x < 64) {
+    const int n = pair_few(out, a.Nk, a.n_keep, s_lists, s_lists + kFew);
+    if (threadIdx.x == 0) s_n = n;
+  }
+  __threadfence_block();       // rows of idx that this work-group wrote lie before the ones that the moves write
+  __syncthreads();
+  const int n = s_n;
+  if (!move) {
+    int32_t* to = lists + static_cast<int64_t>(sel) * 2 * room;
+    if (static_cast<int>(threadIdx.x) < n) {
+      to[threadIdx.x] = s_lists[threadIdx.x];
+      to[room + threadIdx.x] = s_lists[kFew + threadIdx.x];
+    }
+    if (threadIdx.x == 0) counts[sel] = n;
+    return;
+  }
+  for (int h = sel * m.per; h < (sel + 1) * m.per; ++h) {
+    move_rows(m, h, n, s_lists, s_lists + kFew, threadIdx.x, kSelThreads);
+    move_book(m, h, sel, n, s_lists, s_lists + kFew, threadIdx.x, kSelThreads);
+  }
+}
+
+// With `least` (slices of 64 kItems x 16 rows in grid.x) the slice's leavers go there, else they leave at once.
+template <int kItems>
+__global__ __launch_bounds__(kSelThreads) void evict_few_kernel(Ranks a, int room, int32_t* __restrict__ counts,
+                                                                int32_t* __restrict__ lists, Moves m, int move, Least* least) {
+  __shared__ Least s_least[kFew][kSelWaves];
+  const int sel = blockIdx.y, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const HeadRanks head(a, sel);
+  const int64_t j0 = (static_cast<int64_t>(blockIdx.x) * kSelWaves + wave) * 64 * kItems + lane;
+  HeadRanks::Row row[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) row[i] = head.fetch(static_cast<int>(min(j0 + i * 64, static_cast<int64_t>(a.Nk) - 1)));
+  const int64_t border = head.border();
+  uint32_t key[kItems], there = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int64_t j = j0 + i * 64;
+    key[i] = head.rank(row[i], static_cast<int>(j), border);
+    if (j < a.Nk) there |= 1u << i;
+    if (m.idx != nullptr && j < a.n_keep) m.idx[sel * m.idx_stride_h + j] = static_cast<int32_t>(j);
+  }
+  const int n_out = a.Nk - a.n_keep;
+  int out[kFew] = {};
+  Least mine = {0, -1};
+  auto look = [&] {            // the lane's rows ascend: of equal ranks the last one wins
+    mine = {0, -1};
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if ((there >> i & 1) && (mine.row < 0 || key[i] <= mine.rank)) mine = {key[i], static_cast<int>(j0) + i * 64};
+  };
+  look();
+#pragma unroll
+  for (int k = 0; k < kFew; ++k) {
+    if (k >= n_out) break;
+    const Least x = block_least(mine, s_least[k]);
+    out[k] = x.row;
+    if (least != nullptr && threadIdx.x == 0) least[(static_cast<int64_t>(sel) * gridDim.x + blockIdx.x) * n_out + k] = x;
+    if (x.row >= 0 && x.row == mine.row) {      // its lane looks at its others
+      there &= ~(1u << ((x.row - j0) >> 6));
+      look();
+    }
+  }
+  if (least == nullptr) finish_few(out, a, sel, room, counts, lists, m, move);
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_few_join_kernel(Ranks a, int room, int32_t* __restrict__ counts,
+                                                                     int32_t* __restrict__ lists, Moves m, int move,
+                                                                     const Least* __restrict__ least, int n_least) {
+  __shared__ Least s_least[kFew][kSelWaves];
+  const int sel = blockIdx.x, n_out = a.Nk - a.n_keep;
+  const Least* from = least + static_cast<int64_t>(sel) * n_least;
+  int out[kFew] = {};
+  Least mine = {0, -1};
+  auto look = [&](int n_gone) {
+    mine = {0, -1};
+    for (int c = threadIdx.x; c < n_least; c += kSelThreads) {
+      const Least x = from[c];
+      bool gone = false;
+#pragma unroll
+      for (int p = 0; p < kFew; ++p) gone |= p < n_gone && x.row == out[p];
+      if (!gone) mine.take(x.rank, x.row);
+    }
+  };
+  look(0);
+#pragma unroll
+  for (int k = 0; k < kFew; ++k) {
+    if (k >= n_out) break;
+    out[k] = block_least(mine, s_least[k]).row;
+    if (out[k] == mine.row) look(k + 1);
+  }
+  finish_few(out, a, sel, room, counts, lists, m, move);
+}
+
+// ------------------------------------------------------------------------------------------
 // More rows: slices of them, a work-group each, in four launches.
 //   count    ranks (written out: the rows' t lies 12 bytes apart) and the slice's counts of the top bits
 //   gather   the bin that the threshold lies in; rows above and below it are decided, rows in it are
@@ -300,8 +457,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
 //   resolve  a work-group per selection head: the cut, and where every slice's holes and movers begin
 //   place    the lists
 // ------------------------------------------------------------------------------------------
-constexpr int kSlice = 4096, kMaxSlices = 512, kItemsOfSlice = kSlice / kSelThreads;
-
 struct Slices {
   int n, rows, row_bits;      // slices, rows of one (a multiple of kSlice), bits of a row number
   Divisor by_rows;
@@ -542,10 +697,12 @@ constexpr int64_t kMoveWithSelect = 64 << 10;     // bytes that a work-group of 
 // What a call keeps in its workspace; `base` may be NULL where only the size is asked for.
 struct EvictPlan {
   int room, n_slices, slice_rows;       // room: of a list; n_slices 0: one work-group per selection head
+  bool few;                             // rows that leave are found one by one
   int32_t *counts, *lists;
+  Least* least;                         // of few and several slices: [Hsel][n_slices][rows that leave]
   Slices s;
   size_t bytes;
-  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), s{0, 0, 0, Divisor(1)} {
+  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), few(few_leave(Nk, n_keep)), least(nullptr), s{0, 0, 0, Divisor(1)} {
     size_t at = 0;
     auto take = [&](size_t n) {
       void* p = static_cast<uint8_t*>(base) + at;
@@ -555,7 +712,11 @@ struct EvictPlan {
     const size_t heads = Hsel;
     counts = static_cast<int32_t*>(take(heads * 4));
     lists = static_cast<int32_t*>(take(heads * 2 * room * 4));
-    if (Nk > kMaxInRegisters) {
+    const int64_t pieces = ceil_div(Nk, kSlice);
+    if (few && Nk > kSlice && (Nk > kMaxInRegisters || pieces * Hsel <= 128)) {
+      n_slices = static_cast<int>(pieces);
+      least = static_cast<Least*>(take(heads * n_slices * (Nk - n_keep) * sizeof(Least)));
+    } else if (!few && Nk > kMaxInRegisters) {
       slice_rows = kSlice * ceil_div(ceil_div(Nk, kSlice), kMaxSlices);
       n_slices = ceil_div(Nk, slice_rows);
       int row_bits = 1;
@@ -600,9 +761,25 @@ int evict(const char* who, Moves m, int64_t row_bytes, int H, int32_t* pos, int6
   PC_REQUIRE(units <= INT_MAX - (1 << 22), PC_ERR_SHAPE, "%s: %d rows may move in one call", who, plan.room);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Ranks a = {weights, pos, w_stride_h, pos_stride_h, Nk, n_keep, n_anchor, recent_t};
-  if (plan.n_slices == 0) {
-    const int move = plan.room * row_bytes * m.per <= kMoveWithSelect;
-    const int items = ceil_div(Nk, kSelThreads);
+  const int move = plan.room * row_bytes * m.per <= kMoveWithSelect, items = ceil_div(Nk, kSelThreads);
+  if (plan.few && plan.n_slices > 0) {
+    evict_few_kernel<kItemsOfSlice><<<dim3(plan.n_slices, Hsel), kSelThreads, 0, s>>>(a, plan.room, plan.counts, plan.lists, m, 0, plan.least);
+    PC_CHECK_LAUNCH(who);
+    evict_few_join_kernel<<<Hsel, kSelThreads, 0, s>>>(a, plan.room, plan.counts, plan.lists, m, move, plan.least,
+                                                       plan.n_slices * (Nk - n_keep));
+    PC_CHECK_LAUNCH(who);
+    if (move) return PC_OK;
+  } else if (plan.few) {
+    const auto kernel = items <= 2    ? evict_few_kernel<2>
+                        : items <= 4  ? evict_few_kernel<4>
+                        : items <= 8  ? evict_few_kernel<8>
+                        : items <= 12 ? evict_few_kernel<12>
+                        : items <= 16 ? evict_few_kernel<16>
+                                      : evict_few_kernel<24>;
+    kernel<<<dim3(1, Hsel), kSelThreads, 0, s>>>(a, plan.room, plan.counts, plan.lists, m, move, nullptr);
+    PC_CHECK_LAUNCH(who);
+    if (move) return PC_OK;
+  } else if (plan.n_slices == 0) {
     const auto kernel = items <= 2    ? evict_select_kernel<2>
                         : items <= 4  ? evict_select_kernel<4>
                         : items <= 6  ? evict_select_kernel<6>

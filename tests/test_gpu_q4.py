@@ -355,6 +355,25 @@ def test_evict_weights_that_tie(Nk, what):
         check_evict("q4", 2, 2, Nk, n_keep, w=np.stack([w, np.roll(w, 7)]))
 
 
+@pytest.mark.parametrize("Nk", [5, 64, 1030, 4096, 4097, 8321, 24576, 24577, 30000, 100001])
+@pytest.mark.parametrize("n_out", [1, 2, 3, 4, 5, 8, 9])
+def test_evict_few(Nk, n_out):
+    """A token or a few leave: found one by one up to eight, with ties, protected rows and rows of the newest among them."""
+    rng = np.random.default_rng(Nk + n_out)
+    if n_out >= Nk:
+        return
+    w = rng.integers(0, max(2, Nk // 3), (3, Nk)) * 0.5
+    w[1] = rng.choice([np.nan, 0.0, -0.0, 1.0, np.inf], Nk)
+    w[2, -n_out:] = -1.0                   # all that leave lie behind n_keep: nothing moves
+    t = np.stack([np.arange(Nk), rng.integers(0, 9, Nk), np.arange(Nk)])
+    check_evict("q4", 3, 3, Nk, Nk - n_out, w=w, t=t, n_anchor=min(2, Nk - n_out), recent_t=0 if n_out == 2 else 2)
+    check_evict("bf16", 6, 3, Nk, Nk - n_out, w=w, with_pos=False, with_idx=n_out % 2 == 0)
+    if Nk in (1030, 30000):
+        check_evict("f32", 60, 1, Nk, Nk - n_out, D=128, w=w[:1])      # too much to move in the same launch
+        check_evict("bf16", 2, 2, Nk, Nk - n_out, n_anchor=Nk - n_out, w=w[:2])     # every row below n_keep an anchor
+        check_evict("q4", 1, 1, Nk, Nk - n_out, w=w[:1], t=np.zeros((1, Nk)), recent_t=1)     # every row recent
+
+
 @pytest.mark.parametrize("Nk,n_keep,n_anchor,recent_t", [
     (50, 20, 20, 0), (50, 20, 0, 1), (50, 20, 5, 30), (50, 3, 3, 1000), (9000, 40, 10, 5), (9000, 8999, 4000, 2 ** 31 - 1)])
 @pytest.mark.parametrize("order", ["up", "same", "mixed", "far"])
