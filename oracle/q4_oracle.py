@@ -26,23 +26,18 @@ def q4_nearest(v: float) -> int:
 def q4_store(x):
     """x [..][D] -> (codes uint8 [..][D/2], scale bytes uint8 [..][D/32])."""
     x = np.asarray(x, np.float64)
-    flat = x.reshape(-1, x.shape[-1] // 32, 32)
-    codes = np.zeros(flat.shape, np.uint8)
-    scales = np.zeros(flat.shape[:2], np.uint8)
+    groups = x.reshape(-1, 32)
+    bad = ~np.all(np.isfinite(groups), -1)
+    v = np.where(bad[:, None], 0.0, groups)
+    largest = 7.0 * 2.0 ** np.arange(-120.0, 126.0)                 # that a group may hold, by its exponent
+    e = np.minimum(np.searchsorted(largest, np.max(np.abs(v), -1), "left"), 245) - 120
     borders = (GRID[1:] + GRID[:-1]) / 2
-    for i in range(flat.shape[0]):
-        for g in range(flat.shape[1]):
-            v = flat[i, g]
-            if not np.all(np.isfinite(v)):
-                scales[i, g] = 255
-                continue
-            e = q4_scale_exponent(np.max(np.abs(v)))
-            scales[i, g] = e + 127
-            a = np.abs(v) / 2.0 ** e
-            low, high = np.searchsorted(borders, a, "left"), np.searchsorted(borders, a, "right")
-            codes[i, g] = np.where(low % 2 == 0, low, high) + 8 * np.signbit(v)   # low < high only on a border
-    codes = codes.reshape(x.shape)
-    return codes[..., 0::2] | (codes[..., 1::2] << 4), scales.reshape(x.shape[:-1] + (-1,))
+    a = np.abs(v) / 2.0 ** e[:, None].astype(np.float64)
+    low, high = np.searchsorted(borders, a, "left"), np.searchsorted(borders, a, "right")
+    codes = np.where(low % 2 == 0, low, high) + 8 * np.signbit(v)   # low < high only on a border
+    codes = np.where(bad[:, None], 0, codes).astype(np.uint8).reshape(x.shape)
+    scales = np.where(bad, 255, e + 127).astype(np.uint8).reshape(x.shape[:-1] + (-1,))
+    return codes[..., 0::2] | (codes[..., 1::2] << 4), scales
 
 
 def q4_load(codes, scales):

@@ -40,6 +40,9 @@ def test_oracle_codes_are_the_nearest():
                                    (7 * 2.0 ** -120, -120), (8 * 2.0 ** -120, -119), (3.4e38, 125), (7 * 2.0 ** 124, 124)])
 def test_oracle_scale(top, e):
     assert orc.q4_scale_exponent(top) == e
+    x = np.zeros((1, 32))
+    x[0, 5] = -top
+    assert orc.q4_store(x)[1][0, 0] == e + 127
 
 
 def test_oracle_round_trip_error():
