@@ -170,15 +170,15 @@ template <typename T, int D>
 struct QueryFrags {
   static constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kSteps = D / 32;
   bf16x8 f[kSteps][kParts];
-  // the row's dims g D/4 + 8 b .. + 7
-  __device__ __forceinline__ void load(const T* row, int g) {
+  // the row's dims g D/4 + 8 b .. + 7, from its 16-byte chunks
+  template <class Chunk>
+  __device__ __forceinline__ void from(Chunk&& chunk, int g) {
 #pragma unroll
     for (int b = 0; b < kSteps; ++b) {
-      const T* src = row + g * (D / 4) + b * 8;
       if constexpr (kParts == 1) {
-        f[b][0] = *reinterpret_cast<const bf16x8*>(src);
+        f[b][0] = __builtin_bit_cast(bf16x8, chunk(g * (D / 32) + b));
       } else {
-        const f32x4 x = load_f32x4(src), y = load_f32x4(src + 4);
+        const f32x4 x = __builtin_bit_cast(f32x4, chunk(g * (D / 16) + 2 * b)), y = __builtin_bit_cast(f32x4, chunk(g * (D / 16) + 2 * b + 1));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           __bf16 hi, mid, lo;
@@ -188,15 +188,23 @@ struct QueryFrags {
       }
     }
   }
+  __device__ __forceinline__ void load(const T* row, int g) {
+    from([&](int c) { return load_chunk(row + c * (16 / static_cast<int>(sizeof(T)))); }, g);
+  }
+  // fp32 rows only promise element alignment; the hardware takes 16-byte accesses at any dword
+  static __device__ __forceinline__ u32x4 load_chunk(const T* p) {
+    if constexpr (kParts == 1) return *reinterpret_cast<const u32x4*>(p);
+    else return __builtin_bit_cast(u32x4, load_f32x4(p));
+  }
 };
 
-// A lane's piece of a key row: D/8 bytes of codes, as D/32 dwords.
+// A lane's piece of a key row: D/8 bytes of codes, as D/32 dwords; `row` is counted from the bases.
 template <int D>
 struct KeyCodes {
   uint32_t w[D / 32];
   int byte;
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t row, int g) {
-    const uint8_t* src = codes + row * (D / 2) + g * (D / 8);
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, uint32_t row, int g) {
+    const uint8_t* src = codes + (row * (D / 2) + g * (D / 8));
     if constexpr (D == 128) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(src);
       w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
@@ -246,26 +254,63 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
   KeyCodes<D> raw_k[2];
   u32x4 raw_v[kVLoads];
   int raw_s[kVLoads];
-  auto fetch = [&](int step) {
-    const int64_t k0 = static_cast<int64_t>(step) * kStep;
+  // From the step's first row by scalar bases; the lanes' offsets are the same in every step but the one with the last row,
+  // which stands for those that are not there.
+  auto fetch_rows = [&](const uint8_t* kcs, const uint8_t* kss, const uint8_t* vcs, const uint8_t* vss, uint32_t last) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) raw_k[t].load(kc, ks, min(k0 + t * 16 + r, static_cast<int64_t>(a.Nk) - 1), g);
+    for (int t = 0; t < 2; ++t) raw_k[t].load(kcs, kss, min(static_cast<uint32_t>(t * 16 + r), last), g);
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i) {
-      const int64_t row = min(k0 + i * kVRows + lane / kGroups, static_cast<int64_t>(a.Nk) - 1);
-      raw_v[i] = *reinterpret_cast<const u32x4*>(vc + row * (D / 2) + lane % kGroups * 16);
-      raw_s[i] = vs[row * kGroups + lane % kGroups];
+      const uint32_t row = min(static_cast<uint32_t>(i * kVRows + lane / kGroups), last);
+      raw_v[i] = *reinterpret_cast<const u32x4*>(vcs + (row * (D / 2) + lane % kGroups * 16));
+      raw_s[i] = vss[row * kGroups + lane % kGroups];
     }
   };
-  int step = split * a.share_steps + wave;
-  if (step < step_end) fetch(step);
-
+  auto fetch = [&](int step) {
+    const int64_t k0 = static_cast<int64_t>(step) * kStep;
+    const uint8_t *kcs = kc + k0 * (D / 2), *kss = ks + k0 * kGroups, *vcs = vc + k0 * (D / 2), *vss = vs + k0 * kGroups;
+    if (k0 + kStep <= a.Nk) fetch_rows(kcs, kss, vcs, vss, kStep - 1);
+    else fetch_rows(kcs, kss, vcs, vss, static_cast<uint32_t>(a.Nk - 1 - k0));
+  };
+  // The queries are fetched in front of the first codes: loads end in order, and a wait for queries behind codes would be a
+  // wait for both (in the loop, where the compiler puts it, it made every step wait for the next one's codes).  Two tiles
+  // of them go through LDS, a few chunks per thread: as fragments every wave would fetch both, 64 KB per work-group in
+  // front of the codes (8/2 heads x 64 rows x 4,000 keys 12.6 -> 11.9 us); one tile is quicker without the barrier
+  // (16/4 x 1 x 41,800 11.9 -> 11.4).
+  auto row_of = [&](int i) {
+    const int rho = min(tile * kRT * 16 + i, n_rows - 1), head = a.by_nq.of(rho);
+    return Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D;
+  };
   QueryFrags<T, D> q[kRT];
+  int step = split * a.share_steps + wave;
+  if constexpr (kRT == 1) {
+    q[0].load(row_of(r), g);
+    asm volatile("" ::: "memory");
+    if (step < step_end) fetch(step);
+  } else {
+    constexpr int kOfChunk = 16 / static_cast<int>(sizeof(T)), kRowChunks = D / kOfChunk, kChunks = 16 * kRT * kRowChunks;
+    constexpr int kPerThread = kChunks / kThreads > 0 ? kChunks / kThreads : 1;
+    static_assert(kChunks % kThreads == 0 || kChunks < kThreads, "whole rounds of chunks");
+    __shared__ __align__(16) uint8_t smem_q[kChunks * 16];
+    lds_byte* s_q = (lds_byte*)smem_q;
+    auto place = [](int row, int c) { return (row * kRowChunks + (c ^ (row & (kRowChunks < 16 ? kRowChunks - 1 : 15)))) * 16; };
+    u32x4 chunk[kPerThread];
 #pragma unroll
-  for (int rt = 0; rt < kRT; ++rt) {
-    const int rho = min((tile * kRT + rt) * 16 + r, n_rows - 1);
-    const int head = a.by_nq.of(rho);
-    q[rt].load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
+    for (int k = 0; k < kPerThread; ++k) {
+      const int c = (static_cast<int>(threadIdx.x) + k * kThreads) % kChunks;
+      chunk[k] = QueryFrags<T, D>::load_chunk(row_of(c / kRowChunks) + c % kRowChunks * kOfChunk);
+    }
+    asm volatile("" ::: "memory");
+    if (step < step_end) fetch(step);
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+      const int c = static_cast<int>(threadIdx.x) + k * kThreads;
+      if (c < kChunks) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(s_q + place(c / kRowChunks, c % kRowChunks)) = chunk[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < kRT; ++rt)
+      q[rt].from([&](int c) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(s_q + place(rt * 16 + r, c)); }, g);
   }
   f32x4 o[kRT][D / 16];
   float m[kRT], l[kRT];
@@ -306,6 +351,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
 #pragma unroll
       for (int t = 0; t < 2; ++t) s[t] = scores<T, D>(kf[t], q[rt]);
       if (k0 + kStep > a.Nk) {
+        asm volatile("" ::: "memory");     // a branch, not 24 selects in every step
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -566,6 +612,7 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
   const int row_wave = wave & (a.dealt - 1), step = 16 * a.dealt;
   const int groups = blockDim.x / 64 / a.dealt;
   const int block0 = block * groups * kKeys, k0 = block0 + wave / a.dealt * kKeys;
+  const int k_first = min(k0, a.Nk - 1);      // the last work-group's waves may lie behind the last key
   const int n_rows = a.rep * a.by_nq.d, per = a.Hkv / a.Hsel;
   float sum[kTiles] = {};
   for (int kvh = sel * per; kvh < (sel + 1) * per; ++kvh) {
@@ -573,8 +620,9 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       KeyCodes<D> raw;
-      raw.load(a.cache.k_codes + kvh * a.cache.code_stride_h, a.cache.k_scales + kvh * a.cache.scale_stride_h,
-               min(k0 + t * 16 + r, a.Nk - 1), g);
+      raw.load(a.cache.k_codes + (kvh * a.cache.code_stride_h + static_cast<int64_t>(k_first) * (D / 2)),
+               a.cache.k_scales + (kvh * a.cache.scale_stride_h + static_cast<int64_t>(k_first) * (D / 32)),
+               min(t * 16 + r, a.Nk - 1 - k_first), g);
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) kf[t][b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
     }
