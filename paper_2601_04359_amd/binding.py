@@ -602,6 +602,14 @@ def q4_cache(Hkv: int, cap: int, D: int, device="cuda:0"):
     return tuple(torch.zeros((Hkv, cap, w), dtype=torch.uint8, device=device) for w in (D // 2, D // 32) * 2)
 
 
+def _rows_follow(t, name: str) -> None:
+    """As _rows_dense; where there is one row, what lies between rows does not matter ([1][H][D] seen as [H][1][D])."""
+    if t.shape[-2] > 1:
+        return _rows_dense(t, name)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise PackCacheError(-2, f"{name}: the last dimension must be contiguous")
+
+
 def _on_device(**tensors) -> None:
     """Calls go to the current device's stream: everything has to be there."""
     import torch
@@ -663,8 +671,8 @@ def pc_q4_store(K, V, cache, row0: int, pos_new=None, pos=None, weights=None) ->
     if K.shape != V.shape or K.dim() != 3 or K.shape[0] != H or K.shape[2] != D or K.dtype != V.dtype:
         raise PackCacheError(-2, f"K and V must be [{H}][n][{D}] of one type, got {tuple(K.shape)} and {tuple(V.shape)}")
     n = K.shape[1]
-    _rows_dense(K, "K")
-    _rows_dense(V, "V")
+    _rows_follow(K, "K")
+    _rows_follow(V, "V")
     if row0 < 0 or row0 + n > cap:
         raise PackCacheError(-2, f"rows {row0} .. {row0 + n} of a cache of {cap}")
     if (pos is None) != (pos_new is None):
@@ -694,7 +702,7 @@ def pc_q4_load(cache, row0: int, K=None, V=None):
         if t is not None:
             if tuple(t.shape) != (H, n, D) or t.dtype != some.dtype:
                 raise PackCacheError(-2, f"{name} must be [{H}][n][{D}], both of one type, got {tuple(t.shape)}")
-            _rows_dense(t, name)
+            _rows_follow(t, name)
     if row0 < 0 or row0 + n > cap:
         raise PackCacheError(-2, f"rows {row0} .. {row0 + n} of a cache of {cap}")
     _on_device(K=K, V=V)
@@ -721,12 +729,12 @@ def pc_q4_attn(Q, cache, Nk: int, scale: float, O=None, lse=None, weights=None, 
     if Q.dim() != 3 or Q.shape[2] != D or Q.shape[0] % Hkv:
         raise PackCacheError(-2, f"Q must be [a multiple of {Hkv}][Nq][{D}], got {tuple(Q.shape)}")
     Hq, Nq, _ = Q.shape
-    _rows_dense(Q, "Q")
+    _rows_follow(Q, "Q")
     if O is None:
         O = torch.empty((Hq, Nq, D), dtype=Q.dtype, device=Q.device)
     if tuple(O.shape) != (Hq, Nq, D) or O.dtype != Q.dtype:
         raise PackCacheError(-2, f"O must be [{Hq}][{Nq}][{D}] of Q's type, got {O.dtype} {tuple(O.shape)}")
-    _rows_dense(O, "O")
+    _rows_follow(O, "O")
     if not 1 <= Nk <= cap:
         raise PackCacheError(-2, f"Nk = {Nk} of a cache of {cap} rows")
     if lse is not None and (tuple(lse.shape) != (Hq, Nq) or not lse.is_contiguous() or lse.dtype != torch.float32):
@@ -790,7 +798,7 @@ def pc_evict(K, V, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, recent
     _on_device(K=K, V=V)
     _check(lib().pc_evict(K.data_ptr(), V.data_ptr(), _dtype_code(K), H, D, K.stride(0), V.stride(0), _ptr(pos),
                           0 if pos is None else pos.stride(0), weights.data_ptr(), weights.stride(0), hsel, int(Nk), int(n_keep),
-                          int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+                          int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws), 0 if ws is None else ws.nbytes, _stream()))
     return min(Nk, n_keep)
 
 
@@ -805,5 +813,5 @@ def pc_q4_evict(cache, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, re
     hsel, idx_stride, ws = _evict_book(pos, weights, H, cap, Nk, n_keep, idx, ws, cache[0])
     _check(lib().pc_q4_evict(C.byref(q4), H, D, _ptr(pos), 0 if pos is None else pos.stride(0), weights.data_ptr(),
                              weights.stride(0), hsel, int(Nk), int(n_keep), int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws),
-                             0 if ws is None else ws.numel(), _stream()))
+                             0 if ws is None else ws.nbytes, _stream()))
     return min(Nk, n_keep)

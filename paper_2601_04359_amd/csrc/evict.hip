@@ -458,8 +458,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_few_join_kernel(Ranks a, in
 //   place    the lists
 // ------------------------------------------------------------------------------------------
 struct Slices {
-  int n, rows, row_bits;      // slices, rows of one (a multiple of kSlice), bits of a row number
-  Divisor by_rows;
+  int n, rows, rows_log2, row_bits;      // slices, rows of one (kSlice times a power of two), bits of a row number
   uint32_t* ranks;            // [Hsel][Nk]
   int32_t* hist;              // [Hsel][n][kTopBins]
   uint64_t* candidates;       // [Hsel][Nk]
@@ -586,7 +585,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_gather_kernel(Ranks a, Slic
 __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Slices s, int32_t* __restrict__ counts) {
   constexpr int kHeld = 12;          // candidates of a thread that stay in registers; more are read again each time
   __shared__ int hist[2048], s_wave[kSelWaves], s_found[3], s_holes[kMaxSlices], s_movers[kMaxSlices];
-  const int sel = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int sel = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t* cand = s.candidates + static_cast<int64_t>(sel) * a.Nk;
   int32_t* decided = s.decided + static_cast<int64_t>(sel) * s.n * 2;
   const uint32_t bin = s.head[sel * 4];
@@ -621,12 +621,23 @@ __global__ __launch_bounds__(kSelThreads) void evict_resolve_kernel(Ranks a, Sli
     whole = s_found[2] == left;
   }
   __syncthreads();
-  each([&](uint64_t o) {
-    const int row = row_of(o, s.row_bits);
+  // candidates lie slice by slice, so a wave's are of one slice or two: one addition for all of a slice's
+  auto tally = [&](uint64_t o, bool there) {
+    const int row = row_of(o, s.row_bits), slice = row >> s.rows_log2;
     const bool stays = o >= prefix;
-    if (row < a.n_keep && !stays) atomicAdd(&s_holes[s.by_rows.of(row)], 1);
-    if (row >= a.n_keep && stays) atomicAdd(&s_movers[s.by_rows.of(row)], 1);
-  });
+    const bool hole = there && row < a.n_keep && !stays, mover = there && row >= a.n_keep && stays;
+    for (uint64_t todo = __ballot(hole || mover); todo != 0;) {
+      const int at = __builtin_amdgcn_readlane(slice, __builtin_ctzll(todo));
+      const uint64_t h = __ballot(hole && slice == at), m = __ballot(mover && slice == at);
+      if (lane == 0 && h != 0) atomicAdd(&s_holes[at], __popcll(h));
+      if (lane == 0 && m != 0) atomicAdd(&s_movers[at], __popcll(m));
+      todo &= ~(h | m);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (i * kSelThreads + wave * 64 < n) tally(held[i], i * kSelThreads + static_cast<int>(threadIdx.x) < n);
+  for (int c = kHeld * kSelThreads + threadIdx.x; c - lane < n; c += kSelThreads) tally(cand[min(c, n - 1)], c < n);
   __syncthreads();
   // where the slices' holes and movers begin: a wave each, 64 slices at a time
   if (wave < 2) {
@@ -702,7 +713,7 @@ struct EvictPlan {
   Least* least;                         // of few and several slices: [Hsel][n_slices][rows that leave]
   Slices s;
   size_t bytes;
-  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), few(few_leave(Nk, n_keep)), least(nullptr), s{0, 0, 0, Divisor(1)} {
+  EvictPlan(int Hsel, int Nk, int n_keep, void* base) : room(std::min(Nk - n_keep, n_keep)), n_slices(0), slice_rows(0), few(few_leave(Nk, n_keep)), least(nullptr), s() {
     size_t at = 0;
     auto take = [&](size_t n) {
       void* p = static_cast<uint8_t*>(base) + at;
@@ -717,11 +728,14 @@ struct EvictPlan {
       n_slices = static_cast<int>(pieces);
       least = static_cast<Least*>(take(heads * n_slices * (Nk - n_keep) * sizeof(Least)));
     } else if (!few && Nk > kMaxInRegisters) {
-      slice_rows = kSlice * ceil_div(ceil_div(Nk, kSlice), kMaxSlices);
+      int rows_log2 = 12;
+      static_assert(kSlice == 1 << 12, "the least slice");
+      while (((Nk - 1) >> rows_log2) >= kMaxSlices) ++rows_log2;
+      slice_rows = 1 << rows_log2;
       n_slices = ceil_div(Nk, slice_rows);
       int row_bits = 1;
       while ((1ll << row_bits) < Nk) ++row_bits;
-      s = {n_slices, slice_rows, row_bits, Divisor(slice_rows), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+      s = {n_slices, slice_rows, rows_log2, row_bits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
       s.ranks = static_cast<uint32_t*>(take(heads * Nk * 4));
       s.hist = static_cast<int32_t*>(take(heads * n_slices * kTopBins * 4));
       s.candidates = static_cast<uint64_t*>(take(heads * Nk * 8));

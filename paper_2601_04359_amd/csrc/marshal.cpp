@@ -377,6 +377,10 @@ struct Place {
     return true;
   }
 };
+// rows dense, or one row: what would lie between rows does not matter then
+bool rows_follow(const at::Tensor& t) {
+  return t.dim() == 3 && (t.size(2) <= 1 || t.stride(2) == 1) && (t.size(1) <= 1 || t.stride(1) == t.size(2));
+}
 bool optional(PyObject* o, const at::Tensor** t) { return o == Py_None || (*t = plain(o)) != nullptr; }
 void* pointer(const at::Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
 
@@ -441,8 +445,8 @@ PyObject* q4_store(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // K, V
   Book book;
   int32_t row0;
   int n;
-  PLAIN_OR_NONE(K && V && cache.from(a[2]) && as_int(a[3], &row0) && optional(a[4], &fresh) && rows_dense(*K, 3) &&
-                rows_dense(*V, 3) && K->sizes() == V->sizes() && K->scalar_type() == V->scalar_type() &&
+  PLAIN_OR_NONE(K && V && cache.from(a[2]) && as_int(a[3], &row0) && optional(a[4], &fresh) && rows_follow(*K) &&
+                rows_follow(*V) && K->sizes() == V->sizes() && K->scalar_type() == V->scalar_type() &&
                 K->size(0) == cache.H && K->size(2) == cache.D && size_as_int(K->size(1), &n) && row0 >= 0 &&
                 static_cast<int64_t>(row0) + n <= cache.cap &&
                 book.from(a[5], a[6], cache.H, static_cast<int64_t>(row0) + n) && !fresh == !book.pos);
@@ -473,7 +477,7 @@ PyObject* q4_load(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // cache
   int n;
   PLAIN_OR_NONE(some.dim() == 3 && size_as_int(some.size(1), &n) && row0 >= 0 && static_cast<int64_t>(row0) + n <= cache.cap);
   for (const at::Tensor* t : {K, V})
-    PLAIN_OR_NONE(!t || (rows_dense(*t, 3) && t->size(0) == cache.H && t->size(1) == n && t->size(2) == cache.D &&
+    PLAIN_OR_NONE(!t || (rows_follow(*t) && t->size(0) == cache.H && t->size(1) == n && t->size(2) == cache.D &&
                          t->scalar_type() == some.scalar_type()));
   const int dt = dtype_code(some);
   Place at;
@@ -497,7 +501,7 @@ PyObject* q4_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // Q, ca
   double scale, decay;
   int Hq, Nq;
   PLAIN_OR_NONE(Q && O && cache.from(a[1]) && as_int(a[2], &Nk) && as_double(a[3], &scale) && optional(a[5], &lse) &&
-                as_double(a[7], &decay) && optional(a[8], &ws) && rows_dense(*Q, 3) && rows_dense(*O, 3) &&
+                as_double(a[7], &decay) && optional(a[8], &ws) && rows_follow(*Q) && rows_follow(*O) &&
                 O->sizes() == Q->sizes() && O->scalar_type() == Q->scalar_type() && Q->size(2) == cache.D && cache.H > 0 &&
                 size_as_int(Q->size(0), &Hq) && size_as_int(Q->size(1), &Nq) && Hq % cache.H == 0 && Nk >= 1 &&
                 Nk <= cache.cap && book.from(Py_None, a[6], cache.H, Nk));

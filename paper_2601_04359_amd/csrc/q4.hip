@@ -856,6 +856,7 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
              "%s: Hq=%d must be a positive multiple of Hkv=%d, Nq=%d and Nk=%d at least 1", who, Hq, Hkv, Nq, Nk);
   PC_REQUIRE(scale > 0.f && isfinite(scale), PC_ERR_SHAPE, "%s: scale %g must be > 0", who, scale);
   PC_REQUIRE(Q && O, PC_ERR_NULL, "%s: Q or O is NULL", who);
+  PC_REQUIRE(Q != O, PC_ERR_SHAPE, "%s: O may not be Q: the weights read the queries again", who);
   if (int rc = check_q4_cache(cache, D, who)) return rc;
   if (int rc = check_q4_span(cache, Hkv, 0, Nk, D, who)) return rc;
   PC_REQUIRE(Hq == 1 || (q_stride_h >= static_cast<int64_t>(Nq) * D && o_stride_h >= static_cast<int64_t>(Nq) * D), PC_ERR_SHAPE,

@@ -465,6 +465,30 @@ def test_both_halves_of_the_binding_give_the_same_bits(monkeypatch, Nq):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_one_row_of_any_stride(monkeypatch, native):
+    """One token's heads as a projection leaves them, [1][H][D], seen as [H][1][D]."""
+    from paper_2601_04359_amd import binding
+    assert pk.lib() and binding._NATIVE
+    if not native:
+        monkeypatch.setattr(binding, "_NATIVE", False)
+    H, Hq, D = 4, 8, 128
+    x = torch.randn((3, 1, Hq, D), device=DEV).to(torch.bfloat16)
+    K, V, Q = (t.transpose(0, 1) for t in (x[0, :, :H], x[1, :, 3:3 + H], x[2]))
+    a, b = pk.q4_cache(H, 3, D), pk.q4_cache(H, 3, D)
+    pk.pc_q4_store(K, V, a, 1)
+    pk.pc_q4_store(K.contiguous(), V.contiguous(), b, 1)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+    out = torch.zeros((1, Hq, D), device=DEV, dtype=torch.bfloat16)
+    pk.pc_q4_attn(Q, a, 2, 0.1, O=out.transpose(0, 1))
+    assert torch.equal(out.transpose(0, 1), pk.pc_q4_attn(Q.contiguous(), b, 2, 0.1))
+    k = torch.zeros((1, H, D), device=DEV)
+    pk.pc_q4_load(a, 1, K=k.transpose(0, 1))
+    assert torch.equal(k.transpose(0, 1), pk.pc_q4_load(b, 1, K=torch.zeros((H, 1, D), device=DEV))[0])
+    with pytest.raises(pk.PackCacheError):
+        pk.pc_q4_store(x[0, 0, :H, ::2][:, None], x[0, 0, :H, ::2][:, None], pk.q4_cache(H, 3, 64), 0)      # dims apart
+
+
 def step_inputs(rng, layers, Hq, Hkv, n, D, t):
     K, V = (torch.from_numpy(rng.standard_normal((layers, Hkv, n, D))).to(torch.bfloat16).to(DEV) for _ in range(2))
     Q = torch.from_numpy(rng.standard_normal((layers, Hq, n, D)) * 2).to(torch.bfloat16).to(DEV)

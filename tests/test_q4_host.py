@@ -101,7 +101,7 @@ def load(L, **kw):
 
 
 def attn(L, **kw):
-    a = dict(Q=A, cache=cache(), dtype=1, Hq=8, Hkv=4, Nq=1, Nk=1000, D=128, qs=1 << 20, os=1 << 20, scale=0.1, O=A, lse=None,
+    a = dict(Q=A + 4096, cache=cache(), dtype=1, Hq=8, Hkv=4, Nq=1, Nk=1000, D=128, qs=1 << 20, os=1 << 20, scale=0.1, O=A, lse=None,
              w=None, wst=0, Hsel=0, decay=1.0, ws=A, ws_bytes=1 << 40, stream=None)
     a.update(kw)
     return L.pc_q4_attn(*a.values())
@@ -152,7 +152,7 @@ def test_load_refuses(L, kw, status):
     (dict(Nk=(1 << 30) + 1), SHAPE), (dict(Hq=2 ** 20, Hkv=2 ** 20, Nq=2 ** 20), SHAPE), (dict(scale=0.0), SHAPE),
     (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE), (dict(Q=None), NULL), (dict(O=None), NULL),
     (dict(Nq=5, qs=4 * 128), SHAPE), (dict(Nq=5, os=4 * 128), SHAPE), (dict(qs=132), SHAPE), (dict(O=A + 4), SHAPE),
-    (dict(dtype=0, Q=A + 1), SHAPE), (dict(Nk=1 << 20), SHAPE), (dict(w=A, Hsel=2, wst=1000), SHAPE), (dict(w=A, Hsel=0), SHAPE),
+    (dict(Q=A), SHAPE), (dict(dtype=0, Q=A + 1), SHAPE), (dict(Nk=1 << 20), SHAPE), (dict(w=A, Hsel=2, wst=1000), SHAPE), (dict(w=A, Hsel=0), SHAPE),
     (dict(w=A, Hsel=4, wst=999), SHAPE), (dict(w=A, Hsel=1, decay=-0.5), BUDGET), (dict(w=A, Hsel=1, decay=float("nan")), BUDGET),
     (dict(w=A, Hsel=1, decay=float("inf")), BUDGET), (dict(w=A, Hsel=1, ws=None), WORKSPACE), (dict(w=A, Hsel=1, ws=A + 8), WORKSPACE),
     (dict(w=A, Hsel=1, ws_bytes=16), WORKSPACE), (dict(Nk=100000, cache=cache(code_stride_h=1 << 30, scale_stride_h=1 << 26), ws=None), WORKSPACE)])
