@@ -49,6 +49,12 @@ inline int allow_dynamic_lds(const void* kernel, size_t bytes, std::atomic<uint6
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// pc_score; with decay >= 0 (bf16 only) a key's score is added to decay times what stands in its place (0: replaces it).
+int score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs, int Nk, int D, int64_t q_stride_h,
+               int64_t k_stride_h, const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
+               int64_t score_stride_h, int share_heads, int key_begin, int key_end, float decay, void* ws, size_t ws_bytes,
+               void* stream);
+
 // ---- device-side types -----------------------------------------------------------------
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;

@@ -672,16 +672,6 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
   }
 }
 
-// weights = decay * weights + scores, a row of blocks per selection head
-__global__ __launch_bounds__(256) void q4_add_kernel(float* __restrict__ weights, int64_t w_stride_h, const float* __restrict__ score,
-                                                     int Nk, float decay) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= Nk) return;
-  float* w = weights + blockIdx.y * w_stride_h + j;
-  const float x = score[static_cast<int64_t>(blockIdx.y) * Nk + j];
-  *w = decay == 0.f ? x : fmaf(decay, *w, x);
-}
-
 // ------------------------------------------------------------------------------------------
 // host
 // ------------------------------------------------------------------------------------------
@@ -693,7 +683,7 @@ constexpr int kExpandRows = 768;
 struct Q4Plan {
   bool expand, keep_logits;     // the cache as bf16 rows and pc_frame_attn; weights from kept logits
   int row_tiles, n_splits;      // tiles of 16 queries per work-group, key shares
-  float *part_o, *lse, *logits, *score;
+  float *part_o, *lse, *logits;
   float2* part_ml;
   uint16_t *k_rows, *v_rows;
   void* attn_ws;
@@ -714,10 +704,7 @@ struct Q4Plan {
       k_rows = static_cast<uint16_t*>(take(bytes_kv));
       v_rows = static_cast<uint16_t*>(take(bytes_kv));
       attn_bytes = pc_frame_attn_workspace_bytes_for(dtype, Hq, Hkv, Nq, Nk, D);
-      if (weights) {
-        attn_bytes = std::max(attn_bytes, std::max(pc_score_workspace_bytes(Hq, Hkv, Nq, Nk, 0), pc_score_workspace_bytes(Hq, Hkv, Nq, Nk, 1)));
-        score = static_cast<float*>(take(static_cast<int64_t>(Hkv) * Nk * 4));
-      }
+      if (weights) attn_bytes = std::max(attn_bytes, pc_score_workspace_bytes(Hq, Hkv, Nq, Nk, 1));
       attn_ws = take(attn_bytes);
     } else {
       row_tiles = rows <= 16 ? 1 : 2;
@@ -883,12 +870,8 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
                                plan.attn_ws, plan.attn_bytes, stream))
       return rc;
     if (weights == nullptr) return PC_OK;
-    if (int rc = pc_score(Q, plan.k_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, nullptr, scale, e, Nq, plan.score, Nk,
-                          Hsel != Hkv, 0, 0, plan.attn_ws, plan.attn_bytes, stream))
-      return rc;
-    q4_add_kernel<<<dim3(ceil_div(Nk, 256), Hsel), 256, 0, s>>>(weights, weights_stride_h, plan.score, Nk, decay);
-    PC_CHECK_LAUNCH(who);
-    return PC_OK;
+    return score_keys(Q, plan.k_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, nullptr, scale, e, Nq, weights, weights_stride_h,
+                      Hsel != Hkv, 0, 0, decay, plan.attn_ws, plan.attn_bytes, stream);
   }
   auto run = [&](auto zero, auto dims) -> int {
     using T = decltype(zero);

@@ -898,9 +898,13 @@ __device__ __forceinline__ float parts_sum(const float* part, int n_parts, int64
   for (int p = 0; p < kMaxQSplits; ++p) sum += v[p];   // a missing part adds +0: the sum is unchanged
   return sum;
 }
+// What becomes of the value that a sum meets: replaced (decay < 0 or 0), or decay times it is added.
+__device__ __forceinline__ void put_score(float* out, float sum, float decay) {
+  *out = decay > 0.f ? fmaf(decay, *out, sum) : sum;
+}
 // out[h][j] = that sum; with share_heads (n_parts = 1) the heads are summed, head 0 first, into out[j].
 __global__ void score_reduce(const float* __restrict__ part, float* __restrict__ out, int64_t out_stride_h,
-                             int n_parts, int Hkv, int Nk, int share_heads) {
+                             int n_parts, int Hkv, int Nk, int share_heads, float decay) {
   const int j = blockIdx.x * blockDim.x + threadIdx.x;
   if (j >= Nk) return;
   if (share_heads) {
@@ -912,10 +916,11 @@ __global__ void score_reduce(const float* __restrict__ part, float* __restrict__
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[i];
     }
-    out[j] = s;
+    put_score(out + j, s, decay);
   } else {
     const int h = blockIdx.y;
-    out[h * out_stride_h + j] = parts_sum(part, n_parts, static_cast<int64_t>(Hkv) * Nk, static_cast<int64_t>(h) * Nk + j);
+    put_score(out + h * out_stride_h + j,
+              parts_sum(part, n_parts, static_cast<int64_t>(Hkv) * Nk, static_cast<int64_t>(h) * Nk + j), decay);
   }
 }
 // The same for share_heads and several parts: a wave per head (eight at most) and 64 keys per work-group, so that
@@ -925,7 +930,7 @@ __global__ void score_reduce(const float* __restrict__ part, float* __restrict__
 constexpr int kReduceHeads = 8;
 __global__ __launch_bounds__(64 * kReduceHeads) void score_reduce_heads(const float* __restrict__ part,
                                                                         float* __restrict__ out, int n_parts, int Hkv,
-                                                                        int Nk) {
+                                                                        int Nk, float decay) {
   __shared__ float s_sum[kReduceHeads][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6, j = blockIdx.x * 64 + lane;
@@ -939,7 +944,7 @@ __global__ __launch_bounds__(64 * kReduceHeads) void score_reduce_heads(const fl
     if (wave == 0)
       for (int i = 0; i < min(waves, Hkv - h0); ++i) total += s_sum[i][lane];
   }
-  if (wave == 0 && j < Nk) out[j] = total;
+  if (wave == 0 && j < Nk) put_score(out + j, total, decay);
 }
 
 // ---- fp32 tier ------------------------------------------------------------------------------
@@ -1303,11 +1308,10 @@ extern "C" int pc_score_cut(int Hq, int Hkv, int n_qs, int Nk, int n_scored, flo
   return PC_OK;
 }
 
-extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs,
-                        int Nk, int D, int64_t q_stride_h, int64_t k_stride_h,
-                        const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
-                        int64_t score_stride_h, int share_heads, int key_begin, int key_end,
-                        void* ws, size_t ws_bytes, void* stream) {
+int pc::score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs, int Nk, int D, int64_t q_stride_h,
+                   int64_t k_stride_h, const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
+                   int64_t score_stride_h, int share_heads, int key_begin, int key_end, float decay, void* ws,
+                   size_t ws_bytes, void* stream) {
   PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "pc_score: dtype %d", dtype);
   PC_REQUIRE(Hq > 0 && Hkv > 0 && Hq % Hkv == 0, PC_ERR_SHAPE,
              "pc_score: Hq=%d must be a positive multiple of Hkv=%d", Hq, Hkv);
@@ -1375,7 +1379,7 @@ extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hk
       PC_CHECK_LAUNCH("pc_score row pass");
     }
     RowNorm norm = {nullptr, lse, lse_stride_h, q_rows, ws_part, static_cast<int64_t>(Hq) * n_qs, row.n_splits, rep, by_qs};
-    const bool direct = col.n_qsplits == 1 && !share_heads;
+    const bool direct = col.n_qsplits == 1 && !share_heads && decay < 0.f;
     float* col_out = direct ? score_r : ws_col;
     const int64_t col_stride = direct ? score_stride_h : nkr;
     if (!col.prepares) {
@@ -1402,10 +1406,10 @@ extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hk
     if (!direct) {
       if (share_heads && col.n_qsplits > 1)
         score_reduce_heads<<<ceil_div(nkr, 64), 64 * std::min(Hkv, kReduceHeads), 0, s>>>(ws_col, score_r, col.n_qsplits,
-                                                                                         Hkv, nkr);
+                                                                                         Hkv, nkr, decay);
       else
         score_reduce<<<dim3(ceil_div(nkr, 256), share_heads ? 1 : Hkv), 256, 0, s>>>(
-            ws_col, score_r, score_stride_h, col.n_qsplits, Hkv, nkr, share_heads);
+            ws_col, score_r, score_stride_h, col.n_qsplits, Hkv, nkr, share_heads, decay);
       PC_CHECK_LAUNCH("pc_score reduce");
     }
     return PC_OK;
@@ -1424,9 +1428,18 @@ extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hk
                      q_stride_h, k_stride_h, scale, s);
     PC_CHECK_LAUNCH("pc_score passes");
     if (share_heads) {
-      score_reduce<<<ceil_div(nkr, 256), 256, 0, s>>>(ws_col, score + key_begin, score_stride_h, 1, Hkv, nkr, 1);
+      score_reduce<<<ceil_div(nkr, 256), 256, 0, s>>>(ws_col, score + key_begin, score_stride_h, 1, Hkv, nkr, 1, decay);
       PC_CHECK_LAUNCH("pc_score head sum");
     }
   }
   return PC_OK;
+}
+
+extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs,
+                        int Nk, int D, int64_t q_stride_h, int64_t k_stride_h,
+                        const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
+                        int64_t score_stride_h, int share_heads, int key_begin, int key_end,
+                        void* ws, size_t ws_bytes, void* stream) {
+  return score_keys(Qs, K, dtype, Hq, Hkv, n_qs, Nk, D, q_stride_h, k_stride_h, q_rows, scale, lse, lse_stride_h, score,
+                    score_stride_h, share_heads, key_begin, key_end, -1.f, ws, ws_bytes, stream);
 }
