@@ -632,6 +632,8 @@ def _q4_struct(cache):
     if (vc.shape != kc.shape or vs.shape != ks.shape or ks.shape[:2] != kc.shape[:2] or kc.shape[2] != 16 * ks.shape[2]
             or vc.stride(0) != kc.stride(0) or vs.stride(0) != ks.stride(0)):
         raise PackCacheError(-2, "codes [Hkv][cap][D/2] and scales [Hkv][cap][D/32] of K and V must agree in shape and stride")
+    if kc.shape[0] < 1:
+        raise PackCacheError(-2, "a 4-bit cache has at least one head")
     _on_device(k_codes=kc, k_scales=ks, v_codes=vc, v_scales=vs)
     return (_Q4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), kc.stride(0), ks.stride(0)),
             kc.shape[0], kc.shape[1], 2 * kc.shape[2])

@@ -232,3 +232,12 @@ def test_stack_refuses():
     s.n_new = 1
     with pytest.raises(ValueError):
         s.append(1, torch.zeros((2, 2, 128)), torch.zeros((2, 2, 128)), torch.zeros((2, 3), dtype=torch.int32))
+
+
+def test_a_cache_without_heads_is_refused():
+    """Such a cache has no heads to share query heads among: refused before anything divides by their number."""
+    empty = tuple(torch.zeros((0, 8, w), dtype=torch.uint8) for w in (64, 4, 64, 4))
+    with pytest.raises(pk.PackCacheError, match="at least one head"):
+        pk.pc_q4_attn(torch.zeros((2, 1, 128)), empty, 4, 0.1)
+    with pytest.raises(pk.PackCacheError, match="at least one head"):
+        pk.pc_q4_store(torch.zeros((0, 1, 128)), torch.zeros((0, 1, 128)), empty, 0)
