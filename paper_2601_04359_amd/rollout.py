@@ -295,7 +295,7 @@ class EvictingStack:
     Per step:
         append(layer, K, V, pos)   the step's keys (rotated on insertion) and values enter the layer's cache
         attend(layer, Q)           the step's queries over the cache with the new rows in it; every key's
-                                   attention weight is added to its sum (times `decay` per step)
+                                   attention weight is added to `decay` times its sum, in every call
         end_step()                 a cache above its budget loses the rows of least weight, all layers in one call
 
     Rows below n_anchor (the prompt) and rows whose t coordinate is within recent_t of the newest row's are kept
