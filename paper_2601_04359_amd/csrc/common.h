@@ -80,6 +80,22 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return static_cast<uint32_t>(f32_to_bf16(lo)) | (static_cast<uint32_t>(f32_to_bf16(hi)) << 16);
 }
 
+// Softmax exponents.  A probability is 2^(s c - m), m the reference: the largest s c, rounded.  One fma forms the
+// exponent of the product that was not rounded, so the largest key's own is the rounding of m and not 0.  That is as
+// good a reference as long as it is small, but an ulp of a reference beyond 2^31 is more than 2^8: the largest key's
+// probability overflows, or is 0.  Logits of that size belong to keys that a caller hides behind a coordinate of its
+// own; where a row has seen no others, the product is rounded as the reference was.
+constexpr float kFarRef = 0x1p24f;
+__device__ __forceinline__ bool far_ref(float m) { return !(fabsf(m) < kFarRef); }
+__device__ __forceinline__ float far_exponent(float s, float c, float m) {
+  float x;
+  {
+#pragma clang fp contract(off)
+    x = s * c;
+  }
+  return x - m;
+}
+
 // Work-group index -> logical index such that work-groups that land on the same XCD
 // (the hardware deals consecutive work-group ids round-robin over the 8 XCDs, each with
 // its own L2) receive a contiguous range of logical indices.

@@ -9,7 +9,7 @@
 namespace pc {
 namespace {
 
-constexpr float kNoRef = -3.0e38f;     // the reference of a row that has seen no score yet
+constexpr float kNoRef = -3.402823466e38f;     // the reference of a row that has seen no score yet
 
 // ------------------------------------------------------------------------------------------
 // pc_q4_store, pc_q4_load.  Bound: bytes.  A lane owns eight elements, so four lanes are a group and agree on its
@@ -133,7 +133,8 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
 //   * The result leaves lane (q, g) with keys 4 g .. 4 g + 3 of query q, of two tiles of 16: the eight k-slots of
 //     O^T += V^T P^T.  V is converted by the lane that loads it (one scale for its 32 dims) and goes
 //     through LDS of the wave's own as bf16 rows, read back by transposing loads.
-//   * Softmax in base 2 against a reference that lags the maximum by at most 2^8; sums in fp32.
+//   * Softmax in base 2 against a reference that lags the maximum by at most 2^8; sums in fp32.  Far references take
+//     exponents of their own (see far_exponent).
 //   * fp32 queries and probabilities are three bf16 parts each: keys and values are exact in bf16, so the
 //     products are exact and the sums are the fp32 ones.
 // ------------------------------------------------------------------------------------------
@@ -157,6 +158,7 @@ struct AttnArgs {
   float2* part_ml;
   float* lse;                               // natural logarithm, or NULL
   float* lse2;                              // base 2, for the weights, or NULL
+  float2* ref;                              // the same in its two terms: reference and log2 of the sum
   float* logits;                            // [rows_all][whole steps] for the weights of few rows, or NULL
   int64_t rows_all;
 };
@@ -376,9 +378,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
         for (int db = 0; db < D / 16; ++db) o[rt][db] *= alpha;
         m[rt] = m_new;
       }
+      // a far reference's exponents come to the common fma as products of c, with 0 as their reference
+      const bool far = far_ref(m[rt]);
+      const float ref = far ? 0.f : m[rt];
+      if (__any(far)) {
+        const float by = 1.f / a.c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (far) s[i >> 2][i & 3] = far_exponent(s[i >> 2][i & 3], a.c, m[rt]) * by;
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], a.c, -m[rt]));
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], a.c, -ref));
         l[rt] += p;
         if constexpr (kParts == 1) {
           pf[rt][0][i] = static_cast<__bf16>(p);
@@ -450,9 +461,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
           store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
         }
         if (u == 0) {
-          const float e2 = M + log2f(lt);
+          const float log_l = log2f(lt), e2 = M + log_l;
           if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
-          if (a.lse2 != nullptr) a.lse2[at] = e2;
+          if (a.lse2 != nullptr) {
+            a.lse2[at] = e2;
+            a.ref[at] = make_float2(M, log_l);
+          }
         }
       }
     }
@@ -498,7 +512,9 @@ template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O, AttnArgs a, JoinArgs j) {
   constexpr int kUnits = D / 4, kLanes = kJoinThreads / kUnits;
   __shared__ f32x4 s_o[kLanes][kUnits];
-  __shared__ float s_w[kMaxShares], s_e2[kMaxJoinRows];
+  __shared__ float s_w[kMaxShares];
+  __shared__ float2 s_ref[kMaxJoinRows];      // of a row: reference and log2 of its sum
+  __shared__ int s_far;                       // a row with a far reference has been seen
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (static_cast<int>(blockIdx.x) < j.row_blocks) {
     const int64_t at = blockIdx.x;
@@ -539,9 +555,12 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
       store_f32x4(to, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
     }
     if (u == 0) {
-      const float e2 = row.x + log2f(row.y);
+      const float log_l = log2f(row.y), e2 = row.x + log_l;
       if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
-      if (a.lse2 != nullptr) a.lse2[at] = e2;
+      if (a.lse2 != nullptr) {
+        a.lse2[at] = e2;
+        a.ref[at] = make_float2(row.x, log_l);
+      }
     }
     return;
   }
@@ -554,25 +573,41 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
   const bool mine = k0 < j.Nk;
   const float* from = a.logits + row0 * j.logit_stride + (mine ? k0 : 0);
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (threadIdx.x == 0) s_far = 0;
   for (int r0 = 0; r0 < per; r0 += kMaxJoinRows) {
     const int n = min(per - r0, kMaxJoinRows);
     __syncthreads();
     for (int r = wave; r < n; r += kJoinThreads / 64) {
-      float e2;
+      float2 ref;
       if (j.n_splits > 1) {
-        const float2 row = join_ml(a.part_ml + row0 + r0 + r, a.rows_all, j.n_splits, lane);
-        e2 = row.x + log2f(row.y);
+        ref = join_ml(a.part_ml + row0 + r0 + r, a.rows_all, j.n_splits, lane);
+        ref.y = log2f(ref.y);
       } else {
-        e2 = a.lse2[row0 + r0 + r];
+        ref = a.ref[row0 + r0 + r];
       }
-      if (lane == 0) s_e2[r] = e2;
+      if (lane == 0) {
+        s_ref[r] = ref;
+        if (far_ref(ref.x)) s_far = 1;
+      }
     }
     __syncthreads();
+    if (s_far == 0) {
 #pragma unroll 4
-    for (int r = 0; r < n; ++r) {
-      const f32x4 s = *reinterpret_cast<const f32x4*>(from + (r0 + r) * j.logit_stride);
+      for (int r = 0; r < n; ++r) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(from + (r0 + r) * j.logit_stride);
+        const float e2 = s_ref[r].x + s_ref[r].y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(s[i], j.c, -s_e2[r]));
+        for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(s[i], j.c, -e2));
+      }
+    } else {
+      for (int r = 0; r < n; ++r) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(from + (r0 + r) * j.logit_stride);
+        const float2 ref = s_ref[r];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum[i] += __builtin_amdgcn_exp2f(far_ref(ref.x) ? far_exponent(s[i], j.c, ref.x) - ref.y
+                                                          : fmaf(s[i], j.c, -(ref.x + ref.y)));
+      }
     }
   }
   float* w = j.weights + sel * j.w_stride_h + k0;
@@ -598,6 +633,7 @@ struct WeighArgs {
   int64_t q_stride_h, w_stride_h;
   float c, decay;
   const float* lse;                         // base 2
+  const float2* ref;                        // the same in its two terms
   float* weights;
 };
 template <typename T, int D, int kTiles>
@@ -629,6 +665,14 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
     const float* lse = a.lse + static_cast<int64_t>(kvh) * n_rows;
     QueryFrags<T, D> next;
     float next_e2[4];
+    auto scores_of = [](const QueryFrags<T, D>& q, const bf16x8 (&k)[D / 32]) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.f[b][p], k[b], s, 0, 0, 0);
+      return s;
+    };
     auto fetch = [&](int row0) {
       const int rho = min(row0 + r, n_rows - 1);
       const int head = a.by_nq.of(rho);
@@ -637,21 +681,37 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
       for (int i = 0; i < 4; ++i) next_e2[i] = lse[min(row0 + g * 4 + i, n_rows - 1)];
     };
     if (row_wave * 16 < n_rows) fetch(row_wave * 16);
+    bool far = false;           // a row of a far reference has been left out
     for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
       const QueryFrags<T, D> q = next;
       float e2[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e2[i] = row0 + g * 4 + i < n_rows ? next_e2[i] : INFINITY;   // a row that is not there: probability 0
+      for (int i = 0; i < 4; ++i) {
+        far |= fabsf(next_e2[i]) >= kFarRef;
+        e2[i] = row0 + g * 4 + i < n_rows && !(fabsf(next_e2[i]) >= kFarRef) ? next_e2[i] : INFINITY;    // probability 0
+      }
       if (row0 + step < n_rows) fetch(row0 + step);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int p = QueryFrags<T, D>::kParts - 1; p >= 0; --p)
-#pragma unroll
-          for (int b = 0; b < D / 32; ++b) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.f[b][p], kf[t][b], s, 0, 0, 0);
+        const f32x4 s = scores_of(q, kf[t]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[t] += __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -e2[i]));
+      }
+    }
+    if (!__any(far)) continue;
+    // those rows: here the logarithm of the sum would be lost in the rounding of the reference's sum with it
+    for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
+      fetch(row0);
+      const float2* ref = a.ref + static_cast<int64_t>(kvh) * n_rows;
+      float2 e2[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        e2[i] = row0 + g * 4 + i < n_rows && fabsf(next_e2[i]) >= kFarRef ? ref[row0 + g * 4 + i] : make_float2(0.f, INFINITY);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const f32x4 s = scores_of(next, kf[t]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[t] += __builtin_amdgcn_exp2f(far_exponent(s[i], a.c, e2[i].x) - e2[i].y);
       }
     }
   }
@@ -686,7 +746,7 @@ struct Q4Plan {
   bool expand, keep_logits;     // the cache as bf16 rows and pc_frame_attn; weights from kept logits
   int row_tiles, n_splits;      // tiles of 16 queries per work-group, key shares
   float *part_o, *lse, *logits;
-  float2* part_ml;
+  float2 *part_ml, *ref;
   uint16_t *k_rows, *v_rows;
   void* attn_ws;
   size_t attn_bytes, bytes;    // of attn_ws, which the scoring takes after the attention
@@ -725,6 +785,7 @@ struct Q4Plan {
       if (keep_logits) logits = static_cast<float*>(take(all * steps * kStep * 4));
     }
     if (weights) lse = static_cast<float*>(take(all * 4));
+    if (weights && !expand) ref = static_cast<float2*>(take(all * 8));
     bytes = at;
   }
 
@@ -881,7 +942,7 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
     const T* q = static_cast<const T*>(Q);
     const int tiles_q = ceil_div(rows, 16 * plan.row_tiles), steps = ceil_div(Nk, kStep);
     const AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, ceil_div(steps, plan.n_splits),
-                        q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.logits,
+                        q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.ref, plan.logits,
                         static_cast<int64_t>(Hkv) * rows};
     const auto kernel = plan.row_tiles == 1 ? q4_attn_kernel<T, kDims, 1> : q4_attn_kernel<T, kDims, 2>;
     kernel<<<a.n_tiles * plan.n_splits, kThreads, 0, s>>>(q, static_cast<T*>(O), a);
@@ -904,7 +965,7 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
       int groups = 1;           // powers of two: a compute unit holds eight waves of the widest form
       while (groups * dealt < kWaves && (keys == 128 ? wide : narrow) >= 1024 * groups) groups *= 2;
       const WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, groups * keys)), dealt,
-                           q_stride_h, weights_stride_h, c, decay, plan.lse, weights};
+                           q_stride_h, weights_stride_h, c, decay, plan.lse, plan.ref, weights};
       auto weigh = q4_weigh_kernel<T, kDims, 4>;
       if constexpr (sizeof(T) == 2)
         if (keys == 128) weigh = q4_weigh_kernel<T, kDims, 8>;

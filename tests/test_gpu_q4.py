@@ -258,6 +258,51 @@ def test_attn_masked_by_a_coordinate(dtype, Nq):
     assert (w[:, :Nk][:, torch.from_numpy(hidden).to(DEV)] == 0).all()
 
 
+def check_hidden_rows(dtype, D, Hq, Hkv, Nq, Nk, weights, big, level, scale, first_visible):
+    """Keys hidden through dimensions of their own: a third of the rows sees the keys from first_visible on, one in three, a
+    third sees none (all hidden alike: every key weighs the same), a third sees none and hides some twice (the others share).
+    The rows without a visible key are zero in every other dimension, so that their logits are exact in any precision."""
+    rng = np.random.default_rng(Nk + Nq + int(np.log2(big) - level))
+    K, V, Q = (rng.standard_normal((h, n, D)) for h, n in ((Hkv, Nk), (Hkv, Nk), (Hq, Nq)))
+    hidden = (np.arange(Nk) % 3 != 0) | (np.arange(Nk) < first_visible)
+    K[..., D - 32:], Q[..., D - 32:] = 0.0, 0.0
+    K[..., D - 1], K[..., D - 2] = np.where(hidden, level, 0.0), level
+    kind = np.arange(Hq * Nq).reshape(Hq, Nq) % 3
+    Q[kind > 0] = 0.0
+    Q[..., D - 1], Q[..., D - 2] = np.where(kind != 1, big, 0.0), np.where(kind > 0, big, 0.0)
+    cache, Qd = packed(K, V), torch.from_numpy(Q).to(TYPES[dtype]).to(DEV)
+    lse = torch.empty((Hq, Nq), device=DEV)
+    w = None if weights is None else torch.full((1 if weights == "one" else Hkv, Nk), 2.0, device=DEV)
+    O = pk.pc_q4_attn(Qd, cache, Nk, scale, lse=lse, weights=w, decay=0.5)
+    Kv, Vv = cache_values(cache, Nk)
+    want, want_l, mass = orc.attn(f64(Qd), Kv, Vv, scale)
+    spread = orc.attn(f64(Qd), Kv, np.abs(Vv), scale)[0]
+    # the logits that are not hidden; those of the other rows are exact, 0 beside their reference, which leaves the logarithm of
+    # the sum: log2(Nk) <= 15 in half a step of its own, less than (D + 16) u A
+    A = max(15.0, float(np.abs(f64(Qd)[..., :D - 32]).sum(-1).max() * np.abs(Kv).max() * scale))
+    e = (D + 16) * U * A + 8 * U
+    tol = (2 * e + (Nk + 64) * U) * spread + (2.0 ** -8 * (np.abs(want) + spread) if dtype == "bf16" else 0)
+    assert np.all(np.abs(f64(O) - want) <= tol + 1e-30), np.abs(f64(O) - want).max()
+    # scale to base 2, the product, and back: 4 roundings of a far logit
+    assert np.all(np.abs(f64(lse) - want_l) <= (D + 16) * U * A + (5 * np.abs(want_l) + Nk + 64) * U)
+    if w is not None:
+        mass = mass.sum(0, keepdims=True) if weights == "one" else mass
+        n = Hq * Nq if weights == "one" else Hq // Hkv * Nq
+        assert np.all(np.abs(f64(w) - (1.0 + mass)) <= (2 * e + (n + 64) * U) * mass + 2 * U * (1.0 + mass))
+
+
+HIDDEN_BY = [(1e12, -2.0, 0.125), (1e20, -2.0, 128 ** -0.5), (1e30, -1.0, 0.125), (1e30, -3.0, 0.1)]     # a query's entry, a key's, the scale
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("weights", ["each", "one"])
+@pytest.mark.parametrize("big,level,scale", HIDDEN_BY)
+@pytest.mark.parametrize("D,Hq,Hkv,Nq,Nk,first", [(128, 4, 2, 1, 3000, 1500), (64, 6, 2, 5, 700, 300), (128, 4, 2, 33, 900, 290),
+                                                  (128, 6, 3, 1, 90, 40), (64, 2, 1, 130, 3000, 1100)])
+def test_attn_hidden_keys_and_rows_without_any_other(dtype, weights, big, level, scale, D, Hq, Hkv, Nq, Nk, first):
+    check_hidden_rows(dtype, D, Hq, Hkv, Nq, Nk, weights, big, level, scale, first)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Nq", [1, 20, 130])
 def test_attn_not_a_number(dtype, Nq):
