@@ -157,11 +157,17 @@ struct AttnArgs {
   float* part_o;                            // NULL: one share
   float2* part_ml;
   float* lse;                               // natural logarithm, or NULL
-  float* lse2;                              // base 2, for the weights, or NULL
+  float* lse2;                              // base 2, for the weights, or NULL; of a row with a far reference: infinity
   float2* ref;                              // the same in its two terms: reference and log2 of the sum
   float* logits;                            // [rows_all][whole steps] for the weights of few rows, or NULL
   int64_t rows_all;
 };
+
+// What the scoring subtracts; infinity for a row of a far reference: probability 0 until its two terms are read.
+__device__ __forceinline__ float lse2_of(float m, float log_l) {
+  const float e2 = m + log_l;
+  return far_ref(m) && e2 == e2 ? INFINITY : e2;
+}
 
 template <int D>
 __device__ __forceinline__ int v_place(int key, int chunk) {      // a 32-byte chunk of a key's row in LDS
@@ -379,13 +385,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
         m[rt] = m_new;
       }
       // a far reference's exponents come to the common fma as products of c, with 0 as their reference
-      const bool far = far_ref(m[rt]);
-      const float ref = far ? 0.f : m[rt];
-      if (__any(far)) {
+      float ref = m[rt];
+      if (__any(far_ref(ref))) {
+        asm volatile("" ::: "memory");     // a branch
+        const bool far = far_ref(ref);
         const float by = 1.f / a.c;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (far) s[i >> 2][i & 3] = far_exponent(s[i >> 2][i & 3], a.c, m[rt]) * by;
+          if (far) s[i >> 2][i & 3] = far_exponent(s[i >> 2][i & 3], a.c, ref) * by;
+        if (far) ref = 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -464,7 +472,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
           const float log_l = log2f(lt), e2 = M + log_l;
           if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
           if (a.lse2 != nullptr) {
-            a.lse2[at] = e2;
+            a.lse2[at] = lse2_of(M, log_l);
             a.ref[at] = make_float2(M, log_l);
           }
         }
@@ -558,7 +566,7 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
       const float log_l = log2f(row.y), e2 = row.x + log_l;
       if (a.lse != nullptr) a.lse[at] = e2 * 0.6931471805599453f;
       if (a.lse2 != nullptr) {
-        a.lse2[at] = e2;
+        a.lse2[at] = lse2_of(row.x, log_l);
         a.ref[at] = make_float2(row.x, log_l);
       }
     }
@@ -632,8 +640,8 @@ struct WeighArgs {
   int dealt;                                // waves that share keys: 1, 2, 4 or 8
   int64_t q_stride_h, w_stride_h;
   float c, decay;
-  const float* lse;                         // base 2
-  const float2* ref;                        // the same in its two terms
+  const float* lse2;                        // see AttnArgs
+  const float2* ref;
   float* weights;
 };
 template <typename T, int D, int kTiles>
@@ -662,7 +670,7 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
 #pragma unroll
       for (int b = 0; b < D / 32; ++b) kf[t][b] = q4_to_bf16(raw.w[b], q4_scale(raw.byte));
     }
-    const float* lse = a.lse + static_cast<int64_t>(kvh) * n_rows;
+    const float* lse2 = a.lse2 + static_cast<int64_t>(kvh) * n_rows;
     QueryFrags<T, D> next;
     float next_e2[4];
     auto scores_of = [](const QueryFrags<T, D>& q, const bf16x8 (&k)[D / 32]) {
@@ -678,17 +686,17 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
       const int head = a.by_nq.of(rho);
       next.load(Q + (kvh * a.rep + head) * a.q_stride_h + static_cast<int64_t>(rho - head * a.by_nq.d) * D, g);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) next_e2[i] = lse[min(row0 + g * 4 + i, n_rows - 1)];
+      for (int i = 0; i < 4; ++i) next_e2[i] = lse2[min(row0 + g * 4 + i, n_rows - 1)];
     };
     if (row_wave * 16 < n_rows) fetch(row_wave * 16);
-    bool far = false;           // a row of a far reference has been left out
+    float top = 0.f;            // infinity: a row of a far reference has been left out
     for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
       const QueryFrags<T, D> q = next;
       float e2[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        far |= fabsf(next_e2[i]) >= kFarRef;
-        e2[i] = row0 + g * 4 + i < n_rows && !(fabsf(next_e2[i]) >= kFarRef) ? next_e2[i] : INFINITY;    // probability 0
+        top = fmaxf(top, next_e2[i]);
+        e2[i] = row0 + g * 4 + i < n_rows ? next_e2[i] : INFINITY;   // a row that is not there: probability 0
       }
       if (row0 + step < n_rows) fetch(row0 + step);
 #pragma unroll
@@ -698,7 +706,7 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
         for (int i = 0; i < 4; ++i) sum[t] += __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -e2[i]));
       }
     }
-    if (!__any(far)) continue;
+    if (!__any(top == INFINITY)) continue;
     // those rows: here the logarithm of the sum would be lost in the rounding of the reference's sum with it
     for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
       fetch(row0);
@@ -706,7 +714,7 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
       float2 e2[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        e2[i] = row0 + g * 4 + i < n_rows && fabsf(next_e2[i]) >= kFarRef ? ref[row0 + g * 4 + i] : make_float2(0.f, INFINITY);
+        e2[i] = row0 + g * 4 + i < n_rows && next_e2[i] == INFINITY ? ref[row0 + g * 4 + i] : make_float2(0.f, INFINITY);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const f32x4 s = scores_of(next, kf[t]);
