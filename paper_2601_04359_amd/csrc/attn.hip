@@ -101,14 +101,15 @@ __device__ __forceinline__ int take_share(int& L, int n_units) {
 // Keys of a score -inf, or of a mask value far below the rest, weigh nothing, and a wave may see a half
 // tile of nothing else before its first real key.  c general: a reference of -inf makes the row sum
 // NaN or inf, so every half tile is redone until there is a finite one, and a redo without one adds
-// zeros.  kUnitC: products must not start from such a reference (inf - inf, or a score lost in the
-// rounding of -m_ref: an ulp at kLowestStart is 2^-11): they start from zero instead, and while any
-// query of the wave is in that state (low_ref) every half tile is redone.
+// zeros.  A far reference's probabilities (see far_exponent) are formed in the redo, so while any query of the
+// wave has one (redo_all) every half tile is redone.  kUnitC: products must not start from a low reference
+// (inf - inf, or a score lost in the rounding of -m_ref: an ulp at kLowestStart is 2^-11): they start from
+// zero instead, and every half tile is redone for as long.
 template <bool kUnitC>
 __device__ __forceinline__ void pipeline_phase(
     const lds_u8* k_half, const int (&k_off)[8], const lds_u8* v_half, const int (&v_off)[4],
     const bf16x8 (&qf)[8], f32x16& s_nxt, const bf16x8 (&p_mm)[2], f32x16 (&o)[4], const f32x16& s_cur,
-    bf16x8 (&p_cur)[2], float& m_ref, float& l_run, float c, f32x16& neg_m, bool& low_ref) {
+    bf16x8 (&p_cur)[2], float& m_ref, float& l_run, float c, f32x16& neg_m, bool& redo_all) {
   // fragment k: 0..7 -> K rows, contraction step k; 8..15 -> V^T (key step (k-8)/4, block (k-8)%4)
   auto frag = [&](int k) -> bf16x8 {
     if (k < 8) {
@@ -164,7 +165,7 @@ __device__ __forceinline__ void pipeline_phase(
 #pragma unroll
   for (int half = 0; half < 2; ++half) asm volatile("" : "+v"(p_cur[half]));
   asm volatile("" : "+v"(psum));
-  if ((kUnitC && low_ref) || __any(!(psum <= kRescaleTrigger))) {  // also catches inf and NaN
+  if (redo_all || __any(!(psum <= kRescaleTrigger))) {  // also catches inf and NaN
     float mx = s_cur[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s_cur[i]);
@@ -175,15 +176,17 @@ __device__ __forceinline__ void pipeline_phase(
     const bool none = m_new == -INFINITY;   // no key of a finite score yet
     const float alpha = none ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
     const float m_use = none ? 0.f : m_new - start;
+    if constexpr (!kUnitC) redo_all = __any(far_ref(m_new));
     psum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      pv[i] = kUnitC ? __builtin_amdgcn_exp2f(s_cur[i] - m_use) : __builtin_amdgcn_exp2f(fmaf(s_cur[i], c, -m_use));
+      pv[i] = __builtin_amdgcn_exp2f(kUnitC ? s_cur[i] - m_use
+                                            : far_ref(m_use) ? far_exponent(s_cur[i], c, m_use) : fmaf(s_cur[i], c, -m_use));
       psum += pv[i];
     }
     if constexpr (kUnitC) {
       const float start_new = m_new >= kLowestStart ? m_new : 0.f;
-      low_ref = __any(!(m_new >= kLowestStart));
+      redo_all = __any(!(m_new >= kLowestStart));
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s_acc[i] -= start_new - start;
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
       pB[ks][e] = static_cast<__bf16>(0.f);
     }
   float m_ref = -INFINITY, l_run = 0.f;
-  bool low_ref = false;   // wave-uniform
+  bool redo_all = false;   // wave-uniform
   f32x16 neg_m;
 #pragma unroll
   for (int i = 0; i < 16; ++i) neg_m[i] = 0.f;
@@ -344,9 +347,10 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sA[i]);
     m_ref = wave_half_max(mx) * c;
+    if constexpr (!kUnitC) redo_all = __any(far_ref(m_ref));
     if constexpr (kUnitC) {
       const float start = m_ref >= kLowestStart ? m_ref : 0.f;
-      low_ref = __any(!(m_ref >= kLowestStart));
+      redo_all = __any(!(m_ref >= kLowestStart));
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         sA[i] -= start;
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
     // ---- phase 1: S_B(j), O += V_B(j-1) P_B(j-1)  |  P_A(j) ----
     if (active) {
       pipeline_phase<kUnitC>(smem + k_cur + 32 * kRowBytes, k_off, smem + v_prev + 32 * kRowBytes, v_off, qf, sB, pB, o, sA,
-                     pA, m_ref, l_run, c, neg_m, low_ref);
+                     pA, m_ref, l_run, c, neg_m, redo_all);
       if (left < kBN) mask_tail(sB, left - 32 - g * 4);
     }
     // One barrier per tile: every wave is past K(j) and V(j-1), and K(j+1), V(j) (fetched
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
     // (after the last tile S_A is formed from a clamped tile and never used)
     if (active) {
       pipeline_phase<kUnitC>(smem + k_nxt, k_off, smem + v_cur, v_off, qf, sA, pA, o, sB, pB, m_ref, l_run, c, neg_m,
-                             low_ref);
+                             redo_all);
       if (left < 2 * kBN) mask_tail(sA, left - kBN - g * 4);
     }
   };
@@ -689,20 +693,27 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_small_kernel(
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
     mx = wave_half_max(mx) * c;
-    if (__any(!(mx <= m + 8.f))) {     // the reference lags by at most 2^8
+    float ref = m;
+    if (__any(!(mx <= m + 8.f) || far_ref(m))) {     // the reference lags by at most 2^8
       const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
       l *= alpha;
 #pragma unroll
       for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-      m = m_new;
+      ref = m = m_new;
+      if (far_ref(m)) {      // its exponents come to the common fma as products of c, with 0 as their reference
+        const float by = 1.f / c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = far_exponent(sc[i], c, m) * by;
+        ref = 0.f;
+      }
     }
     bf16x8 p[2];
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -m));
+      const float e = __builtin_amdgcn_exp2f(fmaf(sc[i], c, -ref));
       sum += e;
       p[i >> 3][i & 7] = static_cast<__bf16>(e);
     }
@@ -828,7 +839,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_mid_kernel(
 #pragma unroll
     for (int e = 0; e < 8; ++e) pA[ks][e] = pB[ks][e] = static_cast<__bf16>(0.f);
   float m_ref = -INFINITY, l_run = 0.f;
-  bool low_ref = false;   // wave-uniform
+  bool redo_all = false;   // wave-uniform
   auto mask_tail = [&](f32x16& sc, int t) {
     const int left = k_end - key_at(t);
     if (left >= 32) return;
@@ -857,9 +868,10 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_mid_kernel(
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sA[i]);
     m_ref = wave_half_max(mx) * c;
+    if constexpr (!kUnitC) redo_all = __any(far_ref(m_ref));
     if constexpr (kUnitC) {
       const float start = m_ref >= kLowestStart ? m_ref : 0.f;
-      low_ref = __any(!(m_ref >= kLowestStart));
+      redo_all = __any(!(m_ref >= kLowestStart));
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         sA[i] -= start;
@@ -882,7 +894,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_mid_kernel(
     constexpr int k_nxt = ((u + 1) & (kSlots - 1)) * kTile, v_prev = (kSlots + ((u + kSlots - 1) & (kSlots - 1))) * kTile;
     if (active) {
       pipeline_phase<kUnitC>(smem + k_nxt, k_off, smem + v_prev, v_off, qf, s_nxt, p_mm, o, s_cur, p_cur, m_ref, l_run, c,
-                             neg_m, low_ref);
+                             neg_m, redo_all);
       mask_tail(s_nxt, p + 1);
     }
     if constexpr (kR == 4) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");

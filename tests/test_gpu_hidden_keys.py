@@ -1,0 +1,70 @@
+"""Keys that a caller hides through dimensions of their own, by logits from -1e8 to -1e30: pc_frame_attn and pc_score.
+
+Rows of three kinds, a third each: some keys visible; all hidden alike (every key weighs the same); all hidden and some twice
+(the others share).  The rows without a visible key are zero in every other dimension: their logits are exact in any precision.
+
+Tolerances, with u = 2^-24 and A the largest sum_d |q_d k_d| * scale over visible keys: a logit is off by (D + 8) u A, a probability
+by a factor of 1 + e, e = (D + 16) u A + 8 u, and by half a step of bf16 before the second product; O once more by half a step.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_04359_amd as pk
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+D = 128
+# a query's entry, a key's, the scale (the exponent of the largest key's probability is far from 0 unless the product is rounded)
+HIDDEN_BY = [(1e8, -3.0, 128 ** -0.5), (1e12, -2.0, 0.125), (1e20, -2.0, 128 ** -0.5), (1e30, -1.0, 0.125), (1e30, -3.0, 0.1)]
+
+
+def hidden_inputs(hq, hkv, nq, nk, big, level, first_visible):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(nq + nk)
+    Q, K, V = (torch.empty((h, n, D), device=DEV).normal_(generator=g) for h, n in ((hq, nq), (hkv, nk), (hkv, nk)))
+    j = torch.arange(nk, device=DEV)
+    hidden = (j % 3 != 0) | (j < first_visible)
+    Q[..., 96:], K[..., 96:] = 0.0, 0.0
+    K[..., 127], K[..., 126] = hidden * level, level
+    kind = (torch.arange(hq * nq, device=DEV) % 3).view(hq, nq)
+    Q[kind > 0] = 0.0
+    Q[..., 127], Q[..., 126] = (kind != 1) * big, (kind > 0) * big
+    return [x.to(torch.bfloat16) for x in (Q, K, V)] + [kind, hidden]
+
+
+def reference(Q, K, V, scale, rows):
+    """O, lse, probabilities (per query head) and sum_j p_j |v_j| of these rows, in 64 bits."""
+    rep = Q.shape[0] // K.shape[0]
+    out = []
+    for h in range(Q.shape[0]):
+        s = Q[h, rows].double() @ K[h // rep].double().t().contiguous() * scale
+        lse = torch.logsumexp(s, 1)
+        m = s.amax(1, keepdim=True)
+        p = torch.exp(s - m)
+        p = p / p.sum(1, keepdim=True)
+        v = V[h // rep].double()
+        out.append((p @ v, lse, p, p @ v.abs()))
+    return [torch.stack(x) for x in zip(*out)]
+
+
+# 32 rows per work-group whole and in shares, 64, 128 and 256, the last also in shares
+SHAPES = [(8, 2, 252, 1804), (2, 1, 184, 5000), (16, 4, 666, 1786), (6, 2, 1593, 1701), (16, 4, 4032, 2048), (16, 4, 1008, 7455), (4, 2, 7, 33)]
+
+
+@pytest.mark.parametrize("big,level,scale", HIDDEN_BY)
+@pytest.mark.parametrize("first", [0, 0.4, 0.9])
+@pytest.mark.parametrize("hq,hkv,nq,nk", SHAPES)
+def test_frame_attn_hidden_keys_and_rows_without_any_other(hq, hkv, nq, nk, first, big, level, scale):
+    Q, K, V, kind, hidden = hidden_inputs(hq, hkv, nq, nk, big, level, int(first * nk))
+    lse = torch.empty((hq, nq), device=DEV)
+    O = pk.pc_frame_attn(Q, K, V, nk, scale, lse=lse)
+    rows = torch.arange(0, nq, max(1, nq // 40), device=DEV)
+    Ow, Lw, _, spread = reference(Q, K, V, scale, rows)
+    A = max(15.0, float(Q[..., :96].float().abs().sum(-1).max() * K[..., :96].float().abs().max() * scale))
+    e = (D + 16) * U * A + 8 * U
+    tol = (2 * e + (nk + 64) * U) * spread + 2.0 ** -8 * (Ow.abs() + spread)
+    err = (O[:, rows].double() - Ow).abs()
+    assert (err <= tol).all(), (err.max().item(), O.isnan().sum().item())
+    assert ((lse[:, rows].double() - Lw).abs() <= (D + 16) * U * A + (5 * Lw.abs() + nk + 64) * U).all()
