@@ -375,25 +375,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && kRT == 1 ? 4 : 2) void 
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
       mx *= a.c;
-      if (__any(!(mx <= m[rt] + 8.f))) {
+      float ref = m[rt];
+      if (__any(!(mx <= m[rt] + 8.f) || far_ref(m[rt]))) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         const float m_new = fmaxf(m[rt], mx), alpha = __builtin_amdgcn_exp2f(m[rt] - m_new);
         l[rt] *= alpha;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) o[rt][db] *= alpha;
-        m[rt] = m_new;
-      }
-      // a far reference's exponents come to the common fma as products of c, with 0 as their reference
-      float ref = m[rt];
-      if (__any(far_ref(ref))) {
-        asm volatile("" ::: "memory");     // a branch
-        const bool far = far_ref(ref);
-        const float by = 1.f / a.c;
+        ref = m[rt] = m_new;
+        if (far_ref(m_new)) {     // its exponents come to the common fma as products of c, with 0 as their reference
+          const float by = 1.f / a.c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (far) s[i >> 2][i & 3] = far_exponent(s[i >> 2][i & 3], a.c, ref) * by;
-        if (far) ref = 0.f;
+          for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = far_exponent(s[i >> 2][i & 3], a.c, m_new) * by;
+          ref = 0.f;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
