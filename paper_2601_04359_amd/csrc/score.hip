@@ -123,7 +123,8 @@ __device__ __forceinline__ void row_epilogue(int i, const f32x16 (&s)[2], const 
     psum[b] += __builtin_amdgcn_exp2f(kZeroRef ? s[b][e + k] : fmaf(s[b][e + k], c, -st.m[b]));
 }
 // After the phase: add the partial sums; if one ran away (a score outgrew the reference, or
-// the reference is still the initial sentinel) redo that half tile against its exact maximum.
+// the reference is still the initial sentinel) redo that half tile against its exact maximum.  While a
+// reference is far (see far_exponent) every half tile is redone.
 // kZeroRef: the sums may grow to 2^100 instead; zero_ref is cleared by a redo, and every half tile
 // after it is redone until the caller has left the loop for the general one.
 template <bool kZeroRef = false>
@@ -132,15 +133,21 @@ __device__ __forceinline__ void row_commit(const f32x16 (&s)[2], RowState& st, f
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     asm volatile("" : "+v"(psum[b]));
-    if (kZeroRef ? !zero_ref || __any(!(psum[b] <= 0x1p100f)) : __any(!(psum[b] <= kRowTrigger))) {
+    if (kZeroRef ? !zero_ref || __any(!(psum[b] <= 0x1p100f)) : __any(!(psum[b] <= kRowTrigger) || far_ref(st.m[b]))) {
       if (kZeroRef) zero_ref = false;
       float mx = fmaxf(s[b][0], s[b][1]);
 #pragma unroll
       for (int k = 2; k < 16; k += 2) mx = fmaxf(mx, fmaxf(s[b][k], s[b][k + 1]));
       const float m_new = fmaxf(st.m[b], mx * c);
       float sum = 0.f;
+      if (!__any(far_ref(m_new))) {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f(fmaf(s[b][k], c, -m_new));
+        for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f(fmaf(s[b][k], c, -m_new));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          sum += __builtin_amdgcn_exp2f(far_ref(m_new) ? far_exponent(s[b][k], c, m_new) : fmaf(s[b][k], c, -m_new));
+      }
       st.l[b] = st.l[b] * __builtin_amdgcn_exp2f(st.m[b] - m_new) + sum;
       st.m[b] = m_new;
     } else {
@@ -326,7 +333,8 @@ __global__ __launch_bounds__(kThreads, 1) void score_rowpass_bf16(
 // Negated base-2 normalisers of the scoring rows of KV head kvh (numbered head after head), from one of
 // three sources: an array of them (`ready`), the caller's natural-log LSE (`lse`, indexed like the rows
 // of Qs), or the row pass's n_splits (reference, sum) pairs, merged in split order: -log2 sum_j
-// 2^(c * s_j).  Rows past the last one give -inf: they add nothing.
+// 2^(c * s_j).  Rows past the last one give -inf: they add nothing.  So do rows whose normaliser is beyond kFarRef (they
+// see hidden keys only): the logarithm of their sum is lost in it, and so is where their largest key lies.
 struct RowNorm {
   const float* ready;        // [Hkv][rep * n_qs], or NULL
   const float* lse;          // the caller's, or NULL
@@ -383,7 +391,7 @@ __device__ __forceinline__ void row_norms(const RowNorm& a, int kvh, int rho0, i
   }
 #pragma unroll
   for (int i = 0; i < kN; ++i)
-    if (rho0 + i * step >= n_rows) v[i] = -INFINITY;
+    if (rho0 + i * step >= n_rows || fabsf(v[i]) >= kFarRef) v[i] = -INFINITY;
 }
 // The `ready` array, for calls whose many work-groups would each do the same merging.
 __global__ __launch_bounds__(256) void score_row_norms(RowNorm a, float* __restrict__ out) {

@@ -68,3 +68,22 @@ def test_frame_attn_hidden_keys_and_rows_without_any_other(hq, hkv, nq, nk, firs
     err = (O[:, rows].double() - Ow).abs()
     assert (err <= tol).all(), (err.max().item(), O.isnan().sum().item())
     assert ((lse[:, rows].double() - Lw).abs() <= (D + 16) * U * A + (5 * Lw.abs() + nk + 64) * U).all()
+
+
+@pytest.mark.parametrize("big,level,scale", HIDDEN_BY)
+@pytest.mark.parametrize("first", [0, 0.4, 0.9])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("hq,hkv,nq,nk", [(8, 2, 100, 1804), (2, 1, 64, 300), (16, 4, 512, 12000), (4, 2, 7, 33), (16, 4, 330, 7300)])
+def test_score_hidden_keys_and_rows_without_any_other(hq, hkv, nq, nk, given, first, big, level, scale):
+    """A row that sees nothing but hidden keys adds nothing to any score; the others add nothing to hidden keys."""
+    Q, K, V, kind, hidden = hidden_inputs(hq, hkv, nq, nk, big, level, int(first * nk))
+    rows = torch.arange(nq, device=DEV)
+    _, Lw, p, _ = reference(Q, K, V, scale, rows)
+    score = pk.pc_score(Q, K, nk, scale, lse=Lw.float() if given else None).double()
+    sees = (kind == 0).double()[..., None]
+    want = (p * sees).view(hkv, hq // hkv * nq, nk).sum(1)
+    assert (score[:, hidden] == 0).all()
+    A = max(15.0, float(Q[..., :96].float().abs().sum(-1).max() * K[..., :96].float().abs().max() * scale))
+    # a log-sum-exp of its own or a given one in fp32, and its change of base: three roundings of at most A
+    rel = 2 * ((D + 16) * U * A + 8 * U) + 3 * U * A + (hq // hkv * nq + 64) * U
+    assert ((score - want).abs() <= rel * want + 1e-30).all(), (score - want).abs().max().item()
