@@ -72,6 +72,12 @@ __device__ __forceinline__ void stage_tile(const uint16_t* __restrict__ base_h, 
 struct RowAt {
   int head, row;
 };
+// The log-sum-exp of a row with reference m and sum l (base 2), and, if asked for, its two terms.
+__device__ __forceinline__ void put_lse(float* __restrict__ lse, float2* __restrict__ ref, int64_t at, float m, float l) {
+  const float log_l = log2f(l);
+  lse[at] = (m + log_l) * 0.6931471805599453f;
+  if (ref != nullptr) ref[at] = make_float2(m, log_l);
+}
 __device__ __forceinline__ RowAt row_at(int rho, int kvh, int rep, const Divisor& by_nq) {
   const int in_group = by_nq.of(rho);
   return {kvh * rep + in_group, rho - in_group * by_nq.d};
@@ -223,7 +229,7 @@ __device__ __forceinline__ void pipeline_phase(
 template <bool kUnitC>
 __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
-    uint16_t* __restrict__ O, float* __restrict__ lse, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
+    uint16_t* __restrict__ O, float* __restrict__ lse, float2* __restrict__ ref, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
     int64_t kv_stride_h, int64_t o_stride_h, float c, Divisor by_tiles_q, int n_whole, int n_cut, int share_tiles,
     float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t row_whole, int64_t rows_cut) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -468,8 +474,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_kernel(
     }
   }
   if (rho < n_rows) {
-    if (lse != nullptr && g == 0)
-      lse[at] = (m_ref + log2f(l_tot)) * 0.6931471805599453f;
+    if (lse != nullptr && g == 0) put_lse(lse, ref, at, m_ref, l_tot);
   }
 }
 
@@ -483,7 +488,8 @@ constexpr size_t kMergeBytes = 8 * kWaveOBytes + 8 * 32 * 8;
 template <int kR, int kBlocks>
 __device__ __forceinline__ void merge_waves(lds_u8* smem, const f32x16 (&o)[kBlocks], int dim0, float m, float l, int wave, int lane,
                                             int tile, int kvh, int split, uint16_t* __restrict__ O,
-                                            float* __restrict__ lse, int rep, const Divisor& by_nq, int64_t o_stride_h,
+                                            float* __restrict__ lse, float2* __restrict__ ref, int rep, const Divisor& by_nq,
+                                            int64_t o_stride_h,
                                             float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t rows_all) {
   auto piece = [&](int w, int i, int of_lane) {
     return reinterpret_cast<__attribute__((address_space(3))) f32x4*>(smem + w * kWaveOBytes + i * 1024 + (of_lane ^ i) * 16);
@@ -541,7 +547,7 @@ __device__ __forceinline__ void merge_waves(lds_u8* smem, const f32x16 (&o)[kBlo
       out[t * 2 + 1] = pack_bf16x2(acc[t][2] * inv, acc[t][3] * inv);
     }
     *reinterpret_cast<u32x4*>(O + to.head * o_stride_h + static_cast<int64_t>(to.row) * kD + dim0 + i * 8) = out;
-    if (lse != nullptr && dim0 + i == 0) lse[at] = (M + log2f(lt)) * 0.6931471805599453f;
+    if (lse != nullptr && dim0 + i == 0) put_lse(lse, ref, at, M, lt);
   }
 }
 
@@ -571,7 +577,7 @@ static_assert(2 * kSmallTileBytes <= kWaveOBytes, "a wave stages K and V in the 
 template <int kBlocks>
 __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_small_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
-    uint16_t* __restrict__ O, float* __restrict__ lse, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
+    uint16_t* __restrict__ O, float* __restrict__ lse, float2* __restrict__ ref, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
     int64_t kv_stride_h, int64_t o_stride_h, float c, Divisor by_tiles_q, int n_tiles, int share_steps,
     float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t rows_all) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -727,7 +733,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_small_kernel(
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   l = wave_half_sum(l);
 
-  merge_waves<1, kBlocks>((lds_u8*)smem_raw, o, dim0, m, l, wave, lane, tile, kvh, split, O, lse, rep, by_nq, o_stride_h, part_o, part_ml,
+  merge_waves<1, kBlocks>((lds_u8*)smem_raw, o, dim0, m, l, wave, lane, tile, kvh, split, O, lse, ref, rep, by_nq, o_stride_h, part_o, part_ml,
                  rows_all);
 }
 
@@ -748,7 +754,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_small_kernel(
 template <bool kUnitC, int kR>
 __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_mid_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
-    uint16_t* __restrict__ O, float* __restrict__ lse, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
+    uint16_t* __restrict__ O, float* __restrict__ lse, float2* __restrict__ ref, int rep, Divisor by_nq, int Nk, int64_t q_stride_h,
     int64_t kv_stride_h, int64_t o_stride_h, float c, Divisor by_tiles_q, int n_tiles, int share_steps,
     float* __restrict__ part_o, float2* __restrict__ part_ml, int64_t rows_all) {
   static_assert(kR == 2 || kR == 4, "row groups");
@@ -941,7 +947,7 @@ __global__ __launch_bounds__(kPPThreads, 1) void attn_bf16_mid_kernel(
   const float l_tot = wave_half_sum(l_run);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // tiles past the end may still be landing
   __syncthreads();
-  merge_waves<kR, 4>(smem, o, 0, fmaxf(m_ref, kNoRef), l_tot, wave, lane, tile, kvh, split, O, lse, rep, by_nq, o_stride_h, part_o,
+  merge_waves<kR, 4>(smem, o, 0, fmaxf(m_ref, kNoRef), l_tot, wave, lane, tile, kvh, split, O, lse, ref, rep, by_nq, o_stride_h, part_o,
                   part_ml, rows_all);
 }
 
@@ -956,7 +962,7 @@ __device__ __forceinline__ float natural_lse(float m, float l) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_merge_kernel(const float* __restrict__ part_o,
                                                          const float2* __restrict__ part_ml,
-                                                         T* __restrict__ O, float* __restrict__ lse,
+                                                         T* __restrict__ O, float* __restrict__ lse, float2* __restrict__ ref,
                                                          int Hq, int Nq, int64_t o_stride_h, int n_splits,
                                                          int64_t row_whole) {
   constexpr bool kF32 = sizeof(T) == 4;
@@ -1007,7 +1013,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const float* __restrict
     packed[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
     packed[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
     *reinterpret_cast<u32x2*>(out) = packed;
-    if (lse != nullptr && c == 0) lse[at] = (M + log2f(l)) * 0.6931471805599453f;
+    if (lse != nullptr && c == 0) put_lse(lse, ref, at, M, l);
   }
 }
 
@@ -1538,7 +1544,7 @@ int attn_f32(const float* Q, const float* K, const float* V, int Hq, int rep, in
   if (n_splits > 1) {
     constexpr int kRowsPerBlock = 256 / (D / 4);
     attn_merge_kernel<float, D><<<static_cast<unsigned>((rows + kRowsPerBlock - 1) / kRowsPerBlock), 256, 0, s>>>(
-        part_o, part_ml, O, lse, Hq, Nq, o_stride_h, n_splits, 0);
+        part_o, part_ml, O, lse, nullptr, Hq, Nq, o_stride_h, n_splits, 0);
     PC_CHECK_LAUNCH("pc_frame_attn merge");
   }
   return PC_OK;
@@ -1596,10 +1602,9 @@ extern "C" int pc_frame_attn_cut(int dtype, int Hq, int Hkv, int Nq, int Nk, int
   return PC_OK;
 }
 
-extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dtype, int Hq,
-                             int Hkv, int Nq, int Nk, int D, int64_t q_stride_h,
-                             int64_t kv_stride_h, int64_t o_stride_h, float scale, void* O,
-                             float* lse, void* ws, size_t ws_bytes, void* stream) {
+int pc::frame_attn(const void* Q, const void* K, const void* V, int dtype, int Hq, int Hkv, int Nq, int Nk, int D,
+                   int64_t q_stride_h, int64_t kv_stride_h, int64_t o_stride_h, float scale, void* O, float* lse, float2* ref,
+                   void* ws, size_t ws_bytes, void* stream) {
   PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "pc_frame_attn: dtype %d", dtype);
   PC_REQUIRE(Hq > 0 && Hkv > 0 && Hq % Hkv == 0, PC_ERR_SHAPE,
              "pc_frame_attn: Hq=%d must be a positive multiple of Hkv=%d", Hq, Hkv);
@@ -1646,7 +1651,7 @@ extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dt
       if (int rc = allow(kernel, kMergeBytes, lds_ok[3 + wide * 2 + unit_c])) return rc;
       const int share_steps = ceil_div(ceil_div(Nk, 32 * (wide ? 2 : 4)), plan.n_splits);
       kernel<<<n_tiles * plan.n_splits, kPPThreads, kMergeBytes, s>>>(
-          q, k, v, o, lse, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_tiles,
+          q, k, v, o, lse, ref, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_tiles,
           share_steps, part_o, part_ml, rows_cut);
     } else if (plan.rows == kSmallRows) {
       const int blocks = small_blocks(n_tiles * plan.n_splits);
@@ -1654,7 +1659,7 @@ extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dt
       if (int rc = allow(kernel, kSmallSmem, lds_ok[blocks == 4 ? 2 : 6 + blocks])) return rc;
       const int share_steps = ceil_div(ceil_div(Nk, kSmallKeys), plan.n_splits);
       kernel<<<n_tiles * plan.n_splits * (4 / blocks), kPPThreads, kSmallSmem, s>>>(
-          q, k, v, o, lse, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_tiles,
+          q, k, v, o, lse, ref, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_tiles,
           share_steps, part_o, part_ml, rows_cut);
     } else {
       const auto kernel = unit_c ? attn_bf16_kernel<true> : attn_bf16_kernel<false>;
@@ -1662,13 +1667,13 @@ extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dt
       const int n_whole = plan.n_splits > 1 ? plan.n_whole : n_tiles, n_cut = n_tiles - n_whole;
       const int share_tiles = ceil_div(ceil_div(Nk, kBN), plan.n_splits);
       kernel<<<n_whole + n_cut * plan.n_splits, kPPThreads, kSmemBytes, s>>>(
-          q, k, v, o, lse, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_whole,
+          q, k, v, o, lse, ref, rep, Divisor(Nq), Nk, q_stride_h, kv_stride_h, o_stride_h, c, Divisor(n_tiles_q), n_whole,
           n_cut, share_tiles, part_o, part_ml, plan.row_whole, rows_cut);
     }
     if (plan.n_splits > 1) {
       PC_CHECK_LAUNCH("pc_frame_attn");
       attn_merge_kernel<uint16_t, kD><<<static_cast<unsigned>((rows_cut + 7) / 8), 256, 0, s>>>(
-          part_o, part_ml, o, lse, Hq, Nq, o_stride_h, plan.n_splits, plan.row_whole);
+          part_o, part_ml, o, lse, ref, Hq, Nq, o_stride_h, plan.n_splits, plan.row_whole);
     }
   } else {
     PC_REQUIRE(D == 64 || D == 128, PC_ERR_UNSUPPORTED, "pc_frame_attn: fp32 tier needs D=64 or 128, got %d", D);
@@ -1682,4 +1687,12 @@ extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dt
   }
   PC_CHECK_LAUNCH("pc_frame_attn");
   return PC_OK;
+}
+
+extern "C" int pc_frame_attn(const void* Q, const void* K, const void* V, int dtype, int Hq,
+                             int Hkv, int Nq, int Nk, int D, int64_t q_stride_h,
+                             int64_t kv_stride_h, int64_t o_stride_h, float scale, void* O,
+                             float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return frame_attn(Q, K, V, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, kv_stride_h, o_stride_h, scale, O, lse, nullptr, ws, ws_bytes,
+                    stream);
 }

@@ -49,11 +49,23 @@ inline int allow_dynamic_lds(const void* kernel, size_t bytes, std::atomic<uint6
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// pc_score; with decay >= 0 (bf16 only) a key's score is added to decay times what stands in its place (0: replaces it).
+// pc_frame_attn; ref, bf16 only: log-sum-exps in base 2 and their two terms, [Hq][Nq] (reference, log2 of the sum), or NULL.
+int frame_attn(const void* Q, const void* K, const void* V, int dtype, int Hq, int Hkv, int Nq, int Nk, int D,
+               int64_t q_stride_h, int64_t kv_stride_h, int64_t o_stride_h, float scale, void* O, float* lse, float2* ref,
+               void* ws, size_t ws_bytes, void* stream);
+
+// pc_score up to the last addition.  With `parts` (bf16 only, lse given; score, its stride and share_heads are not looked
+// at) the sums stay in the workspace as parts, to be added up in their order, and *any_far is set to 1 where a row has been
+// left out because its normaliser is beyond kFarRef.
+struct ScoreParts {
+  const float* sums;        // [n][Hkv][Nk]
+  int n;                    // kMaxScoreParts at most
+};
+constexpr int kMaxScoreParts = 8;
 int score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs, int Nk, int D, int64_t q_stride_h,
                int64_t k_stride_h, const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
-               int64_t score_stride_h, int share_heads, int key_begin, int key_end, float decay, void* ws, size_t ws_bytes,
-               void* stream);
+               int64_t score_stride_h, int share_heads, int key_begin, int key_end, ScoreParts* parts, int32_t* any_far,
+               void* ws, size_t ws_bytes, void* stream);
 
 // ---- device-side types -----------------------------------------------------------------
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;

@@ -96,10 +96,11 @@ __global__ __launch_bounds__(kCopyThreads) void q4_store_kernel(const T* __restr
 
 template <typename T, int D>
 __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K, T* __restrict__ V, RowsAt at, Q4Rows cache,
-                                                               int row0, int first_unit, int n_units) {
+                                                               int row0, int first_unit, int n_units, int32_t* clear) {
   constexpr int kLanes = D / 8;
   const int n = at.by_n.d;
   const int64_t idx = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x;
+  if (clear != nullptr && idx == 0) *clear = 0;
   int unit = static_cast<int>(idx / kLanes);
   const int part = static_cast<int>(idx % kLanes);
   if (unit >= n_units) return;
@@ -628,6 +629,9 @@ __global__ __launch_bounds__(kJoinThreads) void q4_join_kernel(T* __restrict__ O
 // has keys of its own: dealing 16 row tiles of 60,000 keys over eight waves converted every key eight times (57 us
 // instead of 35), and 128 keys per wave halve the queries' way through L2 (24).  With one sum for all heads a wave
 // walks the KV heads as well.
+// kRest: the last launch of the form for many rows.  pc_score's column pass has summed the rows' probabilities, but for rows
+// of a far reference, which it leaves out; this adds its parts up (a wave per KV head of a shared sum) and, where there are
+// such rows, their probabilities.
 // ------------------------------------------------------------------------------------------
 struct WeighArgs {
   Q4Rows cache;
@@ -636,11 +640,13 @@ struct WeighArgs {
   int dealt;                                // waves that share keys: 1, 2, 4 or 8
   int64_t q_stride_h, w_stride_h;
   float c, decay;
-  const float* lse2;                        // see AttnArgs
+  const float* lse2;                        // see AttnArgs; kRest: natural log-sum-exps
   const float2* ref;
   float* weights;
+  ScoreParts parts;                         // kRest
+  const int32_t* any_far;
 };
-template <typename T, int D, int kTiles>
+template <typename T, int D, int kTiles, bool kRest = false>
 __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict__ Q, WeighArgs a) {
   constexpr int kKeys = 16 * kTiles;
   __shared__ float s_sum[kWaves][kKeys];
@@ -655,7 +661,25 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
   const int k_first = min(k0, a.Nk - 1);      // the last work-group's waves may lie behind the last key
   const int n_rows = a.rep * a.by_nq.d, per = a.Hkv / a.Hsel;
   float sum[kTiles] = {};
-  for (int kvh = sel * per; kvh < (sel + 1) * per; ++kvh) {
+  float parts = 0.f, old = 0.f;
+  int heads_end = (sel + 1) * per;
+  if constexpr (kRest) {
+    static_assert(kKeys == 64, "a lane per key");
+    const int key = min(block0 + lane, a.Nk - 1);
+    const int any_far = *a.any_far;
+    if (a.decay != 0.f) old = a.weights[sel * a.w_stride_h + key];
+    const float* from = a.parts.sums + key;
+    for (int kvh = sel * per + wave; kvh < heads_end; kvh += a.dealt) {
+      float v[kMaxScoreParts];
+#pragma unroll
+      for (int p = 0; p < kMaxScoreParts; ++p)
+        v[p] = p < a.parts.n ? from[(static_cast<int64_t>(p) * a.Hkv + kvh) * a.Nk] : 0.f;
+#pragma unroll
+      for (int p = 0; p < kMaxScoreParts; ++p) parts += v[p];
+    }
+    if (any_far == 0) heads_end = 0;
+  }
+  for (int kvh = sel * per; kvh < heads_end; ++kvh) {
     bf16x8 kf[kTiles][D / 32];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -684,9 +708,9 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
 #pragma unroll
       for (int i = 0; i < 4; ++i) next_e2[i] = lse2[min(row0 + g * 4 + i, n_rows - 1)];
     };
-    if (row_wave * 16 < n_rows) fetch(row_wave * 16);
-    float top = 0.f;            // infinity: a row of a far reference has been left out
-    for (int row0 = row_wave * 16; row0 < n_rows; row0 += step) {
+    if (!kRest && row_wave * 16 < n_rows) fetch(row_wave * 16);
+    float top = kRest ? INFINITY : 0.f;            // infinity: a row of a far reference has been left out
+    for (int row0 = row_wave * 16; !kRest && row0 < n_rows; row0 += step) {
       const QueryFrags<T, D> q = next;
       float e2[4];
 #pragma unroll
@@ -709,13 +733,20 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
       const float2* ref = a.ref + static_cast<int64_t>(kvh) * n_rows;
       float2 e2[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        e2[i] = row0 + g * 4 + i < n_rows && next_e2[i] == INFINITY ? ref[row0 + g * 4 + i] : make_float2(0.f, INFINITY);
+      for (int i = 0; i < 4; ++i) {
+        // (kRest: as the column pass decided)
+        const bool far = kRest ? fabsf(next_e2[i] * 1.4426950408889634f) >= kFarRef : next_e2[i] == INFINITY;
+        e2[i] = row0 + g * 4 + i < n_rows && far ? ref[row0 + g * 4 + i] : make_float2(0.f, INFINITY);
+      }
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const f32x4 s = scores_of(next, kf[t]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[t] += __builtin_amdgcn_exp2f(far_exponent(s[i], a.c, e2[i].x) - e2[i].y);
+        for (int i = 0; i < 4; ++i) {
+          // (a score summed in another order than the reference's may lie an ulp above it, and that is no small number here)
+          const float x = far_exponent(s[i], a.c, e2[i].x);
+          sum[t] += __builtin_amdgcn_exp2f((x > 0.f ? 0.f : x) - e2[i].y);
+        }
       }
     }
   }
@@ -725,6 +756,10 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
     sum[t] += __shfl_xor(sum[t], 32);
     if (g == 0) s_sum[wave][t * 16 + r] = sum[t];
   }
+  if constexpr (kRest) {
+    wave_lds_sync();
+    s_sum[wave][lane] += parts;
+  }
   __syncthreads();
   // key i of the work-group: of the waves from i / kKeys * dealt on
   for (int i = threadIdx.x; i < groups * kKeys && block0 + i < a.Nk; i += blockDim.x) {
@@ -732,7 +767,8 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
     float x = 0.f;
     for (int w = 0; w < a.dealt; ++w) x += s_sum[from + w][i % kKeys];
     float* w = a.weights + sel * a.w_stride_h + block0 + i;
-    *w = a.decay == 0.f ? x : fmaf(a.decay, *w, x);
+    if (!kRest && a.decay != 0.f) old = *w;
+    *w = a.decay == 0.f ? x : fmaf(a.decay, old, x);
   }
 }
 
@@ -751,6 +787,7 @@ struct Q4Plan {
   int row_tiles, n_splits;      // tiles of 16 queries per work-group, key shares
   float *part_o, *lse, *logits;
   float2 *part_ml, *ref;
+  int32_t* any_far;
   uint16_t *k_rows, *v_rows;
   void* attn_ws;
   size_t attn_bytes, bytes;    // of attn_ws, which the scoring takes after the attention
@@ -788,8 +825,11 @@ struct Q4Plan {
       }
       if (keep_logits) logits = static_cast<float*>(take(all * steps * kStep * 4));
     }
-    if (weights) lse = static_cast<float*>(take(all * 4));
-    if (weights && !expand) ref = static_cast<float2*>(take(all * 8));
+    if (weights) {
+      lse = static_cast<float*>(take(all * 4));
+      ref = static_cast<float2*>(take(all * 8));
+      if (expand) any_far = static_cast<int32_t*>(take(4));
+    }
     bytes = at;
   }
 
@@ -857,9 +897,10 @@ extern "C" int pc_q4_store(const void* K, const void* V, int dtype, int H, int n
   return PC_OK;
 }
 
-extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype, void* K, void* V,
-                          int64_t k_stride_h, int64_t v_stride_h, void* stream) {
-  const char* who = "pc_q4_load";
+namespace {
+// clear: a word that is set to 0 as well, or NULL
+int load_rows(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype, void* K, void* V, int64_t k_stride_h,
+              int64_t v_stride_h, int32_t* clear, void* stream, const char* who) {
   if (int rc = check_kind(dtype, D, who)) return rc;
   PC_REQUIRE(H > 0 && n >= 0 && row0 >= 0, PC_ERR_SHAPE, "%s: H=%d n=%d row0=%d", who, H, n, row0);
   if (int rc = check_q4_cache(cache, D, who)) return rc;
@@ -877,7 +918,7 @@ extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int 
   const int first = K ? 0 : static_cast<int>(per);
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel, auto* k, auto* v) {
-    kernel<<<blocks, kCopyThreads, 0, s>>>(k, v, at, rows_of(cache), row0, first, static_cast<int>(units));
+    kernel<<<blocks, kCopyThreads, 0, s>>>(k, v, at, rows_of(cache), row0, first, static_cast<int>(units), clear);
   };
   if (dtype == PC_BF16) {
     auto *k = static_cast<uint16_t*>(K), *v = static_cast<uint16_t*>(V);
@@ -888,6 +929,12 @@ extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int 
   }
   PC_CHECK_LAUNCH(who);
   return PC_OK;
+}
+}  // namespace
+
+extern "C" int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype, void* K, void* V,
+                          int64_t k_stride_h, int64_t v_stride_h, void* stream) {
+  return load_rows(cache, H, row0, n, D, dtype, K, V, k_stride_h, v_stride_h, nullptr, stream, "pc_q4_load");
 }
 
 namespace {
@@ -931,14 +978,23 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
   if (plan.expand) {
     // rows as they lie in the cache, so that one launch's worth of copying serves every query row
     const int64_t per = static_cast<int64_t>(Nk) * D;
-    if (int rc = pc_q4_load(cache, Hkv, 0, Nk, D, PC_BF16, plan.k_rows, plan.v_rows, per, per, stream)) return rc;
-    float* e = lse != nullptr ? lse : weights != nullptr ? plan.lse : nullptr;
-    if (int rc = pc_frame_attn(Q, plan.k_rows, plan.v_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, o_stride_h, scale, O, e,
-                               plan.attn_ws, plan.attn_bytes, stream))
+    if (int rc = load_rows(cache, Hkv, 0, Nk, D, PC_BF16, plan.k_rows, plan.v_rows, per, per, plan.any_far, stream, who)) return rc;
+    float* e = lse != nullptr ? lse : plan.lse;
+    if (int rc = frame_attn(Q, plan.k_rows, plan.v_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, o_stride_h, scale, O, e, plan.ref,
+                            plan.attn_ws, plan.attn_bytes, stream))
       return rc;
     if (weights == nullptr) return PC_OK;
-    return score_keys(Q, plan.k_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, nullptr, scale, e, Nq, weights, weights_stride_h,
-                      Hsel != Hkv, 0, 0, decay, plan.attn_ws, plan.attn_bytes, stream);
+    ScoreParts parts;
+    if (int rc = score_keys(Q, plan.k_rows, dtype, Hq, Hkv, Nq, Nk, D, q_stride_h, per, nullptr, scale, e, Nq, nullptr, 0, 0, 0, 0,
+                            &parts, plan.any_far, plan.attn_ws, plan.attn_bytes, stream))
+      return rc;
+    int waves = 1;
+    while (waves < kWaves && waves < Hkv / Hsel) waves *= 2;
+    const WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, 64)), waves, q_stride_h,
+                         weights_stride_h, c, decay, e, plan.ref, weights, parts, plan.any_far};
+    q4_weigh_kernel<uint16_t, 128, 4, true><<<w.by_blocks.d * Hsel, 64 * waves, 0, s>>>(static_cast<const uint16_t*>(Q), w);
+    PC_CHECK_LAUNCH(who);
+    return PC_OK;
   }
   auto run = [&](auto zero, auto dims) -> int {
     using T = decltype(zero);
@@ -969,7 +1025,7 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
       int groups = 1;           // powers of two: a compute unit holds eight waves of the widest form
       while (groups * dealt < kWaves && (keys == 128 ? wide : narrow) >= 1024 * groups) groups *= 2;
       const WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, groups * keys)), dealt,
-                           q_stride_h, weights_stride_h, c, decay, plan.lse, plan.ref, weights};
+                           q_stride_h, weights_stride_h, c, decay, plan.lse, plan.ref, weights, {}, nullptr};
       auto weigh = q4_weigh_kernel<T, kDims, 4>;
       if constexpr (sizeof(T) == 2)
         if (keys == 128) weigh = q4_weigh_kernel<T, kDims, 8>;

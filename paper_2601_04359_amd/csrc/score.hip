@@ -47,7 +47,7 @@ constexpr int kPrepTiles = 64;       // tiles whose rows pass 2 prepares in LDS 
 constexpr int kPrepRows = (kPrepTiles + kStages) * kTileRows;
 constexpr size_t kColSmem = kStages * kTileBytes + kPrepRows * 12;
 constexpr int kMaxSplits = 32;       // key splits of pass 1
-constexpr int kMaxQSplits = 8;       // query splits of pass 2
+constexpr int kMaxQSplits = kMaxScoreParts;   // query splits of pass 2
 constexpr float kNoMax = -1e30f;     // finite stand-in for "no key seen yet"
 
 // Every staging point issues kTileLoads direct loads per wave and nothing else is in flight in the loops:
@@ -344,6 +344,7 @@ struct RowNorm {
   int64_t part_stride;       // Hkv * rep * n_qs
   int n_splits, rep;
   Divisor by_qs;             // by n_qs
+  int32_t* any_far;          // 1 is written where a row is left out, or NULL
 };
 // v[i]: row rho0 + i * step.  The loads of all of them are in flight together.
 template <int kN>
@@ -390,8 +391,11 @@ __device__ __forceinline__ void row_norms(const RowNorm& a, int kvh, int rho0, i
     }
   }
 #pragma unroll
-  for (int i = 0; i < kN; ++i)
-    if (rho0 + i * step >= n_rows || fabsf(v[i]) >= kFarRef) v[i] = -INFINITY;
+  for (int i = 0; i < kN; ++i) {
+    const bool far = fabsf(v[i]) >= kFarRef;
+    if (far && a.any_far != nullptr) *a.any_far = 1;
+    if (rho0 + i * step >= n_rows || far) v[i] = -INFINITY;
+  }
 }
 // The `ready` array, for calls whose many work-groups would each do the same merging.
 __global__ __launch_bounds__(256) void score_row_norms(RowNorm a, float* __restrict__ out) {
@@ -906,13 +910,9 @@ __device__ __forceinline__ float parts_sum(const float* part, int n_parts, int64
   for (int p = 0; p < kMaxQSplits; ++p) sum += v[p];   // a missing part adds +0: the sum is unchanged
   return sum;
 }
-// What becomes of the value that a sum meets: replaced (decay < 0 or 0), or decay times it is added.
-__device__ __forceinline__ void put_score(float* out, float sum, float decay) {
-  *out = decay > 0.f ? fmaf(decay, *out, sum) : sum;
-}
 // out[h][j] = that sum; with share_heads (n_parts = 1) the heads are summed, head 0 first, into out[j].
 __global__ void score_reduce(const float* __restrict__ part, float* __restrict__ out, int64_t out_stride_h,
-                             int n_parts, int Hkv, int Nk, int share_heads, float decay) {
+                             int n_parts, int Hkv, int Nk, int share_heads) {
   const int j = blockIdx.x * blockDim.x + threadIdx.x;
   if (j >= Nk) return;
   if (share_heads) {
@@ -924,11 +924,10 @@ __global__ void score_reduce(const float* __restrict__ part, float* __restrict__
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[i];
     }
-    put_score(out + j, s, decay);
+    out[j] = s;
   } else {
     const int h = blockIdx.y;
-    put_score(out + h * out_stride_h + j,
-              parts_sum(part, n_parts, static_cast<int64_t>(Hkv) * Nk, static_cast<int64_t>(h) * Nk + j), decay);
+    out[h * out_stride_h + j] = parts_sum(part, n_parts, static_cast<int64_t>(Hkv) * Nk, static_cast<int64_t>(h) * Nk + j);
   }
 }
 // The same for share_heads and several parts: a wave per head (eight at most) and 64 keys per work-group, so that
@@ -938,7 +937,7 @@ __global__ void score_reduce(const float* __restrict__ part, float* __restrict__
 constexpr int kReduceHeads = 8;
 __global__ __launch_bounds__(64 * kReduceHeads) void score_reduce_heads(const float* __restrict__ part,
                                                                         float* __restrict__ out, int n_parts, int Hkv,
-                                                                        int Nk, float decay) {
+                                                                        int Nk) {
   __shared__ float s_sum[kReduceHeads][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6, j = blockIdx.x * 64 + lane;
@@ -952,7 +951,7 @@ __global__ __launch_bounds__(64 * kReduceHeads) void score_reduce_heads(const fl
     if (wave == 0)
       for (int i = 0; i < min(waves, Hkv - h0); ++i) total += s_sum[i][lane];
   }
-  if (wave == 0 && j < Nk) put_score(out + j, total, decay);
+  if (wave == 0 && j < Nk) out[j] = total;
 }
 
 // ---- fp32 tier ------------------------------------------------------------------------------
@@ -1318,18 +1317,18 @@ extern "C" int pc_score_cut(int Hq, int Hkv, int n_qs, int Nk, int n_scored, flo
 
 int pc::score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, int n_qs, int Nk, int D, int64_t q_stride_h,
                    int64_t k_stride_h, const int32_t* q_rows, float scale, const float* lse, int64_t lse_stride_h, float* score,
-                   int64_t score_stride_h, int share_heads, int key_begin, int key_end, float decay, void* ws,
-                   size_t ws_bytes, void* stream) {
+                   int64_t score_stride_h, int share_heads, int key_begin, int key_end, ScoreParts* parts,
+                   int32_t* any_far, void* ws, size_t ws_bytes, void* stream) {
   PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "pc_score: dtype %d", dtype);
   PC_REQUIRE(Hq > 0 && Hkv > 0 && Hq % Hkv == 0, PC_ERR_SHAPE,
              "pc_score: Hq=%d must be a positive multiple of Hkv=%d", Hq, Hkv);
   PC_REQUIRE(n_qs >= 1 && Nk >= 1, PC_ERR_SHAPE, "pc_score: n_qs=%d Nk=%d must be >= 1", n_qs, Nk);
   PC_REQUIRE(scale > 0.f && isfinite(scale), PC_ERR_SHAPE, "pc_score: scale %g must be > 0", scale);
-  PC_REQUIRE(Qs && K && score, PC_ERR_NULL, "pc_score: Qs, K or score is NULL");
+  PC_REQUIRE(Qs && K && (score || parts), PC_ERR_NULL, "pc_score: Qs, K or score is NULL");
   PC_REQUIRE((q_rows != nullptr || q_stride_h >= static_cast<int64_t>(n_qs) * D || Hq == 1) &&
                  (k_stride_h >= static_cast<int64_t>(Nk) * D || Hkv == 1),
              PC_ERR_SHAPE, "pc_score: a head stride is smaller than rows*D");
-  PC_REQUIRE(share_heads || Hkv == 1 || score_stride_h >= Nk, PC_ERR_SHAPE,
+  PC_REQUIRE(parts || share_heads || Hkv == 1 || score_stride_h >= Nk, PC_ERR_SHAPE,
              "pc_score: score head stride %lld < Nk", static_cast<long long>(score_stride_h));
   if (key_end <= 0) key_end = Nk;  // 0: up to the last key
   PC_REQUIRE(key_begin >= 0 && key_begin < key_end && key_end <= Nk, PC_ERR_SHAPE,
@@ -1386,8 +1385,8 @@ int pc::score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, in
       }
       PC_CHECK_LAUNCH("pc_score row pass");
     }
-    RowNorm norm = {nullptr, lse, lse_stride_h, q_rows, ws_part, static_cast<int64_t>(Hq) * n_qs, row.n_splits, rep, by_qs};
-    const bool direct = col.n_qsplits == 1 && !share_heads && decay < 0.f;
+    RowNorm norm = {nullptr, lse, lse_stride_h, q_rows, ws_part, static_cast<int64_t>(Hq) * n_qs, row.n_splits, rep, by_qs, any_far};
+    const bool direct = col.n_qsplits == 1 && !share_heads && parts == nullptr;
     float* col_out = direct ? score_r : ws_col;
     const int64_t col_stride = direct ? score_stride_h : nkr;
     if (!col.prepares) {
@@ -1411,13 +1410,15 @@ int pc::score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, in
           ceil_div(ceil_div(rep * n_qs, kTileRows), col.n_qsplits));
     }
     PC_CHECK_LAUNCH("pc_score column pass");
-    if (!direct) {
+    if (parts != nullptr) {
+      *parts = {ws_col, col.n_qsplits};
+    } else if (!direct) {
       if (share_heads && col.n_qsplits > 1)
         score_reduce_heads<<<ceil_div(nkr, 64), 64 * std::min(Hkv, kReduceHeads), 0, s>>>(ws_col, score_r, col.n_qsplits,
-                                                                                         Hkv, nkr, decay);
+                                                                                         Hkv, nkr);
       else
         score_reduce<<<dim3(ceil_div(nkr, 256), share_heads ? 1 : Hkv), 256, 0, s>>>(
-            ws_col, score_r, score_stride_h, col.n_qsplits, Hkv, nkr, share_heads, decay);
+            ws_col, score_r, score_stride_h, col.n_qsplits, Hkv, nkr, share_heads);
       PC_CHECK_LAUNCH("pc_score reduce");
     }
     return PC_OK;
@@ -1436,7 +1437,7 @@ int pc::score_keys(const void* Qs, const void* K, int dtype, int Hq, int Hkv, in
                      q_stride_h, k_stride_h, scale, s);
     PC_CHECK_LAUNCH("pc_score passes");
     if (share_heads) {
-      score_reduce<<<ceil_div(nkr, 256), 256, 0, s>>>(ws_col, score + key_begin, score_stride_h, 1, Hkv, nkr, 1, decay);
+      score_reduce<<<ceil_div(nkr, 256), 256, 0, s>>>(ws_col, score + key_begin, score_stride_h, 1, Hkv, nkr, 1);
       PC_CHECK_LAUNCH("pc_score head sum");
     }
   }
@@ -1449,5 +1450,5 @@ extern "C" int pc_score(const void* Qs, const void* K, int dtype, int Hq, int Hk
                         int64_t score_stride_h, int share_heads, int key_begin, int key_end,
                         void* ws, size_t ws_bytes, void* stream) {
   return score_keys(Qs, K, dtype, Hq, Hkv, n_qs, Nk, D, q_stride_h, k_stride_h, q_rows, scale, lse, lse_stride_h, score,
-                    score_stride_h, share_heads, key_begin, key_end, -1.f, ws, ws_bytes, stream);
+                    score_stride_h, share_heads, key_begin, key_end, nullptr, nullptr, ws, ws_bytes, stream);
 }

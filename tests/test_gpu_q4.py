@@ -303,6 +303,13 @@ def test_attn_hidden_keys_and_rows_without_any_other(dtype, weights, big, level,
     check_hidden_rows(dtype, D, Hq, Hkv, Nq, Nk, weights, big, level, scale, first)
 
 
+@pytest.mark.parametrize("weights", ["each", "one", None])
+@pytest.mark.parametrize("big,level,scale", HIDDEN_BY)
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk,first", [(4, 2, 400, 900, 290), (16, 8, 385, 130, 60), (6, 2, 1000, 33, 10), (2, 1, 800, 3000, 1500)])
+def test_attn_many_rows_hidden_keys_and_rows_without_any_other(weights, big, level, scale, Hq, Hkv, Nq, Nk, first):
+    check_hidden_rows("bf16", 128, Hq, Hkv, Nq, Nk, weights, big, level, scale, first)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Nq", [1, 20, 130])
 def test_attn_not_a_number(dtype, Nq):
