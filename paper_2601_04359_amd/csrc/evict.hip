@@ -841,6 +841,7 @@ extern "C" int pc_evict(void* K, void* V, int dtype, int H, int D, int64_t k_str
   PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "%s: dtype %d", who, dtype);
   PC_REQUIRE(D > 0 && D <= 1024 && D % 8 == 0, PC_ERR_UNSUPPORTED, "%s: D=%d must be a multiple of 8, at most 1024", who, D);
   PC_REQUIRE(K && V, PC_ERR_NULL, "%s: K or V is NULL", who);
+  if (H == 1) k_stride_h = v_stride_h = static_cast<int64_t>(Nk) * D;     // one head has no stride that matters
   PC_REQUIRE(H <= 1 || (k_stride_h >= static_cast<int64_t>(Nk) * D && v_stride_h >= static_cast<int64_t>(Nk) * D), PC_ERR_SHAPE,
              "%s: a head stride is smaller than rows*D", who);
   const int elt = dtype == PC_BF16 ? 2 : 4;

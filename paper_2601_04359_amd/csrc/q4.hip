@@ -873,7 +873,8 @@ extern "C" int pc_q4_store(const void* K, const void* V, int dtype, int H, int n
              PC_ERR_SHAPE, "%s: rows up to %lld do not fit the strides of pos or weights", who, static_cast<long long>(end));
   if (n == 0) return PC_OK;
   PC_REQUIRE(K && V, PC_ERR_NULL, "%s: K or V is NULL", who);
-  PC_REQUIRE(H == 1 || (k_stride_h >= static_cast<int64_t>(n) * D && v_stride_h >= static_cast<int64_t>(n) * D), PC_ERR_SHAPE,
+  if (H == 1) k_stride_h = v_stride_h = static_cast<int64_t>(n) * D;      // one head has no stride that matters
+  PC_REQUIRE(k_stride_h >= static_cast<int64_t>(n) * D && v_stride_h >= static_cast<int64_t>(n) * D, PC_ERR_SHAPE,
              "%s: a head stride is smaller than rows*D", who);
   PC_REQUIRE(aligned16(K, k_stride_h, dtype) && aligned16(V, v_stride_h, dtype), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
@@ -907,8 +908,9 @@ int load_rows(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype
   if (int rc = check_q4_span(cache, H, row0, n, D, who)) return rc;
   PC_REQUIRE(K || V, PC_ERR_NULL, "%s: K and V are NULL", who);
   if (n == 0) return PC_OK;
-  PC_REQUIRE(H == 1 || ((!K || k_stride_h >= static_cast<int64_t>(n) * D) && (!V || v_stride_h >= static_cast<int64_t>(n) * D)),
-             PC_ERR_SHAPE, "%s: a head stride is smaller than rows*D", who);
+  if (H == 1) k_stride_h = v_stride_h = static_cast<int64_t>(n) * D;
+  PC_REQUIRE((!K || k_stride_h >= static_cast<int64_t>(n) * D) && (!V || v_stride_h >= static_cast<int64_t>(n) * D), PC_ERR_SHAPE,
+             "%s: a head stride is smaller than rows*D", who);
   PC_REQUIRE((!K || aligned16(K, k_stride_h, dtype)) && (!V || aligned16(V, v_stride_h, dtype)), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
   const int64_t per = static_cast<int64_t>(H) * n, units = per * ((K != nullptr) + (V != nullptr));
@@ -960,7 +962,8 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
   PC_REQUIRE(Q != O, PC_ERR_SHAPE, "%s: O may not be Q: the weights read the queries again", who);
   if (int rc = check_q4_cache(cache, D, who)) return rc;
   if (int rc = check_q4_span(cache, Hkv, 0, Nk, D, who)) return rc;
-  PC_REQUIRE(Hq == 1 || (q_stride_h >= static_cast<int64_t>(Nq) * D && o_stride_h >= static_cast<int64_t>(Nq) * D), PC_ERR_SHAPE,
+  if (Hq == 1) q_stride_h = o_stride_h = static_cast<int64_t>(Nq) * D;    // one head has no stride that matters
+  PC_REQUIRE(q_stride_h >= static_cast<int64_t>(Nq) * D && o_stride_h >= static_cast<int64_t>(Nq) * D, PC_ERR_SHAPE,
              "%s: a head stride is smaller than rows*D", who);
   PC_REQUIRE(aligned16(Q, q_stride_h, dtype) && aligned16(O, o_stride_h, dtype), PC_ERR_SHAPE,
              "%s: bf16 tensors and head strides must be 16-byte aligned", who);

@@ -541,6 +541,27 @@ def test_one_row_of_any_stride(monkeypatch, native):
         pk.pc_q4_store(x[0, 0, :H, ::2][:, None], x[0, 0, :H, ::2][:, None], pk.q4_cache(H, 3, 64), 0)      # dims apart
 
 
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("Nq", [1, 30, 767, 768])
+def test_one_head_of_any_stride(Nq, weights):
+    """A single head as a projection leaves it, [Nq][1][D], seen as [1][Nq][D]: its stride between heads is D, or anything."""
+    D, Nk = 128, 300
+    x, k, v = (torch.randn((n, 1, D), device=DEV).to(torch.bfloat16) for n in (Nq, Nk, Nk))
+    Q, K, V = (t.transpose(0, 1) for t in (x, k, v))
+    assert Q.stride(0) == D
+    cache, w, wo = pk.q4_cache(1, Nk, D), torch.zeros((1, Nk), device=DEV), torch.zeros((1, Nk), device=DEV)
+    pk.pc_q4_store(K, V, cache, 0)
+    out = torch.zeros((Nq, 1, D), device=DEV, dtype=torch.bfloat16)
+    pk.pc_q4_attn(Q, cache, Nk, 0.1, O=out.transpose(0, 1), weights=w if weights else None)
+    want = pk.pc_q4_attn(x.view(1, Nq, D), cache, Nk, 0.1, weights=wo if weights else None)
+    assert torch.equal(out.transpose(0, 1), want) and torch.equal(w, wo)
+    back = torch.zeros((Nk, 1, D), device=DEV)
+    pk.pc_q4_load(cache, 0, K=back.transpose(0, 1))
+    assert torch.equal(back.transpose(0, 1), pk.pc_q4_load(cache, 0, K=torch.zeros((1, Nk, D), device=DEV))[0])
+    odd = torch.as_strided(x, (1, Nq, D), (Nq * D + 1, D, 1))
+    assert torch.equal(pk.pc_q4_attn(odd, cache, Nk, 0.1), pk.pc_q4_attn(x.view(1, Nq, D), cache, Nk, 0.1))
+
+
 def step_inputs(rng, layers, Hq, Hkv, n, D, t):
     K, V = (torch.from_numpy(rng.standard_normal((layers, Hkv, n, D))).to(torch.bfloat16).to(DEV) for _ in range(2))
     Q = torch.from_numpy(rng.standard_normal((layers, Hq, n, D)) * 2).to(torch.bfloat16).to(DEV)

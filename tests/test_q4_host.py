@@ -185,6 +185,19 @@ def test_calls_that_do_nothing(L):
     assert q4_evict(L, n_keep=0, ws=None) == 0
 
 
+HIP = -7
+
+
+def test_one_head_has_no_stride_to_be_checked(L):
+    """Each call gets past the strides: what is missing is the workspace, or a launch (there is no device to launch on)."""
+    for st in (0, 128, 1001):
+        assert attn(L, Hq=1, Hkv=1, Nq=5, qs=st, os=st, w=A, Hsel=1, ws=None) == WORKSPACE
+        assert evict(L, H=1, Hsel=1, ks=st, vs=st, ws=None) == WORKSPACE
+    if not torch.cuda.is_available():
+        for st in (0, 128, 1001):
+            assert store(L, H=1, ks=st, vs=st) == HIP and load(L, H=1, ks=st, vs=st) == HIP
+
+
 def test_workspaces(L):
     assert pk.pc_evict_workspace_bytes(4, 100, 100) == 0 and pk.pc_evict_workspace_bytes(4, 100, 0) == 0
     assert pk.pc_evict_workspace_bytes(0, 100, 50) == 0 and pk.pc_evict_workspace_bytes(4, 100, 99) > 0
