@@ -404,7 +404,7 @@ int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtyp
 /* ---------------------------------------------------------------------------------------
  * pc_q4_attn -- pc_frame_attn over the first Nk rows of a 4-bit cache, for one token up to whole
  * frames: O = softmax(Q K^T * scale) V, no mask.
- *   Q, O     dev [Hq][Nq][D] of dtype, head strides in elements, two buffers; Nq, Nk >= 1, Nk <= 2^30
+ *   Q, O     dev [Hq][Nq][D] of dtype, head strides in elements, without a byte in common; Nq, Nk >= 1, Nk <= 2^30
  *   lse      dev or NULL, fp32 [Hq][Nq] = ln sum_j exp(scale * q.k_j)
  *   weights  dev or NULL, fp32 [Hsel][Nk], Hsel = Hkv or 1: every key's attention weight is added to its
  *            sum, weights[h][j] = decay * weights[h][j] + the sum of row j's probabilities over the

@@ -847,6 +847,18 @@ Q4Rows rows_of(const pc_q4_cache* c) {
   return {c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->code_stride_h, c->scale_stride_h};
 }
 
+// Whether the `bytes` of some head of a share one with those of some head of b; strides in bytes, `bytes` at least.
+bool heads_overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int H, int64_t bytes) {
+  const int64_t gap = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  if (gap >= (H - 1) * a_stride + bytes || -gap >= (H - 1) * b_stride + bytes) return false;
+  for (int i = 0; i < H; ++i) {      // heads may be interleaved: the two heads of b around head i of a
+    const int64_t x = i * a_stride - gap, j = x >= 0 ? x / b_stride : -1;
+    if (j >= 0 && j < H && x - j * b_stride < bytes) return true;
+    if (j + 1 < H && (j + 1) * b_stride - x < bytes) return true;
+  }
+  return false;
+}
+
 bool aligned16(const void* p, int64_t stride, int dtype) {
   return dtype == PC_F32 ? reinterpret_cast<uintptr_t>(p) % 4 == 0
                          : reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0;
@@ -959,7 +971,6 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
              "%s: Hq=%d must be a positive multiple of Hkv=%d, Nq=%d and Nk=%d at least 1", who, Hq, Hkv, Nq, Nk);
   PC_REQUIRE(scale > 0.f && isfinite(scale), PC_ERR_SHAPE, "%s: scale %g must be > 0", who, scale);
   PC_REQUIRE(Q && O, PC_ERR_NULL, "%s: Q or O is NULL", who);
-  PC_REQUIRE(Q != O, PC_ERR_SHAPE, "%s: O may not be Q: the weights read the queries again", who);
   if (int rc = check_q4_cache(cache, D, who)) return rc;
   if (int rc = check_q4_span(cache, Hkv, 0, Nk, D, who)) return rc;
   if (Hq == 1) q_stride_h = o_stride_h = static_cast<int64_t>(Nq) * D;    // one head has no stride that matters
@@ -967,6 +978,9 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
              "%s: a head stride is smaller than rows*D", who);
   PC_REQUIRE(aligned16(Q, q_stride_h, dtype) && aligned16(O, o_stride_h, dtype), PC_ERR_SHAPE,
              "%s: bf16 tensors and head strides must be 16-byte aligned", who);
+  const int elt = dtype == PC_BF16 ? 2 : 4;
+  PC_REQUIRE(!heads_overlap(Q, q_stride_h * elt, O, o_stride_h * elt, Hq, static_cast<int64_t>(Nq) * D * elt), PC_ERR_SHAPE,
+             "%s: O may not overlap Q: queries are read again behind the first outputs", who);
   if (weights != nullptr) {
     PC_REQUIRE(Hsel == 1 || Hsel == Hkv, PC_ERR_SHAPE, "%s: weights of %d heads for %d KV heads", who, Hsel, Hkv);
     PC_REQUIRE(Hsel == 1 || weights_stride_h >= Nk, PC_ERR_SHAPE, "%s: weights' head stride is smaller than Nk", who);

@@ -198,6 +198,29 @@ def test_one_head_has_no_stride_to_be_checked(L):
             assert store(L, H=1, ks=st, vs=st) == HIP and load(L, H=1, ks=st, vs=st) == HIP
 
 
+def test_attn_refuses_an_output_that_overlaps_the_queries(L):
+    """Against a comparison of every head with every head; interleaved heads do not overlap."""
+    rng = np.random.default_rng(3)
+    seen = [0, 0]
+    for _ in range(3000):
+        Hkv, rep, Nq, dtype = int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(0, 2))
+        elt, size = (4, 2)[dtype], Nq * 64
+        qs, os_ = (size + int(rng.integers(0, 4)) * size // 2 // 8 * 8 for _ in range(2))
+        if rng.random() < 0.5:
+            os_ = qs
+        gap = int(rng.integers(-Hkv * rep * 2 * size * elt // 16, Hkv * rep * 2 * size * elt // 16)) * 16
+        if rng.random() < 0.5:
+            gap = int(rng.integers(-4, 5)) * size * elt // 2
+        q0, o0 = A, A + gap
+        hits = any(q0 + i * qs * elt < o0 + j * os_ * elt + size * elt and o0 + j * os_ * elt < q0 + i * qs * elt + size * elt
+                   for i in range(Hkv * rep) for j in range(Hkv * rep))
+        status = attn(L, Q=q0, O=o0, dtype=dtype, D=64, Hq=Hkv * rep, Hkv=Hkv, Nq=Nq, qs=qs, os=os_, w=A, Hsel=1, ws=None)
+        assert status == (SHAPE if hits else WORKSPACE), (Hkv * rep, Nq, dtype, qs, os_, gap)
+        assert not hits or b"overlap" in L.pc_last_error_detail()
+        seen[hits] += 1
+    assert min(seen) > 300, seen
+
+
 def test_workspaces(L):
     assert pk.pc_evict_workspace_bytes(4, 100, 100) == 0 and pk.pc_evict_workspace_bytes(4, 100, 0) == 0
     assert pk.pc_evict_workspace_bytes(0, 100, 50) == 0 and pk.pc_evict_workspace_bytes(4, 100, 99) > 0
