@@ -17,6 +17,9 @@ constexpr float kNoRef = -3.402823466e38f;     // the reference of a row that ha
 // many heads fills a launch.
 // ------------------------------------------------------------------------------------------
 constexpr int kCopyThreads = 256;
+// Threads of a launch along one axis fit 32 bits.  Rows of K and of V that one launch copies, in threads:
+constexpr int64_t kMaxThreads = UINT32_MAX;
+inline int64_t copy_threads(int64_t rows, int D) { return (rows * (D / 8) + kCopyThreads - 1) / kCopyThreads * kCopyThreads; }
 
 struct RowsAt {          // rows 0 .. n - 1 of H heads of two tensors
   int H, D;
@@ -778,7 +781,8 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
 constexpr size_t kWsAlign = 256;
 // Query rows of a KV head from which on the cache is turned into bf16 rows first.
 // 16/4 heads, direct and over expanded rows: 512 rows x 60,000 keys 92 and 123 us, 768 rows 160 and 144; x 16,000 34 and 44,
-// 54 and 53.  Short caches of three heads to a KV head lose by it (24/8, 768 rows x 4,000 keys 28 and 36 us).
+// 54 and 53.  Short caches of three heads to a KV head lose by it (24/8, 768 rows x 4,000 keys 28 and 36 us).  A cache of
+// more rows than one launch expands is read as it lies.
 constexpr int kExpandRows = 768;
 
 // How a call is made, and what lies where in its workspace (`base` may be NULL where only the size is asked for).
@@ -801,7 +805,7 @@ struct Q4Plan {
       at += align_up(static_cast<size_t>(n), kWsAlign);
       return p;
     };
-    expand = dtype == PC_BF16 && D == 128 && rows >= kExpandRows;
+    expand = dtype == PC_BF16 && D == 128 && rows >= kExpandRows && copy_threads(2ll * Hkv * Nk, D) <= kMaxThreads;
     if (expand) {
       const int64_t bytes_kv = static_cast<int64_t>(Hkv) * Nk * D * 2;
       k_rows = static_cast<uint16_t*>(take(bytes_kv));
@@ -891,8 +895,9 @@ extern "C" int pc_q4_store(const void* K, const void* V, int dtype, int H, int n
   PC_REQUIRE(aligned16(K, k_stride_h, dtype) && aligned16(V, v_stride_h, dtype), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
   const int64_t units = 2ll * H * n;
-  PC_REQUIRE(units <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
-  const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
+  PC_REQUIRE(units <= INT_MAX - kCopyThreads && copy_threads(units, D) <= kMaxThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who,
+             static_cast<long long>(units));
+  const int blocks = static_cast<int>(copy_threads(units, D) / kCopyThreads);
   const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
   const Book b = {pos_new, pos, weights, pos_stride_h, weights_stride_h, book ? Hsel : 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -926,8 +931,9 @@ int load_rows(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtype
   PC_REQUIRE((!K || aligned16(K, k_stride_h, dtype)) && (!V || aligned16(V, v_stride_h, dtype)), PC_ERR_SHAPE,
              "%s: bf16 rows and head strides must be 16-byte aligned", who);
   const int64_t per = static_cast<int64_t>(H) * n, units = per * ((K != nullptr) + (V != nullptr));
-  PC_REQUIRE(2 * per <= INT_MAX - kCopyThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who, static_cast<long long>(units));
-  const int blocks = static_cast<int>((units * (D / 8) + kCopyThreads - 1) / kCopyThreads);
+  PC_REQUIRE(2 * per <= INT_MAX - kCopyThreads && copy_threads(units, D) <= kMaxThreads, PC_ERR_SHAPE, "%s: %lld rows in one call", who,
+             static_cast<long long>(units));
+  const int blocks = static_cast<int>(copy_threads(units, D) / kCopyThreads);
   const RowsAt at = {H, D, Divisor(n), k_stride_h, v_stride_h};
   const int first = K ? 0 : static_cast<int>(per);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1018,6 +1024,17 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
     constexpr int kDims = decltype(dims)::value;
     const T* q = static_cast<const T*>(Q);
     const int tiles_q = ceil_div(rows, 16 * plan.row_tiles), steps = ceil_div(Nk, kStep);
+    // 128 keys per wave of the scoring where that leaves most of the chip's 1,024 SIMDs one; else waves share keys until there
+    // are two per SIMD.  Work-groups of few waves where keys are few: the chip has room for them side by side.
+    const int64_t wide = static_cast<int64_t>(ceil_div(Nk, 128)) * Hsel, narrow = static_cast<int64_t>(ceil_div(Nk, 64)) * Hsel;
+    const int keys = sizeof(T) == 2 && wide >= 448 ? 128 : 64;      // (fp32 queries in three parts leave no registers for it)
+    int dealt = 1;
+    while (keys == 64 && dealt < kWaves && 16 * dealt < rows && narrow * dealt < 2048) dealt *= 2;
+    int groups = 1;           // powers of two: a compute unit holds eight waves of the widest form
+    while (groups * dealt < kWaves && (keys == 128 ? wide : narrow) >= 1024 * groups) groups *= 2;
+    PC_REQUIRE(static_cast<int64_t>(tiles_q) * Hkv * plan.n_splits * kThreads <= kMaxThreads &&
+                   (weights == nullptr || static_cast<int64_t>(ceil_div(Nk, groups * keys)) * Hsel * 64 * groups * dealt <= kMaxThreads),
+               PC_ERR_SHAPE, "%s: Hq=%d x Nq=%d rows over Nk=%d keys in one call", who, Hq, Nq, Nk);
     const AttnArgs a = {rows_of(cache), rep, Nk, Divisor(Nq), Divisor(tiles_q), tiles_q * Hkv, ceil_div(steps, plan.n_splits),
                         q_stride_h, o_stride_h, c, plan.part_o, plan.part_ml, lse, plan.lse, plan.ref, plan.logits,
                         static_cast<int64_t>(Hkv) * rows};
@@ -1033,14 +1050,6 @@ extern "C" int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, in
       PC_CHECK_LAUNCH(who);
     }
     if (weights != nullptr && !plan.keep_logits) {
-      // 128 keys per wave where that leaves most of the chip's 1,024 SIMDs one; else waves share keys until there are two
-      // per SIMD.  Work-groups of few waves where keys are few: the chip has room for them side by side.
-      const int64_t wide = static_cast<int64_t>(ceil_div(Nk, 128)) * Hsel, narrow = static_cast<int64_t>(ceil_div(Nk, 64)) * Hsel;
-      const int keys = sizeof(T) == 2 && wide >= 448 ? 128 : 64;      // (fp32 queries in three parts leave no registers for it)
-      int dealt = 1;
-      while (keys == 64 && dealt < kWaves && 16 * dealt < rows && narrow * dealt < 2048) dealt *= 2;
-      int groups = 1;           // powers of two: a compute unit holds eight waves of the widest form
-      while (groups * dealt < kWaves && (keys == 128 ? wide : narrow) >= 1024 * groups) groups *= 2;
       const WeighArgs w = {rows_of(cache), rep, Nk, Hkv, Hsel, Divisor(Nq), Divisor(ceil_div(Nk, groups * keys)), dealt,
                            q_stride_h, weights_stride_h, c, decay, plan.lse, plan.ref, weights, {}, nullptr};
       auto weigh = q4_weigh_kernel<T, kDims, 4>;

@@ -221,6 +221,27 @@ def test_attn_refuses_an_output_that_overlaps_the_queries(L):
     assert min(seen) > 300, seen
 
 
+def test_calls_beyond_one_launch_are_refused(L):
+    """A launch has fewer than 2^32 threads: refused just above, not by the runtime, and before anything is launched."""
+    big = cache(code_stride_h=1 << 40, scale_stride_h=1 << 36)
+    for D, n in ((128, 2 ** 27), (64, 2 ** 28)):            # n rows of K and of V, 8 elements per thread
+        for H in (1, 4):
+            kw = dict(D=D, H=H, n=n // H, cache=big)
+            assert store(L, **kw, ks=1 << 40, vs=1 << 40) == SHAPE and b"pc_q4_store" in L.pc_last_error_detail()
+            assert load(L, **kw, ks=1 << 40, vs=1 << 40) == SHAPE and b"pc_q4_load" in L.pc_last_error_detail()
+    # 32 rows per work-group of 512 threads
+    for dtype, Hkv in ((0, 1), (0, 4), (1, 2)):
+        st = attn(L, D=64, dtype=dtype, Hq=Hkv, Hkv=Hkv, Nq=2 ** 28 // Hkv, qs=1 << 40, os=1 << 40, Q=A + (1 << 60), cache=big)
+        assert st == SHAPE and b"pc_q4_attn" in L.pc_last_error_detail()
+
+
+def test_a_cache_beyond_one_launch_is_not_expanded(L):
+    """From 768 rows on a cache is expanded to bf16 rows (2 x 256 bytes for each), up to what one launch copies."""
+    rows = lambda Hkv, Nk: pk.pc_q4_attn_workspace_bytes(pk.PC_BF16, 2 * Hkv, Hkv, 1000, Nk, 128) // (Hkv * Nk * 512)
+    for Hkv in (1, 4):
+        assert rows(Hkv, 2 ** 27 // Hkv - 16) == 1 and rows(Hkv, 2 ** 27 // Hkv) == 0 and rows(Hkv, 2 ** 27 // Hkv + 1) == 0
+
+
 def test_workspaces(L):
     assert pk.pc_evict_workspace_bytes(4, 100, 100) == 0 and pk.pc_evict_workspace_bytes(4, 100, 0) == 0
     assert pk.pc_evict_workspace_bytes(0, 100, 50) == 0 and pk.pc_evict_workspace_bytes(4, 100, 99) > 0
