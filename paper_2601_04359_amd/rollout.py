@@ -318,28 +318,38 @@ class EvictingStack:
         self.weights = torch.zeros((n_layers * self.hsel, self.capacity), dtype=torch.float32, device=device)
         self.nk = 0      # rows when a step begins
         self.n_new = 0   # rows of the step under way
+        self._appended: set[int] = set()   # layers that have them
 
     def layer(self, layer: int):
         """The layer's part: (4-bit cache, pos, weights), as views."""
+        if not 0 <= layer < self.L:
+            raise ValueError(f"layer {layer} of {self.L}")
         a, s = layer * self.Hkv, layer * self.hsel
         return (tuple(t[a:a + self.Hkv] for t in self.cache), self.pos[s:s + self.hsel], self.weights[s:s + self.hsel])
 
     def append(self, layer: int, K, V, pos_new, rotate: bool = True) -> None:
         """K, V [Hkv][n][D] of the step become the layer's newest rows, at coordinates pos_new (int32 [n][3], device);
-        with `rotate` the keys are rotated in place first.  Every layer of a step appends the same number of rows."""
+        with `rotate` the keys are rotated in place first.  Every layer of a step appends once, the same number of rows."""
         n = K.shape[1]
+        if n < 1:
+            raise ValueError("a step appends at least one row")
         if self.nk + n > self.capacity:
             raise ValueError(f"cache capacity {self.capacity} < {self.nk} + {n}")
         if self.n_new not in (0, n):
             raise ValueError(f"{n} rows after {self.n_new} in another layer of the same step")
-        self.n_new = n
+        if layer in self._appended:
+            raise ValueError(f"layer {layer} has its rows of this step; end_step() begins the next one")
         cache, pos, weights = self.layer(layer)
         if rotate:
             pk.pc_rope3d(K, pos_new, self.sections, self.base)
         pk.pc_q4_store(K, V, cache, self.nk, pos_new=pos_new, pos=pos, weights=weights)
+        self.n_new = n
+        self._appended.add(layer)
 
     def attend(self, layer: int, Q, O=None, q_pos=None, lse=None, accumulate: bool = True):
         """Queries Q [Hq][n][D] over the layer's cache -> O.  q_pos (int32 [n][3], device): rotate Q in place first."""
+        if self._appended and layer not in self._appended:
+            raise ValueError(f"layer {layer} has no rows of this step yet")
         if q_pos is not None:
             pk.pc_rope3d(Q, q_pos, self.sections, self.base)
         cache, _, weights = self.layer(layer)
@@ -348,6 +358,9 @@ class EvictingStack:
 
     def end_step(self) -> int:
         """The step's rows are part of the cache; above the budget all layers are cut to it.  Returns the rows left."""
+        if self._appended and len(self._appended) < self.L:
+            raise ValueError(f"layers {sorted(set(range(self.L)) - self._appended)} have no rows of this step")
+        self._appended.clear()
         self.nk, self.n_new = self.nk + self.n_new, 0
         if self.nk > self.budget:
             self.nk = pk.pc_q4_evict(self.cache, self.pos, self.weights, self.nk, self.budget, self.n_anchor, self.recent_t)

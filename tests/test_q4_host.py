@@ -298,3 +298,52 @@ def test_a_cache_without_heads_is_refused():
         pk.pc_q4_attn(torch.zeros((2, 1, 128)), empty, 4, 0.1)
     with pytest.raises(pk.PackCacheError, match="at least one head"):
         pk.pc_q4_store(torch.zeros((0, 1, 128)), torch.zeros((0, 1, 128)), empty, 0)
+
+
+def test_stack_refuses_layers_that_are_not_in_step(monkeypatch):
+    """Every layer appends once per step: a second append, an attend in front of it and a step without one are errors, and a
+    store that is refused leaves the step as it was."""
+    from paper_2601_04359_amd import rollout
+    calls = []
+
+    def stored(*args, **kw):
+        calls.append("store")
+        if len(calls) == 1:
+            raise pk.PackCacheError(-2, "refused")
+
+    monkeypatch.setattr(rollout.pk, "pc_q4_store", stored)
+    monkeypatch.setattr(rollout.pk, "pc_q4_attn", lambda *a, **kw: calls.append(("attn", a[2])))
+    monkeypatch.setattr(rollout.pk, "pc_q4_evict", lambda *a, **kw: calls.append(("evict", a[3])) or a[4])
+    s = EvictingStack(2, 4, 2, 128, budget=8, scale=0.1, step_rows=4, device="cpu")
+    x, pos, q = torch.zeros((2, 3, 128)), torch.zeros((3, 3), dtype=torch.int32), torch.zeros((4, 3, 128))
+
+    def append(layer):
+        s.append(layer, x, x, pos, rotate=False)
+
+    with pytest.raises(pk.PackCacheError):
+        append(0)
+    assert s.n_new == 0 and s.end_step() == 0
+    for layer in (-1, 2):
+        with pytest.raises(ValueError):
+            append(layer)
+        with pytest.raises(ValueError):
+            s.attend(layer, q)
+    with pytest.raises(ValueError):
+        s.append(0, x[:, :0], x[:, :0], pos[:0], rotate=False)
+    for step in (0, 1, 2):
+        append(1)
+        with pytest.raises(ValueError):
+            append(1)
+        with pytest.raises(ValueError):
+            s.attend(0, q)
+        with pytest.raises(ValueError):
+            s.end_step()
+        s.attend(1, q)
+        assert calls[-1] == ("attn", min(3 * step + 3, 11))
+        append(0)
+        s.attend(0, q)
+        s.attend(1, q, accumulate=False)
+        assert s.end_step() == min(3 * step + 3, 8)
+    assert calls[-1] == ("evict", 9) and s.nk == 8
+    s.attend(0, q)                             # between steps: the cache as it stands
+    assert calls[-1] == ("attn", 8)
