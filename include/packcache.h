@@ -427,7 +427,8 @@ int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, int Hq, int H
  * in rows 0 .. n_keep - 1, in place.  For every selection head on its own, in this order:
  *   rows below n_anchor, and rows whose t = pos[row][0] is above t of row Nk - 1 minus recent_t
  *   (recent_t = 0: none; pos may then be NULL); then larger weights first, NaN last; equal ones: the
- *   lower row first.
+ *   lower row first.  Rows of the first two kinds are equal: if there are more than n_keep of them, the lowest
+ *   stay and the newest leave, so n_keep has to hold the anchors and every row of the last recent_t.
  * A kept row below n_keep stays where it is.  The kept rows from n_keep on fill the rows that were
  * evicted below n_keep, both in ascending order: attention does not ask for an order of its keys,
  * and only these rows move (K, V, pos and weights, bit for bit).  Rows from n_keep on are left as they

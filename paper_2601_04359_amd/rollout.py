@@ -299,16 +299,29 @@ class EvictingStack:
         end_step()                 a cache above its budget loses the rows of least weight, all layers in one call
 
     Rows below n_anchor (the prompt) and rows whose t coordinate is within recent_t of the newest row's are kept
-    whatever their weight.  With the budget reached, a step of n rows goes from budget to budget + n rows and back:
+    whatever their weight.  New rows need that: a row's sum begins at 0 and competes with sums over all earlier steps, so
+    without a window (recent_t = 0 and no decay) a step's own rows tend to be the ones that leave, and the cache stays what
+    it was when it filled up.  The default window is half of what the anchors leave.  A window is counted in t: where rows
+    share one (the tokens of a frame), rows_per_t says how many, and anchors and window together have to fit the budget (of
+    more protected rows than that the lowest would stay, and the newest leave).
+
+    attend() applies no mask: the rows of one step see each other.  Text that must not look ahead goes in token by token.
+
+    With the budget reached, a step of n rows goes from budget to budget + n rows and back:
     the same launches every time, so a step can be recorded into a HIP graph and replayed.
     """
 
     def __init__(self, n_layers: int, Hq: int, Hkv: int, D: int, budget: int, scale: float, step_rows: int = 1,
-                 n_anchor: int = 0, recent_t: int = 0, decay: float = 1.0, sections=(32, 48, 48), base: float = 10000.0,
-                 device="cuda:0", share_heads: bool = False):
+                 n_anchor: int = 0, recent_t: int | None = None, decay: float = 1.0, sections=(32, 48, 48),
+                 base: float = 10000.0, device="cuda:0", share_heads: bool = False, rows_per_t: int = 1):
         import torch
-        if not 0 <= n_anchor <= budget or budget < 1 or step_rows < 1:
-            raise ValueError(f"budget {budget} rows, {n_anchor} of them anchors, {step_rows} new ones per step")
+        if not 0 <= n_anchor <= budget or budget < 1 or step_rows < 1 or rows_per_t < 1:
+            raise ValueError(f"budget {budget} rows, {n_anchor} of them anchors, {step_rows} new ones per step, {rows_per_t} per t")
+        room = budget - n_anchor
+        if recent_t is None:
+            recent_t = max(room // 2 // rows_per_t, int(room >= rows_per_t))
+        if recent_t < 0 or recent_t * rows_per_t > room:
+            raise ValueError(f"{n_anchor} anchors and the rows of {recent_t} t, {rows_per_t} each, in a budget of {budget}")
         self.L, self.Hq, self.Hkv, self.D, self.budget, self.scale = n_layers, Hq, Hkv, D, budget, scale
         self.capacity, self.n_anchor, self.recent_t, self.decay = budget + step_rows, n_anchor, recent_t, decay
         self.sections, self.base, self.hsel = tuple(sections), base, 1 if share_heads else Hkv

@@ -347,3 +347,33 @@ def test_stack_refuses_layers_that_are_not_in_step(monkeypatch):
     assert calls[-1] == ("evict", 9) and s.nk == 8
     s.attend(0, q)                             # between steps: the cache as it stands
     assert calls[-1] == ("attn", 8)
+
+
+@pytest.mark.parametrize("budget,n_anchor,rows_per_t", [(40, 0, 1), (41, 7, 1), (60, 4, 6), (13, 1, 6), (5, 4, 1), (9, 9, 1)])
+def test_stack_keeps_the_newest_rows_by_default(budget, n_anchor, rows_per_t):
+    """Attention that looks at all rows alike, over ten budgets' worth of single rows: the defaults keep the newest row at every
+    step and let the window move with it.  (Without a window the newest row's sum is the least: nothing ever changes.)"""
+    s = EvictingStack(1, 2, 1, 64, budget, 0.1, n_anchor=n_anchor, rows_per_t=rows_per_t, device="cpu")
+    assert s.recent_t * rows_per_t <= budget - n_anchor and (s.recent_t > 0) == (budget - n_anchor >= rows_per_t)
+    t, w = np.zeros(0, np.int64), np.zeros(0)
+    for step in range(10 * budget):
+        t, w = np.append(t, step // rows_per_t), np.append(w, 0.0)
+        w = s.decay * w + 1.0 / len(w)
+        src = orc.evict_rows(w, t, len(w), min(budget, len(w)), n_anchor, s.recent_t)
+        t, w = t[src], w[src]
+        if s.recent_t:
+            assert step // rows_per_t in t
+            assert (t == step // rows_per_t).sum() == step % rows_per_t + 1 or step < budget
+    assert (np.sort(t)[::-1][:s.recent_t] >= (step - budget) // rows_per_t).all()
+
+
+def test_stack_refuses_a_window_that_its_budget_cannot_hold():
+    def stack(**kw):
+        return EvictingStack(1, 2, 1, 64, scale=0.1, device="cpu", **kw)
+
+    for kw in (dict(budget=10, recent_t=11), dict(budget=10, n_anchor=4, recent_t=7), dict(budget=10, recent_t=4, rows_per_t=3),
+               dict(budget=10, recent_t=-1), dict(budget=10, rows_per_t=0), dict(budget=10, recent_t=2 ** 31 - 1)):
+        with pytest.raises(ValueError):
+            stack(**kw)
+    assert stack(budget=10, n_anchor=4, recent_t=6).recent_t == 6 and stack(budget=10, recent_t=3, rows_per_t=3).recent_t == 3
+    assert stack(budget=10, recent_t=0).recent_t == 0 and stack(budget=10, n_anchor=10).recent_t == 0
