@@ -17,7 +17,8 @@ DEV = "cuda:0"
 U = 2.0 ** -24
 D = 128
 # a query's entry, a key's, the scale (the exponent of the largest key's probability is far from 0 unless the product is rounded)
-HIDDEN_BY = [(1e8, -3.0, 128 ** -0.5), (1e12, -2.0, 0.125), (1e20, -2.0, 128 ** -0.5), (1e30, -1.0, 0.125), (1e30, -3.0, 0.1)]
+HIDDEN_BY = [(1e8, -3.0, 128 ** -0.5), (1e12, -2.0, 0.125), (1e20, -2.0, 128 ** -0.5), (1e30, -1.0, 0.125), (1e30, -3.0, 0.1),
+             (1e20, -2.0, pk.PC_SCALE_FOLDED)]     # the shorter loops
 
 
 def hidden_inputs(hq, hkv, nq, nk, big, level, first_visible):

@@ -186,6 +186,28 @@ def test_attn_weights(dtype, weights, Hq, Hkv, Nq, Nk, D, decay):
     check_attn(dtype, Hq, Hkv, Nq, Nk, D, weights=weights, decay=decay, lse=Nk % 2 == 0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk", [(16, 8, 20, 8300), (16, 8, 20, 16500), (24, 8, 9, 12289)])
+def test_attn_weights_of_many_keys(dtype, D, Hq, Hkv, Nq, Nk):
+    """Waves with keys of their own, one, two and four groups of them per work-group, 64 and 128 keys each, the last work-group's
+    in part behind the last key."""
+    check_attn(dtype, Hq, Hkv, Nq, Nk, D, weights="each", decay=0.75)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk", [(128, 16, 1, 700), (128, 16, 1, 3000), (72, 6, 1, 1100), (36, 18, 4, 90)])
+def test_attn_weights_of_many_heads_in_one_sum(dtype, Hq, Hkv, Nq, Nk):
+    """More than 64 kept logit rows behind one sum, in one share of the keys and in several."""
+    check_attn(dtype, Hq, Hkv, Nq, Nk, 64, weights="one", decay=0.9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,Nq,Nk,first", [(128, 16, 1, 700, 350), (128, 16, 1, 3000, 1000), (16, 8, 20, 16500, 9000)])
+def test_attn_hidden_keys_of_many_heads_and_keys(dtype, Hq, Hkv, Nq, Nk, first):
+    check_hidden_rows(dtype, 128, Hq, Hkv, Nq, Nk, "one" if Nq == 1 else "each", 1e20, -2.0, 128 ** -0.5, first)
+
+
 @pytest.mark.parametrize("weights", [None, "each", "one"])
 @pytest.mark.parametrize("Hq,Hkv,Nq,Nk,gaps,decay", [
     (4, 1, 192, 33, 0, 1.0), (8, 2, 200, 300, 0, 0.9), (6, 2, 257, 1000, 5, 0.0), (4, 1, 1000, 1, 0, 0.5), (16, 4, 193, 130, 3, 2.0),
@@ -308,6 +330,12 @@ def test_attn_hidden_keys_and_rows_without_any_other(dtype, weights, big, level,
 @pytest.mark.parametrize("Hq,Hkv,Nq,Nk,first", [(4, 2, 400, 900, 290), (16, 8, 385, 130, 60), (6, 2, 1000, 33, 10), (2, 1, 800, 3000, 1500)])
 def test_attn_many_rows_hidden_keys_and_rows_without_any_other(weights, big, level, scale, Hq, Hkv, Nq, Nk, first):
     check_hidden_rows("bf16", 128, Hq, Hkv, Nq, Nk, weights, big, level, scale, first)
+
+
+@pytest.mark.parametrize("Nq", [1, 30, 400])
+def test_attn_hidden_keys_of_queries_that_carry_the_scale(Nq):
+    """ln 2 as the scale: the form for many rows takes pc_frame_attn's and pc_score's shorter loops."""
+    check_hidden_rows("bf16", 128, 4, 2, Nq, 900, "each", 1e20, -2.0, pk.PC_SCALE_FOLDED, 290)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
