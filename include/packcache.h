@@ -411,8 +411,10 @@ int pc_q4_load(const pc_q4_cache* cache, int H, int row0, int n, int D, int dtyp
  *            Nq rows and the query heads of KV head h (Hsel = 1: all of them).  decay >= 0; 0 does
  *            not read the old value.  The order of the sum is fixed: results are bit-reproducible.
  *   ws       dev, pc_q4_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls
- *            that may overlap on the GPU must not share one.
- * fp32 queries: products and sums are those of fp32 (the cache's values are exact).
+ *            that may overlap on the GPU must not share one.  From 768 query rows per KV head on (bf16, D = 128)
+ *            it holds the Nk rows in bf16: 512 bytes per row and KV head, where the cache has 136.
+ * fp32 queries: products and sums are those of fp32 (the cache's values are exact).  bf16 queries: probabilities
+ * are rounded to bf16 for the product with V, as in pc_frame_attn; lse and weights are not affected.
  * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_BUDGET (decay),
  * PC_ERR_WORKSPACE, PC_ERR_HIP.
  */

@@ -295,13 +295,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(Ranks a, int 
 // ------------------------------------------------------------------------------------------
 // Few rows leave (a cache at its budget that takes a token or a few per step): they are found one after another as
 // the least of all, at one barrier each (0.56 us; 1.2 in two launches), where a threshold takes three counted passes:
-// 4 heads losing one of 3,000 rows 8.3 -> 4.9 us, of 24,000 28 -> 8.2, of 193,792 50 -> 12.4; 112 heads one of 8,321 17.9 -> 13.3.
+// 4 heads losing one of 3,000 rows 8.1 -> 4.8 us, of 24,000 28 -> 8.1, of 193,792 50 -> 12.1; 112 heads one of 8,321 17.9 -> 13.2.
 // Two launches, for caches beyond the registers and where work-groups of 4,096 rows are half of the chip at most: those
 // find the least of theirs, and a work-group per selection head the least of these (8,321 rows of 4 heads 8.0 us, 8.7 in
-// one launch; of 112 heads 15.2 and 13.3).
+// one launch, 24,000 rows 8.0 and 15.8, 5,000 rows 7.6 and 6.8; of 112 heads 15.1 and 13.1).
 // ------------------------------------------------------------------------------------------
 constexpr int kFew = 8;
-// up to four rows of any cache, up to eight of more than 16,384 rows (eight of 1,180 rows 8.4 us one by one, 7.2 by a threshold)
+// up to four rows of any cache, up to eight of more than 16,384 rows (eight of 1,180 rows 7.7 us one by one, 6.3 by a threshold, of
+// 10,000 16.5 and 14.0, of 16,384 16.6 and 19.6; four of 3,000 6.6 and 8.1)
 inline bool few_leave(int Nk, int n_keep) { return Nk - n_keep <= (Nk > 16 * kSelThreads ? kFew : kFew / 2); }
 
 // The row that leaves first: lowest rank, of equal ones the highest row; row -1: none.
@@ -794,6 +795,8 @@ int evict(const char* who, Moves m, int64_t row_bytes, int H, int32_t* pos, int6
     PC_CHECK_LAUNCH(who);
     if (move) return PC_OK;
   } else if (plan.n_slices == 0) {
+    // six and ten rows per thread beside eight and twelve: 4 heads x 5,500 rows 12.8 us, 13.4 with eight, x 9,500 16.3 and 17.2 with
+    // twelve; 28 heads 10.7 and 11.3, 13.6 and 14.3; 112 heads 17.3 and 17.7, 25.1 and 25.7
     const auto kernel = items <= 2    ? evict_select_kernel<2>
                         : items <= 4  ? evict_select_kernel<4>
                         : items <= 6  ? evict_select_kernel<6>

@@ -139,6 +139,10 @@ __global__ __launch_bounds__(kCopyThreads) void q4_load_kernel(T* __restrict__ K
 //     through LDS of the wave's own as bf16 rows, read back by transposing loads.
 //   * Softmax in base 2 against a reference that lags the maximum by at most 2^8; sums in fp32.  Far references take
 //     exponents of their own (see far_exponent).
+//   * bf16 queries: a probability is rounded to bf16 in front of the second product, half a step of its size, as in
+//     pc_frame_attn; the sum it is divided by, the log-sum-exp and the weights are those of the unrounded ones.  Where one
+//     key dominates, the output is off by that and its own rounding (0.0024 of its size, 0.0017 with fp32 probabilities).  A
+//     second part would double the products of a loop whose registers are full at two tiles.
 //   * fp32 queries and probabilities are three bf16 parts each: keys and values are exact in bf16, so the
 //     products are exact and the sums are the fp32 ones.
 // ------------------------------------------------------------------------------------------
@@ -780,9 +784,10 @@ __global__ __launch_bounds__(kThreads) void q4_weigh_kernel(const T* __restrict_
 // ------------------------------------------------------------------------------------------
 constexpr size_t kWsAlign = 256;
 // Query rows of a KV head from which on the cache is turned into bf16 rows first.
-// 16/4 heads, direct and over expanded rows: 512 rows x 60,000 keys 92 and 123 us, 768 rows 160 and 144; x 16,000 34 and 44,
-// 54 and 53.  Short caches of three heads to a KV head lose by it (24/8, 768 rows x 4,000 keys 28 and 36 us).  A cache of
-// more rows than one launch expands is read as it lies.
+// 16/4 heads, direct and over expanded rows: 512 rows x 60,000 keys 96 and 120 us, 768 rows 163 and 144; x 16,000 38 and 46,
+// 56 and 57; x 1,179 13.5 and 12.1, 16.1 and 12.5.  Short caches of three heads to a KV head lose by it (24/8, 768 rows x 4,000
+// keys 30 and 36 us, x 60,000 301 and 255).  The rows are a workspace of 512 bytes per row and KV head.  A cache of more rows
+// than one launch expands is read as it lies.
 constexpr int kExpandRows = 768;
 
 // How a call is made, and what lies where in its workspace (`base` may be NULL where only the size is asked for).
