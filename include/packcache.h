@@ -162,8 +162,8 @@ int pc_rebase(void* K, int dtype, int Hkv, int D, int64_t k_stride_h, int32_t* p
  *          every query's softmax normaliser.  For callers that know which rows can be pruned at
  *          all (anchors never are; a frame that already sits at its budget is not either) and do
  *          not want to pay for scores nobody reads.
- * bf16: a query whose log-sum-exp is beyond +-2^24 ln 2 (1.16e7: it sees nothing but keys that the caller
- * hides) adds nothing to any score; fp32 has no digit left for its probabilities.
+ * A query whose log-sum-exp is beyond +-2^24 ln 2 (1.16e7: it sees nothing but keys that the caller hides)
+ * adds nothing to any score: that number has no digit left to tell its probabilities by.
  * Summation order is fixed (no atomics): results are bit-reproducible.
  * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_WORKSPACE,
  * PC_ERR_HIP.

@@ -955,6 +955,8 @@ __global__ __launch_bounds__(64 * kReduceHeads) void score_reduce_heads(const fl
 }
 
 // ---- fp32 tier ------------------------------------------------------------------------------
+// A row whose log-sum-exp (natural) is that far adds nothing, as in row_norms.
+__device__ __forceinline__ bool far_lse(float x) { return fabsf(x) >= kFarRef * 0.6931471805599453f; }
 // Both passes on the 16x16x4 fp32 MFMA (fp32 operands and accumulation), S^T = K Q^T: lane
 // (r = l % 16, kg = l / 16) holds dims 16 s + 4 kg .. + 3 of key row r and of query row r as
 // 16-byte loads, the four MFMAs of step s contract over (kg, element e), and the result leaves the
@@ -1084,7 +1086,7 @@ __global__ __launch_bounds__(kF32Threads) void score_colpass_f32(const float* __
       const int qr = q_rows ? q_rows[rowc] : rowc;
       q[t].load(Qs + h * q_stride_h + static_cast<int64_t>(qr) * D, kg);
       const float x = lse[h * lse_stride_h + (lse_by_q_row ? qr : rowc)];
-      ls[t] = u0 + t < n_units && row < n_qs ? x : INFINITY;  // padding adds nothing
+      ls[t] = u0 + t < n_units && row < n_qs && !far_lse(x) ? x : INFINITY;  // padding adds nothing
     }
     f32x4 sc[2];
     f32_products<D>(k, q[0], k, q[1], sc);
@@ -1137,7 +1139,7 @@ __global__ __launch_bounds__(kF32Threads) void score_colpass_f32_few(const float
     const int row = min(rho, n_rows - 1) - in_group * n_qs, qr = q_rows ? q_rows[row] : row;
     q[t].load(Qs + h * q_stride_h + static_cast<int64_t>(qr) * D, kg);
     const float x = lse[h * lse_stride_h + (lse_by_q_row ? qr : row)];
-    ls[t] = rho < n_rows ? x : INFINITY;  // padding adds nothing
+    ls[t] = rho < n_rows && !far_lse(x) ? x : INFINITY;  // padding adds nothing
   };
   auto add = [&](const f32x4& sc, int t) {
 #pragma unroll

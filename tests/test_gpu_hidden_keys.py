@@ -21,18 +21,18 @@ HIDDEN_BY = [(1e8, -3.0, 128 ** -0.5), (1e12, -2.0, 0.125), (1e20, -2.0, 128 ** 
              (1e20, -2.0, pk.PC_SCALE_FOLDED)]     # the shorter loops
 
 
-def hidden_inputs(hq, hkv, nq, nk, big, level, first_visible):
+def hidden_inputs(hq, hkv, nq, nk, big, level, first_visible, D=D, dtype=torch.bfloat16):
     g = torch.Generator(device=DEV)
     g.manual_seed(nq + nk)
     Q, K, V = (torch.empty((h, n, D), device=DEV).normal_(generator=g) for h, n in ((hq, nq), (hkv, nk), (hkv, nk)))
     j = torch.arange(nk, device=DEV)
     hidden = (j % 3 != 0) | (j < first_visible)
-    Q[..., 96:], K[..., 96:] = 0.0, 0.0
-    K[..., 127], K[..., 126] = hidden * level, level
+    Q[..., D - 32:], K[..., D - 32:] = 0.0, 0.0
+    K[..., D - 1], K[..., D - 2] = hidden * level, level
     kind = (torch.arange(hq * nq, device=DEV) % 3).view(hq, nq)
     Q[kind > 0] = 0.0
-    Q[..., 127], Q[..., 126] = (kind != 1) * big, (kind > 0) * big
-    return [x.to(torch.bfloat16) for x in (Q, K, V)] + [kind, hidden]
+    Q[..., D - 1], Q[..., D - 2] = (kind != 1) * big, (kind > 0) * big
+    return [x.to(dtype) for x in (Q, K, V)] + [kind, hidden]
 
 
 def reference(Q, K, V, scale, rows):
@@ -88,3 +88,23 @@ def test_score_hidden_keys_and_rows_without_any_other(hq, hkv, nq, nk, given, fi
     # a log-sum-exp of its own or a given one in fp32, and its change of base: three roundings of at most A
     rel = 2 * ((D + 16) * U * A + 8 * U) + 3 * U * A + (hq // hkv * nq + 64) * U
     assert ((score - want).abs() <= rel * want + 1e-30).all(), (score - want).abs().max().item()
+
+
+@pytest.mark.parametrize("big,level,scale", HIDDEN_BY)
+@pytest.mark.parametrize("first", [0, 0.9])
+@pytest.mark.parametrize("D,hq,hkv,nq,nk", [(64, 2, 1, 64, 336), (128, 8, 2, 100, 700), (64, 4, 2, 7, 33), (128, 4, 1, 300, 90)])
+def test_f32_hidden_keys_and_rows_without_any_other(D, hq, hkv, nq, nk, first, big, level, scale):
+    Q, K, V, kind, hidden = hidden_inputs(hq, hkv, nq, nk, big, level, int(first * nk), D, torch.float32)
+    lse = torch.empty((hq, nq), device=DEV)
+    O = pk.pc_frame_attn(Q, K, V, nk, scale, lse=lse)
+    Ow, Lw, p, spread = reference(Q, K, V, scale, torch.arange(nq, device=DEV))
+    A = max(15.0, float(Q[..., :D - 32].abs().sum(-1).max() * K[..., :D - 32].abs().max() * scale))
+    e = (D + 16) * U * A + 8 * U
+    err = (O.double() - Ow).abs()
+    assert (err <= (2 * e + (nk + 64) * U) * spread + 1e-30).all(), (err.max().item(), O.isnan().sum().item())
+    assert ((lse.double() - Lw).abs() <= (D + 16) * U * A + (5 * Lw.abs() + nk + 64) * U).all()
+    want = (p * (kind == 0).double()[..., None]).view(hkv, hq // hkv * nq, nk).sum(1)
+    rel = 2 * e + 3 * U * A + (hq // hkv * nq + 64) * U
+    for given in (None, lse):
+        score = pk.pc_score(Q, K, nk, scale, lse=given).double()
+        assert (score[:, hidden] == 0).all() and ((score - want).abs() <= rel * want + 1e-30).all(), (score - want).abs().max().item()
