@@ -436,7 +436,8 @@ int pc_q4_attn(const void* Q, const pc_q4_cache* cache, int dtype, int Hq, int H
  * and only these rows move (K, V, pos and weights, bit for bit).  Rows from n_keep on are left as they
  * were.  Order in time has to be read from pos, not from the row.
  *   K, V     dev [H][cap][D] of dtype, head strides in elements, 16-byte aligned; D % 8 == 0, D <= 1024
- *   pos      dev or NULL, int32 [Hsel][cap][3]; weights dev fp32 [Hsel][cap]; strides in elements.
+ *   pos      dev or NULL, int32 [Hsel][cap][3]; weights dev fp32 [Hsel][cap]; strides in elements.  pc_q4_attn
+ *            accumulates weights; for a cache in bf16 or fp32 they are the caller's running sum of what pc_score gives.
  *            Head h belongs to selection head h / (H / Hsel): Hsel = H, one per KV head; H / Hsel > 1,
  *            heads that share a selection (of each of several layers).
  *   idx_out  dev or NULL, int32 [Hsel][n_keep]: the row that each of rows 0 .. n_keep - 1 holds now
