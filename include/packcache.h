@@ -61,7 +61,7 @@ typedef struct pc_segment {
   int32_t frame; /* frame id (caller's bookkeeping; copied through) */
 } pc_segment;
 
-#define PC_VERSION 106          /* goes up with every change of an entry point's arguments, and with new ones */
+#define PC_VERSION 107          /* goes up with every change of an entry point's arguments, and with new ones */
 #define PC_MAX_SEGMENTS 120
 #define PC_MAX_SELECT_LEN 4096 /* longest FRAME segment the register-resident select handles
                                   (one work-group per segment); longer segments take a slower
@@ -454,6 +454,91 @@ int pc_q4_evict(const pc_q4_cache* cache, int H, int D, int32_t* pos, int64_t po
                 float* weights, int64_t weights_stride_h, int Hsel, int Nk, int n_keep, int n_anchor,
                 int recent_t, int32_t* idx_out, int64_t idx_stride_h, void* ws, size_t ws_bytes,
                 void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Several sequences at once.  T query rows lie one behind the other; `offs` says whose they are:
+ *   offs     HOST or NULL, int32 [n_seq + 1], not descending, from 0 up to T at most: rows offs[s] ..
+ *            offs[s + 1] - 1 are sequence s (none: nothing happens for it); rows from offs[n_seq] on belong
+ *            to nobody and their outputs are left as they were.  NULL: T / n_seq rows each.
+ * Everything else about the sequences is read on the device, so that a step of one row each can be recorded into a
+ * HIP graph and replayed as the sequences grow.  dtype: bf16 and fp32, D = 64 or 128 (the MFMA forms of bf16 need
+ * D = 128; bf16 with D = 64 runs on the fp32 matrix instructions).  Pointers and strides are 16-byte aligned.
+ *
+ * pc_prompt_attn -- causal attention over whole prompts: row i of a sequence with nq queries and nk keys sees its
+ * keys 0 .. nk - nq + i.
+ *   Q, O     dev [Hq][Tq][D] of dtype, head strides in elements; O has no byte in common with Q, K or V
+ *   K, V     dev [Hkv][Tk][D]
+ *   offs_q   HOST, offsets of Q's rows;  offs_k  HOST or NULL, offsets of K's and V's rows (NULL: offs_q).
+ *            nk > nq: the rows are the last ones of a sequence whose earlier keys are there already;
+ *            nk < nq: the first nq - nk rows see nothing: O = 0, lse = -inf.
+ *   lse      dev or NULL, fp32 [Hq][Tq] = ln sum_j exp(scale * q.k_j) over the keys seen
+ *   scale    > 0; PC_SCALE_FOLDED as in pc_frame_attn
+ * What a row does not see does not reach it, a NaN or an infinity there neither.
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_HIP.
+ */
+int pc_prompt_attn(const void* Q, const void* K, const void* V, int dtype, int Hq, int Hkv, int Tq, int Tk,
+                   int D, int64_t q_stride_h, int64_t k_stride_h, int64_t v_stride_h, int64_t o_stride_h,
+                   float scale, const int32_t* offs_q, const int32_t* offs_k, int n_seq, void* O, float* lse,
+                   void* stream);
+
+/* A cache in pages of page_rows rows (a multiple of 64).  Row r of page p of head h is the D elements from
+ * p * stride_page + h * stride_h + r * D on, in K and in V.  A page's number is the same for all heads. */
+typedef struct pc_pages {
+  void* K;                /* dev */
+  void* V;                /* dev */
+  int64_t stride_page;    /* elements */
+  int64_t stride_h;       /* elements */
+  int32_t n_pages;
+  int32_t page_rows;
+} pc_pages;
+
+/* ---------------------------------------------------------------------------------------
+ * pc_page_store -- the rows of a step go into the pages, rotated on the way.  Row i of the nq rows of sequence s
+ * becomes row r = lens[s] - nq + i of the sequence: row r % page_rows of page table[s][r / page_rows].
+ *   K, V     dev [Hkv][T][D] of dtype, head strides in elements
+ *   table    dev int32 [n_seq][table_width], row stride in elements: the pages of each sequence, in order
+ *   lens     dev int32 [n_seq]: rows of each sequence, the new ones among them
+ *   pos      dev or NULL, int32 [T][3]: keys (and queries) are turned by their row's (t, h, w), bit for bit as
+ *            pc_rope3d turns them, sections and base as there.  NULL: keys go in as they are.
+ *   K_out    dev or NULL, [Hkv][T][D]: the keys as stored, e.g. for pc_prompt_attn; may be K itself
+ *   Q, Q_out dev or NULL, [Hq][T][D]: queries to be turned and multiplied by out_scale, and where they go (may be Q
+ *            itself); they need pos.  Rows of nobody are not turned.
+ * A row whose r is negative or beyond the table, or whose page number is not one of 0 .. n_pages - 1, is not stored
+ * (lens[s] = 0: a sequence that pauses); Q_out and K_out are written all the same.  Two rows that are sent to the same
+ * place leave either.
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_HIP.
+ */
+int pc_page_store(const void* K, const void* V, int dtype, int Hkv, int T, int D, int64_t k_stride_h,
+                  int64_t v_stride_h, const pc_pages* pages, const int32_t* table, int table_width,
+                  int64_t table_stride, const int32_t* lens, const int32_t* offs, int n_seq,
+                  const int32_t* pos, int sec_t, int sec_h, int sec_w, double base, void* K_out,
+                  int64_t k_out_stride_h, const void* Q, void* Q_out, int Hq, int64_t q_stride_h,
+                  int64_t q_out_stride_h, double out_scale, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * pc_page_attn -- attention of a step's rows over the pages: row i of the nq rows of sequence s sees the rows 0 ..
+ * lens[s] - nq + i of its sequence (its own is the last of them), as pc_page_store left them.
+ *   Q, O     dev [Hq][T][D] of dtype, head strides in elements, without a byte in common
+ *   table, lens, offs, n_seq   as in pc_page_store
+ *   max_len  no sequence counts for more rows than this, whatever lens says; at most table_width * page_rows.  Work is laid out for
+ *            it, so a bound near the longest sequence is worth having
+ *   shared, n_shared   dev int32 [ceil(n_shared / page_rows)] or NULL, 0: the first n_shared rows of every sequence
+ *            are the same (a common prompt, one video's cache).  They are read through `shared`, once for all
+ *            sequences, the rows behind them through `table`.  A sequence of fewer rows sees that many of them.
+ *   lse      dev or NULL, fp32 [Hq][T]
+ *   ws       dev, pc_page_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls that may
+ *            overlap on the GPU must not share one.
+ * A row that sees nothing (lens[s] = 0) gets O = 0 and lse = -inf.  A page number that is not one of 0 .. n_pages - 1
+ * stands for rows that nobody sees.  The order of the sums is fixed: results are bit-reproducible.
+ * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_WORKSPACE, PC_ERR_HIP.
+ */
+size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, int n_seq,
+                                    int max_len, int n_shared);
+int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int Hq, int Hkv, int T, int D,
+                 int64_t q_stride_h, int64_t o_stride_h, float scale, const int32_t* table, int table_width,
+                 int64_t table_stride, const int32_t* lens, const int32_t* offs, int n_seq, int max_len,
+                 const int32_t* shared, int n_shared, void* O, float* lse, void* ws, size_t ws_bytes,
+                 void* stream);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,8 @@ __all__ = [
     "pc_compact_workspace_bytes", "pc_compact_prepared", "pc_compact_static", "pc_compact_static_capacity", "pc_frame_attn", "pc_frame_attn_workspace_bytes",
     "pc_frame_attn_workspace_bytes_for", "pc_frame_attn_cut", "pc_score_cut", "pc_compact_cut",
     "segment_budgets", "q4_cache", "pc_q4_store", "pc_q4_load", "pc_q4_attn", "pc_q4_attn_workspace_bytes", "pc_evict",
-    "pc_q4_evict", "pc_evict_workspace_bytes",
+    "pc_q4_evict", "pc_evict_workspace_bytes", "pc_prompt_attn", "page_cache", "pc_page_store", "pc_page_attn",
+    "pc_page_attn_workspace_bytes",
 ]
 
 PC_F32, PC_BF16 = 0, 1
@@ -58,6 +59,11 @@ class pc_segment(C.Structure):
 class _Q4(C.Structure):    # pc_q4_cache
     _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
                 ("code_stride_h", C.c_int64), ("scale_stride_h", C.c_int64)]
+
+
+class _Pages(C.Structure):    # pc_pages
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("stride_page", C.c_int64), ("stride_h", C.c_int64),
+                ("n_pages", C.c_int32), ("page_rows", C.c_int32)]
 
 
 def lib_path() -> str:
@@ -128,6 +134,15 @@ def lib() -> C.CDLL:
         evict_tail = [vp, i64, vp, i64] + [C.c_int] * 5 + [vp, i64, vp, sz, vp]
         L.pc_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, i64, i64] + evict_tail
         L.pc_q4_evict.argtypes = [q4p, C.c_int, C.c_int] + evict_tail
+        pagesp = C.POINTER(_Pages)
+        L.pc_prompt_attn.argtypes = [vp, vp, vp] + [C.c_int] * 6 + [i64] * 4 + [C.c_float, i32p, i32p, C.c_int, vp, vp, vp]
+        L.pc_page_store.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, i64, i64, pagesp, vp, C.c_int, i64, vp, i32p,
+                                    C.c_int, vp, C.c_int, C.c_int, C.c_int, C.c_double, vp, i64, vp, vp, C.c_int, i64, i64,
+                                    C.c_double, vp]
+        L.pc_page_attn_workspace_bytes.restype = sz
+        L.pc_page_attn_workspace_bytes.argtypes = [C.c_int] * 5 + [i32p] + [C.c_int] * 3
+        L.pc_page_attn.argtypes = [vp, pagesp] + [C.c_int] * 5 + [i64, i64, C.c_float, vp, C.c_int, i64, vp, i32p, C.c_int,
+                                   C.c_int, vp, C.c_int, vp, vp, vp, sz, vp]
         L.pc_last_error_detail()    # touches the library's thread-local storage (see build.build_marshal)
         _LIB = L
     if _NATIVE is None and "torch" in sys.modules:
@@ -817,3 +832,161 @@ def pc_q4_evict(cache, pos, weights, Nk: int, n_keep: int, n_anchor: int = 0, re
                              weights.stride(0), hsel, int(Nk), int(n_keep), int(n_anchor), int(recent_t), _ptr(idx), idx_stride, _ptr(ws),
                              0 if ws is None else ws.nbytes, _stream()))
     return min(Nk, n_keep)
+
+
+# ---- several sequences at once: prompts, and a cache in pages -----------------------------------------------
+def _heads_of_rows(t, name: str, heads, rows, D, like=None):
+    """t is [heads][rows][D] (None: any number) with dense rows, of like's type; its sizes."""
+    if t.dim() != 3 or any(w is not None and w != n for n, w in zip(t.shape, (heads, rows, D))):
+        raise PackCacheError(-2, f"{name} must be [{heads or 'H'}][{rows if rows is not None else 'rows'}][{D or 'D'}], got {tuple(t.shape)}")
+    if like is not None and t.dtype != like.dtype:
+        raise PackCacheError(-3, f"{name} is {t.dtype}, not {like.dtype}")
+    _rows_follow(t, name)
+    return t.shape
+
+
+def _offsets(offs, name: str, n_seq=None):
+    """Host offsets as int32 [n_seq + 1]."""
+    offs = [int(v) for v in offs]
+    if len(offs) < 1 or (n_seq is not None and len(offs) != n_seq + 1):
+        raise PackCacheError(-2, f"{name}: {len(offs)} offsets for {n_seq if n_seq is not None else 'any number of'} sequences")
+    if max(offs) > 2 ** 31 - 1 or min(offs) < 0:
+        raise PackCacheError(-2, f"{name}: offsets from {min(offs)} to {max(offs)}")
+    return (C.c_int32 * len(offs))(*offs)
+
+
+def _out_and_lse(Q, O, lse):
+    import torch
+    if O is None:
+        O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    _heads_of_rows(O, "O", *Q.shape, like=Q)
+    if lse is not None and (tuple(lse.shape) != tuple(Q.shape[:2]) or not lse.is_contiguous() or lse.dtype != torch.float32):
+        raise PackCacheError(-2, f"lse must be a contiguous fp32 [{Q.shape[0]}][{Q.shape[1]}] tensor")
+    return O
+
+
+def pc_prompt_attn(Q, K, V, scale: float, offs_q, offs_k=None, O=None, lse=None):
+    """Causal attention over packed prompts: Q [Hq][Tq][D] (bf16/fp32), K, V [Hkv][Tk][D] -> O [Hq][Tq][D].  offs_q: host
+    offsets [n_seq + 1] of the sequences in Q's rows; offs_k: in K's and V's (None: the same).  Row i of nq sees keys
+    0 .. nk - nq + i; a row that sees none gets O = 0 and lse (fp32 [Hq][Tq]) = -inf.  Rows of no sequence are left as they
+    were."""
+    Hq, Tq, D = _heads_of_rows(Q, "Q", None, None, None)
+    Hkv, Tk, _ = _heads_of_rows(K, "K", None, None, D, like=Q)
+    _heads_of_rows(V, "V", Hkv, Tk, D, like=Q)
+    oq = _offsets(offs_q, "offs_q")
+    n_seq = len(oq) - 1
+    ok = None if offs_k is None else _offsets(offs_k, "offs_k", n_seq)
+    O = _out_and_lse(Q, O, lse)
+    _on_device(Q=Q, K=K, V=V, O=O, lse=lse)
+    _check(lib().pc_prompt_attn(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), Hq, Hkv, Tq, Tk, D, Q.stride(0),
+                                K.stride(0), V.stride(0), O.stride(0), float(scale), oq, ok, n_seq, O.data_ptr(), _ptr(lse),
+                                _stream()))
+    return O
+
+
+def page_cache(n_pages: int, Hkv: int, page_rows: int, D: int, dtype=None, device="cuda:0"):
+    """An empty cache in pages: (K, V), each [n_pages][Hkv][page_rows][D] (bf16 unless a type is given).  Any two tensors of
+    these shapes and one set of strides are one, if each page's rows of a head are dense."""
+    import torch
+    if D not in (64, 128) or page_rows < 64 or page_rows % 64:
+        raise PackCacheError(-4, f"pages of {page_rows} x {D}: rows a multiple of 64, D = 64 or 128")
+    return tuple(torch.zeros((n_pages, Hkv, page_rows, D), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
+                 for _ in range(2))
+
+
+def _pages_struct(pages, like):
+    """(struct, Hkv) of a cache in pages."""
+    try:
+        K, V = pages
+    except (TypeError, ValueError):
+        raise PackCacheError(-2, "a cache in pages is (K, V)") from None
+    for t, name in ((K, "K pages"), (V, "V pages")):
+        if t.dim() != 4 or t.dtype != like.dtype or t.shape[3] != like.shape[2]:
+            raise PackCacheError(-2, f"{name}: {like.dtype} [n_pages][Hkv][page_rows][{like.shape[2]}], got {t.dtype} {tuple(t.shape)}")
+        _rows_dense(t, name)
+    if K.shape != V.shape or K.stride() != V.stride():
+        raise PackCacheError(-2, "K and V pages must agree in shape and stride")
+    _on_device(**{"K pages": K, "V pages": V})
+    return _Pages(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.shape[0], K.shape[2]), K.shape[1]
+
+
+def _sequences(table, lens, offs, T: int):
+    """(number, table stride, offsets or None) of the sequences of a step."""
+    import torch
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[1] < 1 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise PackCacheError(-2, f"table: int32 [n_seq][pages], got {table.dtype} {tuple(table.shape)}")
+    n_seq = table.shape[0]
+    if lens.dtype != torch.int32 or tuple(lens.shape) != (n_seq,) or not lens.is_contiguous():
+        raise PackCacheError(-2, f"lens: contiguous int32 [{n_seq}], got {lens.dtype} {tuple(lens.shape)}")
+    _on_device(table=table, lens=lens)
+    return n_seq, table.stride(0), None if offs is None else _offsets(offs, "offs", n_seq)
+
+
+def pc_page_store(K, V, pages, table, lens, offs=None, pos=None, sections=None, base: float = 10000.0, K_out=None, Q=None,
+                  Q_out=None, out_scale: float = 1.0) -> None:
+    """The T new rows K, V [Hkv][T][D] (bf16/fp32) of a step go into the pages (K, V, each [n_pages][Hkv][page_rows][D]).  Row
+    i of the nq rows of sequence s becomes its row lens[s] - nq + i, in page table[s][..] (int32 [n_seq][pages]; lens
+    int32 [n_seq], the new rows counted).  offs: host offsets [n_seq + 1] of the sequences in the T rows; None: T / n_seq each.
+    pos (int32 [T][3]) and sections: keys are turned as pc_rope3d turns them; K_out (may be K): the keys as stored;
+    Q [Hq][T][D] -> Q_out (may be Q): queries turned and multiplied by out_scale.  Rows without a page are not stored."""
+    import torch
+    Hkv, T, D = _heads_of_rows(K, "K", None, None, None)
+    _heads_of_rows(V, "V", Hkv, T, D, like=K)
+    p, heads = _pages_struct(pages, K)
+    if heads != Hkv:
+        raise PackCacheError(-2, f"pages of {heads} heads, rows of {Hkv}")
+    n_seq, table_stride, o = _sequences(table, lens, offs, T)
+    if K_out is not None:
+        _heads_of_rows(K_out, "K_out", Hkv, T, D, like=K)
+    if (Q is None) != (Q_out is None):
+        raise PackCacheError(-1, "Q and Q_out go together")
+    if Q is not None:
+        _heads_of_rows(Q, "Q", None, T, D, like=K)
+        _heads_of_rows(Q_out, "Q_out", *Q.shape, like=K)
+    if (pos is None) != (sections is None):
+        raise PackCacheError(-1, "pos and sections go together")
+    if pos is not None and (pos.dtype != torch.int32 or tuple(pos.shape) != (T, 3) or not pos.is_contiguous()):
+        raise PackCacheError(-2, f"pos: contiguous int32 [{T}][3], got {pos.dtype} {tuple(pos.shape)}")
+    sec = (0, 0, 0) if sections is None else [int(v) for v in sections]
+    _on_device(K=K, V=V, pos=pos, K_out=K_out, Q=Q, Q_out=Q_out)
+    _check(lib().pc_page_store(K.data_ptr(), V.data_ptr(), _dtype_code(K), Hkv, T, D, K.stride(0), V.stride(0), C.byref(p),
+                               table.data_ptr(), table.shape[1], table_stride, lens.data_ptr(), o, n_seq, _ptr(pos), sec[0], sec[1],
+                               sec[2], float(base), _ptr(K_out), 0 if K_out is None else K_out.stride(0), _ptr(Q), _ptr(Q_out),
+                               0 if Q is None else Q.shape[0], 0 if Q is None else Q.stride(0), 0 if Q is None else Q_out.stride(0),
+                               float(out_scale), _stream()))
+
+
+def pc_page_attn_workspace_bytes(dtype: int, Hq: int, Hkv: int, T: int, D: int, n_seq: int, max_len: int, n_shared: int = 0,
+                                 offs=None) -> int:
+    o = None if offs is None else _offsets(offs, "offs", n_seq)
+    return lib().pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, o, n_seq, max_len, n_shared)
+
+
+def pc_page_attn(Q, pages, table, lens, max_len: int, scale: float, offs=None, shared=None, n_shared: int = 0, O=None, lse=None,
+                 ws=None):
+    """The T rows Q [Hq][T][D] of a step over a cache in pages -> O [Hq][T][D]: row i of the nq rows of sequence s sees its rows
+    0 .. lens[s] - nq + i.  pages, table, lens, offs as in pc_page_store; max_len bounds lens.  shared (int32 [pages]),
+    n_shared: the first n_shared rows of all sequences are those of these pages, read once for all.  lse fp32 [Hq][T].  ws: not to be
+    shared by calls that may overlap; None: one of the call's own, from torch's allocator."""
+    import torch
+    Hq, T, D = _heads_of_rows(Q, "Q", None, None, None)
+    p, Hkv = _pages_struct(pages, Q)
+    if Hkv < 1 or Hq % Hkv:
+        raise PackCacheError(-2, f"{Hq} query heads for {Hkv} KV heads")
+    n_seq, table_stride, o = _sequences(table, lens, offs, T)
+    if (shared is None) != (n_shared == 0):
+        raise PackCacheError(-1, "shared and n_shared go together")
+    if shared is not None and (shared.dtype != torch.int32 or shared.dim() != 1 or not shared.is_contiguous()
+                               or shared.shape[0] * p.page_rows < n_shared):
+        raise PackCacheError(-2, f"shared: contiguous int32 page numbers of {n_shared} rows, got {shared.dtype} {tuple(shared.shape)}")
+    O = _out_and_lse(Q, O, lse)
+    dtype = _dtype_code(Q)
+    if ws is None and T and n_seq:
+        nws = lib().pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, o, n_seq, int(max_len), int(n_shared))
+        if nws:
+            ws = _workspace(nws, Q)
+    _on_device(Q=Q, O=O, lse=lse, ws=ws, shared=shared)
+    _check(lib().pc_page_attn(Q.data_ptr(), C.byref(p), dtype, Hq, Hkv, T, D, Q.stride(0), O.stride(0), float(scale), table.data_ptr(),
+                              table.shape[1], table_stride, lens.data_ptr(), o, n_seq, int(max_len), _ptr(shared), int(n_shared),
+                              O.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream()))
+    return O

@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libpackcache.so")
 MARSHAL_PATH = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["host.cpp", "rope.hip", "attn.hip", "score.hip", "compact.hip", "q4.hip", "evict.hip"]
+SOURCES = ["host.cpp", "rope.hip", "attn.hip", "score.hip", "compact.hip", "q4.hip", "evict.hip", "page_store.hip",
+           "seq_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

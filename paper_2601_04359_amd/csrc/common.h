@@ -152,6 +152,7 @@ __device__ __forceinline__ int lanes_below(uint64_t mask, int base) {  // base +
 struct Divisor {
   uint32_t m;
   int sh, d;
+  Divisor() : Divisor(1) {}
   explicit Divisor(int by) : sh(31), d(by) {
     while (sh < 62 && (1ll << (sh - 31)) < by) ++sh;
     m = static_cast<uint32_t>((1ull << sh) / by + 1);

@@ -1,0 +1,477 @@
+// pc_prompt_attn and pc_page_attn: attention with a limit per row, over packed prompts and over a cache held in pages.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+#include <numeric>
+#include <vector>
+
+#include "lds_dma.h"
+#include "seq_rows.h"
+
+namespace pc {
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// The general form: any type and D, on the 16x16x4 fp32 MFMA.  A work-group has 16 query rows, its four waves take the keys
+// in steps of 16 by turns and merge their (O, m, l) through LDS once.
+//   * S^T = K Q^T: lane (r = l % 16, kg = l / 16) holds key row r, dims 16 s + 4 kg .. + 3; the four products of step s contract
+//     over (kg, element), the same permutation of the head dimension on both operands.
+//   * The result leaves lane (q = l % 16, kg) with keys 4 kg .. + 3 of its query: P^T is the B operand of O^T += V^T P^T
+//     (product e contracts over keys 4 kg + e), and row r of output block (db, e) stands for dim 64 db + 4 r + e, so that V
+//     comes in 16-byte pieces and O leaves in them.
+//   * A score is s (c + c_lo), and the reference is subtracted from the rounded product: the largest key's exponent is 0
+//     however large the logits are.
+//   * A key that a row does not see has p = 0, and 0 times a NaN in V would reach the row: in steps where some row does not
+//     see all keys, values that are not finite are taken out of the product and added to the rows that see them.
+// ------------------------------------------------------------------------------------------
+constexpr int kGenRows = 16, kGenWaves = 4, kGenKeys = 16;
+
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const T* p) {
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const f32x4*>(p);
+  const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+  return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
+               __uint_as_float(v[1] & 0xFFFF0000u)};
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, f32x4 v) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = v;
+  else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+template <typename T, int D, bool kPages>
+__global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a) {
+  constexpr int kSteps = D / 16, kBlocks = D / 64;
+  __shared__ float o_lds[kGenWaves][kGenRows][D];
+  __shared__ float2 ml_lds[kGenWaves][kGenRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, kg = lane >> 4;
+  const RowSet r = kPages ? page_rows<kGenRows>(a, blockIdx.x, lane) : prompt_rows<kGenRows>(a, blockIdx.x, lane);
+  if (r.idle) return;
+  const int n_set = r.n_tok * a.rep, rho = min(r.tile * kGenRows + r16, n_set - 1);
+  const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
+  const int lim = limit_of(a, r, tok);
+  int lim_max = lim, lim_min = lim > 0 ? lim : INT_MAX;   // over the rows that see something
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) {
+    lim_max = max(lim_max, __shfl_xor(lim_max, x));
+    lim_min = min(lim_min, __shfl_xor(lim_min, x));
+  }
+  const int end = min(r.end, __builtin_amdgcn_readfirstlane(lim_max));
+  lim_min = __builtin_amdgcn_readfirstlane(lim_min);
+
+  f32x4 qf[kSteps];
+  const T* q = static_cast<const T*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * D + kg * 4;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) qf[s] = load4(q + s * 16);
+
+  const T* Kh = static_cast<const T*>(a.K) + r.kvh * a.k_stride;
+  const T* Vh = static_cast<const T*>(a.V) + r.kvh * a.v_stride;
+  f32x4 acc[kBlocks][4];
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[db][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kNothing, l = 0.f;
+
+  for (int kb = r.begin + wave * kGenKeys; kb < end; kb += kGenWaves * kGenKeys) {
+    int64_t base;   // of row 0 of what the keys of this step lie in, elements
+    int first = 0;  // and the key that is row 0
+    if constexpr (kPages) {
+      const int in_table = a.by_page.of(kb), page = r.pages[in_table];
+      if (page < 0 || page >= a.n_pages) continue;
+      base = page * a.page_stride, first = in_table * a.by_page.d;
+    } else {
+      base = static_cast<int64_t>(r.k0) * D;
+    }
+    const int last = r.n_keys - 1;
+    auto row = [&](int j) { return base + static_cast<int64_t>(min(max(j, r.lo), last) - first) * D; };
+    if (kb + kGenKeys <= r.lo) continue;   // every key of the step lies in front: row() must not reach another page
+    f32x4 kf[kSteps], vf[4][kBlocks];
+    {
+      const T* p = Kh + row(kb + r16) + kg * 4;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) kf[s] = load4(p + s * 16);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const T* p = Vh + row(kb + kg * 4 + e) + r16 * 4;
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db) vf[e][db] = load4(p + db * 64);
+    }
+    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[s][e], qf[s][e], sc, 0, 0, 0);
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(sc[e], a.c, sc[e] * a.c_lo);
+    if (kb + kGenKeys > lim_min || kb < r.lo) {
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = kb + kg * 4 + e;
+        if (j >= lim || j < r.lo) x[e] = -INFINITY;
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= not_finite(vf[e][db][i]);
+      }
+      if (__any(odd)) {
+        for (int k = 0; k < kGenKeys; ++k) {
+          const int j = kb + k;
+          if (j >= lim || j < r.lo) continue;
+#pragma unroll
+          for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
+              const f32x4 v = load4(Vh + row(j) + db * 64 + kg * 16 + i * 4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (not_finite(v[e])) acc[db][e][i] += v[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (not_finite(vf[e][db][i])) vf[e][db][i] = 0.f;
+      }
+    }
+    float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    if (__any(mx > m)) {
+      const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[db][e] *= alpha;
+      m = m_new;
+    }
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(x[e] - m);
+      l += p[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[db][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][db][i], p[e], acc[db][i], 0, 0, 0);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(&o_lds[wave][r16][db * 64 + kg * 16 + i * 4]) = f32x4{acc[db][0][i], acc[db][1][i], acc[db][2][i], acc[db][3][i]};
+  if (kg == 0) ml_lds[wave][r16] = make_float2(m, l);
+  __syncthreads();
+  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;   // 16 threads per row, D / 16 dims each
+  const int rho_w = r.tile * kGenRows + row;
+  if (rho_w >= n_set) return;
+  float M = kNothing, L = 0.f;
+#pragma unroll
+  for (int w = 0; w < kGenWaves; ++w) M = fmaxf(M, ml_lds[w][row].x);
+  f32x4 out[kBlocks];
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db) out[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kGenWaves; ++w) {
+    const float2 ml = ml_lds[w][row];
+    const float by = __builtin_amdgcn_exp2f(ml.x - M);
+    L += by * ml.y;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db) out[db] += by * *reinterpret_cast<const f32x4*>(&o_lds[w][row][db * 64 + c * 4]);
+  }
+  const int tok_w = a.by_rep.of(rho_w), head_w = r.kvh * a.rep + rho_w - tok_w * a.rep;
+  const int64_t t = r.t0 + tok_w;
+  if (a.part_o != nullptr) {
+    const int64_t at = (static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep + head_w) * a.T + t;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db) *reinterpret_cast<f32x4*>(a.part_o + at * D + db * 64 + c * 4) = out[db];
+    if (c == 0) a.part_ml[at] = make_float2(M, L);
+    return;
+  }
+  const bool none = limit_of(a, r, tok_w) <= r.lo;
+  const float inv = none ? 0.f : 1.f / L;
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db)
+    store4(static_cast<T*>(a.O) + head_w * a.o_stride + t * D + db * 64 + c * 4, none ? f32x4{0.f, 0.f, 0.f, 0.f} : out[db] * inv);
+  if (a.lse != nullptr && c == 0) a.lse[head_w * static_cast<int64_t>(a.T) + t] = none ? -INFINITY : lse_of(M, L);
+}
+
+// ------------------------------------------------------------------------------------------
+// The shares of a row joined: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s with M = max_s m_s, over the shares that
+// have written something, in their order.  A thread has four dims of a row.
+// ------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
+  constexpr int kLanes = D / 4;
+  const int n = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  const int Hq = a.by_hkv.d * a.rep;
+  if (n >= Hq * a.n_rows) return;
+  const int head = n / a.n_rows, t = a.row0 + n - head * a.n_rows;
+  const int s = seq_of_row(a.seqs, t);
+  if (s < 0) return;
+  const bool even = a.seqs.per > 0;
+  const int len = max(0, min(a.lens[even ? s : a.seqs.k0[s]], a.max_len));
+  const int end = even ? (s + 1) * a.seqs.per : a.seqs.q0[s] + a.seqs.nq[s];
+  const int parts = a.shared_parts + own_parts_of(a, len);
+  const int64_t step = static_cast<int64_t>(Hq) * a.T, at = static_cast<int64_t>(head) * a.T + t;
+  T* out = static_cast<T*>(a.O) + head * a.o_stride + static_cast<int64_t>(t) * D + c * 4;
+  float M = kNothing, L = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (len - (end - t) + 1 > 0) {
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, a.part_ml[p * step + at].x);
+    for (int p = 0; p < parts; ++p) {
+      const float2 ml = a.part_ml[p * step + at];
+      const float by = __builtin_amdgcn_exp2f(ml.x - M);
+      L += by * ml.y;
+      acc += by * *reinterpret_cast<const f32x4*>(a.part_o + (p * step + at) * D + c * 4);
+    }
+    acc *= 1.f / L;
+  }
+  store4(out, acc);
+  if (a.lse != nullptr && c == 0) a.lse[at] = lse_of(M, L);
+}
+
+// ---- how a call is cut ---------------------------------------------------------------------------------------------
+// Shares of `keys` keys so that `work_groups` of them become about `wanted`; a share has at least `least` keys.
+int share_of(int keys, int work_groups, int wanted, int least) {
+  const int shares = std::max(1, std::min({wanted / std::max(1, work_groups), keys / least, 64}));
+  return ceil_div(ceil_div(keys, shares), kPageStep) * kPageStep;
+}
+
+// How pc_page_attn cuts a launch's keys.
+struct PagePlan {
+  int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
+  int own_tiles = 0, own_parts = 0, own_keys = kPageStep;
+  int parts() const { return shared_parts + own_parts; }
+  // n_rows tokens in all, own_tiles row tiles over all sequences
+  PagePlan(int Hkv, int rep, int n_rows, int tiles, int rows_per_tile, int n_shared, int max_len) {
+    own_tiles = tiles;
+    if (n_shared > 0) {
+      shared_tiles = ceil_div(n_rows * rep, rows_per_tile);
+      shared_keys = share_of(n_shared, shared_tiles * Hkv, 1024, 256);
+      shared_parts = ceil_div(n_shared, shared_keys);
+    }
+    const int own = max_len - n_shared / kPageStep * kPageStep;
+    if (max_len > n_shared) {
+      own_keys = share_of(own, own_tiles * Hkv, 1024, 256);
+      own_parts = ceil_div(own, own_keys);
+    }
+  }
+};
+
+size_t part_bytes(int parts, int Hq, int T, int D) {
+  return parts <= 1 ? 0 : align_up(static_cast<size_t>(parts) * Hq * T * D * sizeof(float), 256) + static_cast<size_t>(parts) * Hq * T * sizeof(float2);
+}
+
+int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
+  if (offs == nullptr) return n_seq * ceil_div(T / n_seq * rep, rows);
+  int n = 0;
+  for (int s = 0; s < n_seq; ++s) n += ceil_div((offs[s + 1] - offs[s]) * rep, rows);
+  return n;
+}
+
+// Calls f(first, count) for the launches that a call's sequences are dealt to; f returns a status.
+template <class F>
+int each_launch(const int32_t* offs, int n_seq, F&& f) {
+  if (offs == nullptr) return f(0, n_seq);
+  for (int s0 = 0; s0 < n_seq; s0 += kSeqs)
+    if (int rc = f(s0, std::min(kSeqs, n_seq - s0))) return rc;
+  return PC_OK;
+}
+
+void set_scale(RowsArgs& a, float scale) {
+  const double c = static_cast<double>(scale) * 1.4426950408889634074;
+  a.c = static_cast<float>(c);
+  a.c_lo = static_cast<float>(c - a.c);
+}
+
+int check_attn(const char* who, int dtype, int Hq, int Hkv, int D, float scale) {
+  PC_REQUIRE(dtype == PC_F32 || dtype == PC_BF16, PC_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  PC_REQUIRE(Hkv >= 1 && Hq >= 1 && Hq % Hkv == 0, PC_ERR_SHAPE, "%s: Hq=%d must be a multiple of Hkv=%d", who, Hq, Hkv);
+  PC_REQUIRE(D == 64 || D == 128, PC_ERR_UNSUPPORTED, "%s: D=%d (64 or 128)", who, D);
+  PC_REQUIRE(scale > 0.f && isfinite(scale), PC_ERR_SHAPE, "%s: scale %g must be > 0", who, scale);
+  return PC_OK;
+}
+
+template <template <typename, int> class Launch>
+void by_type(int dtype, int D, const RowsArgs& a, dim3 grid, hipStream_t s) {
+  if (dtype == PC_BF16) D == 128 ? Launch<uint16_t, 128>::go(a, grid, s) : Launch<uint16_t, 64>::go(a, grid, s);
+  else D == 128 ? Launch<float, 128>::go(a, grid, s) : Launch<float, 64>::go(a, grid, s);
+}
+template <typename T, int D>
+struct GeneralPrompt {
+  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_general_kernel<T, D, false><<<grid, kGenWaves * 64, 0, s>>>(a); }
+};
+template <typename T, int D>
+struct GeneralPages {
+  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_general_kernel<T, D, true><<<grid, kGenWaves * 64, 0, s>>>(a); }
+};
+template <typename T, int D>
+struct Join {
+  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_join_kernel<T, D><<<grid, 256, 0, s>>>(a); }
+};
+
+}  // namespace
+}  // namespace pc
+
+using namespace pc;
+
+extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int dtype, int Hq, int Hkv, int Tq, int Tk,
+                              int D, int64_t q_stride_h, int64_t k_stride_h, int64_t v_stride_h, int64_t o_stride_h,
+                              float scale, const int32_t* offs_q, const int32_t* offs_k, int n_seq, void* O, float* lse,
+                              void* stream) {
+  const char* who = "pc_prompt_attn";
+  if (int rc = check_attn(who, dtype, Hq, Hkv, D, scale)) return rc;
+  PC_REQUIRE(Tq >= 0 && Tk >= 0 && n_seq >= 0, PC_ERR_SHAPE, "%s: Tq=%d Tk=%d n_seq=%d", who, Tq, Tk, n_seq);
+  if (n_seq == 0) return PC_OK;
+  PC_REQUIRE(offs_q != nullptr, PC_ERR_NULL, "%s: offs_q is NULL", who);
+  if (int rc = check_offsets(who, "offs_q", offs_q, n_seq, Tq)) return rc;
+  if (offs_k == nullptr) offs_k = offs_q;
+  if (int rc = check_offsets(who, "offs_k", offs_k, n_seq, Tk)) return rc;
+  if (offs_q[n_seq] == offs_q[0]) return PC_OK;
+  const int rep = Hq / Hkv;
+  PC_REQUIRE(static_cast<int64_t>(Hq) * Tq <= INT32_MAX / 2 && Tk <= INT32_MAX / 2, PC_ERR_UNSUPPORTED, "%s: %d heads x %d rows, %d keys",
+             who, Hq, Tq, Tk);
+  PC_REQUIRE(Q && O && (Tk == 0 || (K && V)), PC_ERR_NULL, "%s: Q, K, V or O is NULL", who);
+  const int elt = dtype == PC_BF16 ? 2 : 4;
+  const int64_t q_rows = static_cast<int64_t>(Tq) * D, k_rows = static_cast<int64_t>(Tk) * D;
+  PC_REQUIRE((Hq == 1 || (q_stride_h >= q_rows && o_stride_h >= q_rows)) && (Hkv == 1 || (k_stride_h >= k_rows && v_stride_h >= k_rows)),
+             PC_ERR_SHAPE, "%s: a head stride is smaller than the rows it must hold", who);
+  PC_REQUIRE(aligned_16B(Q, q_stride_h, elt) && aligned_16B(K, k_stride_h, elt) && aligned_16B(V, v_stride_h, elt) &&
+                 aligned_16B(O, o_stride_h, elt), PC_ERR_SHAPE, "%s: tensors and head strides must be 16-byte aligned", who);
+  PC_REQUIRE(!overlap(O, o_stride_h * elt, Hq, q_rows * elt, Q, q_stride_h * elt, Hq, q_rows * elt) &&
+                 (Tk == 0 || (!overlap(O, o_stride_h * elt, Hq, q_rows * elt, K, k_stride_h * elt, Hkv, k_rows * elt) &&
+                              !overlap(O, o_stride_h * elt, Hq, q_rows * elt, V, v_stride_h * elt, Hkv, k_rows * elt))),
+             PC_ERR_SHAPE, "%s: O may not overlap Q, K or V", who);
+  RowsArgs a = {};
+  a.Q = Q, a.K = K, a.V = V, a.O = O, a.lse = lse;
+  a.q_stride = q_stride_h, a.k_stride = k_stride_h, a.v_stride = v_stride_h, a.o_stride = o_stride_h;
+  a.rep = rep, a.T = Tq, a.by_rep = Divisor(rep), a.by_hkv = Divisor(Hkv);
+  set_scale(a, scale);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  // sequences without rows have nothing to do; the longest come first, so that those of a launch are about as long
+  struct Seq {
+    int q0, nq, k0, nk;
+  };
+  std::vector<Seq> seqs;
+  try {
+    for (int s = 0; s < n_seq; ++s)
+      if (offs_q[s + 1] > offs_q[s]) seqs.push_back({offs_q[s], offs_q[s + 1] - offs_q[s], offs_k[s], offs_k[s + 1] - offs_k[s]});
+    if (static_cast<int>(seqs.size()) > kSeqs) std::stable_sort(seqs.begin(), seqs.end(), [](const Seq& x, const Seq& y) { return x.nk > y.nk; });
+  } catch (const std::bad_alloc&) {
+    PC_FAIL(PC_ERR_SHAPE, "%s: no memory for a table of %d sequences", who, n_seq);
+  }
+  for (size_t s0 = 0; s0 < seqs.size(); s0 += kSeqs) {
+    const int n = static_cast<int>(std::min<size_t>(kSeqs, seqs.size() - s0));
+    a.seqs.n = n, a.seqs.per = 0;
+    a.n_tiles = 0, a.max_level = 0;
+    for (int s = 0; s < n; ++s) {
+      const Seq& q = seqs[s0 + s];
+      a.seqs.q0[s] = q.q0, a.seqs.nq[s] = q.nq, a.seqs.k0[s] = q.k0, a.seqs.nk[s] = q.nk;
+      const int tiles = ceil_div(q.nq * rep, kGenRows);
+      a.n_tiles += tiles;
+      a.max_level = std::max(a.max_level, static_cast<int>(static_cast<int64_t>(std::max(0, q.nk - q.nq)) * rep / kGenRows) + tiles);
+    }
+    by_type<GeneralPrompt>(dtype, D, a, dim3(a.n_tiles * Hkv), st);
+    PC_CHECK_LAUNCH(who);
+  }
+  return PC_OK;
+}
+
+extern "C" size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, int n_seq,
+                                               int max_len, int n_shared) {
+  if (dtype < 0 || dtype > 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || T < 1 || n_seq < 1 || max_len < 1 || n_shared < 0 || (D != 64 && D != 128)) return 0;
+  if (offs == nullptr ? T % n_seq != 0 : check_offsets("pc_page_attn_workspace_bytes", "offs", offs, n_seq, T) != PC_OK) return 0;
+  size_t most = 0;
+  each_launch(offs, n_seq, [&](int s0, int n) {
+    const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
+    const PagePlan plan(Hkv, Hq / Hkv, o != nullptr ? o[n] - o[0] : T, row_tiles(o, n, T, Hq / Hkv, kGenRows), kGenRows, n_shared, max_len);
+    most = std::max(most, part_bytes(plan.parts(), Hq, T, D));
+    return PC_OK;
+  });
+  return most;
+}
+
+extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int Hq, int Hkv, int T, int D,
+                            int64_t q_stride_h, int64_t o_stride_h, float scale, const int32_t* table, int table_width,
+                            int64_t table_stride, const int32_t* lens, const int32_t* offs, int n_seq, int max_len,
+                            const int32_t* shared, int n_shared, void* O, float* lse, void* ws, size_t ws_bytes,
+                            void* stream) {
+  const char* who = "pc_page_attn";
+  if (int rc = check_attn(who, dtype, Hq, Hkv, D, scale)) return rc;
+  PC_REQUIRE(T >= 0 && n_seq >= 0, PC_ERR_SHAPE, "%s: T=%d n_seq=%d", who, T, n_seq);
+  const int elt = dtype == PC_BF16 ? 2 : 4;
+  if (int rc = check_pages(who, pages, Hkv, D, elt)) return rc;
+  if (T == 0 || n_seq == 0) return PC_OK;
+  if (int rc = check_sequences(who, table, table_width, table_stride, lens, offs, n_seq, T)) return rc;
+  const int64_t room = static_cast<int64_t>(table_width) * pages->page_rows;
+  PC_REQUIRE(max_len >= 1 && max_len <= room && max_len <= INT32_MAX / 2, PC_ERR_SHAPE, "%s: max_len=%d, a table row holds %lld", who, max_len,
+             static_cast<long long>(room));
+  PC_REQUIRE(n_shared >= 0 && (n_shared == 0) == (shared == nullptr) && n_shared <= INT32_MAX / 2, PC_ERR_SHAPE,
+             "%s: n_shared=%d goes with a list of pages", who, n_shared);
+  PC_REQUIRE(Q && O, PC_ERR_NULL, "%s: Q or O is NULL", who);
+  PC_REQUIRE(static_cast<int64_t>(Hq) * T <= INT32_MAX / 64, PC_ERR_UNSUPPORTED, "%s: %d heads x %d rows", who, Hq, T);
+  const int64_t per_head = static_cast<int64_t>(T) * D;
+  PC_REQUIRE(Hq == 1 || (q_stride_h >= per_head && o_stride_h >= per_head), PC_ERR_SHAPE, "%s: a head stride is smaller than T*D", who);
+  PC_REQUIRE(aligned_16B(Q, q_stride_h, elt) && aligned_16B(O, o_stride_h, elt), PC_ERR_SHAPE,
+             "%s: tensors and head strides must be 16-byte aligned", who);
+  PC_REQUIRE(!overlap(O, o_stride_h * elt, Hq, per_head * elt, Q, q_stride_h * elt, Hq, per_head * elt), PC_ERR_SHAPE,
+             "%s: O may not overlap Q: queries are read again behind the first outputs", who);
+  n_shared = std::min(n_shared, max_len);   // nobody sees more
+  const size_t need = pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, offs, n_seq, max_len, n_shared);
+  PC_REQUIRE(need == 0 || (ws != nullptr && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 16 == 0), PC_ERR_WORKSPACE,
+             "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, need, ws_bytes);
+  const int rep = Hq / Hkv;
+  RowsArgs a = {};
+  a.Q = Q, a.K = pages->K, a.V = pages->V, a.O = O, a.lse = lse;
+  a.q_stride = q_stride_h, a.k_stride = a.v_stride = pages->stride_h, a.o_stride = o_stride_h;
+  a.table = table, a.lens = lens, a.shared = shared, a.table_stride = table_stride, a.page_stride = pages->stride_page;
+  a.n_pages = pages->n_pages, a.n_shared = n_shared, a.max_len = max_len, a.by_page = Divisor(pages->page_rows);
+  a.rep = rep, a.T = T, a.by_rep = Divisor(rep), a.by_hkv = Divisor(Hkv);
+  set_scale(a, scale);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return each_launch(offs, n_seq, [&](int s0, int n) -> int {
+    const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
+    a.row0 = o != nullptr ? o[0] : 0, a.n_rows = o != nullptr ? o[n] - o[0] : T;
+    if (a.n_rows == 0) return PC_OK;
+    a.seqs.n = n, a.seqs.per = o != nullptr ? 0 : T / n;
+    if (o == nullptr) {
+      a.seqs.by_per = Divisor(a.seqs.per);
+      a.tiles_per_seq = ceil_div(a.seqs.per * rep, kGenRows), a.by_tiles_per_seq = Divisor(a.tiles_per_seq);
+    } else {
+      for (int s = 0; s < n; ++s) a.seqs.q0[s] = o[s], a.seqs.nq[s] = o[s + 1] - o[s], a.seqs.k0[s] = s0 + s;
+    }
+    const PagePlan plan(Hkv, rep, a.n_rows, row_tiles(o, n, T, rep, kGenRows), kGenRows, n_shared, max_len);
+    a.n_tiles = plan.own_tiles, a.by_tiles = Divisor(plan.own_tiles);
+    a.shared_tiles = plan.shared_tiles, a.shared_parts = plan.shared_parts, a.shared_keys = plan.shared_keys;
+    a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles));
+    a.own_parts = plan.own_parts, a.own_keys = plan.own_keys;
+    a.part_o = nullptr, a.part_ml = nullptr;
+    if (plan.parts() > 1) {
+      a.part_o = static_cast<float*>(ws);
+      a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) +
+                                            align_up(static_cast<size_t>(plan.parts()) * Hq * T * D * sizeof(float), 256));
+    }
+    by_type<GeneralPages>(dtype, D, a, dim3((plan.shared_tiles * plan.shared_parts + plan.own_tiles * plan.own_parts) * Hkv), st);
+    PC_CHECK_LAUNCH(who);
+    if (plan.parts() <= 1) return PC_OK;
+    by_type<Join>(dtype, D, a, dim3(ceil_div(Hq * a.n_rows, 256 / (D / 4))), st);
+    PC_CHECK_LAUNCH(who);
+    return PC_OK;
+  });
+}

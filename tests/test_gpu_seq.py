@@ -1,0 +1,531 @@
+"""Prompts, a cache in pages and its attention (pc_prompt_attn, pc_page_store, pc_page_attn) against plain 64-bit forms.
+
+Stored rows have to be equal bit for bit to what pc_rope3d makes of them.  Tolerances of the attention, element by element,
+with u = 2^-24 (half a step of fp32), A = the largest sum_d |q_d k_d| * scale that a row meets, in units of the logits:
+  * a logit: D products summed in fp32 in any order, the scale folded into base 2 (three roundings), the subtraction
+    of the reference: |ds| <= (D + 8) u A; the exponential adds a step of its result (2 u) and its argument's rounding, up
+    to u * 2 A * log2(e).  A probability is off by a factor of at most 1 + e, e = (D + 16) u A + 8 u.
+  * O, fp32 inputs: (2 e + (Nk + 64) u) sum_j p_j |v_j|: probability and normaliser, sums of Nk terms, merges.
+  * O, bf16 inputs: the probabilities are rounded to bf16 before the second product and O at the end, half a step each:
+    2^-8 (|O| + sum_j p_j |v_j|) more.
+  * lse: (D + 16) u A + (|lse| + Nk + 64) u.
+(Nk u is the worst case of a serial sum.)
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_04359_amd as pk
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+SECTIONS = {128: (32, 48, 48), 64: (16, 24, 24)}
+NAN = float("nan")
+
+
+def offsets(counts, start=0):
+    return [start + int(v) for v in np.concatenate([[0], np.cumsum(counts)])]
+
+
+def normal(gen, *shape):
+    return torch.empty(shape, device=DEV).normal_(generator=gen)
+
+
+def generator(seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    return gen
+
+
+def check_rows(dtype, got, got_lse, q, k, v, scale, first):
+    """One head: row i of q [nq][D] sees keys below first + i of k, v [nk][D]; got [nq][D], got_lse [nq] or None."""
+    nq, D = q.shape
+    nk = k.shape[0]
+    q, k, v, got = (x.detach().double() for x in (q, k, v, got))
+    seen = torch.arange(nk, device=DEV)[None] < first + torch.arange(nq, device=DEV)[:, None]
+    none = ~seen.any(1)
+    assert (got[none] == 0).all()
+    if got_lse is not None:
+        assert (got_lse[none] == -float("inf")).all()
+    if none.all():
+        return
+    z = torch.where(seen, q @ k.t().contiguous() * scale, -float("inf"))[~none]
+    size = torch.where(seen, q.abs() @ k.abs().t().contiguous() * scale, 0.0)[~none].amax(1)
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    O, mass = p @ v, p @ v.abs()
+    e = ((D + 16) * U * size + 8 * U)[:, None]
+    tol = (2 * e + (nk + 64) * U) * mass
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * (O.abs() + mass)
+    err = (got[~none] - O).abs()
+    assert (err <= tol).all(), f"O off by {(err / tol).max().item():.2f} tolerances"
+    if got_lse is not None:
+        tol = (D + 16) * U * size + (lse.abs() + nk + 64) * U
+        err = (got_lse[~none].double() - lse).abs()
+        assert (err <= tol).all(), f"lse off by {(err / tol).max().item():.2f} tolerances"
+
+
+# ------------------------------------------------------------------------------ prompts
+def run_prompt(dtype, Hq, Hkv, D, nq, nk=None, *, seed=0, scale=None, start=0, spare=3, lse=True, make=None):
+    """Packed prompts with `start` rows of nobody in front and `spare` behind, gaps between heads; checks every sequence."""
+    gen, dt = generator(seed + sum(nq) * 7 + D), TYPES[dtype]
+    scale = D ** -0.5 if scale is None else scale
+    oq = offsets(nq, start)
+    ok = None if nk is None else offsets(nk, 2)
+    Tq, Tk = oq[-1] + spare, (oq[-1] if ok is None else ok[-1]) + spare
+    Q = normal(gen, Hq, Tq + 1, D).to(dt)[:, :Tq]
+    big = normal(gen, Hkv, Tk + 5, D), normal(gen, Hkv, Tk + 2, D)
+    K, V = big[0].to(dt)[:, 2:Tk + 2], big[1].to(dt)[:, :Tk]
+    if make is not None:
+        make(Q, K, V)
+    kq = oq if ok is None else ok
+    for x in (K, V):      # rows of nobody
+        x[:, :kq[0]], x[:, kq[-1]:] = NAN, NAN
+    O = torch.full((Hq, Tq + 2, D), 7.0, dtype=dt, device=DEV)[:, :Tq]
+    L = torch.full((Hq, Tq), 7.0, device=DEV) if lse else None
+    got = pk.pc_prompt_attn(Q, K, V, scale, oq, ok, O=O, lse=L)
+    assert got is O
+    for s in range(len(nq)):
+        a, b = oq[s], oq[s + 1]
+        for h in range(Hq if b > a else 0):
+            g = h // (Hq // Hkv)
+            k, v = K[g, kq[s]:kq[s + 1]], V[g, kq[s]:kq[s + 1]]
+            check_rows(dtype, O[h, a:b], None if L is None else L[h, a:b], Q[h, a:b], k, v, scale, k.shape[0] - (b - a) + 1)
+    for rest in (slice(0, oq[0]), slice(oq[-1], Tq)):
+        assert (O[:, rest] == 7.0).all() and (L is None or (L[:, rest] == 7.0).all())
+    return Q, K, V, O, L
+
+
+HEADS = [(2, 1), (8, 2), (6, 2), (4, 4), (5, 1)]
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
+@pytest.mark.parametrize("nq", [[1], [17], [33, 1, 0, 5], [64, 63, 65, 127, 129], [300, 1], [0, 0, 2, 0]])
+def test_prompt(dtype, D, Hq, Hkv, nq):
+    run_prompt(dtype, Hq, Hkv, D, nq, start=len(nq) - 1)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("nq,nk", [([1], [1000]), ([5, 40], [700, 41]), ([64, 64], [64, 65]), ([7, 3, 200], [5, 0, 190]), ([100], [300]),
+                                   ([3], [0]), ([130, 20, 1], [129, 500, 63])])
+def test_prompt_with_other_keys(dtype, D, nq, nk):
+    run_prompt(dtype, 8, 2, D, nq, nk)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,nq", [("bf16", 4, 1, [1500]), ("bf16", 16, 4, [2049]), ("bf16", 24, 8, [777, 1300]), ("bf16", 16, 4, [4500]),
+                                             ("bf16", 3, 3, [3001]), ("f32", 2, 1, [1100]), ("bf16", 32, 2, [600, 601, 3, 90])])
+def test_prompt_long(dtype, Hq, Hkv, nq):
+    run_prompt(dtype, Hq, Hkv, 128, nq)
+
+
+@pytest.mark.parametrize("n_seq", [64, 65, 150])
+def test_prompt_of_many_sequences(n_seq):
+    rng = np.random.default_rng(n_seq)
+    nq = [int(v) for v in rng.integers(0, 40, n_seq)]
+    run_prompt("bf16", 4, 2, 128, nq, lse=n_seq != 65)
+    run_prompt("bf16", 4, 2, 128, nq, [max(0, n + int(d)) for n, d in zip(nq, rng.integers(-3, 30, n_seq))])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,at", [([90], [(0, 40)]), ([200, 300], [(0, 199), (1, 17), (1, 280)]), ([700], [(0, 3), (0, 650)])])
+def test_prompt_what_a_row_does_not_see_does_not_reach_it(dtype, nq, at):
+    """NaN and infinity in keys and values that only later rows of the sequence see."""
+    Hq, Hkv, D = 4, 2, 128
+    oq = offsets(nq)
+    where = [(s, oq[s] + i) for s, i in at]
+    gen = generator(5)
+    Q, K, V = (normal(gen, H, oq[-1], D).to(TYPES[dtype]) for H in (Hq, Hkv, Hkv))
+    clean = pk.pc_prompt_attn(Q, K, V, D ** -0.5, oq)
+    for i, (s, j) in enumerate(where):
+        V[:, j, 5 + i], V[:, j, 77] = NAN, float("inf")
+        if i % 2:
+            K[:, j, 9] = NAN
+    got = pk.pc_prompt_attn(Q, K, V, D ** -0.5, oq)
+    hit = torch.zeros(oq[-1], dtype=torch.bool, device=DEV)
+    for s, j in where:
+        hit[j:oq[s + 1]] = True
+    assert got[:, ~hit].isfinite().all()
+    assert torch.equal(got[:, ~hit], clean[:, ~hit]) or (got[:, ~hit].float() - clean[:, ~hit].float()).abs().max() < 0.02
+    for i, (s, j) in enumerate(where):
+        assert not got[:, j:oq[s + 1], 5 + i].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("level", [1e8, 1e30])
+def test_prompt_hidden_keys(dtype, level):
+    """Keys that a coordinate of their own hides: rows that see others too weigh those alone, the rest are numbers."""
+    Hq, Hkv, D, n = 4, 2, 128, 150
+    gen = generator(3)
+    Q, K, V = (normal(gen, H, n, D).to(TYPES[dtype]) for H in (Hq, Hkv, Hkv))
+    Q[..., 0], K[..., 0] = 1.0, 0.0
+    K[:, :40, 0] = -level
+    L = torch.empty((Hq, n), device=DEV)
+    O = pk.pc_prompt_attn(Q, K, V, D ** -0.5, [0, n], lse=L)
+    assert O.isfinite().all() and L.isfinite().all()
+    for h in range(Hq):
+        check_rows(dtype, O[h, 40:], None, Q[h, 40:], K[h // 2, 40:], V[h // 2, 40:], D ** -0.5, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_prompt_reference_moves(dtype, order):
+    def make(Q, K, V):
+        n = K.shape[1]
+        ramp = torch.linspace(0, 6, n, device=DEV)
+        K.mul_((ramp if order == "rising" else 6 - ramp)[None, :, None].to(K.dtype))
+    run_prompt(dtype, 8, 2, 128, [500], make=make)
+
+
+def test_prompt_folded_scale():
+    run_prompt("bf16", 8, 2, 128, [333, 70], scale=pk.PC_SCALE_FOLDED)
+    run_prompt("f32", 8, 2, 128, [333, 70], scale=pk.PC_SCALE_FOLDED)
+
+
+@pytest.mark.parametrize("dtype,nq", [("bf16", [300, 20]), ("bf16", [2300]), ("f32", [100, 30])])
+def test_prompt_is_reproducible_and_captured(dtype, nq):
+    Q, K, V, O, L = run_prompt(dtype, 8, 2, 128, nq)
+    oq, out, lse = offsets(nq), torch.zeros_like(Q), torch.zeros(Q.shape[:2], device=DEV)
+    pk.pc_prompt_attn(Q, K, V, 128 ** -0.5, oq, O=out, lse=lse)
+    want, want_lse = out.clone(), lse.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pk.pc_prompt_attn(Q, K, V, 128 ** -0.5, oq, O=out, lse=lse)
+    for _ in range(3):
+        out.zero_(), lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+# ------------------------------------------------------------------------------ pages
+class Paged:
+    """Sequences of given lengths, in 64-bit-free plain form (K, V [Hkv][len][D] each) and in pages: everything that no sequence
+    owns is NaN, table entries behind a sequence's last page are out of range."""
+
+    def __init__(self, dtype, Hkv, D, lens, page=64, shared=0, seed=0, strided=False, make=None, width_more=2):
+        gen, dt = generator(seed + sum(max(n, 0) for n in lens) + D), TYPES[dtype]
+        self.dtype, self.D, self.Hkv, self.page, self.n_shared = dtype, D, Hkv, page, shared
+        self.lens_host = [max(0, n) for n in lens]
+        longest = max(max(self.lens_host), shared, 1)
+        common = [normal(gen, Hkv, shared, D).to(dt) for _ in range(2)]
+        self.seqs = []
+        for n in self.lens_host:
+            kv = [torch.cat((c[:, :n], normal(gen, Hkv, max(0, n - shared), D).to(dt)), 1) for c in common]
+            self.seqs.append(kv)
+        if make is not None:
+            make(self)
+        need = [-(-n // page) for n in self.lens_host]
+        n_common = -(-shared // page)
+        n_pages = sum(need) + n_common + 3
+        free = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).tolist()
+        width = -(-longest // page) + width_more
+        self.table = torch.full((len(lens), width + 1), n_pages + 5, dtype=torch.int32)[:, :width]
+        if strided:      # heads outside, pages inside: a cache of one sequence's layout seen as pages
+            big = [torch.full((Hkv, n_pages + 1, page, D), NAN, dtype=dt, device=DEV) for _ in range(2)]
+            self.pages = tuple(x[:, :n_pages].transpose(0, 1) for x in big)
+        else:
+            self.pages = tuple(torch.full((n_pages, Hkv, page, D), NAN, dtype=dt, device=DEV) for _ in range(2))
+        self.shared = None
+        if shared:
+            ids = [free.pop() for _ in range(n_common)]
+            self.shared = torch.tensor(ids, dtype=torch.int32, device=DEV)
+            self.put(ids, common, 0, shared)
+        for s, n in enumerate(self.lens_host):
+            ids = [free.pop() for _ in range(need[s])]
+            self.table[s, :need[s]] = torch.tensor(ids, dtype=torch.int32)
+            self.put(ids, self.seqs[s], shared, n)     # the common rows in its own pages are nothing that is read
+        self.table = self.table.to(DEV)
+        self.lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+
+    def put(self, ids, rows, begin, end):
+        for i, p in enumerate(ids):
+            a, b = max(i * self.page, begin), min((i + 1) * self.page, end)
+            if a < b:
+                for pool, x in zip(self.pages, rows):
+                    pool[p, :, a - i * self.page:b - i * self.page] = x[:, a:b]
+
+
+def run_pages(dtype, Hq, Hkv, D, lens, n, *, page=64, shared=0, ragged=None, seed=0, scale=None, max_len=None, lse=True, strided=False,
+              make=None, ws=None, paged=None):
+    """n rows of every sequence (ragged: that many of each) over pages; checks every row."""
+    pg = paged or Paged(dtype, Hkv, D, lens, page, shared, seed, strided, make)
+    scale = D ** -0.5 if scale is None else scale
+    rows = ragged if ragged is not None else [n] * len(lens)
+    offs = offsets(rows, 1 if ragged is not None else 0)
+    T = offs[-1] + (2 if ragged is not None else 0)
+    gen = generator(seed + 17)
+    Q = normal(gen, Hq, T + 1, D).to(TYPES[dtype])[:, :T]
+    O = torch.full((Hq, T + 1, D), 7.0, dtype=TYPES[dtype], device=DEV)[:, :T]
+    L = torch.full((Hq, T), 7.0, device=DEV) if lse else None
+    longest = max(max(pg.lens_host), 1) if max_len is None else max_len
+    got = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, longest, scale, offs=offs if ragged is not None else None, shared=pg.shared,
+                          n_shared=shared, O=O, lse=L, ws=ws)
+    assert got is O
+    for s, (k, v) in enumerate(pg.seqs):
+        a, b = offs[s], offs[s + 1]
+        for h in range(Hq if b > a else 0):
+            g = h // (Hq // Hkv)
+            check_rows(dtype, O[h, a:b], None if L is None else L[h, a:b], Q[h, a:b], k[g], v[g], scale, int(pg.lens[s]) - (b - a) + 1)
+    for rest in (slice(0, offs[0]), slice(offs[-1], T)):
+        assert (O[:, rest] == 7.0).all() and (L is None or (L[:, rest] == 7.0).all())
+    return pg, Q, O, L
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (6, 2), (4, 4), (5, 1), (32, 2)])
+@pytest.mark.parametrize("lens,n", [([1], 1), ([130, 64, 0, 1], 1), ([63, 200], 3), ([500, 65, 640], 1), ([40, 1000], 17)])
+def test_page_attn(dtype, D, Hq, Hkv, lens, n):
+    run_pages(dtype, Hq, Hkv, D, lens, n)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [64, 192])
+@pytest.mark.parametrize("shared", [1, 63, 64, 300, 777])
+@pytest.mark.parametrize("n,more", [(1, [1, 5, 64]), (1, [700, 0, 1]), (4, [4, 90, 3])])
+def test_page_attn_common_rows(dtype, D, page, shared, n, more):
+    """more: rows of each sequence behind the common ones; fewer than n: some rows see common rows only."""
+    run_pages(dtype, 8, 2, D, [shared + m for m in more], n, page=page, shared=shared)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,shared", [([0, 400, 5, 130], 128), ([300, 299, 0, 0], 300), ([0, 0], 70), ([-3, 100], 64), ([2, 1, 64], 200)])
+def test_page_attn_sequences_shorter_than_the_common_rows(dtype, lens, shared):
+    run_pages(dtype, 8, 2, 128, lens, 1, shared=shared)
+    run_pages(dtype, 8, 2, 128, lens, 3, shared=shared, seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shared", [0, 100])
+def test_page_attn_ragged(dtype, shared):
+    rng = np.random.default_rng(shared)
+    rows = [1, 0, 40, 7, 130, 1]
+    run_pages(dtype, 8, 2, 128, [shared + n + int(v) for n, v in zip(rows, (500, 30, 0, 64, 200, 0))], None, ragged=rows, shared=shared)
+    rows = [int(v) for v in rng.integers(0, 6, 140)]        # three launches
+    run_pages(dtype, 4, 2, 128, [shared + n + int(v) for n, v in zip(rows, rng.integers(0, 200, 140))], None, ragged=rows, shared=shared)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,lens,n,shared", [
+    ("bf16", 16, 4, [5000, 3, 2049], 1, 0), ("bf16", 16, 4, [9000 + i for i in range(20)], 1, 9000), ("bf16", 4, 1, [4100, 300], 1, 0),
+    ("bf16", 16, 4, [3000 + 40 * i for i in range(3)], 40, 2900), ("bf16", 24, 8, [4500], 300, 0), ("f32", 8, 2, [2500 + i for i in range(5)], 1, 2400),
+    ("bf16", 8, 2, [2100] * 130, 1, 2000), ("bf16", 16, 2, [1000 + i for i in range(70)], 2, 0)])
+def test_page_attn_long(dtype, Hq, Hkv, lens, n, shared):
+    run_pages(dtype, Hq, Hkv, 128, lens, n, shared=shared, page=128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_page_attn_strided_pages_and_bounds(dtype):
+    """Heads outside of the pages; a bound far above the lengths, and one below them."""
+    lens = [300, 65, 128]
+    pg, Q, O, L = run_pages(dtype, 8, 2, 128, lens, 1, strided=True, shared=40)
+    O2 = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, 64 * pg.table.shape[1], 128 ** -0.5, shared=pg.shared, n_shared=40)
+    assert (O2.float() - O.float()).abs().max() < 0.02
+    cut = Paged(dtype, 2, 128, [min(n, 100) for n in lens], shared=40)
+    got = pk.pc_page_attn(Q, cut.pages, cut.table, pg.lens, 100, 128 ** -0.5, shared=cut.shared, n_shared=40)
+    want = pk.pc_page_attn(Q, cut.pages, cut.table, cut.lens, 100, 128 ** -0.5, shared=cut.shared, n_shared=40)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,shared", [(1, 0), (5, 0), (1, 200), (70, 130)])
+def test_page_attn_pages_that_are_not_there(dtype, n, shared):
+    """A page number out of range stands for rows that nobody sees."""
+    lens = [400, 500]
+    pg = Paged(dtype, 2, 128, lens, shared=shared)
+    for at, bad in ((3, -1), (4, 2 ** 30)):
+        pg.table[0, at] = bad
+        if shared:
+            pg.shared[1] = bad
+    T = 2 * n
+    Q = normal(generator(1), 8, T, 128).to(TYPES[dtype])
+    L = torch.empty((8, T), device=DEV)
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, 500, 128 ** -0.5, shared=pg.shared, n_shared=shared, lse=L)
+    for s in range(2):
+        gone = torch.zeros(lens[s], dtype=torch.bool, device=DEV)
+        if s == 0:
+            gone[max(192, shared):320] = True
+        if shared:
+            gone[64:min(128, shared)] = True
+        for h in range(8):
+            for i in range(n):
+                at = s * n + i
+                keep = ~gone & (torch.arange(lens[s], device=DEV) <= lens[s] - n + i)
+                k, v = (x[h // 4][keep] for x in pg.seqs[s])
+                check_rows(dtype, O[h, at:at + 1], L[h, at:at + 1], Q[h, at:at + 1], k, v, 128 ** -0.5, k.shape[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,shared", [(6, 0), (6, 128), (40, 0), (90, 70)])
+def test_page_attn_what_a_row_does_not_see_does_not_reach_it(dtype, n, shared):
+    def make(p):
+        k, v = p.seqs[1]
+        v[:, 190, 7], v[:, 193, 9], k[:, 192, 3] = NAN, float("inf"), NAN
+    lens = [400, 194, 300]
+    pg = Paged(dtype, 2, 128, lens, shared=shared, make=make)
+    Q = normal(generator(2), 8, 3 * n, 128).to(TYPES[dtype])
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, 400, 128 ** -0.5, shared=pg.shared, n_shared=shared)
+    first = n + 190 - (194 - n)       # the row that is row 190 of its sequence, if it is among the new ones
+    clean = [i for i in range(3 * n) if not max(first, n) <= i < 2 * n]
+    assert O[:, clean].isfinite().all()
+    assert not O[:, max(first, n):2 * n, 7].isfinite().any() and not O[:, 2 * n - 1].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_page_attn_hidden_keys(dtype):
+    def make(p):
+        for k, v in p.seqs:
+            k[..., 0] = 0.0
+            k[:, 30:150, 0] = -1e30
+    for lens, shared in (([200, 151, 600], 0), ([200, 151, 600], 20)):
+        pg = Paged(dtype, 2, 128, lens, shared=shared, make=make if not shared else None)
+        Q = normal(generator(2), 8, len(lens), 128).to(TYPES[dtype])
+        Q[..., 0] = 1.0
+        L = torch.empty((8, len(lens)), device=DEV)
+        O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, 600, 128 ** -0.5, shared=pg.shared, n_shared=shared, lse=L)
+        assert O.isfinite().all()
+        for s in range(len(lens)):
+            keep = torch.ones(lens[s], dtype=torch.bool, device=DEV)
+            if not shared:
+                keep[30:150] = False
+            for h in range(8):
+                k, v = (x[h // 4][keep] for x in pg.seqs[s])
+                check_rows(dtype, O[h, s:s + 1], L[h, s:s + 1], Q[h, s:s + 1], k, v, 128 ** -0.5, k.shape[0])
+
+
+@pytest.mark.parametrize("dtype,shared", [("bf16", 0), ("bf16", 700), ("f32", 100)])
+def test_page_attn_is_reproducible_and_captured(dtype, shared):
+    """The lengths grow between replays of one graph."""
+    lens = [shared + 1, shared + 64, shared + 400]
+    pg, Q, O, L = run_pages(dtype, 8, 2, 128, lens, 1, shared=shared)
+    out = torch.zeros_like(O)
+    nws = pk.pc_page_attn_workspace_bytes(pk.PC_BF16 if dtype == "bf16" else pk.PC_F32, 8, 2, 3, 128, 3, shared + 400, shared)
+    ws = torch.full((max(nws, 16),), 0xA5, dtype=torch.uint8, device=DEV)
+    call = lambda: pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, shared + 400, 128 ** -0.5, shared=pg.shared, n_shared=shared, O=out, ws=ws)
+    call()
+    assert torch.equal(out, O)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for d in (0, 1, 30):
+        pg.lens.copy_(torch.tensor([max(1, n - d) for n in lens], dtype=torch.int32))
+        out.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        call()
+        assert torch.equal(got, out)
+
+
+# ------------------------------------------------------------------------------ rows into pages
+def turned(x, pos, D, scale=1.0):
+    y = x.contiguous().clone()
+    if y.shape[1]:
+        pk.pc_rope3d(y, pos, SECTIONS[D], out_scale=scale)
+    return y
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,page,before,rows,ragged", [
+    (8, 2, 64, [0], [1], False), (8, 2, 64, [63, 64, 0, 200], [1, 1, 1, 1], False), (6, 3, 128, [5, 130], [3, 3], False),
+    (5, 1, 64, [0, 60, 0, 7], [70, 0, 1, 130], True), (16, 4, 192, [100] * 70, [2] * 70, True), (24, 8, 64, [0, 31], [257, 33], True)])
+def test_store(dtype, D, Hq, Hkv, page, before, rows, ragged):
+    gen, dt = generator(len(before) + D), TYPES[dtype]
+    lens = [b + n for b, n in zip(before, rows)]
+    pg = Paged(dtype, Hkv, D, lens, page, width_more=0, strided=Hkv == 2)
+    offs = offsets(rows, 1 if ragged else 0)
+    T = offs[-1] + (2 if ragged else 0)
+    K, V = normal(gen, Hkv, T + 3, D).to(dt)[:, :T], normal(gen, Hkv, T + 1, D).to(dt)[:, :T]
+    Q = normal(gen, Hq, T + 2, D).to(dt)[:, :T]
+    pos = torch.randint(-50, 5000, (T, 3), dtype=torch.int32, device=DEV, generator=gen)
+    o = offs if ragged else None
+    mine = slice(offs[0], offs[-1])
+    want_k, want_q = turned(K, pos, D), turned(Q, pos, D, 0.3)
+    before_pages = [x.clone() for x in pg.pages]
+
+    def check(k_rows):
+        for pool, x, was in zip(pg.pages, (k_rows, V), before_pages):
+            want = was.clone()
+            for s in range(len(rows)):
+                for i in range(rows[s]):
+                    r = lens[s] - rows[s] + i
+                    want[pg.table[s, r // page].item(), :, r % page] = x[:, offs[s] + i]
+            assert torch.equal(torch.nan_to_num(pool.float(), 123.0), torch.nan_to_num(want.float(), 123.0))
+    K_out, Q_out = torch.full_like(K, 7.0), torch.full_like(Q, 7.0)
+    K_was, V_was = K.clone(), V.clone()
+    pk.pc_page_store(K, V, pg.pages, pg.table, pg.lens, offs=o, pos=pos, sections=SECTIONS[D], K_out=K_out, Q=Q, Q_out=Q_out, out_scale=0.3)
+    check(want_k)
+    assert torch.equal(K_out[:, mine], want_k[:, mine]) and torch.equal(Q_out[:, mine], want_q[:, mine])
+    for rest in (slice(0, offs[0]), slice(offs[-1], T)):
+        assert (K_out[:, rest] == 7.0).all() and (Q_out[:, rest] == 7.0).all()
+    assert torch.equal(K, K_was) and torch.equal(V, V_was)
+    for pool, was in zip(pg.pages, before_pages):
+        pool.copy_(was)
+    pk.pc_page_store(K, V, pg.pages, pg.table, pg.lens, offs=o, pos=pos, sections=SECTIONS[D], K_out=K, Q=Q, Q_out=Q, out_scale=0.3)
+    check(want_k)       # in place
+    assert torch.equal(K[:, mine], want_k[:, mine]) and torch.equal(Q[:, mine], want_q[:, mine])
+    for pool, was in zip(pg.pages, before_pages):
+        pool.copy_(was)
+    K.copy_(K_was)
+    K[:, mine.start, 3] = NAN
+    pk.pc_page_store(K, V, pg.pages, pg.table, pg.lens, offs=o)     # as they are
+    check(K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_store_rows_without_a_page(dtype):
+    """Pausing sequences, lengths beyond the table, page numbers out of range: nothing is stored, the rest is."""
+    Hkv, D, page = 2, 128, 64
+    pg = Paged(dtype, Hkv, D, [64, 1, 128, 60, 60], page, width_more=0)
+    lens = torch.tensor([0, -5, 200, 60, 1], dtype=torch.int32, device=DEV)      # idle; negative; behind the table; bad page; fine
+    pg.table[3, 0] = -2
+    T, gen = 5, generator(4)
+    K, V = normal(gen, Hkv, T, D).to(TYPES[dtype]), normal(gen, Hkv, T, D).to(TYPES[dtype])
+    pos = torch.zeros((T, 3), dtype=torch.int32, device=DEV)
+    was = [x.clone() for x in pg.pages]
+    K_out = torch.zeros_like(K)
+    pk.pc_page_store(K, V, pg.pages, pg.table, lens, pos=pos, sections=SECTIONS[D], K_out=K_out)
+    for pool, w, x in zip(pg.pages, was, (K, V)):
+        w[pg.table[4, 0].item(), :, 0] = x[:, 4]
+        assert torch.equal(torch.nan_to_num(pool.float(), 123.0), torch.nan_to_num(w.float(), 123.0))
+    assert torch.equal(K_out, K)
+
+
+# ------------------------------------------------------------------------------ large offsets, streams
+def test_offsets_beyond_32_bits():
+    """Pages whose elements lie beyond 2^32 bytes and 2^31 elements, K and V of 4.5 GiB each."""
+    Hkv, D, page = 2, 128, 64
+    n_pages = (2 ** 31 + 2 ** 28) // (Hkv * page * D)
+    K = torch.empty((n_pages, Hkv, page, D), dtype=torch.bfloat16, device=DEV)
+    pages = (K, torch.empty_like(K))
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32, device=DEV)
+    gen = generator(9)
+    k, v = (normal(gen, Hkv, 150, D).to(torch.bfloat16) for _ in range(2))
+    lens = torch.tensor([150], dtype=torch.int32, device=DEV)
+    pk.pc_page_store(k, v, pages, table, lens)
+    assert torch.equal(pages[0][n_pages - 2, :, :22], k[:, 128:]) and torch.equal(pages[1][n_pages - 1], v[:, :64])
+    Q = normal(gen, 8, 1, D).to(torch.bfloat16)
+    O = pk.pc_page_attn(Q, pages, table, lens, 150, D ** -0.5)
+    for h in range(8):
+        check_rows("bf16", O[h], None, Q[h], k[h // 4], v[h // 4], D ** -0.5, 150)
+
+
+def test_calls_on_two_streams_do_not_meet():
+    pgs = [Paged("bf16", 2, 128, [700 + i, 300], shared=200, seed=i) for i in range(2)]
+    Qs = [normal(generator(i), 8, 2, 128).to(torch.bfloat16) for i in range(2)]
+    call = lambda i: pk.pc_page_attn(Qs[i], pgs[i].pages, pgs[i].table, pgs[i].lens, 701, 128 ** -0.5, shared=pgs[i].shared, n_shared=200)
+    want = [call(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        got = []
+        for i, st in enumerate(streams):
+            st.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(st):
+                got.append(call(i))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

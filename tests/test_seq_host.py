@@ -1,0 +1,160 @@
+"""Prompts and pages on the CPU: what the entry points refuse, and calls that do nothing.
+
+The library checks its arguments before any device work, so refusals are asked for with made-up addresses here."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+import paper_2601_04359_amd as pk
+from paper_2601_04359_amd import binding
+
+NULL, SHAPE, DTYPE, UNSUPPORTED, WORKSPACE = -1, -2, -3, -4, -6
+A = 1 << 40       # made-up addresses, far apart
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(binding.lib_path()):
+        from paper_2601_04359_amd.build import build_library
+        build_library()
+    return binding.lib()
+
+
+def ints(v):
+    return None if v is None else (C.c_int32 * len(v))(*v)
+
+
+def prompt(L, **kw):
+    a = dict(Q=A, K=2 * A, V=3 * A, dtype=pk.PC_BF16, Hq=8, Hkv=2, Tq=100, Tk=100, D=128, qs=12800, ks=12800, vs=12800, os=12800,
+             scale=0.1, oq=[0, 40, 100], ok=None, n=2, O=4 * A, lse=None)
+    a.update(kw)
+    return L.pc_prompt_attn(a["Q"], a["K"], a["V"], a["dtype"], a["Hq"], a["Hkv"], a["Tq"], a["Tk"], a["D"], a["qs"], a["ks"], a["vs"],
+                            a["os"], a["scale"], ints(a["oq"]), ints(a["ok"]), a["n"], a["O"], a["lse"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(Q=None), NULL), (dict(K=None), NULL), (dict(V=None), NULL), (dict(O=None), NULL), (dict(oq=None), NULL),
+    (dict(dtype=2), DTYPE), (dict(D=96), UNSUPPORTED), (dict(D=256), UNSUPPORTED), (dict(Hq=7), SHAPE), (dict(Hkv=0), SHAPE),
+    (dict(scale=0.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE), (dict(Tq=-1), SHAPE), (dict(n=-1), SHAPE),
+    (dict(oq=[0, 40, 101]), SHAPE), (dict(oq=[-1, 40, 100]), SHAPE), (dict(oq=[0, 60, 50]), SHAPE), (dict(ok=[0, 40, 101]), SHAPE),
+    (dict(ok=[0, 60, 50]), SHAPE), (dict(qs=12792), SHAPE), (dict(os=12792), SHAPE), (dict(ks=12792), SHAPE), (dict(vs=12792), SHAPE),
+    (dict(qs=12801), SHAPE), (dict(Q=A + 8), SHAPE), (dict(O=4 * A + 2), SHAPE), (dict(K=2 * A + 4), SHAPE),
+    (dict(O=A), SHAPE), (dict(O=A + 2 * 12800 * 7), SHAPE), (dict(O=2 * A - 16), SHAPE), (dict(O=3 * A + 256), SHAPE),
+    (dict(Tq=2 ** 30, qs=2 ** 38, os=2 ** 38), UNSUPPORTED), (dict(Tk=2 ** 31 - 1, ks=2 ** 40, vs=2 ** 40), UNSUPPORTED)])
+def test_prompt_refuses(L, kw, status):
+    assert prompt(L, **kw) == status, L.pc_last_error_detail()
+
+
+def test_calls_that_do_nothing(L):
+    assert prompt(L, n=0) == 0 and prompt(L, oq=[5, 5, 5], ok=[0, 3, 9]) == 0
+    assert store(L, T=0) == 0 and store(L, n=0) == 0
+    assert attn(L, T=0) == 0 and attn(L, n=0) == 0
+
+
+def pages(**kw):
+    a = dict(K=5 * A, V=6 * A, stride_page=2 * 64 * 128, stride_h=64 * 128, n_pages=10, page_rows=64)
+    a.update(kw)
+    return binding._Pages(*a.values())
+
+
+def store(L, pg=None, **kw):
+    a = dict(K=A, V=2 * A, dtype=pk.PC_BF16, Hkv=2, T=4, D=128, ks=512, vs=512, table=7 * A, width=3, ts=3, lens=8 * A, offs=None, n=4,
+             pos=9 * A, sec=(32, 48, 48), base=1e4, Ko=None, kos=512, Q=3 * A, Qo=4 * A, Hq=8, qs=512, qos=512, out=1.0)
+    a.update(kw)
+    p = C.byref(pages() if pg is None else pg) if pg is not False else None
+    return L.pc_page_store(a["K"], a["V"], a["dtype"], a["Hkv"], a["T"], a["D"], a["ks"], a["vs"], p, a["table"], a["width"], a["ts"],
+                           a["lens"], ints(a["offs"]), a["n"], a["pos"], *a["sec"], a["base"], a["Ko"], a["kos"], a["Q"], a["Qo"], a["Hq"],
+                           a["qs"], a["qos"], a["out"], None)
+
+
+def attn(L, pg=None, **kw):
+    a = dict(Q=A, dtype=pk.PC_BF16, Hq=8, Hkv=2, T=4, D=128, qs=512, os=512, scale=0.1, table=7 * A, width=3, ts=3, lens=8 * A, offs=None,
+             n=4, max_len=100, shared=None, n_shared=0, O=2 * A, lse=None, ws=3 * A, wb=1 << 30)
+    a.update(kw)
+    p = C.byref(pages() if pg is None else pg) if pg is not False else None
+    return L.pc_page_attn(a["Q"], p, a["dtype"], a["Hq"], a["Hkv"], a["T"], a["D"], a["qs"], a["os"], a["scale"], a["table"], a["width"],
+                          a["ts"], a["lens"], ints(a["offs"]), a["n"], a["max_len"], a["shared"], a["n_shared"], a["O"], a["lse"], a["ws"],
+                          a["wb"], None)
+
+
+BAD_PAGES = [(pages(K=None), NULL), (pages(V=None), NULL), (False, NULL), (pages(n_pages=0), SHAPE), (pages(page_rows=32), SHAPE),
+             (pages(page_rows=100), SHAPE), (pages(page_rows=0), SHAPE), (pages(stride_h=64 * 128 - 8), SHAPE),
+             (pages(stride_page=64 * 128 - 8), SHAPE), (pages(K=5 * A + 2), SHAPE), (pages(V=6 * A + 8), SHAPE),
+             (pages(stride_h=64 * 128 + 1), SHAPE), (pages(stride_page=2 * 64 * 128 + 4), SHAPE)]
+BAD_SEQUENCES = [(dict(table=None), NULL), (dict(lens=None), NULL), (dict(width=0), SHAPE), (dict(ts=2), SHAPE), (dict(T=5), SHAPE),
+                 (dict(offs=[0, 1, 2, 3, 5]), SHAPE), (dict(offs=[0, 2, 1, 3, 4]), SHAPE), (dict(offs=[-1, 1, 2, 3, 4]), SHAPE),
+                 (dict(T=-1), SHAPE), (dict(n=-1), SHAPE), (dict(dtype=3), DTYPE), (dict(D=32), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("pg,status", BAD_PAGES)
+def test_pages_are_checked(L, pg, status):
+    assert store(L, pg) == status and attn(L, pg) == status
+
+
+@pytest.mark.parametrize("kw,status", BAD_SEQUENCES)
+def test_sequences_are_checked(L, kw, status):
+    assert store(L, **kw) == status and attn(L, **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(K=None), NULL), (dict(V=None), NULL), (dict(Q=None), NULL), (dict(Qo=None), NULL), (dict(pos=None), NULL), (dict(Hkv=0), SHAPE),
+    (dict(sec=(32, 48, 46)), SHAPE), (dict(sec=(31, 49, 48)), SHAPE), (dict(sec=(-2, 82, 48)), SHAPE), (dict(base=0.0), SHAPE),
+    (dict(out=0.0), SHAPE), (dict(out=float("inf")), SHAPE), (dict(ks=504), SHAPE), (dict(vs=504), SHAPE), (dict(qs=504), SHAPE),
+    (dict(qos=504), SHAPE), (dict(Ko=10 * A, kos=504), SHAPE), (dict(Ko=10 * A + 8), SHAPE), (dict(K=A + 2), SHAPE), (dict(Q=3 * A + 4), SHAPE),
+    (dict(Hq=0), SHAPE), (dict(width=2 ** 26, ts=2 ** 26), SHAPE)])
+def test_store_refuses(L, kw, status):
+    assert store(L, **kw) == status, L.pc_last_error_detail()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(Q=None), NULL), (dict(O=None), NULL), (dict(Hq=7), SHAPE), (dict(scale=-1.0), SHAPE), (dict(max_len=0), SHAPE), (dict(max_len=193), SHAPE),
+    (dict(shared=10 * A), SHAPE), (dict(n_shared=5), SHAPE), (dict(shared=10 * A, n_shared=-5), SHAPE), (dict(O=A), SHAPE),
+    (dict(O=A + 512 * 2 * 8 - 16), SHAPE), (dict(qs=504), SHAPE), (dict(os=504), SHAPE), (dict(Q=A + 8), SHAPE), (dict(O=2 * A + 8), SHAPE),
+    (dict(max_len=192, shared=10 * A, n_shared=100, ws=None), WORKSPACE), (dict(max_len=192, shared=10 * A, n_shared=100, wb=64), WORKSPACE),
+    (dict(max_len=192, shared=10 * A, n_shared=100, ws=3 * A + 8), WORKSPACE),
+    (dict(T=2 ** 23, n=2 ** 23, qs=2 ** 30, os=2 ** 30), UNSUPPORTED)])
+def test_attn_refuses(L, kw, status):
+    assert attn(L, **kw) == status, L.pc_last_error_detail()
+
+
+def test_workspaces(L):
+    size = lambda **kw: pk.pc_page_attn_workspace_bytes(**{**dict(dtype=pk.PC_BF16, Hq=8, Hkv=2, T=4, D=128, n_seq=4, max_len=100), **kw})
+    assert size(n_shared=50) >= 2 * 8 * 4 * (128 * 4 + 8)          # the common rows and the others: two shares at least
+    assert size(Hq=7) == 0 and size(D=96) == 0 and size(T=5) == 0 and size(max_len=0) == 0 and size(dtype=2) == 0
+    assert size(offs=[0, 1, 2, 3, 9], T=9, n_shared=50) > 0 and size(offs=[0, 2, 1, 3, 4]) == 0
+
+
+# ------------------------------------------------------------------------------ the binding
+def test_binding_refuses_what_does_not_fit(L):
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+
+    def refused(f, *a, **kw):
+        with pytest.raises(pk.PackCacheError) as e:
+            f(*a, **kw)
+        return e.value.status
+    Q, K = bf(8, 10, 128), bf(2, 10, 128)
+    assert refused(pk.pc_prompt_attn, Q[0], K, K, 0.1, [0, 10]) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K, K[:, :9], 0.1, [0, 10]) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K.float(), K, 0.1, [0, 10]) == DTYPE
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, []) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, [0, 10], [0, 5, 10]) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, [0, 2 ** 31]) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, [0, 10], O=Q[:, :9]) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, [0, 10], lse=torch.zeros(8, 9)) == SHAPE
+    assert refused(pk.pc_prompt_attn, Q, K.transpose(0, 1).contiguous().transpose(0, 1), K, 0.1, [0, 10]) == SHAPE     # rows not dense
+    assert refused(pk.pc_prompt_attn, Q, K, K, 0.1, [0, 10]) == SHAPE                                                  # not on the GPU
+    pg = (bf(3, 2, 64, 128), bf(3, 2, 64, 128))
+    for f in (lambda *a, **k: pk.pc_page_store(K, K, *a, **k), lambda p, t, n, **k: pk.pc_page_attn(Q, p, t, n, 64, 0.1, **k)):
+        assert refused(f, pg[0][0], i32(10, 2), i32(10)) == SHAPE
+        assert refused(f, (pg[0], pg[1][:2]), i32(10, 2), i32(10)) == SHAPE
+        assert refused(f, (pg[0].float(), pg[1].float()), i32(10, 2), i32(10)) == SHAPE
+        assert refused(f, pg, i32(10, 2), i32(10)) == SHAPE                  # not on the GPU
+    with pytest.raises(pk.PackCacheError):
+        pk.page_cache(3, 2, 100, 128, device="cpu")
+    k, v = pk.page_cache(3, 2, 128, 64, dtype=torch.float32, device="cpu")
+    assert k.shape == v.shape == (3, 2, 128, 64) and k.dtype == torch.float32
+    with pytest.raises(pk.PackCacheError):
+        binding._sequences(i32(4, 2).long(), i32(4), None, 4)
