@@ -1,0 +1,832 @@
+// The bf16 forms of the attention on several sequences (D = 128, gfx950 only), on the 32x32x16 bf16 MFMA.
+//
+// Scores are formed transposed, S^T = K Q^T: a lane holds ONE query (column l % 32) and 16 of 32 keys (with g = l / 32, keys
+// 8 i + 4 g .. + 3, i = 0 .. 3), so that a row's limit, reference and sum are per-lane numbers and the probabilities are
+// the B operand of O^T += V^T P^T as they stand.  What a row does not see gets the score -inf, in the tiles where a row
+// of the work-group does not see everything; a tile of keys lies in one page.
+#pragma once
+
+#include <limits.h>
+
+#include <type_traits>
+
+#include "attn_phase.h"
+#include "seq_rows.h"
+
+namespace pc {
+
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+
+// The sign bits of those halves of a dword that are bf16 numbers which are not finite: an exponent of ones carries into the
+// sign.  By whole dwords, so that no comparison takes a pair of scalar registers of its own.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t odd_bf16(u32x4 v) { return odd_halves(v[0]) | odd_halves(v[1]) | odd_halves(v[2]) | odd_halves(v[3]); }
+__device__ __forceinline__ u32x4 finite_bf16(u32x4 v) {   // those as zeros
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] &= ~((odd_halves(v[i]) >> 15) * 0xFFFFu);
+  return v;
+}
+// Those of a row of V added to a lane's output: dims 32 db + 8 a + 4 g .. + 3 are accumulators 4 a .. of block db.
+__device__ __forceinline__ void add_odd(f32x16 (&o)[4], const uint16_t* v, int g) {
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(v + db * 32 + a * 8 + g * 4);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t odd = w[e] & (odd_halves(w[e]) >> 15) * 0xFFFFu;
+        o[db][a * 4 + e * 2] += __uint_as_float(odd << 16);
+        o[db][a * 4 + e * 2 + 1] += __uint_as_float(odd & 0xFFFF0000u);
+      }
+    }
+}
+// Scores of keys `from` .. `upto` - 1, counted from a lane's first, stay; the others become -inf.
+__device__ __forceinline__ int keys_below(int n) {   // the accumulators of keys below n
+  int bits = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) bits |= ((1 << min(max(n - 8 * q, 0), 4)) - 1) << (4 * q);
+  return bits;
+}
+__device__ __forceinline__ void hide(f32x16& sc, int from, int upto) {
+  const int seen = keys_below(upto) & ~keys_below(from);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t keep = static_cast<uint32_t>(__builtin_amdgcn_sbfe(seen, i, 1));
+    sc[i] = __uint_as_float((__float_as_uint(sc[i]) & keep) | (0xFF800000u & ~keep));
+  }
+}
+
+// A pointer that is the same in every lane, in scalar registers (with page numbers in it, the compiler does not always see
+// that it is).
+template <bool kPages>
+__device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
+  if constexpr (!kPages) return p;
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+  return reinterpret_cast<const uint16_t*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// Where a work-group's keys lie.  The page of a tile (its number, -1: none) comes from the lanes' registers, 64 tiles at a
+// time.
+template <bool kPages, int kTile>
+struct KeyTiles {
+  const RowsArgs& a;
+  const RowSet& r;
+  const uint16_t *Kh, *Vh;
+  int stride;      // tiles from one of this wave's to its next, and the first of them: key begin + (first + i * stride) kTile
+  int first, ids, lane;
+  __device__ __forceinline__ KeyTiles(const RowsArgs& args, const RowSet& set, int first_tile, int tile_stride, int l)
+      : a(args), r(set), Kh(static_cast<const uint16_t*>(args.K) + set.kvh * args.k_stride),
+        Vh(static_cast<const uint16_t*>(args.V) + set.kvh * args.v_stride), stride(tile_stride), first(first_tile), ids(-1), lane(l) {}
+  __device__ __forceinline__ int key_of(int i) const { return r.begin + (first + i * stride) * kTile; }
+  __device__ __forceinline__ void fetch(int i0, int end) {   // the pages of tiles i0 .. i0 + 63
+    if constexpr (kPages) {
+      const int k = key_of(i0 + lane);
+      ids = -1;
+      if (k < end) ids = r.pages[a.by_page.of(k)];
+      if (ids >= a.n_pages || k + kTile <= r.lo) ids = -1;   // no page, or no row of it is asked for
+    }
+  }
+  __device__ __forceinline__ int page(int i) const { return kPages ? __builtin_amdgcn_readlane(ids, i & 63) : 0; }
+  // row `key` of the cache, in elements from Kh or Vh on
+  __device__ __forceinline__ int64_t at(int key, int pg) const {
+    if constexpr (kPages) return pg * a.page_stride + static_cast<int64_t>(key - a.by_page.of(key) * a.by_page.d) * kD;
+    return static_cast<int64_t>(r.k0 + key) * kD;
+  }
+  // byte offset of chunk `chunk` of row key0 + row of a tile that begins with key0: rows that do not exist are read as the
+  // nearest that does
+  __device__ __forceinline__ uint32_t offset(int key0, int row, int chunk) const {
+    return (min(max(key0 + row, r.lo), r.n_keys - 1) - key0) * kRowBytes + chunk * 16;
+  }
+};
+
+// The end of a work-group whose waves share rows: wave w has (O, m, l) of rows 32 (w % kR) .. + 31 of the tile over its part of
+// the keys.  Piece i of a wave's O = accumulators 4 i .. + 3 of every lane = dims 8 i + 4 g .. + 3 of its row, lanes permuted by
+// i so that the reads use every bank; a thread adds up eight dims of a row, in the order of the waves, and rows leave whole.
+constexpr int kWaveOBytes = 32 * kD * 4;
+template <int kR, int kG>
+__device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, lds_u8* smem, const f32x16 (&o)[4], float m, float l,
+                                            int wave, int lane) {
+  constexpr int kWaves = kR * kG;
+  auto piece = [&](int w, int i, int of_lane) {
+    return reinterpret_cast<lds_f32x4*>(smem + w * kWaveOBytes + i * 1024 + (of_lane ^ i) * 16);
+  };
+  auto* s_ml = reinterpret_cast<__attribute__((address_space(3))) float*>(smem + kWaves * kWaveOBytes);
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *piece(wave, db * 4 + q, lane) = f32x4{o[db][q * 4], o[db][q * 4 + 1], o[db][q * 4 + 2], o[db][q * 4 + 3]};
+  if (lane < 32) {
+    s_ml[(wave * 32 + lane) * 2] = m;
+    s_ml[(wave * 32 + lane) * 2 + 1] = l;
+  }
+  __syncthreads();
+  const int i = threadIdx.x & 15, n_set = r.n_tok * a.rep;
+#pragma unroll
+  for (int pass = 0; pass < 8 * kR / kWaves; ++pass) {
+    const int in_tile = pass * 4 * kWaves + (threadIdx.x >> 4), rg = in_tile >> 5, row = in_tile & 31;
+    const int rho = r.tile * 32 * kR + in_tile;
+    if (rho >= n_set) return;
+    float mw[kG], M = kNothing, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kG; ++w) {
+      mw[w] = s_ml[((w * kR + rg) * 32 + row) * 2];
+      M = fmaxf(M, mw[w]);
+    }
+    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int w = 0; w < kG; ++w) {
+      const float by = __builtin_amdgcn_exp2f(mw[w] - M);
+      L += by * s_ml[((w * kR + rg) * 32 + row) * 2 + 1];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) acc[t] += by * *piece(w * kR + rg, i, t * 32 + row);
+    }
+    const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
+    const int64_t t = r.t0 + tok;
+    if (a.part_o != nullptr) {
+      const int64_t at = (static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep + head) * a.T + t;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(a.part_o + at * kD + i * 8 + h * 4) = acc[h];
+      if (i == 0) a.part_ml[at] = make_float2(M, L);
+      continue;
+    }
+    const bool none = limit_of(a, r, tok) <= r.lo;
+    const float inv = none ? 0.f : 1.f / L;
+    u32x4 out = {0u, 0u, 0u, 0u};
+    if (!none) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        out[h * 2] = pack_bf16x2(acc[h][0] * inv, acc[h][1] * inv);
+        out[h * 2 + 1] = pack_bf16x2(acc[h][2] * inv, acc[h][3] * inv);
+      }
+    }
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.O) + head * a.o_stride + t * kD + i * 8) = out;
+    if (a.lse != nullptr && i == 0) a.lse[head * static_cast<int64_t>(a.T) + t] = none ? -INFINITY : lse_of(M, L);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows: 32 query rows per work-group.  The eight waves take the keys in steps of 32 by turns, each through LDS of its
+// own, so that the loop has no barrier (a step's fragments go to registers at once, the next step is fetched behind them);
+// (O, m, l) of the waves are merged through LDS once.  Bound: the bytes of K and V, or latency.
+// ------------------------------------------------------------------------------------------
+constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 8;
+constexpr int kFewTileBytes = kFewKeys * kRowBytes;
+constexpr int kFewWaveBytes = kWaveOBytes;     // a wave's O; while it runs, a step's K and V
+constexpr size_t kFewSmem = kFewWaves * (kFewWaveBytes + 32 * 8) + kFewRows * kRowBytes;
+static_assert(2 * kFewTileBytes <= kFewWaveBytes, "a wave's K and V");
+
+template <bool kPages>
+__global__ __launch_bounds__(kFewWaves * 64, 1) void rows_few_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, g = lane >> 5;
+  const RowSet r = kPages ? page_rows<kFewRows>(a, blockIdx.x, lane) : prompt_rows<kFewRows>(a, blockIdx.x, lane);
+  if (r.idle) return;
+  const int n_set = r.n_tok * a.rep;
+  const lds_u8* lds = smem + wave * kFewWaveBytes;
+  const uint32_t lds_w = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
+  const lds_u8* q_tile = smem + kFewWaves * (kFewWaveBytes + 32 * 8);
+  KeyTiles<kPages, kFewKeys> keys(a, r, wave, kFewWaves, lane);
+  keys.fetch(0, r.end);
+
+  {   // four query rows per wave
+    const int row = wave * 4 + (lane >> 4), rho = min(r.tile * kFewRows + row, n_set - 1);
+    const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
+    dma_16B(static_cast<const uint16_t*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * kD + k_chunk_pos(row, lane & 15) * 8,
+            static_cast<uint32_t>(reinterpret_cast<uintptr_t>(q_tile)) + wave * 1024);
+  }
+  auto stage = [&](int i) {   // step i of this wave: 32 rows of K and of V; false: they are nobody's
+    const int pg = keys.page(i);
+    if (pg < 0) return false;
+    const int k0 = keys.key_of(i);
+    const int64_t at = keys.at(k0, pg);
+    const uint16_t *kb = keys.Kh + at, *vb = keys.Vh + at;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int row = p * 4 + (lane >> 4), pos = lane & 15;
+      dma_16B_at(kb, keys.offset(k0, row, k_chunk_pos(row, pos)), lds_w + p * 1024);
+      dma_16B_at(vb, keys.offset(k0, row, v_chunk_pos(row, pos)), lds_w + kFewTileBytes + p * 1024);
+    }
+    return true;
+  };
+  // the first step goes out before the rows' limits are known; it may turn out to be needed by none
+  bool there = keys.key_of(0) < r.end && stage(0);
+
+  const int tok = a.by_rep.of(min(r.tile * kFewRows + l32, n_set - 1));
+  const int lim = limit_of(a, r, tok);
+  int lim_max = lim, lim_min = lim > 0 ? lim : INT_MAX;   // over the rows that see something
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) {
+    lim_max = max(lim_max, __shfl_xor(lim_max, x));
+    lim_min = min(lim_min, __shfl_xor(lim_min, x));
+  }
+  const int end = min(r.end, __builtin_amdgcn_readfirstlane(lim_max));
+  lim_min = __builtin_amdgcn_readfirstlane(lim_min);
+
+  int k_off[8], v_off[4];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) k_off[s] = l32 * kRowBytes + k_chunk_pos(l32, 2 * s + g) * 16;
+  {
+    const int r16 = lane & 15, G = (lane >> 4) & 1, row = g * 4 + (r16 >> 2);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const int dim = db * 32 + G * 16 + 4 * (r16 & 3);
+      v_off[db] = kFewTileBytes + row * kRowBytes + v_chunk_pos(row, dim >> 3) * 16 + (dim & 7) * 2;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) qf[s] = lds_frag(q_tile + k_off[s]);
+
+  f32x16 o[4];
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m = kNothing, l = 0.f;
+  for (int i = 0;; ++i) {
+    const int k0 = keys.key_of(i);
+    if (k0 >= end) break;
+    const bool now = there;
+    const int64_t at = kPages && now ? keys.at(k0, keys.page(i)) : keys.at(k0, 0);
+    // This step's rows have landed (they are all that is in flight): every fragment goes to registers, so that the next
+    // step's rows can be fetched into the same LDS at once.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bf16x8 kf[8], vf[2][4];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) kf[s] = lds_frag(lds + k_off[s]);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const lds_u8* src = lds + v_off[db] + ks * 16 * kRowBytes;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+            reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(src)));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+            reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(src + 8 * kRowBytes)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          vf[ks][db][e] = lo[e];
+          vf[ks][db][4 + e] = hi[e];
+        }
+      }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(kf[s]));
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(vf[ks][db]));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (kPages && (i & 63) == 63) keys.fetch(i + 1, r.end);
+    there = keys.key_of(i + 1) < end && stage(i + 1);
+    if (!now) continue;
+
+    f32x16 sc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
+    if (k0 + kFewKeys > lim_min || k0 < r.lo) {
+      hide(sc, r.lo - k0 - g * 4, lim - k0 - g * 4);
+      uint32_t odd = 0;   // 0 times what is not finite would reach rows that do not see it
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) odd |= odd_bf16(__builtin_bit_cast(u32x4, vf[ks][db]));
+      if (__any(odd != 0)) {
+        for (int j = max(k0, r.lo); j < min(k0 + kFewKeys, r.n_keys); ++j)
+          if (j < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(j - k0) * kD, g);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int db = 0; db < 4; ++db) vf[ks][db] = __builtin_bit_cast(bf16x8, finite_bf16(__builtin_bit_cast(u32x4, vf[ks][db])));
+      }
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e]);
+    mx = wave_half_max(mx) * a.c;
+    float ref = m;
+    if (__any(!(mx <= m + 8.f) || far_ref(m))) {     // the reference lags by at most 2^8
+      const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
+      ref = m = m_new;
+      if (far_ref(m)) {      // its exponents come to the common fma as products of c, with 0 as their reference
+        const float by = 1.f / a.c;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = far_exponent(sc[e], a.c, m) * by;
+        ref = 0.f;
+      }
+    }
+    bf16x8 p[2];
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(sc[e], a.c, -ref));
+      sum += x;
+      p[e >> 3][e & 7] = static_cast<__bf16>(x);
+    }
+    l += sum;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][db], p[ks], o[db], 0, 0, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // a first step that was needed by none may be in flight
+  l = wave_half_sum(l);
+
+  merge_waves<1, kFewWaves>(a, r, smem, o, m, l, wave, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// Many rows: 128 query rows per work-group, 32 for each of four waves, two work-groups per compute unit.  Keys in tiles of
+// 64, two of K and two of V in LDS (64 KB), processed as halves A and B of 32 keys; every wave runs
+//     phase 1 of tile j:  S_B(j), O += V_B(j-1) P_B(j-1)  |  P_A(j)
+//     phase 2 of tile j:  S_A(j+1), O += V_A(j) P_A(j)    |  P_B(j)
+// (pipeline_phase).  One barrier per tile, after phase 1: behind it K(j+2) and V(j+1) are fetched into the slots just
+// released.  Bound: the matrix pipe, which the other work-group of the unit keeps busy while one waits at its barrier.
+// ------------------------------------------------------------------------------------------
+constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves, kManyKeys = 64;
+constexpr int kManyTileBytes = kManyKeys * kRowBytes;
+constexpr size_t kManySmem = 4 * kManyTileBytes + kManyWaves * 8;   // tiles, the waves' limits
+
+template <bool kUnitC, bool kPages>
+__global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lds_mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + wave * 4096;
+  const int l32 = lane & 31, g = lane >> 5;
+  const RowSet r = kPages ? page_rows<kManyRows>(a, blockIdx.x, lane) : prompt_rows<kManyRows>(a, blockIdx.x, lane);
+  if (r.idle) return;
+  const int n_set = r.n_tok * a.rep, row_first = r.tile * kManyRows + wave * 32;
+  const bool active = row_first < n_set;   // wave-uniform
+  const int rho = min(row_first + l32, n_set - 1);
+  const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
+
+  KeyTiles<kPages, kManyKeys> keys(a, r, 0, 1, lane);
+  auto k_slot = [](int t) { return (t & 1) * kManyTileBytes; };
+  auto v_slot = [](int t) { return (2 + (t & 1)) * kManyTileBytes; };
+  // a wave's 16 rows of a tile; rows that are nobody's are zeros
+  auto stage = [&](auto is_v, int j, int pg, int slot) {
+    if (pg < 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        reinterpret_cast<lds_u32x4*>(smem + slot + (wave * 4 + i) * 1024)[lane] = u32x4{0u, 0u, 0u, 0u};
+      return;
+    }
+    const int k0 = keys.key_of(j);
+    const uint16_t* base = (decltype(is_v)::value ? keys.Vh : keys.Kh) + keys.at(k0, pg);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = (wave * 4 + i) * 4 + (lane >> 4), pos = lane & 15;
+      dma_16B_at(base, keys.offset(k0, row, decltype(is_v)::value ? v_chunk_pos(row, pos) : k_chunk_pos(row, pos)),
+                 lds_mine + slot + i * 1024);
+    }
+  };
+  keys.fetch(0, r.end);
+  int pg = keys.page(0), pg_next = keys.page(1);   // pages of tiles j and j + 1
+  if (r.begin < r.end) {   // the first tiles go out before it is known how many there are
+    stage(std::false_type{}, 0, pg, k_slot(0));
+    stage(std::true_type{}, 0, pg, v_slot(0));
+    if (keys.key_of(1) < r.end) stage(std::false_type{}, 1, pg_next, k_slot(1));
+  }
+  // the slot of V(-1) is read once against zero probabilities: clear it
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<lds_u32x4*>(smem + v_slot(1) + (wave * 4 + i) * 1024)[lane] = u32x4{0u, 0u, 0u, 0u};
+
+  // the wave's queries, as fragments
+  bf16x8 qf[8];
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * kD + g * 8;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
+  }
+  // What the rows see.  One that sees none of these keys takes part as if it saw all, and its result is thrown away.
+  const int lim_true = limit_of(a, r, tok);
+  const bool sees = lim_true > max(r.lo, r.begin);
+  const int lim = sees ? lim_true : INT_MAX;
+  int lim_max = sees ? lim_true : 0, lim_min = lim;
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) {
+    lim_max = max(lim_max, __shfl_xor(lim_max, x));
+    lim_min = min(lim_min, __shfl_xor(lim_min, x));
+  }
+  lim_min = __builtin_amdgcn_readfirstlane(lim_min);   // of the wave
+  auto* s_lim = reinterpret_cast<__attribute__((address_space(3))) int*>(smem + 4 * kManyTileBytes);   // behind the tiles
+  if (lane == 0) s_lim[wave * 2] = active ? lim_max : 0, s_lim[wave * 2 + 1] = active ? lim_min : INT_MAX;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();   // K(0), V(0), K(1) and the limits
+  int all_max = 0, all_min = INT_MAX;                  // of the work-group
+#pragma unroll
+  for (int w = 0; w < kManyWaves; ++w) all_max = max(all_max, s_lim[w * 2]), all_min = min(all_min, s_lim[w * 2 + 1]);
+  all_max = __builtin_amdgcn_readfirstlane(all_max), all_min = __builtin_amdgcn_readfirstlane(all_min);
+  const int end = min(r.end, all_max), n = (end - r.begin + kManyKeys - 1) / kManyKeys;
+
+  int k_off[8], v_off[4];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) k_off[s] = l32 * kRowBytes + k_chunk_pos(l32, 2 * s + g) * 16;
+  {
+    const int r16 = lane & 15, G = (lane >> 4) & 1, row = g * 4 + (r16 >> 2);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const int dim = db * 32 + G * 16 + 4 * (r16 & 3);
+      v_off[db] = row * kRowBytes + v_chunk_pos(row, dim >> 3) * 16 + (dim & 7) * 2;
+    }
+  }
+  f32x16 o[4], sA, sB, neg_m;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db][i] = 0.f;
+    sA[i] = sB[i] = neg_m[i] = 0.f;
+  }
+  bf16x8 pA[2], pB[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pA[ks][e] = pB[ks][e] = static_cast<__bf16>(0.f);
+  float m_ref = -INFINITY, l_run = 0.f;
+  bool redo_all = false;   // wave-uniform
+
+  // hides what a row does not see of the 32 keys from key0 on; `there`: they have a page
+  auto mask = [&](f32x16& sc, int key0, bool there) {
+    if (key0 + 32 <= lim_min && key0 >= r.lo && there) return;
+    hide(sc, r.lo - key0 - g * 4, there ? lim - key0 - g * 4 : 0);
+  };
+  if (n > 0) {
+    if (active) {  // S_A of tile 0 and the first reference
+      f32x16 zero;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_frag(smem + k_slot(0) + k_off[s]), qf[s], s == 0 ? zero : sA, 0, 0, 0);
+      mask(sA, r.begin, pg >= 0);
+      float mx = sA[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sA[i]);
+      m_ref = wave_half_max(mx) * a.c;
+      if constexpr (!kUnitC) redo_all = __any(far_ref(m_ref));
+      if constexpr (kUnitC) {
+        const float start = m_ref >= kLowestStart ? m_ref : 0.f;
+        redo_all = __any(!(m_ref >= kLowestStart));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sA[i] -= start;
+          neg_m[i] = -start;
+        }
+      }
+    }
+    auto tile = [&](int j, auto parity) {
+      constexpr int u = decltype(parity)::value;
+      constexpr int k_cur = u * kManyTileBytes, k_nxt = (u ^ 1) * kManyTileBytes;
+      constexpr int v_cur = (2 + u) * kManyTileBytes, v_prev = (2 + (u ^ 1)) * kManyTileBytes;
+      const int key0 = r.begin + j * kManyKeys;
+      if (active) {
+        pipeline_phase<kUnitC>(smem + k_cur + 32 * kRowBytes, k_off, smem + v_prev + 32 * kRowBytes, v_off, qf, sB, pB, o, sA, pA, m_ref,
+                               l_run, a.c, neg_m, redo_all);
+        mask(sB, key0 + 32, pg >= 0);
+      }
+      // every wave is past K(j) and V(j-1); K(j+1) and V(j) have landed
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (kPages && ((j + 2) & 63) == 0) keys.fetch(j + 2, r.end);
+      const int pg_after = keys.page(j + 2);
+      if (j + 2 < n) stage(std::false_type{}, j + 2, pg_after, k_cur);
+      if (j + 1 < n) stage(std::true_type{}, j + 1, pg_next, v_prev);
+      if (key0 + kManyKeys > all_min || key0 < r.lo) {
+        // Some row does not see all of this tile, and 0 times what is not finite would reach it: such values are added to
+        // the rows that see them and taken out of the tile.
+        lds_u32x4* mine = reinterpret_cast<lds_u32x4*>(smem + v_cur) + threadIdx.x * 4;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= odd_bf16(mine[i]);
+        if (__syncthreads_or(odd != 0)) {
+          if (active) {
+            const int64_t at = pg >= 0 ? keys.at(key0, pg) : 0;
+            for (int k = max(key0, r.lo); pg >= 0 && k < min(key0 + kManyKeys, r.n_keys); ++k)
+              if (k < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(k - key0) * kD, g);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine[i] = finite_bf16(mine[i]);
+          __syncthreads();
+        }
+      }
+      if (active) {
+        pipeline_phase<kUnitC>(smem + k_nxt, k_off, smem + v_cur, v_off, qf, sA, pA, o, sB, pB, m_ref, l_run, a.c, neg_m, redo_all);
+        mask(sA, key0 + kManyKeys, pg_next >= 0);
+      }
+      pg = pg_next, pg_next = pg_after;
+    };
+    for (int j = 0; j < n; j += 2) {
+      tile(j, std::integral_constant<int, 0>{});
+      if (j + 1 >= n) break;
+      tile(j + 1, std::integral_constant<int, 1>{});
+    }
+    if (active) {  // O += V_B(n-1) P_B(n-1)
+      const lds_u8* v_half = smem + v_slot(n - 1) + 32 * kRowBytes;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const lds_u8* p = v_half + v_off[db] + ks * 16 * kRowBytes;
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(p)));
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(p + 8 * kRowBytes)));
+          bf16x8 vf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vf[e] = lo[e];
+            vf[4 + e] = hi[e];
+          }
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pB[ks], o[db], 0, 0, 0);
+        }
+    }
+  }
+  const float l_tot = wave_half_sum(l_run);
+  __syncthreads();   // every wave has read its last tile; LDS takes the rows
+  if (!active) return;
+  const int rows_w = min(32, n_set - row_first);
+  lds_u8* mine = smem + wave * kManyTileBytes;
+  auto row_to = [&](int row, int* h) {   // token of a row of the wave, and its head
+    const int rh = row_first + row, tk = a.by_rep.of(rh);
+    *h = r.kvh * a.rep + rh - tk * a.rep;
+    return static_cast<int64_t>(r.t0 + tk);
+  };
+  if (a.part_o != nullptr) {   // un-normalised, as fp32 rows
+    const int64_t first = static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v = {o[db][q * 4], o[db][q * 4 + 1], o[db][q * 4 + 2], o[db][q * 4 + 3]};
+        if (!sees) v = f32x4{0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<lds_f32x4*>(mine + l32 * 512 + ((db * 8 + q * 2 + g) ^ l32) * 16) = v;
+      }
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = i * 2 + g;
+      const f32x4 v = *reinterpret_cast<const lds_f32x4*>(mine + row * 512 + l32 * 16);
+      int h;
+      const int64_t t = row_to(min(row, rows_w - 1), &h);
+      if (row < rows_w) *reinterpret_cast<f32x4*>(a.part_o + ((first + h) * a.T + t) * kD + (l32 ^ row) * 4) = v;
+    }
+    if (g == 0 && l32 < rows_w) a.part_ml[(first + head) * a.T + r.t0 + tok] = sees ? make_float2(fmaxf(m_ref, kNothing), l_tot) : make_float2(kNothing, 0.f);
+    return;
+  }
+  const float inv = sees ? 1.f / l_tot : 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      u32x2 out = {pack_bf16x2(o[db][q * 4 + 0] * inv, o[db][q * 4 + 1] * inv), pack_bf16x2(o[db][q * 4 + 2] * inv, o[db][q * 4 + 3] * inv)};
+      if (!sees) out = u32x2{0u, 0u};
+      *reinterpret_cast<lds_u32x2*>(mine + l32 * kRowBytes + k_chunk_pos(l32, db * 4 + q) * 16 + g * 8) = out;
+    }
+  wave_lds_sync();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = i * 4 + (lane >> 4), chunk = k_chunk_pos(row, lane & 15);
+    const u32x4 v = *reinterpret_cast<const lds_u32x4*>(mine + row * kRowBytes + (lane & 15) * 16);
+    int h;
+    const int64_t t = row_to(min(row, rows_w - 1), &h);
+    if (row < rows_w) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.O) + h * a.o_stride + t * kD + chunk * 8) = v;
+  }
+  if (a.lse != nullptr && g == 0 && l32 < rows_w) a.lse[head * static_cast<int64_t>(a.T) + r.t0 + tok] = sees ? lse_of(m_ref, l_tot) : -INFINITY;
+}
+
+// ------------------------------------------------------------------------------------------
+// Between the two: 64 query rows per work-group, a wave for each pair of one of two row groups and one of two key groups, two
+// work-groups per compute unit; the keys are dealt to the key groups in tiles of 32, and the groups' (O, m, l) are merged through LDS.
+//     phase j:  S(j+1), O += V(j-1) P(j-1)  |  P(j)
+// One barrier behind it; then K(j+3) and V(j+1) are fetched into the slots just released.  The longest work-group has half of
+// the products that it has with 128 rows, which is what a call of few work-groups waits for; where there are many, K and V
+// come through L2 twice as often per product.
+// ------------------------------------------------------------------------------------------
+constexpr int kMidWaves = 4, kMidRows = 64;
+constexpr size_t kMidSmem = kMidWaves * (kWaveOBytes + 32 * 8);
+
+template <bool kUnitC, bool kPages>
+__global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a) {
+  constexpr int kR = 2, kG = 2, kS = 2;   // row groups, key groups, slots per operand and key group
+  constexpr int kKeys = 32 * kG, kTile = kKeys * kRowBytes;   // of a phase
+  static_assert(2 * kS * kTile <= kMidWaves * kWaveOBytes, "tiles");
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, g = lane >> 5, rg = wave % kR, kg = wave / kR;
+  const RowSet r = kPages ? page_rows<kMidRows>(a, blockIdx.x, lane) : prompt_rows<kMidRows>(a, blockIdx.x, lane);
+  if (r.idle) return;
+  const int n_set = r.n_tok * a.rep, row_first = (r.tile * kR + rg) * 32;
+  const bool active = row_first < n_set;   // wave-uniform
+  const int rho = min(row_first + l32, n_set - 1);
+  const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
+
+  const uint32_t lds_mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + wave * 4096;
+  KeyTiles<kPages, kKeys> keys(a, r, 0, 1, lane);
+  auto k_slot = [](int t) { return (t & 1) * kTile; };
+  auto v_slot = [](int t) { return (kS + (t & 1)) * kTile; };
+  // a wave's 16 rows of a tile; rows that are nobody's are zeros
+  auto stage = [&](auto is_v, int j, int pg, int slot) {
+    if (pg < 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        reinterpret_cast<lds_u32x4*>(smem + slot + (wave * 4 + i) * 1024)[lane] = u32x4{0u, 0u, 0u, 0u};
+      return;
+    }
+    const int k0 = keys.key_of(j);
+    const uint16_t* base = uniform<kPages>((decltype(is_v)::value ? keys.Vh : keys.Kh) + keys.at(k0, pg));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = (wave * 4 + i) * 4 + (lane >> 4), pos = lane & 15;
+      dma_16B_at(base, keys.offset(k0, row, decltype(is_v)::value ? v_chunk_pos(row, pos) : k_chunk_pos(row, pos)),
+                 __builtin_amdgcn_readfirstlane(lds_mine + slot + i * 1024));
+    }
+  };
+  keys.fetch(0, r.end);
+  int pg = keys.page(0), pg_next = keys.page(1), pg_after = keys.page(2);   // of tiles j, j + 1, j + 2
+  if (r.begin < r.end) {   // the first tiles go out before it is known how many there are
+    stage(std::false_type{}, 0, pg, k_slot(0));
+    stage(std::true_type{}, 0, pg, v_slot(0));
+    if (keys.key_of(1) < r.end) stage(std::false_type{}, 1, pg_next, k_slot(1));
+  }
+  // the slot of V(-1) is read once against zero probabilities: clear it
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<lds_u32x4*>(smem + v_slot(1) + (wave * 4 + i) * 1024)[lane] = u32x4{0u, 0u, 0u, 0u};
+
+  // the wave's queries, as fragments
+  bf16x8 qf[8];
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * kD + g * 8;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
+  }
+  // What the rows see, as in rows_many_kernel.
+  const int lim_true = limit_of(a, r, tok);
+  const bool sees = lim_true > max(r.lo, r.begin);
+  const int lim = sees ? lim_true : INT_MAX;
+  int lim_max = sees ? lim_true : 0, lim_min = lim;
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) {
+    lim_max = max(lim_max, __shfl_xor(lim_max, x));
+    lim_min = min(lim_min, __shfl_xor(lim_min, x));
+  }
+  lim_min = __builtin_amdgcn_readfirstlane(lim_min);   // of the wave
+  auto* s_lim = reinterpret_cast<__attribute__((address_space(3))) int*>(smem + kMidWaves * kWaveOBytes);   // behind the tiles
+  if (lane == 0 && kg == 0) s_lim[rg * 2] = active ? lim_max : 0, s_lim[rg * 2 + 1] = active ? lim_min : INT_MAX;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();   // K(0), V(0), K(1) and the limits
+  int all_max = 0, all_min = INT_MAX;                  // of the work-group
+#pragma unroll
+  for (int w = 0; w < kR; ++w) all_max = max(all_max, s_lim[w * 2]), all_min = min(all_min, s_lim[w * 2 + 1]);
+  all_max = __builtin_amdgcn_readfirstlane(all_max), all_min = __builtin_amdgcn_readfirstlane(all_min);
+  const int end = min(r.end, all_max), n = (end - r.begin + kKeys - 1) / kKeys;
+
+  int k_off[8], v_off[4];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) k_off[s] = (kg * 32 + l32) * kRowBytes + k_chunk_pos(l32, 2 * s + g) * 16;
+  {
+    const int r16 = lane & 15, G = (lane >> 4) & 1, row = g * 4 + (r16 >> 2);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const int dim = db * 32 + G * 16 + 4 * (r16 & 3);
+      v_off[db] = (kg * 32 + row) * kRowBytes + v_chunk_pos(row, dim >> 3) * 16 + (dim & 7) * 2;
+    }
+  }
+  f32x16 o[4], sA, sB, neg_m;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db][i] = 0.f;
+    sA[i] = sB[i] = neg_m[i] = 0.f;
+  }
+  bf16x8 pA[2], pB[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pA[ks][e] = pB[ks][e] = static_cast<__bf16>(0.f);
+  float m_ref = -INFINITY, l_run = 0.f;
+  bool redo_all = false;   // wave-uniform
+
+  // hides what a row does not see of its half of tile j, whose page is pg
+  auto mask = [&](f32x16& sc, int j, int pg) {
+    const int key0 = keys.key_of(j) + kg * 32;
+    if (key0 + 32 <= lim_min && key0 >= r.lo && pg >= 0) return;
+    hide(sc, r.lo - key0 - g * 4, pg >= 0 ? lim - key0 - g * 4 : 0);
+  };
+  if (n > 0) {
+    if (active) {  // scores of tile 0 and the first reference
+      f32x16 zero;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_frag(smem + k_slot(0) + k_off[s]), qf[s], s == 0 ? zero : sA, 0, 0, 0);
+      mask(sA, 0, pg);
+      float mx = sA[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sA[i]);
+      m_ref = wave_half_max(mx) * a.c;
+      if constexpr (!kUnitC) redo_all = __any(far_ref(m_ref));
+      if constexpr (kUnitC) {
+        const float start = m_ref >= kLowestStart ? m_ref : 0.f;
+        redo_all = __any(!(m_ref >= kLowestStart));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sA[i] -= start;
+          neg_m[i] = -start;
+        }
+      }
+    }
+    __syncthreads();               // K(0) has been read by all
+    if (n > 2) stage(std::false_type{}, 2, pg_after, k_slot(2));
+    auto phase = [&](int j, auto parity, const f32x16& s_cur, f32x16& s_nxt, const bf16x8 (&p_mm)[2], bf16x8 (&p_cur)[2]) {
+      constexpr int u = decltype(parity)::value;   // of j
+      constexpr int k_nxt = (u ^ 1) * kTile, v_cur = (kS + u) * kTile, v_prev = (kS + (u ^ 1)) * kTile;
+      if (active) {
+        pipeline_phase<kUnitC>(smem + k_nxt, k_off, smem + v_prev, v_off, qf, s_nxt, p_mm, o, s_cur, p_cur, m_ref, l_run, a.c, neg_m, redo_all);
+        mask(s_nxt, j + 1, pg_next);
+      }
+      // every wave is past K(j+1) and V(j-1); K(j+2) and V(j) have landed
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (kPages && ((j + 3) & 63) == 0) keys.fetch(j + 3, r.end);
+      const int pg_third = keys.page(j + 3);
+      if (j + 3 < n) stage(std::false_type{}, j + 3, pg_third, k_nxt);
+      if (j + 1 < n) stage(std::true_type{}, j + 1, pg_next, v_prev);
+      const int key0 = r.begin + j * kKeys;
+      if (key0 + kKeys > all_min || key0 < r.lo) {
+        // as in rows_many_kernel; a wave adds what is in its half
+        lds_u32x4* mine = reinterpret_cast<lds_u32x4*>(smem + v_cur) + threadIdx.x * 4;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= odd_bf16(mine[i]);
+        if (__syncthreads_or(odd != 0)) {
+          const int k0 = key0 + kg * 32;
+          if (active && pg >= 0) {
+            const uint16_t* rows = keys.Vh + keys.at(key0, pg);
+            for (int k = max(k0, r.lo); k < min(k0 + 32, r.n_keys); ++k)
+              if (k < lim) add_odd(o, rows + static_cast<int64_t>(k - key0) * kD, g);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine[i] = finite_bf16(mine[i]);
+          __syncthreads();
+        }
+      }
+      pg = pg_next, pg_next = pg_after, pg_after = pg_third;
+    };
+    for (int j = 0; j < n; j += 2) {
+      phase(j, std::integral_constant<int, 0>{}, sA, sB, pB, pA);
+      if (j + 1 >= n) break;
+      phase(j + 1, std::integral_constant<int, 1>{}, sB, sA, pA, pB);
+    }
+    if (active) {  // O += V(n-1) P(n-1)
+      const lds_u8* v_last = smem + v_slot(n - 1);
+      const bool odd = (n & 1) != 0;   // the last phase was an even one: its probabilities are pA
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const lds_u8* p = v_last + v_off[db] + ks * 16 * kRowBytes;
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(p)));
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(p + 8 * kRowBytes)));
+          bf16x8 vf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vf[e] = lo[e];
+            vf[4 + e] = hi[e];
+          }
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, odd ? pA[ks] : pB[ks], o[db], 0, 0, 0);
+        }
+    }
+  }
+  float l_tot = wave_half_sum(l_run), m_end = fmaxf(m_ref, kNothing);
+  if (!sees) {
+    l_tot = 0.f, m_end = kNothing;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  }
+  __syncthreads();   // every wave has read its last tile; LDS takes the rows
+  merge_waves<kR, kG>(a, r, smem, o, m_end, l_tot, wave, lane);
+}
+
+}  // namespace pc

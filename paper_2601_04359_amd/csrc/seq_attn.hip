@@ -6,8 +6,7 @@
 #include <numeric>
 #include <vector>
 
-#include "lds_dma.h"
-#include "seq_rows.h"
+#include "rows_bf16.h"
 
 namespace pc {
 namespace {
@@ -213,76 +212,142 @@ __global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a
 
 // ------------------------------------------------------------------------------------------
 // The shares of a row joined: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s with M = max_s m_s, over the shares that
-// have written something, in their order.  A thread has four dims of a row.
+// have written something.  A thread has four dims of a row; kSplit groups of them take the row's shares by turns and add
+// up in LDS (few rows come in many shares, and one after the other they would wait for as many loads).
 // ------------------------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, int kSplit>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
-  constexpr int kLanes = D / 4;
-  const int n = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kSplit), kBatch = 4;
+  __shared__ f32x4 acc_lds[kSplit > 1 ? 256 : 1];
+  __shared__ float l_lds[kSplit > 1 ? 256 / kLanes : 1];
+  const int group = threadIdx.x / kLanes, c = threadIdx.x % kLanes, turn = group % kSplit;
+  const int n = blockIdx.x * kRows + group / kSplit;
   const int Hq = a.by_hkv.d * a.rep;
-  if (n >= Hq * a.n_rows) return;
-  const int head = n / a.n_rows, t = a.row0 + n - head * a.n_rows;
+  const bool there = n < Hq * a.n_rows;
+  const int head = there ? n / a.n_rows : 0, t = a.row0 + (there ? n - head * a.n_rows : 0);
   const int s = seq_of_row(a.seqs, t);
-  if (s < 0) return;
   const bool even = a.seqs.per > 0;
   const int len = max(0, min(a.lens[even ? s : a.seqs.k0[s]], a.max_len));
   const int end = even ? (s + 1) * a.seqs.per : a.seqs.q0[s] + a.seqs.nq[s];
-  const int parts = a.shared_parts + own_parts_of(a, len);
+  const bool none = len - (end - t) + 1 <= 0;
+  const int parts = none ? 0 : a.shared_parts + own_parts_of(a, len);
   const int64_t step = static_cast<int64_t>(Hq) * a.T, at = static_cast<int64_t>(head) * a.T + t;
-  T* out = static_cast<T*>(a.O) + head * a.o_stride + static_cast<int64_t>(t) * D + c * 4;
-  float M = kNothing, L = 0.f;
+  float M = kNothing;
+  for (int p = c; p < parts; p += kLanes) M = fmaxf(M, a.part_ml[p * step + at].x);
+#pragma unroll
+  for (int x = 1; x < kLanes; x *= 2) M = fmaxf(M, __shfl_xor(M, x, kLanes));
+  float L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (len - (end - t) + 1 > 0) {
-    for (int p = 0; p < parts; ++p) M = fmaxf(M, a.part_ml[p * step + at].x);
-    for (int p = 0; p < parts; ++p) {
-      const float2 ml = a.part_ml[p * step + at];
-      const float by = __builtin_amdgcn_exp2f(ml.x - M);
-      L += by * ml.y;
-      acc += by * *reinterpret_cast<const f32x4*>(a.part_o + (p * step + at) * D + c * 4);
+  for (int p0 = turn; p0 < parts; p0 += kBatch * kSplit) {
+    f32x4 v[kBatch];
+    float2 ml[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int64_t from = min(p0 + i * kSplit, parts - 1) * step + at;
+      ml[i] = a.part_ml[from];
+      v[i] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + c * 4);
     }
-    acc *= 1.f / L;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float by = p0 + i * kSplit < parts ? __builtin_amdgcn_exp2f(ml[i].x - M) : 0.f;
+      L += by * ml[i].y;
+      acc += by * v[i];
+    }
   }
-  store4(out, acc);
-  if (a.lse != nullptr && c == 0) a.lse[at] = lse_of(M, L);
+  if constexpr (kSplit > 1) {
+    acc_lds[threadIdx.x] = acc;
+    if (c == 0) l_lds[group] = L;
+    __syncthreads();
+    if (turn != 0) return;
+#pragma unroll
+    for (int i = 1; i < kSplit; ++i) {
+      acc += acc_lds[threadIdx.x + i * kLanes];
+      L += l_lds[group + i];
+    }
+  }
+  if (!there) return;
+  if (!none) acc *= 1.f / L;
+  store4(static_cast<T*>(a.O) + head * a.o_stride + static_cast<int64_t>(t) * D + c * 4, acc);
+  if (a.lse != nullptr && c == 0) a.lse[at] = none ? -INFINITY : lse_of(M, L);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
-// Shares of `keys` keys so that `work_groups` of them become about `wanted`; a share has at least `least` keys.
-int share_of(int keys, int work_groups, int wanted, int least) {
-  const int shares = std::max(1, std::min({wanted / std::max(1, work_groups), keys / least, 64}));
-  return ceil_div(ceil_div(keys, shares), kPageStep) * kPageStep;
-}
+enum Form { kGeneral, kFew, kMid, kMany };
+int rows_of(Form f) { return f == kGeneral ? kGenRows : f == kFew ? kFewRows : f == kMid ? kMidRows : kManyRows; }
 
-// How pc_page_attn cuts a launch's keys.
-struct PagePlan {
-  int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
-  int own_tiles = 0, own_parts = 0, own_keys = kPageStep;
-  int parts() const { return shared_parts + own_parts; }
-  // n_rows tokens in all, own_tiles row tiles over all sequences
-  PagePlan(int Hkv, int rep, int n_rows, int tiles, int rows_per_tile, int n_shared, int max_len) {
-    own_tiles = tiles;
-    if (n_shared > 0) {
-      shared_tiles = ceil_div(n_rows * rep, rows_per_tile);
-      shared_keys = share_of(n_shared, shared_tiles * Hkv, 1024, 256);
-      shared_parts = ceil_div(n_shared, shared_keys);
-    }
-    const int own = max_len - n_shared / kPageStep * kPageStep;
-    if (max_len > n_shared) {
-      own_keys = share_of(own, own_tiles * Hkv, 1024, 256);
-      own_parts = ceil_div(own, own_keys);
-    }
-  }
-};
-
-size_t part_bytes(int parts, int Hq, int T, int D) {
-  return parts <= 1 ? 0 : align_up(static_cast<size_t>(parts) * Hq * T * D * sizeof(float), 256) + static_cast<size_t>(parts) * Hq * T * sizeof(float2);
+// Microseconds that `groups` work-groups of a bf16 form take, `steps` steps in all and `longest` in the one with the most (256
+// keys for kFew, 64 for the others).  Either they fill the chip (what a work-group costs beside its steps, and a step, in time
+// of a compute unit), or the longest is waited for; its steps take longer with a second work-group on its unit.  Fitted to
+// prompts of 40 to 16,384 rows in 8/2, 16/4 and 24/8 heads in all three forms, within 8 % from 1,000 rows on.  Both sides, us:
+//   few | mid    8/2 x 2,048: 23 | 32    16/4 x 1,024: 17 | 20    16/4 x 2,048: 42 | 34    24/8 x 1,024: 24 | 21
+//   mid | many   8/2 x 8,192: 161 | 176  16/4 x 3,000: 53 | 63    16/4 x 4,288: 97 | 99    24/8 x 4,288: 140 | 118
+double estimate(Form f, double groups, double steps, double longest) {
+  const bool shared_unit = groups > 280;
+  if (f == kFew) return std::max(5.0 + 1.75 * longest, 2.5 + (3.6 * groups + 1.25 * steps) / 256);
+  if (f == kMid) return std::max(7.5 + (shared_unit ? 0.84 : 0.75) * longest, 6.0 + (2.9 * groups + 0.549 * steps) / 256);
+  return std::max(7.0 + (shared_unit ? 1.3 : 1.07) * longest, 5.0 + (3.0 * groups + 0.953 * steps) / 256);
 }
+int keys_per_step(Form f) { return f == kFew ? 256 : 64; }
 
 int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
   if (offs == nullptr) return n_seq * ceil_div(T / n_seq * rep, rows);
   int n = 0;
   for (int s = 0; s < n_seq; ++s) n += ceil_div((offs[s + 1] - offs[s]) * rep, rows);
   return n;
+}
+
+// How pc_page_attn cuts the keys of a launch's sequences: a form, and the length of a share.  The common rows and the sequences'
+// own ones are cut alike and go in one launch.  Beside the estimate above there are the bytes of K and V (5 TB/s), and the
+// shares' join: a launch, and the fp32 rows that are written and read (4 TB/s).
+struct PagePlan {
+  Form form = kGeneral;
+  int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
+  int own_tiles = 0, own_parts = 0, own_keys = kPageStep;
+  int parts() const { return shared_parts + own_parts; }
+  PagePlan(int dtype, int D, int Hkv, int rep, int T, const int32_t* offs, int n_seq, int n_shared, int max_len) {
+    const int n_rows = offs != nullptr ? offs[n_seq] - offs[0] : T;
+    const int own = max_len > n_shared ? max_len - n_shared / kPageStep * kPageStep : 0;
+    auto take = [&](Form f, int share) {
+      form = f;
+      shared_tiles = n_shared > 0 ? ceil_div(n_rows * rep, rows_of(f)) : 0;
+      own_tiles = own > 0 ? row_tiles(offs, n_seq, T, rep, rows_of(f)) : 0;
+      shared_keys = own_keys = share;
+      shared_parts = ceil_div(n_shared, share);
+      own_parts = ceil_div(own, share);
+    };
+    const int longest = std::max(n_shared, own);
+    if (dtype != PC_BF16 || D != kD) {
+      take(kGeneral, kPageStep);
+      const int tiles = std::max(1, shared_tiles + own_tiles) * Hkv;
+      const int shares = std::max(1, std::min({1024 / tiles, longest / 256, 64}));
+      take(kGeneral, ceil_div(ceil_div(longest, shares), kPageStep) * kPageStep);
+      return;
+    }
+    const double bytes_us = (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5e6;
+    double best = 1e30;
+    Form best_form = kFew;
+    int best_share = kPageStep;
+    for (Form f : {kFew, kMid, kMany}) {
+      const int step = keys_per_step(f);
+      for (int share = 256;; share = std::max(share + 64, share * 5 / 4 / kPageStep * kPageStep)) {
+        share = std::min(share, ceil_div(longest, kPageStep) * kPageStep);
+        take(f, share);
+        if (parts() <= 96) {
+          const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * own_parts);
+          const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
+          const double join = parts() > 1 ? 3.0 + static_cast<double>(n_rows) * rep * Hkv * parts() * 1040.0 / 4e6 : 0.0;
+          const double cost = std::max(estimate(f, groups, steps, ceil_div(share, step)), 4.0 + bytes_us) + join;
+          if (cost < best) best = cost, best_form = f, best_share = share;
+        }
+        if (share >= longest) break;
+      }
+    }
+    take(best_form, best_share);
+  }
+};
+
+size_t part_bytes(int parts, int Hq, int T, int D) {
+  return parts <= 1 ? 0 : align_up(static_cast<size_t>(parts) * Hq * T * D * sizeof(float), 256) + static_cast<size_t>(parts) * Hq * T * sizeof(float2);
 }
 
 // Calls f(first, count) for the launches that a call's sequences are dealt to; f returns a status.
@@ -308,23 +373,28 @@ int check_attn(const char* who, int dtype, int Hq, int Hkv, int D, float scale) 
   return PC_OK;
 }
 
-template <template <typename, int> class Launch>
-void by_type(int dtype, int D, const RowsArgs& a, dim3 grid, hipStream_t s) {
-  if (dtype == PC_BF16) D == 128 ? Launch<uint16_t, 128>::go(a, grid, s) : Launch<uint16_t, 64>::go(a, grid, s);
-  else D == 128 ? Launch<float, 128>::go(a, grid, s) : Launch<float, 64>::go(a, grid, s);
+template <bool kPages>
+int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a, int blocks, hipStream_t s) {
+  if (form == kGeneral) {
+    auto* kernel = dtype == PC_BF16 ? (D == 128 ? rows_general_kernel<uint16_t, 128, kPages> : rows_general_kernel<uint16_t, 64, kPages>)
+                                    : (D == 128 ? rows_general_kernel<float, 128, kPages> : rows_general_kernel<float, 64, kPages>);
+    kernel<<<blocks, kGenWaves * 64, 0, s>>>(a);
+  } else if (form == kFew) {
+    static std::atomic<uint64_t> ok;
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(rows_few_kernel<kPages>), kFewSmem, ok, who)) return rc;
+    rows_few_kernel<kPages><<<blocks, kFewWaves * 64, kFewSmem, s>>>(a);
+  } else {
+    static std::atomic<uint64_t> ok[4];
+    const bool unit_c = a.c == 1.0f, many = form == kMany;
+    auto* kernel = many ? (unit_c ? rows_many_kernel<true, kPages> : rows_many_kernel<false, kPages>)
+                        : (unit_c ? rows_mid_kernel<true, kPages> : rows_mid_kernel<false, kPages>);
+    const size_t bytes = many ? kManySmem : kMidSmem;
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[many * 2 + unit_c], who)) return rc;
+    kernel<<<blocks, (many ? kManyWaves : kMidWaves) * 64, bytes, s>>>(a);
+  }
+  PC_CHECK_LAUNCH(who);
+  return PC_OK;
 }
-template <typename T, int D>
-struct GeneralPrompt {
-  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_general_kernel<T, D, false><<<grid, kGenWaves * 64, 0, s>>>(a); }
-};
-template <typename T, int D>
-struct GeneralPages {
-  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_general_kernel<T, D, true><<<grid, kGenWaves * 64, 0, s>>>(a); }
-};
-template <typename T, int D>
-struct Join {
-  static void go(const RowsArgs& a, dim3 grid, hipStream_t s) { rows_join_kernel<T, D><<<grid, 256, 0, s>>>(a); }
-};
 
 }  // namespace
 }  // namespace pc
@@ -379,16 +449,33 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
   for (size_t s0 = 0; s0 < seqs.size(); s0 += kSeqs) {
     const int n = static_cast<int>(std::min<size_t>(kSeqs, seqs.size() - s0));
     a.seqs.n = n, a.seqs.per = 0;
+    // the form with the lowest estimate
+    Form form = kGeneral;
+    double best = 1e30;
+    for (Form f : {kFew, kMid, kMany}) {
+      if (dtype != PC_BF16 || D != kD) break;
+      double groups = 0, steps = 0, longest = 0;
+      for (int s = 0; s < n; ++s) {
+        const Seq& q = seqs[s0 + s];
+        const double tiles = ceil_div(q.nq * rep, rows_of(f)), last = std::max(0, q.nk), first = std::max(0.0, last - q.nq);
+        groups += tiles * Hkv;
+        steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
+        longest = std::max(longest, std::ceil(last / keys_per_step(f)));
+      }
+      const double cost = estimate(f, groups, steps, longest);
+      if (cost < best) best = cost, form = f;
+    }
+    const int rows = rows_of(form);
     a.n_tiles = 0, a.max_level = 0;
     for (int s = 0; s < n; ++s) {
       const Seq& q = seqs[s0 + s];
       a.seqs.q0[s] = q.q0, a.seqs.nq[s] = q.nq, a.seqs.k0[s] = q.k0, a.seqs.nk[s] = q.nk;
-      const int tiles = ceil_div(q.nq * rep, kGenRows);
+      const int tiles = ceil_div(q.nq * rep, rows);
       a.n_tiles += tiles;
-      a.max_level = std::max(a.max_level, static_cast<int>(static_cast<int64_t>(std::max(0, q.nk - q.nq)) * rep / kGenRows) + tiles);
+      a.max_level = std::max(a.max_level, static_cast<int>(static_cast<int64_t>(std::max(0, q.nk - q.nq)) * rep / rows) + tiles);
     }
-    by_type<GeneralPrompt>(dtype, D, a, dim3(a.n_tiles * Hkv), st);
-    PC_CHECK_LAUNCH(who);
+    a.fold = form == kMany || form == kMid ? std::max(1, 256 / Hkv) : 0;
+    if (int rc = launch_rows<false>(who, form, dtype, D, a, a.n_tiles * Hkv, st)) return rc;
   }
   return PC_OK;
 }
@@ -400,7 +487,7 @@ extern "C" size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T
   size_t most = 0;
   each_launch(offs, n_seq, [&](int s0, int n) {
     const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
-    const PagePlan plan(Hkv, Hq / Hkv, o != nullptr ? o[n] - o[0] : T, row_tiles(o, n, T, Hq / Hkv, kGenRows), kGenRows, n_shared, max_len);
+    const PagePlan plan(dtype, D, Hkv, Hq / Hkv, T, o, n, std::min(n_shared, max_len), max_len);
     most = std::max(most, part_bytes(plan.parts(), Hq, T, D));
     return PC_OK;
   });
@@ -450,14 +537,12 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     a.row0 = o != nullptr ? o[0] : 0, a.n_rows = o != nullptr ? o[n] - o[0] : T;
     if (a.n_rows == 0) return PC_OK;
     a.seqs.n = n, a.seqs.per = o != nullptr ? 0 : T / n;
-    if (o == nullptr) {
-      a.seqs.by_per = Divisor(a.seqs.per);
-      a.tiles_per_seq = ceil_div(a.seqs.per * rep, kGenRows), a.by_tiles_per_seq = Divisor(a.tiles_per_seq);
-    } else {
+    if (o == nullptr) a.seqs.by_per = Divisor(a.seqs.per);
+    else
       for (int s = 0; s < n; ++s) a.seqs.q0[s] = o[s], a.seqs.nq[s] = o[s + 1] - o[s], a.seqs.k0[s] = s0 + s;
-    }
-    const PagePlan plan(Hkv, rep, a.n_rows, row_tiles(o, n, T, rep, kGenRows), kGenRows, n_shared, max_len);
-    a.n_tiles = plan.own_tiles, a.by_tiles = Divisor(plan.own_tiles);
+    const PagePlan plan(dtype, D, Hkv, rep, T, o, n, n_shared, max_len);
+    a.n_tiles = plan.own_tiles, a.by_tiles = Divisor(std::max(1, plan.own_tiles));
+    a.tiles_per_seq = std::max(1, ceil_div(a.seqs.per * rep, rows_of(plan.form))), a.by_tiles_per_seq = Divisor(a.tiles_per_seq);
     a.shared_tiles = plan.shared_tiles, a.shared_parts = plan.shared_parts, a.shared_keys = plan.shared_keys;
     a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles));
     a.own_parts = plan.own_parts, a.own_keys = plan.own_keys;
@@ -467,10 +552,17 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
       a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) +
                                             align_up(static_cast<size_t>(plan.parts()) * Hq * T * D * sizeof(float), 256));
     }
-    by_type<GeneralPages>(dtype, D, a, dim3((plan.shared_tiles * plan.shared_parts + plan.own_tiles * plan.own_parts) * Hkv), st);
-    PC_CHECK_LAUNCH(who);
+    const int common = plan.shared_tiles * plan.shared_parts, own = plan.own_tiles * plan.own_parts;
+    a.n_common = common;
+    if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, (common + own) * Hkv, st)) return rc;
     if (plan.parts() <= 1) return PC_OK;
-    by_type<Join>(dtype, D, a, dim3(ceil_div(Hq * a.n_rows, 256 / (D / 4))), st);
+    // one row per work-group where there are many shares of it, else eight (sixteen at D = 64)
+    const bool many = plan.parts() > 6;
+    auto* join = dtype == PC_BF16 ? (D == 128 ? (many ? rows_join_kernel<uint16_t, 128, 8> : rows_join_kernel<uint16_t, 128, 1>)
+                                              : (many ? rows_join_kernel<uint16_t, 64, 8> : rows_join_kernel<uint16_t, 64, 1>))
+                                  : (D == 128 ? (many ? rows_join_kernel<float, 128, 8> : rows_join_kernel<float, 128, 1>)
+                                              : (many ? rows_join_kernel<float, 64, 8> : rows_join_kernel<float, 64, 1>));
+    join<<<ceil_div(Hq * a.n_rows, 256 / (D / 4) / (many ? 8 : 1)), 256, 0, st>>>(a);
     PC_CHECK_LAUNCH(who);
     return PC_OK;
   });

@@ -27,10 +27,12 @@ struct RowsArgs {
   int row0, n_rows;           // the launch's part of them
   Divisor by_rep, by_hkv;
   SeqTable seqs;
+  int fold;                   // pc_prompt_attn: row tiles (of a KV head) that the chip's compute units get first; 0: no second ones
   int max_level;              // pc_prompt_attn, several sequences: above every tile's level
   int tiles_per_seq, n_tiles; // row tiles of one KV head: of a sequence (where all have as many), of all
   Divisor by_tiles_per_seq, by_tiles;
   // shares of the keys
+  int n_common;               // work-groups of this launch that have common rows, per KV head
   int shared_tiles, shared_parts, shared_keys;   // row tiles over the common rows; their shares, keys of each
   Divisor by_shared_tiles;
   int own_parts, own_keys;                       // shares of the rows behind them, keys of each
@@ -67,12 +69,14 @@ __device__ __forceinline__ int limit_of(const RowsArgs& a, const RowSet& r, int 
 // pc_prompt_attn: work-groups in the order of what they have to do, longest first (a causal tile's work goes with where
 // it ends, and the chip is filled from the front).  A tile's level is the number of row tiles' worth of keys in front of its
 // own; tiles of one level follow each other, KV heads fastest, so that with 1, 2, 4, 8 or more heads an XCD's
-// work-groups read few of them.
+// work-groups read few of them.  Where two work-groups share a compute unit, the second 256 come shortest first: unit i
+// gets number i and number 256 + i, and in plain order the first units would have the longest of both.
 template <int R>
 __device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int block, int lane) {
   RowSet r = {};
-  const int u = a.by_hkv.of(block);
+  int u = a.by_hkv.of(block);
   r.kvh = block - u * a.by_hkv.d;
+  if (u >= a.fold && u < 2 * a.fold) u = min(2 * a.fold, a.n_tiles) - 1 - (u - a.fold);
   int s = 0;
   if (a.seqs.n == 1) {
     r.tile = a.n_tiles - 1 - u;
@@ -108,8 +112,7 @@ __device__ __forceinline__ RowSet page_rows(const RowsArgs& a, int block, int la
   RowSet r = {};
   int u = a.by_hkv.of(block);
   r.kvh = block - u * a.by_hkv.d;
-  const int n_common = a.shared_tiles * a.shared_parts;
-  if (u < n_common) {
+  if (u < a.n_common) {
     r.common = true;
     r.part = a.by_shared_tiles.of(u);
     r.tile = u - r.part * a.shared_tiles;
@@ -119,7 +122,7 @@ __device__ __forceinline__ RowSet page_rows(const RowsArgs& a, int block, int la
     r.pages = a.shared;
     return r;
   }
-  u -= n_common;
+  u -= a.n_common;
   const int share = a.by_tiles.of(u);
   u -= share * a.n_tiles;
   int number, nq;
