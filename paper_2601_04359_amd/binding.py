@@ -166,6 +166,8 @@ def _bind_native(L) -> None:
         _marshal.bind_q4(*[C.cast(f, C.c_void_p).value for f in (L.pc_q4_store, L.pc_q4_load, L.pc_q4_attn,
                                                                  L.pc_q4_attn_workspace_bytes, L.pc_evict, L.pc_q4_evict,
                                                                  L.pc_evict_workspace_bytes)])
+        _marshal.bind_seq(*[C.cast(f, C.c_void_p).value for f in (L.pc_prompt_attn, L.pc_page_store, L.pc_page_attn,
+                                                                  L.pc_page_attn_workspace_bytes)])
         _NATIVE = _marshal
     except (ImportError, AttributeError) as e:
         _NATIVE = False
@@ -870,6 +872,11 @@ def pc_prompt_attn(Q, K, V, scale: float, offs_q, offs_k=None, O=None, lse=None)
     offsets [n_seq + 1] of the sequences in Q's rows; offs_k: in K's and V's (None: the same).  Row i of nq sees keys
     0 .. nk - nq + i; a row that sees none gets O = 0 and lse (fp32 [Hq][Tq]) = -inf.  Rows of no sequence are left as they
     were."""
+    if _NATIVE and O is not None:
+        r = _NATIVE.prompt_attn(Q, K, V, scale, offs_q, offs_k, O, lse)
+        if r is not None:
+            _check(r)
+            return O
     Hq, Tq, D = _heads_of_rows(Q, "Q", None, None, None)
     Hkv, Tk, _ = _heads_of_rows(K, "K", None, None, D, like=Q)
     _heads_of_rows(V, "V", Hkv, Tk, D, like=Q)
@@ -929,6 +936,10 @@ def pc_page_store(K, V, pages, table, lens, offs=None, pos=None, sections=None, 
     int32 [n_seq], the new rows counted).  offs: host offsets [n_seq + 1] of the sequences in the T rows; None: T / n_seq each.
     pos (int32 [T][3]) and sections: keys are turned as pc_rope3d turns them; K_out (may be K): the keys as stored;
     Q [Hq][T][D] -> Q_out (may be Q): queries turned and multiplied by out_scale.  Rows without a page are not stored."""
+    if _NATIVE:
+        r = _NATIVE.page_store(K, V, pages, table, lens, offs, pos, sections, base, K_out, Q, Q_out, out_scale)
+        if r is not None:
+            return _check(r)
     import torch
     Hkv, T, D = _heads_of_rows(K, "K", None, None, None)
     _heads_of_rows(V, "V", Hkv, T, D, like=K)
@@ -968,6 +979,11 @@ def pc_page_attn(Q, pages, table, lens, max_len: int, scale: float, offs=None, s
     0 .. lens[s] - nq + i.  pages, table, lens, offs as in pc_page_store; max_len bounds lens.  shared (int32 [pages]),
     n_shared: the first n_shared rows of all sequences are those of these pages, read once for all.  lse fp32 [Hq][T].  ws: not to be
     shared by calls that may overlap; None: one of the call's own, from torch's allocator."""
+    if _NATIVE and O is not None:
+        r = _NATIVE.page_attn(Q, pages, table, lens, max_len, scale, offs, shared, n_shared, O, lse, ws)
+        if r is not None:
+            _check(r)
+            return O
     import torch
     Hq, T, D = _heads_of_rows(Q, "Q", None, None, None)
     p, Hkv = _pages_struct(pages, Q)

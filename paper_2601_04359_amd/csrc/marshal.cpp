@@ -42,6 +42,12 @@ struct Q4Library {
   decltype(&pc_q4_evict) q4_evict;
   decltype(&pc_evict_workspace_bytes) evict_bytes;
 } q4 = {};
+struct SeqLibrary {
+  decltype(&pc_prompt_attn) prompt;
+  decltype(&pc_page_store) store;
+  decltype(&pc_page_attn) attn;
+  decltype(&pc_page_attn_workspace_bytes) attn_bytes;
+} seq = {};
 PyObject* current_device = nullptr;   // torch's raw queries of the current device and of its stream
 PyObject* raw_stream = nullptr;
 
@@ -591,6 +597,172 @@ PyObject* q4_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // cach
   END_HANDLE_TH_ERRORS
 }
 
+// ---- several sequences at once: prompts, and a cache in pages -----------------------------------------
+PyObject* bind_seq(PyObject*, PyObject* const* a, Py_ssize_t n) {   // 4 addresses
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "bind_seq: 4 arguments");
+    return nullptr;
+  }
+  void* p[4];
+  for (int i = 0; i < 4; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  if (PyErr_Occurred()) return nullptr;
+  seq = {reinterpret_cast<decltype(&pc_prompt_attn)>(p[0]), reinterpret_cast<decltype(&pc_page_store)>(p[1]),
+         reinterpret_cast<decltype(&pc_page_attn)>(p[2]), reinterpret_cast<decltype(&pc_page_attn_workspace_bytes)>(p[3])};
+  Py_RETURN_NONE;
+}
+bool ready_seq() { return ready() && seq.prompt != nullptr; }
+
+// [H][rows][D] with dense rows, of the type of `like`; H < 0: any number
+bool heads_of_rows(const at::Tensor* t, int64_t H, int64_t rows, int64_t D, const at::Tensor& like) {
+  return t && rows_follow(*t) && (H < 0 || t->size(0) == H) && t->size(1) == rows && t->size(2) == D &&
+         t->scalar_type() == like.scalar_type();
+}
+bool lse_fits(const at::Tensor* lse, const at::Tensor& Q) {
+  return !lse || (lse->scalar_type() == at::kFloat && lse->dim() == 2 && lse->size(0) == Q.size(0) && lse->size(1) == Q.size(1) &&
+                  lse->is_contiguous());
+}
+// host offsets [n_seq + 1]; n_seq < 0: any number
+bool as_offsets(PyObject* o, int64_t n_seq, std::vector<int32_t>& v) {
+  if (!is_table(o)) return false;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+  if (n < 1 || (n_seq >= 0 && n != n_seq + 1) || !as_ints(o, n, v)) return false;
+  for (int32_t x : v)
+    if (x < 0) return false;
+  return true;
+}
+// What binding.py's _pages_struct and _sequences accept.
+struct Sequences {
+  pc_pages p;
+  const at::Tensor *K = nullptr, *V = nullptr, *table = nullptr, *lens = nullptr;
+  int Hkv, n_seq, width;
+  std::vector<int32_t> offs;
+  bool uneven;
+  bool from(PyObject* pages, PyObject* t, PyObject* l, PyObject* o, const at::Tensor& like) {
+    if (!PyTuple_CheckExact(pages) || PyTuple_GET_SIZE(pages) != 2) return false;
+    K = plain(PyTuple_GET_ITEM(pages, 0)), V = plain(PyTuple_GET_ITEM(pages, 1)), table = plain(t), lens = plain(l);
+    if (!K || !V || !table || !lens || !rows_dense(*K, 4) || !rows_dense(*V, 4) || K->sizes() != V->sizes() ||
+        K->strides() != V->strides() || K->scalar_type() != like.scalar_type() || V->scalar_type() != like.scalar_type() ||
+        K->size(3) != like.size(2))
+      return false;
+    if (table->scalar_type() != at::kInt || table->dim() != 2 || table->size(1) < 1 || (table->size(1) > 1 && table->stride(1) != 1) ||
+        lens->scalar_type() != at::kInt || lens->dim() != 1 || lens->size(0) != table->size(0) || !lens->is_contiguous())
+      return false;
+    int n_pages, rows;
+    if (!size_as_int(K->size(0), &n_pages) || !size_as_int(K->size(1), &Hkv) || !size_as_int(K->size(2), &rows) ||
+        !size_as_int(table->size(0), &n_seq) || !size_as_int(table->size(1), &width) || Hkv < 1)
+      return false;
+    p = {K->mutable_data_ptr(), V->mutable_data_ptr(), K->stride(0), K->stride(1), n_pages, rows};
+    uneven = o != Py_None;
+    return !uneven || as_offsets(o, n_seq, offs);
+  }
+  bool on(const Place& at) const { return at.holds({K, V, table, lens}); }
+  const int32_t* offsets() const { return uneven ? offs.data() : nullptr; }
+  const int32_t* table_at() const { return static_cast<int32_t*>(table->mutable_data_ptr()); }
+  const int32_t* lens_at() const { return static_cast<int32_t*>(lens->mutable_data_ptr()); }
+};
+
+PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {   // Q, K, V, scale, offs_q, offs_k, O, lse
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 8 && ready_seq());
+  const at::Tensor *Q = plain(a[0]), *K = plain(a[1]), *V = plain(a[2]), *O = plain(a[6]), *lse = nullptr;
+  double scale;
+  PLAIN_OR_NONE(Q && K && Q->dim() == 3 && K->dim() == 3 && as_double(a[3], &scale) && optional(a[7], &lse));
+  const int64_t d = Q->size(2);
+  int Hq, Hkv, Tq, Tk, D;
+  PLAIN_OR_NONE(heads_of_rows(Q, -1, Q->size(1), d, *Q) && heads_of_rows(K, -1, K->size(1), d, *Q) &&
+                heads_of_rows(V, K->size(0), K->size(1), d, *Q) && heads_of_rows(O, Q->size(0), Q->size(1), d, *Q) && lse_fits(lse, *Q) &&
+                size_as_int(Q->size(0), &Hq) && size_as_int(K->size(0), &Hkv) && size_as_int(Q->size(1), &Tq) &&
+                size_as_int(K->size(1), &Tk) && size_as_int(d, &D));
+  std::vector<int32_t> oq, ok;
+  PLAIN_OR_NONE(as_offsets(a[4], -1, oq) && (a[5] == Py_None || as_offsets(a[5], static_cast<int64_t>(oq.size()) - 1, ok)));
+  const int dt = dtype_code(*Q);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && at.holds({Q, K, V, O, lse}));
+  void *qp = pointer(Q), *kp = pointer(K), *vp = pointer(V), *op = pointer(O);
+  auto* lp = static_cast<float*>(pointer(lse));
+  const int64_t qs = Q->stride(0), ks = K->stride(0), vs = V->stride(0), os = O->stride(0);
+  return PyLong_FromLong(unlocked([&] {
+    return seq.prompt(qp, kp, vp, dt, Hq, Hkv, Tq, Tk, D, qs, ks, vs, os, static_cast<float>(scale), oq.data(),
+                      ok.empty() ? nullptr : ok.data(), static_cast<int>(oq.size()) - 1, op, lp, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// K, V, pages, table, lens, offs, pos, sections, base, K_out, Q, Q_out, out_scale
+PyObject* page_store(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 13 && ready_seq());
+  const at::Tensor *K = plain(a[0]), *V = plain(a[1]), *pos = nullptr, *Ko = nullptr, *Q = nullptr, *Qo = nullptr;
+  Sequences s;
+  double base, out_scale;
+  PLAIN_OR_NONE(K && K->dim() == 3 && s.from(a[2], a[3], a[4], a[5], *K) && optional(a[6], &pos) && as_double(a[8], &base) &&
+                optional(a[9], &Ko) && optional(a[10], &Q) && optional(a[11], &Qo) && as_double(a[12], &out_scale));
+  const int64_t t = K->size(1), d = K->size(2);
+  int T, D, Hq = 0;
+  PLAIN_OR_NONE(heads_of_rows(K, s.Hkv, t, d, *K) && heads_of_rows(V, s.Hkv, t, d, *K) && (!Ko || heads_of_rows(Ko, s.Hkv, t, d, *K)) &&
+                !Q == !Qo && (!Q || (heads_of_rows(Q, -1, t, d, *K) && heads_of_rows(Qo, Q->size(0), t, d, *K) && size_as_int(Q->size(0), &Hq))) &&
+                size_as_int(t, &T) && size_as_int(d, &D) && !pos == (a[7] == Py_None));
+  int32_t sec[3] = {0, 0, 0};
+  if (pos) {
+    PLAIN_OR_NONE(pos->scalar_type() == at::kInt && pos->dim() == 2 && pos->size(0) == t && pos->size(1) == 3 && pos->is_contiguous() &&
+                  is_table(a[7]) && PySequence_Fast_GET_SIZE(a[7]) >= 3);
+    for (int i = 0; i < 3; ++i) PLAIN_OR_NONE(as_int(PySequence_Fast_GET_ITEM(a[7], i), &sec[i]));
+  }
+  const int dt = dtype_code(*K);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && s.on(at) && at.holds({K, V, pos, Ko, Q, Qo}));
+  void *kp = pointer(K), *vp = pointer(V), *kop = pointer(Ko), *qp = pointer(Q), *qop = pointer(Qo);
+  auto* pp = static_cast<int32_t*>(pointer(pos));
+  const int64_t ks = K->stride(0), vs = V->stride(0), kos = Ko ? Ko->stride(0) : 0, qs = Q ? Q->stride(0) : 0, qos = Q ? Qo->stride(0) : 0;
+  const int64_t ts = s.table->stride(0);
+  const int32_t *tp = s.table_at(), *lp = s.lens_at();
+  return PyLong_FromLong(unlocked([&] {
+    return seq.store(kp, vp, dt, s.Hkv, T, D, ks, vs, &s.p, tp, s.width, ts, lp, s.offsets(), s.n_seq, pp, sec[0], sec[1], sec[2], base,
+                     kop, kos, qp, qop, Hq, qs, qos, out_scale, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// Q, pages, table, lens, max_len, scale, offs, shared, n_shared, O, lse, ws
+PyObject* page_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  PLAIN_OR_NONE(n_args == 12 && ready_seq());
+  const at::Tensor *Q = plain(a[0]), *O = plain(a[9]), *shared = nullptr, *lse = nullptr, *ws = nullptr;
+  Sequences s;
+  int32_t max_len, n_shared;
+  double scale;
+  PLAIN_OR_NONE(Q && Q->dim() == 3 && s.from(a[1], a[2], a[3], a[6], *Q) && as_int(a[4], &max_len) && as_double(a[5], &scale) &&
+                optional(a[7], &shared) && as_int(a[8], &n_shared) && optional(a[10], &lse) && optional(a[11], &ws));
+  int Hq, T, D;
+  PLAIN_OR_NONE(heads_of_rows(Q, -1, Q->size(1), Q->size(2), *Q) && heads_of_rows(O, Q->size(0), Q->size(1), Q->size(2), *Q) &&
+                lse_fits(lse, *Q) && size_as_int(Q->size(0), &Hq) && size_as_int(Q->size(1), &T) && size_as_int(Q->size(2), &D) &&
+                Hq % s.Hkv == 0 && (shared == nullptr) == (n_shared == 0));
+  PLAIN_OR_NONE(!shared || (shared->scalar_type() == at::kInt && shared->dim() == 1 && shared->is_contiguous() &&
+                            shared->size(0) * s.p.page_rows >= n_shared));
+  const int dt = dtype_code(*Q);
+  Place at;
+  if (!at.find()) return nullptr;
+  PLAIN_OR_NONE(dt >= 0 && s.on(at) && at.holds({Q, O, shared, lse, ws}));
+  at::Tensor own;
+  if (!ws && T > 0 && s.n_seq > 0) {
+    const size_t bytes = seq.attn_bytes(dt, Hq, s.Hkv, T, D, s.offsets(), s.n_seq, max_len, n_shared);
+    if (bytes) ws = &(own = make_workspace(bytes, *Q));
+  }
+  void *qp = pointer(Q), *op = pointer(O), *wp = pointer(ws);
+  auto* lp = static_cast<float*>(pointer(lse));
+  auto* sp = static_cast<int32_t*>(pointer(shared));
+  const int64_t qs = Q->stride(0), os = O->stride(0), ts = s.table->stride(0);
+  const size_t wn = ws ? ws->nbytes() : 0;
+  const int32_t *tp = s.table_at(), *np = s.lens_at();
+  return PyLong_FromLong(unlocked([&] {
+    return seq.attn(qp, &s.p, dt, Hq, s.Hkv, T, D, qs, os, static_cast<float>(scale), tp, s.width, ts, np, s.offsets(), s.n_seq, max_len,
+                    sp, n_shared, op, lp, wp, wn, at.stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
 // Rows start .. start + n - 1 of three caches as views: K, V, pos, dim, start, n
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
@@ -672,7 +844,8 @@ PyObject* prunable_span(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 PyMethodDef methods[] = {ENTRY(bind),       ENTRY(rope3d),      ENTRY(score),  ENTRY(compact),
                          ENTRY(compact_batch), ENTRY(frame_attn), ENTRY(rows), ENTRY(budget), ENTRY(segment_budgets),
                          ENTRY(past_frames), ENTRY(prunable_span), ENTRY(bind_q4), ENTRY(q4_store), ENTRY(q4_load),
-                         ENTRY(q4_attn), ENTRY(evict), ENTRY(q4_evict), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(q4_attn), ENTRY(evict), ENTRY(q4_evict), ENTRY(bind_seq),
+                         ENTRY(prompt_attn), ENTRY(page_store), ENTRY(page_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -277,16 +277,23 @@ int rows_of(Form f) { return f == kGeneral ? kGenRows : f == kFew ? kFewRows : f
 
 // Microseconds that `groups` work-groups of a bf16 form take, `steps` steps in all and `longest` in the one with the most (256
 // keys for kFew, 64 for the others).  Either they fill the chip (what a work-group costs beside its steps, and a step, in time
-// of a compute unit), or the longest is waited for; its steps take longer with a second work-group on its unit.  Fitted to
-// prompts of 40 to 16,384 rows in 8/2, 16/4 and 24/8 heads in all three forms, within 8 % from 1,000 rows on.  Both sides, us:
+// of a compute unit), or the longest is waited for; its steps take longer with a second work-group on its unit (`paired`).
+struct Cost {
+  double alone, per_step, paired, start, per_group, step;
+  double operator()(double groups, double steps, double longest) const {
+    return std::max(alone + (groups > 280 ? paired : per_step) * longest, start + (per_group * groups + step * steps) / 256);
+  }
+};
+// Prompts: fitted to 40 to 16,384 rows in 8/2, 16/4 and 24/8 heads in all three forms, within 8 % from 1,000 rows on.  Both
+// sides, us:
 //   few | mid    8/2 x 2,048: 23 | 32    16/4 x 1,024: 17 | 20    16/4 x 2,048: 42 | 34    24/8 x 1,024: 24 | 21
 //   mid | many   8/2 x 8,192: 161 | 176  16/4 x 3,000: 53 | 63    16/4 x 4,288: 97 | 99    24/8 x 4,288: 140 | 118
-double estimate(Form f, double groups, double steps, double longest) {
-  const bool shared_unit = groups > 280;
-  if (f == kFew) return std::max(5.0 + 1.75 * longest, 2.5 + (3.6 * groups + 1.25 * steps) / 256);
-  if (f == kMid) return std::max(7.5 + (shared_unit ? 0.84 : 0.75) * longest, 6.0 + (2.9 * groups + 0.549 * steps) / 256);
-  return std::max(7.0 + (shared_unit ? 1.3 : 1.07) * longest, 5.0 + (3.0 * groups + 0.953 * steps) / 256);
-}
+constexpr Cost kPromptCost[3] = {{5.0, 1.75, 1.75, 2.5, 3.6, 1.25}, {7.5, 0.75, 0.84, 6.0, 2.9, 0.549}, {7.0, 1.07, 1.3, 5.0, 3.0, 0.953}};
+// Pages: fitted to 34 shapes (1 to 256 sequences of 1 to 1,000 new rows, up to 41,800 common rows and 10,000 own ones) in all
+// three forms and up to twelve lengths of a share; the choice is 5 % off the best of them at the mean.  Both sides, 16/4 heads,
+// 41,800 common rows, us:
+//   few | mid | many   8 tokens: 23 | 25 | 27   16: 35 | 28 | 31   64: 54 | 52 | 52   256: 161 | 139 | 132
+constexpr Cost kPagesCost[3] = {{3.9, 1.58, 1.58, 2.65, 5.3, 1.48}, {4.9, 1.0, 1.0, 8.0, 2.0, 0.58}, {4.8, 1.44, 1.44, 9.8, 0.1, 0.993}};
 int keys_per_step(Form f) { return f == kFew ? 256 : 64; }
 
 int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
@@ -297,8 +304,8 @@ int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
 }
 
 // How pc_page_attn cuts the keys of a launch's sequences: a form, and the length of a share.  The common rows and the sequences'
-// own ones are cut alike and go in one launch.  Beside the estimate above there are the bytes of K and V (5 TB/s), and the
-// shares' join: a launch, and the fp32 rows that are written and read (4 TB/s).
+// own ones are cut alike and go in one launch.  Beside the costs above there are the bytes of K and V (5.5 TB/s), and the
+// shares' join: a launch, and the fp32 rows that are written and read (4.3 TB/s).
 struct PagePlan {
   Form form = kGeneral;
   int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
@@ -323,7 +330,7 @@ struct PagePlan {
       take(kGeneral, ceil_div(ceil_div(longest, shares), kPageStep) * kPageStep);
       return;
     }
-    const double bytes_us = (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5e6;
+    const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5.5e6;
     double best = 1e30;
     Form best_form = kFew;
     int best_share = kPageStep;
@@ -335,8 +342,8 @@ struct PagePlan {
         if (parts() <= 96) {
           const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * own_parts);
           const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
-          const double join = parts() > 1 ? 3.0 + static_cast<double>(n_rows) * rep * Hkv * parts() * 1040.0 / 4e6 : 0.0;
-          const double cost = std::max(estimate(f, groups, steps, ceil_div(share, step)), 4.0 + bytes_us) + join;
+          const double join = parts() > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts() * 1040.0 / 4.3e6 : 0.0;
+          const double cost = std::max(kPagesCost[f - kFew](groups, steps, ceil_div(share, step)), bytes_us) + join;
           if (cost < best) best = cost, best_form = f, best_share = share;
         }
         if (share >= longest) break;
@@ -462,7 +469,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
         steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
         longest = std::max(longest, std::ceil(last / keys_per_step(f)));
       }
-      const double cost = estimate(f, groups, steps, longest);
+      const double cost = kPromptCost[f - kFew](groups, steps, longest);
       if (cost < best) best = cost, form = f;
     }
     const int rows = rows_of(form);

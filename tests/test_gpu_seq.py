@@ -529,3 +529,30 @@ def test_calls_on_two_streams_do_not_meet():
                 got.append(call(i))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_both_halves_of_the_binding_give_the_same_bits(monkeypatch):
+    from paper_2601_04359_amd import binding
+    assert binding._NATIVE
+    results = []
+    for native in (binding._NATIVE, False):
+        monkeypatch.setattr(binding, "_NATIVE", native)
+        _, _, _, O, L = run_prompt("bf16", 8, 2, 128, [40, 333], [40, 500], lse=True)
+        out = [O, L]
+        for ragged, shared in ((None, 0), (None, 200), ([1, 5, 2], 130)):
+            _, _, O, L = run_pages("bf16", 8, 2, 128, [300, 210, 400], 1 if ragged is None else None, ragged=ragged, shared=shared)
+            out += [O, L]
+        test_store("bf16", 128, 8, 2, 64, [63, 64, 0, 200], [1, 1, 1, 1], False)
+        test_store("f32", 64, 5, 1, 64, [0, 60, 0, 7], [70, 0, 1, 130], True)
+        results.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    if native is False:
+        monkeypatch.undo()
+    Q = torch.zeros((8, 4, 128), dtype=torch.bfloat16, device=DEV)
+    pages, table, lens = pk.page_cache(3, 2, 64, 128), torch.zeros((4, 2), dtype=torch.int32, device=DEV), torch.ones(4, dtype=torch.int32, device=DEV)
+    for bad in (dict(max_len=129), dict(max_len=0), dict(lens=lens.long()), dict(table=table[:3]), dict(pages=pages[0]), dict(n_shared=5),
+                dict(shared=table[0, :1], n_shared=65), dict(offs=[0, 2, 4]), dict(offs=[0, 1, 2, 3, 5]), dict(lens=lens.cpu()),
+                dict(ws=torch.zeros(1, dtype=torch.uint8, device=DEV), shared=table[0], n_shared=65), dict(O=Q), dict(scale=-1.0)):
+        kw = {**dict(pages=pages, table=table, lens=lens, max_len=128, scale=0.1, O=torch.empty_like(Q)), **bad}
+        with pytest.raises(pk.PackCacheError):
+            pk.pc_page_attn(Q, kw.pop("pages"), kw.pop("table"), kw.pop("lens"), kw.pop("max_len"), kw.pop("scale"), **kw)
