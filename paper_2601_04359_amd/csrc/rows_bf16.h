@@ -148,7 +148,7 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
     const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
     const int64_t t = r.t0 + tok;
     if (a.part_o != nullptr) {
-      const int64_t at = (static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep + head) * a.T + t;
+      const int64_t at = static_cast<int64_t>(r.slot) * a.slot_rows + in_tile;
 #pragma unroll
       for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(a.part_o + at * kD + i * 8 + h * 4) = acc[h];
       if (i == 0) a.part_ml[at] = make_float2(M, L);
@@ -181,13 +181,9 @@ constexpr size_t kFewSmem = kFewWaves * (kFewWaveBytes + 32 * 8) + kFewRows * kR
 static_assert(2 * kFewTileBytes <= kFewWaveBytes, "a wave's K and V");
 
 template <bool kPages>
-__global__ __launch_bounds__(kFewWaves * 64, 1) void rows_few_kernel(RowsArgs a) {
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  lds_u8* smem = (lds_u8*)smem_raw;
+__device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds_u8* smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g = lane >> 5;
-  const RowSet r = kPages ? page_rows<kFewRows>(a, blockIdx.x, lane) : prompt_rows<kFewRows>(a, blockIdx.x, lane);
-  if (r.idle) return;
   const int n_set = r.n_tok * a.rep;
   const lds_u8* lds = smem + wave * kFewWaveBytes;
   const uint32_t lds_w = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
@@ -210,8 +206,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void rows_few_kernel(RowsArgs a)
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
       const int row = p * 4 + (lane >> 4), pos = lane & 15;
-      dma_16B_at(kb, keys.offset(k0, row, k_chunk_pos(row, pos)), lds_w + p * 1024);
-      dma_16B_at(vb, keys.offset(k0, row, v_chunk_pos(row, pos)), lds_w + kFewTileBytes + p * 1024);
+      dma_16B_at(kb, keys.offset(k0, row, k_chunk_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + p * 1024));
+      dma_16B_at(vb, keys.offset(k0, row, v_chunk_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + kFewTileBytes + p * 1024));
     }
     return true;
   };
@@ -363,14 +359,10 @@ constexpr int kManyTileBytes = kManyKeys * kRowBytes;
 constexpr size_t kManySmem = 4 * kManyTileBytes + kManyWaves * 8;   // tiles, the waves' limits
 
 template <bool kUnitC, bool kPages>
-__global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs a) {
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  lds_u8* smem = (lds_u8*)smem_raw;
+__device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, lds_u8* smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lds_mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + wave * 4096;
   const int l32 = lane & 31, g = lane >> 5;
-  const RowSet r = kPages ? page_rows<kManyRows>(a, blockIdx.x, lane) : prompt_rows<kManyRows>(a, blockIdx.x, lane);
-  if (r.idle) return;
   const int n_set = r.n_tok * a.rep, row_first = r.tile * kManyRows + wave * 32;
   const bool active = row_first < n_set;   // wave-uniform
   const int rho = min(row_first + l32, n_set - 1);
@@ -568,7 +560,7 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs 
     return static_cast<int64_t>(r.t0 + tk);
   };
   if (a.part_o != nullptr) {   // un-normalised, as fp32 rows
-    const int64_t first = static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep;
+    const int64_t first = static_cast<int64_t>(r.slot) * a.slot_rows + wave * 32;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -582,11 +574,9 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs 
     for (int i = 0; i < 16; ++i) {
       const int row = i * 2 + g;
       const f32x4 v = *reinterpret_cast<const lds_f32x4*>(mine + row * 512 + l32 * 16);
-      int h;
-      const int64_t t = row_to(min(row, rows_w - 1), &h);
-      if (row < rows_w) *reinterpret_cast<f32x4*>(a.part_o + ((first + h) * a.T + t) * kD + (l32 ^ row) * 4) = v;
+      if (row < rows_w) *reinterpret_cast<f32x4*>(a.part_o + (first + row) * kD + (l32 ^ row) * 4) = v;
     }
-    if (g == 0 && l32 < rows_w) a.part_ml[(first + head) * a.T + r.t0 + tok] = sees ? make_float2(fmaxf(m_ref, kNothing), l_tot) : make_float2(kNothing, 0.f);
+    if (g == 0 && l32 < rows_w) a.part_ml[first + l32] = sees ? make_float2(fmaxf(m_ref, kNothing), l_tot) : make_float2(kNothing, 0.f);
     return;
   }
   const float inv = sees ? 1.f / l_tot : 0.f;
@@ -622,16 +612,12 @@ constexpr int kMidWaves = 4, kMidRows = 64;
 constexpr size_t kMidSmem = kMidWaves * (kWaveOBytes + 32 * 8);
 
 template <bool kUnitC, bool kPages>
-__global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a) {
+__device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds_u8* smem) {
   constexpr int kR = 2, kG = 2, kS = 2;   // row groups, key groups, slots per operand and key group
   constexpr int kKeys = 32 * kG, kTile = kKeys * kRowBytes;   // of a phase
   static_assert(2 * kS * kTile <= kMidWaves * kWaveOBytes, "tiles");
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  lds_u8* smem = (lds_u8*)smem_raw;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g = lane >> 5, rg = wave % kR, kg = wave / kR;
-  const RowSet r = kPages ? page_rows<kMidRows>(a, blockIdx.x, lane) : prompt_rows<kMidRows>(a, blockIdx.x, lane);
-  if (r.idle) return;
   const int n_set = r.n_tok * a.rep, row_first = (r.tile * kR + rg) * 32;
   const bool active = row_first < n_set;   // wave-uniform
   const int rho = min(row_first + l32, n_set - 1);
@@ -676,7 +662,7 @@ __global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a)
 #pragma unroll
     for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + s * 16);
   }
-  // What the rows see, as in rows_many_kernel.
+  // What the rows see, as in rows_many.
   const int lim_true = limit_of(a, r, tok);
   const bool sees = lim_true > max(r.lo, r.begin);
   const int lim = sees ? lim_true : INT_MAX;
@@ -771,7 +757,7 @@ __global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a)
       if (j + 1 < n) stage(std::true_type{}, j + 1, pg_next, v_prev);
       const int key0 = r.begin + j * kKeys;
       if (key0 + kKeys > all_min || key0 < r.lo) {
-        // as in rows_many_kernel; a wave adds what is in its half
+        // as in rows_many; a wave adds what is in its half
         lds_u32x4* mine = reinterpret_cast<lds_u32x4*>(smem + v_cur) + threadIdx.x * 4;
         uint32_t odd = 0;
 #pragma unroll
@@ -827,6 +813,26 @@ __global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a)
   }
   __syncthreads();   // every wave has read its last tile; LDS takes the rows
   merge_waves<kR, kG>(a, r, smem, o, m_end, l_tot, wave, lane);
+}
+
+// ---- the kernels -----------------------------------------------------------------------------------------------------
+template <bool kPages>
+__global__ __launch_bounds__(kFewWaves * 64, 1) void rows_few_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  each_unit<kFewRows, kPages>(a, (lds_int*)(smem + kFewSmem), [&](const RowSet& r) { rows_few<kPages>(a, r, smem); });
+}
+template <bool kUnitC, bool kPages>
+__global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  each_unit<kMidRows, kPages>(a, (lds_int*)(smem + kMidSmem), [&](const RowSet& r) { rows_mid<kUnitC, kPages>(a, r, smem); });
+}
+template <bool kUnitC, bool kPages>
+__global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  each_unit<kManyRows, kPages>(a, (lds_int*)(smem + kManySmem), [&](const RowSet& r) { rows_many<kUnitC, kPages>(a, r, smem); });
 }
 
 }  // namespace pc

@@ -40,14 +40,11 @@ __device__ __forceinline__ void store4(T* p, f32x4 v) {
 }
 
 template <typename T, int D, bool kPages>
-__global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a) {
+__device__ __forceinline__ void rows_general(const RowsArgs& a, const RowSet& r, float (&o_lds)[kGenWaves][kGenRows][D],
+                                             float2 (&ml_lds)[kGenWaves][kGenRows]) {
   constexpr int kSteps = D / 16, kBlocks = D / 64;
-  __shared__ float o_lds[kGenWaves][kGenRows][D];
-  __shared__ float2 ml_lds[kGenWaves][kGenRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, kg = lane >> 4;
-  const RowSet r = kPages ? page_rows<kGenRows>(a, blockIdx.x, lane) : prompt_rows<kGenRows>(a, blockIdx.x, lane);
-  if (r.idle) return;
   const int n_set = r.n_tok * a.rep, rho = min(r.tile * kGenRows + r16, n_set - 1);
   const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
   const int lim = limit_of(a, r, tok);
@@ -196,7 +193,7 @@ __global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a
   const int tok_w = a.by_rep.of(rho_w), head_w = r.kvh * a.rep + rho_w - tok_w * a.rep;
   const int64_t t = r.t0 + tok_w;
   if (a.part_o != nullptr) {
-    const int64_t at = (static_cast<int64_t>(r.part) * a.by_hkv.d * a.rep + head_w) * a.T + t;
+    const int64_t at = static_cast<int64_t>(r.slot) * a.slot_rows + row;
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db) *reinterpret_cast<f32x4*>(a.part_o + at * D + db * 64 + c * 4) = out[db];
     if (c == 0) a.part_ml[at] = make_float2(M, L);
@@ -208,6 +205,14 @@ __global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a
   for (int db = 0; db < kBlocks; ++db)
     store4(static_cast<T*>(a.O) + head_w * a.o_stride + t * D + db * 64 + c * 4, none ? f32x4{0.f, 0.f, 0.f, 0.f} : out[db] * inv);
   if (a.lse != nullptr && c == 0) a.lse[head_w * static_cast<int64_t>(a.T) + t] = none ? -INFINITY : lse_of(M, L);
+}
+
+template <typename T, int D, bool kPages>
+__global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a) {
+  __shared__ float o_lds[kGenWaves][kGenRows][D];
+  __shared__ float2 ml_lds[kGenWaves][kGenRows];
+  __shared__ int plan[kPages ? kPlanBytes / 4 : 1];
+  each_unit<kGenRows, kPages>(a, (lds_int*)plan, [&](const RowSet& r) { rows_general<T, D, kPages>(a, r, o_lds, ml_lds); });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -225,15 +230,34 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   const int Hq = a.by_hkv.d * a.rep;
   const bool there = n < Hq * a.n_rows;
   const int head = there ? n / a.n_rows : 0, t = a.row0 + (there ? n - head * a.n_rows : 0);
-  const int s = seq_of_row(a.seqs, t);
+  const int s = max(0, seq_of_row(a.seqs, t));
   const bool even = a.seqs.per > 0;
-  const int len = max(0, min(a.lens[even ? s : a.seqs.k0[s]], a.max_len));
-  const int end = even ? (s + 1) * a.seqs.per : a.seqs.q0[s] + a.seqs.nq[s];
-  const bool none = len - (end - t) + 1 <= 0;
-  const int parts = none ? 0 : a.shared_parts + own_parts_of(a, len);
-  const int64_t step = static_cast<int64_t>(Hq) * a.T, at = static_cast<int64_t>(head) * a.T + t;
+  const int len = len_of(a, s), q0 = even ? s * a.seqs.per : a.seqs.q0[s], nq = even ? a.seqs.per : a.seqs.nq[s];
+  const bool none = len - (q0 + nq - t) + 1 <= 0;
+  // where the shares of the row are: its row in the tiles over the common rows, and in those over its sequence's own
+  const int kvh = a.by_rep.of(head), hh = head - kvh * a.rep, common = n_common(a);
+  const int rho_c = (t - a.row0) * a.rep + hh, rho = (t - q0) * a.rep + hh;
+  const int tile_c = a.by_tile.of(rho_c), tile = a.by_tile.of(rho), keys = own_keys_of(a, len);
+  const bool fixed = a.own_parts > 0;
+  const int share = fixed ? a.own_keys : keys > 0 ? a.cut[0] : 1, own = ceil_of(keys, share, 1.f / share);
+  const int tiles = even ? a.tiles_per_seq : a.by_tile.of(nq * a.rep + a.by_tile.d - 1);
+  const int64_t slots = static_cast<int64_t>(kvh) * (common + a.own_cap);
+  const int64_t at_c = (slots + tile_c) * a.slot_rows + rho_c - tile_c * a.by_tile.d;
+  int first = 0;     // the sequence's first unit
+  if (keys > 0) {
+    if (!fixed) first = a.cut[1 + s];
+    else if (even) first = s * a.by_parts.d;
+    else
+      for (int q = 0; q < s; ++q) first += a.by_tile.of(a.seqs.nq[q] * a.rep + a.by_tile.d - 1) * a.own_parts;
+  }
+  const int64_t at_o = (slots + common + first + tile) * a.slot_rows + rho - tile * a.by_tile.d;
+  const int parts = none ? 0 : a.shared_parts + own;
+  auto place = [&](int p) {
+    return p < a.shared_parts ? at_c + static_cast<int64_t>(p) * a.shared_tiles * a.slot_rows
+                              : at_o + static_cast<int64_t>(p - a.shared_parts) * tiles * a.slot_rows;
+  };
   float M = kNothing;
-  for (int p = c; p < parts; p += kLanes) M = fmaxf(M, a.part_ml[p * step + at].x);
+  for (int p = c; p < parts; p += kLanes) M = fmaxf(M, a.part_ml[place(p)].x);
 #pragma unroll
   for (int x = 1; x < kLanes; x *= 2) M = fmaxf(M, __shfl_xor(M, x, kLanes));
   float L = 0.f;
@@ -243,7 +267,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
     float2 ml[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int64_t from = min(p0 + i * kSplit, parts - 1) * step + at;
+      const int64_t from = place(min(p0 + i * kSplit, parts - 1));
       ml[i] = a.part_ml[from];
       v[i] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + c * 4);
     }
@@ -268,7 +292,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   if (!there) return;
   if (!none) acc *= 1.f / L;
   store4(static_cast<T*>(a.O) + head * a.o_stride + static_cast<int64_t>(t) * D + c * 4, acc);
-  if (a.lse != nullptr && c == 0) a.lse[at] = none ? -INFINITY : lse_of(M, L);
+  if (a.lse != nullptr && c == 0) a.lse[static_cast<int64_t>(head) * a.T + t] = none ? -INFINITY : lse_of(M, L);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
@@ -303,66 +327,81 @@ int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
   return n;
 }
 
-// How pc_page_attn cuts the keys of a launch's sequences: a form, and the length of a share.  The common rows and the sequences'
-// own ones are cut alike and go in one launch.  Beside the costs above there are the bytes of K and V (5.5 TB/s), and the
-// shares' join: a launch, and the fp32 rows that are written and read (4.3 TB/s).
+// How pc_page_attn cuts a launch's work: a form, the shares of the common rows, and room for units over the sequences' own rows,
+// which the device cuts (plan_pages); here their lengths are only known to be max_len at most, and taken to be that.  Beside
+// the costs above there are the bytes of K and V (5.5 TB/s), and the shares' join: a launch, and the fp32 rows that are written
+// and read (4.3 TB/s).
 struct PagePlan {
   Form form = kGeneral;
   int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
-  int own_tiles = 0, own_parts = 0, own_keys = kPageStep;
-  int parts() const { return shared_parts + own_parts; }
+  int own_tiles = 0, own_parts = 0, own_cap = 0;   // own_parts 0: the device cuts
+  int slot_rows = 0, slots = 1024, least_keys = 4 * kPageStep;
+  bool joined = false;           // results are shares
   PagePlan(int dtype, int D, int Hkv, int rep, int T, const int32_t* offs, int n_seq, int n_shared, int max_len) {
     const int n_rows = offs != nullptr ? offs[n_seq] - offs[0] : T;
     const int own = max_len > n_shared ? max_len - n_shared / kPageStep * kPageStep : 0;
+    int most = offs == nullptr ? T / n_seq : 0;
+    for (int s = 0; offs != nullptr && s < n_seq; ++s) most = std::max(most, offs[s + 1] - offs[s]);
+    int parts = 0;
     auto take = [&](Form f, int share) {
       form = f;
       shared_tiles = n_shared > 0 ? ceil_div(n_rows * rep, rows_of(f)) : 0;
       own_tiles = own > 0 ? row_tiles(offs, n_seq, T, rep, rows_of(f)) : 0;
-      shared_keys = own_keys = share;
+      shared_keys = share;
       shared_parts = ceil_div(n_shared, share);
-      own_parts = ceil_div(own, share);
+      parts = shared_parts + ceil_div(own, share);
     };
-    const int longest = std::max(n_shared, own);
+    const int longest = std::max(n_shared, own), whole = ceil_div(longest, kPageStep) * kPageStep;
     if (dtype != PC_BF16 || D != kD) {
       take(kGeneral, kPageStep);
       const int tiles = std::max(1, shared_tiles + own_tiles) * Hkv;
       const int shares = std::max(1, std::min({1024 / tiles, longest / 256, 64}));
       take(kGeneral, ceil_div(ceil_div(longest, shares), kPageStep) * kPageStep);
-      return;
-    }
-    const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5.5e6;
-    double best = 1e30;
-    Form best_form = kFew;
-    int best_share = kPageStep;
-    for (Form f : {kFew, kMid, kMany}) {
-      const int step = keys_per_step(f);
-      for (int share = 256;; share = std::max(share + 64, share * 5 / 4 / kPageStep * kPageStep)) {
-        share = std::min(share, ceil_div(longest, kPageStep) * kPageStep);
-        take(f, share);
-        if (parts() <= 96) {
-          const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * own_parts);
-          const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
-          const double join = parts() > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts() * 1040.0 / 4.3e6 : 0.0;
-          const double cost = std::max(kPagesCost[f - kFew](groups, steps, ceil_div(share, step)), bytes_us) + join;
-          if (cost < best) best = cost, best_form = f, best_share = share;
+    } else {
+      const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5.5e6;
+      double best = 1e30;
+      Form best_form = kFew;
+      int best_share = whole;
+      for (Form f : {kFew, kMid, kMany}) {
+        const int step = keys_per_step(f);
+        for (int share = 256;; share = std::max(share + 64, share * 5 / 4 / kPageStep * kPageStep)) {
+          share = std::min(share, whole);
+          take(f, share);
+          if (parts <= 96) {
+            const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * ceil_div(own, share));
+            const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
+            const double join = parts > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts * 1040.0 / 4.3e6 : 0.0;
+            const double cost = std::max(kPagesCost[f - kFew](groups, steps, ceil_div(share, step)), bytes_us) + join;
+            if (cost < best) best = cost, best_form = f, best_share = share;
+          }
+          if (share >= whole) break;
         }
-        if (share >= longest) break;
       }
+      take(best_form, best_share);
+      slots = form == kFew ? 256 : 512;
     }
-    take(best_form, best_share);
+    // The own rows' shares are as long as the common ones' while that bounds what a work-group has, whatever the lengths are:
+    // it saves the work-groups 2 us of cutting.  Beyond kFixedKeys the device cuts by the lengths that there are.
+    constexpr int kFixedKeys = 2048;
+    if (own > 0 && std::min(shared_keys, own) <= kFixedKeys) own_parts = ceil_div(own, shared_keys);
+    joined = own > 0 && own_parts == 0 ? true : shared_parts + own_parts > 1;
+    while (static_cast<int64_t>(own_tiles) * ceil_div(own, least_keys) > INT_MAX / 2) least_keys *= 2;   // sums of units are 32-bit numbers
+    own_cap = own_parts > 0 ? own_tiles * own_parts
+                            : static_cast<int>(std::min<int64_t>(static_cast<int64_t>(own_tiles) * ceil_div(own, 256), own_tiles + ceil_div(slots, Hkv)));
+    slot_rows = std::min(rows_of(form), std::max(n_shared > 0 ? n_rows : 0, own > 0 ? most : 0) * rep);
   }
+  int units() const { return shared_tiles * shared_parts + own_cap; }
+  size_t o_bytes(int Hkv, int D) const { return align_up(static_cast<size_t>(Hkv) * units() * slot_rows * D * sizeof(float), 256); }
+  size_t ml_bytes(int Hkv) const { return align_up(static_cast<size_t>(Hkv) * units() * slot_rows * sizeof(float2), 256); }
+  size_t bytes(int Hkv, int D) const { return joined ? o_bytes(Hkv, D) + ml_bytes(Hkv) + (1 + kPageSeqs) * sizeof(int) : 0; }
 };
-
-size_t part_bytes(int parts, int Hq, int T, int D) {
-  return parts <= 1 ? 0 : align_up(static_cast<size_t>(parts) * Hq * T * D * sizeof(float), 256) + static_cast<size_t>(parts) * Hq * T * sizeof(float2);
-}
 
 // Calls f(first, count) for the launches that a call's sequences are dealt to; f returns a status.
 template <class F>
 int each_launch(const int32_t* offs, int n_seq, F&& f) {
-  if (offs == nullptr) return f(0, n_seq);
-  for (int s0 = 0; s0 < n_seq; s0 += kSeqs)
-    if (int rc = f(s0, std::min(kSeqs, n_seq - s0))) return rc;
+  const int most = offs != nullptr ? kSeqs : kPageSeqs;
+  for (int s0 = 0; s0 < n_seq; s0 += most)
+    if (int rc = f(s0, std::min(most, n_seq - s0))) return rc;
   return PC_OK;
 }
 
@@ -388,14 +427,14 @@ int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a,
     kernel<<<blocks, kGenWaves * 64, 0, s>>>(a);
   } else if (form == kFew) {
     static std::atomic<uint64_t> ok;
-    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(rows_few_kernel<kPages>), kFewSmem, ok, who)) return rc;
-    rows_few_kernel<kPages><<<blocks, kFewWaves * 64, kFewSmem, s>>>(a);
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(rows_few_kernel<kPages>), kFewSmem + kPlanBytes, ok, who)) return rc;
+    rows_few_kernel<kPages><<<blocks, kFewWaves * 64, kFewSmem + kPlanBytes, s>>>(a);
   } else {
     static std::atomic<uint64_t> ok[4];
     const bool unit_c = a.c == 1.0f, many = form == kMany;
     auto* kernel = many ? (unit_c ? rows_many_kernel<true, kPages> : rows_many_kernel<false, kPages>)
                         : (unit_c ? rows_mid_kernel<true, kPages> : rows_mid_kernel<false, kPages>);
-    const size_t bytes = many ? kManySmem : kMidSmem;
+    const size_t bytes = (many ? kManySmem : kMidSmem) + kPlanBytes;
     if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[many * 2 + unit_c], who)) return rc;
     kernel<<<blocks, (many ? kManyWaves : kMidWaves) * 64, bytes, s>>>(a);
   }
@@ -494,8 +533,8 @@ extern "C" size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T
   size_t most = 0;
   each_launch(offs, n_seq, [&](int s0, int n) {
     const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
-    const PagePlan plan(dtype, D, Hkv, Hq / Hkv, T, o, n, std::min(n_shared, max_len), max_len);
-    most = std::max(most, part_bytes(plan.parts(), Hq, T, D));
+    const PagePlan plan(dtype, D, Hkv, Hq / Hkv, o != nullptr ? T : T / n_seq * n, o, n, std::min(n_shared, max_len), max_len);
+    most = std::max(most, plan.bytes(Hkv, D));
     return PC_OK;
   });
   return most;
@@ -541,30 +580,40 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
   hipStream_t st = static_cast<hipStream_t>(stream);
   return each_launch(offs, n_seq, [&](int s0, int n) -> int {
     const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
-    a.row0 = o != nullptr ? o[0] : 0, a.n_rows = o != nullptr ? o[n] - o[0] : T;
+    const int per = o != nullptr ? 0 : T / n_seq, rows = o != nullptr ? T : per * n;
+    a.row0 = o != nullptr ? o[0] : 0, a.n_rows = o != nullptr ? o[n] - o[0] : rows;
     if (a.n_rows == 0) return PC_OK;
-    a.seqs.n = n, a.seqs.per = o != nullptr ? 0 : T / n;
-    if (o == nullptr) a.seqs.by_per = Divisor(a.seqs.per);
-    else
+    a.seqs.n = n, a.seqs.per = per;
+    if (o == nullptr) {   // the launch's rows and sequences begin at s0's
+      const int64_t at = static_cast<int64_t>(s0) * per;
+      a.Q = static_cast<const uint8_t*>(Q) + at * D * elt, a.O = static_cast<uint8_t*>(O) + at * D * elt;
+      a.lse = lse != nullptr ? lse + at : nullptr;
+      a.table = table + s0 * table_stride, a.lens = lens + s0;
+      a.seqs.by_per = Divisor(per);
+    } else {
       for (int s = 0; s < n; ++s) a.seqs.q0[s] = o[s], a.seqs.nq[s] = o[s + 1] - o[s], a.seqs.k0[s] = s0 + s;
-    const PagePlan plan(dtype, D, Hkv, rep, T, o, n, n_shared, max_len);
-    a.n_tiles = plan.own_tiles, a.by_tiles = Divisor(std::max(1, plan.own_tiles));
-    a.tiles_per_seq = std::max(1, ceil_div(a.seqs.per * rep, rows_of(plan.form))), a.by_tiles_per_seq = Divisor(a.tiles_per_seq);
+    }
+    const PagePlan plan(dtype, D, Hkv, rep, rows, o, n, n_shared, max_len);
+    a.tiles_per_seq = std::max(1, ceil_div(per * rep, rows_of(plan.form)));
     a.shared_tiles = plan.shared_tiles, a.shared_parts = plan.shared_parts, a.shared_keys = plan.shared_keys;
     a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles));
-    a.own_parts = plan.own_parts, a.own_keys = plan.own_keys;
-    a.part_o = nullptr, a.part_ml = nullptr;
-    if (plan.parts() > 1) {
-      a.part_o = static_cast<float*>(ws);
-      a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) +
-                                            align_up(static_cast<size_t>(plan.parts()) * Hq * T * D * sizeof(float), 256));
+    a.own_parts = plan.own_parts, a.own_keys = plan.shared_keys, a.by_parts = Divisor(std::max(1, plan.own_parts * a.tiles_per_seq));
+    a.own_cap = plan.own_cap, a.slots = plan.slots, a.slot_rows = plan.slot_rows, a.by_tile = Divisor(rows_of(plan.form));
+    a.unit_us = plan.form == kFew ? 4.5f : 5.f;
+    a.key_us = plan.form == kGeneral ? 0.04f : plan.form == kFew ? 0.0059f : plan.form == kMid ? 0.0156f : 0.0225f;
+    a.step_bytes_us = 2.f * kPageStep * D * elt / 5.5e6f;
+    a.least_keys = plan.least_keys;
+    a.part_o = nullptr, a.part_ml = nullptr, a.cut = nullptr;
+    if (plan.joined) {
+      auto* at = static_cast<uint8_t*>(ws);
+      a.part_o = reinterpret_cast<float*>(at);
+      a.part_ml = reinterpret_cast<float2*>(at + plan.o_bytes(Hkv, D));
+      a.cut = reinterpret_cast<int*>(at + plan.o_bytes(Hkv, D) + plan.ml_bytes(Hkv));
     }
-    const int common = plan.shared_tiles * plan.shared_parts, own = plan.own_tiles * plan.own_parts;
-    a.n_common = common;
-    if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, (common + own) * Hkv, st)) return rc;
-    if (plan.parts() <= 1) return PC_OK;
-    // one row per work-group where there are many shares of it, else eight (sixteen at D = 64)
-    const bool many = plan.parts() > 6;
+    if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, plan.units() * Hkv, st)) return rc;
+    if (!plan.joined) return PC_OK;
+    // one row per work-group where there may be many shares of it, else eight (sixteen at D = 64)
+    const bool many = plan.shared_parts > 6 || Hq * a.n_rows <= 2048;
     auto* join = dtype == PC_BF16 ? (D == 128 ? (many ? rows_join_kernel<uint16_t, 128, 8> : rows_join_kernel<uint16_t, 128, 1>)
                                               : (many ? rows_join_kernel<uint16_t, 64, 8> : rows_join_kernel<uint16_t, 64, 1>))
                                   : (D == 128 ? (many ? rows_join_kernel<float, 128, 8> : rows_join_kernel<float, 128, 1>)

@@ -10,6 +10,8 @@
 
 namespace pc {
 
+typedef __attribute__((address_space(3))) int lds_int;
+
 constexpr float kNothing = -3.402823466e38f;   // the reference of a row that has seen no key: finite, so that sums merge
 
 struct RowsArgs {
@@ -24,20 +26,28 @@ struct RowsArgs {
   Divisor by_page;
   // rows
   int rep, T;                 // T: rows of O and lse
-  int row0, n_rows;           // the launch's part of them
+  int row0, n_rows;           // the launch's part of them (one number of rows each: row0 = 0, tensors and tables begin there)
   Divisor by_rep, by_hkv;
   SeqTable seqs;
   int fold;                   // pc_prompt_attn: row tiles (of a KV head) that the chip's compute units get first; 0: no second ones
   int max_level;              // pc_prompt_attn, several sequences: above every tile's level
-  int tiles_per_seq, n_tiles; // row tiles of one KV head: of a sequence (where all have as many), of all
-  Divisor by_tiles_per_seq, by_tiles;
-  // shares of the keys
-  int n_common;               // work-groups of this launch that have common rows, per KV head
+  int n_tiles;                // pc_prompt_attn: row tiles of one KV head
+  // pc_page_attn: units of work per KV head, and where their results go
   int shared_tiles, shared_parts, shared_keys;   // row tiles over the common rows; their shares, keys of each
   Divisor by_shared_tiles;
-  int own_parts, own_keys;                       // shares of the rows behind them, keys of each
-  float* part_o;              // [parts][Hq][T][D], un-normalised; NULL: one share, the result itself
-  float2* part_ml;            // [parts][Hq][T]: reference (base 2) and sum
+  int tiles_per_seq;          // row tiles of a sequence, where all have as many
+  int own_parts, own_keys;    // > 0: shares of the own rows as the host has cut them; 0: the device does
+  Divisor by_parts;
+  int own_cap;                // units over the sequences' own rows at most
+  float unit_us, key_us;      // what a unit and a key cost a work-group
+  float step_bytes_us;        // what 64 keys of a head cost HBM
+  int least_keys;             // of a share
+  int slots;                  // work-groups that the chip takes at once
+  int slot_rows;              // rows of a slot
+  Divisor by_tile;            // rows of a tile
+  float* part_o;              // [Hkv][n_common + own_cap][slot_rows][D], un-normalised; NULL: one share, the result itself
+  float2* part_ml;            // [Hkv][..][slot_rows]: reference (base 2) and sum
+  int* cut;                   // [1 + n_seq]: keys of a share of the own rows, the first unit of each sequence's
   float c, c_lo;              // scale * log2(e) in two floats
 };
 
@@ -50,9 +60,8 @@ struct RowSet {
   int begin, end;       // the work-group's
   int k0;               // pc_prompt_attn: row of key 0
   const int32_t* pages; // page numbers of the keys
-  int part;
+  int slot;             // where the result goes, if it is a share's
   bool common;
-  bool idle;            // nothing to do, not even an empty result
 };
 
 // The keys that token i of the set sees: those below this (0: none).
@@ -106,54 +115,178 @@ __device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int block, int 
   return r;
 }
 
-// pc_page_attn: first the work-groups over the common rows, then those over each sequence's own, shares slowest.
+// pc_page_attn.  The lengths are known on the device only, and sequences may be of any lengths beside each other, so that every
+// work-group cuts the work for itself, all alike: shares of `keys` keys of every sequence, and the units (sequence, share, row tile)
+// numbered through.  plan_pages finds the length of a share among six, from an eighth of what a work-group would have if all
+// had the same up to four times that: the rounds of units take their time, or HBM does for the keys of all; of equals the
+// longest.  It is work of one wave, on sums over lanes.
+constexpr int kPageSeqs = 256;                 // sequences of a launch at most, four per lane
+struct PageUnits {
+  int keys, total;    // keys of a share, units over own rows
+  lds_int* first;     // [kPageSeqs]: units in front of each sequence; then their lengths
+};
+__device__ __forceinline__ int ceil_of(int x, int by, float inv) {   // ceil(x / by), 0 <= x < 2^30
+  const int n = x + by - 1;
+  int q = static_cast<int>(static_cast<float>(n) * inv);
+  if (q * by > n) --q;
+  else if (n - q * by >= by) ++q;
+  return q;
+}
+__device__ __forceinline__ int len_of(const RowsArgs& a, int s) {
+  return max(0, min(a.lens[a.seqs.per > 0 ? s : a.seqs.k0[s]], a.max_len));
+}
+// Keys of a sequence from where its own rows begin, whole steps.
+__device__ __forceinline__ int own_keys_of(const RowsArgs& a, int len) {
+  return len > a.n_shared ? len - a.n_shared / kPageStep * kPageStep : 0;
+}
+__device__ __forceinline__ int n_common(const RowsArgs& a) { return a.shared_tiles * a.shared_parts; }
+
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix_sum(x), 63); }
+
+template <int R, int kPer>   // sequences per lane
+__device__ __forceinline__ void cut_pages(const RowsArgs& a, lds_int* plan, int lane) {
+  int keys[kPer], tiles[kPer], lens[kPer], longest = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int s = i * 64 + lane;
+    const bool there = s < a.seqs.n;
+    tiles[i] = !there ? 0 : a.seqs.per > 0 ? a.tiles_per_seq : (a.seqs.nq[s & (kSeqs - 1)] * a.rep + R - 1) / R;
+    lens[i] = there ? len_of(a, s) : 0;
+    keys[i] = tiles[i] > 0 ? own_keys_of(a, lens[i]) : 0;
+    longest = max(longest, keys[i]);
+    total += (keys[i] + kPageStep - 1) / kPageStep * tiles[i];   // (per steps of 64 keys)
+  }
+  longest = __builtin_amdgcn_readlane(wave_scan(longest, 0, [](int x, int y) { return max(x, y); }), 63);
+  total = wave_total(total);
+  const int whole = (max(longest, 1) + kPageStep - 1) / kPageStep * kPageStep;
+  int best = whole;
+  if (a.part_o != nullptr) {
+    constexpr int kTries = 6;
+    const float even = static_cast<float>(total) * kPageStep * a.by_hkv.d / a.slots;
+    int share[kTries], units[kTries];
+#pragma unroll
+    for (int t = 0; t < kTries; ++t) {
+      share[t] = min(max((static_cast<int>(even * (0.125f * (1 << t))) + kPageStep - 1) / kPageStep * kPageStep, a.least_keys), whole);
+      units[t] = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) units[t] += tiles[i] * ceil_of(keys[i], share[t], 1.f / share[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kTries; ++t) units[t] = wave_total(units[t]);
+    const float all_us = static_cast<float>(total) * a.by_hkv.d * a.step_bytes_us;
+    float best_us = 3e38f;
+#pragma unroll
+    for (int t = 0; t < kTries; ++t) {
+      const float rounds = ceilf(static_cast<float>(units[t] + n_common(a)) * a.by_hkv.d / a.slots);
+      const float us = fmaxf(rounds * (a.unit_us + a.key_us * share[t]), all_us);
+      if (units[t] <= a.own_cap && us <= best_us) best_us = us, best = share[t];    // (whole sequences always fit)
+    }
+  }
+  const float inv = 1.f / best;
+  int base = 0;
+#pragma unroll
+  for (int i = 0; i < kPageSeqs / 64; ++i) {
+    if (i < kPer) {
+      const int units = tiles[i % kPer] * (a.part_o != nullptr ? ceil_of(keys[i % kPer], best, inv) : 1), upto = wave_prefix_sum(units);
+      plan[i * 64 + lane] = base + upto - units;
+      plan[kPageSeqs + 2 + i * 64 + lane] = lens[i % kPer];
+      if (blockIdx.x == 0 && a.part_o != nullptr && i * 64 + lane < a.seqs.n) a.cut[1 + i * 64 + lane] = base + upto - units;
+      base += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  if (lane == 0) {
+    plan[kPageSeqs] = best, plan[kPageSeqs + 1] = base;
+    if (blockIdx.x == 0 && a.part_o != nullptr) a.cut[0] = best;
+  }
+}
 template <int R>
-__device__ __forceinline__ RowSet page_rows(const RowsArgs& a, int block, int lane) {
-  RowSet r = {};
-  int u = a.by_hkv.of(block);
-  r.kvh = block - u * a.by_hkv.d;
-  if (u < a.n_common) {
+__device__ __forceinline__ PageUnits plan_pages(const RowsArgs& a, lds_int* plan, int wave, int lane) {
+  if (a.own_parts > 0) return {a.own_keys, a.own_cap, plan};
+  if (wave == 0) {
+    if (a.seqs.n <= 64) cut_pages<R, 1>(a, plan, lane);
+    else cut_pages<R, kPageSeqs / 64>(a, plan, lane);
+  }
+  __syncthreads();
+  return {__builtin_amdgcn_readfirstlane(plan[kPageSeqs]), __builtin_amdgcn_readfirstlane(plan[kPageSeqs + 1]), plan};
+}
+constexpr int kPlanBytes = (2 * kPageSeqs + 2) * 4;
+
+// Unit `unit` of the launch, KV heads fastest, first those over the common rows; false: there are no more.
+template <int R>
+__device__ __forceinline__ bool page_rows(const RowsArgs& a, const PageUnits& units, int unit, int lane, RowSet& r) {
+  int u = a.by_hkv.of(unit);
+  r = {};
+  r.kvh = unit - u * a.by_hkv.d;
+  const int common = n_common(a);
+  if (u >= common + units.total) return false;
+  r.slot = r.kvh * (common + a.own_cap) + u;
+  if (u < common) {
     r.common = true;
-    r.part = a.by_shared_tiles.of(u);
-    r.tile = u - r.part * a.shared_tiles;
+    const int share = a.by_shared_tiles.of(u);
+    r.tile = u - share * a.shared_tiles;
     r.t0 = a.row0, r.n_tok = a.n_rows;
     r.n_keys = a.n_shared;
-    r.begin = r.part * a.shared_keys, r.end = min(r.begin + a.shared_keys, a.n_shared);
+    r.begin = share * a.shared_keys, r.end = min(r.begin + a.shared_keys, a.n_shared);
     r.pages = a.shared;
-    return r;
+    return true;
   }
-  u -= a.n_common;
-  const int share = a.by_tiles.of(u);
-  u -= share * a.n_tiles;
-  int number, nq;
-  if (a.seqs.per > 0) {
-    number = a.by_tiles_per_seq.of(u);
-    r.tile = u - number * a.tiles_per_seq;
-    nq = a.seqs.per, r.t0 = number * nq;
+  u -= common;
+  int s, tiles = a.tiles_per_seq, share = 0;
+  if (a.own_parts > 0 && a.seqs.per > 0) {
+    s = a.by_parts.of(u);     // (units of a sequence: its tiles times the shares)
+    u -= s * a.by_parts.d;
   } else {
-    const int tiles = lane < a.seqs.n ? (a.seqs.nq[lane] * a.rep + R - 1) / R : 0;
-    const int upto = wave_prefix_sum(tiles);
-    const int s = __builtin_ctzll(__ballot(upto > u));
-    r.tile = u - (__builtin_amdgcn_readlane(upto, s) - __builtin_amdgcn_readlane(tiles, s));
-    number = a.seqs.k0[s], nq = a.seqs.nq[s], r.t0 = a.seqs.q0[s];
+    s = -1;                   // the last sequence that begins at or in front of u
+    if (a.own_parts > 0) {    // from a table's rows (64 sequences at most)
+      const int units = lane < a.seqs.n ? (a.seqs.nq[lane] * a.rep + R - 1) / R * a.own_parts : 0, first = wave_prefix_sum(units) - units;
+      s = __popcll(__ballot(lane < a.seqs.n && first <= u)) - 1;
+      u -= __builtin_amdgcn_readlane(first, s);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPageSeqs / 64; ++i)
+        if (i * 64 < a.seqs.n) s += __popcll(__ballot(i * 64 + lane < a.seqs.n && units.first[i * 64 + lane] <= u));
+      s = __builtin_amdgcn_readfirstlane(s);
+      u -= __builtin_amdgcn_readfirstlane(units.first[s]);
+    }
   }
-  r.n_tok = nq;
-  const int len = min(a.lens[number], a.max_len);
+  int number = s;
+  if (a.seqs.per > 0) {
+    r.n_tok = a.seqs.per, r.t0 = s * r.n_tok;
+  } else {
+    number = a.seqs.k0[s], r.n_tok = a.seqs.nq[s], r.t0 = a.seqs.q0[s];
+    tiles = (r.n_tok * a.rep + R - 1) / R;
+  }
+  for (r.tile = u; r.tile >= tiles; r.tile -= tiles) ++share;
+  const int len = a.own_parts > 0 ? min(a.lens[number], a.max_len) : units.first[kPageSeqs + 2 + s];
   r.pages = a.table + number * a.table_stride;
-  r.lo = a.n_shared, r.n_keys = max(len, 0), r.first = len - nq + 1;
-  const int from = a.n_shared / kPageStep * kPageStep;
-  r.begin = from + share * a.own_keys, r.end = min(r.begin + a.own_keys, r.n_keys);
-  r.part = a.shared_parts + share;
-  // a result of nothing is written only where nobody else writes the row
-  if (len <= a.n_shared || r.begin >= r.n_keys) r.end = r.begin, r.idle = a.part_o != nullptr;
-  return r;
+  r.lo = a.n_shared, r.n_keys = max(len, 0), r.first = len - r.n_tok + 1;
+  r.begin = a.n_shared / kPageStep * kPageStep + share * units.keys;
+  r.end = min(r.begin + units.keys, r.n_keys);
+  if (len <= a.n_shared || r.end < r.begin) r.end = r.begin;
+  // behind the sequence's end: an empty result is written only where nobody else writes the row
+  return r.begin < r.end || a.part_o == nullptr;
 }
 
-// How many of the shares over a sequence's own rows have written something: those in front of its end.
-__device__ __forceinline__ int own_parts_of(const RowsArgs& a, int len) {
-  if (len <= a.n_shared) return 0;
-  const int n = len - a.n_shared / kPageStep * kPageStep;
-  return (n + a.own_keys - 1) / a.own_keys;
+// A work-group has one tile of a prompt, or one unit of pages; those behind the last unit end at once (a loop over units took
+// 100 registers more, spilled).
+template <int R, bool kPages, class Body>
+__device__ __forceinline__ void each_unit(const RowsArgs& a, lds_int* plan, Body&& body) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (!kPages) {
+    body(prompt_rows<R>(a, blockIdx.x, lane));
+  } else {
+    const PageUnits units = plan_pages<R>(a, plan, wave, lane);
+    RowSet r;
+    if (!page_rows<R>(a, units, blockIdx.x, lane, r)) return;
+    // the same in every lane, and in scalar registers: the compiler does not see it of what has gone through LDS
+    for (int* v : {&r.kvh, &r.tile, &r.t0, &r.n_tok, &r.first, &r.lo, &r.n_keys, &r.begin, &r.end, &r.slot})
+      *v = __builtin_amdgcn_readfirstlane(*v);
+    const uint64_t at = reinterpret_cast<uint64_t>(r.pages);
+    const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at)),
+                   high = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+    r.pages = reinterpret_cast<const int32_t*>(static_cast<uint64_t>(high) << 32 | low);
+    body(r);
+  }
 }
 
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u; }

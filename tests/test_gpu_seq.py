@@ -311,7 +311,8 @@ def test_page_attn_ragged(dtype, shared):
 @pytest.mark.parametrize("dtype,Hq,Hkv,lens,n,shared", [
     ("bf16", 16, 4, [5000, 3, 2049], 1, 0), ("bf16", 16, 4, [9000 + i for i in range(20)], 1, 9000), ("bf16", 4, 1, [4100, 300], 1, 0),
     ("bf16", 16, 4, [3000 + 40 * i for i in range(3)], 40, 2900), ("bf16", 24, 8, [4500], 300, 0), ("f32", 8, 2, [2500 + i for i in range(5)], 1, 2400),
-    ("bf16", 8, 2, [2100] * 130, 1, 2000), ("bf16", 16, 2, [1000 + i for i in range(70)], 2, 0)])
+    ("bf16", 8, 2, [2100] * 130, 1, 2000), ("bf16", 4, 2, [70 + i % 90 for i in range(600)], 1, 64),
+    ("f32", 4, 2, [1 + i % 300 for i in range(300)], 2, 0), ("bf16", 16, 4, [9000, 1, 64, 3000, 0, 200, 129, 5000], 1, 0), ("bf16", 16, 2, [1000 + i for i in range(70)], 2, 0)])
 def test_page_attn_long(dtype, Hq, Hkv, lens, n, shared):
     run_pages(dtype, Hq, Hkv, 128, lens, n, shared=shared, page=128)
 
