@@ -23,6 +23,10 @@ by token), held in 4 bits and kept within a budget by what attention itself look
 the frames' age: pc_q4_store, pc_q4_attn (which adds up every key's attention weight) and one
 pc_q4_evict for all layers when a step ends.
 
+PagedStack holds the caches of several sequences at once in pages of one pool: prompts of any lengths go in together
+(pc_prompt_attn), a sequence can be continued several ways at once without a copy of what is common, and a step's rows of all
+sequences are stored (pc_page_store, with the rotation on the way) and attended to (pc_page_attn, the common rows once for all).
+
 With slide_t_scale set the window slides (Sec. 3.4, Slide-Cache): when a step begins, the
 oldest frames that the step before evicted completely leave the segment table and
 pc_rebase lowers the temporal coordinate of every retained frame row by slide_t_scale per
@@ -378,3 +382,180 @@ class EvictingStack:
         if self.nk > self.budget:
             self.nk = pk.pc_q4_evict(self.cache, self.pos, self.weights, self.nk, self.budget, self.n_anchor, self.recent_t)
         return self.nk
+
+
+class PagedStack:
+    """The caches of a stack of layers for several sequences, in pages of one pool.
+
+        a = s.open()                      a sequence without rows
+        b, c = s.fork(a, 2)               sequences that begin with a's rows; the pages are common, one that is not full is
+                                          copied when either goes on
+        s.begin([a, b, c], rows)          a step: new rows of each, one number or one per sequence
+        O = s.attend(layer, Q, K, V, pos) their rows, one sequence behind the other: stored in the layer's pages with the
+                                          rotation on the way, then attended to; row i of a sequence sees its rows up to its own
+        s.close(a)                        its pages are free, but for those that others have in common with it
+
+    Q [Hq][T][D] and K, V [Hkv][T][D] of the step are not rotated yet; Q is rotated in place, and so is K in a step of new
+    sequences.  pos int32 [T][3] on the device.  A step in which every sequence is new runs pc_prompt_attn over its own rows, every other one pc_page_attn over
+    the pages, with the pages that all of the step's sequences begin with read once for all.
+
+    The pages of a step are decided in begin(), on the host; attend() only launches.  With the same sequences and one row each, a
+    step's launches are the same while n_shared and max_len are, so that attend() can be recorded into a HIP graph: begin()
+    writes the lengths and tables into the same device buffers before every replay (max_len: a bound for as long as the graph
+    is to last).
+    """
+
+    def __init__(self, n_layers: int, Hq: int, Hkv: int, D: int, n_pages: int, scale: float, page_rows: int = 64,
+                 max_seqs: int = 64, max_rows: int | None = None, sections=(32, 48, 48), base: float = 10000.0, dtype=None,
+                 device="cuda:0", fold_scale: bool = True):
+        import torch
+        if n_layers < 1 or Hkv < 1 or Hq < 1 or Hq % Hkv or n_pages < 1 or max_seqs < 1:
+            raise ValueError(f"{n_layers} layers of {Hq}/{Hkv} heads, {n_pages} pages, {max_seqs} sequences")
+        self.L, self.Hq, self.Hkv, self.D, self.page_rows, self.scale = n_layers, Hq, Hkv, D, page_rows, scale
+        self.sections, self.base = tuple(sections), base
+        # the softmax scale rides on the query rotation (see RollingLayer)
+        self.q_out_scale = pk.folded_q_scale(scale) if fold_scale else 1.0
+        self.call_scale = pk.PC_SCALE_FOLDED if fold_scale else scale
+        pools = pk.page_cache(n_layers * n_pages, Hkv, page_rows, D, dtype, device)
+        self.K, self.V = (t.view(n_layers, n_pages, Hkv, page_rows, D) for t in pools)
+        max_rows = n_pages * page_rows if max_rows is None else max_rows
+        self.width = max(1, -(-max_rows // page_rows))     # pages of a sequence at most
+        self.table = torch.zeros((max_seqs, self.width), dtype=torch.int32, device=device)
+        self.lens = torch.zeros((max_seqs,), dtype=torch.int32, device=device)
+        self.shared = torch.zeros((self.width,), dtype=torch.int32, device=device)
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._users = [0] * n_pages                        # sequences that a page belongs to
+        self._pages: dict[int, list[int]] = {}
+        self._rows: dict[int, int] = {}
+        self._next = 0
+        self._step = None                                  # (sequences, offsets or None, fresh)
+        self.n_shared = self.max_len = 0
+
+    # ---- sequences (host only) ----------------------------------------------------------------
+    def open(self) -> int:
+        self._next += 1
+        self._pages[self._next], self._rows[self._next] = [], 0
+        return self._next
+
+    def rows(self, seq: int) -> int:
+        """Rows of a sequence."""
+        return self._rows[self._known(seq)]
+
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def _known(self, seq: int) -> int:
+        if seq not in self._rows:
+            raise ValueError(f"sequence {seq} is not open")
+        return seq
+
+    def fork(self, seq: int, n: int = 1) -> list[int]:
+        """n further sequences that begin with seq's rows."""
+        self._known(seq)
+        out = []
+        for _ in range(n):
+            new = self.open()
+            self._pages[new], self._rows[new] = list(self._pages[seq]), self._rows[seq]
+            for p in self._pages[new]:
+                self._users[p] += 1
+            out.append(new)
+        return out
+
+    def close(self, seq: int) -> None:
+        for p in self._pages.pop(self._known(seq)):
+            self._users[p] -= 1
+            if self._users[p] == 0:
+                self._free.append(p)
+        del self._rows[seq]
+        self._step = None
+
+    # ---- one step -----------------------------------------------------------------------------
+    def begin(self, seqs, rows=1, max_len: int | None = None) -> None:
+        """The step's sequences and how many new rows each of them gets.  max_len: a bound on the rows of any of them, for
+        attend() to lay its work out for (None: the longest)."""
+        import torch
+        seqs = [self._known(q) for q in seqs]
+        counts = [int(rows)] * len(seqs) if isinstance(rows, int) else [int(r) for r in rows]
+        if not seqs or len(set(seqs)) < len(seqs) or len(seqs) > self.table.shape[0] or len(counts) != len(seqs) or min(counts) < 0:
+            raise ValueError(f"a step of {len(seqs)} sequences (each once, {self.table.shape[0]} at most), new rows {rows}")
+        R = self.page_rows
+        # what the step needs: whole new pages, and a copy of a page that is not full and not the sequence's alone (one that
+        # several of the step's sequences leave for copies may keep its last user)
+        longest = max(self._rows[q] + n for q, n in zip(seqs, counts))
+        if max_len is not None and not longest <= max_len <= self.width * R:
+            raise ValueError(f"max_len {max_len}: {longest} rows, {self.width * R} at most")
+        need, users = 0, {}
+        for q, n in zip(seqs, counts):
+            have, after = self._rows[q], self._rows[q] + n
+            if -(-after // R) > self.width:
+                raise ValueError(f"sequence {q}: {after} rows, {self.width * R} at most")
+            need += -(-after // R) - len(self._pages[q])
+            if n and have % R:
+                p = self._pages[q][-1]
+                if users.setdefault(p, self._users[p]) > 1:
+                    users[p] -= 1
+                    need += 1
+        if need > len(self._free):
+            raise ValueError(f"{need} pages needed, {len(self._free)} free")
+        fresh = all(self._rows[q] == 0 for q in seqs)
+        copies = []
+        for q, n in zip(seqs, counts):
+            pages = self._pages[q]
+            if n and self._rows[q] % R and self._users[pages[-1]] > 1:
+                p = self._free.pop()
+                copies.append((pages[-1], p))
+                self._users[pages[-1]] -= 1
+                self._users[p], pages[-1] = 1, p
+            self._rows[q] += n
+            while len(pages) * R < self._rows[q]:
+                p = self._free.pop()
+                self._users[p] = 1
+                pages.append(p)
+        device = self.K.device
+        if copies:
+            old, new = (torch.tensor(v, device=device) for v in zip(*copies))
+            for t in (self.K, self.V):
+                t[:, new] = t[:, old]
+        lists = [self._pages[q] for q in seqs]
+        common = 0
+        if len(seqs) > 1:
+            while all(len(v) > common and v[common] == lists[0][common] for v in lists):
+                common += 1
+        # (a page that is common and not full has no new rows in it: every sequence of it ends there alike)
+        self.n_shared = min([common * R] + [self._rows[q] for q in seqs])
+        self.max_len = max(1, longest if max_len is None else int(max_len))
+        n_cols = max(1, max(len(v) for v in lists))
+        host = torch.zeros((len(seqs), n_cols + 1), dtype=torch.int32)
+        for i, v in enumerate(lists):
+            host[i, :len(v)] = torch.tensor(v, dtype=torch.int32)
+            host[i, n_cols] = self._rows[seqs[i]]
+        host = host.to(device)
+        self.table[:len(seqs), :n_cols] = host[:, :n_cols]
+        self.lens[:len(seqs)] = host[:, n_cols]
+        self.shared[:n_cols] = host[0, :n_cols]
+        offs = [0]
+        for n in counts:
+            offs.append(offs[-1] + n)
+        even = len(set(counts)) == 1
+        self._step = (len(seqs), offs, even, fresh)
+
+    def attend(self, layer: int, Q, K, V, pos, O=None, lse=None):
+        """The step's rows of one layer: into the pages, and their attention -> O."""
+        import torch
+        if self._step is None:
+            raise ValueError("begin() names the step's sequences first")
+        if not 0 <= layer < self.L:
+            raise ValueError(f"layer {layer} of {self.L}")
+        n, offs, even, fresh = self._step
+        if Q.shape[1] != offs[-1]:
+            raise ValueError(f"{Q.shape[1]} rows in a step of {offs[-1]}")
+        table, lens, pages = self.table[:n], self.lens[:n], (self.K[layer], self.V[layer])
+        o = None if even else offs
+        pk.pc_page_store(K, V, pages, table, lens, offs=o, pos=pos, sections=self.sections, base=self.base,
+                         K_out=K if fresh else None, Q=Q, Q_out=Q, out_scale=self.q_out_scale)
+        if O is None:
+            O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        if fresh:
+            return pk.pc_prompt_attn(Q, K, V, self.call_scale, offs, O=O, lse=lse)
+        return pk.pc_page_attn(Q, pages, table, lens, self.max_len, self.call_scale, offs=o,
+                               shared=self.shared if self.n_shared else None, n_shared=self.n_shared, O=O, lse=lse)

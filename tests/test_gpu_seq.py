@@ -16,6 +16,7 @@ import pytest
 import torch
 
 import paper_2601_04359_amd as pk
+from paper_2601_04359_amd.rollout import PagedStack
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -557,3 +558,134 @@ def test_both_halves_of_the_binding_give_the_same_bits(monkeypatch):
         kw = {**dict(pages=pages, table=table, lens=lens, max_len=128, scale=0.1, O=torch.empty_like(Q)), **bad}
         with pytest.raises(pk.PackCacheError):
             pk.pc_page_attn(Q, kw.pop("pages"), kw.pop("table"), kw.pop("lens"), kw.pop("max_len"), kw.pop("scale"), **kw)
+
+
+# ------------------------------------------------------------------------------ the operators together
+class Twin:
+    """A PagedStack and its sequences in plain form; every attend() is checked row by row."""
+
+    def __init__(self, dtype="bf16", layers=2, Hq=8, Hkv=2, D=128, n_pages=60, seed=0, **kw):
+        self.s = PagedStack(layers, Hq, Hkv, D, n_pages, D ** -0.5, sections=SECTIONS[D], dtype=TYPES[dtype], fold_scale=False, **kw)
+        for t in (self.s.K, self.s.V):
+            t.fill_(NAN)
+        self.dtype, self.gen, self.plain = dtype, generator(seed), {}
+
+    def open(self):
+        q = self.s.open()
+        self.plain[q] = [[torch.empty((self.s.Hkv, 0, self.s.D), dtype=TYPES[self.dtype], device=DEV) for _ in range(2)] for _ in range(self.s.L)]
+        return q
+
+    def fork(self, q, n=1):
+        out = self.s.fork(q, n)
+        for f in out:
+            self.plain[f] = [[x.clone() for x in kv] for kv in self.plain[q]]
+        return out
+
+    def step(self, seqs, rows, **kw):
+        s = self.s
+        counts = [rows] * len(seqs) if isinstance(rows, int) else rows
+        offs = offsets(counts)
+        T = offs[-1]
+        s.begin(seqs, rows, **kw)
+        for layer in range(s.L):
+            Q, K, V = (normal(self.gen, H, T, s.D).to(TYPES[self.dtype]) for H in (s.Hq, s.Hkv, s.Hkv))
+            pos = torch.randint(0, 900, (T, 3), dtype=torch.int32, device=DEV, generator=self.gen)
+            k, q = turned(K, pos, s.D), turned(Q, pos, s.D)
+            L = torch.empty((s.Hq, T), device=DEV)
+            O = s.attend(layer, Q, K, V, pos, lse=L)
+            assert torch.equal(Q, q)
+            for i, seq in enumerate(seqs):
+                a, b = offs[i], offs[i + 1]
+                kv = self.plain[seq][layer]
+                kv[0], kv[1] = torch.cat((kv[0], k[:, a:b]), 1), torch.cat((kv[1], V[:, a:b]), 1)
+                for h in range(s.Hq if b > a else 0):
+                    g = h // (s.Hq // s.Hkv)
+                    check_rows(self.dtype, O[h, a:b], L[h, a:b], q[h, a:b], kv[0][g], kv[1][g], s.scale, kv[0].shape[1] - (b - a) + 1)
+        for seq in seqs:
+            assert s.rows(seq) == self.plain[seq][0][0].shape[1]
+
+
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 64), ("bf16", 64, 64), ("f32", 128, 128)])
+def test_stack_of_sequences(dtype, D, page):
+    t = Twin(dtype, D=D, page_rows=page, n_pages=40)
+    a, b, c = t.open(), t.open(), t.open()
+    t.step([a, b, c], [130, 1, 64])               # prompts
+    t.step([a, b, c], 1)
+    d, e = t.fork(a, 2)                           # in the middle of a page
+    t.step([a, d, e], 1)                          # copies; two pages are common
+    assert t.s.n_shared == 131 // page * page
+    t.step([d, e], [40, 1])
+    t.step([a, b, c, d, e], [1, 0, 3, 70, 2])     # no page is common to all
+    assert t.s.n_shared == 0
+    free = t.s.free_pages()
+    f, = t.fork(d)
+    t.step([d, f], 0)                             # nothing new: the whole sequence is common, the page that is not full as well
+    assert t.s.n_shared == t.s.rows(d) and t.s.free_pages() == free
+    t.step([f], 5)
+    t.step([d, f], 1)
+    for q in (a, b, e, f):
+        t.s.close(q)
+    g = t.open()
+    t.step([g], [200])                            # pages that others have left
+    t.step([c, d, g], [1, 1, 1], max_len=page * 5)
+    for q in (c, d, g):
+        t.s.close(q)
+    assert t.s.free_pages() == 40
+
+
+def test_stack_of_many_branches():
+    """A prompt continued 20 ways, token by token across the border of a page; then one of them 10 ways."""
+    t = Twin(n_pages=90, layers=1, Hq=16, Hkv=4)
+    a = t.open()
+    t.step([a], [700])
+    branches = [a] + t.fork(a, 19)
+    for _ in range(3):
+        t.step(branches, 1)
+        assert t.s.n_shared == 640
+    t.step(branches, 66)
+    for q in branches[1:]:
+        t.s.close(q)
+    more = [a] + t.fork(a, 9)
+    t.step(more, 2)
+    assert t.s.n_shared == 768 and t.s.rows(a) == 771
+
+
+def test_stack_step_in_a_graph():
+    """Steps of one token, recorded once: begin() moves the lengths and tables between the replays."""
+    layers, Hq, Hkv, D = 2, 8, 2, 128
+    gen = generator(3)
+    stacks = [PagedStack(layers, Hq, Hkv, D, 40, D ** -0.5, max_rows=512) for _ in range(2)]
+    rows = lambda n: [normal(gen, layers, H, n, D).to(torch.bfloat16) for H in (Hq, Hkv, Hkv)]
+    Q, K, V = rows(150)
+    pos = torch.randint(0, 900, (150, 3), dtype=torch.int32, device=DEV, generator=gen)
+    seqs = []
+    for s in stacks:
+        a = s.open()
+        s.begin([a], 150)
+        for l in range(layers):
+            s.attend(l, Q[l].clone(), K[l].clone(), V[l], pos)
+        seqs.append([a] + s.fork(a, 2))
+        s.begin(seqs[-1], 1, max_len=512)
+        for l in range(layers):
+            s.attend(l, Q[l, :, :3].clone(), K[l, :, :3].clone(), V[l, :, :3], pos[:3])
+    fixed = [x[:, :, :3].clone() for x in (Q, K, V)]
+    p, O = pos[:3].clone(), torch.empty((layers, Hq, 3, D), dtype=torch.bfloat16, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    stacks[0].begin(seqs[0], 1, max_len=512)
+    with torch.cuda.graph(graph):
+        for l in range(layers):
+            stacks[0].attend(l, fixed[0][l], fixed[1][l], fixed[2][l], p, O=O[l])
+    for step in range(70):                        # across a page's border
+        new = rows(3)
+        if step:
+            stacks[0].begin(seqs[0], 1, max_len=512)
+        stacks[1].begin(seqs[1], 1, max_len=512)
+        assert stacks[0].n_shared == stacks[1].n_shared == 128
+        for x, y in zip(fixed, new):
+            x.copy_(y)
+        p.random_(0, 900, generator=gen)
+        graph.replay()
+        torch.cuda.synchronize()
+        for l in range(layers):
+            want = stacks[1].attend(l, new[0][l], new[1][l], new[2][l], p)
+            assert torch.equal(O[l], want)

@@ -9,6 +9,7 @@ import torch
 
 import paper_2601_04359_amd as pk
 from paper_2601_04359_amd import binding
+from paper_2601_04359_amd.rollout import PagedStack
 
 NULL, SHAPE, DTYPE, UNSUPPORTED, WORKSPACE = -1, -2, -3, -4, -6
 A = 1 << 40       # made-up addresses, far apart
@@ -158,3 +159,70 @@ def test_binding_refuses_what_does_not_fit(L):
     assert k.shape == v.shape == (3, 2, 128, 64) and k.dtype == torch.float32
     with pytest.raises(pk.PackCacheError):
         binding._sequences(i32(4, 2).long(), i32(4), None, 4)
+
+
+# ------------------------------------------------------------------------------ the stack's bookkeeping
+def stack(**kw):
+    return PagedStack(**{**dict(n_layers=2, Hq=4, Hkv=2, D=64, n_pages=8, scale=0.1, device="cpu"), **kw})
+
+
+def test_stack_pages_follow_the_sequences():
+    s = stack()
+    a, b = s.open(), s.open()
+    s.begin([a, b], [130, 64])
+    assert s.free_pages() == 4 and s.rows(a) == 130 and s.n_shared == 0 and s.max_len == 130
+    s.K[:, s._pages[a][2], :, :2] = 3.0
+    c, d = s.fork(a, 2)
+    assert s.free_pages() == 4 and s.rows(c) == 130
+    s.begin([c, d], 1)                      # both leave a's last page for copies of it
+    assert s.free_pages() == 2 and s.n_shared == 128
+    assert len({s._pages[q][2] for q in (a, c, d)}) == 3 and s._pages[a][:2] == s._pages[c][:2] == s._pages[d][:2]
+    assert (s.K[:, s._pages[c][2], :, :2] == 3.0).all() and (s.K[:, s._pages[d][2], :, :2] == 3.0).all()
+    assert s.lens[:2].tolist() == [131, 131] and s.table[0, :3].tolist() == s._pages[c] and s.shared[:2].tolist() == s._pages[c][:2]
+    s.close(a)
+    assert s.free_pages() == 3
+    s.begin([c, d], [0, 0])
+    assert s.n_shared == 128
+    s.begin([c], 1)
+    assert s.n_shared == 0
+    s.close(c), s.close(d), s.close(b)
+    assert s.free_pages() == 8 and sorted(s._free) == list(range(8))
+
+
+def test_the_last_user_of_a_page_keeps_it():
+    s = stack(n_pages=3)
+    a = s.open()
+    s.begin([a], 70)
+    b, = s.fork(a)
+    s.begin([a, b], 1)                      # one copy is enough for the two
+    assert s.free_pages() == 0 and s._pages[a][1] != s._pages[b][1]
+
+
+def test_stack_of_sequences_refuses():
+    for bad in (dict(n_layers=0), dict(Hq=3), dict(n_pages=0), dict(max_seqs=0)):
+        with pytest.raises(ValueError):
+            stack(**bad)
+    for bad in (dict(D=96), dict(page_rows=48)):
+        with pytest.raises(pk.PackCacheError):
+            stack(**bad)
+    s = stack(max_seqs=2, max_rows=256)
+    a, b, c = s.open(), s.open(), s.open()
+    s.begin([a, b], [100, 256])
+    free = s.free_pages()
+    for seqs, rows, kw in (([a, b, c], 1, {}), ([a, a], 1, {}), ([], 1, {}), ([a, b], [1], {}), ([a], [-1], {}), ([b], 1, {}), ([99], 1, {}),
+                           ([a, c], [100, 256], {}), ([a], 1, dict(max_len=100)), ([a], 1, dict(max_len=257))):
+        with pytest.raises(ValueError):
+            s.begin(seqs, rows, **kw)
+        assert s.free_pages() == free and [s.rows(q) for q in (a, b, c)] == [100, 256, 0]      # as it was
+    s.begin([a], 1)
+    Q, K = torch.zeros((4, 1, 64), dtype=torch.bfloat16), torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        s.attend(2, Q, K, K, None)
+    with pytest.raises(ValueError):
+        s.attend(0, torch.zeros((4, 2, 64)), K, K, None)
+    s.close(c)
+    with pytest.raises(ValueError):
+        s.attend(0, Q, K, K, None)           # the step is over
+    for f in (s.close, s.fork, s.rows):
+        with pytest.raises(ValueError):
+            f(c)
