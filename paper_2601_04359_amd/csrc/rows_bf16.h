@@ -1,4 +1,5 @@
-// The bf16 forms of the attention on several sequences (D = 128, gfx950 only), on the 32x32x16 bf16 MFMA.
+// The bf16 forms of the attention on several sequences (gfx950 only), on the 32x32x16 bf16 MFMA: one for D = 64 and 128, two for
+// 128.
 //
 // Scores are formed transposed, S^T = K Q^T: a lane holds ONE query (column l % 32) and 16 of 32 keys (with g = l / 32, keys
 // 8 i + 4 g .. + 3, i = 0 .. 3), so that a row's limit, reference and sum are per-lane numbers and the probabilities are
@@ -29,9 +30,10 @@ __device__ __forceinline__ u32x4 finite_bf16(u32x4 v) {   // those as zeros
   return v;
 }
 // Those of a row of V added to a lane's output: dims 32 db + 8 a + 4 g .. + 3 are accumulators 4 a .. of block db.
-__device__ __forceinline__ void add_odd(f32x16 (&o)[4], const uint16_t* v, int g) {
+template <int kBlocks>
+__device__ __forceinline__ void add_odd(f32x16 (&o)[kBlocks], const uint16_t* v, int g) {
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
       const u32x2 w = *reinterpret_cast<const u32x2*>(v + db * 32 + a * 8 + g * 4);
@@ -71,7 +73,7 @@ __device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
 
 // Where a work-group's keys lie.  The page of a tile (its number, -1: none) comes from the lanes' registers, 64 tiles at a
 // time.
-template <bool kPages, int kTile>
+template <bool kPages, int kTile, int D = kD>
 struct KeyTiles {
   const RowsArgs& a;
   const RowSet& r;
@@ -93,30 +95,31 @@ struct KeyTiles {
   __device__ __forceinline__ int page(int i) const { return kPages ? __builtin_amdgcn_readlane(ids, i & 63) : 0; }
   // row `key` of the cache, in elements from Kh or Vh on
   __device__ __forceinline__ int64_t at(int key, int pg) const {
-    if constexpr (kPages) return pg * a.page_stride + static_cast<int64_t>(key - a.by_page.of(key) * a.by_page.d) * kD;
-    return static_cast<int64_t>(r.k0 + key) * kD;
+    if constexpr (kPages) return pg * a.page_stride + static_cast<int64_t>(key - a.by_page.of(key) * a.by_page.d) * D;
+    return static_cast<int64_t>(r.k0 + key) * D;
   }
   // byte offset of chunk `chunk` of row key0 + row of a tile that begins with key0: rows that do not exist are read as the
   // nearest that does
   __device__ __forceinline__ uint32_t offset(int key0, int row, int chunk) const {
-    return (min(max(key0 + row, r.lo), r.n_keys - 1) - key0) * kRowBytes + chunk * 16;
+    return (min(max(key0 + row, r.lo), r.n_keys - 1) - key0) * (2 * D) + chunk * 16;
   }
 };
 
 // The end of a work-group whose waves share rows: wave w has (O, m, l) of rows 32 (w % kR) .. + 31 of the tile over its part of
 // the keys.  Piece i of a wave's O = accumulators 4 i .. + 3 of every lane = dims 8 i + 4 g .. + 3 of its row, lanes permuted by
 // i so that the reads use every bank; a thread adds up eight dims of a row, in the order of the waves, and rows leave whole.
-constexpr int kWaveOBytes = 32 * kD * 4;
-template <int kR, int kG>
-__device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, lds_u8* smem, const f32x16 (&o)[4], float m, float l,
+template <int D>
+constexpr int kWaveOBytes = 32 * D * 4;
+template <int D, int kR, int kG>
+__device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, lds_u8* smem, const f32x16 (&o)[D / 32], float m, float l,
                                             int wave, int lane) {
   constexpr int kWaves = kR * kG;
   auto piece = [&](int w, int i, int of_lane) {
-    return reinterpret_cast<lds_f32x4*>(smem + w * kWaveOBytes + i * 1024 + (of_lane ^ i) * 16);
+    return reinterpret_cast<lds_f32x4*>(smem + w * kWaveOBytes<D> + i * 1024 + (of_lane ^ i) * 16);
   };
-  auto* s_ml = reinterpret_cast<__attribute__((address_space(3))) float*>(smem + kWaves * kWaveOBytes);
+  auto* s_ml = reinterpret_cast<__attribute__((address_space(3))) float*>(smem + kWaves * kWaveOBytes<D>);
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       *piece(wave, db * 4 + q, lane) = f32x4{o[db][q * 4], o[db][q * 4 + 1], o[db][q * 4 + 2], o[db][q * 4 + 3]};
@@ -125,12 +128,13 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
     s_ml[(wave * 32 + lane) * 2 + 1] = l;
   }
   __syncthreads();
-  const int i = threadIdx.x & 15, n_set = r.n_tok * a.rep;
+  constexpr int kThreads = D / 8, kPass = kWaves * 64 / kThreads;   // threads of a row, rows at a time
+  const int i = threadIdx.x % kThreads, n_set = r.n_tok * a.rep;
 #pragma unroll
-  for (int pass = 0; pass < 8 * kR / kWaves; ++pass) {
-    const int in_tile = pass * 4 * kWaves + (threadIdx.x >> 4), rg = in_tile >> 5, row = in_tile & 31;
+  for (int pass = 0; pass * kPass < 32 * kR; ++pass) {
+    const int in_tile = pass * kPass + threadIdx.x / kThreads, rg = in_tile >> 5, row = in_tile & 31;
     const int rho = r.tile * 32 * kR + in_tile;
-    if (rho >= n_set) return;
+    if (in_tile >= 32 * kR || rho >= n_set) return;
     float mw[kG], M = kNothing, L = 0.f;
 #pragma unroll
     for (int w = 0; w < kG; ++w) {
@@ -150,7 +154,7 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
     if (a.part_o != nullptr) {
       const int64_t at = static_cast<int64_t>(r.slot) * a.slot_rows + in_tile;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(a.part_o + at * kD + i * 8 + h * 4) = acc[h];
+      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(a.part_o + at * D + i * 8 + h * 4) = acc[h];
       if (i == 0) a.part_ml[at] = make_float2(M, L);
       continue;
     }
@@ -164,7 +168,7 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
         out[h * 2 + 1] = pack_bf16x2(acc[h][2] * inv, acc[h][3] * inv);
       }
     }
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.O) + head * a.o_stride + t * kD + i * 8) = out;
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.O) + head * a.o_stride + t * D + i * 8) = out;
     if (a.lse != nullptr && i == 0) a.lse[head * static_cast<int64_t>(a.T) + t] = none ? -INFINITY : lse_of(M, L);
   }
 }
@@ -175,26 +179,32 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
 // (O, m, l) of the waves are merged through LDS once.  Bound: the bytes of K and V, or latency.
 // ------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 8;
-constexpr int kFewTileBytes = kFewKeys * kRowBytes;
-constexpr int kFewWaveBytes = kWaveOBytes;     // a wave's O; while it runs, a step's K and V
-constexpr size_t kFewSmem = kFewWaves * (kFewWaveBytes + 32 * 8) + kFewRows * kRowBytes;
-static_assert(2 * kFewTileBytes <= kFewWaveBytes, "a wave's K and V");
+template <int D>
+constexpr size_t kFewSmem = kFewWaves * (kWaveOBytes<D> + 32 * 8) + kFewRows * D * 2;
 
-template <bool kPages>
+template <int D, bool kPages>
 __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds_u8* smem) {
+  constexpr int kRow = 2 * D, kTileBytes = kFewKeys * kRow;   // a row in LDS, a step's K or V
+  constexpr int kChunks = kRow / 16, kRows = 64 / kChunks;    // 16-byte chunks of a row, rows of a load of 1 KB
+  constexpr int kSteps = D / 16, kBlocks = D / 32;
+  static_assert(2 * kTileBytes <= kWaveOBytes<D>, "a wave's K and V lie where its O goes");
+  // Where chunk c of row r lies.  Rows of 128 bytes: two rows make 256 bytes, and what a quarter wave reads (one chunk of 16
+  // rows of K, two chunks of four rows of V) uses every bank there too.
+  auto k_pos = [](int row, int chunk) { return D == 128 ? k_chunk_pos(row, chunk) : chunk ^ ((row >> 1) & 7); };
+  auto v_pos = [](int row, int chunk) { return D == 128 ? v_chunk_pos(row, chunk) : chunk ^ (((row >> 1) & 3) << 1); };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g = lane >> 5;
   const int n_set = r.n_tok * a.rep;
-  const lds_u8* lds = smem + wave * kFewWaveBytes;
+  const lds_u8* lds = smem + wave * kWaveOBytes<D>;
   const uint32_t lds_w = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-  const lds_u8* q_tile = smem + kFewWaves * (kFewWaveBytes + 32 * 8);
-  KeyTiles<kPages, kFewKeys> keys(a, r, wave, kFewWaves, lane);
+  const lds_u8* q_tile = smem + kFewWaves * (kWaveOBytes<D> + 32 * 8);
+  KeyTiles<kPages, kFewKeys, D> keys(a, r, wave, kFewWaves, lane);
   keys.fetch(0, r.end);
 
-  {   // four query rows per wave
-    const int row = wave * 4 + (lane >> 4), rho = min(r.tile * kFewRows + row, n_set - 1);
+  if (wave * kRows < kFewRows) {   // four query rows per wave (D = 64: eight of each of the first four waves)
+    const int row = wave * kRows + lane / kChunks, rho = min(r.tile * kFewRows + row, n_set - 1);
     const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
-    dma_16B(static_cast<const uint16_t*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * kD + k_chunk_pos(row, lane & 15) * 8,
+    dma_16B(static_cast<const uint16_t*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * D + k_pos(row, lane % kChunks) * 8,
             static_cast<uint32_t>(reinterpret_cast<uintptr_t>(q_tile)) + wave * 1024);
   }
   auto stage = [&](int i) {   // step i of this wave: 32 rows of K and of V; false: they are nobody's
@@ -204,10 +214,10 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
     const int64_t at = keys.at(k0, pg);
     const uint16_t *kb = keys.Kh + at, *vb = keys.Vh + at;
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const int row = p * 4 + (lane >> 4), pos = lane & 15;
-      dma_16B_at(kb, keys.offset(k0, row, k_chunk_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + p * 1024));
-      dma_16B_at(vb, keys.offset(k0, row, v_chunk_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + kFewTileBytes + p * 1024));
+    for (int p = 0; p < kFewKeys / kRows; ++p) {
+      const int row = p * kRows + lane / kChunks, pos = lane % kChunks;
+      dma_16B_at(kb, keys.offset(k0, row, k_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + p * 1024));
+      dma_16B_at(vb, keys.offset(k0, row, v_pos(row, pos)), __builtin_amdgcn_readfirstlane(lds_w + kTileBytes + p * 1024));
     }
     return true;
   };
@@ -225,26 +235,26 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
   const int end = min(r.end, __builtin_amdgcn_readfirstlane(lim_max));
   lim_min = __builtin_amdgcn_readfirstlane(lim_min);
 
-  int k_off[8], v_off[4];
+  int k_off[kSteps], v_off[kBlocks];
 #pragma unroll
-  for (int s = 0; s < 8; ++s) k_off[s] = l32 * kRowBytes + k_chunk_pos(l32, 2 * s + g) * 16;
+  for (int s = 0; s < kSteps; ++s) k_off[s] = l32 * kRow + k_pos(l32, 2 * s + g) * 16;
   {
     const int r16 = lane & 15, G = (lane >> 4) & 1, row = g * 4 + (r16 >> 2);
 #pragma unroll
-    for (int db = 0; db < 4; ++db) {
+    for (int db = 0; db < kBlocks; ++db) {
       const int dim = db * 32 + G * 16 + 4 * (r16 & 3);
-      v_off[db] = kFewTileBytes + row * kRowBytes + v_chunk_pos(row, dim >> 3) * 16 + (dim & 7) * 2;
+      v_off[db] = kTileBytes + row * kRow + v_pos(row, dim >> 3) * 16 + (dim & 7) * 2;
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  bf16x8 qf[8];
+  bf16x8 qf[kSteps];
 #pragma unroll
-  for (int s = 0; s < 8; ++s) qf[s] = lds_frag(q_tile + k_off[s]);
+  for (int s = 0; s < kSteps; ++s) qf[s] = lds_frag(q_tile + k_off[s]);
 
-  f32x16 o[4];
+  f32x16 o[kBlocks];
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m = kNothing, l = 0.f;
@@ -256,18 +266,18 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
     // This step's rows have landed (they are all that is in flight): every fragment goes to registers, so that the next
     // step's rows can be fetched into the same LDS at once.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    bf16x8 kf[8], vf[2][4];
+    bf16x8 kf[kSteps], vf[2][kBlocks];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) kf[s] = lds_frag(lds + k_off[s]);
+    for (int s = 0; s < kSteps; ++s) kf[s] = lds_frag(lds + k_off[s]);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        const lds_u8* src = lds + v_off[db] + ks * 16 * kRowBytes;
+      for (int db = 0; db < kBlocks; ++db) {
+        const lds_u8* src = lds + v_off[db] + ks * 16 * kRow;
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
             reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(src)));
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-            reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(src + 8 * kRowBytes)));
+            reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(const_cast<lds_u8*>(src + 8 * kRow)));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           vf[ks][db][e] = lo[e];
@@ -275,11 +285,11 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
         }
       }
 #pragma unroll
-    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(kf[s]));
+    for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(kf[s]));
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(vf[ks][db]));
+      for (int db = 0; db < kBlocks; ++db) asm volatile("" : "+v"(vf[ks][db]));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (kPages && (i & 63) == 63) keys.fetch(i + 1, r.end);
     there = keys.key_of(i + 1) < end && stage(i + 1);
@@ -289,21 +299,21 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
+    for (int s = 0; s < kSteps; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
     if (k0 + kFewKeys > lim_min || k0 < r.lo) {
       hide(sc, r.lo - k0 - g * 4, lim - k0 - g * 4);
       uint32_t odd = 0;   // 0 times what is not finite would reach rows that do not see it
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int db = 0; db < 4; ++db) odd |= odd_bf16(__builtin_bit_cast(u32x4, vf[ks][db]));
+        for (int db = 0; db < kBlocks; ++db) odd |= odd_bf16(__builtin_bit_cast(u32x4, vf[ks][db]));
       if (__any(odd != 0)) {
         for (int j = max(k0, r.lo); j < min(k0 + kFewKeys, r.n_keys); ++j)
-          if (j < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(j - k0) * kD, g);
+          if (j < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(j - k0) * D, g);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-          for (int db = 0; db < 4; ++db) vf[ks][db] = __builtin_bit_cast(bf16x8, finite_bf16(__builtin_bit_cast(u32x4, vf[ks][db])));
+          for (int db = 0; db < kBlocks; ++db) vf[ks][db] = __builtin_bit_cast(bf16x8, finite_bf16(__builtin_bit_cast(u32x4, vf[ks][db])));
       }
     }
     float mx = sc[0];
@@ -315,7 +325,7 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
       const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
       l *= alpha;
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
+      for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[db][e] *= alpha;
       ref = m = m_new;
@@ -338,12 +348,12 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int db = 0; db < 4; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][db], p[ks], o[db], 0, 0, 0);
+      for (int db = 0; db < kBlocks; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][db], p[ks], o[db], 0, 0, 0);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // a first step that was needed by none may be in flight
   l = wave_half_sum(l);
 
-  merge_waves<1, kFewWaves>(a, r, smem, o, m, l, wave, lane);
+  merge_waves<D, 1, kFewWaves>(a, r, smem, o, m, l, wave, lane);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -609,13 +619,13 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
 // come through L2 twice as often per product.
 // ------------------------------------------------------------------------------------------
 constexpr int kMidWaves = 4, kMidRows = 64;
-constexpr size_t kMidSmem = kMidWaves * (kWaveOBytes + 32 * 8);
+constexpr size_t kMidSmem = kMidWaves * (kWaveOBytes<kD> + 32 * 8);
 
 template <bool kUnitC, bool kPages>
 __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds_u8* smem) {
   constexpr int kR = 2, kG = 2, kS = 2;   // row groups, key groups, slots per operand and key group
   constexpr int kKeys = 32 * kG, kTile = kKeys * kRowBytes;   // of a phase
-  static_assert(2 * kS * kTile <= kMidWaves * kWaveOBytes, "tiles");
+  static_assert(2 * kS * kTile <= kMidWaves * kWaveOBytes<kD>, "tiles");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g = lane >> 5, rg = wave % kR, kg = wave / kR;
   const int n_set = r.n_tok * a.rep, row_first = (r.tile * kR + rg) * 32;
@@ -673,7 +683,7 @@ __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds
     lim_min = min(lim_min, __shfl_xor(lim_min, x));
   }
   lim_min = __builtin_amdgcn_readfirstlane(lim_min);   // of the wave
-  auto* s_lim = reinterpret_cast<__attribute__((address_space(3))) int*>(smem + kMidWaves * kWaveOBytes);   // behind the tiles
+  auto* s_lim = reinterpret_cast<__attribute__((address_space(3))) int*>(smem + kMidWaves * kWaveOBytes<kD>);   // behind the tiles
   if (lane == 0 && kg == 0) s_lim[rg * 2] = active ? lim_max : 0, s_lim[rg * 2 + 1] = active ? lim_min : INT_MAX;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();   // K(0), V(0), K(1) and the limits
@@ -812,15 +822,15 @@ __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   }
   __syncthreads();   // every wave has read its last tile; LDS takes the rows
-  merge_waves<kR, kG>(a, r, smem, o, m_end, l_tot, wave, lane);
+  merge_waves<kD, kR, kG>(a, r, smem, o, m_end, l_tot, wave, lane);
 }
 
 // ---- the kernels -----------------------------------------------------------------------------------------------------
-template <bool kPages>
-__global__ __launch_bounds__(kFewWaves * 64, 1) void rows_few_kernel(RowsArgs a) {
+template <int D, bool kPages>
+__global__ __launch_bounds__(kFewWaves * 64, D == 64 ? 4 : 1) void rows_few_kernel(RowsArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   lds_u8* smem = (lds_u8*)smem_raw;
-  each_unit<kFewRows, kPages>(a, (lds_int*)(smem + kFewSmem), [&](const RowSet& r) { rows_few<kPages>(a, r, smem); });
+  each_unit<kFewRows, kPages>(a, (lds_int*)(smem + kFewSmem<D>), [&](const RowSet& r) { rows_few<D, kPages>(a, r, smem); });
 }
 template <bool kUnitC, bool kPages>
 __global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a) {

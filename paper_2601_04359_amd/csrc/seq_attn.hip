@@ -7,212 +7,15 @@
 #include <vector>
 
 #include "rows_bf16.h"
+#include "rows_f32.h"
 
 namespace pc {
 namespace {
 
-// ------------------------------------------------------------------------------------------
-// The general form: any type and D, on the 16x16x4 fp32 MFMA.  A work-group has 16 query rows, its four waves take the keys
-// in steps of 16 by turns and merge their (O, m, l) through LDS once.
-//   * S^T = K Q^T: lane (r = l % 16, kg = l / 16) holds key row r, dims 16 s + 4 kg .. + 3; the four products of step s contract
-//     over (kg, element), the same permutation of the head dimension on both operands.
-//   * The result leaves lane (q = l % 16, kg) with keys 4 kg .. + 3 of its query: P^T is the B operand of O^T += V^T P^T
-//     (product e contracts over keys 4 kg + e), and row r of output block (db, e) stands for dim 64 db + 4 r + e, so that V
-//     comes in 16-byte pieces and O leaves in them.
-//   * A score is s (c + c_lo), and the reference is subtracted from the rounded product: the largest key's exponent is 0
-//     however large the logits are.
-//   * A key that a row does not see has p = 0, and 0 times a NaN in V would reach the row: in steps where some row does not
-//     see all keys, values that are not finite are taken out of the product and added to the rows that see them.
-// ------------------------------------------------------------------------------------------
-constexpr int kGenRows = 16, kGenWaves = 4, kGenKeys = 16;
-
-template <typename T>
-__device__ __forceinline__ f32x4 load4(const T* p) {
-  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const f32x4*>(p);
-  const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-  return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
-               __uint_as_float(v[1] & 0xFFFF0000u)};
-}
 template <typename T>
 __device__ __forceinline__ void store4(T* p, f32x4 v) {
   if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = v;
   else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-}
-
-template <typename T, int D, bool kPages>
-__device__ __forceinline__ void rows_general(const RowsArgs& a, const RowSet& r, float (&o_lds)[kGenWaves][kGenRows][D],
-                                             float2 (&ml_lds)[kGenWaves][kGenRows]) {
-  constexpr int kSteps = D / 16, kBlocks = D / 64;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r16 = lane & 15, kg = lane >> 4;
-  const int n_set = r.n_tok * a.rep, rho = min(r.tile * kGenRows + r16, n_set - 1);
-  const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
-  const int lim = limit_of(a, r, tok);
-  int lim_max = lim, lim_min = lim > 0 ? lim : INT_MAX;   // over the rows that see something
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) {
-    lim_max = max(lim_max, __shfl_xor(lim_max, x));
-    lim_min = min(lim_min, __shfl_xor(lim_min, x));
-  }
-  const int end = min(r.end, __builtin_amdgcn_readfirstlane(lim_max));
-  lim_min = __builtin_amdgcn_readfirstlane(lim_min);
-
-  f32x4 qf[kSteps];
-  const T* q = static_cast<const T*>(a.Q) + head * a.q_stride + static_cast<int64_t>(r.t0 + tok) * D + kg * 4;
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) qf[s] = load4(q + s * 16);
-
-  const T* Kh = static_cast<const T*>(a.K) + r.kvh * a.k_stride;
-  const T* Vh = static_cast<const T*>(a.V) + r.kvh * a.v_stride;
-  f32x4 acc[kBlocks][4];
-#pragma unroll
-  for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[db][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = kNothing, l = 0.f;
-
-  for (int kb = r.begin + wave * kGenKeys; kb < end; kb += kGenWaves * kGenKeys) {
-    int64_t base;   // of row 0 of what the keys of this step lie in, elements
-    int first = 0;  // and the key that is row 0
-    if constexpr (kPages) {
-      const int in_table = a.by_page.of(kb), page = r.pages[in_table];
-      if (page < 0 || page >= a.n_pages) continue;
-      base = page * a.page_stride, first = in_table * a.by_page.d;
-    } else {
-      base = static_cast<int64_t>(r.k0) * D;
-    }
-    const int last = r.n_keys - 1;
-    auto row = [&](int j) { return base + static_cast<int64_t>(min(max(j, r.lo), last) - first) * D; };
-    if (kb + kGenKeys <= r.lo) continue;   // every key of the step lies in front: row() must not reach another page
-    f32x4 kf[kSteps], vf[4][kBlocks];
-    {
-      const T* p = Kh + row(kb + r16) + kg * 4;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) kf[s] = load4(p + s * 16);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const T* p = Vh + row(kb + kg * 4 + e) + r16 * 4;
-#pragma unroll
-      for (int db = 0; db < kBlocks; ++db) vf[e][db] = load4(p + db * 64);
-    }
-    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[s][e], qf[s][e], sc, 0, 0, 0);
-    float x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = fmaf(sc[e], a.c, sc[e] * a.c_lo);
-    if (kb + kGenKeys > lim_min || kb < r.lo) {
-      bool odd = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = kb + kg * 4 + e;
-        if (j >= lim || j < r.lo) x[e] = -INFINITY;
-#pragma unroll
-        for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) odd |= not_finite(vf[e][db][i]);
-      }
-      if (__any(odd)) {
-        for (int k = 0; k < kGenKeys; ++k) {
-          const int j = kb + k;
-          if (j >= lim || j < r.lo) continue;
-#pragma unroll
-          for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
-              const f32x4 v = load4(Vh + row(j) + db * 64 + kg * 16 + i * 4);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (not_finite(v[e])) acc[db][e][i] += v[e];
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (not_finite(vf[e][db][i])) vf[e][db][i] = 0.f;
-      }
-    }
-    float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    if (__any(mx > m)) {
-      const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[db][e] *= alpha;
-      m = m_new;
-    }
-    float p[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(x[e] - m);
-      l += p[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[db][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][db][i], p[e], acc[db][i], 0, 0, 0);
-  }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-
-#pragma unroll
-  for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(&o_lds[wave][r16][db * 64 + kg * 16 + i * 4]) = f32x4{acc[db][0][i], acc[db][1][i], acc[db][2][i], acc[db][3][i]};
-  if (kg == 0) ml_lds[wave][r16] = make_float2(m, l);
-  __syncthreads();
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;   // 16 threads per row, D / 16 dims each
-  const int rho_w = r.tile * kGenRows + row;
-  if (rho_w >= n_set) return;
-  float M = kNothing, L = 0.f;
-#pragma unroll
-  for (int w = 0; w < kGenWaves; ++w) M = fmaxf(M, ml_lds[w][row].x);
-  f32x4 out[kBlocks];
-#pragma unroll
-  for (int db = 0; db < kBlocks; ++db) out[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < kGenWaves; ++w) {
-    const float2 ml = ml_lds[w][row];
-    const float by = __builtin_amdgcn_exp2f(ml.x - M);
-    L += by * ml.y;
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db) out[db] += by * *reinterpret_cast<const f32x4*>(&o_lds[w][row][db * 64 + c * 4]);
-  }
-  const int tok_w = a.by_rep.of(rho_w), head_w = r.kvh * a.rep + rho_w - tok_w * a.rep;
-  const int64_t t = r.t0 + tok_w;
-  if (a.part_o != nullptr) {
-    const int64_t at = static_cast<int64_t>(r.slot) * a.slot_rows + row;
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db) *reinterpret_cast<f32x4*>(a.part_o + at * D + db * 64 + c * 4) = out[db];
-    if (c == 0) a.part_ml[at] = make_float2(M, L);
-    return;
-  }
-  const bool none = limit_of(a, r, tok_w) <= r.lo;
-  const float inv = none ? 0.f : 1.f / L;
-#pragma unroll
-  for (int db = 0; db < kBlocks; ++db)
-    store4(static_cast<T*>(a.O) + head_w * a.o_stride + t * D + db * 64 + c * 4, none ? f32x4{0.f, 0.f, 0.f, 0.f} : out[db] * inv);
-  if (a.lse != nullptr && c == 0) a.lse[head_w * static_cast<int64_t>(a.T) + t] = none ? -INFINITY : lse_of(M, L);
-}
-
-template <typename T, int D, bool kPages>
-__global__ __launch_bounds__(kGenWaves * 64) void rows_general_kernel(RowsArgs a) {
-  __shared__ float o_lds[kGenWaves][kGenRows][D];
-  __shared__ float2 ml_lds[kGenWaves][kGenRows];
-  __shared__ int plan[kPages ? kPlanBytes / 4 : 1];
-  each_unit<kGenRows, kPages>(a, (lds_int*)plan, [&](const RowSet& r) { rows_general<T, D, kPages>(a, r, o_lds, ml_lds); });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -296,8 +99,8 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
-enum Form { kGeneral, kFew, kMid, kMany };
-int rows_of(Form f) { return f == kGeneral ? kGenRows : f == kFew ? kFewRows : f == kMid ? kMidRows : kManyRows; }
+enum Form { kF32One, kF32Two, kFew, kMid, kMany };
+int rows_of(Form f) { return f == kF32One ? 16 : f == kF32Two ? 32 : f == kFew ? kFewRows : f == kMid ? kMidRows : kManyRows; }
 
 // Microseconds that `groups` work-groups of a bf16 form take, `steps` steps in all and `longest` in the one with the most (256
 // keys for kFew, 64 for the others).  Either they fill the chip (what a work-group costs beside its steps, and a step, in time
@@ -318,7 +121,17 @@ constexpr Cost kPromptCost[3] = {{5.0, 1.75, 1.75, 2.5, 3.6, 1.25}, {7.5, 0.75, 
 // 41,800 common rows, us:
 //   few | mid | many   8 tokens: 23 | 25 | 27   16: 35 | 28 | 31   64: 54 | 52 | 52   256: 161 | 139 | 132
 constexpr Cost kPagesCost[3] = {{3.9, 1.58, 1.58, 2.65, 5.3, 1.48}, {4.9, 1.0, 1.0, 8.0, 2.0, 0.58}, {4.8, 1.44, 1.44, 9.8, 0.1, 0.993}};
-int keys_per_step(Form f) { return f == kFew ? 256 : 64; }
+// fp32, D = 128 and 64 (from prompts of 40 to 1,200 rows).  Both sides, 16 | 32 rows, us: 8/2 heads x 1,200 rows, D = 128, 51 | 62;
+// two such prompts 94 | 84; 24/8 x 1,200 and 700 187 | 140.
+constexpr Cost kF32Cost[2][2] = {{{5.5, 3.2, 3.75, 3.0, 2.0, 3.6}, {6.5, 2.7, 2.9, 3.0, 2.0, 2.8}},
+                                 {{3.2, 2.1, 2.1, 3.0, 1.5, 1.6}, {5.3, 1.4, 1.5, 3.0, 1.5, 1.45}}};
+const Cost& cost_of(Form f, int D, bool pages) {
+  return f <= kF32Two ? kF32Cost[D == 64][f] : (pages ? kPagesCost : kPromptCost)[f - kFew];
+}
+int keys_per_step(Form f) { return f == kFew ? 256 : f == kF32One ? 128 : 64; }
+// The forms that a call may take: first .. last.
+Form first_form(int dtype) { return dtype == PC_F32 ? kF32One : kFew; }
+Form last_form(int dtype, int D) { return dtype == PC_F32 ? kF32Two : D == kD ? kMany : kFew; }
 
 int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
   if (offs == nullptr) return n_seq * ceil_div(T / n_seq * rep, rows);
@@ -332,7 +145,7 @@ int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
 // the costs above there are the bytes of K and V (5.5 TB/s), and the shares' join: a launch, and the fp32 rows that are written
 // and read (4.3 TB/s).
 struct PagePlan {
-  Form form = kGeneral;
+  Form form = kF32One;
   int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
   int own_tiles = 0, own_parts = 0, own_cap = 0;   // own_parts 0: the device cuts
   int slot_rows = 0, slots = 1024, least_keys = 4 * kPageStep;
@@ -352,17 +165,13 @@ struct PagePlan {
       parts = shared_parts + ceil_div(own, share);
     };
     const int longest = std::max(n_shared, own), whole = ceil_div(longest, kPageStep) * kPageStep;
-    if (dtype != PC_BF16 || D != kD) {
-      take(kGeneral, kPageStep);
-      const int tiles = std::max(1, shared_tiles + own_tiles) * Hkv;
-      const int shares = std::max(1, std::min({1024 / tiles, longest / 256, 64}));
-      take(kGeneral, ceil_div(ceil_div(longest, shares), kPageStep) * kPageStep);
-    } else {
-      const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 4.0 * kD / 5.5e6;
+    {
+      const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 2.0 * D * (dtype == PC_BF16 ? 2 : 4) / 5.5e6;
       double best = 1e30;
-      Form best_form = kFew;
+      Form best_form = first_form(dtype);
       int best_share = whole;
-      for (Form f : {kFew, kMid, kMany}) {
+      for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
+        const Form f = static_cast<Form>(i);
         const int step = keys_per_step(f);
         for (int share = 256;; share = std::max(share + 64, share * 5 / 4 / kPageStep * kPageStep)) {
           share = std::min(share, whole);
@@ -370,8 +179,8 @@ struct PagePlan {
           if (parts <= 96) {
             const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * ceil_div(own, share));
             const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
-            const double join = parts > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts * 1040.0 / 4.3e6 : 0.0;
-            const double cost = std::max(kPagesCost[f - kFew](groups, steps, ceil_div(share, step)), bytes_us) + join;
+            const double join = parts > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts * (8.0 * D + 16) / 4.3e6 : 0.0;
+            const double cost = std::max(cost_of(f, D, true)(groups, steps, ceil_div(share, step)), bytes_us) + join;
             if (cost < best) best = cost, best_form = f, best_share = share;
           }
           if (share >= whole) break;
@@ -421,14 +230,21 @@ int check_attn(const char* who, int dtype, int Hq, int Hkv, int D, float scale) 
 
 template <bool kPages>
 int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a, int blocks, hipStream_t s) {
-  if (form == kGeneral) {
-    auto* kernel = dtype == PC_BF16 ? (D == 128 ? rows_general_kernel<uint16_t, 128, kPages> : rows_general_kernel<uint16_t, 64, kPages>)
-                                    : (D == 128 ? rows_general_kernel<float, 128, kPages> : rows_general_kernel<float, 64, kPages>);
-    kernel<<<blocks, kGenWaves * 64, 0, s>>>(a);
+  if (form == kF32One || form == kF32Two) {
+    static std::atomic<uint64_t> ok[4];
+    const bool two = form == kF32Two;
+    auto* kernel = D == 128 ? (two ? rows_f32_kernel<128, kPages, 2, 4> : rows_f32_kernel<128, kPages, 1, 8>)
+                            : (two ? rows_f32_kernel<64, kPages, 2, 4> : rows_f32_kernel<64, kPages, 1, 8>);
+    const size_t bytes = (D == 128 ? kF32Smem<128, 2, 4> : kF32Smem<64, 2, 4>) + kPlanBytes;
+    static_assert(kF32Smem<128, 2, 4> == kF32Smem<128, 1, 8> && kF32Smem<64, 2, 4> == kF32Smem<64, 1, 8>, "the waves' O");
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[(D == 128) * 2 + two], who)) return rc;
+    kernel<<<blocks, (two ? 4 : 8) * 64, bytes, s>>>(a);
   } else if (form == kFew) {
-    static std::atomic<uint64_t> ok;
-    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(rows_few_kernel<kPages>), kFewSmem + kPlanBytes, ok, who)) return rc;
-    rows_few_kernel<kPages><<<blocks, kFewWaves * 64, kFewSmem + kPlanBytes, s>>>(a);
+    static std::atomic<uint64_t> ok[2];
+    auto* kernel = D == 128 ? rows_few_kernel<128, kPages> : rows_few_kernel<64, kPages>;
+    const size_t bytes = (D == 128 ? kFewSmem<128> : kFewSmem<64>) + kPlanBytes;
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[D == 128], who)) return rc;
+    kernel<<<blocks, kFewWaves * 64, bytes, s>>>(a);
   } else {
     static std::atomic<uint64_t> ok[4];
     const bool unit_c = a.c == 1.0f, many = form == kMany;
@@ -496,10 +312,10 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
     const int n = static_cast<int>(std::min<size_t>(kSeqs, seqs.size() - s0));
     a.seqs.n = n, a.seqs.per = 0;
     // the form with the lowest estimate
-    Form form = kGeneral;
+    Form form = kF32One;
     double best = 1e30;
-    for (Form f : {kFew, kMid, kMany}) {
-      if (dtype != PC_BF16 || D != kD) break;
+    for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
+      const Form f = static_cast<Form>(i);
       double groups = 0, steps = 0, longest = 0;
       for (int s = 0; s < n; ++s) {
         const Seq& q = seqs[s0 + s];
@@ -508,7 +324,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
         steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
         longest = std::max(longest, std::ceil(last / keys_per_step(f)));
       }
-      const double cost = kPromptCost[f - kFew](groups, steps, longest);
+      const double cost = cost_of(f, D, false)(groups, steps, longest);
       if (cost < best) best = cost, form = f;
     }
     const int rows = rows_of(form);
@@ -600,7 +416,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     a.own_parts = plan.own_parts, a.own_keys = plan.shared_keys, a.by_parts = Divisor(std::max(1, plan.own_parts * a.tiles_per_seq));
     a.own_cap = plan.own_cap, a.slots = plan.slots, a.slot_rows = plan.slot_rows, a.by_tile = Divisor(rows_of(plan.form));
     a.unit_us = plan.form == kFew ? 4.5f : 5.f;
-    a.key_us = plan.form == kGeneral ? 0.04f : plan.form == kFew ? 0.0059f : plan.form == kMid ? 0.0156f : 0.0225f;
+    a.key_us = dtype == PC_F32 ? 0.025f : plan.form == kFew ? 0.0059f : plan.form == kMid ? 0.0156f : 0.0225f;
     a.step_bytes_us = 2.f * kPageStep * D * elt / 5.5e6f;
     a.least_keys = plan.least_keys;
     a.part_o = nullptr, a.part_ml = nullptr, a.cut = nullptr;

@@ -289,7 +289,11 @@ __device__ __forceinline__ void each_unit(const RowsArgs& a, lds_int* plan, Body
   }
 }
 
-__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u; }
+// All ones for a number that is not finite, else 0: an exponent of ones carries into the sign.  (By whole words, so that no
+// comparison takes a pair of scalar registers of its own.)
+__device__ __forceinline__ uint32_t odd_mask(float v) {
+  return static_cast<uint32_t>(static_cast<int32_t>((__float_as_uint(v) & 0x7F800000u) + 0x00800000u) >> 31);
+}
 
 // ln(2^m l), rounded once: m may reach hundreds where l's logarithm is small
 __device__ __forceinline__ float lse_of(float m, float l) {
