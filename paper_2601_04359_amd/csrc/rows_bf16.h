@@ -832,17 +832,35 @@ __global__ __launch_bounds__(kFewWaves * 64, D == 64 ? 4 : 1) void rows_few_kern
   lds_u8* smem = (lds_u8*)smem_raw;
   each_unit<kFewRows, kPages>(a, (lds_int*)(smem + kFewSmem<D>), [&](const RowSet& r) { rows_few<D, kPages>(a, r, smem); });
 }
-template <bool kUnitC, bool kPages>
+template <bool kUnitC>
 __global__ __launch_bounds__(kMidWaves * 64, 2) void rows_mid_kernel(RowsArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   lds_u8* smem = (lds_u8*)smem_raw;
-  each_unit<kMidRows, kPages>(a, (lds_int*)(smem + kMidSmem), [&](const RowSet& r) { rows_mid<kUnitC, kPages>(a, r, smem); });
+  each_unit<kMidRows, true>(a, (lds_int*)(smem + kMidSmem), [&](const RowSet& r) { rows_mid<kUnitC, true>(a, r, smem); });
 }
-template <bool kUnitC, bool kPages>
+template <bool kUnitC>
 __global__ __launch_bounds__(kManyWaves * 64, 2) void rows_many_kernel(RowsArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   lds_u8* smem = (lds_u8*)smem_raw;
-  each_unit<kManyRows, kPages>(a, (lds_int*)(smem + kManySmem), [&](const RowSet& r) { rows_many<kUnitC, kPages>(a, r, smem); });
+  each_unit<kManyRows, true>(a, (lds_int*)(smem + kManySmem), [&](const RowSet& r) { rows_many<kUnitC, true>(a, r, smem); });
+}
+// Prompts take both forms in one launch: the n_heavy longest tiles of 128 rows as two of 64, the others whole.  All of them start
+// early, the long ones end as early as 64 rows can, and most products still are those of 128.
+template <bool kUnitC>
+__global__ __launch_bounds__(kManyWaves * 64, 2) void rows_prompt_kernel(RowsArgs a) {
+  static_assert(kMidWaves == kManyWaves && 2 * kMidRows == kManyRows, "one launch");
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  lds_u8* smem = (lds_u8*)smem_raw;
+  const int lane = threadIdx.x & 63;
+  const int u = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - u * a.by_hkv.d;
+  const bool heavy = u < 2 * a.n_heavy;
+  RowSet r = prompt_rows<kManyRows>(a, heavy ? u >> 1 : u - a.n_heavy, kvh, lane);
+  if (heavy) {
+    r.tile = r.tile * 2 + (u & 1);
+    if (r.tile * kMidRows < r.n_tok * a.rep) rows_mid<kUnitC, false>(a, r, smem);
+  } else {
+    rows_many<kUnitC, false>(a, r, smem);
+  }
 }
 
 }  // namespace pc

@@ -140,6 +140,45 @@ int row_tiles(const int32_t* offs, int n_seq, int T, int rep, int rows) {
   return n;
 }
 
+// How pc_prompt_attn cuts a launch: the form with the lowest cost.  kMany: the n_heavy longest tiles (per KV head) are taken as two
+// of 64 rows, those that would take longer than everything together.  16/4 heads, us, with none, all and these of the
+// tiles: one prompt of 4,288 rows 98.6, 98.2, 90.9; nine of 1 to 2,049 rows 49.8, 50.9, 42.7; 6,000 rows 157.7, 180, 157.4.
+struct Seq {
+  int q0, nq, k0, nk;
+};
+struct PromptPlan {
+  Form form;
+  int n_heavy = 0;
+  PromptPlan(int dtype, int D, int Hkv, int rep, const Seq* seqs, int n) {
+    form = first_form(dtype);
+    double best = 1e30, many_us = 0;
+    for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
+      const Form f = static_cast<Form>(i);
+      double groups = 0, steps = 0, longest = 0;
+      for (int s = 0; s < n; ++s) {
+        const double tiles = ceil_div(seqs[s].nq * rep, rows_of(f)), last = std::max(0, seqs[s].nk), first = std::max(0.0, last - seqs[s].nq);
+        groups += tiles * Hkv;
+        steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
+        longest = std::max(longest, std::ceil(last / keys_per_step(f)));
+      }
+      const Cost& cost = cost_of(f, D, false);
+      if (f == kMany) many_us = cost.start + (cost.per_group * groups + cost.step * steps) / 256;
+      const double us = cost(groups, steps, longest);
+      if (us < best) best = us, form = f;
+    }
+    if (form < kMid) return;
+    // tiles with more keys than a work-group of 128 rows adds in the time that all of them take
+    const Cost& cost = cost_of(kMany, D, false);
+    const double x = (many_us - cost.alone) / cost.paired * keys_per_step(kMany);
+    for (int s = 0; s < n; ++s) {
+      const int tiles = ceil_div(seqs[s].nq * rep, kManyRows);
+      const double light = std::floor((x - (seqs[s].nk - seqs[s].nq)) * rep / kManyRows);   // tile i ends at key nk - nq + (i + 1) 128 / rep
+      n_heavy += static_cast<int>(tiles - std::min<double>(std::max(0.0, light), tiles));
+    }
+    form = kMany;
+  }
+};
+
 // How pc_page_attn cuts a launch's work: a form, the shares of the common rows, and room for units over the sequences' own rows,
 // which the device cuts (plan_pages); here their lengths are only known to be max_len at most, and taken to be that.  Beside
 // the costs above there are the bytes of K and V (5.5 TB/s), and the shares' join: a launch, and the fp32 rows that are written
@@ -248,11 +287,14 @@ int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a,
   } else {
     static std::atomic<uint64_t> ok[4];
     const bool unit_c = a.c == 1.0f, many = form == kMany;
-    auto* kernel = many ? (unit_c ? rows_many_kernel<true, kPages> : rows_many_kernel<false, kPages>)
-                        : (unit_c ? rows_mid_kernel<true, kPages> : rows_mid_kernel<false, kPages>);
-    const size_t bytes = (many ? kManySmem : kMidSmem) + kPlanBytes;
-    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[many * 2 + unit_c], who)) return rc;
-    kernel<<<blocks, (many ? kManyWaves : kMidWaves) * 64, bytes, s>>>(a);
+    void (*kernel)(RowsArgs);
+    if constexpr (kPages)
+      kernel = many ? (unit_c ? rows_many_kernel<true> : rows_many_kernel<false>) : (unit_c ? rows_mid_kernel<true> : rows_mid_kernel<false>);
+    else
+      kernel = unit_c ? rows_prompt_kernel<true> : rows_prompt_kernel<false>;
+    constexpr size_t kBytes = std::max(kManySmem, kMidSmem) + (kPages ? kPlanBytes : 0);
+    if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes, ok[many * 2 + unit_c], who)) return rc;
+    kernel<<<blocks, kManyWaves * 64, kBytes, s>>>(a);
   }
   PC_CHECK_LAUNCH(who);
   return PC_OK;
@@ -297,9 +339,6 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
   set_scale(a, scale);
   hipStream_t st = static_cast<hipStream_t>(stream);
   // sequences without rows have nothing to do; the longest come first, so that those of a launch are about as long
-  struct Seq {
-    int q0, nq, k0, nk;
-  };
   std::vector<Seq> seqs;
   try {
     for (int s = 0; s < n_seq; ++s)
@@ -311,24 +350,9 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
   for (size_t s0 = 0; s0 < seqs.size(); s0 += kSeqs) {
     const int n = static_cast<int>(std::min<size_t>(kSeqs, seqs.size() - s0));
     a.seqs.n = n, a.seqs.per = 0;
-    // the form with the lowest estimate
-    Form form = kF32One;
-    double best = 1e30;
-    for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
-      const Form f = static_cast<Form>(i);
-      double groups = 0, steps = 0, longest = 0;
-      for (int s = 0; s < n; ++s) {
-        const Seq& q = seqs[s0 + s];
-        const double tiles = ceil_div(q.nq * rep, rows_of(f)), last = std::max(0, q.nk), first = std::max(0.0, last - q.nq);
-        groups += tiles * Hkv;
-        steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
-        longest = std::max(longest, std::ceil(last / keys_per_step(f)));
-      }
-      const double cost = cost_of(f, D, false)(groups, steps, longest);
-      if (cost < best) best = cost, form = f;
-    }
-    const int rows = rows_of(form);
-    a.n_tiles = 0, a.max_level = 0;
+    const PromptPlan plan(dtype, D, Hkv, rep, seqs.data() + s0, n);
+    const int rows = rows_of(plan.form);
+    a.n_tiles = 0, a.max_level = 0, a.n_heavy = plan.n_heavy;
     for (int s = 0; s < n; ++s) {
       const Seq& q = seqs[s0 + s];
       a.seqs.q0[s] = q.q0, a.seqs.nq[s] = q.nq, a.seqs.k0[s] = q.k0, a.seqs.nk[s] = q.nk;
@@ -336,8 +360,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
       a.n_tiles += tiles;
       a.max_level = std::max(a.max_level, static_cast<int>(static_cast<int64_t>(std::max(0, q.nk - q.nq)) * rep / rows) + tiles);
     }
-    a.fold = form == kMany || form == kMid ? std::max(1, 256 / Hkv) : 0;
-    if (int rc = launch_rows<false>(who, form, dtype, D, a, a.n_tiles * Hkv, st)) return rc;
+    if (int rc = launch_rows<false>(who, plan.form, dtype, D, a, (a.n_tiles + a.n_heavy) * Hkv, st)) return rc;
   }
   return PC_OK;
 }

@@ -29,7 +29,7 @@ struct RowsArgs {
   int row0, n_rows;           // the launch's part of them (one number of rows each: row0 = 0, tensors and tables begin there)
   Divisor by_rep, by_hkv;
   SeqTable seqs;
-  int fold;                   // pc_prompt_attn: row tiles (of a KV head) that the chip's compute units get first; 0: no second ones
+  int n_heavy;                // pc_prompt_attn: tiles of 128 rows (of a KV head), the longest, that are two work-groups' of 64
   int max_level;              // pc_prompt_attn, several sequences: above every tile's level
   int n_tiles;                // pc_prompt_attn: row tiles of one KV head
   // pc_page_attn: units of work per KV head, and where their results go
@@ -78,14 +78,11 @@ __device__ __forceinline__ int limit_of(const RowsArgs& a, const RowSet& r, int 
 // pc_prompt_attn: work-groups in the order of what they have to do, longest first (a causal tile's work goes with where
 // it ends, and the chip is filled from the front).  A tile's level is the number of row tiles' worth of keys in front of its
 // own; tiles of one level follow each other, KV heads fastest, so that with 1, 2, 4, 8 or more heads an XCD's
-// work-groups read few of them.  Where two work-groups share a compute unit, the second 256 come shortest first: unit i
-// gets number i and number 256 + i, and in plain order the first units would have the longest of both.
+// work-groups read few of them.
 template <int R>
-__device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int block, int lane) {
+__device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int u, int kvh, int lane) {   // tile u of a KV head
   RowSet r = {};
-  int u = a.by_hkv.of(block);
-  r.kvh = block - u * a.by_hkv.d;
-  if (u >= a.fold && u < 2 * a.fold) u = min(2 * a.fold, a.n_tiles) - 1 - (u - a.fold);
+  r.kvh = kvh;
   int s = 0;
   if (a.seqs.n == 1) {
     r.tile = a.n_tiles - 1 - u;
@@ -273,7 +270,8 @@ template <int R, bool kPages, class Body>
 __device__ __forceinline__ void each_unit(const RowsArgs& a, lds_int* plan, Body&& body) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if constexpr (!kPages) {
-    body(prompt_rows<R>(a, blockIdx.x, lane));
+    const int u = a.by_hkv.of(blockIdx.x);
+    body(prompt_rows<R>(a, u, blockIdx.x - u * a.by_hkv.d, lane));
   } else {
     const PageUnits units = plan_pages<R>(a, plan, wave, lane);
     RowSet r;
