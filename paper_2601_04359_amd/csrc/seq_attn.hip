@@ -27,7 +27,7 @@ template <typename T, int D, int kSplit>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kSplit), kBatch = 4;
   __shared__ f32x4 acc_lds[kSplit > 1 ? 256 : 1];
-  __shared__ float l_lds[kSplit > 1 ? 256 / kLanes : 1];
+  __shared__ float2 ml_lds[kSplit > 1 ? 256 / kLanes : 1];
   const int group = threadIdx.x / kLanes, c = threadIdx.x % kLanes, turn = group % kSplit;
   const int n = blockIdx.x * kRows + group / kSplit;
   const int Hq = a.by_hkv.d * a.rep;
@@ -47,11 +47,12 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   const int64_t slots = static_cast<int64_t>(kvh) * (common + a.own_cap);
   const int64_t at_c = (slots + tile_c) * a.slot_rows + rho_c - tile_c * a.by_tile.d;
   int first = 0;     // the sequence's first unit
-  if (keys > 0) {
-    if (!fixed) first = a.cut[1 + s];
-    else if (even) first = s * a.by_parts.d;
-    else
-      for (int q = 0; q < s; ++q) first += a.by_tile.of(a.seqs.nq[q] * a.rep + a.by_tile.d - 1) * a.own_parts;
+  if (!fixed) {
+    if (keys > 0) first = a.cut[1 + s];
+  } else if (even) {
+    first = s * a.by_parts.d;
+  } else {
+    for (int q = 0; q < s; ++q) first += a.by_tile.of(a.seqs.nq[q] * a.rep + a.by_tile.d - 1) * a.own_parts;
   }
   const int64_t at_o = (slots + common + first + tile) * a.slot_rows + rho - tile * a.by_tile.d;
   const int parts = none ? 0 : a.shared_parts + own;
@@ -59,37 +60,52 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
     return p < a.shared_parts ? at_c + static_cast<int64_t>(p) * a.shared_tiles * a.slot_rows
                               : at_o + static_cast<int64_t>(p - a.shared_parts) * tiles * a.slot_rows;
   };
-  float M = kNothing;
-  for (int p = c; p < parts; p += kLanes) M = fmaxf(M, a.part_ml[place(p)].x);
-#pragma unroll
-  for (int x = 1; x < kLanes; x *= 2) M = fmaxf(M, __shfl_xor(M, x, kLanes));
-  float L = 0.f;
+  // What a batch reads depends on the lengths only where the device has cut by them: the first one is on its way before they
+  // are known, and what lies behind the shares that there are (it may be anything) does not count.
+  const int last = (fixed ? a.shared_parts + a.own_parts : max(parts, 1)) - 1;
+  float M = kNothing, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = turn; p0 < parts; p0 += kBatch * kSplit) {
+  int p0 = turn;
+  do {
     f32x4 v[kBatch];
     float2 ml[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int64_t from = place(min(p0 + i * kSplit, parts - 1));
+      const int64_t from = place(min(p0 + i * kSplit, last));
       ml[i] = a.part_ml[from];
       v[i] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + c * 4);
     }
+    float top = M;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const float by = p0 + i * kSplit < parts ? __builtin_amdgcn_exp2f(ml[i].x - M) : 0.f;
+      if (p0 + i * kSplit >= parts) ml[i] = {kNothing, 0.f}, v[i] = {0.f, 0.f, 0.f, 0.f};
+      top = fmaxf(top, ml[i].x);
+    }
+    const float keep = __builtin_amdgcn_exp2f(M - top);
+    M = top, L *= keep, acc *= keep;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float by = __builtin_amdgcn_exp2f(ml[i].x - M);
       L += by * ml[i].y;
       acc += by * v[i];
     }
-  }
+    p0 += kBatch * kSplit;
+  } while (p0 < parts);
   if constexpr (kSplit > 1) {
     acc_lds[threadIdx.x] = acc;
-    if (c == 0) l_lds[group] = L;
+    if (c == 0) ml_lds[group] = {M, L};
     __syncthreads();
     if (turn != 0) return;
+    const float own_m = M;
+#pragma unroll
+    for (int i = 1; i < kSplit; ++i) M = fmaxf(M, ml_lds[group + i].x);
+    const float keep = __builtin_amdgcn_exp2f(own_m - M);
+    L *= keep, acc *= keep;
 #pragma unroll
     for (int i = 1; i < kSplit; ++i) {
-      acc += acc_lds[threadIdx.x + i * kLanes];
-      L += l_lds[group + i];
+      const float by = __builtin_amdgcn_exp2f(ml_lds[group + i].x - M);
+      acc += by * acc_lds[threadIdx.x + i * kLanes];
+      L += by * ml_lds[group + i].y;
     }
   }
   if (!there) return;
