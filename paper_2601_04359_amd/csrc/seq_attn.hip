@@ -451,7 +451,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     const PagePlan plan(dtype, D, Hkv, rep, rows, o, n, n_shared, max_len);
     a.tiles_per_seq = std::max(1, ceil_div(per * rep, rows_of(plan.form)));
     a.shared_tiles = plan.shared_tiles, a.shared_parts = plan.shared_parts, a.shared_keys = plan.shared_keys;
-    a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles));
+    a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles)), a.by_rest = Divisor(std::max(1, plan.shared_parts * Hkv % 8));
     a.own_parts = plan.own_parts, a.own_keys = plan.shared_keys, a.by_parts = Divisor(std::max(1, plan.own_parts * a.tiles_per_seq));
     a.own_cap = plan.own_cap, a.slots = plan.slots, a.slot_rows = plan.slot_rows, a.by_tile = Divisor(rows_of(plan.form));
     a.unit_us = plan.form == kFew ? 4.5f : 5.f;

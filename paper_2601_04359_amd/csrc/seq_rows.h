@@ -34,7 +34,7 @@ struct RowsArgs {
   int n_tiles;                // pc_prompt_attn: row tiles of one KV head
   // pc_page_attn: units of work per KV head, and where their results go
   int shared_tiles, shared_parts, shared_keys;   // row tiles over the common rows; their shares, keys of each
-  Divisor by_shared_tiles;
+  Divisor by_shared_tiles, by_rest;   // by_rest: shares of all heads that eight do not divide
   int tiles_per_seq;          // row tiles of a sequence, where all have as many
   int own_parts, own_keys;    // > 0: shares of the own rows as the host has cut them; 0: the device does
   Divisor by_parts;
@@ -208,26 +208,37 @@ __device__ __forceinline__ PageUnits plan_pages(const RowsArgs& a, lds_int* plan
 }
 constexpr int kPlanBytes = (2 * kPageSeqs + 2) * 4;
 
-// Unit `unit` of the launch, KV heads fastest, first those over the common rows; false: there are no more.
+// Unit `unit` of the launch, first those over the common rows; false: there are no more.  The row tiles over one share of a KV
+// head's common rows read the same keys: they are dealt to one XCD (work-groups go to the eight in turn), so that its L2 reads
+// them from memory once.  What does not go into eights, and the units over own rows, come with KV heads fastest.
 template <int R>
 __device__ __forceinline__ bool page_rows(const RowsArgs& a, const PageUnits& units, int unit, int lane, RowSet& r) {
-  int u = a.by_hkv.of(unit);
+  const int common = n_common(a), shares = a.by_hkv.d * a.shared_parts;
   r = {};
-  r.kvh = unit - u * a.by_hkv.d;
-  const int common = n_common(a);
-  if (u >= common + units.total) return false;
-  r.slot = r.kvh * (common + a.own_cap) + u;
-  if (u < common) {
+  if (unit < common * a.by_hkv.d) {
+    const int in_eights = shares & ~7, rest = unit - in_eights * a.shared_tiles;
+    int at;
+    if (rest < 0) {
+      const int i = unit >> 3, round = a.by_shared_tiles.of(i);
+      r.tile = i - round * a.shared_tiles, at = round * 8 + (unit & 7);
+    } else {
+      r.tile = a.by_rest.of(rest), at = in_eights + rest - r.tile * a.by_rest.d;
+    }
+    const int share = a.by_hkv.of(at);
+    r.kvh = at - share * a.by_hkv.d;
+    r.slot = r.kvh * (common + a.own_cap) + share * a.shared_tiles + r.tile;
     r.common = true;
-    const int share = a.by_shared_tiles.of(u);
-    r.tile = u - share * a.shared_tiles;
     r.t0 = a.row0, r.n_tok = a.n_rows;
     r.n_keys = a.n_shared;
     r.begin = share * a.shared_keys, r.end = min(r.begin + a.shared_keys, a.n_shared);
     r.pages = a.shared;
     return true;
   }
-  u -= common;
+  unit -= common * a.by_hkv.d;
+  int u = a.by_hkv.of(unit);
+  r.kvh = unit - u * a.by_hkv.d;
+  if (u >= units.total) return false;
+  r.slot = r.kvh * (common + a.own_cap) + common + u;
   int s, tiles = a.tiles_per_seq, share = 0;
   if (a.own_parts > 0 && a.seqs.per > 0) {
     s = a.by_parts.of(u);     // (units of a sequence: its tiles times the shares)
