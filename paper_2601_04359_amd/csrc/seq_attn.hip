@@ -132,18 +132,11 @@ struct Cost {
 //   few | mid    8/2 x 2,048: 23 | 32    16/4 x 1,024: 17 | 20    16/4 x 2,048: 42 | 34    24/8 x 1,024: 24 | 21
 //   mid | many   8/2 x 8,192: 161 | 176  16/4 x 3,000: 53 | 63    16/4 x 4,288: 97 | 99    24/8 x 4,288: 140 | 118
 constexpr Cost kPromptCost[3] = {{5.0, 1.75, 1.75, 2.5, 3.6, 1.25}, {7.5, 0.75, 0.84, 6.0, 2.9, 0.549}, {7.0, 1.07, 1.3, 5.0, 3.0, 0.953}};
-// Pages: fitted to 34 shapes (1 to 256 sequences of 1 to 1,000 new rows, up to 41,800 common rows and 10,000 own ones) in all
-// three forms and up to twelve lengths of a share; the choice is 5 % off the best of them at the mean.  Both sides, 16/4 heads,
-// 41,800 common rows, us:
-//   few | mid | many   8 tokens: 23 | 25 | 27   16: 35 | 28 | 31   64: 54 | 52 | 52   256: 161 | 139 | 132
-constexpr Cost kPagesCost[3] = {{3.9, 1.58, 1.58, 2.65, 5.3, 1.48}, {4.9, 1.0, 1.0, 8.0, 2.0, 0.58}, {4.8, 1.44, 1.44, 9.8, 0.1, 0.993}};
 // fp32, D = 128 and 64 (from prompts of 40 to 1,200 rows).  Both sides, 16 | 32 rows, us: 8/2 heads x 1,200 rows, D = 128, 51 | 62;
 // two such prompts 94 | 84; 24/8 x 1,200 and 700 187 | 140.
 constexpr Cost kF32Cost[2][2] = {{{5.5, 3.2, 3.75, 3.0, 2.0, 3.6}, {6.5, 2.7, 2.9, 3.0, 2.0, 2.8}},
                                  {{3.2, 2.1, 2.1, 3.0, 1.5, 1.6}, {5.3, 1.4, 1.5, 3.0, 1.5, 1.45}}};
-const Cost& cost_of(Form f, int D, bool pages) {
-  return f <= kF32Two ? kF32Cost[D == 64][f] : (pages ? kPagesCost : kPromptCost)[f - kFew];
-}
+const Cost& cost_of(Form f, int D) { return f <= kF32Two ? kF32Cost[D == 64][f] : kPromptCost[f - kFew]; }
 int keys_per_step(Form f) { return f == kFew ? 256 : f == kF32One ? 128 : 64; }
 // The forms that a call may take: first .. last.
 Form first_form(int dtype) { return dtype == PC_F32 ? kF32One : kFew; }
@@ -177,14 +170,14 @@ struct PromptPlan {
         steps += tiles * Hkv * ((first + last) / 2 / keys_per_step(f) + 0.5);
         longest = std::max(longest, std::ceil(last / keys_per_step(f)));
       }
-      const Cost& cost = cost_of(f, D, false);
+      const Cost& cost = cost_of(f, D);
       if (f == kMany) many_us = cost.start + (cost.per_group * groups + cost.step * steps) / 256;
       const double us = cost(groups, steps, longest);
       if (us < best) best = us, form = f;
     }
     if (form < kMid) return;
     // tiles with more keys than a work-group of 128 rows adds in the time that all of them take
-    const Cost& cost = cost_of(kMany, D, false);
+    const Cost& cost = cost_of(kMany, D);
     const double x = (many_us - cost.alone) / cost.paired * keys_per_step(kMany);
     for (int s = 0; s < n; ++s) {
       const int tiles = ceil_div(seqs[s].nq * rep, kManyRows);
@@ -195,58 +188,93 @@ struct PromptPlan {
   }
 };
 
+// Microseconds of a launch of pc_page_attn: units over common rows of one length, and behind them units over own rows of
+// another, go to the places that the chip has for a form's work-groups (`slots`; two on a compute unit take `paired` for a
+// step, one alone takes `step`), each place taking the next unit when it is done with one.
+struct PagesCost {
+  double unit, step, paired, start;
+  int slots;
+  double operator()(int common, int common_steps, int own, int own_steps) const {
+    const bool alone = slots == 256 || common + own <= 256;
+    const double own_us = unit + own_steps * (alone ? step : paired);
+    double us = start;
+    int left = own;
+    if (common > 0) {
+      const double one = unit + common_steps * step, two = unit + common_steps * (slots == 256 ? step : paired);
+      const int rounds = common / slots, rest = common - rounds * slots;
+      us += rounds * two;
+      if (rest > 0) {     // the last round: own rows' units go into the places left
+        const double last = slots == 256 ? one : rest > 256 ? two : one + (two - one) * std::min(1.0, own * own_us / (256 * one));
+        us += last;
+        if (own > 0) left = std::max(0, own - (slots - rest) * static_cast<int>(std::min(last / own_us, 1e4)));
+      }
+    }
+    return us + ceil_div(left, alone ? 256 : slots) * own_us;
+  }
+};
+// Fitted to 2,600 launches: 78 shapes (1 to 256 sequences of 1 to 1,000 new rows, up to 41,800 common rows and 2,000 own
+// ones) in each form, and up to 25 lengths of a share.  Within 5 % at the mean; the choice is 3 % off the best of them at the
+// mean (8 % where rounds of the chip did not count).  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
+//   few | mid | many   32 tokens: 35 | 38 | 40   64: 60 | 49 | 48   256: 151 | 141 | 131
+constexpr PagesCost kPagesCost[3] = {{3.8, 1.42, 1.42, 2.7, 256}, {2.0, 0.875, 1.2, 5.3, 512}, {0.0, 1.28, 1.84, 6.7, 512}};
+constexpr PagesCost kPagesFew64 = {2.5, 0.89, 1.54, 2.1, 512};
+// 16 | 32 rows, 16/4 heads: 32 tokens behind 10,000 rows 50 | 66; 8 x 32 tokens behind 4,000 rows 119 | 108.
+constexpr PagesCost kPagesF32[2][2] = {{{5.0, 2.95, 2.95, 4.9, 256}, {5.1, 3.14, 4.98, 6.7, 512}},
+                                       {{2.7, 1.55, 2.83, 3.4, 512}, {0.1, 1.5, 2.74, 6.65, 512}}};
+const PagesCost& pages_cost_of(Form f, int D) {
+  return f <= kF32Two ? kPagesF32[D == 64][f] : D == 64 ? kPagesFew64 : kPagesCost[f - kFew];
+}
+
 // How pc_page_attn cuts a launch's work: a form, the shares of the common rows, and room for units over the sequences' own rows,
 // which the device cuts (plan_pages); here their lengths are only known to be max_len at most, and taken to be that.  Beside
 // the costs above there are the bytes of K and V (5.5 TB/s), and the shares' join: a launch, and the fp32 rows that are written
-// and read (4.3 TB/s).
+// and read (4.4 TB/s).  Candidates are the lengths that give 1, 2, 3, ... shares, and those whose units just fill the chip.
+constexpr int kMostParts = 96;   // shares of a row
+constexpr int kFixedKeys = 2048;
 struct PagePlan {
   Form form = kF32One;
   int shared_tiles = 0, shared_parts = 0, shared_keys = kPageStep;
   int own_tiles = 0, own_parts = 0, own_cap = 0;   // own_parts 0: the device cuts
-  int slot_rows = 0, slots = 1024, least_keys = 4 * kPageStep;
+  int slot_rows = 0, slots = 0, least_keys = 4 * kPageStep;
+  float unit_us = 0.f, key_us = 0.f;
   bool joined = false;           // results are shares
   PagePlan(int dtype, int D, int Hkv, int rep, int T, const int32_t* offs, int n_seq, int n_shared, int max_len) {
     const int n_rows = offs != nullptr ? offs[n_seq] - offs[0] : T;
     const int own = max_len > n_shared ? max_len - n_shared / kPageStep * kPageStep : 0;
     int most = offs == nullptr ? T / n_seq : 0;
     for (int s = 0; offs != nullptr && s < n_seq; ++s) most = std::max(most, offs[s + 1] - offs[s]);
-    int parts = 0;
-    auto take = [&](Form f, int share) {
-      form = f;
-      shared_tiles = n_shared > 0 ? ceil_div(n_rows * rep, rows_of(f)) : 0;
-      own_tiles = own > 0 ? row_tiles(offs, n_seq, T, rep, rows_of(f)) : 0;
-      shared_keys = share;
-      shared_parts = ceil_div(n_shared, share);
-      parts = shared_parts + ceil_div(own, share);
-    };
-    const int longest = std::max(n_shared, own), whole = ceil_div(longest, kPageStep) * kPageStep;
-    {
-      const double bytes_us = 3.2 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 2.0 * D * (dtype == PC_BF16 ? 2 : 4) / 5.5e6;
-      double best = 1e30;
-      Form best_form = first_form(dtype);
-      int best_share = whole;
-      for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
-        const Form f = static_cast<Form>(i);
-        const int step = keys_per_step(f);
-        for (int share = 256;; share = std::max(share + 64, share * 5 / 4 / kPageStep * kPageStep)) {
-          share = std::min(share, whole);
-          take(f, share);
-          if (parts <= 96) {
-            const double groups = Hkv * (static_cast<double>(shared_tiles) * shared_parts + static_cast<double>(own_tiles) * ceil_div(own, share));
-            const double steps = Hkv * (static_cast<double>(shared_tiles) * ceil_div(n_shared, step) + static_cast<double>(own_tiles) * ceil_div(own, step));
-            const double join = parts > 1 ? 4.3 + static_cast<double>(n_rows) * rep * Hkv * parts * (8.0 * D + 16) / 4.3e6 : 0.0;
-            const double cost = std::max(cost_of(f, D, true)(groups, steps, ceil_div(share, step)), bytes_us) + join;
-            if (cost < best) best = cost, best_form = f, best_share = share;
-          }
-          if (share >= whole) break;
-        }
-      }
-      take(best_form, best_share);
-      slots = form == kFew ? 256 : 512;
+    const int longest = std::max({n_shared, own, 1}), whole = ceil_div(longest, kPageStep) * kPageStep;
+    const double bytes_us = 4.5 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 2.0 * D * (dtype == PC_BF16 ? 2 : 4) / 5.5e6;
+    double best = 1e30;
+    for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
+      const Form f = static_cast<Form>(i);
+      const PagesCost& cost = pages_cost_of(f, D);
+      const int step = keys_per_step(f), tiles_c = n_shared > 0 ? ceil_div(n_rows * rep, rows_of(f)) : 0,
+                tiles_o = own > 0 ? row_tiles(offs, n_seq, T, rep, rows_of(f)) : 0;
+      auto weigh = [&](int pieces) {
+        const int share = std::min(whole, std::max(4 * kPageStep, ceil_div(ceil_div(longest, pieces), kPageStep) * kPageStep));
+        const int parts_c = ceil_div(n_shared, share), parts_o = ceil_div(own, share);
+        const double units = static_cast<double>(Hkv) * (static_cast<double>(tiles_c) * parts_c + static_cast<double>(tiles_o) * parts_o);
+        if (parts_c + parts_o > kMostParts || (units > 1e6 && pieces > 1)) return;
+        const double join = parts_c + parts_o > 1 ? 4.4 + static_cast<double>(n_rows) * rep * Hkv * (parts_c + parts_o) * (8.0 * D + 16) / 4.4e6 : 0.0;
+        const double us = join + std::max(bytes_us, units > 1e6 ? 1e12 + units : cost(Hkv * tiles_c * parts_c, ceil_div(std::min(share, n_shared), step),
+                                                                                  Hkv * tiles_o * parts_o, ceil_div(std::min(share, own), step)));
+        if (us >= best) return;
+        best = us, form = f;
+        shared_tiles = tiles_c, own_tiles = tiles_o, shared_keys = share, shared_parts = parts_c;
+      };
+      for (int pieces = 1; pieces <= kMostParts; pieces += 1 + pieces / 6) weigh(pieces);
+      for (int fill = 256; fill <= 1536; fill += 256)
+        if (const int pieces = fill / (Hkv * std::max(tiles_c, tiles_o)); pieces > 1 && pieces <= kMostParts) weigh(pieces);
     }
+    const PagesCost& cost = pages_cost_of(form, D);
+    slots = form == kFew ? 256 : cost.slots;   // (D = 64: its longer shares cost less than the join of more)
+    // a key of own rows comes from HBM: in 512 bytes a unit of kFew waits for them, not for its products
+    unit_us = form == kFew ? 4.5f : 5.f;
+    key_us = form == kFew ? (D == 64 ? 0.0054f : 0.0105f) : form == kF32One ? (D == 64 ? 0.0135f : 0.027f)
+                          : static_cast<float>(cost.paired / keys_per_step(form));
     // The own rows' shares are as long as the common ones' while that bounds what a work-group has, whatever the lengths are:
     // it saves the work-groups 2 us of cutting.  Beyond kFixedKeys the device cuts by the lengths that there are.
-    constexpr int kFixedKeys = 2048;
     if (own > 0 && std::min(shared_keys, own) <= kFixedKeys) own_parts = ceil_div(own, shared_keys);
     joined = own > 0 && own_parts == 0 ? true : shared_parts + own_parts > 1;
     while (static_cast<int64_t>(own_tiles) * ceil_div(own, least_keys) > INT_MAX / 2) least_keys *= 2;   // sums of units are 32-bit numbers
@@ -454,9 +482,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles)), a.by_rest = Divisor(std::max(1, plan.shared_parts * Hkv % 8));
     a.own_parts = plan.own_parts, a.own_keys = plan.shared_keys, a.by_parts = Divisor(std::max(1, plan.own_parts * a.tiles_per_seq));
     a.own_cap = plan.own_cap, a.slots = plan.slots, a.slot_rows = plan.slot_rows, a.by_tile = Divisor(rows_of(plan.form));
-    a.unit_us = plan.form == kFew ? 4.5f : 5.f;
-    a.key_us = dtype == PC_F32 ? 0.025f : plan.form == kFew ? 0.0059f : plan.form == kMid ? 0.0156f : 0.0225f;
-    a.step_bytes_us = 2.f * kPageStep * D * elt / 5.5e6f;
+    a.unit_us = plan.unit_us, a.key_us = plan.key_us;
     a.least_keys = plan.least_keys;
     a.part_o = nullptr, a.part_ml = nullptr, a.cut = nullptr;
     if (plan.joined) {

@@ -39,8 +39,7 @@ struct RowsArgs {
   int own_parts, own_keys;    // > 0: shares of the own rows as the host has cut them; 0: the device does
   Divisor by_parts;
   int own_cap;                // units over the sequences' own rows at most
-  float unit_us, key_us;      // what a unit and a key cost a work-group
-  float step_bytes_us;        // what 64 keys of a head cost HBM
+  float unit_us, key_us;      // what a unit and a key of its own rows cost a work-group
   int least_keys;             // of a share
   int slots;                  // work-groups that the chip takes at once
   int slot_rows;              // rows of a slot
@@ -114,9 +113,10 @@ __device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int u, int kvh,
 
 // pc_page_attn.  The lengths are known on the device only, and sequences may be of any lengths beside each other, so that every
 // work-group cuts the work for itself, all alike: shares of `keys` keys of every sequence, and the units (sequence, share, row tile)
-// numbered through.  plan_pages finds the length of a share among six, from an eighth of what a work-group would have if all
-// had the same up to four times that: the rounds of units take their time, or HBM does for the keys of all; of equals the
-// longest.  It is work of one wave, on sums over lanes.
+// numbered through.  plan_pages finds the length of a share among ten, from a third of what a work-group would have if all
+// had the same up to three times that: the one with the shortest rounds of units (of equals the longest).  Mostly that is the
+// one whose units just go into one round: 24/8 heads, 16 sequences of 1 to 27,575 keys (251 us of a copy), shares of 1, 1.4, 2 and
+// 2.8 times the even one 266, 219, 247 and 295 us.  It is work of one wave, on sums over lanes.
 constexpr int kPageSeqs = 256;                 // sequences of a launch at most, four per lane
 struct PageUnits {
   int keys, total;    // keys of a share, units over own rows
@@ -158,24 +158,24 @@ __device__ __forceinline__ void cut_pages(const RowsArgs& a, lds_int* plan, int 
   const int whole = (max(longest, 1) + kPageStep - 1) / kPageStep * kPageStep;
   int best = whole;
   if (a.part_o != nullptr) {
-    constexpr int kTries = 6;
+    constexpr int kTries = 10;
+    constexpr float kOf[kTries] = {0.35f, 0.5f, 0.7f, 1.f, 1.15f, 1.3f, 1.45f, 1.7f, 2.f, 2.8f};
     const float even = static_cast<float>(total) * kPageStep * a.by_hkv.d / a.slots;
     int share[kTries], units[kTries];
 #pragma unroll
     for (int t = 0; t < kTries; ++t) {
-      share[t] = min(max((static_cast<int>(even * (0.125f * (1 << t))) + kPageStep - 1) / kPageStep * kPageStep, a.least_keys), whole);
+      share[t] = min(max((static_cast<int>(even * kOf[t]) + kPageStep - 1) / kPageStep * kPageStep, a.least_keys), whole);
       units[t] = 0;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) units[t] += tiles[i] * ceil_of(keys[i], share[t], 1.f / share[t]);
     }
 #pragma unroll
     for (int t = 0; t < kTries; ++t) units[t] = wave_total(units[t]);
-    const float all_us = static_cast<float>(total) * a.by_hkv.d * a.step_bytes_us;
     float best_us = 3e38f;
 #pragma unroll
     for (int t = 0; t < kTries; ++t) {
       const float rounds = ceilf(static_cast<float>(units[t] + n_common(a)) * a.by_hkv.d / a.slots);
-      const float us = fmaxf(rounds * (a.unit_us + a.key_us * share[t]), all_us);
+      const float us = rounds * (a.unit_us + a.key_us * share[t]);
       if (units[t] <= a.own_cap && us <= best_us) best_us = us, best = share[t];    // (whole sequences always fit)
     }
   }
