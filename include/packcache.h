@@ -461,8 +461,8 @@ int pc_q4_evict(const pc_q4_cache* cache, int H, int D, int32_t* pos, int64_t po
  *            offs[s + 1] - 1 are sequence s (none: nothing happens for it); rows from offs[n_seq] on belong
  *            to nobody and their outputs are left as they were.  NULL: T / n_seq rows each.
  * Everything else about the sequences is read on the device, so that a step of one row each can be recorded into a
- * HIP graph and replayed as the sequences grow.  dtype: bf16 and fp32, D = 64 or 128 (the MFMA forms of bf16 need
- * D = 128; bf16 with D = 64 runs on the fp32 matrix instructions).  Pointers and strides are 16-byte aligned.
+ * HIP graph and replayed as the sequences grow.  dtype: bf16 and fp32, D = 64 or 128 (bf16 with D = 128 comes in work-groups
+ * of 32, 64 or 128 query rows, bf16 with D = 64 of 32, fp32 of 16 or 32).  Pointers and strides are 16-byte aligned.
  *
  * pc_prompt_attn -- causal attention over whole prompts: row i of a sequence with nq queries and nk keys sees its
  * keys 0 .. nk - nq + i.

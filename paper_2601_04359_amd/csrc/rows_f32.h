@@ -11,7 +11,8 @@
 //     see all keys, values that are not finite are taken out of the product and added to the rows that see them.
 // K and V come straight from L2 to registers, the next step's K behind this one's scores and its V behind this one's
 // products.  Bound: what a compute unit draws from L2 with 16 rows (16 KB per 2 x 32 products of 32 cycles and wave at D = 128),
-// the products with 32; latency where there are few keys, which is why 16 rows come with eight waves.
+// the products with 32; latency where there are few keys, which is why 16 rows come with eight waves.  Measured, D = 128: prompts of
+// 40, 252, 333 and 1 rows, 8/2 heads, 15.4 us; 64 tokens with 1,000 rows each in pages, 16/4 heads, 45 us (5.8 TB/s).
 #pragma once
 
 #include <limits.h>
@@ -126,99 +127,99 @@ __device__ __forceinline__ void rows_f32(const RowsArgs& a, const RowSet& r, flo
 
   int kb = r.begin + wave * kF32Keys;
   if (kb < end) {
-  Place now = place(kb);
-  load_k(now, kb);
-  load_v(now, kb);
-  do {
-    const int kb_next = kb + kW * kF32Keys;
-    const Place next = place(kb_next);
-    float x[kQ][4];
-#pragma unroll
-    for (int n = 0; n < kQ; ++n) {
-      f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};   // two chains
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const f32x4 q = q_frag(n, s);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[s][e], q[e], sc[s & 1], 0, 0, 0);
-      }
-      sc[0] += sc[1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] = fmaf(sc[0][e], a.c, sc[0][e] * a.c_lo);
-    }
-    load_k(next, kb_next);
-    if (now.there) {
-      if (kb + kF32Keys > lim_min || kb < r.lo) {
-        uint32_t odd = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = kb + kg * 4 + e;
-#pragma unroll
-          for (int n = 0; n < kQ; ++n)
-            if (j >= lim[n] || j < r.lo) x[n][e] = -INFINITY;
-#pragma unroll
-          for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) odd |= odd_mask(vf[e][db][i]);
-        }
-        if (__any(odd != 0)) {
-          for (int j = max(kb, r.lo); j < min(kb + kF32Keys, r.n_keys); ++j)
-#pragma unroll
-            for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
-                const f32x4 v = load_16B(Vh + row_at(now, j) + db * 64 + kg * 16 + i * 4);
-#pragma unroll
-                for (int n = 0; n < kQ; ++n)
-                  if (j < lim[n]) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[n][db][e][i] += __uint_as_float(__float_as_uint(v[e]) & odd_mask(v[e]));
-                  }
-              }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                vf[e][db][i] = __uint_as_float(__float_as_uint(vf[e][db][i]) & ~odd_mask(vf[e][db][i]));
-        }
-      }
-      float p[kQ][4];
+    Place now = place(kb);
+    load_k(now, kb);
+    load_v(now, kb);
+    do {
+      const int kb_next = kb + kW * kF32Keys;
+      const Place next = place(kb_next);
+      float x[kQ][4];
 #pragma unroll
       for (int n = 0; n < kQ; ++n) {
-        float mx = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (__any(mx > m[n])) {
-          const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - m_new);
-          l[n] *= alpha;
+        f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};   // two chains
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const f32x4 q = q_frag(n, s);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[s][e], q[e], sc[s & 1], 0, 0, 0);
+        }
+        sc[0] += sc[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = fmaf(sc[0][e], a.c, sc[0][e] * a.c_lo);
+      }
+      load_k(next, kb_next);
+      if (now.there) {
+        if (kb + kF32Keys > lim_min || kb < r.lo) {
+          uint32_t odd = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = kb + kg * 4 + e;
+#pragma unroll
+            for (int n = 0; n < kQ; ++n)
+              if (j >= lim[n] || j < r.lo) x[n][e] = -INFINITY;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) odd |= odd_mask(vf[e][db][i]);
+          }
+          if (__any(odd != 0)) {
+            for (int j = max(kb, r.lo); j < min(kb + kF32Keys, r.n_keys); ++j)
+#pragma unroll
+              for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
+                  const f32x4 v = load_16B(Vh + row_at(now, j) + db * 64 + kg * 16 + i * 4);
+#pragma unroll
+                  for (int n = 0; n < kQ; ++n)
+                    if (j < lim[n]) {
+#pragma unroll
+                      for (int e = 0; e < 4; ++e) acc[n][db][e][i] += __uint_as_float(__float_as_uint(v[e]) & odd_mask(v[e]));
+                    }
+                }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  vf[e][db][i] = __uint_as_float(__float_as_uint(vf[e][db][i]) & ~odd_mask(vf[e][db][i]));
+          }
+        }
+        float p[kQ][4];
+#pragma unroll
+        for (int n = 0; n < kQ; ++n) {
+          float mx = fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3]));
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          if (__any(mx > m[n])) {
+            const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - m_new);
+            l[n] *= alpha;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[n][db][e] *= alpha;
+            m[n] = m_new;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[n][e] = __builtin_amdgcn_exp2f(x[n][e] - m[n]);
+            l[n] += p[n][e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[n][db][e] *= alpha;
-          m[n] = m_new;
-        }
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[n][e] = __builtin_amdgcn_exp2f(x[n][e] - m[n]);
-          l[n] += p[n][e];
-        }
+              for (int n = 0; n < kQ; ++n)
+                acc[n][db][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][db][i], p[n][e], acc[n][db][i], 0, 0, 0);
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < kQ; ++n)
-              acc[n][db][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][db][i], p[n][e], acc[n][db][i], 0, 0, 0);
-    }
-    load_v(next, kb_next);
-    now = next;
-    kb = kb_next;
-  } while (kb < end);
+      load_v(next, kb_next);
+      now = next;
+      kb = kb_next;
+    } while (kb < end);
   }
 
   if constexpr (kQ > 1) __syncthreads();   // the queries have been read by all

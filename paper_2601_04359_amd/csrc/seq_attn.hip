@@ -213,12 +213,12 @@ struct PagesCost {
   }
 };
 // Fitted to 2,600 launches: 78 shapes (1 to 256 sequences of 1 to 1,000 new rows, up to 41,800 common rows and 2,000 own
-// ones) in each form, and up to 25 lengths of a share.  Within 5 % at the mean; the choice is 3 % off the best of them at the
-// mean (8 % where rounds of the chip did not count).  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
-//   few | mid | many   32 tokens: 35 | 38 | 40   64: 60 | 49 | 48   256: 151 | 141 | 131
+// ones) in each form, and up to 25 lengths of a share, within 5 % at the mean.  The choice is 4 % off the best of them at the mean,
+// and 8 % on 19 other shapes.  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
+//   few | mid | many   32 tokens: 35 | 36 | 37   64: 54 | 49 | 48   256: 168 | 139 | 131
 constexpr PagesCost kPagesCost[3] = {{3.8, 1.42, 1.42, 2.7, 256}, {2.0, 0.875, 1.2, 5.3, 512}, {0.0, 1.28, 1.84, 6.7, 512}};
 constexpr PagesCost kPagesFew64 = {2.5, 0.89, 1.54, 2.1, 512};
-// 16 | 32 rows, 16/4 heads: 32 tokens behind 10,000 rows 50 | 66; 8 x 32 tokens behind 4,000 rows 119 | 108.
+// 16 | 32 rows, 16/4 heads, D = 128: 64 tokens with 1,000 rows each 45 | 65; 8 x 32 tokens behind 4,000 rows 117 | 108.
 constexpr PagesCost kPagesF32[2][2] = {{{5.0, 2.95, 2.95, 4.9, 256}, {5.1, 3.14, 4.98, 6.7, 512}},
                                        {{2.7, 1.55, 2.83, 3.4, 512}, {0.1, 1.5, 2.74, 6.65, 512}}};
 const PagesCost& pages_cost_of(Form f, int D) {
@@ -257,6 +257,7 @@ struct PagePlan {
         const double units = static_cast<double>(Hkv) * (static_cast<double>(tiles_c) * parts_c + static_cast<double>(tiles_o) * parts_o);
         if (parts_c + parts_o > kMostParts || (units > 1e6 && pieces > 1)) return;
         const double join = parts_c + parts_o > 1 ? 4.4 + static_cast<double>(n_rows) * rep * Hkv * (parts_c + parts_o) * (8.0 * D + 16) / 4.4e6 : 0.0;
+        if (join + bytes_us >= best) return;
         const double us = join + std::max(bytes_us, units > 1e6 ? 1e12 + units : cost(Hkv * tiles_c * parts_c, ceil_div(std::min(share, n_shared), step),
                                                                                   Hkv * tiles_o * parts_o, ceil_div(std::min(share, own), step)));
         if (us >= best) return;
@@ -265,7 +266,7 @@ struct PagePlan {
       };
       for (int pieces = 1; pieces <= kMostParts; pieces += 1 + pieces / 6) weigh(pieces);
       for (int fill = 256; fill <= 1536; fill += 256)
-        if (const int pieces = fill / (Hkv * std::max(tiles_c, tiles_o)); pieces > 1 && pieces <= kMostParts) weigh(pieces);
+        if (const int pieces = fill / (Hkv * std::max({tiles_c, tiles_o, 1})); pieces > 1 && pieces <= kMostParts) weigh(pieces);
     }
     const PagesCost& cost = pages_cost_of(form, D);
     slots = form == kFew ? 256 : cost.slots;   // (D = 64: its longer shares cost less than the join of more)
@@ -295,6 +296,11 @@ int each_launch(const int32_t* offs, int n_seq, F&& f) {
   for (int s0 = 0; s0 < n_seq; s0 += most)
     if (int rc = f(s0, std::min(most, n_seq - s0))) return rc;
   return PC_OK;
+}
+
+PagePlan plan_of(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, int n_seq, int s0, int n, int max_len, int n_shared) {
+  return PagePlan(dtype, D, Hkv, Hq / Hkv, offs != nullptr ? T : T / n_seq * n, offs != nullptr ? offs + s0 : nullptr, n,
+                  std::min(n_shared, max_len), max_len);
 }
 
 void set_scale(RowsArgs& a, float scale) {
@@ -415,9 +421,7 @@ extern "C" size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T
   if (offs == nullptr ? T % n_seq != 0 : check_offsets("pc_page_attn_workspace_bytes", "offs", offs, n_seq, T) != PC_OK) return 0;
   size_t most = 0;
   each_launch(offs, n_seq, [&](int s0, int n) {
-    const int32_t* o = offs != nullptr ? offs + s0 : nullptr;
-    const PagePlan plan(dtype, D, Hkv, Hq / Hkv, o != nullptr ? T : T / n_seq * n, o, n, std::min(n_shared, max_len), max_len);
-    most = std::max(most, plan.bytes(Hkv, D));
+    most = std::max(most, plan_of(dtype, Hq, Hkv, T, D, offs, n_seq, s0, n, max_len, n_shared).bytes(Hkv, D));
     return PC_OK;
   });
   return most;
@@ -449,7 +453,10 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
   PC_REQUIRE(!overlap(O, o_stride_h * elt, Hq, per_head * elt, Q, q_stride_h * elt, Hq, per_head * elt), PC_ERR_SHAPE,
              "%s: O may not overlap Q: queries are read again behind the first outputs", who);
   n_shared = std::min(n_shared, max_len);   // nobody sees more
-  const size_t need = pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, offs, n_seq, max_len, n_shared);
+  // the plan of a call's only launch serves both its workspace and the launch
+  const bool one = n_seq <= (offs != nullptr ? kSeqs : kPageSeqs);
+  const PagePlan first = plan_of(dtype, Hq, Hkv, T, D, offs, n_seq, 0, std::min(n_seq, offs != nullptr ? kSeqs : kPageSeqs), max_len, n_shared);
+  const size_t need = one ? first.bytes(Hkv, D) : pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, offs, n_seq, max_len, n_shared);
   PC_REQUIRE(need == 0 || (ws != nullptr && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 16 == 0), PC_ERR_WORKSPACE,
              "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, need, ws_bytes);
   const int rep = Hq / Hkv;
@@ -476,7 +483,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     } else {
       for (int s = 0; s < n; ++s) a.seqs.q0[s] = o[s], a.seqs.nq[s] = o[s + 1] - o[s], a.seqs.k0[s] = s0 + s;
     }
-    const PagePlan plan(dtype, D, Hkv, rep, rows, o, n, n_shared, max_len);
+    const PagePlan plan = s0 == 0 ? first : plan_of(dtype, Hq, Hkv, T, D, offs, n_seq, s0, n, max_len, n_shared);
     a.tiles_per_seq = std::max(1, ceil_div(per * rep, rows_of(plan.form)));
     a.shared_tiles = plan.shared_tiles, a.shared_parts = plan.shared_parts, a.shared_keys = plan.shared_keys;
     a.by_shared_tiles = Divisor(std::max(1, plan.shared_tiles)), a.by_rest = Divisor(std::max(1, plan.shared_parts * Hkv % 8));

@@ -128,6 +128,25 @@ def test_workspaces(L):
 
 
 # ------------------------------------------------------------------------------ the binding
+@pytest.mark.parametrize("dtype", [pk.PC_BF16, pk.PC_F32])
+@pytest.mark.parametrize("shared", [0, 70])
+def test_sequences_that_are_all_empty_need_nothing(L, dtype, shared):
+    for offs in ([0, 0, 0], [2, 2, 2]):
+        assert L.pc_page_attn_workspace_bytes(dtype, 8, 2, 4, 128, ints(offs), 2, 100, shared) >= 0
+
+
+@pytest.mark.parametrize("dtype", [pk.PC_BF16, pk.PC_F32])
+def test_workspaces_of_the_largest_calls_are_counted(L, dtype):
+    """Every size that a call may have gets a plan: no overflow on the way to it, and never fewer bytes than the partial rows take."""
+    for Hq, Hkv, T, n_seq, max_len, shared in [(1, 1, 1, 1, 1 << 29, 0), (1, 1, 1, 1, 1 << 29, 1 << 29), (32, 1, 1 << 20, 1 << 20, 1 << 20, 0),
+                                               (32, 32, 1 << 20, 1, 1 << 29, 1 << 28), (128, 8, 1 << 18, 4, 1 << 24, 1 << 23), (1, 1, 1, 1, 1, 0),
+                                               (33, 11, 7, 7, 65, 64), (64, 64, 1 << 19, 1 << 19, 64, 63)]:
+        for D in (64, 128):
+            size = L.pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, None, n_seq, max_len, shared)
+            launch = T // n_seq * min(n_seq, 256)
+            assert size < 1 << 62 and (size == 0 or size >= launch * Hq * D * 4)
+
+
 def test_binding_refuses_what_does_not_fit(L):
     bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
