@@ -500,13 +500,15 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
     }
     if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, plan.units() * Hkv, st)) return rc;
     if (!plan.joined) return PC_OK;
-    // one row per work-group where there may be many shares of it, else eight (sixteen at D = 64)
-    const bool many = plan.shared_parts > 6 || Hq * a.n_rows <= 2048;
-    auto* join = dtype == PC_BF16 ? (D == 128 ? (many ? rows_join_kernel<uint16_t, 128, 8> : rows_join_kernel<uint16_t, 128, 1>)
-                                              : (many ? rows_join_kernel<uint16_t, 64, 8> : rows_join_kernel<uint16_t, 64, 1>))
-                                  : (D == 128 ? (many ? rows_join_kernel<float, 128, 8> : rows_join_kernel<float, 128, 1>)
-                                              : (many ? rows_join_kernel<float, 64, 8> : rows_join_kernel<float, 64, 1>));
-    join<<<ceil_div(Hq * a.n_rows, 256 / (D / 4) / (many ? 8 : 1)), 256, 0, st>>>(a);
+    // Few rows: one per work-group, its shares read by eight groups of threads at once; else eight rows (sixteen at D = 64).  Eight
+    // at once | one, whole calls, 16/4 heads, us: 512 rows per head of 9 shares 151 | 142, 256 of 5 shares 53 | 47; 24/8 heads,
+    // 64 of 10 shares 72.9 | 75.6.
+    const bool few_rows = Hq * a.n_rows <= 2048;
+    auto* join = dtype == PC_BF16 ? (D == 128 ? (few_rows ? rows_join_kernel<uint16_t, 128, 8> : rows_join_kernel<uint16_t, 128, 1>)
+                                              : (few_rows ? rows_join_kernel<uint16_t, 64, 8> : rows_join_kernel<uint16_t, 64, 1>))
+                                  : (D == 128 ? (few_rows ? rows_join_kernel<float, 128, 8> : rows_join_kernel<float, 128, 1>)
+                                              : (few_rows ? rows_join_kernel<float, 64, 8> : rows_join_kernel<float, 64, 1>));
+    join<<<ceil_div(Hq * a.n_rows, 256 / (D / 4) / (few_rows ? 8 : 1)), 256, 0, st>>>(a);
     PC_CHECK_LAUNCH(who);
     return PC_OK;
   });
