@@ -212,11 +212,12 @@ struct PagesCost {
     return us + ceil_div(left, alone ? 256 : slots) * own_us;
   }
 };
-// Fitted to 2,600 launches: 78 shapes (1 to 256 sequences of 1 to 1,000 new rows, up to 41,800 common rows and 2,000 own
-// ones) in each form, and up to 25 lengths of a share, within 5 % at the mean.  The choice is 4 % off the best of them at the mean,
-// and 8 % on 19 other shapes.  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
+// Fitted to 3,800 launches (61 shapes of 1 to 256 sequences with 1 to 1,000 new rows, up to 41,800 common rows and 2,000 own ones, in
+// each form, up to 25 lengths of a share): first the times, then the choice, which is 3 % off the best of a shape's launches
+// at the mean, 15 % at most.  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
 //   few | mid | many   32 tokens: 35 | 36 | 37   64: 54 | 49 | 48   256: 168 | 139 | 131
-constexpr PagesCost kPagesCost[3] = {{3.8, 1.42, 1.42, 2.7, 256}, {2.0, 0.875, 1.2, 5.3, 512}, {0.0, 1.28, 1.84, 6.7, 512}};
+// fp32 and D = 64: to 18 shapes each.
+constexpr PagesCost kPagesCost[3] = {{3.2, 1.67, 1.67, 2.45, 256}, {2.1, 0.913, 1.064, 5.2, 512}, {0.0, 1.22, 1.45, 6.9, 512}};
 constexpr PagesCost kPagesFew64 = {2.5, 0.89, 1.54, 2.1, 512};
 // 16 | 32 rows, 16/4 heads, D = 128: 64 tokens with 1,000 rows each 45 | 65; 8 x 32 tokens behind 4,000 rows 117 | 108.
 constexpr PagesCost kPagesF32[2][2] = {{{5.0, 2.95, 2.95, 4.9, 256}, {5.1, 3.14, 4.98, 6.7, 512}},
@@ -227,8 +228,8 @@ const PagesCost& pages_cost_of(Form f, int D) {
 
 // How pc_page_attn cuts a launch's work: a form, the shares of the common rows, and room for units over the sequences' own rows,
 // which the device cuts (plan_pages); here their lengths are only known to be max_len at most, and taken to be that.  Beside
-// the costs above there are the bytes of K and V (5.5 TB/s), and the shares' join: a launch, and the fp32 rows that are written
-// and read (4.4 TB/s).  Candidates are the lengths that give 1, 2, 3, ... shares, and those whose units just fill the chip.
+// the costs above there are the bytes of K and V (6.1 TB/s), and the shares' join: a launch, and the fp32 rows that are written
+// and read (3.8 TB/s).  Candidates are the lengths that give 1, 2, 3, ... shares, and those whose units just fill the chip.
 constexpr int kMostParts = 96;   // shares of a row
 constexpr int kFixedKeys = 2048;
 struct PagePlan {
@@ -244,7 +245,7 @@ struct PagePlan {
     int most = offs == nullptr ? T / n_seq : 0;
     for (int s = 0; offs != nullptr && s < n_seq; ++s) most = std::max(most, offs[s + 1] - offs[s]);
     const int longest = std::max({n_shared, own, 1}), whole = ceil_div(longest, kPageStep) * kPageStep;
-    const double bytes_us = 4.5 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 2.0 * D * (dtype == PC_BF16 ? 2 : 4) / 5.5e6;
+    const double bytes_us = 4.5 + (n_shared + static_cast<double>(own) * n_seq) * Hkv * 2.0 * D * (dtype == PC_BF16 ? 2 : 4) / 6.1e6;
     double best = 1e30;
     for (int i = first_form(dtype); i <= last_form(dtype, D); ++i) {
       const Form f = static_cast<Form>(i);
@@ -256,7 +257,7 @@ struct PagePlan {
         const int parts_c = ceil_div(n_shared, share), parts_o = ceil_div(own, share);
         const double units = static_cast<double>(Hkv) * (static_cast<double>(tiles_c) * parts_c + static_cast<double>(tiles_o) * parts_o);
         if (parts_c + parts_o > kMostParts || (units > 1e6 && pieces > 1)) return;
-        const double join = parts_c + parts_o > 1 ? 4.4 + static_cast<double>(n_rows) * rep * Hkv * (parts_c + parts_o) * (8.0 * D + 16) / 4.4e6 : 0.0;
+        const double join = parts_c + parts_o > 1 ? 5.4 + static_cast<double>(n_rows) * rep * Hkv * (parts_c + parts_o) * (8.0 * D + 16) / 3.8e6 : 0.0;
         if (join + bytes_us >= best) return;
         const double us = join + std::max(bytes_us, units > 1e6 ? 1e12 + units : cost(Hkv * tiles_c * parts_c, ceil_div(std::min(share, n_shared), step),
                                                                                   Hkv * tiles_o * parts_o, ceil_div(std::min(share, own), step)));
