@@ -419,6 +419,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
 extern "C" size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, int n_seq,
                                                int max_len, int n_shared) {
   if (dtype < 0 || dtype > 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || T < 1 || n_seq < 1 || max_len < 1 || n_shared < 0 || (D != 64 && D != 128)) return 0;
+  if (static_cast<int64_t>(Hq) * T > INT32_MAX / 64 || max_len > INT32_MAX / 2 || n_shared > INT32_MAX / 2) return 0;   // (refused by the call)
   if (offs == nullptr ? T % n_seq != 0 : check_offsets("pc_page_attn_workspace_bytes", "offs", offs, n_seq, T) != PC_OK) return 0;
   size_t most = 0;
   each_launch(offs, n_seq, [&](int s0, int n) {

@@ -396,8 +396,8 @@ class PagedStack:
         s.close(a)                        its pages are free, but for those that others have in common with it
 
     Q [Hq][T][D] and K, V [Hkv][T][D] of the step are not rotated yet; Q is rotated in place, and so is K in a step of new
-    sequences.  pos int32 [T][3] on the device.  A step in which every sequence is new runs pc_prompt_attn over its own rows, every other one pc_page_attn over
-    the pages, with the pages that all of the step's sequences begin with read once for all.
+    sequences.  pos int32 [T][3] on the device.  A step in which every sequence is new runs pc_prompt_attn over its own rows,
+    every other one pc_page_attn over the pages, with the pages that all of the step's sequences begin with read once for all.
 
     The pages of a step are decided in begin(), on the host; attend() only launches.  With the same sequences and one row each, a
     step's launches are the same while n_shared and max_len are, so that attend() can be recorded into a HIP graph: begin()

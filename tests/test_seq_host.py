@@ -135,6 +135,13 @@ def test_sequences_that_are_all_empty_need_nothing(L, dtype, shared):
         assert L.pc_page_attn_workspace_bytes(dtype, 8, 2, 4, 128, ints(offs), 2, 100, shared) >= 0
 
 
+def test_workspaces_of_what_is_refused_are_nothing(L):
+    big = 2 ** 31 - 1
+    for Hq, Hkv, T, max_len, shared in [(64, 64, big, 100, 0), (64, 64, 2 ** 30, 100, 50), (1, 1, 4, big, 0), (1, 1, 4, 100, big),
+                                        (2 ** 20, 2 ** 20, 2 ** 20, 100, 0)]:
+        assert L.pc_page_attn_workspace_bytes(pk.PC_BF16, Hq, Hkv, T, 128, None, 1, max_len, shared) == 0
+
+
 @pytest.mark.parametrize("dtype", [pk.PC_BF16, pk.PC_F32])
 def test_workspaces_of_the_largest_calls_are_counted(L, dtype):
     """Every size that a call may have gets a plan: no overflow on the way to it, and never fewer bytes than the partial rows take."""
