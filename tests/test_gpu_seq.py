@@ -318,6 +318,41 @@ def test_page_attn_long(dtype, Hq, Hkv, lens, n, shared):
     run_pages(dtype, Hq, Hkv, 128, lens, n, shared=shared, page=128)
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("Hq,Hkv,n_seq,n,shared", [(9, 3, 5, 40, 2600), (11, 11, 3, 9, 1500), (7, 1, 6, 30, 4100), (13, 13, 2, 70, 600), (20, 5, 33, 1, 3000)])
+def test_page_attn_tiles_of_common_rows_in_any_number(dtype, D, Hq, Hkv, n_seq, n, shared):
+    """Shares times heads that eight divide, do not divide, and are fewer than; several tiles of each."""
+    run_pages(dtype, Hq, Hkv, D, [shared + n + 13 * i for i in range(n_seq)], n, shared=shared)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,n,shared,max_len", [([5, 900, 1, 0], 1, 0, 2000), ([310, 305, 1200, 300], 2, 300, 2200), ([40, 9000, 3], 1, 0, 30000),
+                                                   ([500, 460, 420], 100, 400, 1300)])
+def test_page_attn_what_the_workspace_holds_does_not_count(dtype, lens, n, shared, max_len):
+    """Shares for rows up to max_len that the sequences do not have are not written by anybody: the memory may hold anything."""
+    nws = pk.pc_page_attn_workspace_bytes(pk.PC_BF16 if dtype == "bf16" else pk.PC_F32, 8, 2, n * len(lens), 128, len(lens), max_len, shared)
+    page = 64
+    pg = Paged(dtype, 2, 128, lens, page, shared, width_more=-(-max_len // page))
+    outs = []
+    for fill in (255, 127, 0):      # NaN, 3e38, 0
+        ws = torch.full((max(nws, 1),), fill, dtype=torch.uint8, device=DEV)
+        outs.append(run_pages(dtype, 8, 2, 128, lens, n, shared=shared, max_len=max_len, ws=ws, paged=pg)[2:])
+    for O, L in outs[1:]:
+        assert torch.equal(O, outs[0][0]) and torch.equal(L, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_page_attn_launches_without_rows(dtype):
+    """More sequences than a launch has, the first launch's (or all) without rows."""
+    rows = [0] * 64 + [3, 0, 70]
+    run_pages(dtype, 8, 2, 128, [100 + n for n in rows], None, ragged=rows, shared=50)
+    pg = Paged(dtype, 2, 128, [90, 80], shared=70)
+    Q, O = torch.randn(8, 4, 128, device=DEV).to(TYPES[dtype]), torch.full((8, 4, 128), 7.0, dtype=TYPES[dtype], device=DEV)
+    for offs in ([0, 0, 0], [2, 2, 2]):
+        pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, 90, 0.1, offs=offs, shared=pg.shared, n_shared=70, O=O)
+    assert (O == 7.0).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_page_attn_strided_pages_and_bounds(dtype):
     """Heads outside of the pages; a bound far above the lengths, and one below them."""
