@@ -3,7 +3,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <numeric>
 #include <vector>
 
 #include "rows_bf16.h"
