@@ -6,7 +6,7 @@
 //     (product e contracts over keys 4 kg + e), and row r of output block (db, e) stands for dim 64 db + 4 r + e, so that V
 //     comes in 16-byte pieces and O leaves in them.
 //   * A score is s (c + c_lo), and the reference is subtracted from the rounded product: the largest key's exponent is 0
-//     however large the logits are.
+//     however large the logits are.  c_lo > 0: a score of -inf stays one.
 //   * A key that a row does not see has p = 0, and 0 times a NaN in V would reach the row: in steps where some row does not
 //     see all keys, values that are not finite are taken out of the product and added to the rows that see them.
 // K and V come straight from L2 to registers, the next step's K behind this one's scores and its V behind this one's

@@ -304,10 +304,13 @@ PagePlan plan_of(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, 
                   std::min(n_shared, max_len), max_len);
 }
 
-void set_scale(RowsArgs& a, float scale) {
+// fp32: c is rounded down and c_lo above zero (by 2^-30 of c at least, which is far below a rounding), so that a score of -inf stays
+// -inf in s c + s c_lo and is no NaN.  bf16 has c alone, to the nearest.
+void set_scale(RowsArgs& a, int dtype, float scale) {
   const double c = static_cast<double>(scale) * 1.4426950408889634074;
   a.c = static_cast<float>(c);
-  a.c_lo = static_cast<float>(c - a.c);
+  if (dtype == PC_F32 && a.c > c) a.c = nextafterf(a.c, 0.f);
+  a.c_lo = std::max(static_cast<float>(std::max(c - a.c, c * 0x1p-30)), 0x1p-149f);
 }
 
 int check_attn(const char* who, int dtype, int Hq, int Hkv, int D, float scale) {
@@ -387,7 +390,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
   a.Q = Q, a.K = K, a.V = V, a.O = O, a.lse = lse;
   a.q_stride = q_stride_h, a.k_stride = k_stride_h, a.v_stride = v_stride_h, a.o_stride = o_stride_h;
   a.rep = rep, a.T = Tq, a.by_rep = Divisor(rep), a.by_hkv = Divisor(Hkv);
-  set_scale(a, scale);
+  set_scale(a, dtype, scale);
   hipStream_t st = static_cast<hipStream_t>(stream);
   // sequences without rows have nothing to do; the longest come first, so that those of a launch are about as long
   std::vector<Seq> seqs;
@@ -468,7 +471,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
   a.table = table, a.lens = lens, a.shared = shared, a.table_stride = table_stride, a.page_stride = pages->stride_page;
   a.n_pages = pages->n_pages, a.n_shared = n_shared, a.max_len = max_len, a.by_page = Divisor(pages->page_rows);
   a.rep = rep, a.T = T, a.by_rep = Divisor(rep), a.by_hkv = Divisor(Hkv);
-  set_scale(a, scale);
+  set_scale(a, dtype, scale);
   hipStream_t st = static_cast<hipStream_t>(stream);
   return each_launch(offs, n_seq, [&](int s0, int n) -> int {
     const int32_t* o = offs != nullptr ? offs + s0 : nullptr;

@@ -47,7 +47,7 @@ struct RowsArgs {
   float* part_o;              // [Hkv][n_common + own_cap][slot_rows][D], un-normalised; NULL: one share, the result itself
   float2* part_ml;            // [Hkv][..][slot_rows]: reference (base 2) and sum
   int* cut;                   // [1 + n_seq]: keys of a share of the own rows, the first unit of each sequence's
-  float c, c_lo;              // scale * log2(e) in two floats
+  float c, c_lo;              // scale * log2(e) in two floats, c_lo > 0 (fp32; bf16: c alone)
 };
 
 // What a work-group has.

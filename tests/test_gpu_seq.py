@@ -724,3 +724,73 @@ def test_stack_step_in_a_graph():
         for l in range(layers):
             want = stacks[1].attend(l, new[0][l], new[1][l], new[2][l], p)
             assert torch.equal(O[l], want)
+
+
+# ------------------------------------------------------------------------------ scores of -inf
+def check_kept(dtype, O, L, Q, kv, keep, scale, none=0):
+    """Rows one by one: row i of O, L, Q [Hq][n][..] weighs the keys of kv (K, V [Hkv][nk][D]) that keep [n][nk] has; `none` of the rows
+    have no such key, and give 0 and -inf."""
+    Hq, n, _ = O.shape
+    for i in range(n):
+        for h in range(Hq):
+            k, v = (x[h // (Hq // kv[0].shape[0])][keep[i]] for x in kv)
+            if k.shape[0] == 0:
+                assert (O[h, i] == 0).all() and L[h, i] == -float("inf")
+            else:
+                check_rows(dtype, O[h, i:i + 1], L[h, i:i + 1], Q[h, i:i + 1], k, v, scale, k.shape[0])
+    assert (~keep.any(1)).sum() == none
+
+
+def causal(n, nk, gone):
+    """keep [n][nk] of the last n rows of a sequence of nk, without the keys in `gone`."""
+    at = torch.arange(nk, device=DEV)
+    keep = at[None] <= nk - n + torch.arange(n, device=DEV)[:, None]
+    return keep & ~torch.isin(at, torch.tensor(list(gone), dtype=torch.int64, device=DEV))[None]
+
+
+OVERFLOWS = [17, 18, 40, 63, 64, 70]
+
+
+def overflow(Q, K):
+    """Products of these keys with every query are beyond the range of 32 bits."""
+    Q[..., 0], K[..., 0] = 8.0, 0.0
+    K[:, [j for j in OVERFLOWS if j < K.shape[1]], 0] = -3e38
+
+
+def rewrite(pg, change):
+    """change(K, V) of every sequence's rows, the common ones among them, in plain form and in the pages."""
+    for K, V in pg.seqs:
+        change(K, V)
+    longest = max(range(len(pg.seqs)), key=lambda s: pg.lens_host[s])
+    if pg.n_shared:
+        pg.put(pg.shared.tolist(), [x[:, :pg.n_shared] for x in pg.seqs[longest]], 0, pg.n_shared)
+    for s, n in enumerate(pg.lens_host):
+        pg.put(pg.table[s, :-(-n // pg.page)].tolist(), pg.seqs[s], pg.n_shared, n)
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 128), ("f32", 64), ("bf16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("scale", [128 ** -0.5, 0.1, 0.125, pk.PC_SCALE_FOLDED])
+@pytest.mark.parametrize("n", [75, 700])
+def test_prompt_scores_of_minus_infinity_weigh_nothing(dtype, D, scale, n):
+    Hq, Hkv = 4, 2
+    gen = generator(n)
+    Q, K, V = (normal(gen, H, n, D).to(TYPES[dtype]) for H in (Hq, Hkv, Hkv))
+    overflow(Q, K)
+    L = torch.empty((Hq, n), device=DEV)
+    O = pk.pc_prompt_attn(Q, K, V, scale, [0, n], lse=L)
+    rows = list(range(0, 17, 5)) + list(range(17, 75, 3)) + [n - 1]
+    check_kept(dtype, O[:, rows], L[:, rows], Q[:, rows], (K, V), causal(n, n, OVERFLOWS)[rows], scale)
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 128), ("f32", 64), ("bf16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("scale", [128 ** -0.5, 0.1, 0.125, pk.PC_SCALE_FOLDED])
+@pytest.mark.parametrize("lens,n,shared", [([100, 300], 1, 0), ([100, 300], 1, 66), ([120, 300], 30, 20)])
+def test_page_attn_scores_of_minus_infinity_weigh_nothing(dtype, D, scale, lens, n, shared):
+    pg = Paged(dtype, 2, D, lens, shared=shared)
+    Q = normal(generator(1), 4, 2 * n, D).to(TYPES[dtype])
+    rewrite(pg, lambda K, V: overflow(Q, K))
+    L = torch.empty((4, 2 * n), device=DEV)
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max(lens), scale, shared=pg.shared, n_shared=shared, lse=L)
+    for s in range(2):
+        mine = slice(s * n, (s + 1) * n)
+        check_kept(dtype, O[:, mine], L[:, mine], Q[:, mine], pg.seqs[s], causal(n, lens[s], OVERFLOWS), scale)
