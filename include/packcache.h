@@ -528,8 +528,8 @@ int pc_page_store(const void* K, const void* V, int dtype, int Hkv, int T, int D
  *   lse      dev or NULL, fp32 [Hq][T]
  *   ws       dev, pc_page_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls that may
  *            overlap on the GPU must not share one.
- * A row that sees nothing (lens[s] = 0) gets O = 0 and lse = -inf.  A page number that is not one of 0 .. n_pages - 1
- * stands for rows that nobody sees.  The order of the sums is fixed: results are bit-reproducible.
+ * A row that sees nothing (lens[s] = 0, or none of its pages is there) gets O = 0 and lse = -inf.  A page number that is not
+ * one of 0 .. n_pages - 1 stands for rows that nobody sees.  The order of the sums is fixed: results are bit-reproducible.
  * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_WORKSPACE, PC_ERR_HIP.
  */
 size_t pc_page_attn_workspace_bytes(int dtype, int Hq, int Hkv, int T, int D, const int32_t* offs, int n_seq,

@@ -158,7 +158,7 @@ __device__ __forceinline__ void merge_waves(const RowsArgs& a, const RowSet& r, 
       if (i == 0) a.part_ml[at] = make_float2(M, L);
       continue;
     }
-    const bool none = limit_of(a, r, tok) <= r.lo;
+    const bool none = sees_none(a, r, limit_of(a, r, tok), L);
     const float inv = none ? 0.f : 1.f / L;
     u32x4 out = {0u, 0u, 0u, 0u};
     if (!none) {
@@ -592,13 +592,14 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
     if (g == 0 && l32 < rows_w) a.part_ml[first + l32] = sees ? make_float2(fmaxf(m_ref, kNothing), l_tot) : make_float2(kNothing, 0.f);
     return;
   }
-  const float inv = sees ? 1.f / l_tot : 0.f;
+  const bool none = !sees || sees_none(a, r, lim, l_tot);
+  const float inv = none ? 0.f : 1.f / l_tot;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       u32x2 out = {pack_bf16x2(o[db][q * 4 + 0] * inv, o[db][q * 4 + 1] * inv), pack_bf16x2(o[db][q * 4 + 2] * inv, o[db][q * 4 + 3] * inv)};
-      if (!sees) out = u32x2{0u, 0u};
+      if (none) out = u32x2{0u, 0u};
       *reinterpret_cast<lds_u32x2*>(mine + l32 * kRowBytes + k_chunk_pos(l32, db * 4 + q) * 16 + g * 8) = out;
     }
   wave_lds_sync();
@@ -610,7 +611,7 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
     const int64_t t = row_to(min(row, rows_w - 1), &h);
     if (row < rows_w) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.O) + h * a.o_stride + t * kD + chunk * 8) = v;
   }
-  if (a.lse != nullptr && g == 0 && l32 < rows_w) a.lse[head * static_cast<int64_t>(a.T) + r.t0 + tok] = sees ? lse_of(m_ref, l_tot) : -INFINITY;
+  if (a.lse != nullptr && g == 0 && l32 < rows_w) a.lse[head * static_cast<int64_t>(a.T) + r.t0 + tok] = none ? -INFINITY : lse_of(m_ref, l_tot);
 }
 
 // ------------------------------------------------------------------------------------------

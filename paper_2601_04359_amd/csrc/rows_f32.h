@@ -261,7 +261,7 @@ __device__ __forceinline__ void rows_f32(const RowsArgs& a, const RowSet& r, flo
     }
     const int tok = a.by_rep.of(rho), head = r.kvh * a.rep + rho - tok * a.rep;
     const int64_t t = r.t0 + tok;
-    const bool none = limit_of(a, r, tok) <= r.lo;
+    const bool none = sees_none(a, r, limit_of(a, r, tok), L);
     if (none) out = f32x4{0.f, 0.f, 0.f, 0.f};
     else out *= 1.f / L;
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.O) + head * a.o_stride + t * D + c * 4) = out;

@@ -36,7 +36,8 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
   const int s = max(0, seq_of_row(a.seqs, t));
   const bool even = a.seqs.per > 0;
   const int len = len_of(a, s), q0 = even ? s * a.seqs.per : a.seqs.q0[s], nq = even ? a.seqs.per : a.seqs.nq[s];
-  const bool none = len - (q0 + nq - t) + 1 <= 0;
+  const int lim = len - (q0 + nq - t) + 1;
+  bool none = lim <= 0;
   // where the shares of the row are: its row in the tiles over the common rows, and in those over its sequence's own
   const int kvh = a.by_rep.of(head), hh = head - kvh * a.rep, common = n_common(a);
   const int rho_c = (t - a.row0) * a.rep + hh, rho = (t - q0) * a.rep + hh;
@@ -109,7 +110,11 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsArgs a) {
     }
   }
   if (!there) return;
+  if (!none && L == 0.f)
+    none = !any_page(a, a.shared, 0, min(lim, a.n_shared)) &&
+           !any_page(a, a.table + (even ? s : a.seqs.k0[s]) * a.table_stride, a.n_shared, lim);
   if (!none) acc *= 1.f / L;
+  else acc = f32x4{0.f, 0.f, 0.f, 0.f};
   store4(static_cast<T*>(a.O) + head * a.o_stride + static_cast<int64_t>(t) * D + c * 4, acc);
   if (a.lse != nullptr && c == 0) a.lse[static_cast<int64_t>(head) * a.T + t] = none ? -INFINITY : lse_of(M, L);
 }

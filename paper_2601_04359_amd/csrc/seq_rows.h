@@ -74,6 +74,18 @@ __device__ __forceinline__ int limit_of(const RowsArgs& a, const RowSet& r, int 
   return min(max(len - (end - t) + 1, 0), r.n_keys);
 }
 
+// Whether any of keys from .. upto - 1 has a page.  Asked of rows whose weights add up to 0: they have seen nothing if none has (O = 0),
+// and otherwise scores of -inf alone, which are no numbers.
+__device__ __forceinline__ bool any_page(const RowsArgs& a, const int32_t* pages, int from, int upto) {
+  for (int p = a.by_page.of(from), last = a.by_page.of(upto - 1); from < upto && p <= last; ++p)
+    if (static_cast<uint32_t>(pages[p]) < static_cast<uint32_t>(a.n_pages)) return true;
+  return false;
+}
+// The same of a row's limit in its set; prompts have no pages, and all of their keys.
+__device__ __forceinline__ bool sees_none(const RowsArgs& a, const RowSet& r, int lim, float sum) {
+  return lim <= r.lo || (r.pages != nullptr && sum == 0.f && !any_page(a, r.pages, r.lo, lim));
+}
+
 // pc_prompt_attn: work-groups in the order of what they have to do, longest first (a causal tile's work goes with where
 // it ends, and the chip is filled from the front).  A tile's level is the number of row tiles' worth of keys in front of its
 // own; tiles of one level follow each other, KV heads fastest, so that with 1, 2, 4, 8 or more heads an XCD's

@@ -794,3 +794,58 @@ def test_page_attn_scores_of_minus_infinity_weigh_nothing(dtype, D, scale, lens,
     for s in range(2):
         mine = slice(s * n, (s + 1) * n)
         check_kept(dtype, O[:, mine], L[:, mine], Q[:, mine], pg.seqs[s], causal(n, lens[s], OVERFLOWS), scale)
+
+
+# ------------------------------------------------------------------------------ pages that are all missing
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("scale", [0.1, pk.PC_SCALE_FOLDED])
+@pytest.mark.parametrize("lens,n,shared,missing,missing_shared", [
+    ([1, 90], 1, 0, [(0, 0)], []),                                   # a padded place: one row, no page
+    ([200, 90], 1, 0, [(0, 0), (0, 1), (0, 2), (0, 3)], []),
+    ([100, 70], 70, 0, [(0, 0), (1, 0)], []),                        # the first page, and rows that begin in it
+    ([600, 300], 300, 0, [(0, 0), (0, 4), (0, 5), (1, 0), (1, 1)], []),
+    ([3000, 2900], 1, 0, [(1, i) for i in range(46)], []),           # joined shares
+    ([230, 214], 2, 200, [(1, 3)], [0, 1, 2, 3]),                    # nothing in common, and nothing of one's own
+    ([200, 200], 2, 200, [], [0, 1, 2, 3]),                          # common rows only
+    ([2700, 2750], 150, 2600, [(0, i) for i in range(40, 43)], list(range(41)))])
+def test_page_attn_rows_without_any_page(dtype, D, scale, lens, n, shared, missing, missing_shared):
+    """A row all of whose keys lie in pages that are not there sees nothing: O = 0, lse = -inf."""
+    pg = Paged(dtype, 2, D, lens, shared=shared)
+    gone = [set(), set()]
+    for s, i in missing:
+        pg.table[s, i] = -1 if i % 2 else 2 ** 30
+        gone[s] |= {j for j in range(i * 64, i * 64 + 64) if j >= shared}
+    for i in missing_shared:
+        pg.shared[i] = -1 if i % 2 else 2 ** 30
+        for s in range(2):
+            gone[s] |= {j for j in range(i * 64, i * 64 + 64) if j < shared}
+    Q = normal(generator(1), 4, 2 * n, D).to(TYPES[dtype])
+    L = torch.full((4, 2 * n), 7.0, device=DEV)
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max(lens), scale, shared=pg.shared, n_shared=shared, lse=L)
+    empty = 0
+    for s in range(2):
+        keep = causal(n, lens[s], gone[s])
+        nothing = ~keep.any(1)
+        empty += int(nothing.sum())
+        mine = slice(s * n, (s + 1) * n)
+        rows = [i for i in range(n) if n < 40 or i % 17 == 0 or i in (63, 64, n - 1)]
+        assert (O[:, mine][:, nothing] == 0).all() and (L[:, mine][:, nothing] == -float("inf")).all()
+        check_kept(dtype, O[:, mine][:, rows], L[:, mine][:, rows], Q[:, mine][:, rows], pg.seqs[s], keep[rows], scale, int(nothing[rows].sum()))
+    assert empty > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,n,shared", [([90, 70], 1, 0), ([90, 70], 70, 0), ([300, 320], 2, 200)])
+def test_page_attn_rows_without_any_page_do_not_hide_a_nan(dtype, lens, n, shared):
+    """A query that is not a number leaves none, with pages and beside rows without."""
+    pg = Paged(dtype, 2, 128, lens, shared=shared)
+    pg.table[0, :] = -1
+    if shared:
+        pg.shared[:] = -1
+    Q = normal(generator(1), 4, 2 * n, 128).to(TYPES[dtype])
+    Q[1, 2 * n - 1, 5], Q[2, 0, 5] = NAN, NAN
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max(lens), 0.1, shared=pg.shared, n_shared=shared)
+    assert O[1, 2 * n - 1].isnan().all() and (O[:, :n] == 0).all()
+    ok = torch.ones((4, 2 * n), dtype=torch.bool, device=DEV)
+    ok[1, 2 * n - 1] = False
+    assert O[ok].isfinite().all()
