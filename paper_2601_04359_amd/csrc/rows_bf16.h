@@ -29,7 +29,8 @@ __device__ __forceinline__ u32x4 finite_bf16(u32x4 v) {   // those as zeros
   for (int i = 0; i < 4; ++i) v[i] &= ~((odd_halves(v[i]) >> 15) * 0xFFFFu);
   return v;
 }
-// Those of a row of V added to a lane's output: dims 32 db + 8 a + 4 g .. + 3 are accumulators 4 a .. of block db.
+// Those of a row of V added to a lane's output, behind its last key: an infinity that went in earlier would meet the rescaling of
+// what it stands in, and 0 times it is no number.  dims 32 db + 8 a + 4 g .. + 3 are accumulators 4 a .. of block db.
 template <int kBlocks>
 __device__ __forceinline__ void add_odd(f32x16 (&o)[kBlocks], const uint16_t* v, int g) {
 #pragma unroll
@@ -97,6 +98,17 @@ struct KeyTiles {
   __device__ __forceinline__ int64_t at(int key, int pg) const {
     if constexpr (kPages) return pg * a.page_stride + static_cast<int64_t>(key - a.by_page.of(key) * a.by_page.d) * D;
     return static_cast<int64_t>(r.k0 + key) * D;
+  }
+  // Values that are not finite of keys from .. from + 31 of the tile that begins with key0 are added to the rows that see them, if
+  // some row does not (see all_below): they have been taken out of the tile.
+  template <int kBlocks>
+  __device__ __forceinline__ void add_odd_rows(f32x16 (&o)[kBlocks], int key0, int from, int all_below, int lim, int g) const {
+    if (key0 + kTile <= all_below && key0 >= r.lo) return;
+    const int pg = kPages ? r.pages[a.by_page.of(key0)] : 0;
+    if (kPages && (pg < 0 || pg >= a.n_pages)) return;
+    const uint16_t* rows = Vh + at(key0, pg);
+    for (int k = max(from, r.lo); k < min(from + 32, r.n_keys); ++k)
+      if (k < lim) add_odd(o, rows + static_cast<int64_t>(k - key0) * D, g);
   }
   // byte offset of chunk `chunk` of row key0 + row of a tile that begins with key0: rows that do not exist are read as the
   // nearest that does
@@ -259,11 +271,11 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m = kNothing, l = 0.f;
+  int odd_first = INT_MAX, odd_last = -1;   // steps with values that are not finite and not seen by all
   for (int i = 0;; ++i) {
     const int k0 = keys.key_of(i);
     if (k0 >= end) break;
     const bool now = there;
-    const int64_t at = kPages && now ? keys.at(k0, keys.page(i)) : keys.at(k0, 0);
     // This step's rows have landed (they are all that is in flight): every fragment goes to registers, so that the next
     // step's rows can be fetched into the same LDS at once.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -309,8 +321,7 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
 #pragma unroll
         for (int db = 0; db < kBlocks; ++db) odd |= odd_bf16(__builtin_bit_cast(u32x4, vf[ks][db]));
       if (__any(odd != 0)) {
-        for (int j = max(k0, r.lo); j < min(k0 + kFewKeys, r.n_keys); ++j)
-          if (j < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(j - k0) * D, g);
+        odd_first = min(odd_first, i), odd_last = i;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -353,6 +364,7 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // a first step that was needed by none may be in flight
   l = wave_half_sum(l);
+  for (int i = odd_first; i <= odd_last; ++i) keys.add_odd_rows(o, keys.key_of(i), keys.key_of(i), lim_min, lim, g);
 
   merge_waves<D, 1, kFewWaves>(a, r, smem, o, m, l, wave, lane);
 }
@@ -465,6 +477,7 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
     for (int e = 0; e < 8; ++e) pA[ks][e] = pB[ks][e] = static_cast<__bf16>(0.f);
   float m_ref = -INFINITY, l_run = 0.f;
   bool redo_all = false;   // wave-uniform
+  int odd_first = INT_MAX, odd_last = -1;   // tiles with values that are not finite and not seen by all
 
   // hides what a row does not see of the 32 keys from key0 on; `there`: they have a page
   auto mask = [&](f32x16& sc, int key0, bool there) {
@@ -513,18 +526,14 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
       if (j + 2 < n) stage(std::false_type{}, j + 2, pg_after, k_cur);
       if (j + 1 < n) stage(std::true_type{}, j + 1, pg_next, v_prev);
       if (key0 + kManyKeys > all_min || key0 < r.lo) {
-        // Some row does not see all of this tile, and 0 times what is not finite would reach it: such values are added to
-        // the rows that see them and taken out of the tile.
+        // Some row does not see all of this tile, and 0 times what is not finite would reach it: such values are taken out of
+        // the tile and added to the rows that see them in the end.
         lds_u32x4* mine = reinterpret_cast<lds_u32x4*>(smem + v_cur) + threadIdx.x * 4;
         uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) odd |= odd_bf16(mine[i]);
         if (__syncthreads_or(odd != 0)) {
-          if (active) {
-            const int64_t at = pg >= 0 ? keys.at(key0, pg) : 0;
-            for (int k = max(key0, r.lo); pg >= 0 && k < min(key0 + kManyKeys, r.n_keys); ++k)
-              if (k < lim) add_odd(o, keys.Vh + at + static_cast<int64_t>(k - key0) * kD, g);
-          }
+          odd_first = min(odd_first, j), odd_last = j;
 #pragma unroll
           for (int i = 0; i < 4; ++i) mine[i] = finite_bf16(mine[i]);
           __syncthreads();
@@ -560,6 +569,9 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
           }
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pB[ks], o[db], 0, 0, 0);
         }
+      for (int j = odd_first; j <= odd_last; ++j)
+#pragma unroll 1
+        for (int half = 0; half < 64; half += 32) keys.add_odd_rows(o, keys.key_of(j), keys.key_of(j) + half, all_min, lim, g);
     }
   }
   const float l_tot = wave_half_sum(l_run);
@@ -722,6 +734,7 @@ __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds
     for (int e = 0; e < 8; ++e) pA[ks][e] = pB[ks][e] = static_cast<__bf16>(0.f);
   float m_ref = -INFINITY, l_run = 0.f;
   bool redo_all = false;   // wave-uniform
+  int odd_first = INT_MAX, odd_last = -1;   // as in rows_many
 
   // hides what a row does not see of its half of tile j, whose page is pg
   auto mask = [&](f32x16& sc, int j, int pg) {
@@ -771,18 +784,13 @@ __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds
       if (j + 1 < n) stage(std::true_type{}, j + 1, pg_next, v_prev);
       const int key0 = r.begin + j * kKeys;
       if (key0 + kKeys > all_min || key0 < r.lo) {
-        // as in rows_many; a wave adds what is in its half
+        // as in rows_many; a wave adds what is in its half in the end
         lds_u32x4* mine = reinterpret_cast<lds_u32x4*>(smem + v_cur) + threadIdx.x * 4;
         uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) odd |= odd_bf16(mine[i]);
         if (__syncthreads_or(odd != 0)) {
-          const int k0 = key0 + kg * 32;
-          if (active && pg >= 0) {
-            const uint16_t* rows = keys.Vh + keys.at(key0, pg);
-            for (int k = max(k0, r.lo); k < min(k0 + 32, r.n_keys); ++k)
-              if (k < lim) add_odd(o, rows + static_cast<int64_t>(k - key0) * kD, g);
-          }
+          odd_first = min(odd_first, j), odd_last = j;
 #pragma unroll
           for (int i = 0; i < 4; ++i) mine[i] = finite_bf16(mine[i]);
           __syncthreads();
@@ -815,6 +823,7 @@ __device__ __forceinline__ void rows_mid(const RowsArgs& a, const RowSet& r, lds
           }
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, odd ? pA[ks] : pB[ks], o[db], 0, 0, 0);
         }
+      for (int i = odd_first; i <= odd_last; ++i) keys.add_odd_rows(o, keys.key_of(i), keys.key_of(i) + kg * 32, all_min, lim, g);
     }
   }
   float l_tot = wave_half_sum(l_run), m_end = fmaxf(m_ref, kNothing);

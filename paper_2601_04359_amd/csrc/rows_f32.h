@@ -8,7 +8,8 @@
 //   * A score is s (c + c_lo), and the reference is subtracted from the rounded product: the largest key's exponent is 0
 //     however large the logits are.  c_lo > 0: a score of -inf stays one.
 //   * A key that a row does not see has p = 0, and 0 times a NaN in V would reach the row: in steps where some row does not
-//     see all keys, values that are not finite are taken out of the product and added to the rows that see them.
+//     see all keys, values that are not finite are taken out of the product and added to the rows that see them, behind the last
+//     key: an infinity that went in earlier would meet the rescaling of what it stands in.
 // K and V come straight from L2 to registers, the next step's K behind this one's scores and its V behind this one's
 // products.  Bound: what a compute unit draws from L2 with 16 rows (16 KB per 2 x 32 products of 32 cycles and wave at D = 128),
 // the products with 32; latency where there are few keys, which is why 16 rows come with eight waves.  Measured, D = 128: prompts of
@@ -126,6 +127,7 @@ __device__ __forceinline__ void rows_f32(const RowsArgs& a, const RowSet& r, flo
   };
 
   int kb = r.begin + wave * kF32Keys;
+  int odd_first = INT_MAX, odd_last = -1;   // first keys of steps with such values
   if (kb < end) {
     Place now = place(kb);
     load_k(now, kb);
@@ -163,19 +165,7 @@ __device__ __forceinline__ void rows_f32(const RowsArgs& a, const RowSet& r, flo
               for (int i = 0; i < 4; ++i) odd |= odd_mask(vf[e][db][i]);
           }
           if (__any(odd != 0)) {
-            for (int j = max(kb, r.lo); j < min(kb + kF32Keys, r.n_keys); ++j)
-#pragma unroll
-              for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
-                  const f32x4 v = load_16B(Vh + row_at(now, j) + db * 64 + kg * 16 + i * 4);
-#pragma unroll
-                  for (int n = 0; n < kQ; ++n)
-                    if (j < lim[n]) {
-#pragma unroll
-                      for (int e = 0; e < 4; ++e) acc[n][db][e][i] += __uint_as_float(__float_as_uint(v[e]) & odd_mask(v[e]));
-                    }
-                }
+            odd_first = min(odd_first, kb), odd_last = kb;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -220,6 +210,24 @@ __device__ __forceinline__ void rows_f32(const RowsArgs& a, const RowSet& r, flo
       now = next;
       kb = kb_next;
     } while (kb < end);
+#pragma unroll 1
+    for (kb = odd_first; kb <= odd_last; kb += kW * kF32Keys) {
+      const Place t = place(kb);
+      if (!t.there || !(kb + kF32Keys > lim_min || kb < r.lo)) continue;
+      for (int j = max(kb, r.lo); j < min(kb + kF32Keys, r.n_keys); ++j)
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {   // this lane's dims 64 db + 16 kg + 4 i + e are rows 4 kg + i of block (db, e)
+            const f32x4 v = load_16B(Vh + row_at(t, j) + db * 64 + kg * 16 + i * 4);
+#pragma unroll
+            for (int n = 0; n < kQ; ++n)
+              if (j < lim[n]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][db][e][i] += __uint_as_float(__float_as_uint(v[e]) & odd_mask(v[e]));
+              }
+          }
+    }
   }
 
   if constexpr (kQ > 1) __syncthreads();   // the queries have been read by all

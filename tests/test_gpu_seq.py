@@ -849,3 +849,47 @@ def test_page_attn_rows_without_any_page_do_not_hide_a_nan(dtype, lens, n, share
     ok = torch.ones((4, 2 * n), dtype=torch.bool, device=DEV)
     ok[1, 2 * n - 1] = False
     assert O[ok].isfinite().all()
+
+
+# ------------------------------------------------------------------------------ infinities that are seen
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,n", [("bf16", 128, 8, 2, 40), ("bf16", 64, 8, 2, 300), ("bf16", 128, 16, 4, 2049), ("bf16", 128, 3, 3, 3001),
+                                              ("f32", 128, 4, 2, 150), ("f32", 64, 2, 1, 1100)])
+@pytest.mark.parametrize("at", [0, 5, 31, 33, -1, -40])
+@pytest.mark.parametrize("scale", [0.1, pk.PC_SCALE_FOLDED])
+def test_prompt_an_infinity_that_is_seen_arrives_as_one(dtype, D, Hq, Hkv, n, at, scale):
+    """A single infinite value in V: infinite in its dim in the rows that see it, whatever tile or form it is read by, and numbers
+    everywhere else."""
+    gen, at = generator(n), at % n
+    Q, K, V = (normal(gen, H, n, D).to(TYPES[dtype]) for H in (Hq, Hkv, Hkv))
+    V[:, at, 9], V[:, at, D - 1] = float("inf"), -float("inf")
+    O = pk.pc_prompt_attn(Q, K, V, scale, [0, n])
+    assert (O[:, at:, 9] == float("inf")).all() and (O[:, at:, D - 1] == -float("inf")).all()
+    V[:, at, 9], V[:, at, D - 1] = 0.0, 0.0
+    rest = torch.ones((n, D), dtype=torch.bool, device=DEV)
+    rest[at:, 9], rest[at:, D - 1] = False, False
+    assert torch.equal(O[:, rest], pk.pc_prompt_attn(Q, K, V, scale, [0, n])[:, rest])
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,shared", [(1, 0), (6, 0), (50, 0), (300, 0), (6, 40), (50, 40), (300, 40), (300, 1960)])
+@pytest.mark.parametrize("back", [1, 2, 40, None])
+@pytest.mark.parametrize("scale", [0.1, pk.PC_SCALE_FOLDED])
+def test_page_attn_an_infinity_that_is_seen_arrives_as_one(dtype, D, n, shared, back, scale):
+    """back: so many rows in front of the sequence's end; None: the first row behind the common ones."""
+    lens = [shared + 330, shared + 400, shared + 301]
+    at = lens[1] - back if back is not None else shared
+    pg = Paged(dtype, 2, D, lens, shared=shared)
+    Q = normal(generator(2), 8, 3 * n, D).to(TYPES[dtype])
+    call = lambda: pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max(lens), scale, shared=pg.shared, n_shared=shared)
+
+    def put(x, y):
+        pg.seqs[1][1][:, at, 9], pg.seqs[1][1][:, at, D - 1] = x, y
+        rewrite(pg, lambda K, V: None)
+    put(float("inf"), -float("inf"))
+    O = call()
+    first = n + max(0, at - (lens[1] - n))      # the rows of the sequence that see it
+    assert (O[:, first:2 * n, 9] == float("inf")).all() and (O[:, first:2 * n, D - 1] == -float("inf")).all()
+    put(0.0, 0.0)
+    rest = torch.ones((3 * n, D), dtype=torch.bool, device=DEV)
+    rest[first:2 * n, 9], rest[first:2 * n, D - 1] = False, False
+    assert torch.equal(O[:, rest], call()[:, rest])
