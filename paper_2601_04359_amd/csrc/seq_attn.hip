@@ -417,7 +417,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
       a.seqs.q0[s] = q.q0, a.seqs.nq[s] = q.nq, a.seqs.k0[s] = q.k0, a.seqs.nk[s] = q.nk;
       const int tiles = ceil_div(q.nq * rep, rows);
       a.n_tiles += tiles;
-      a.max_level = std::max(a.max_level, static_cast<int>(static_cast<int64_t>(std::max(0, q.nk - q.nq)) * rep / rows) + tiles);
+      a.max_level = std::max(a.max_level, level_of(q.nq, q.nk, rep, rows) + tiles);
     }
     if (int rc = launch_rows<false>(who, plan.form, dtype, D, a, (a.n_tiles + a.n_heavy) * Hkv, st)) return rc;
   }

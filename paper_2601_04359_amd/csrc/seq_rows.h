@@ -90,6 +90,11 @@ __device__ __forceinline__ bool sees_none(const RowsArgs& a, const RowSet& r, in
 // it ends, and the chip is filled from the front).  A tile's level is the number of row tiles' worth of keys in front of its
 // own; tiles of one level follow each other, KV heads fastest, so that with 1, 2, 4, 8 or more heads an XCD's
 // work-groups read few of them.
+// (beyond 2^29 rows' worth the order no longer matters, and levels stay numbers of 32 bits)
+__host__ __device__ inline int level_of(int nq, int nk, int rep, int rows) {
+  const int64_t level = nk > nq ? static_cast<int64_t>(nk - nq) * rep / rows : 0;
+  return static_cast<int>(level < (1 << 29) ? level : 1 << 29);
+}
 template <int R>
 __device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int u, int kvh, int lane) {   // tile u of a KV head
   RowSet r = {};
@@ -100,7 +105,7 @@ __device__ __forceinline__ RowSet prompt_rows(const RowsArgs& a, int u, int kvh,
   } else {
     const int nq = lane < a.seqs.n ? a.seqs.nq[lane] : 0, nk = lane < a.seqs.n ? a.seqs.nk[lane] : 0;
     const int tiles = (nq * a.rep + R - 1) / R;
-    const int base = nk > nq ? static_cast<int>(static_cast<int64_t>(nk - nq) * a.rep / R) : 0;
+    const int base = level_of(nq, nk, a.rep, R);
     auto above = [&](int x) {   // tiles of level x or more
       return __builtin_amdgcn_readlane(wave_prefix_sum(min(max(base + tiles - x, 0), tiles)), 63);
     };

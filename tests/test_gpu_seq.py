@@ -893,3 +893,20 @@ def test_page_attn_an_infinity_that_is_seen_arrives_as_one(dtype, D, n, shared, 
     rest = torch.ones((3 * n, D), dtype=torch.bool, device=DEV)
     rest[first:2 * n, 9], rest[first:2 * n, D - 1] = False, False
     assert torch.equal(O[:, rest], call()[:, rest])
+
+
+# ------------------------------------------------------------------------------ many query heads behind many keys
+@pytest.mark.parametrize("dtype,D,Hq", [("bf16", 64, 2 ** 16), ("bf16", 128, 2 ** 19)])
+def test_prompt_tiles_behind_more_than_32_bits_of_rows(dtype, D, Hq):
+    """Two sequences of one token in very many heads of one KV head, one of them behind 2^20 keys: the keys in front of it, counted in
+    row tiles (of 32 and of 128 rows), are beyond 2^31."""
+    nk = [100, 2 ** 20 + 5000]
+    gen, oq, ok = generator(6), [0, 1, 2], offsets(nk)
+    Q = normal(gen, Hq, 2, D).to(TYPES[dtype])
+    K, V = (normal(gen, 1, ok[-1], D).to(TYPES[dtype]) for _ in range(2))
+    L = torch.empty((Hq, 2), device=DEV)
+    O = pk.pc_prompt_attn(Q, K, V, D ** -0.5, oq, ok, lse=L)
+    for h in (0, 1, 31, 32, 127, 128, 40000, Hq - 1):
+        for s in range(2):
+            mine = slice(ok[s], ok[s + 1])
+            check_rows(dtype, O[h, s:s + 1], L[h, s:s + 1], Q[h, s:s + 1], K[0, mine], V[0, mine], D ** -0.5, nk[s])
