@@ -183,27 +183,29 @@ extern "C" int pc_page_store(const void* K, const void* V, int dtype, int Hkv, i
   }
   const int items = kTokPerBlock * a.by_chunks.d * (2 * ceil_div(Hkv, kHeadsInFlight) + ceil_div(a.Hq, kHeadsInFlight));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  auto launch = [&](int row0, int n_rows) {
-    a.row0 = row0, a.n_rows = n_rows;
-    const int blocks = ceil_div(n_rows, kTokPerBlock);
-    const dim3 grid(blocks, std::min(ceil_div(items, kThreads), ceil_div(512, blocks)));
-    auto* kernel = dtype == PC_BF16 ? (turn ? page_store_kernel<uint16_t, true> : page_store_kernel<uint16_t, false>)
-                                    : (turn ? page_store_kernel<float, true> : page_store_kernel<float, false>);
-    kernel<<<grid, kThreads, 0, st>>>(a);
+  auto launch = [&](int row0, int n_rows) -> int {
+    constexpr int kMost = static_cast<int>(kMaxThreads / kThreads) * kTokPerBlock;   // rows of a launch
+    for (int done = 0; done < n_rows; done += a.n_rows) {
+      a.row0 = row0 + done, a.n_rows = std::min(n_rows - done, kMost);
+      const int blocks = ceil_div(a.n_rows, kTokPerBlock);
+      const dim3 grid(blocks, std::min(ceil_div(items, kThreads), ceil_div(512, blocks)));
+      auto* kernel = dtype == PC_BF16 ? (turn ? page_store_kernel<uint16_t, true> : page_store_kernel<uint16_t, false>)
+                                      : (turn ? page_store_kernel<float, true> : page_store_kernel<float, false>);
+      kernel<<<grid, kThreads, 0, st>>>(a);
+      PC_CHECK_LAUNCH(who);
+    }
+    return PC_OK;
   };
   if (offs == nullptr) {
     a.seqs.n = n_seq, a.seqs.per = T / n_seq, a.seqs.by_per = Divisor(T / n_seq);
-    launch(0, T);
-    PC_CHECK_LAUNCH(who);
-    return PC_OK;
+    return launch(0, T);
   }
   for (int s0 = 0; s0 < n_seq; s0 += kSeqs) {
     const int n = std::min(kSeqs, n_seq - s0), rows = offs[s0 + n] - offs[s0];
     if (rows == 0) continue;
     a.seqs.n = n, a.seqs.per = 0;
     for (int s = 0; s < n; ++s) a.seqs.q0[s] = offs[s0 + s], a.seqs.nq[s] = offs[s0 + s + 1] - offs[s0 + s], a.seqs.k0[s] = s0 + s;
-    launch(offs[s0], rows);
-    PC_CHECK_LAUNCH(who);
+    if (int rc = launch(offs[s0], rows)) return rc;
   }
   return PC_OK;
 }

@@ -8,6 +8,8 @@ namespace pc {
 constexpr int kSeqs = 64;        // sequences of one launch's table: one per lane of a wave
 constexpr int kPageStep = 64;    // pages are a multiple of this many rows: no tile of keys crosses one
 
+constexpr int64_t kMaxThreads = UINT32_MAX;   // of a launch along one axis
+
 // The sequences of a launch, by value.  per > 0: `n` sequences of `per` rows each, and the arrays are not looked at.
 struct SeqTable {
   int n, per;

@@ -327,7 +327,9 @@ int check_attn(const char* who, int dtype, int Hq, int Hkv, int D, float scale) 
 }
 
 template <bool kPages>
-int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a, int blocks, hipStream_t s) {
+int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a, int64_t blocks, hipStream_t s) {
+  const int waves = form == kF32Two ? 4 : form == kF32One ? 8 : form == kFew ? kFewWaves : kManyWaves;
+  PC_REQUIRE(blocks * waves * 64 <= kMaxThreads, PC_ERR_UNSUPPORTED, "%s: %lld work-groups in one launch", who, static_cast<long long>(blocks));
   if (form == kF32One || form == kF32Two) {
     static std::atomic<uint64_t> ok[4];
     const bool two = form == kF32Two;
@@ -336,13 +338,13 @@ int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a,
     const size_t bytes = (D == 128 ? kF32Smem<128, 2, 4> : kF32Smem<64, 2, 4>) + kPlanBytes;
     static_assert(kF32Smem<128, 2, 4> == kF32Smem<128, 1, 8> && kF32Smem<64, 2, 4> == kF32Smem<64, 1, 8>, "the waves' O");
     if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[(D == 128) * 2 + two], who)) return rc;
-    kernel<<<blocks, (two ? 4 : 8) * 64, bytes, s>>>(a);
+    kernel<<<blocks, waves * 64, bytes, s>>>(a);
   } else if (form == kFew) {
     static std::atomic<uint64_t> ok[2];
     auto* kernel = D == 128 ? rows_few_kernel<128, kPages> : rows_few_kernel<64, kPages>;
     const size_t bytes = (D == 128 ? kFewSmem<128> : kFewSmem<64>) + kPlanBytes;
     if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, ok[D == 128], who)) return rc;
-    kernel<<<blocks, kFewWaves * 64, bytes, s>>>(a);
+    kernel<<<blocks, waves * 64, bytes, s>>>(a);
   } else {
     static std::atomic<uint64_t> ok[4];
     const bool unit_c = a.c == 1.0f, many = form == kMany;
@@ -353,7 +355,7 @@ int launch_rows(const char* who, Form form, int dtype, int D, const RowsArgs& a,
       kernel = unit_c ? rows_prompt_kernel<true> : rows_prompt_kernel<false>;
     constexpr size_t kBytes = std::max(kManySmem, kMidSmem) + (kPages ? kPlanBytes : 0);
     if (int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kBytes, ok[many * 2 + unit_c], who)) return rc;
-    kernel<<<blocks, kManyWaves * 64, kBytes, s>>>(a);
+    kernel<<<blocks, waves * 64, kBytes, s>>>(a);
   }
   PC_CHECK_LAUNCH(who);
   return PC_OK;
@@ -419,7 +421,7 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
       a.n_tiles += tiles;
       a.max_level = std::max(a.max_level, level_of(q.nq, q.nk, rep, rows) + tiles);
     }
-    if (int rc = launch_rows<false>(who, plan.form, dtype, D, a, (a.n_tiles + a.n_heavy) * Hkv, st)) return rc;
+    if (int rc = launch_rows<false>(who, plan.form, dtype, D, a, static_cast<int64_t>(a.n_tiles + a.n_heavy) * Hkv, st)) return rc;
   }
   return PC_OK;
 }
@@ -508,7 +510,7 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
       a.part_ml = reinterpret_cast<float2*>(at + plan.o_bytes(Hkv, D));
       a.cut = reinterpret_cast<int*>(at + plan.o_bytes(Hkv, D) + plan.ml_bytes(Hkv));
     }
-    if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, plan.units() * Hkv, st)) return rc;
+    if (int rc = launch_rows<true>(who, plan.form, dtype, D, a, static_cast<int64_t>(plan.units()) * Hkv, st)) return rc;
     if (!plan.joined) return PC_OK;
     // Few rows: one per work-group, its shares read by eight groups of threads at once; else eight rows (sixteen at D = 64).  Eight
     // at once | one, whole calls, 16/4 heads, us: 512 rows per head of 9 shares 151 | 142, 256 of 5 shares 53 | 47; 24/8 heads,

@@ -910,3 +910,23 @@ def test_prompt_tiles_behind_more_than_32_bits_of_rows(dtype, D, Hq):
         for s in range(2):
             mine = slice(ok[s], ok[s + 1])
             check_rows(dtype, O[h, s:s + 1], L[h, s:s + 1], Q[h, s:s + 1], K[0, mine], V[0, mine], D ** -0.5, nk[s])
+
+
+# ------------------------------------------------------------------------------ rows beyond one launch
+def test_store_of_more_rows_than_a_launch_has_threads_for():
+    """2^26 + 1,000 rows of one sequence, of which the pages hold the last 500; four rows take 256 threads."""
+    T, D, n = 2 ** 26 + 1000, 64, 500
+    K, V = (torch.zeros((1, T, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    gen = generator(8)
+    for x in (K, V):
+        x[:, T - 600:] = normal(gen, 1, 600, D).to(torch.bfloat16)
+    pages, table = pk.page_cache(9, 1, 64, D), torch.arange(8, 0, -1, dtype=torch.int32, device=DEV)[None].contiguous()
+    K_out = torch.empty_like(K)
+    for offs in (None, [0, T]):
+        for x in (*pages, K_out):
+            x.fill_(7.0)
+        pk.pc_page_store(K, V, pages, table, torch.tensor([n], dtype=torch.int32, device=DEV), offs=offs, K_out=K_out)
+        for pool, x in zip(pages, (K, V)):
+            got = pool[table[0].long(), 0].reshape(-1, D)
+            assert torch.equal(got[:n], x[0, T - n:]) and (got[n:] == 7.0).all() and (pool[0] == 7.0).all()
+        assert torch.equal(K_out, K)

@@ -252,3 +252,15 @@ def test_stack_of_sequences_refuses():
     for f in (s.close, s.fork, s.rows):
         with pytest.raises(ValueError):
             f(c)
+
+
+# ------------------------------------------------------------------------------ launches
+@pytest.mark.parametrize("dtype,D", [(pk.PC_BF16, 128), (pk.PC_BF16, 64), (pk.PC_F32, 128), (pk.PC_F32, 64)])
+def test_more_work_groups_than_a_launch_has_threads_for(L, dtype, D):
+    """Threads of a launch fit 32 bits: calls with more are refused, and not left to fail behind the checks."""
+    H = 2 ** 24
+    kw = dict(dtype=dtype, D=D, Hq=H, Hkv=H)
+    assert prompt(L, **kw, Tq=1, Tk=1, n=1, oq=[0, 1], qs=D, ks=D, vs=D, os=D) == UNSUPPORTED, L.pc_last_error_detail()
+    assert prompt(L, **kw, Tq=60, Tk=60, n=60, oq=list(range(61)), qs=60 * D, ks=60 * D, vs=60 * D, os=60 * D) == UNSUPPORTED
+    pg = pages(stride_h=64 * D, stride_page=64 * D * H, n_pages=1)
+    assert attn(L, pg, **kw, T=1, n=1, max_len=64, width=1, ts=1, qs=D, os=D, wb=1 << 40) == UNSUPPORTED, L.pc_last_error_detail()
