@@ -246,6 +246,7 @@ struct PagePlan {
   bool joined = false;           // results are shares
   PagePlan(int dtype, int D, int Hkv, int rep, int T, const int32_t* offs, int n_seq, int n_shared, int max_len) {
     const int n_rows = offs != nullptr ? offs[n_seq] - offs[0] : T;
+    if (n_rows == 0) return;       // nothing is launched
     const int own = max_len > n_shared ? max_len - n_shared / kPageStep * kPageStep : 0;
     int most = offs == nullptr ? T / n_seq : 0;
     for (int s = 0; offs != nullptr && s < n_seq; ++s) most = std::max(most, offs[s + 1] - offs[s]);

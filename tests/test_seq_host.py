@@ -264,3 +264,27 @@ def test_more_work_groups_than_a_launch_has_threads_for(L, dtype, D):
     assert prompt(L, **kw, Tq=60, Tk=60, n=60, oq=list(range(61)), qs=60 * D, ks=60 * D, vs=60 * D, os=60 * D) == UNSUPPORTED
     pg = pages(stride_h=64 * D, stride_page=64 * D * H, n_pages=1)
     assert attn(L, pg, **kw, T=1, n=1, max_len=64, width=1, ts=1, qs=D, os=D, wb=1 << 40) == UNSUPPORTED, L.pc_last_error_detail()
+
+
+# ------------------------------------------------------------------------------ workspaces
+@pytest.mark.parametrize("dtype", [pk.PC_BF16, pk.PC_F32])
+@pytest.mark.parametrize("shared", [0, 70])
+@pytest.mark.parametrize("offs", [[0, 0, 0], [2, 2, 2], [3] * 131])
+def test_calls_without_rows_need_no_workspace(L, dtype, shared, offs):
+    n = len(offs) - 1
+    assert L.pc_page_attn_workspace_bytes(dtype, 8, 2, 4, 64, ints(offs), n, 100, shared) == 0
+    kw = dict(dtype=dtype, offs=offs, n=n, shared=10 * A if shared else None, n_shared=shared, ws=None, wb=0, D=64, qs=256, os=256)
+    assert attn(L, pages(stride_h=64 * 64, stride_page=2 * 64 * 64), **kw) == 0, L.pc_last_error_detail()
+
+
+@pytest.mark.parametrize("dtype", [pk.PC_BF16, pk.PC_F32])
+@pytest.mark.parametrize("Hq,Hkv,T,n_seq,max_len,shared,joined", [
+    (8, 2, 4, 4, 100, 50, True),                # common rows and others
+    (8, 2, 4, 4, 64, 64, False),                # nothing but common rows, few
+    (8, 2, 4, 4, 64, 0, False), (8, 2, 1, 1, 1, 0, False),
+    (8, 2, 1, 1, 1 << 20, 0, True),             # one row behind many
+    (8, 2, 1, 1, 40000, 40000, True), (16, 4, 64, 64, 42000, 41800, True), (1, 1, 1, 1, 1 << 29, 1 << 28, True)])
+def test_workspaces_hold_the_shares_that_are_joined(L, dtype, Hq, Hkv, T, n_seq, max_len, shared, joined):
+    for D in (64, 128):
+        size = L.pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, None, n_seq, max_len, shared)
+        assert size >= 2 * Hq * T * (D + 2) * 4 if joined else size == 0      # two shares of every row at least
