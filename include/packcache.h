@@ -471,7 +471,7 @@ int pc_q4_evict(const pc_q4_cache* cache, int H, int D, int32_t* pos, int64_t po
  *   offs_q   HOST, offsets of Q's rows;  offs_k  HOST or NULL, offsets of K's and V's rows (NULL: offs_q).
  *            nk > nq: the rows are the last ones of a sequence whose earlier keys are there already;
  *            nk < nq: the first nq - nk rows see nothing: O = 0, lse = -inf.
- *   lse      dev or NULL, fp32 [Hq][Tq] = ln sum_j exp(scale * q.k_j) over the keys seen
+ *   lse      dev or NULL, fp32 [Hq][Tq] = ln sum_j exp(scale * q.k_j) over the keys seen; apart from the others as O is
  *   scale    > 0; PC_SCALE_FOLDED as in pc_frame_attn
  * What a row does not see does not reach it, a NaN or an infinity there neither.
  * Errors: PC_ERR_NULL, PC_ERR_DTYPE, PC_ERR_SHAPE, PC_ERR_UNSUPPORTED, PC_ERR_HIP.
@@ -503,6 +503,8 @@ typedef struct pc_pages {
  *   K_out    dev or NULL, [Hkv][T][D]: the keys as stored, e.g. for pc_prompt_attn; may be K itself
  *   Q, Q_out dev or NULL, [Hq][T][D]: queries to be turned and multiplied by out_scale, and where they go (may be Q
  *            itself); they need pos.  Rows of nobody are not turned.
+ * But for K_out = K and Q_out = Q (address and head stride) K_out and Q_out have no byte in common with an input, the pages or
+ * each other.  K, V and Q may be rows of pages that this call does not write.
  * A row whose r is negative or beyond the table, or whose page number is not one of 0 .. n_pages - 1, is not stored
  * (lens[s] = 0: a sequence that pauses); Q_out and K_out are written all the same.  Two rows that are sent to the same
  * place leave either.
@@ -525,7 +527,7 @@ int pc_page_store(const void* K, const void* V, int dtype, int Hkv, int T, int D
  *   shared, n_shared   dev int32 [ceil(n_shared / page_rows)] or NULL, 0: the first n_shared rows of every sequence
  *            are the same (a common prompt, one video's cache).  They are read through `shared`, once for all
  *            sequences, the rows behind them through `table`.  A sequence of fewer rows sees that many of them.
- *   lse      dev or NULL, fp32 [Hq][T]
+ *   lse      dev or NULL, fp32 [Hq][T].  O, lse and ws have no byte in common with each other, Q or the pages
  *   ws       dev, pc_page_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls that may
  *            overlap on the GPU must not share one.
  * A row that sees nothing (lens[s] = 0, or none of its pages is there) gets O = 0 and lse = -inf.  A page number that is not

@@ -168,6 +168,18 @@ extern "C" int pc_page_store(const void* K, const void* V, int dtype, int Hkv, i
     PC_REQUIRE(aligned_16B(Q, q_stride_h, elt) && aligned_16B(Q_out, q_out_stride_h, elt), PC_ERR_SHAPE,
                "%s: tensors and head strides must be 16-byte aligned", who);
   }
+  // what is written is nobody's input, but for rows that take the place of their own
+  const int64_t bytes = per_head * elt;
+  const Extent at_k = {K, Hkv, bytes, k_stride_h * elt}, at_v = {V, Hkv, bytes, v_stride_h * elt}, at_q = {Q, Hq, bytes, q_stride_h * elt},
+               to_k = {K_out, Hkv, bytes, k_out_stride_h * elt}, to_q = {Q_out, Hq, bytes, q_out_stride_h * elt};
+  PC_REQUIRE(to_k.is(at_k) || !meet(to_k, at_k), PC_ERR_SHAPE, "%s: K_out is neither K nor apart from it", who);
+  PC_REQUIRE(to_q.is(at_q) || !meet(to_q, at_q), PC_ERR_SHAPE, "%s: Q_out is neither Q nor apart from it", who);
+  PC_REQUIRE(!meet(to_k, at_v) && !meet(to_k, at_q) && !meet(to_q, at_k) && !meet(to_q, at_v) && !meet(to_k, to_q), PC_ERR_SHAPE,
+             "%s: K_out or Q_out overlaps another input or each other", who);
+  for (const void* p : {pages->K, pages->V}) {
+    const Extent to = extent_of(p, *pages, Hkv, D, elt);
+    PC_REQUIRE(!meet(to_k, to) && !meet(to_q, to), PC_ERR_SHAPE, "%s: K_out and Q_out may not lie in the pages", who);
+  }
   const bool turn = pos != nullptr;
   StoreArgs a = {};
   a.K = K, a.V = V, a.Q = Q, a.K_out = K_out, a.Q_out = Q_out, a.K_pages = pages->K, a.V_pages = pages->V;

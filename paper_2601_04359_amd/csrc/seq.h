@@ -42,13 +42,37 @@ inline bool aligned_16B(const void* p, int64_t stride, int elt) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * elt % 16 == 0;
 }
 
-// Whether any of Ha heads of a_bytes, a_stride bytes apart, shares a byte with any of Hb heads of b.
-inline bool overlap(const void* a, int64_t a_stride, int Ha, int64_t a_bytes, const void* b, int64_t b_stride, int Hb, int64_t b_bytes) {
-  const int64_t gap = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
-  if (gap >= (Ha - 1) * a_stride + a_bytes || -gap >= (Hb - 1) * b_stride + b_bytes) return false;
-  for (int i = 0; i < Ha; ++i)
-    for (int j = 0; j < Hb; ++j)
-      if (gap + j * b_stride < i * a_stride + a_bytes && i * a_stride < gap + j * b_stride + b_bytes) return true;
+// What a tensor takes of the memory: n heads of `bytes` each, and where it is a cache in pages, as many of them `page_stride` apart.
+// Strides in bytes.
+struct Extent {
+  const void* at;
+  int n;
+  int64_t bytes, stride;
+  int pages = 1;
+  int64_t page_stride = 0;
+  int64_t span() const { return (n - 1) * stride + (pages - 1) * page_stride + bytes; }
+  bool is(const Extent& y) const { return at == y.at && n == y.n && bytes == y.bytes && (n == 1 || stride == y.stride); }
+};
+// Whether two of them have a byte in common.  At most one is in pages.
+inline bool meet(const Extent& x, const Extent& y) {
+  if (x.pages > 1) return meet(y, x);
+  if (x.at == nullptr || y.at == nullptr) return false;
+  const int64_t gap = static_cast<int64_t>(reinterpret_cast<uintptr_t>(y.at) - reinterpret_cast<uintptr_t>(x.at));
+  if (gap >= x.span() || -gap >= y.span()) return false;
+  // whether for an r of 0 .. n - 1 the y.bytes from d + r step on meet the x.bytes from 0 on: the first r that ends behind 0
+  auto any = [&](int64_t d, int64_t step, int n) {
+    const int64_t r = d > -y.bytes || n == 1 ? 0 : (-y.bytes - d) / step + 1;
+    return r < n && d + r * step > -y.bytes && d + r * step < x.bytes;
+  };
+  for (int i = 0; i < x.n; ++i) {
+    const int64_t d = gap - i * x.stride;
+    if (y.pages == 1) {
+      if (any(d, y.stride, y.n)) return true;
+    } else {
+      for (int j = 0; j < y.n; ++j)
+        if (any(d + j * y.stride, y.page_stride, y.pages)) return true;
+    }
+  }
   return false;
 }
 
@@ -63,6 +87,10 @@ inline int check_pages(const char* who, const pc_pages* pages, int Hkv, int D, i
   PC_REQUIRE(aligned_16B(pages->K, pages->stride_page, elt) && aligned_16B(pages->V, pages->stride_h, elt), PC_ERR_SHAPE,
              "%s: pages and their strides must be 16-byte aligned", who);
   return PC_OK;
+}
+
+inline Extent extent_of(const void* pages_kv, const pc_pages& p, int Hkv, int D, int elt) {
+  return {pages_kv, Hkv, static_cast<int64_t>(p.page_rows) * D * elt, p.stride_h * elt, p.n_pages, p.stride_page * elt};
 }
 
 // table, lens and offs of the two calls on pages

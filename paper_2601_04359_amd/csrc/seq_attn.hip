@@ -390,10 +390,11 @@ extern "C" int pc_prompt_attn(const void* Q, const void* K, const void* V, int d
              PC_ERR_SHAPE, "%s: a head stride is smaller than the rows it must hold", who);
   PC_REQUIRE(aligned_16B(Q, q_stride_h, elt) && aligned_16B(K, k_stride_h, elt) && aligned_16B(V, v_stride_h, elt) &&
                  aligned_16B(O, o_stride_h, elt), PC_ERR_SHAPE, "%s: tensors and head strides must be 16-byte aligned", who);
-  PC_REQUIRE(!overlap(O, o_stride_h * elt, Hq, q_rows * elt, Q, q_stride_h * elt, Hq, q_rows * elt) &&
-                 (Tk == 0 || (!overlap(O, o_stride_h * elt, Hq, q_rows * elt, K, k_stride_h * elt, Hkv, k_rows * elt) &&
-                              !overlap(O, o_stride_h * elt, Hq, q_rows * elt, V, v_stride_h * elt, Hkv, k_rows * elt))),
-             PC_ERR_SHAPE, "%s: O may not overlap Q, K or V", who);
+  const Extent at_q = {Q, Hq, q_rows * elt, q_stride_h * elt}, at_o = {O, Hq, q_rows * elt, o_stride_h * elt}, at_lse = {lse, 1, 4ll * Hq * Tq, 0};
+  for (const Extent& x : {at_q, Extent{Tk > 0 ? K : nullptr, Hkv, k_rows * elt, k_stride_h * elt},
+                          Extent{Tk > 0 ? V : nullptr, Hkv, k_rows * elt, v_stride_h * elt}})
+    PC_REQUIRE(!meet(at_o, x) && !meet(at_lse, x), PC_ERR_SHAPE, "%s: O and lse may not overlap Q, K or V", who);
+  PC_REQUIRE(!meet(at_o, at_lse), PC_ERR_SHAPE, "%s: O and lse overlap", who);
   RowsArgs a = {};
   a.Q = Q, a.K = K, a.V = V, a.O = O, a.lse = lse;
   a.q_stride = q_stride_h, a.k_stride = k_stride_h, a.v_stride = v_stride_h, a.o_stride = o_stride_h;
@@ -463,8 +464,13 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
   PC_REQUIRE(Hq == 1 || (q_stride_h >= per_head && o_stride_h >= per_head), PC_ERR_SHAPE, "%s: a head stride is smaller than T*D", who);
   PC_REQUIRE(aligned_16B(Q, q_stride_h, elt) && aligned_16B(O, o_stride_h, elt), PC_ERR_SHAPE,
              "%s: tensors and head strides must be 16-byte aligned", who);
-  PC_REQUIRE(!overlap(O, o_stride_h * elt, Hq, per_head * elt, Q, q_stride_h * elt, Hq, per_head * elt), PC_ERR_SHAPE,
-             "%s: O may not overlap Q: queries are read again behind the first outputs", who);
+  const Extent at_q = {Q, Hq, per_head * elt, q_stride_h * elt}, at_o = {O, Hq, per_head * elt, o_stride_h * elt}, at_lse = {lse, 1, 4ll * Hq * T, 0};
+  PC_REQUIRE(!meet(at_o, at_q) && !meet(at_lse, at_q), PC_ERR_SHAPE,
+             "%s: O and lse may not overlap Q: queries are read again behind the first outputs", who);
+  const Extent at_k = extent_of(pages->K, *pages, Hkv, D, elt), at_v = extent_of(pages->V, *pages, Hkv, D, elt);
+  for (const Extent& x : {at_k, at_v})
+    PC_REQUIRE(!meet(at_o, x) && !meet(at_lse, x), PC_ERR_SHAPE, "%s: O and lse may not lie in the pages", who);
+  PC_REQUIRE(!meet(at_o, at_lse), PC_ERR_SHAPE, "%s: O and lse overlap", who);
   n_shared = std::min(n_shared, max_len);   // nobody sees more
   // the plan of a call's only launch serves both its workspace and the launch
   const bool one = n_seq <= (offs != nullptr ? kSeqs : kPageSeqs);
@@ -472,6 +478,9 @@ extern "C" int pc_page_attn(const void* Q, const pc_pages* pages, int dtype, int
   const size_t need = one ? first.bytes(Hkv, D) : pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, offs, n_seq, max_len, n_shared);
   PC_REQUIRE(need == 0 || (ws != nullptr && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 16 == 0), PC_ERR_WORKSPACE,
              "%s: needs %zu bytes of 16-byte aligned workspace, got %zu", who, need, ws_bytes);
+  const Extent at_ws = {need > 0 ? ws : nullptr, 1, static_cast<int64_t>(need), 0};
+  for (const Extent& x : {at_q, at_o, at_lse, at_k, at_v})
+    PC_REQUIRE(!meet(at_ws, x), PC_ERR_WORKSPACE, "%s: the workspace overlaps Q, O, lse or the pages", who);
   const int rep = Hq / Hkv;
   RowsArgs a = {};
   a.Q = Q, a.K = pages->K, a.V = pages->V, a.O = O, a.lse = lse;

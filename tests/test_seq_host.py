@@ -288,3 +288,62 @@ def test_workspaces_hold_the_shares_that_are_joined(L, dtype, Hq, Hkv, T, n_seq,
     for D in (64, 128):
         size = L.pc_page_attn_workspace_bytes(dtype, Hq, Hkv, T, D, None, n_seq, max_len, shared)
         assert size >= 2 * Hq * T * (D + 2) * 4 if joined else size == 0      # two shares of every row at least
+
+
+# ------------------------------------------------------------------------------ tensors that overlap
+R = 512 * 2             # bytes of a head of the rows in store() and attn()
+P = 64 * 128 * 2        # of a page of one head
+
+
+@pytest.mark.parametrize("kw", [
+    dict(Ko=A + 16), dict(Ko=A + R), dict(Ko=A, kos=1024), dict(Ko=A - R), dict(Ko=2 * A), dict(Ko=2 * A + R), dict(Ko=3 * A),
+    dict(Ko=3 * A + 7 * R), dict(Ko=4 * A + 16), dict(Qo=3 * A + R), dict(Qo=3 * A, qos=520), dict(Qo=3 * A - 8 * R + 16), dict(Qo=A),
+    dict(Qo=2 * A + R), dict(Qo=5 * A), dict(Qo=5 * A + 19 * P), dict(Qo=6 * A + 7 * P), dict(Ko=6 * A + 20 * P - 16), dict(Ko=5 * A - 2 * R + 16)])
+def test_store_refuses_outputs_that_overlap(L, kw):
+    assert store(L, **kw) == SHAPE, L.pc_last_error_detail()
+
+
+def passes(status):
+    """Without a GPU a call that passes its checks ends as an error of HIP."""
+    return status not in (NULL, SHAPE, DTYPE, UNSUPPORTED, WORKSPACE)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses: only where nothing can be launched")
+def test_what_does_not_overlap_is_not_refused(L):
+    """In place; heads, pages and outputs in the gaps of each other."""
+    for kw in (dict(), dict(Ko=A), dict(Qo=3 * A), dict(Ko=A, Qo=3 * A), dict(Ko=A + 2 * R), dict(Ko=A - 2 * R), dict(Qo=3 * A + 8 * R),
+               dict(ks=1024, Ko=A + R, kos=1024), dict(qs=2048, qos=2048, Qo=3 * A + R, Ko=3 * A + 2 * R, kos=2048),
+               dict(Ko=5 * A - 2 * R), dict(Ko=5 * A + 20 * P), dict(K=5 * A, V=6 * A + P)):
+        assert passes(store(L, **kw)), (kw, L.pc_last_error_detail())
+    wide = pages(stride_page=4 * 64 * 128, stride_h=2 * 64 * 128, V=5 * A + P)       # K and V of a head beside each other
+    assert passes(store(L, wide))
+    gaps = pages(stride_page=3 * 64 * 128)                                           # room for a head behind each page
+    assert passes(store(L, gaps, Ko=5 * A + 2 * P, kos=3 * 64 * 128)) and store(L, gaps, Ko=5 * A + 2 * P, kos=64 * 128) == SHAPE
+    for kw in (dict(), dict(lse=4 * A), dict(O=A + 8 * R), dict(O=A + R, qs=1024, os=1024), dict(O=5 * A - 8 * R), dict(lse=2 * A + 8 * R)):
+        assert passes(attn(L, **kw)), (kw, L.pc_last_error_detail())
+    assert passes(attn(L, gaps, O=5 * A + 2 * P, os=3 * 64 * 128)) and attn(L, gaps, O=5 * A + 2 * P, os=64 * 128) == SHAPE
+    need = -(-pk.pc_page_attn_workspace_bytes(pk.PC_BF16, 8, 2, 4, 128, 4, 192, 100) // 16) * 16
+    kw = dict(max_len=192, shared=10 * A, n_shared=100)
+    for at in (A - need, A + 8 * R, 5 * A + 20 * P, 5 * A - need):
+        assert passes(attn(L, ws=at, **kw)), (at, L.pc_last_error_detail())
+    for kw in (dict(), dict(lse=5 * A), dict(lse=4 * A + 8 * 25600), dict(O=A + 25600, qs=25600, os=25600), dict(K=2 * A, V=2 * A)):
+        assert passes(prompt(L, **kw)), (kw, L.pc_last_error_detail())
+
+
+@pytest.mark.parametrize("kw", [
+    dict(lse=A), dict(lse=A + 8 * R - 4), dict(lse=2 * A), dict(lse=2 * A + R - 4), dict(lse=5 * A + 19 * P), dict(lse=6 * A), dict(O=5 * A),
+    dict(O=5 * A + 20 * P - 16), dict(O=6 * A + 3 * P), dict(O=5 * A - 8 * R + 16)])
+def test_attn_refuses_outputs_that_overlap(L, kw):
+    assert attn(L, **kw) == SHAPE, L.pc_last_error_detail()
+
+
+@pytest.mark.parametrize("kw", [dict(ws=A), dict(ws=2 * A), dict(ws=A - 16), dict(ws=2 * A + 8 * R - 16), dict(ws=5 * A + 3 * P), dict(ws=6 * A + 20 * P - 16),
+                                dict(lse=4 * A, ws=4 * A), dict(lse=4 * A, ws=4 * A + 112)])
+def test_attn_refuses_a_workspace_that_overlaps(L, kw):
+    assert attn(L, **kw, max_len=192, shared=10 * A, n_shared=100) == WORKSPACE, L.pc_last_error_detail()
+
+
+@pytest.mark.parametrize("kw", [dict(lse=A), dict(lse=2 * A + 16), dict(lse=3 * A + 2 * 25600 - 4), dict(lse=4 * A + 8 * 25600 - 4), dict(lse=4 * A - 3196),
+                                dict(O=2 * A, os=25600), dict(O=A + 12800, qs=25600, os=25600)])
+def test_prompt_refuses_outputs_that_overlap(L, kw):
+    assert prompt(L, **kw) == SHAPE, L.pc_last_error_detail()
