@@ -399,6 +399,10 @@ class PagedStack:
     sequences.  pos int32 [T][3] on the device.  A step in which every sequence is new runs pc_prompt_attn over its own rows,
     every other one pc_page_attn over the pages, with the pages that all of the step's sequences begin with read once for all.
 
+    Every layer of a step is attended to once.  A step is not over while some layers have its rows and others do not: begin() refuses
+    the next one, and if close() ends it, its sequences can only be closed.  (A step that no layer is attended to stands for one
+    that a graph replays; layers that have been recorded are taken to have theirs.)
+
     The pages of a step are decided in begin(), on the host; attend() only launches.  With the same sequences and one row each, a
     step's launches are the same while n_shared and max_len are, so that attend() can be recorded into a HIP graph: begin()
     writes the lengths and tables into the same device buffers before every replay (max_len: a bound for as long as the graph
@@ -428,7 +432,11 @@ class PagedStack:
         self._pages: dict[int, list[int]] = {}
         self._rows: dict[int, int] = {}
         self._next = 0
-        self._step = None                                  # (sequences, offsets or None, fresh)
+        self._step = None                                  # (sequences, offsets, one number of rows each, fresh)
+        self._growing: list[int] = []                      # the step's sequences with new rows
+        self._attended: set[int] = set()                   # layers that have them
+        self._recorded: set[int] = set()                   # layers that a graph may attend to
+        self._torn: set[int] = set()                       # sequences with rows that not every layer has
         self.n_shared = self.max_len = 0
 
     # ---- sequences (host only) ----------------------------------------------------------------
@@ -449,32 +457,51 @@ class PagedStack:
             raise ValueError(f"sequence {seq} is not open")
         return seq
 
+    def _whole(self, seq: int) -> int:
+        if self._known(seq) in self._torn:
+            raise ValueError(f"sequence {seq} has rows that not every layer has: it can only be closed")
+        return seq
+
+    def _missing(self) -> list[int]:
+        """Layers that have not got the step's rows, if others have."""
+        if not self._attended or not self._growing:
+            return []
+        return [layer for layer in range(self.L) if layer not in self._attended and layer not in self._recorded]
+
     def fork(self, seq: int, n: int = 1) -> list[int]:
         """n further sequences that begin with seq's rows."""
-        self._known(seq)
+        self._whole(seq)
         out = []
         for _ in range(n):
             new = self.open()
             self._pages[new], self._rows[new] = list(self._pages[seq]), self._rows[seq]
             for p in self._pages[new]:
                 self._users[p] += 1
+            if seq in self._growing:
+                self._growing.append(new)
             out.append(new)
         return out
 
     def close(self, seq: int) -> None:
+        """The step under way is over, too."""
         for p in self._pages.pop(self._known(seq)):
             self._users[p] -= 1
             if self._users[p] == 0:
                 self._free.append(p)
         del self._rows[seq]
-        self._step = None
+        if self._missing():
+            self._torn.update(self._growing)
+        self._torn &= self._rows.keys()
+        self._step, self._growing = None, []
 
     # ---- one step -----------------------------------------------------------------------------
     def begin(self, seqs, rows=1, max_len: int | None = None) -> None:
         """The step's sequences and how many new rows each of them gets.  max_len: a bound on the rows of any of them, for
         attend() to lay its work out for (None: the longest)."""
         import torch
-        seqs = [self._known(q) for q in seqs]
+        if self._missing():
+            raise ValueError(f"layers {self._missing()} have not been attended to in the step under way")
+        seqs = [self._whole(q) for q in seqs]
         counts = [int(rows)] * len(seqs) if isinstance(rows, int) else [int(r) for r in rows]
         if not seqs or len(set(seqs)) < len(seqs) or len(seqs) > self.table.shape[0] or len(counts) != len(seqs) or min(counts) < 0:
             raise ValueError(f"a step of {len(seqs)} sequences (each once, {self.table.shape[0]} at most), new rows {rows}")
@@ -538,6 +565,8 @@ class PagedStack:
             offs.append(offs[-1] + n)
         even = len(set(counts)) == 1
         self._step = (len(seqs), offs, even, fresh)
+        self._growing = [q for q, n in zip(seqs, counts) if n]
+        self._attended.clear()
 
     def attend(self, layer: int, Q, K, V, pos, O=None, lse=None):
         """The step's rows of one layer: into the pages, and their attention -> O."""
@@ -549,10 +578,14 @@ class PagedStack:
         n, offs, even, fresh = self._step
         if Q.shape[1] != offs[-1]:
             raise ValueError(f"{Q.shape[1]} rows in a step of {offs[-1]}")
+        recording = torch.cuda.is_current_stream_capturing()
+        if layer in self._attended and self._growing and not recording:
+            raise ValueError(f"layer {layer} has the rows of this step; begin() names the next one")
         table, lens, pages = self.table[:n], self.lens[:n], (self.K[layer], self.V[layer])
         o = None if even else offs
         pk.pc_page_store(K, V, pages, table, lens, offs=o, pos=pos, sections=self.sections, base=self.base,
                          K_out=K if fresh else None, Q=Q, Q_out=Q, out_scale=self.q_out_scale)
+        (self._recorded if recording else self._attended).add(layer)
         if O is None:
             O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         if fresh:

@@ -347,3 +347,100 @@ def test_attn_refuses_a_workspace_that_overlaps(L, kw):
                                 dict(O=2 * A, os=25600), dict(O=A + 12800, qs=25600, os=25600)])
 def test_prompt_refuses_outputs_that_overlap(L, kw):
     assert prompt(L, **kw) == SHAPE, L.pc_last_error_detail()
+
+
+# ------------------------------------------------------------------------------ every layer of a step, once
+@pytest.fixture
+def launches(monkeypatch):
+    """The stack's calls, noted down instead of made; `recording`: whether they go into a graph."""
+    from paper_2601_04359_amd import rollout
+    done = type("Done", (), dict(calls=[], recording=False))()
+    monkeypatch.setattr(rollout.pk, "pc_page_store", lambda *a, **kw: done.calls.append("store"))
+    monkeypatch.setattr(rollout.pk, "pc_prompt_attn", lambda *a, **kw: done.calls.append("prompt"))
+    monkeypatch.setattr(rollout.pk, "pc_page_attn", lambda *a, **kw: done.calls.append("pages"))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: done.recording)
+    return done
+
+
+def step(s, seqs, rows, layers):
+    s.begin(seqs, rows)
+    attend(s, sum([rows] * len(seqs) if isinstance(rows, int) else rows), layers)
+
+
+def attend(s, T, layers):
+    for layer in layers:
+        s.attend(layer, torch.zeros((4, T, 64)), torch.zeros((2, T, 64)), torch.zeros((2, T, 64)), None)
+
+
+def test_a_layer_that_misses_a_step_is_an_error(launches):
+    s = stack(n_layers=3)
+    a, b = s.open(), s.open()
+    step(s, [a, b], [3, 5], (0, 2))
+    with pytest.raises(ValueError, match="1"):
+        s.begin([a, b], 1)
+    assert [s.rows(q) for q in (a, b)] == [3, 5]
+    attend(s, 8, (1,))
+    step(s, [a], 1, (2, 0, 1))
+    assert launches.calls == ["store", "prompt"] * 3 + ["store", "pages"] * 3
+
+
+def test_a_layer_that_is_attended_to_twice_is_an_error(launches):
+    s = stack()
+    a = s.open()
+    step(s, [a], 3, (0,))
+    with pytest.raises(ValueError):
+        attend(s, 3, (0,))
+    assert launches.calls == ["store", "prompt"]
+    attend(s, 3, (1,))
+    step(s, [a], 0, (0, 0, 0))          # nothing new: nothing is stored
+    step(s, [a], 1, (0, 1))
+
+
+def test_a_store_that_fails_may_be_made_again(launches, monkeypatch):
+    from paper_2601_04359_amd import rollout
+    s = stack()
+    a = s.open()
+    s.begin([a], 3)
+    with monkeypatch.context() as m:
+        m.setattr(rollout.pk, "pc_page_store", lambda *a, **kw: (_ for _ in ()).throw(pk.PackCacheError(-2, "no")))
+        with pytest.raises(pk.PackCacheError):
+            attend(s, 3, (0,))
+    attend(s, 3, (0, 1))
+    s.begin([a], 1)
+
+
+def test_sequences_of_a_step_that_close_ends_can_only_be_closed(launches):
+    s = stack()
+    a, b, c, d = (s.open() for _ in range(4))
+    step(s, [a, b, c, d], [3, 70, 0, 4], (0, 1))
+    s.close(d)                                     # every layer has its rows: nobody loses any
+    step(s, [a, b, c], [1, 1, 0], (0,))
+    e, = s.fork(a)
+    s.close(b)                                     # layer 1 has not
+    for q in (a, e):
+        for f in (lambda: s.begin([q], 1), lambda: s.begin([c, q], 1), lambda: s.fork(q)):
+            with pytest.raises(ValueError, match="only be closed"):
+                f()
+        assert s.rows(q) == 4
+    step(s, [c], 2, (0, 1))                        # had no new rows
+    s.close(a), s.close(e), s.close(c)
+    assert s.free_pages() == 8
+    step(s, [s.open()], 3, (0, 1))
+
+
+def test_steps_that_a_graph_replays(launches):
+    """attend() is called once, while it is recorded, and not again."""
+    s = stack()
+    a = s.open()
+    step(s, [a], 3, (0, 1))
+    step(s, [a], 1, (0, 1))
+    launches.recording = True
+    attend(s, 1, (0, 1))                           # behind a first call of the same step
+    launches.recording = False
+    for _ in range(3):
+        s.begin([a], 1)
+    b, = s.fork(a)
+    step(s, [a, b], 1, (0,))                       # a layer by itself, the other one in the graph
+    s.begin([a], 1)
+    s.close(b)
+    s.begin([a], 1)
