@@ -63,6 +63,11 @@ struct RowSet {
   bool common;
 };
 
+// Rows of sequence s of the launch; lens may hold anything.
+__device__ __forceinline__ int len_of(const RowsArgs& a, int s) {
+  return max(0, min(a.lens[a.seqs.per > 0 ? s : a.seqs.k0[s]], a.max_len));
+}
+
 // The keys that token i of the set sees: those below this (0: none).
 __device__ __forceinline__ int limit_of(const RowsArgs& a, const RowSet& r, int i) {
   if (!r.common) return min(max(r.first + i, 0), r.n_keys);
@@ -70,8 +75,7 @@ __device__ __forceinline__ int limit_of(const RowsArgs& a, const RowSet& r, int 
   if (s < 0) return 0;
   const bool even = a.seqs.per > 0;
   const int end = even ? (s + 1) * a.seqs.per : a.seqs.q0[s] + a.seqs.nq[s];
-  const int len = min(a.lens[even ? s : a.seqs.k0[s]], a.max_len);
-  return min(max(len - (end - t) + 1, 0), r.n_keys);
+  return min(max(len_of(a, s) - (end - t) + 1, 0), r.n_keys);
 }
 
 // Whether any of keys from .. upto - 1 has a page.  Asked of rows whose weights add up to 0: they have seen nothing if none has (O = 0),
@@ -145,9 +149,6 @@ __device__ __forceinline__ int ceil_of(int x, int by, float inv) {   // ceil(x /
   if (q * by > n) --q;
   else if (n - q * by >= by) ++q;
   return q;
-}
-__device__ __forceinline__ int len_of(const RowsArgs& a, int s) {
-  return max(0, min(a.lens[a.seqs.per > 0 ? s : a.seqs.k0[s]], a.max_len));
 }
 // Keys of a sequence from where its own rows begin, whole steps.
 __device__ __forceinline__ int own_keys_of(const RowsArgs& a, int len) {
@@ -282,9 +283,9 @@ __device__ __forceinline__ bool page_rows(const RowsArgs& a, const PageUnits& un
     tiles = (r.n_tok * a.rep + R - 1) / R;
   }
   for (r.tile = u; r.tile >= tiles; r.tile -= tiles) ++share;
-  const int len = a.own_parts > 0 ? min(a.lens[number], a.max_len) : units.first[kPageSeqs + 2 + s];
+  const int len = a.own_parts > 0 ? len_of(a, s) : units.first[kPageSeqs + 2 + s];
   r.pages = a.table + number * a.table_stride;
-  r.lo = a.n_shared, r.n_keys = max(len, 0), r.first = len - r.n_tok + 1;
+  r.lo = a.n_shared, r.n_keys = len, r.first = len - r.n_tok + 1;
   r.begin = a.n_shared / kPageStep * kPageStep + share * units.keys;
   r.end = min(r.begin + units.keys, r.n_keys);
   if (len <= a.n_shared || r.end < r.begin) r.end = r.begin;

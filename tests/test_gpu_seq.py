@@ -930,3 +930,25 @@ def test_store_of_more_rows_than_a_launch_has_threads_for():
             got = pool[table[0].long(), 0].reshape(-1, D)
             assert torch.equal(got[:n], x[0, T - n:]) and (got[n:] == 7.0).all() and (pool[0] == 7.0).all()
         assert torch.equal(K_out, K)
+
+
+# ------------------------------------------------------------------------------ lengths that are no lengths
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("n,shared,max_len", [(3, 64, 64), (3, 0, 90), (40, 64, 64), (150, 500, 500), (3, 64, 90), (200, 64, 700)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_page_attn_any_number_as_a_length(dtype, D, n, shared, max_len, ragged):
+    """Negative ones down to the lowest number are sequences without rows, the highest ones end at max_len."""
+    lens = [max_len, 0, 0, max_len, 0]
+    pg = Paged(dtype, 2, D, lens, shared=shared)
+    pg.lens = torch.tensor([2 ** 31 - 1, -2 ** 31, -2 ** 31 + 1, max_len, -1], dtype=torch.int32, device=DEV)
+    T, Hq = 5 * n, 8
+    Q = normal(generator(1), Hq, T, D).to(TYPES[dtype])
+    L = torch.full((Hq, T), 7.0, device=DEV)
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max_len, 0.1, offs=offsets([n] * 5) if ragged else None, shared=pg.shared, n_shared=shared,
+                        lse=L)
+    for s, m in enumerate(lens):
+        mine = slice(s * n, (s + 1) * n)
+        if m == 0:
+            assert (O[:, mine] == 0).all() and (L[:, mine] == -float("inf")).all()
+        for h in range(Hq if m else 0):
+            check_rows(dtype, O[h, mine], L[h, mine], Q[h, mine], pg.seqs[s][0][h // 4], pg.seqs[s][1][h // 4], 0.1, m - n + 1)
