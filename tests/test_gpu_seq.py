@@ -952,3 +952,88 @@ def test_page_attn_any_number_as_a_length(dtype, D, n, shared, max_len, ragged):
             assert (O[:, mine] == 0).all() and (L[:, mine] == -float("inf")).all()
         for h in range(Hq if m else 0):
             check_rows(dtype, O[h, mine], L[h, mine], Q[h, mine], pg.seqs[s][0][h // 4], pg.seqs[s][1][h // 4], 0.1, m - n + 1)
+
+
+# ------------------------------------------------------------------------------ more of the same, where it could go wrong
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("level", [1e8, 1e30])
+@pytest.mark.parametrize("scale", [128 ** -0.5, pk.PC_SCALE_FOLDED])
+@pytest.mark.parametrize("lens,n,shared,hidden", [
+    ([400, 351, 600], 1, 300, [(30, 150), (310, 340)]),           # some of both
+    ([400, 351, 600], 1, 300, [(0, 300)]),                        # all common rows
+    ([400, 351, 600], 40, 300, [(0, 290)]), ([400, 361, 600], 40, 300, [(300, 1000)]),      # all own rows
+    ([2900, 2700, 2650], 1, 2600, [(0, 2500)]), ([2900, 2700, 2650], 1, 2600, [(2600, 3000)]),
+    ([900, 860], 200, 600, [(64, 600)]), ([900, 860], 200, 600, [(0, 64), (600, 1000)]), ([3000, 2900, 70], 1, 0, [(0, 64), (200, 2800)])])
+def test_page_attn_hidden_keys_in_any_share(dtype, D, level, scale, lens, n, shared, hidden):
+    """Keys that a coordinate of their own hides, in common and in own rows: shares of very different references are joined."""
+    at = [j for a, b in hidden for j in range(a, b)]
+
+    def hide(K, V):
+        K[..., 0] = 0.0
+        K[:, [j for j in at if j < K.shape[1]], 0] = -level
+    pg = Paged(dtype, 2, D, lens, shared=shared)
+    rewrite(pg, hide)
+    T = n * len(lens)
+    Q = normal(generator(2), 4, T, D).to(TYPES[dtype])
+    Q[..., 0] = 1.0
+    L = torch.empty((4, T), device=DEV)
+    O = pk.pc_page_attn(Q, pg.pages, pg.table, pg.lens, max(lens), scale, shared=pg.shared, n_shared=shared, lse=L)
+    assert O.isfinite().all() and L.isfinite().all()
+    for s, m in enumerate(lens):
+        keep = causal(n, m, at)
+        rows = [i for i in sorted({0, 1, n // 3, n // 2, n - 1}) if i < n and keep[i].any()]
+        mine = [s * n + i for i in rows]
+        check_kept(dtype, O[:, mine], L[:, mine], Q[:, mine], pg.seqs[s], keep[rows], scale)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,nq,nk", [
+    ("bf16", 64, 8, 2, [2300, 40], None), ("bf16", 64, 2, 1, [5000], None), ("bf16", 64, 6, 6, [700, 1, 900], [3000, 64, 900]), ("f32", 64, 2, 1, [1500], None),
+    ("bf16", 128, 4, 1, [130, 700], [4000, 700]), ("bf16", 64, 64, 1, [90, 33], None), ("bf16", 128, 64, 1, [90, 33], [400, 30])])
+@pytest.mark.parametrize("scale", [0.1, pk.PC_SCALE_FOLDED])
+def test_prompt_longer_ones_of_every_head_size(dtype, D, Hq, Hkv, nq, nk, scale):
+    run_prompt(dtype, Hq, Hkv, D, nq, nk, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("Hq,Hkv,lens,n,shared", [(8, 2, [130, 64, 0, 1], 1, 0), (8, 2, [5000, 300], 1, 0), (16, 4, [700 + 9 * i for i in range(9)], 40, 600),
+                                                  (24, 8, [1500, 400], 300, 0), (16, 4, [4000 + i for i in range(30)], 1, 3900), (64, 1, [90, 500], 3, 60)])
+def test_page_attn_folded_scale(dtype, D, Hq, Hkv, lens, n, shared):
+    run_pages(dtype, Hq, Hkv, D, lens, n, shared=shared, scale=pk.PC_SCALE_FOLDED)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 70])
+def test_page_attn_one_page_at_several_places(dtype, n):
+    """Of one sequence, of two, and of the common rows."""
+    pg = Paged(dtype, 2, 128, [300, 290], shared=128)
+    pg.table[0, 3], pg.table[1, 2], pg.table[1, 3], pg.shared[1] = pg.table[0, 2].item(), pg.table[0, 2].item(), pg.shared[0].item(), pg.shared[0].item()
+    for s in range(2):
+        for x in (0, 1):
+            own, common = pg.seqs[0][x][:, 128:192].clone(), pg.seqs[s][x][:, :64].clone()
+            pg.seqs[s][x][:, 64:128] = common
+            pg.seqs[s][x][:, 128:192] = own
+            pg.seqs[s][x][:, 192:256] = own if s == 0 else common
+    run_pages(dtype, 8, 2, 128, [300, 290], n, shared=128, paged=pg)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Recorded steps of different sizes on one workspace, replayed one behind the other on one stream."""
+    pgs = [Paged("bf16", 2, 128, lens, shared=200, seed=i) for i, lens in enumerate(([700, 300], [260, 1900, 200]))]
+    Qs = [normal(generator(i), 8, n, 128).to(torch.bfloat16) for i, n in enumerate((4, 3))]
+    outs = [torch.zeros_like(q) for q in Qs]
+    sizes = [pk.pc_page_attn_workspace_bytes(pk.PC_BF16, 8, 2, q.shape[1], 128, len(p.lens_host), max(p.lens_host), 200) for q, p in zip(Qs, pgs)]
+    ws = torch.full((max(sizes),), 0xFF, dtype=torch.uint8, device=DEV)
+    call = lambda i, **kw: pk.pc_page_attn(Qs[i], pgs[i].pages, pgs[i].table, pgs[i].lens, max(pgs[i].lens_host), 0.1, shared=pgs[i].shared, n_shared=200, **kw)
+    want, graphs = [call(i) for i in range(2)], []
+    for i in range(2):
+        call(i, O=outs[i], ws=ws)
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(i, O=outs[i], ws=ws)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1, 0)):
+        for x in outs:
+            x.zero_()
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
