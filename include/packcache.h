@@ -526,7 +526,8 @@ int pc_page_store(const void* K, const void* V, int dtype, int Hkv, int T, int D
  *            it, so a bound near the longest sequence is worth having
  *   shared, n_shared   dev int32 [ceil(n_shared / page_rows)] or NULL, 0: the first n_shared rows of every sequence
  *            are the same (a common prompt, one video's cache).  They are read through `shared`, once for all
- *            sequences, the rows behind them through `table`.  A sequence of fewer rows sees that many of them.
+ *            sequences of a launch (256 of them with offs NULL, else 64), the rows behind them through `table`.  A sequence of
+ *            fewer rows sees that many of them.
  *   lse      dev or NULL, fp32 [Hq][T].  O, lse and ws have no byte in common with each other, Q or the pages
  *   ws       dev, pc_page_attn_workspace_bytes(...) bytes, 16-byte aligned (NULL where that is 0).  Calls that may
  *            overlap on the GPU must not share one.

@@ -5,6 +5,10 @@
 // 8 i + 4 g .. + 3, i = 0 .. 3), so that a row's limit, reference and sum are per-lane numbers and the probabilities are
 // the B operand of O^T += V^T P^T as they stand.  What a row does not see gets the score -inf, in the tiles where a row
 // of the work-group does not see everything; a tile of keys lies in one page.
+//
+// Probabilities are rounded to bf16 for the second product, which the bf16 instructions take, and the normaliser sums them as they
+// were: half a step per weight, in directions of their own, against the half step that O is rounded by anyway.  Against 64 bits the
+// timed cases are off by 0.0008 to 0.0024 of O's norm, and with 32-bit probabilities by 0.0007 to 0.0017.
 #pragma once
 
 #include <limits.h>
@@ -376,8 +380,8 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, const RowSet& r, lds
 //     phase 2 of tile j:  S_A(j+1), O += V_A(j) P_A(j)    |  P_B(j)
 // (pipeline_phase).  One barrier per tile, after phase 1: behind it K(j+2) and V(j+1) are fetched into the slots just
 // released.  Bound: the matrix pipe, which the other work-group of the unit keeps busy while one waits at its barrier.  Measured:
-// a prompt of 16,384 rows, 24/8 heads, 1,503 us (1,097 TFLOP/s, 0.89 of a large product's rate).  Eight waves with 128 or 256
-// rows were slower.
+// a prompt of 16,384 rows, 24/8 heads, 1,503 to 1,591 us on several cards (1,036 to 1,097 TFLOP/s, 0.84 to 0.89 of a large product's rate).
+// Eight waves with 128 or 256 rows were slower on causal prompts.
 // ------------------------------------------------------------------------------------------
 constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves, kManyKeys = 64;
 constexpr int kManyTileBytes = kManyKeys * kRowBytes;
@@ -632,7 +636,7 @@ __device__ __forceinline__ void rows_many(const RowsArgs& a, const RowSet& r, ld
 //     phase j:  S(j+1), O += V(j-1) P(j-1)  |  P(j)
 // One barrier behind it; then K(j+3) and V(j+1) are fetched into the slots just released.  The longest work-group has half of
 // the products that it has with 128 rows, which is what a call of few work-groups waits for; where there are many, K and V
-// come through L2 twice as often per product.  Measured: a prompt of 3,000 rows, 16/4 heads, 53 us (63 with 128 rows).
+// come through L2 twice as often per product.  Measured: a prompt of 3,000 rows, 16/4 heads, 53 to 57 us (63 with 128 rows).
 // ------------------------------------------------------------------------------------------
 constexpr int kMidWaves = 4, kMidRows = 64;
 constexpr size_t kMidSmem = kMidWaves * (kWaveOBytes<kD> + 32 * 8);

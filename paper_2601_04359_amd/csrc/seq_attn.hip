@@ -132,8 +132,8 @@ struct Cost {
     return std::max(alone + (groups > 280 ? paired : per_step) * longest, start + (per_group * groups + step * steps) / 256);
   }
 };
-// Prompts: fitted to 40 to 16,384 rows in 8/2, 16/4 and 24/8 heads in all three forms, within 8 % from 1,000 rows on.  Both
-// sides, us:
+// Prompts: fitted to 40 to 16,384 rows in 8/2, 16/4 and 24/8 heads in all three forms, within 8 % from 1,000 rows on, all with a
+// scale of its own (the folded one is 4 to 5 % faster on long prompts and is chosen for as these are).  Both sides, us:
 //   few | mid    8/2 x 2,048: 23 | 32    16/4 x 1,024: 17 | 20    16/4 x 2,048: 42 | 34    24/8 x 1,024: 24 | 21
 //   mid | many   8/2 x 8,192: 161 | 176  16/4 x 3,000: 53 | 63    16/4 x 4,288: 97 | 99    24/8 x 4,288: 140 | 118
 constexpr Cost kPromptCost[3] = {{5.0, 1.75, 1.75, 2.5, 3.6, 1.25}, {7.5, 0.75, 0.84, 6.0, 2.9, 0.549}, {7.0, 1.07, 1.3, 5.0, 3.0, 0.953}};
@@ -221,7 +221,7 @@ struct PagesCost {
 // each form, up to 25 lengths of a share): first the times, then the choice, which is 3 % off the best of a shape's launches
 // at the mean, 15 % at most.  Both sides at the best share of each, 16/4 heads, 41,800 common rows, us:
 //   few | mid | many   32 tokens: 35 | 36 | 37   64: 54 | 49 | 48   256: 168 | 139 | 131
-// fp32 and D = 64: to 18 shapes each.
+// fp32 and D = 64: to 18 shapes each.  bf16 with D = 64 has one form, so that only its shares are chosen.
 constexpr PagesCost kPagesCost[3] = {{3.2, 1.67, 1.67, 2.45, 256}, {2.1, 0.913, 1.064, 5.2, 512}, {0.0, 1.22, 1.45, 6.9, 512}};
 constexpr PagesCost kPagesFew64 = {2.5, 0.89, 1.54, 2.1, 512};
 // 16 | 32 rows, 16/4 heads, D = 128: 64 tokens with 1,000 rows each 45 | 65; 8 x 32 tokens behind 4,000 rows 117 | 108.
