@@ -399,7 +399,7 @@ class PagedStack:
     sequences.  pos int32 [T][3] on the device.  A step in which every sequence is new runs pc_prompt_attn over its own rows,
     every other one pc_page_attn over the pages, with the pages that all of the step's sequences begin with read once for all.
 
-    Every layer of a step is attended to once.  A step is not over while some layers have its rows and others do not: begin() refuses
+    Every layer of a step is attended to once; a further pass over the same rows says so (again=True) and gives them anew.  A step is not over while some layers have its rows and others do not: begin() refuses
     the next one, and if close() ends it, its sequences can only be closed.  (A step that no layer is attended to stands for one
     that a graph replays; layers that have been recorded are taken to have theirs.)
 
@@ -568,8 +568,9 @@ class PagedStack:
         self._growing = [q for q, n in zip(seqs, counts) if n]
         self._attended.clear()
 
-    def attend(self, layer: int, Q, K, V, pos, O=None, lse=None):
-        """The step's rows of one layer: into the pages, and their attention -> O."""
+    def attend(self, layer: int, Q, K, V, pos, O=None, lse=None, again: bool = False):
+        """The step's rows of one layer: into the pages, and their attention -> O.  again: they take the place of those that the layer
+        has of this step (not rotated yet either)."""
         import torch
         if self._step is None:
             raise ValueError("begin() names the step's sequences first")
@@ -578,14 +579,13 @@ class PagedStack:
         n, offs, even, fresh = self._step
         if Q.shape[1] != offs[-1]:
             raise ValueError(f"{Q.shape[1]} rows in a step of {offs[-1]}")
-        recording = torch.cuda.is_current_stream_capturing()
-        if layer in self._attended and self._growing and not recording:
+        if layer in self._attended and self._growing and not again and not torch.cuda.is_current_stream_capturing():
             raise ValueError(f"layer {layer} has the rows of this step; begin() names the next one")
         table, lens, pages = self.table[:n], self.lens[:n], (self.K[layer], self.V[layer])
         o = None if even else offs
         pk.pc_page_store(K, V, pages, table, lens, offs=o, pos=pos, sections=self.sections, base=self.base,
                          K_out=K if fresh else None, Q=Q, Q_out=Q, out_scale=self.q_out_scale)
-        (self._recorded if recording else self._attended).add(layer)
+        (self._recorded if torch.cuda.is_current_stream_capturing() else self._attended).add(layer)
         if O is None:
             O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         if fresh:

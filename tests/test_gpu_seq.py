@@ -1037,3 +1037,26 @@ def test_two_graphs_that_share_a_workspace():
             graphs[i].replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+@pytest.mark.parametrize("rows", [[5, 70], [1, 1]])
+def test_stack_passes_over_one_step(rows):
+    """Rows that are given anew replace those of the pass before: as if only the last pass had been."""
+    results = []
+    for passes in (1, 3):
+        gen = generator(7)
+        s = PagedStack(2, 8, 2, 128, 20, 128 ** -0.5)
+        a, b = s.open(), s.open()
+        draw = lambda n: [normal(gen, H, n, 128).to(torch.bfloat16) for H in (8, 2, 2)]
+        for counts in ([130, 64], rows):
+            s.begin([a, b], counts)
+            T = sum(counts)
+            pos = torch.arange(3 * T, dtype=torch.int32, device=DEV).reshape(T, 3)
+            given = [[draw(T) for _ in range(2)] for _ in range(3)]
+            for i in range(3 - passes, 3):
+                out = [s.attend(l, *given[i][l], pos, again=i > 3 - passes) for l in range(2)]
+            results.append(torch.stack(out))
+        results[-2:] = [torch.cat(results[-2:], 2)]
+        with pytest.raises(ValueError):
+            s.attend(0, *draw(T), pos)
+    assert torch.equal(*results)

@@ -444,3 +444,23 @@ def test_steps_that_a_graph_replays(launches):
     s.begin([a], 1)
     s.close(b)
     s.begin([a], 1)
+
+
+def test_a_further_pass_over_a_step_says_so(launches):
+    s = stack()
+    a = s.open()
+    step(s, [a], 3, (0, 1))
+    for _ in range(2):
+        for layer in range(2):
+            s.attend(layer, torch.zeros((4, 3, 64)), torch.zeros((2, 3, 64)), torch.zeros((2, 3, 64)), None, again=True)
+    assert launches.calls == ["store", "prompt"] * 6 and s.rows(a) == 3
+    s.begin([a], 1)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="tensors that are not on the GPU, and no GPU")
+def test_attend_without_a_gpu_is_refused():
+    s = stack()
+    s.begin([s.open()], 3)
+    bf = lambda *n: torch.zeros(n, dtype=torch.bfloat16)
+    with pytest.raises(pk.PackCacheError):
+        s.attend(0, bf(4, 3, 64), bf(2, 3, 64), bf(2, 3, 64), torch.zeros((3, 3), dtype=torch.int32))
